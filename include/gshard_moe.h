@@ -451,6 +451,111 @@ int gshard_dense_ffn_forward(int64_t n_tokens, int32_t M, int32_t H, int32_t dty
                              const void* x, const void* wi, const void* wo, void* y, void* workspace,
                              size_t workspace_bytes, void* cuda_stream);
 
+/* ---- layer norm -----------------------------------------------------------------------------
+ * The normalisation behind the residual connection of every sub-layer (section 2.1), over the last
+ * dimension of x [n_rows, M]:
+ *   mean = sum x / M, rstd = 1 / sqrt(sum (x - mean)^2 / M + eps), y = gamma (x - mean) rstd + beta
+ * x, y: dtype; gamma, beta [M], mean, rstd [n_rows]: float.  beta, mean and rstd may be NULL (no shift;
+ * statistics not kept).  y may be x itself.  M <= 16384, any M >= 1 (rows that are whole 16-byte words
+ * move fastest); n_rows may be 0.  No workspace. */
+int gshard_layer_norm_forward(int64_t n_rows, int32_t M, int32_t dtype, float eps, const void* x,
+                              const float* gamma, const float* beta, void* y, float* mean, float* rstd,
+                              void* cuda_stream);
+
+/* Backward of the layer norm.  mean, rstd: as the forward returned them.
+ *   dx = rstd (g - sum g / M - z sum (g z) / M) + dskip  with z = (x - mean) rstd, g = gamma dy;
+ *   dgamma = sum over rows of dy z, dbeta = sum over rows of dy: float [M], overwritten, either may be
+ *   NULL.  dskip [n_rows, M] (dtype, may be NULL): the gradient that reaches x past the layer norm, along
+ *   a residual connection.  dx may be dy or dskip itself.  n_rows == 0 gives zero weight gradients.
+ *   workspace: gshard_layer_norm_workspace_bytes() bytes, 256-byte aligned; needed only with dgamma or
+ *   dbeta.  Its contents are scratch, so calls that share one must be ordered on one stream. */
+size_t gshard_layer_norm_workspace_bytes(int64_t n_rows, int32_t M);
+int gshard_layer_norm_backward(int64_t n_rows, int32_t M, int32_t dtype, const void* x, const float* gamma,
+                               const float* mean, const float* rstd, const void* dy, const void* dskip,
+                               void* dx, float* dgamma, float* dbeta, void* workspace,
+                               size_t workspace_bytes, void* cuda_stream);
+
+/* ---- linear -----------------------------------------------------------------------------------
+ * The projections of a Transformer layer, with what surrounds the matrix product in its epilogue:
+ *   pre = x . w + bias, y = activation(pre) + residual
+ * x [n_rows, K], w [K, cols]: dtype; bias [cols]: float; residual, y, pre [n_rows, cols]: out_dtype, which
+ * is dtype or GSHARD_F32 (a router's logits, for instance).  bias, residual and pre may be NULL; pre receives
+ * the pre-activations that the backward takes.  residual may be y itself; no other output may
+ * overlap an operand.  K % 8 == 0 and cols % 8 == 0; n_rows may be 0.
+ * bf16: tensor cores, fp32 accumulation, one rounding per output; fp32: fp32 arithmetic.
+ * workspace: gshard_linear_workspace_bytes() bytes, 256-byte aligned; its first word is the status word
+ * (gshard_moe_last_device_status).  Calls that share a workspace must be ordered on one stream. */
+typedef enum {
+  GSHARD_ACT_NONE = 0,
+  GSHARD_ACT_RELU = 1,
+  GSHARD_ACT_GELU = 2,        /* v * Phi(v), by erf */
+  GSHARD_ACT_GELU_TANH = 3,   /* 0.5 v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) */
+  GSHARD_ACT_SILU = 4         /* v / (1 + exp(-v)) */
+} gshard_activation;
+
+size_t gshard_linear_workspace_bytes(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype,
+                                     int32_t out_dtype, int for_backward);
+int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype,
+                          int32_t activation, const void* x, const void* w, const float* bias,
+                          const void* residual, void* y, void* pre, void* workspace,
+                          size_t workspace_bytes, void* cuda_stream);
+
+/* Backward of the linear operator: dpre = dy activation'(pre), dx = dpre . w^T, dw = x^T . dpre (dtype),
+ * dbias = sum over rows of dpre (float); the residual's gradient is dy itself.  dy and pre: out_dtype; pre
+ * is not read with GSHARD_ACT_NONE.  dx, dw, dbias: overwritten, each may be NULL; dx and dw may not
+ * overlap an operand.  With dtype bf16 dpre is rounded to bf16 once, as an operand of both products.
+ * n_rows == 0 gives zero weight gradients. */
+int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype,
+                           int32_t activation, const void* x, const void* w, const void* pre,
+                           const void* dy, void* dx, void* dw, float* dbias, void* workspace,
+                           size_t workspace_bytes, void* cuda_stream);
+
+/* ---- routing beyond top-2 softmax ---------------------------------------------------------------
+ * Chooses k experts per token from given logits [G, S, E] (dtype):
+ *   scores   s = softmax(logits) or sigmoid(logits) over the E experts.  A logit of -inf or NaN bars the
+ *            expert for the token (score 0); +inf counts as the largest float.
+ *   choice   the k largest s_e + bias_e, largest first, equal values to the lower index (compared as
+ *            real numbers: in 64 bits where fp32 values are close).  bias (float [E], may be NULL) moves the
+ *            choice only, not the weights; an expert whose bias is -inf or NaN is not chosen.
+ *            With groups > 1 the experts form `groups` runs of E / groups, and only those of the
+ *            `groups_kept` best runs compete; a run's value is its best s + bias (group_top == 1) or the
+ *            sum of its two best (group_top == 2).
+ *   weights  scale * s_e of the chosen, or with renormalise != 0 scale * s_e / (sum of the chosen s).
+ * Where fewer than k experts are left the remaining expert_idx are -1 with weight 0 (a padding token: a row
+ * of -inf).
+ *   expert_idx [G,S,k] int32, weight [G,S,k] float; m [G,E] float: mean of s_e over the group's tokens,
+ *   may be NULL; load [G,E] int32: tokens of the group that chose e, may be NULL.
+ * With k = 2 and renormalise = 0 the outputs are what gshard_moe_capacity takes (expert_idx, gate12, m), so
+ * any of these scores can stand in for gshard_moe_gate; that stage expects two experts for every token,
+ * so rows that came out with -1 must not be handed on.
+ * Limits: E <= 16384, k <= 32, groups <= 32 and a divisor of E, k <= groups_kept * E / groups, G <= 65535;
+ * G or S may be 0.
+ * workspace: gshard_moe_route_workspace_bytes() bytes, 256-byte aligned; needed only with m. */
+typedef enum { GSHARD_SCORE_SOFTMAX = 0, GSHARD_SCORE_SIGMOID = 1 } gshard_route_score;
+
+typedef struct {
+  int32_t G, S, E, k;
+  int32_t dtype;         /* gshard_dtype of the logits */
+  int32_t score;         /* gshard_route_score */
+  int32_t groups, groups_kept, group_top;   /* 1, 1, 1: no groups */
+  int32_t renormalise;
+  float scale;
+} gshard_route_config;
+
+size_t gshard_moe_route_workspace_bytes(const gshard_route_config* config);
+int gshard_moe_route(const gshard_route_config* config, const void* logits, const float* bias,
+                     int32_t* expert_idx, float* weight, float* m, int32_t* load, void* workspace,
+                     size_t workspace_bytes, void* cuda_stream);
+
+/* Gradient of <dweight, weight> + <dm, m> with respect to the logits, the choice held constant (the
+ * bias has none).  expert_idx: as the forward returned it; entries outside [0, E) or at barred experts
+ * count as absent, an expert named twice receives both shares.  dweight [G,S,k] float; dm [G,E] float,
+ * may be NULL; dlogits [G,S,E] dtype, overwritten, not the logits themselves.  Renormalised weights without
+ * dm have a gradient at the chosen experts only.  No workspace. */
+int gshard_moe_route_backward(const gshard_route_config* config, const void* logits,
+                              const int32_t* expert_idx, const float* dweight, const float* dm,
+                              void* dlogits, void* cuda_stream);
+
 /* The check that GSHARD_FLAG_DEBUG_CHECKS runs inside the forward, callable on its own: verifies
  * the invariants Algorithm 1 implies for routing->expert_idx, slot, weight, flags and slot_token
  * (all five required) and records GSHARD_ERR_INTERNAL in the status word of `workspace` (its first

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_float, c_int, c_int32, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, Structure, c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
 import torch
 
@@ -42,6 +42,13 @@ GSHARD_FLAG_TF32_EXPERTS = 8192
 GSHARD_FLAG_COMPACT_SLOTS = 16384
 GSHARD_FLAG_DEBUG_CHECKS = 32768
 GSHARD_FLAG_BULK_DISPATCH = 65536
+GSHARD_ACT_NONE = 0
+GSHARD_ACT_RELU = 1
+GSHARD_ACT_GELU = 2
+GSHARD_ACT_GELU_TANH = 3
+GSHARD_ACT_SILU = 4
+GSHARD_SCORE_SOFTMAX = 0
+GSHARD_SCORE_SIGMOID = 1
 
 
 class gshard_moe_shape(Structure):
@@ -78,6 +85,11 @@ class gshard_ep_p2p(Structure):
 
 class gshard_ep_nccl_state(Structure):
     _fields_ = [("opaque", c_void_p * 8)]
+
+
+class gshard_route_config(Structure):
+    _fields_ = [(n, c_int32) for n in ("G", "S", "E", "k", "dtype", "score", "groups", "groups_kept", "group_top",
+                                       "renormalise")] + [("scale", c_float)]
 
 
 EXPORTS = {
@@ -122,6 +134,15 @@ EXPORTS = {
     "gshard_dense_ffn_workspace_bytes": (c_size_t, [ctypes.c_int64, c_int32, c_int32, c_int32]),
     "gshard_dense_ffn_forward": (c_int, [ctypes.c_int64, c_int32, c_int32, c_int32, c_uint32] + [c_void_p] * 5 +
                                  [c_size_t, c_void_p]),
+    "gshard_layer_norm_forward": (c_int, [c_int64, c_int32, c_int32, c_float] + [c_void_p] * 7),
+    "gshard_layer_norm_workspace_bytes": (c_size_t, [c_int64, c_int32]),
+    "gshard_layer_norm_backward": (c_int, [c_int64, c_int32, c_int32] + [c_void_p] * 10 + [c_size_t, c_void_p]),
+    "gshard_linear_workspace_bytes": (c_size_t, [c_int64] + [c_int32] * 4 + [c_int]),
+    "gshard_linear_forward": (c_int, [c_int64] + [c_int32] * 5 + [c_void_p] * 7 + [c_size_t, c_void_p]),
+    "gshard_linear_backward": (c_int, [c_int64] + [c_int32] * 5 + [c_void_p] * 8 + [c_size_t, c_void_p]),
+    "gshard_moe_route_workspace_bytes": (c_size_t, [POINTER(gshard_route_config)]),
+    "gshard_moe_route": (c_int, [POINTER(gshard_route_config)] + [c_void_p] * 7 + [c_size_t, c_void_p]),
+    "gshard_moe_route_backward": (c_int, [POINTER(gshard_route_config)] + [c_void_p] * 6),
     "gshard_moe_debug_wait_timeout": (c_int, [c_void_p, c_uint32, c_void_p]),
     "gshard_moe_check_routing": (c_int, [POINTER(gshard_moe_shape), POINTER(gshard_moe_routing), c_void_p, c_void_p]),
     "gshard_moe_last_device_status": (c_int, [c_void_p, c_void_p]),
@@ -394,6 +415,139 @@ def gshard_dense_ffn_forward(x, wi, wo, y, workspace, stream=None, flags=0):
     H = wi.shape[1]
     _check(load().gshard_dense_ffn_forward(n, M, H, _dtype_code(x), flags, _p(x), _p(wi), _p(wo), _p(y), _p(workspace),
                                            workspace.numel(), _stream(stream)), "gshard_dense_ffn_forward")
+
+
+# ---- layer norm, linear, routing ------------------------------------------------------------------
+# These take tensors of any one GPU: dtype, shape, layout and device of every tensor are checked here, and the
+# call runs on that device's current stream (or the stream given, which must belong to it).
+
+_DTYPE_CODES = {torch.float32: GSHARD_F32, torch.bfloat16: GSHARD_BF16}
+_ACTIVATIONS = {"none": GSHARD_ACT_NONE, "relu": GSHARD_ACT_RELU, "gelu": GSHARD_ACT_GELU,
+                "gelu_tanh": GSHARD_ACT_GELU_TANH, "silu": GSHARD_ACT_SILU}
+_SCORES = {"softmax": GSHARD_SCORE_SOFTMAX, "sigmoid": GSHARD_SCORE_SIGMOID}
+
+
+def _code_of(dtype, what):
+    code = _DTYPE_CODES.get(dtype)
+    if code is None:
+        raise ValueError(f"{what}: dtype {dtype} is not float32 or bfloat16")
+    return code
+
+
+def _arg(t, name, shape, dtype, device):
+    """Pointer of a tensor argument after checking it (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous"))
+    return t.data_ptr()
+
+
+def _workspace(ws, device):
+    if ws is None:
+        return None, 0
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on {device}, got {ws.device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _call(name, device, stream, *args):
+    """Call library function `name` with `device` current, on its current stream or on the one given."""
+    fn = getattr(load(), name)
+    if device.type != "cuda":
+        raise ValueError(f"{name}: tensors must be on a CUDA device, got {device}")
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, _stream(stream)), name)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(stream)), name)
+
+
+def gshard_layer_norm_workspace_bytes(n_rows, M) -> int:
+    return int(load().gshard_layer_norm_workspace_bytes(int(n_rows), int(M)))
+
+
+def gshard_layer_norm_forward(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5, stream=None):
+    """y = gamma (x - mean) rstd + beta over the last dimension of x [n, M]; beta, mean, rstd optional."""
+    code, dev, f32 = _code_of(x.dtype, "x"), x.device, torch.float32
+    n, M = x.shape
+    args = [_arg(x, "x", (n, M), x.dtype, dev), _arg(gamma, "gamma", (M,), f32, dev), _arg(beta, "beta", (M,), f32, dev),
+            _arg(y, "y", (n, M), x.dtype, dev), _arg(mean, "mean", (n,), f32, dev), _arg(rstd, "rstd", (n,), f32, dev)]
+    _call("gshard_layer_norm_forward", dev, stream, n, M, code, float(eps), *args)
+
+
+def gshard_layer_norm_backward(x, gamma, mean, rstd, dy, dx, dgamma=None, dbeta=None, dskip=None, workspace=None,
+                               stream=None):
+    """dx (+ dskip), dgamma and dbeta of the layer norm; workspace is needed with dgamma or dbeta."""
+    code, dev, f32 = _code_of(x.dtype, "x"), x.device, torch.float32
+    n, M = x.shape
+    args = [_arg(x, "x", (n, M), x.dtype, dev), _arg(gamma, "gamma", (M,), f32, dev), _arg(mean, "mean", (n,), f32, dev),
+            _arg(rstd, "rstd", (n,), f32, dev), _arg(dy, "dy", (n, M), x.dtype, dev),
+            _arg(dskip, "dskip", (n, M), x.dtype, dev), _arg(dx, "dx", (n, M), x.dtype, dev),
+            _arg(dgamma, "dgamma", (M,), f32, dev), _arg(dbeta, "dbeta", (M,), f32, dev), *_workspace(workspace, dev)]
+    _call("gshard_layer_norm_backward", dev, stream, n, M, code, *args)
+
+
+def gshard_linear_workspace_bytes(n_rows, K, cols, dtype, out_dtype=None, for_backward=False) -> int:
+    """dtype, out_dtype: torch.float32 or torch.bfloat16 (out_dtype: that of y, dtype where not given)."""
+    code = _code_of(dtype, "dtype")
+    out = code if out_dtype is None else _code_of(out_dtype, "out_dtype")
+    return int(load().gshard_linear_workspace_bytes(int(n_rows), int(K), int(cols), code, out, int(bool(for_backward))))
+
+
+def gshard_linear_forward(x, w, y, bias=None, residual=None, pre=None, activation="none", workspace=None, stream=None):
+    """y = activation(x . w + bias) + residual for x [n, K], w [K, cols]; pre receives x . w + bias."""
+    code, out, dev = _code_of(x.dtype, "x"), _code_of(y.dtype, "y"), x.device
+    (n, K), cols = x.shape, w.shape[-1]
+    args = [_arg(x, "x", (n, K), x.dtype, dev), _arg(w, "w", (K, cols), x.dtype, dev),
+            _arg(bias, "bias", (cols,), torch.float32, dev), _arg(residual, "residual", (n, cols), y.dtype, dev),
+            _arg(y, "y", (n, cols), y.dtype, dev), _arg(pre, "pre", (n, cols), y.dtype, dev), *_workspace(workspace, dev)]
+    _call("gshard_linear_forward", dev, stream, n, K, cols, code, out, _ACTIVATIONS.get(activation, activation), *args)
+
+
+def gshard_linear_backward(x, w, dy, dx=None, dw=None, dbias=None, pre=None, activation="none", workspace=None,
+                           stream=None):
+    """dx, dw, dbias (each optional) of the linear operator; pre as the forward kept it."""
+    code, out, dev = _code_of(x.dtype, "x"), _code_of(dy.dtype, "dy"), x.device
+    (n, K), cols = x.shape, w.shape[-1]
+    args = [_arg(x, "x", (n, K), x.dtype, dev), _arg(w, "w", (K, cols), x.dtype, dev),
+            _arg(pre, "pre", (n, cols), dy.dtype, dev), _arg(dy, "dy", (n, cols), dy.dtype, dev),
+            _arg(dx, "dx", (n, K), x.dtype, dev), _arg(dw, "dw", (K, cols), x.dtype, dev),
+            _arg(dbias, "dbias", (cols,), torch.float32, dev), *_workspace(workspace, dev)]
+    _call("gshard_linear_backward", dev, stream, n, K, cols, code, out, _ACTIVATIONS.get(activation, activation), *args)
+
+
+def make_route(*, G, S, E, k, dtype="f32", score="softmax", groups=1, groups_kept=None, group_top=1, renormalise=True,
+               scale=1.0) -> gshard_route_config:
+    """Routing description; dtype is "f32" | "bf16", score "softmax" | "sigmoid"; groups_kept: all by default."""
+    return gshard_route_config(G, S, E, k, {"f32": GSHARD_F32, "bf16": GSHARD_BF16}[dtype], _SCORES[score], groups,
+                               groups if groups_kept is None else groups_kept, group_top, int(bool(renormalise)),
+                               float(scale))
+
+
+def gshard_moe_route_workspace_bytes(route) -> int:
+    return int(load().gshard_moe_route_workspace_bytes(ctypes.byref(route)))
+
+
+def gshard_moe_route(route, logits, expert_idx, weight, bias=None, m=None, load=None, workspace=None, stream=None):
+    """Chooses route.k experts per token of logits [G, S, E]; workspace is needed with m."""
+    G, S, E, k, dev, f32 = route.G, route.S, route.E, route.k, logits.device, torch.float32
+    dt = torch.bfloat16 if route.dtype == GSHARD_BF16 else f32
+    args = [_arg(logits, "logits", (G, S, E), dt, dev), _arg(bias, "bias", (E,), f32, dev),
+            _arg(expert_idx, "expert_idx", (G, S, k), torch.int32, dev), _arg(weight, "weight", (G, S, k), f32, dev),
+            _arg(m, "m", (G, E), f32, dev), _arg(load, "load", (G, E), torch.int32, dev), *_workspace(workspace, dev)]
+    _call("gshard_moe_route", dev, stream, ctypes.byref(route), *args)
+
+
+def gshard_moe_route_backward(route, logits, expert_idx, dweight, dlogits, dm=None, stream=None):
+    """dlogits of <dweight, weight> + <dm, m> with the choice held constant."""
+    G, S, E, k, dev, f32 = route.G, route.S, route.E, route.k, logits.device, torch.float32
+    dt = torch.bfloat16 if route.dtype == GSHARD_BF16 else f32
+    args = [_arg(logits, "logits", (G, S, E), dt, dev), _arg(expert_idx, "expert_idx", (G, S, k), torch.int32, dev),
+            _arg(dweight, "dweight", (G, S, k), f32, dev), _arg(dm, "dm", (G, E), f32, dev),
+            _arg(dlogits, "dlogits", (G, S, E), dt, dev)]
+    _call("gshard_moe_route_backward", dev, stream, ctypes.byref(route), *args)
 
 
 def gshard_moe_debug_wait_timeout(workspace, limit_us=200, stream=None):

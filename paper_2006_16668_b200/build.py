@@ -12,7 +12,7 @@ LIB = os.path.join(_HERE, "libgshard_moe.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-ldl",
+    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-ldl", "--threads", "0",
 ]
 
 

@@ -64,6 +64,14 @@ void launch_dispatch_compact(const Dims& d, const void* x, const int32_t* crow_t
 // dispatch_combine.cu: dst[b][c][r] = src[b][r][c] for a batch of fp32 matrices [rows, cols].
 void launch_transpose_f32(const float* src, float* dst, int batch, int rows, int cols, cudaStream_t st);
 
+// Epilogue of the linear operator: pre = acc + bias, C = act(pre) + residual; pre optionally kept.
+struct LinearEpilogue {
+  const float* bias;         // [cols] or nullptr
+  const void* residual;      // laid out and typed like C, or nullptr (may be C itself)
+  void* pre;                 // laid out and typed like C, or nullptr
+  int act;                   // gshard_activation
+};
+
 // umma_gemm.cu: batched bf16 GEMM on tcgen05, C[b] = act(A[b] . B[b]).
 struct UmmaGemm {
   const void* A; const void* B; void* C;
@@ -93,6 +101,9 @@ struct UmmaGemm {
   int plain_stores;          // epilogue writes C with 16-byte stores instead of bulk tensor (TMA) stores
   int max_ctas;              // > 0: use at most this many CTAs (persistent grid), leaving the other
                              // multiprocessors to a kernel running beside this one on another stream
+  int splits;                // > 1: the contraction is cut into `splits` runs of whole k-blocks (batch 1); run i writes
+                             // its partial product to C + i * c_bs (fp32), and the caller adds them
+  const LinearEpilogue* linear;   // a_kmajor, !b_kmajor, batch 1: the linear operator's epilogue instead of relu / masks
 };
 int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st);
 // umma2_gemm.cu: the same contraction with the two-SM MMA (CTA pairs, 256 x 256 tiles).

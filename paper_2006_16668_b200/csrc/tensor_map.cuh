@@ -54,9 +54,14 @@ inline bool make_store_map(CUtensorMap* map, void* base, long long cols, long lo
 inline bool store_map_for(const UmmaGemm& g, CUtensorMap* mc) {
   const int esize = g.out_f32 ? 4 : 2;
   if (g.plain_stores || (reinterpret_cast<uintptr_t>(g.C) & 15u) || (g.c_ld * esize) % 16 ||
-      (g.batch > 1 && (g.c_bs * esize) % 16))
+      ((g.batch > 1 || g.splits > 1) && (g.c_bs * esize) % 16))
     return false;
-  return make_store_map(mc, g.C, g.cols, g.rows, g.batch, g.c_ld, g.c_bs, esize);
+  return make_store_map(mc, g.C, g.cols, g.rows, g.splits > 1 ? g.splits : g.batch, g.c_ld, g.c_bs, esize);
+}
+
+// Store map of the pre-activations a linear epilogue keeps (laid out like C).
+inline bool pre_map_for(const UmmaGemm& g, CUtensorMap* mp) {
+  return make_store_map(mp, g.linear->pre, g.cols, g.rows, g.batch, g.c_ld, g.c_bs, g.out_f32 ? 4 : 2);
 }
 
 }  // namespace gshard

@@ -60,6 +60,8 @@ struct Params2 {
   int n_fastest;
   int* status;
   int tma_store;   // epilogue rows leave by bulk tensor stores through map_c
+  int split;       // batch index = run of k_blocks k-blocks of the one problem (operands have no batch)
+  LinearEpilogue lin;   // LIN instantiations only
   // Ragged batches (compacted expert rows): problem b owns the 256-row tiles [tile_base[b], tile_base[b+1])
   // of a device-side prefix array with batch + 1 entries; nullptr = every problem has m_tiles row tiles.
   const int* tile_base;
@@ -79,10 +81,11 @@ __device__ __forceinline__ TileCoord decode(const Params2& p, int tile) {
   return t;
 }
 
-template <bool A_K, bool B_K, bool MASK>
+// LIN: the linear operator's epilogue (map_pre: tensor map of the kept pre-activations).
+template <bool A_K, bool B_K, bool MASK, bool LIN = false>
 __global__ void __launch_bounds__(kThreads, 1)
 umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                  const __grid_constant__ CUtensorMap map_c, const Params2 p) {
+                  const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_pre, const Params2 p) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kBarOff);
@@ -129,25 +132,27 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         if (tile + n_pairs < total_tiles) tn = decode(p, tile + n_pairs);   // the next tile's coordinates load meanwhile
         const int row0 = t.mt * 2 * BM + (int)rank * BM;      // this CTA's 128 rows of the 256-row tile
         const int col0 = t.nt * BN + (int)rank * BNH;         // this CTA's half of the B columns
+        const int kfirst = p.split ? t.b * p.k_blocks : 0, ob = p.split ? 0 : t.b;
         for (int kb = 0; kb < p.k_blocks; ++kb) {
           if (!ptx::mbar_wait(empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
           unsigned char* sa = smem + stage * kStageBytes;
           unsigned char* sb = sa + kABytes;
           const uint32_t bar = ptx::map_to_cta(ptx::smem_u32(full + stage), 0);
           if (rank == 0) ptx::mbar_arrive_expect_tx(full + stage, (uint32_t)(2 * kStageBytes));
+          const int k0 = (kfirst + kb) * BK;
           if (A_K) {
-            ptx::tma_load_3d_pair(sa, &map_a, bar, kb * BK, row0, t.b, pol_a);
+            ptx::tma_load_3d_pair(sa, &map_a, bar, k0, row0, ob, pol_a);
           } else {
 #pragma unroll
             for (int j = 0; j < BM / 64; ++j)
-              ptx::tma_load_3d_pair(sa + j * kBoxBytes, &map_a, bar, row0 + j * 64, kb * BK, t.b, pol_a);
+              ptx::tma_load_3d_pair(sa + j * kBoxBytes, &map_a, bar, row0 + j * 64, k0, ob, pol_a);
           }
           if (B_K) {
-            ptx::tma_load_3d_pair(sb, &map_b, bar, kb * BK, col0, t.b, pol_b);
+            ptx::tma_load_3d_pair(sb, &map_b, bar, k0, col0, ob, pol_b);
           } else {
 #pragma unroll
             for (int j = 0; j < BNH / 64; ++j)
-              ptx::tma_load_3d_pair(sb + j * kBoxBytes, &map_b, bar, col0 + j * 64, kb * BK, t.b, pol_b);
+              ptx::tma_load_3d_pair(sb + j * kBoxBytes, &map_b, bar, col0 + j * 64, k0, ob, pol_b);
           }
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
@@ -200,8 +205,11 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
       const int tile_row0 = t.mt * 2 * BM + (int)rank * BM;     // this CTA's 128 rows of the 256-row tile
       if (!ptx::mbar_wait_warp(acc_full + acc, acc_phase, abort_flag, lane)) { ok = false; break; }
       ptx::tc_fence_after_sync();
-      epilogue_tile<BN, MASK>(p, p.tma_store ? &map_c : nullptr, t, tile_row0, tmem_base + (uint32_t)(acc * BN), q, half,
-                              stg, lane);
+      if constexpr (LIN)
+        epilogue_linear_tile<BN>(p, &map_c, &map_pre, t, tile_row0, tmem_base + (uint32_t)(acc * BN), q, half, stg, lane);
+      else
+        epilogue_tile<BN, MASK>(p, p.tma_store ? &map_c : nullptr, t, tile_row0, tmem_base + (uint32_t)(acc * BN), q, half,
+                                stg, lane);
       ptx::tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive_remote_relaxed(ptx::map_to_cta(ptx::smem_u32(acc_empty + acc), 0));   // the leader's barrier
@@ -445,10 +453,10 @@ int launch2_resident_b(const CUtensorMap& ma, const CUtensorMap& mb, const CUten
   return GSHARD_OK;
 }
 
-template <bool A_K, bool B_K, bool MASK>
+template <bool A_K, bool B_K, bool MASK, bool LIN = false>
 int launch2_t(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const Params2& p, int pairs,
-              cudaStream_t st) {
-  auto kern = umma2_gemm_kernel<A_K, B_K, MASK>;
+              cudaStream_t st, const CUtensorMap* mp = nullptr) {
+  auto kern = umma2_gemm_kernel<A_K, B_K, MASK, LIN>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
     return GSHARD_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
@@ -463,7 +471,7 @@ int launch2_t(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& m
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kern, ma, mb, mc, p) != cudaSuccess) { cudaGetLastError(); return GSHARD_ERR_CUDA; }
+  if (cudaLaunchKernelEx(&cfg, kern, ma, mb, mc, mp ? *mp : mc, p) != cudaSuccess) { cudaGetLastError(); return GSHARD_ERR_CUDA; }
   count_launch();
   return GSHARD_OK;
 }
@@ -491,6 +499,11 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   p.m_tiles = ceil_div(g.rows, 2 * BM); p.n_tiles = ceil_div(g.cols, BN);
   p.total_tiles = p.m_tiles * p.n_tiles * g.batch;
   p.k_blocks = ceil_div(g.K, BK);
+  p.split = 0;
+  if (g.splits > 1) {
+    if (g.batch != 1 || !g.out_f32 || g.tile_base || g.linear || g.mask_bits || g.mask_bits_out) return GSHARD_ERR_INTERNAL;
+    p.split = 1; p.batch = g.splits; p.total_tiles = p.m_tiles * p.n_tiles * g.splits; p.k_blocks = ceil_div(p.k_blocks, g.splits);
+  }
   p.out_f32 = g.out_f32; p.relu = g.relu; p.a_stream = g.a_stream; p.b_stream = g.b_stream;
   p.n_fastest = (g.rows > g.cols) ? 1 : 0;
   p.status = status;
@@ -501,7 +514,7 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   const int sms = device_sms();
   int pairs = sms / 2;
   if (g.max_ctas > 0 && pairs > g.max_ctas / 2) pairs = g.max_ctas / 2 > 0 ? g.max_ctas / 2 : 1;
-  if (!g.a_kmajor && !g.b_kmajor && !g.mask_bits && !g.mask_bits_out && !p.tile_base && !g.out_f32 &&
+  if (!g.a_kmajor && !g.b_kmajor && !g.mask_bits && !g.mask_bits_out && !p.tile_base && !g.out_f32 && !p.split &&
       p.k_blocks <= resb2::kMaxKBlocks && p.m_tiles >= 2) {
     // short contraction, several row tiles per column block: B slice resident, deep A ring
     const int n_groups = p.n_tiles * g.batch;
@@ -510,6 +523,13 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
     return p.m_tiles < 16 ? launch2_resident_b<true>(ma, mb, mc, p, np, st) : launch2_resident_b<false>(ma, mb, mc, p, np, st);
   }
   if (pairs > p.total_tiles && !p.tile_base) pairs = p.total_tiles;   // ragged: count known on the device only
+  if (g.linear) {
+    CUtensorMap mp = mc;
+    if (!g.a_kmajor || g.b_kmajor || g.batch != 1 || p.tile_base || !tma_store) return GSHARD_ERR_INTERNAL;
+    if (g.linear->pre && !pre_map_for(g, &mp)) return GSHARD_ERR_CUDA;
+    p.lin = *g.linear;
+    return launch2_t<true, false, false, true>(ma, mb, mc, p, pairs, st, &mp);
+  }
 #define GSHARD_DISPATCH2(AK, BKM) \
   (p.mask_bits ? launch2_t<AK, BKM, true>(ma, mb, mc, p, pairs, st) : launch2_t<AK, BKM, false>(ma, mb, mc, p, pairs, st))
   if (g.a_kmajor && g.b_kmajor) return GSHARD_DISPATCH2(true, true);

@@ -2,6 +2,7 @@
 // memory, ReLU / mask, conversion, staging in swizzled shared memory, 128-byte row stores.  `P` is
 // the kernel's parameter struct (C, mask, rows, cols, c_ld, c_bs, out_f32, relu).
 #pragma once
+#include "activation.cuh"
 #include "kernels.cuh"
 #include "sm100_ptx.cuh"
 
@@ -175,6 +176,105 @@ __device__ __forceinline__ void epilogue_tile(const P& p, const CUtensorMap* map
       process_chunk<MASK>(r1, p, srow, lane, 4, m1);
       if (map_c) flush_rows_tma(stg, map_c, t.b, row0, col0, lane);
       else flush_rows(stg, p, t.b, row0, col0, lane);
+    }
+  }
+}
+
+// The linear operator's epilogue: pre = acc + bias, C = act(pre) + residual, and pre itself where the caller
+// keeps it.  Same share of the tile and same bulk tensor stores as above.  64 columns per round stay in
+// registers (two TMEM loads), so that pre and C can leave one after the other through the one staging
+// block; the residual's 64 columns of the thread's row are fetched while the accumulator load is in flight.
+// All of it in fp32, rounded once per output.
+template <int BN, typename P>
+__device__ __forceinline__ void epilogue_linear_tile(const P& p, const CUtensorMap* map_c, const CUtensorMap* map_pre,
+                                                     const TileCoord& t, int tile_row0, uint32_t tmem_acc, int q, int half,
+                                                     unsigned char* stg, int lane) {
+  constexpr int kHalfCols = BN / 2;
+  unsigned char* srow = stg + lane * kStgRowBytes;
+  const int row0 = tile_row0 + q * 32;
+  const int row = row0 + lane;
+  const uint32_t t_acc = tmem_acc + (uint32_t)(half * kHalfCols) + ((uint32_t)(q * 32) << 16);
+  struct Plain { int relu, out_f32; } plain{0, p.out_f32};
+#pragma unroll 1
+  for (int c = 0; c < kHalfCols / 64; ++c) {
+    const int col0 = round_col0<BN>(t, half, c);
+    if (col0 >= p.cols) break;                   // uniform over the warp
+    uint32_t r[2][32];
+    ptx::tmem_ld_32x32(t_acc + (uint32_t)(c * 64), r[0]);
+    ptx::tmem_ld_32x32(t_acc + (uint32_t)(c * 64 + 32), r[1]);
+    uint4 res[8];                                // bf16 residual: 64 columns (an fp32 one is read below)
+    const bool has_res = p.lin.residual != nullptr && row < p.rows;
+    const long long off = (long long)row * p.c_ld + col0;
+    if (has_res && !p.out_f32) {
+      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.lin.residual) + off);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) res[i] = col0 + 8 * i < p.cols ? src[i] : make_uint4(0, 0, 0, 0);
+    }
+    store_wait(lane);                            // the previous bulk store has read the staging block
+    ptx::tmem_ld_wait();
+    if (p.lin.bias) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          const int col = col0 + 32 * h + i;
+          if (col < p.cols) {                    // cols is a multiple of 8
+            const float4 b = __ldg(reinterpret_cast<const float4*>(p.lin.bias + col));
+            r[h][i] = __float_as_uint(__uint_as_float(r[h][i]) + b.x);
+            r[h][i + 1] = __float_as_uint(__uint_as_float(r[h][i + 1]) + b.y);
+            r[h][i + 2] = __float_as_uint(__uint_as_float(r[h][i + 2]) + b.z);
+            r[h][i + 3] = __float_as_uint(__uint_as_float(r[h][i + 3]) + b.w);
+          }
+        }
+    }
+    if (p.lin.pre) {
+      process_chunk<false>(r[0], plain, srow, lane, 0, 0);
+      if (p.out_f32) {
+        flush_rows_tma(stg, map_pre, t.b, row0, col0, lane);
+        store_wait(lane);
+        process_chunk<false>(r[1], plain, srow, lane, 0, 0);
+        if (col0 + 32 < p.cols) flush_rows_tma(stg, map_pre, t.b, row0, col0 + 32, lane);
+      } else {
+        process_chunk<false>(r[1], plain, srow, lane, 4, 0);
+        flush_rows_tma(stg, map_pre, t.b, row0, col0, lane);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      activate<32>(r[h], p.lin.act);
+      if (has_res) {
+        if (p.out_f32) {
+          const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(p.lin.residual) + off + 32 * h);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (col0 + 32 * h + 4 * i < p.cols) {
+              const float4 f = src[i];
+              r[h][4 * i] = __float_as_uint(__uint_as_float(r[h][4 * i]) + f.x);
+              r[h][4 * i + 1] = __float_as_uint(__uint_as_float(r[h][4 * i + 1]) + f.y);
+              r[h][4 * i + 2] = __float_as_uint(__uint_as_float(r[h][4 * i + 2]) + f.z);
+              r[h][4 * i + 3] = __float_as_uint(__uint_as_float(r[h][4 * i + 3]) + f.w);
+            }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float f[8];
+            Vec16<__nv_bfloat16>::load(res[4 * h + i], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r[h][8 * i + j] = __float_as_uint(__uint_as_float(r[h][8 * i + j]) + f[j]);
+          }
+        }
+      }
+    }
+    if (p.lin.pre) store_wait(lane);
+    process_chunk<false>(r[0], plain, srow, lane, 0, 0);
+    if (p.out_f32) {
+      flush_rows_tma(stg, map_c, t.b, row0, col0, lane);
+      store_wait(lane);
+      process_chunk<false>(r[1], plain, srow, lane, 0, 0);
+      if (col0 + 32 < p.cols) flush_rows_tma(stg, map_c, t.b, row0, col0 + 32, lane);
+    } else {
+      process_chunk<false>(r[1], plain, srow, lane, 4, 0);
+      flush_rows_tma(stg, map_c, t.b, row0, col0, lane);
     }
   }
 }

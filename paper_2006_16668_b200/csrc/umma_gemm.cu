@@ -64,6 +64,8 @@ struct Params {
   // a launch on CTA pairs covers; nullptr = they start at row 0
   const int* pair_base;
   int tma_store;   // epilogue rows leave by bulk tensor stores through map_c
+  int split;       // batch index = run of k_blocks k-blocks of the one problem (operands have no batch)
+  LinearEpilogue lin;   // LIN instantiations only
 };
 
 // Tile index -> (row tile, column tile, problem).
@@ -87,10 +89,11 @@ __device__ __forceinline__ TileCoord decode(const Params& p, int tile) {
 // 32-bit MN-major operand the instruction returns zeros).  A shared-memory row is still 128 bytes,
 // i.e. 32 elements: a k-block is 32 deep and an MMA contracts 8; stage sizes in bytes are those of
 // the bf16 form.
-template <bool A_K, bool B_K, int BN, bool MASK, bool TF32 = false>
+// LIN: the linear operator's epilogue (map_pre: tensor map of the kept pre-activations).
+template <bool A_K, bool B_K, int BN, bool MASK, bool TF32 = false, bool LIN = false>
 __global__ void __launch_bounds__(kThreads, 1)
 umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                 const __grid_constant__ CUtensorMap map_c, const Params p) {
+                 const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_pre, const Params p) {
   using C_ = Cfg<BN>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -137,24 +140,26 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
       for (int tile = blockIdx.x; tile < total_tiles && ok; tile += gridDim.x) {
         const TileCoord cur = t;
         if (tile + (int)gridDim.x < total_tiles) t = decode(p, tile + gridDim.x);   // the next tile's coordinates load meanwhile
+        const int kfirst = p.split ? cur.b * p.k_blocks : 0, ob = p.split ? 0 : cur.b;
         for (int kb = 0; kb < p.k_blocks; ++kb) {
           if (!ptx::mbar_wait(empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
           unsigned char* sa = smem + stage * C_::stage_bytes;
           unsigned char* sb = sa + kABytes;
           ptx::mbar_arrive_expect_tx(full + stage, (uint32_t)C_::stage_bytes);
+          const int k0 = (kfirst + kb) * BKE;
           if (A_K) {
-            ptx::tma_load_3d(sa, &map_a, full + stage, kb * BKE, cur.mt * BM, cur.b, pol_a);
+            ptx::tma_load_3d(sa, &map_a, full + stage, k0, cur.mt * BM, ob, pol_a);
           } else {
 #pragma unroll
             for (int j = 0; j < BM / kBoxMN; ++j)
-              ptx::tma_load_3d(sa + j * kBoxB, &map_a, full + stage, cur.mt * BM + j * kBoxMN, kb * BKE, cur.b, pol_a);
+              ptx::tma_load_3d(sa + j * kBoxB, &map_a, full + stage, cur.mt * BM + j * kBoxMN, k0, ob, pol_a);
           }
           if (B_K) {
-            ptx::tma_load_3d(sb, &map_b, full + stage, kb * BKE, cur.nt * BN, cur.b, pol_b);
+            ptx::tma_load_3d(sb, &map_b, full + stage, k0, cur.nt * BN, ob, pol_b);
           } else {
 #pragma unroll
             for (int j = 0; j < BN / kBoxMN; ++j)
-              ptx::tma_load_3d(sb + j * kBoxB, &map_b, full + stage, cur.nt * BN + j * kBoxMN, kb * BKE, cur.b, pol_b);
+              ptx::tma_load_3d(sb + j * kBoxB, &map_b, full + stage, cur.nt * BN + j * kBoxMN, k0, ob, pol_b);
           }
           if (++stage == C_::stages) { stage = 0; phase ^= 1u; }
         }
@@ -207,8 +212,11 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
       if (tile + (int)gridDim.x < total_tiles) tn = decode(p, tile + gridDim.x);
       if (!ptx::mbar_wait_warp(acc_full + acc, acc_phase, abort_flag, lane)) { ok = false; break; }
       ptx::tc_fence_after_sync();
-      epilogue_tile<BN, MASK>(p, p.tma_store ? &map_c : nullptr, t, t.mt * BM, tmem_base + (uint32_t)(acc * BN), q, half,
-                              stg, lane);
+      if constexpr (LIN)
+        epilogue_linear_tile<BN>(p, &map_c, &map_pre, t, t.mt * BM, tmem_base + (uint32_t)(acc * BN), q, half, stg, lane);
+      else
+        epilogue_tile<BN, MASK>(p, p.tma_store ? &map_c : nullptr, t, t.mt * BM, tmem_base + (uint32_t)(acc * BN), q, half,
+                                stg, lane);
       ptx::tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive_relaxed(acc_empty + acc);
@@ -399,13 +407,13 @@ umma_gemm_resident_b_kernel(const __grid_constant__ CUtensorMap map_a, const __g
 
 // ---- host side ------------------------------------------------------------------------------
 
-template <bool A_K, bool B_K, int BN, bool MASK, bool TF32 = false>
+template <bool A_K, bool B_K, int BN, bool MASK, bool TF32 = false, bool LIN = false>
 int launch_t(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const Params& p, int grid,
-             cudaStream_t st) {
-  auto kern = umma_gemm_kernel<A_K, B_K, BN, MASK, TF32>;
+             cudaStream_t st, const CUtensorMap* mp = nullptr) {
+  auto kern = umma_gemm_kernel<A_K, B_K, BN, MASK, TF32, LIN>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN>::smem_bytes) != cudaSuccess)
     return GSHARD_ERR_CUDA;
-  kern<<<grid, kThreads, Cfg<BN>::smem_bytes, st>>>(ma, mb, mc, p);
+  kern<<<grid, kThreads, Cfg<BN>::smem_bytes, st>>>(ma, mb, mc, mp ? *mp : mc, p);
   count_launch();
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
 }
@@ -437,6 +445,11 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   p.m_tiles = ceil_div(g.rows, BM); p.n_tiles = ceil_div(g.cols, BN);
   p.total_tiles = p.m_tiles * p.n_tiles * g.batch;
   p.k_blocks = ceil_div(g.K, bke);
+  p.split = 0;
+  if (g.splits > 1) {
+    if (g.batch != 1 || !g.out_f32 || g.tile_base || g.linear || g.mask_bits || g.mask_bits_out) return GSHARD_ERR_INTERNAL;
+    p.split = 1; p.batch = g.splits; p.total_tiles = p.m_tiles * p.n_tiles * g.splits; p.k_blocks = ceil_div(p.k_blocks, g.splits);
+  }
   p.out_f32 = g.out_f32; p.relu = g.relu; p.a_stream = g.a_stream; p.b_stream = g.b_stream;
   // stream the larger operand once: walk the tiles that share it back to back
   p.n_fastest = (g.rows > g.cols) ? 1 : 0;
@@ -449,7 +462,7 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   if (g.tile_base) p.n_fastest = 0;            // ragged lists are walked with the row tiles fastest
   int sms = device_sms();
   if (g.max_ctas > 0 && sms > g.max_ctas) sms = g.max_ctas;
-  if (!g.tf32 && !g.tile_base && !g.a_kmajor && !g.b_kmajor && !g.mask_bits && BN == 256 && p.k_blocks <= resb::kMaxKBlocks && p.m_tiles >= 4) {
+  if (!g.tf32 && !p.split && !g.tile_base && !g.a_kmajor && !g.b_kmajor && !g.mask_bits && BN == 256 && p.k_blocks <= resb::kMaxKBlocks && p.m_tiles >= 4) {
     // short contraction, several row tiles per column block: keep the B tile resident
     const int n_groups = p.n_tiles * g.batch;
     if (cudaFuncSetAttribute(umma_gemm_resident_b_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -460,6 +473,14 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
     return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
   }
   const int grid = (p.total_tiles < sms && !g.tile_base) ? p.total_tiles : sms;   // ragged: count known on the device only
+  if (g.linear) {
+    CUtensorMap mp = mc;
+    if (!g.a_kmajor || g.b_kmajor || g.batch != 1 || g.tf32 || g.tile_base || !tma_store) return GSHARD_ERR_INTERNAL;
+    if (g.linear->pre && !pre_map_for(g, &mp)) return GSHARD_ERR_CUDA;
+    p.lin = *g.linear;
+    return BN == 256 ? launch_t<true, false, 256, false, false, true>(ma, mb, mc, p, grid, st, &mp)
+                     : launch_t<true, false, 128, false, false, true>(ma, mb, mc, p, grid, st, &mp);
+  }
   if (g.tf32)
     return BN == 256 ? launch_t<true, true, 256, false, true>(ma, mb, mc, p, grid, st)
                      : launch_t<true, true, 128, false, true>(ma, mb, mc, p, grid, st);
