@@ -15,6 +15,7 @@
 #include <algorithm>
 
 #include "checks.cuh"
+#include "pack.cuh"
 
 namespace gshard {
 
@@ -24,21 +25,6 @@ constexpr int kLnMaxTeam = 1024;
 constexpr int kLnMaxM = 16 * kLnMaxTeam;
 constexpr int kLnSms = 148;                  // multiprocessors of a B200; only sizes the partial rows
 
-template <typename T, int W> struct alignas(sizeof(T) * W) Pack { T v[W]; };
-
-template <typename T, int W>
-__device__ __forceinline__ void load_pack(const T* p, float* f) {
-  const Pack<T, W> k = *reinterpret_cast<const Pack<T, W>*>(p);
-#pragma unroll
-  for (int j = 0; j < W; ++j) f[j] = to_f32<T>(k.v[j]);
-}
-template <typename T, int W>
-__device__ __forceinline__ void store_pack(T* p, const float* f) {
-  Pack<T, W> k;
-#pragma unroll
-  for (int j = 0; j < W; ++j) k.v[j] = from_f32<T>(f[j]);
-  *reinterpret_cast<Pack<T, W>*>(p) = k;
-}
 // W floats of a parameter vector (16-byte loads where W allows)
 template <int W>
 __device__ __forceinline__ void load_param(const float* p, float* f) {

@@ -12,143 +12,13 @@
 // One warp per token.  Near ties between fp32 values of c would make the choice depend on rounding, so
 // c is compared in 64 bits.
 #include <algorithm>
-#include <cfloat>
-#include <cmath>
 
-#include "checks.cuh"
 #include "plan.cuh"
+#include "route.cuh"
 
 namespace gshard {
 
 namespace {
-
-constexpr int kRouteMaxK = 32;
-constexpr int kRouteMaxGroups = 32;
-constexpr int kRouteTile = 64;              // tokens per partial row of the mean scores
-constexpr unsigned kAll = 0xffffffffu;
-
-struct RouteArgs {
-  const void* logits;
-  const float* bias;
-  int32_t* expert_idx;
-  float* weight;
-  float* rowstat;        // [N][2] softmax maximum and 1 / sum (for the mean scores), or nullptr
-  int32_t* load;         // [G][E] or nullptr
-  long long n;
-  int S, E, k, groups, kept, group_top, sigmoid, renorm;
-  float scale;
-};
-
-// NaN bars like -inf; +inf counts as the largest float, so that differences of logits stay finite.
-template <typename T> __device__ __forceinline__ float usable(T v) {
-  const float f = to_f32<T>(v);
-  return f == f ? fminf(f, FLT_MAX) : -INFINITY;
-}
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, off));
-  return v;
-}
-template <typename F> __device__ __forceinline__ F warp_sum(F v) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(kAll, v, off);
-  return v;
-}
-// larger value first, equal values to the lower index
-__device__ __forceinline__ void warp_best(double& v, int& e) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    const double ov = __shfl_xor_sync(kAll, v, off);
-    const int oe = __shfl_xor_sync(kAll, e, off);
-    if (ov > v || (ov == v && oe < e)) { v = ov; e = oe; }
-  }
-}
-
-// The choice of one token in 64 bits: lane j < k receives the j-th expert (-1: none left).
-template <typename T>
-__device__ __noinline__ int choose_exact(const T* __restrict__ row, const RouteArgs& a, int lane) {
-  const bool scores = a.bias != nullptr || (a.groups > 1 && a.group_top == 2);
-  double top = 0.0, inv = 1.0;
-  if (scores && !a.sigmoid) {
-    float mx = -INFINITY;
-    for (int e = lane; e < a.E; e += 32) mx = fmaxf(mx, usable(row[e]));
-    mx = warp_max(mx);
-    top = mx == -INFINITY ? 0.0 : (double)mx;
-    double s = 0.0;
-    for (int e = lane; e < a.E; e += 32) s += exp((double)usable(row[e]) - top);
-    s = warp_sum(s);
-    inv = s > 0.0 ? s : 1.0;
-  }
-  auto value = [&](int e, bool by_score) -> double {
-    const float l = usable(row[e]);
-    if (l == -INFINITY) return -INFINITY;
-    if (!by_score) return (double)l;
-    const double s = a.sigmoid ? 1.0 / (1.0 + exp(-(double)l)) : exp((double)l - top) / inv;
-    const double c = a.bias ? s + (double)a.bias[e] : s;
-    return c == c ? c : -INFINITY;
-  };
-  unsigned keep = kAll;
-  const int size = a.E / a.groups;
-  if (a.kept < a.groups) {
-    double mine = -INFINITY;                    // lane g: the value of group g
-    for (int g = 0; g < a.groups; ++g) {
-      double b1 = -INFINITY, b2 = -INFINITY;
-      for (int i = lane; i < size; i += 32) {
-        const double v = value(g * size + i, scores);
-        if (v > b1) { b2 = b1; b1 = v; } else if (v > b2) b2 = v;
-      }
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) {
-        const double o1 = __shfl_xor_sync(kAll, b1, off), o2 = __shfl_xor_sync(kAll, b2, off);
-        if (o1 > b1) { b2 = fmax(b1, o2); b1 = o1; } else b2 = fmax(b2, o1);
-      }
-      const double v = (a.group_top == 2 && b2 != -INFINITY) ? b1 + b2 : b1;
-      if (lane == g) mine = v;
-    }
-    keep = 0;
-    bool taken = lane >= a.groups;
-    for (int j = 0; j < a.kept; ++j) {
-      double v = taken ? -INFINITY : mine;
-      int e = taken ? 64 + lane : lane;
-      warp_best(v, e);
-      if (e < 32) keep |= 1u << e;
-      if (e == lane) taken = true;
-    }
-  }
-  int picked = -1;
-  double last = INFINITY;
-  int last_e = -1;
-  for (int j = 0; j < a.k; ++j) {
-    double best = -INFINITY;
-    int at = INT_MAX;
-    for (int e = lane; e < a.E; e += 32) {
-      if (!((keep >> (e / size)) & 1u)) continue;
-      const double v = value(e, a.bias != nullptr);
-      if (v == -INFINITY || v > last || (v == last && e <= last_e)) continue;
-      if (v > best || at == INT_MAX) { best = v; at = e; }
-    }
-    warp_best(best, at);
-    if (at == INT_MAX) break;
-    if (lane == j) picked = at;
-    last = best; last_e = at;
-  }
-  return picked;
-}
-
-// Lane j holds chosen expert idx (or -1) with logit l (or -inf): its score over the largest chosen score, and
-// the sum of those ratios over the warp.  Stays exact where the scores themselves underflow.
-__device__ __forceinline__ float chosen_ratio(float l, int sigmoid, float& total) {
-  float top = warp_max(l);
-  if (top == -INFINITY) top = 0.f;
-  float r;
-  if (!sigmoid) r = expf(l - top);
-  else if (top < 0.f) r = expf(l - top) * (1.f + expf(top)) / (1.f + expf(fminf(l, 0.f)));
-  else r = (1.f + expf(-top)) / (1.f + expf(-l));
-  if (l == -INFINITY) r = 0.f;
-  total = warp_sum(r);
-  return r;
-}
-__device__ __forceinline__ float sigmoid_f(float l) { return 1.f / (1.f + expf(-l)); }
 
 template <typename T>
 __global__ void __launch_bounds__(256) route_fwd_kernel(const RouteArgs a) {
@@ -156,7 +26,7 @@ __global__ void __launch_bounds__(256) route_fwd_kernel(const RouteArgs a) {
   const long long nwarps = ((long long)gridDim.x * blockDim.x) >> 5;
   for (long long t = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5; t < a.n; t += nwarps) {
     const T* row = static_cast<const T*>(a.logits) + t * a.E;
-    const int e = choose_exact<T>(row, a, lane);
+    const int e = choose_exact<T>(row, a, lane, nullptr);
     float mx = 0.f, inv = 0.f;
     if (!a.sigmoid && (a.rowstat || !a.renorm)) {
       mx = -INFINITY;
@@ -203,27 +73,23 @@ __global__ void __launch_bounds__(128) route_colsum_kernel(const T* __restrict__
   partial[((long long)blockIdx.z * tiles + blockIdx.y) * E + e] = sum;
 }
 
-// m[g][e] = (1/S) sum over the tiles, in order.
-__global__ void __launch_bounds__(128) route_mean_kernel(const float* __restrict__ partial, float* __restrict__ m, int tiles,
+// m[g][e] = (1/S) sum over the tiles: 8 strands of tiles in order, then the strands.
+__global__ void __launch_bounds__(256) route_mean_kernel(const float* __restrict__ partial, float* __restrict__ m, int tiles,
                                                          int S, int E) {
-  const int e = blockIdx.x * 128 + threadIdx.x;
-  if (e >= E) return;
-  const float* p = partial + (long long)blockIdx.y * tiles * E + e;
+  __shared__ float part[8][33];
+  const int e = blockIdx.x * 32 + threadIdx.x;
   float s = 0.f;
-  for (int i = 0; i < tiles; ++i) s += p[(long long)i * E];
-  m[(long long)blockIdx.y * E + e] = s / (float)S;
+  if (e < E)
+    for (int i = threadIdx.y; i < tiles; i += 8) s += partial[((long long)blockIdx.y * tiles + i) * E + e];
+  part[threadIdx.y][threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.y == 0 && e < E) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += part[i][threadIdx.x];
+    m[(long long)blockIdx.y * E + e] = s / (float)S;
+  }
 }
-
-struct RouteGradArgs {
-  const void* logits;
-  const int32_t* expert_idx;
-  const float* dweight;
-  const float* dm;       // [G][E] or nullptr
-  void* dlogits;
-  long long n;
-  int S, E, k, sigmoid, renorm;
-  float scale;
-};
 
 // Gradient of sum(dweight w) + sum(dm m) with the choice held constant.  With D = sum_j dw_j w_j / scale:
 //   renormalised   d/dlog s_i = scale w_i (dw_i - D), so dl_i gets that (softmax), times 1 - s_i (sigmoid)
@@ -364,18 +230,29 @@ int gshard_moe_route(const gshard_route_config* config, const void* logits, cons
   a.n = n; a.S = c.S; a.E = c.E; a.k = c.k; a.groups = c.groups; a.kept = c.groups_kept; a.group_top = c.group_top;
   a.sigmoid = c.score == GSHARD_SCORE_SIGMOID; a.renorm = c.renormalise != 0; a.scale = c.scale;
   if (load && cudaMemsetAsync(load, 0, (size_t)c.G * c.E * 4, st) != cudaSuccess) { cudaGetLastError(); return GSHARD_ERR_CUDA; }
+  // kept == groups leaves nothing out
+  if (a.kept == a.groups) a.groups = a.kept = 1;
+  float* partial = m ? reinterpret_cast<float*>(ws + pl.partial) : nullptr;
+  float* sums = pl.tiles == 1 ? m : partial;
+  const bool bf16 = c.dtype == GSHARD_BF16;
+  if (bf16 ? launch_route_fwd_fast<__nv_bfloat16>(a, c.G, sums, st) : launch_route_fwd_fast<float>(a, c.G, sums, st)) {
+    if (m && pl.tiles > 1) {
+      route_mean_kernel<<<dim3(ceil_div(c.E, 32), c.G), dim3(32, 8), 0, st>>>(partial, m, pl.tiles, c.S, c.E);
+      count_launch();
+    }
+    return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
+  }
   const int grid = grid_for_rows(n);
-  if (c.dtype == GSHARD_BF16) route_fwd_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
+  if (bf16) route_fwd_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
   else route_fwd_kernel<float><<<grid, 256, 0, st>>>(a);
   count_launch();
   if (m) {
-    float* partial = reinterpret_cast<float*>(ws + pl.partial);
     const dim3 cg(ceil_div(c.E, 128), pl.tiles, c.G);
-    if (c.dtype == GSHARD_BF16)
+    if (bf16)
       route_colsum_kernel<__nv_bfloat16><<<cg, 128, 0, st>>>(static_cast<const __nv_bfloat16*>(logits), a.rowstat, partial, c.S, c.E, a.sigmoid);
     else
       route_colsum_kernel<float><<<cg, 128, 0, st>>>(static_cast<const float*>(logits), a.rowstat, partial, c.S, c.E, a.sigmoid);
-    route_mean_kernel<<<dim3(ceil_div(c.E, 128), c.G), 128, 0, st>>>(partial, m, pl.tiles, c.S, c.E);
+    route_mean_kernel<<<dim3(ceil_div(c.E, 32), c.G), dim3(32, 8), 0, st>>>(partial, m, pl.tiles, c.S, c.E);
     count_launch(2);
   }
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
@@ -398,10 +275,13 @@ int gshard_moe_route_backward(const gshard_route_config* config, const void* log
   a.n = n; a.S = c.S; a.E = c.E; a.k = c.k; a.sigmoid = c.score == GSHARD_SCORE_SIGMOID; a.renorm = c.renormalise != 0;
   a.scale = c.scale;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int grid = grid_for_rows(n);
-  if (c.dtype == GSHARD_BF16) route_bwd_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
-  else route_bwd_kernel<float><<<grid, 256, 0, st>>>(a);
-  count_launch();
+  const bool bf16 = c.dtype == GSHARD_BF16;
+  if (!(bf16 ? launch_route_bwd_fast<__nv_bfloat16>(a, st) : launch_route_bwd_fast<float>(a, st))) {
+    const int grid = grid_for_rows(n);
+    if (bf16) route_bwd_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
+    else route_bwd_kernel<float><<<grid, 256, 0, st>>>(a);
+    count_launch();
+  }
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
 }
 

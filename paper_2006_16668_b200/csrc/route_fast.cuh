@@ -1,0 +1,717 @@
+// Routing kernels that hold a token's logits in registers: LPR lanes of a warp (8 or 32) share a token, V
+// logits each, and the other lanes work on further tokens.  Included by one source file per logits type.
+//
+// What bounds the pass: the logits are read once, so HBM while few experts are chosen, the arithmetic of
+// the choice with many (8 of 512 in 4 of 8 groups: see the figures at the launcher).  Reductions and
+// the bookkeeping of a pick cost about the same however many tokens the warp holds, which is why eight
+// lanes per token are taken where the experts fit.
+// Layout: with groups, LPR / groups lanes own a group, else all lanes own the whole row; the owners take
+// turns of W consecutive experts, so that loads are whole 16-byte words (W = 1 for rows that are not).  The values
+// that decide the choice lie in shared memory as well, in chunks of 8 per lane with the chunk's maximum in a
+// register: a pick then looks at one chunk of one lane instead of at all its values.
+#pragma once
+#include "route.cuh"
+
+namespace gshard {
+
+namespace {
+
+constexpr int kRouteThreads = 128;
+constexpr int kRouteWarps = kRouteThreads / 32;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 1 / (1 + exp(-l)) to about 2^-22: two approximate operations of 1 to 2 units in the last place
+__device__ __forceinline__ float sigmoid_fast(float l) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(1.f + exp2_approx(-l * kLog2e)));
+  return y;
+}
+
+// two fp32 operations per instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+template <int LPR> __device__ __forceinline__ float seg_max(float v) {
+#pragma unroll
+  for (int off = LPR / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, off));
+  return v;
+}
+template <int LPR> __device__ __forceinline__ float seg_sum(float v) {
+#pragma unroll
+  for (int off = LPR / 2; off > 0; off >>= 1) v += __shfl_xor_sync(kAll, v, off);
+  return v;
+}
+template <int LPR> __device__ __forceinline__ int seg_min(int v) {
+#pragma unroll
+  for (int off = LPR / 2; off > 0; off >>= 1) v = min(v, __shfl_xor_sync(kAll, v, off));
+  return v;
+}
+// chosen_ratio for a token held by LPR lanes
+template <int LPR> __device__ __forceinline__ float seg_ratio(float l, int sigmoid, float& total) {
+  float top = seg_max<LPR>(l);
+  if (top == -INFINITY) top = 0.f;
+  float r;
+  if (!sigmoid) r = expf(l - top);
+  else if (top < 0.f) r = expf(l - top) * (1.f + expf(top)) / (1.f + expf(fminf(l, 0.f)));
+  else r = (1.f + expf(-top)) / (1.f + expf(-l));
+  if (l == -INFINITY) r = 0.f;
+  total = seg_sum<LPR>(r);
+  return r;
+}
+
+// Where a lane's values lie in the row.
+template <int W> struct RouteLane {
+  int base, q, P, size;     // first expert of the lane's group, lane inside the group, lanes per group, experts per group
+  __device__ __forceinline__ int offset(int i) const { return ((i / W) * P + q) * W + i % W; }   // inside the group
+  __device__ __forceinline__ int expert(int i) const { return base + offset(i); }
+};
+
+// V logits of this lane; -inf beyond the group's end (`full`: the group fills the lanes exactly).
+template <typename T, int W, int V>
+__device__ __forceinline__ void load_logits(const T* row, const RouteLane<W>& ln, bool full, float (&v)[V]) {
+  if (full) {
+#pragma unroll
+    for (int j = 0; j < V / W; ++j) load_pack<T, W>(row + ln.base + (j * ln.P + ln.q) * W, v + j * W);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V / W; ++j) {
+      const int off = (j * ln.P + ln.q) * W;
+      if (off < ln.size) {
+        load_pack<T, W>(row + ln.base + off, v + j * W);
+      } else {
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[j * W + w] = -INFINITY;
+      }
+    }
+  }
+}
+// NaN bars like -inf, +inf counts as the largest float
+template <int V> __device__ __forceinline__ void clean(float (&v)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = fminf(fmaxf(v[i], -INFINITY), FLT_MAX);
+}
+
+// 8 consecutive values of a lane (chunk c) out of shared memory.
+__device__ __forceinline__ void chunk_values(const float* st, int lane, int c, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 4) {
+    const float4 f = *reinterpret_cast<const float4*>(st + ((c * 2 + i / 4) * 32 + lane) * 4);
+    x[i] = f.x; x[i + 1] = f.y; x[i + 2] = f.z; x[i + 3] = f.w;
+  }
+}
+__device__ __forceinline__ void chunk_store(float* st, int lane, int i, const float* x) {      // i a multiple of 4
+  *reinterpret_cast<float4*>(st + (i / 4 * 32 + lane) * 4) = make_float4(x[0], x[1], x[2], x[3]);
+}
+
+// A score in 64 bits; norm: the 64-bit sum of exp(l - mx) over the row (softmax).
+__device__ __noinline__ double score64(float l, int sigmoid, float mx, double norm) {
+  return sigmoid ? 1.0 / (1.0 + exp(-(double)l)) : exp((double)l - (double)mx) / norm;
+}
+template <int LPR, int V, int W, typename T>
+__device__ __noinline__ double softmax_norm64(const T* row, const RouteLane<W>& ln, float mx) {
+  double s = 0.0;
+#pragma unroll 1
+  for (int i = 0; i < V; ++i)
+    if (ln.offset(i) < ln.size) s += exp((double)usable(row[ln.expert(i)]) - (double)mx);
+#pragma unroll
+  for (int off = LPR / 2; off > 0; off >>= 1) s += __shfl_xor_sync(kAll, s, off);
+  return s > 0.0 ? s : 1.0;
+}
+
+// BIASED: a bias or sums of group scores decide, so that scores are needed before the choice; else logits do.
+// MEAN: sums of the scores over the block's tokens, in registers, or (64 values per lane) in shared memory, where
+// they leave the registers to more warps.
+template <typename T, int W, int LPR, int V, bool BIASED, bool MEAN>
+__global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BIASED ? 3 : 4) : 1) route_fwd_fast_kernel(const RouteArgs a, float* __restrict__ sums) {
+  constexpr int RPW = 32 / LPR;               // tokens per warp
+  constexpr int NC = V / 8;
+  constexpr bool ACC_SMEM = MEAN && V == 64;
+  extern __shared__ __align__(16) float route_smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int slot = lane / LPR, p = lane % LPR;
+  float* st = route_smem + warp * V * 32;                       // the values that decide; at the end the sums
+  float* sacc = route_smem + (warp + kRouteWarps) * V * 32;     // ACC_SMEM
+  RouteLane<W> ln;
+  ln.P = LPR / a.groups; ln.q = p % ln.P; ln.size = a.E / a.groups; ln.base = p / ln.P * ln.size;
+  const bool by_bias = BIASED && a.bias != nullptr;
+  const bool need_sum = !a.sigmoid && (MEAN || !a.renorm || BIASED);
+  const int t0 = blockIdx.x * kRouteTile, t1 = min(a.S, t0 + kRouteTile);
+  const long long first = (long long)blockIdx.y * a.S;
+  float acc[MEAN && !ACC_SMEM ? V : 4];
+  if (MEAN && !ACC_SMEM) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[ACC_SMEM ? 0 : i] = 0.f;
+  }
+  if (ACC_SMEM) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) *reinterpret_cast<float4*>(sacc + (i / 4 * 32 + lane) * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  // f * s[0..4) of an active token to the sums i .. i + 3
+  auto accumulate = [&](int i, const float* s, float f) {
+    const float2 ff = make_float2(f, f);
+    if (ACC_SMEM) {
+      float4* at = reinterpret_cast<float4*>(sacc + (i / 4 * 32 + lane) * 4);
+      const float4 o = *at;
+      const float2 lo = fma2(make_float2(s[0], s[1]), ff, make_float2(o.x, o.y));
+      const float2 hi = fma2(make_float2(s[2], s[3]), ff, make_float2(o.z, o.w));
+      *at = make_float4(lo.x, lo.y, hi.x, hi.y);
+    } else {
+#pragma unroll
+      for (int w = 0; w < 4; w += 2) {
+        const float2 o = fma2(make_float2(s[w], s[w + 1]), ff, make_float2(acc[ACC_SMEM ? 0 : i + w], acc[ACC_SMEM ? 1 : i + w + 1]));
+        acc[ACC_SMEM ? 0 : i + w] = o.x; acc[ACC_SMEM ? 1 : i + w + 1] = o.y;
+      }
+    }
+  };
+
+  const bool full = ln.size == V * ln.P;
+  for (int s0 = t0 + warp * RPW; s0 < t1; s0 += kRouteWarps * RPW) {
+    const bool active = s0 + slot < t1;
+    const long long t = first + min(s0 + slot, t1 - 1);
+    const T* row = static_cast<const T*>(a.logits) + t * a.E;
+    float v[V];
+    load_logits<T, W, V>(row, ln, full, v);
+    {                                          // the warp's next tokens on their way into L2 meanwhile
+      const int s1 = s0 + kRouteWarps * RPW;
+      const char* ahead = reinterpret_cast<const char*>(static_cast<const T*>(a.logits) + (first + s1) * a.E);
+      const int bytes = min(RPW, t1 - s1) * a.E * (int)sizeof(T);
+      for (int o = lane * 128; o < bytes; o += 4096) asm volatile("prefetch.global.L2 [%0];" ::"l"(ahead + o));
+    }
+    float cm[NC];
+    float mx = -INFINITY, inv = 0.f;
+    double norm64 = 0.0;                       // 64-bit sum of a softmax, once something needs it
+    // Errors of fp32 scores: of a softmax, (V + 32) roundings of its sum and its exponentials; of a sigmoid,
+    // under 2^-20; the sum with the bias half a step.  Values closer than twice that are compared in 64 bits.
+    float slack = 0x1p-20f;
+    if (!BIASED) {
+      // fmaxf passes over NaN, so that the choice needs no clean-up; exponentials of NaN or of infinite
+      // logits are caught by the two tests below
+      __syncwarp();                            // the previous tokens' values have been read
+#pragma unroll
+      for (int i = 0; i < V; i += 4) chunk_store(st, lane, i, v + i);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float m = v[c * 8];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) m = fmaxf(m, v[c * 8 + i]);
+        cm[c] = fmaxf(m, -INFINITY);
+        mx = fmaxf(mx, cm[c]);
+      }
+      if (need_sum) {
+        mx = seg_max<LPR>(mx);
+        const float shift = -mx * kLog2e;      // its rounding is a factor that the sum shares
+        float2 sum2x[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+          const float2 e = fma2(make_float2(v[i], v[i + 1]), make_float2(kLog2e, kLog2e), make_float2(shift, shift));
+          v[i] = exp2_approx(e.x); v[i + 1] = exp2_approx(e.y);
+          sum2x[i / 2 % 2] = add2(sum2x[i / 2 % 2], make_float2(v[i], v[i + 1]));
+        }
+        sum2x[0] = add2(sum2x[0], sum2x[1]);
+        float sum = seg_sum<LPR>(sum2x[0].x + sum2x[0].y);
+        const bool odd = !(fabsf(mx) <= 0x1p20f) || !(sum < INFINITY);
+        if (__any_sync(kAll, odd)) {           // NaN, infinite or huge logits, or no expert at all
+          float u[8], m2 = -INFINITY, sum2 = 0.f;
+#pragma unroll 1
+          for (int c = 0; c < NC; ++c) {
+            chunk_values(st, lane, c, u);
+            for (int i = 0; i < 8; ++i) m2 = fmaxf(m2, u[i]);
+          }
+          m2 = fminf(seg_max<LPR>(m2), FLT_MAX);
+          if (m2 == -INFINITY) m2 = 0.f;
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            chunk_values(st, lane, c, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float e = exp2_approx((fminf(fmaxf(u[i], -INFINITY), FLT_MAX) - m2) * kLog2e);
+              sum2 += e;
+              if (odd) v[c * 8 + i] = e;
+            }
+          }
+          sum2 = seg_sum<LPR>(sum2);
+          if (odd) { mx = m2; sum = sum2; }
+        }
+        inv = sum > 0.f ? 1.f / sum : 0.f;
+      }
+      if (MEAN && a.sigmoid) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = sigmoid_fast(fmaxf(v[i], -INFINITY));
+      }
+      if (MEAN && active) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) accumulate(i, v + i, a.sigmoid ? 1.f : inv);
+      }
+    } else {
+      clean<V>(v);
+      if (need_sum) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) mx = fmaxf(mx, v[i]);
+        mx = seg_max<LPR>(mx);
+        if (mx == -INFINITY) mx = 0.f;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum += exp2_approx((v[i] - mx) * kLog2e);
+        sum = seg_sum<LPR>(sum);
+        inv = sum > 0.f ? 1.f / sum : 0.f;
+        slack = (V + 32) * 0x1p-24f * inv;
+      }
+      __syncwarp();                            // the previous tokens' values have been read
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float best = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < 8; h += 4) {
+          float b[4] = {0.f, 0.f, 0.f, 0.f}, s[4], x[4];
+          if (by_bias) {
+            constexpr int C = W < 4 ? W : 4;
+#pragma unroll
+            for (int w = 0; w < 4; w += C) {
+              const int off = ln.offset(c * 8 + h + w);
+              if (off < ln.size) load_pack<float, C>(a.bias + ln.base + off, b + w);
+            }
+          }
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float l = v[c * 8 + h + w];
+            s[w] = a.sigmoid ? sigmoid_fast(l) : exp2_approx((l - mx) * kLog2e) * inv;
+            // a NaN bias bars; without a bias the logits decide, and the scores only value the groups
+            x[w] = l == -INFINITY ? -INFINITY : by_bias ? fmaxf(s[w] + b[w], -INFINITY) : l;
+            best = fmaxf(best, x[w]);
+          }
+          chunk_store(st, lane, c * 8 + h, x);
+          if (MEAN && active) accumulate(c * 8 + h, s, 1.f);
+        }
+        cm[c] = best;
+      }
+    }
+    if (a.groups > 1) {
+      float top1 = -INFINITY, top2 = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        top2 = fmaxf(top2, fminf(top1, cm[c]));
+        top1 = fmaxf(top1, cm[c]);
+      }
+      if (BIASED && a.group_top == 2) {        // the runner-up may share the best one's chunk
+        int bc = 0;
+#pragma unroll
+        for (int c = NC - 1; c >= 0; --c)
+          if (cm[c] == top1) bc = c;
+        float x[8], x1 = -INFINITY, x2 = -INFINITY;
+        chunk_values(st, lane, bc, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { x2 = fmaxf(x2, fminf(x1, x[i])); x1 = fmaxf(x1, x[i]); }
+        top2 = fmaxf(top2, x2);
+      }
+      for (int off = 1; off < ln.P; off <<= 1) {
+        const float o1 = __shfl_xor_sync(kAll, top1, off), o2 = __shfl_xor_sync(kAll, top2, off);
+        top2 = fmaxf(fminf(top1, o1), fmaxf(top2, o2));
+        top1 = fmaxf(top1, o1);
+      }
+      const float floor2 = a.group_top == 2 ? top2 : top1;
+      if (BIASED && !by_bias) {                // logits so far: scores grow with them
+        top1 = top1 == -INFINITY ? top1 : a.sigmoid ? sigmoid_fast(top1) : exp2_approx((top1 - mx) * kLog2e) * inv;
+        top2 = top2 == -INFINITY ? top2 : a.sigmoid ? sigmoid_fast(top2) : exp2_approx((top2 - mx) * kLog2e) * inv;
+      }
+      const float mine = BIASED && a.group_top == 2 && top2 != -INFINITY ? top1 + top2 : top1;
+      const int group = p / ln.P;
+      int better = 0;
+      for (int g = 0; g < a.groups; ++g) {
+        const float other = __shfl_sync(kAll, mine, slot * LPR + g * ln.P);
+        better += (other > mine || (other == mine && g < group)) ? 1 : 0;
+      }
+      bool keep = better < a.kept;
+      if (BIASED) {
+        const float worst_kept = -seg_max<LPR>(keep ? -mine : -INFINITY);
+        const float best_left = seg_max<LPR>(keep ? -INFINITY : mine);
+        const bool near = best_left != -INFINITY &&
+                          worst_kept - best_left <= 4.f * slack + 0x1p-20f * fmaxf(fabsf(worst_kept), fabsf(best_left));
+        if (__any_sync(kAll, near)) {
+          // the groups' values again in 64 bits, from the few entries that can be among a group's best
+          if (!a.sigmoid && norm64 == 0.0) norm64 = softmax_norm64<LPR, V>(row, ln, mx);
+          const float from = floor2 - (by_bias ? 2.f * slack + 0x1p-21f * fabsf(floor2) : 0.f);
+          double d1 = -INFINITY, d2 = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < NC; ++c) {
+            float x[8];
+            chunk_values(st, lane, c, x);
+            for (int i = 0; i < 8; ++i) {
+              if (x[i] == -INFINITY || !(x[i] >= from || floor2 == -INFINITY)) continue;
+              const int e = ln.expert(c * 8 + i);
+              const double d = score64(usable(row[e]), a.sigmoid, mx, norm64) + (by_bias ? (double)a.bias[e] : 0.0);
+              if (d > d1) { d2 = d1; d1 = d; } else if (d > d2) d2 = d;
+            }
+          }
+          for (int off = 1; off < ln.P; off <<= 1) {
+            const double o1 = __shfl_xor_sync(kAll, d1, off), o2 = __shfl_xor_sync(kAll, d2, off);
+            d2 = fmax(fmin(d1, o1), fmax(d2, o2));
+            d1 = fmax(d1, o1);
+          }
+          const double mine64 = a.group_top == 2 && d2 != -INFINITY ? d1 + d2 : d1;
+          better = 0;
+          for (int g = 0; g < a.groups; ++g) {
+            const double other = __shfl_sync(kAll, mine64, slot * LPR + g * ln.P);
+            better += (other > mine64 || (other == mine64 && g < group)) ? 1 : 0;
+          }
+          keep = better < a.kept;
+        }
+      }
+      if (!keep) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) cm[c] = -INFINITY;
+      }
+    }
+    // Picks.  The lanes whose best value is the token's best look up which one it is (the lowest index wins) and
+    // the winner takes it out of its chunk; values above (lastv, lasti) in the order of choice are taken.
+    float bv = cm[0], lastv = INFINITY;
+#pragma unroll
+    for (int c = 1; c < NC; ++c) bv = fmaxf(bv, cm[c]);
+    // With a bias fp32 values that are too close to call are looked at again: the picks go on behind the k-th as
+    // long as its value is not clearly larger, and lane p also holds the (p + LPR)-th of them.
+    int lasti = -1, picked = -1, extra = -1, held = a.k;
+    float value = -INFINITY, before = INFINITY, kth = INFINITY;
+    bool near = false, more = by_bias;
+    for (int j = 0; j < a.k || (j < 2 * LPR && __any_sync(kAll, more)); ++j) {
+      const float gv = seg_max<LPR>(bv);
+      int e = INT_MAX, bi = 0, bc = 0;
+      float left = -INFINITY;
+      const bool mine = bv == gv && gv != -INFINITY;
+      if (mine) {
+#pragma unroll
+        for (int c = NC - 1; c >= 0; --c)
+          if (cm[c] == bv) bc = c;
+        float x[8];
+        chunk_values(st, lane, bc, x);
+        // taken values of the chunk lie above (lastv, lasti); the first of the rest that equals bv is the pick
+#pragma unroll
+        for (int i = 7; i >= 0; --i)
+          if (x[i] == bv && !(x[i] == lastv && bc * 8 + i <= lasti)) bi = bc * 8 + i;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (x[i] < bv || (x[i] == bv && bc * 8 + i > bi)) left = fmaxf(left, x[i]);
+        e = ln.expert(bi);
+      }
+      int ge = seg_min<LPR>(e);
+      if (by_bias) {
+        const float top = j < a.k ? before : kth;
+        const bool tight = gv != -INFINITY && top - gv <= 2.f * slack + 0x1p-22f * fmaxf(fabsf(top), fabsf(gv));
+        if (j >= a.k) {
+          more = more && tight;
+          if (more) { held = j + 1; near = true; }
+        } else if (j > 0 && tight) {
+          near = true;
+        }
+        before = gv;
+        if (j == a.k - 1) kth = gv;
+      }
+      const int got = ge == INT_MAX || (j >= a.k && !more) ? -1 : ge;
+      if (p == j) { picked = got; value = gv; }
+      if (p + LPR == j) extra = got;
+      if (mine && e == ge) {
+        lastv = bv; lasti = bi;
+        bv = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          if (c == bc) cm[c] = left;
+          bv = fmaxf(bv, cm[c]);
+        }
+      }
+    }
+    if (BIASED && __any_sync(kAll, near)) {
+      if (!a.sigmoid && norm64 == 0.0) norm64 = softmax_norm64<LPR, V>(row, ln, mx);
+      // held picks by their 64-bit values; lane p's two are picks p and p + LPR
+      auto value64 = [&](int e) -> double {
+        return e < 0 ? -INFINITY : score64(usable(row[e]), a.sigmoid, mx, norm64) + (double)a.bias[e];
+      };
+      const double c0 = value64(picked), c1 = extra >= 0 ? value64(extra) : -INFINITY;
+      int rank0 = 0, rank1 = 0;
+      const int most = __reduce_max_sync(kAll, held);
+      for (int q = 0; q < most; ++q) {
+        const int from = slot * LPR + q % LPR;
+        const double oc0 = __shfl_sync(kAll, c0, from), oc1 = __shfl_sync(kAll, c1, from);
+        const int oe0 = __shfl_sync(kAll, picked, from), oe1 = __shfl_sync(kAll, extra, from);
+        const double oc = q < LPR ? oc0 : oc1;
+        const int oe = q < LPR ? oe0 : oe1;
+        if (oe >= 0 && (oc > c0 || (oc == c0 && oe < picked))) ++rank0;
+        if (oe >= 0 && (oc > c1 || (oc == c1 && oe < extra))) ++rank1;
+      }
+      int sorted = -1;
+      for (int q = 0; q < most; ++q) {
+        const int from = slot * LPR + q % LPR;
+        const int r0 = __shfl_sync(kAll, rank0, from), r1 = __shfl_sync(kAll, rank1, from);
+        const int oe0 = __shfl_sync(kAll, picked, from), oe1 = __shfl_sync(kAll, extra, from);
+        const int r = q < LPR ? r0 : r1, oe = q < LPR ? oe0 : oe1;
+        if (oe >= 0 && r == p) sorted = oe;
+      }
+      if (near) picked = sorted;
+      // more near ties than the lanes hold: the whole row in 64 bits
+      unsigned open = __ballot_sync(kAll, more && active && p == 0);
+      while (open) {
+        const int src = __ffs(open) - 1;
+        open &= open - 1;
+        const long long tt = __shfl_sync(kAll, t, src);
+        double* cache = a.E <= V * 16 ? reinterpret_cast<double*>(st) : nullptr;
+        const int e = choose_exact<T>(static_cast<const T*>(a.logits) + tt * a.E, a, lane, cache);
+        const int ep = __shfl_sync(kAll, e, p);
+        if (slot == src / LPR) picked = p < a.k ? ep : -1;
+      }
+    }
+    if (p >= a.k) picked = -1;
+    // without a bias the value that was compared is the logit
+    const float l = picked < 0 ? -INFINITY : by_bias ? usable(row[picked]) : fminf(value, FLT_MAX);
+    float w;
+    if (a.renorm) {
+      float total;
+      w = seg_ratio<LPR>(l, a.sigmoid, total);
+      w = total > 0.f ? a.scale * (w / total) : 0.f;
+    } else {
+      w = picked < 0 ? 0.f : a.scale * (a.sigmoid ? sigmoid_f(l) : expf(l - mx) * inv);
+    }
+    if (active && p < a.k) {
+      a.expert_idx[t * a.k + p] = picked;
+      a.weight[t * a.k + p] = w;
+      if (a.load && picked >= 0) atomicAdd(a.load + (long long)blockIdx.y * a.E + picked, 1);
+    }
+  }
+
+  if (MEAN) {                                  // the block's sum: warps in order, within each the tokens side by side
+    if (!ACC_SMEM) {
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < V; i += 4)
+        *reinterpret_cast<float4*>(st + (i / 4 * 32 + lane) * 4) =
+            make_float4(acc[ACC_SMEM ? 0 : i], acc[ACC_SMEM ? 1 : i + 1], acc[ACC_SMEM ? 2 : i + 2], acc[ACC_SMEM ? 3 : i + 3]);
+    }
+    const float* all = route_smem + (ACC_SMEM ? kRouteWarps * V * 32 : 0);
+    __syncthreads();
+    const float scale = gridDim.x == 1 ? 1.f / (float)a.S : 1.f;       // a single tile is the mean already
+    float* out = sums + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * a.E;
+    for (int c = threadIdx.x; c < V * LPR; c += kRouteThreads) {
+      const int i = c / (LPR * 4) * 4 + c % 4, pp = c / 4 % LPR;
+      RouteLane<W> o = ln;
+      o.q = pp % o.P; o.base = pp / o.P * o.size;
+      if (o.offset(i) < o.size) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < kRouteWarps; ++w)
+#pragma unroll
+          for (int r = 0; r < RPW; ++r) s += all[w * V * 32 + (i / 4 * 32 + r * LPR + pp) * 4 + i % 4];
+        out[o.expert(i)] = s * scale;
+      }
+    }
+  }
+}
+
+// Gradient (see route_bwd_kernel for the formulas).
+template <typename T, int W, int LPR, int V>
+__global__ void __launch_bounds__(kRouteThreads) route_bwd_fast_kernel(const RouteGradArgs a) {
+  constexpr int RPW = 32 / LPR;
+  const int lane = threadIdx.x & 31;
+  const int slot = lane / LPR, p = lane % LPR;
+  const RouteLane<W> ln{0, p, LPR, a.E};
+  const bool soft_stats = !a.sigmoid && (a.dm || !a.renorm);
+  const bool dense = soft_stats || a.dm;
+  const float inv_s = 1.f / (float)a.S;
+  const long long step = (long long)gridDim.x * kRouteWarps * RPW;
+  for (long long b0 = ((long long)blockIdx.x * kRouteWarps + (threadIdx.x >> 5)) * RPW; b0 < a.n; b0 += step) {
+    const bool active = b0 + slot < a.n;
+    const long long t = active ? b0 + slot : a.n - 1;
+    const T* row = static_cast<const T*>(a.logits) + t * a.E;
+    T* out = static_cast<T*>(a.dlogits) + t * a.E;
+    const float* dm = a.dm ? a.dm + t / a.S * a.E : nullptr;
+    int e = -1;
+    float l = -INFINITY, dw = 0.f;
+    if (p < a.k) {
+      e = a.expert_idx[t * a.k + p];
+      if (e < 0 || e >= a.E) e = -1;
+      if (e >= 0) { l = usable(row[e]); dw = a.dweight[t * a.k + p]; }
+      if (l == -INFINITY) e = -1;
+    }
+    float v[V];
+    float mx = 0.f, inv = 0.f;
+    if (dense) {
+      load_logits<T, W, V>(row, ln, a.E == V * LPR, v);
+      clean<V>(v);
+      if (soft_stats) {
+        mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < V; ++i) mx = fmaxf(mx, v[i]);
+        mx = seg_max<LPR>(mx);
+        if (mx == -INFINITY) mx = 0.f;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) { v[i] = exp2_approx((v[i] - mx) * kLog2e); sum += v[i]; }
+        sum = seg_sum<LPR>(sum);
+        inv = sum > 0.f ? 1.f / sum : 0.f;
+      }
+    }
+    float add = 0.f;
+    if (a.renorm) {
+      float total;
+      const float r = seg_ratio<LPR>(l, a.sigmoid, total);
+      const float w = total > 0.f ? r / total : 0.f;
+      const float D = seg_sum<LPR>(e >= 0 ? w * dw : 0.f);
+      add = e >= 0 ? a.scale * w * (dw - D) : 0.f;
+      if (a.sigmoid && e >= 0) add /= 1.f + expf(l);
+    } else if (e >= 0) {
+      const float s = a.sigmoid ? sigmoid_f(l) : expf(l - mx) * inv;
+      add = a.scale * dw * s;
+      if (a.sigmoid) add /= 1.f + expf(l);
+    }
+    float dot = 0.f;
+    if (soft_stats) {
+      if (dm) {
+#pragma unroll
+        for (int j = 0; j < V / W; ++j) {
+          const int off = (j * LPR + p) * W;
+          if (off < a.E) {
+            constexpr int C = W < 4 ? W : 4;
+            float d[W];
+#pragma unroll
+            for (int w = 0; w < W; w += C) load_pack<float, C>(dm + off + w, d + w);
+#pragma unroll
+            for (int w = 0; w < W; ++w) dot = fmaf(v[j * W + w], d[w], dot);
+          }
+        }
+        dot *= inv * inv_s;
+      }
+      dot = seg_sum<LPR>(dot + (a.renorm ? 0.f : add));
+    }
+    float sum = add;
+    bool writes = e >= 0;
+    for (int j = 0; j < a.k; ++j) {              // entries that name the same expert add up; the first of them writes
+      const int oe = __shfl_sync(kAll, e, slot * LPR + j);
+      const float oa = __shfl_sync(kAll, add, slot * LPR + j);
+      if (j != p && oe == e && e >= 0) { sum += oa; if (j < p) writes = false; }
+    }
+    if (writes && dense) {
+      const float d = dm ? dm[e] * inv_s : 0.f;
+      if (a.sigmoid) sum += d * sigmoid_f(l) / (1.f + expf(l));
+      else sum += expf(l - mx) * inv * (d - dot);
+    }
+#pragma unroll
+    for (int j = 0; j < V / W; ++j) {
+      const int off = (j * LPR + p) * W;
+      if (active && off < a.E) {
+        float o[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) o[w] = 0.f;
+        if (dense) {
+          constexpr int C = W < 4 ? W : 4;
+          float d[W];
+#pragma unroll
+          for (int w = 0; w < W; ++w) d[w] = 0.f;
+          if (dm) {
+#pragma unroll
+            for (int w = 0; w < W; w += C) load_pack<float, C>(dm + off + w, d + w);
+          }
+#pragma unroll
+          for (int w = 0; w < W; ++w) {
+            const float x = v[j * W + w];
+            if (a.sigmoid) { const float s = sigmoid_fast(x); o[w] = d[w] * inv_s * s * (1.f - s); }
+            else o[w] = x * inv * (d[w] * inv_s - dot);
+          }
+        }
+        store_pack<T, W>(out + off, o);
+      }
+    }
+    __syncwarp();
+    if (writes && active) out[e] = from_f32<T>(sum);
+  }
+}
+
+template <typename T, int W, int LPR, int V, bool BIASED, bool MEAN>
+bool launch_fwd_m(const RouteArgs& a, int G, float* sums, cudaStream_t st) {
+  constexpr int regions = MEAN && V == 64 ? 2 : 1;
+  constexpr int smem = regions * kRouteWarps * V * 32 * (int)sizeof(float);
+  auto kern = route_fwd_fast_kernel<T, W, LPR, V, BIASED, MEAN>;
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  kern<<<dim3(ceil_div(a.S, kRouteTile), G), kRouteThreads, smem, st>>>(a, sums);
+  count_launch();
+  return true;
+}
+template <typename T, int W, int LPR, int V>
+bool launch_fwd(const RouteArgs& a, int G, float* sums, cudaStream_t st) {
+  const bool biased = a.bias || (a.groups > 1 && a.group_top == 2);
+  return biased ? (sums ? launch_fwd_m<T, W, LPR, V, true, true>(a, G, sums, st) : launch_fwd_m<T, W, LPR, V, true, false>(a, G, sums, st))
+                : (sums ? launch_fwd_m<T, W, LPR, V, false, true>(a, G, sums, st) : launch_fwd_m<T, W, LPR, V, false, false>(a, G, sums, st));
+}
+template <typename T, int W, int LPR, int V>
+void launch_bwd(const RouteGradArgs& a, cudaStream_t st) {
+  const long long blocks = (a.n + kRouteWarps * (32 / LPR) - 1) / (kRouteWarps * (32 / LPR));
+  const int grid = (int)std::min<long long>(blocks, (long long)device_sms() * 64);
+  route_bwd_fast_kernel<T, W, LPR, V><<<grid, kRouteThreads, 0, st>>>(a);
+  count_launch();
+}
+
+// Values per lane (8, 16, 32 or 64) and lanes per token for E experts in `groups` groups; 0 = these kernels do
+// not apply (more than 64 values per lane, or groups that lanes cannot share evenly).
+struct RouteFit { int lpr, v; };
+template <typename T>
+RouteFit route_fit(int E, int groups, int k, long long n, int w) {
+  RouteFit f{0, 0};
+  if (groups & (groups - 1)) return f;
+  for (int lpr : {8, 32}) {
+    // few tokens: a token's latency counts, and a whole warp has it done sooner
+    if (lpr == 8 && (groups > 8 || k > 8 || n < 148 * 16 || w == 1)) continue;
+    const int per = lpr / groups * w;
+    const int v = (E / groups + per - 1) / per * w;
+    if (v > 64) continue;
+    f.lpr = lpr; f.v = v <= 8 ? 8 : v <= 16 ? 16 : v <= 32 ? 32 : 64;
+    break;
+  }
+  return f;
+}
+
+#define GSHARD_ROUTE_V(FN, LPR, W, ...)                                  \
+  (f.v == 8 ? FN<T, W, LPR, 8>(__VA_ARGS__) : f.v == 16 ? FN<T, W, LPR, 16>(__VA_ARGS__) \
+   : f.v == 32 ? FN<T, W, LPR, 32>(__VA_ARGS__) : FN<T, W, LPR, 64>(__VA_ARGS__))
+
+}  // namespace
+
+// sums: partial rows of the mean scores [G][tiles][E] (m itself where there is one tile), or nullptr.
+// false = no kernel here fits the shape.
+template <typename T>
+bool launch_route_fwd_fast(const RouteArgs& a, int G, float* sums, cudaStream_t st) {
+  constexpr int WF = 16 / (int)sizeof(T);
+  const bool whole = a.E / a.groups % WF == 0;             // groups and rows in whole 16-byte words
+  const RouteFit f = route_fit<T>(a.E, a.groups, a.k, a.n, whole ? WF : 1);
+  if (!f.lpr) return false;
+  if (!whole) return f.v <= 16 ? launch_fwd<T, 1, 32, 16>(a, G, sums, st) : launch_fwd<T, 1, 32, 64>(a, G, sums, st);
+  if (f.lpr == 8) return GSHARD_ROUTE_V(launch_fwd, 8, WF, a, G, sums, st);
+  return GSHARD_ROUTE_V(launch_fwd, 32, WF, a, G, sums, st);
+}
+
+template <typename T>
+bool launch_route_bwd_fast(const RouteGradArgs& a, cudaStream_t st) {
+  constexpr int WF = 16 / (int)sizeof(T);
+  const bool whole = a.E % WF == 0;
+  const RouteFit f = route_fit<T>(a.E, 1, a.k, a.n, whole ? WF : 1);
+  if (!f.lpr) return false;
+  if (!whole) f.v <= 16 ? launch_bwd<T, 1, 32, 16>(a, st) : launch_bwd<T, 1, 32, 64>(a, st);
+  else if (f.lpr == 8) GSHARD_ROUTE_V(launch_bwd, 8, WF, a, st);
+  else GSHARD_ROUTE_V(launch_bwd, 32, WF, a, st);
+  return true;
+}
+
+}  // namespace gshard
