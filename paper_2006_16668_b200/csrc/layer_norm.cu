@@ -34,7 +34,7 @@ __device__ __forceinline__ void load_param(const float* p, float* f) {
 }
 
 // Sums of K values over the team.  A team of one warp stays inside the warp; a larger team is the whole
-// block.  `buf` holds 32 * K floats and is reused by the next call: callers alternate two of them.
+// block.  `buf` holds 32 * K floats and is reused by the call after next: callers alternate two of them.
 template <int K>
 __device__ __forceinline__ void team_sum(float (&s)[K], float* buf) {
 #pragma unroll
@@ -45,55 +45,84 @@ __device__ __forceinline__ void team_sum(float (&s)[K], float* buf) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     if (lane == 0)
 #pragma unroll
-      for (int k = 0; k < K; ++k) buf[k * 32 + warp] = s[k];
+      for (int k = 0; k < K; ++k) buf[warp * K + k] = s[k];
     __syncthreads();
+    // every thread adds the warps' sums in the same order, in two strands
+    float odd[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      float t = lane < warps ? buf[k * 32 + lane] : 0.f;
+    for (int k = 0; k < K; ++k) { s[k] = buf[k]; odd[k] = 0.f; }
+    for (int w = 1; w < warps; w += 2) {
 #pragma unroll
-      for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
-      s[k] = t;
+      for (int k = 0; k < K; ++k) {
+        odd[k] += buf[w * K + k];
+        if (w + 1 < warps) s[k] += buf[(w + 1) * K + k];
+      }
     }
+#pragma unroll
+    for (int k = 0; k < K; ++k) s[k] += odd[k];
   }
 }
 
-// NT: threads of the block at most (256: one-warp teams, else one team of the whole block).
-template <typename T, int W, int VPT, int NT>
-__global__ void __launch_bounds__(NT) ln_fwd_kernel(const T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ beta,
-                              T* y, float* __restrict__ mean, float* __restrict__ rstd, long long n, int M, float eps) {
+// The row's values stay in registers in fp32.  AHEAD: the grid is resident, and the next row is loaded (packed)
+// while the current one is worked on; up to 16 values per thread, a thread also keeps its columns' gamma and beta in
+// registers over all its rows.  WHOLE: the row fills the team's packs exactly, which saves a third of the
+// instructions (selects and branches per element).
+template <typename T, int W, int VPT, int NT, int MINB, bool AHEAD, bool WHOLE>
+__global__ void __launch_bounds__(NT, MINB) ln_fwd_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
+                                                          const float* __restrict__ beta, T* y, float* __restrict__ mean,
+                                                          float* __restrict__ rstd, long long n, int M, float eps) {
+  constexpr int NV = W * VPT;
   __shared__ float buf[2][32];
+  constexpr bool whole = WHOLE, KEEP = AHEAD && NV <= 16;
   const int packs = M / W;
   const float inv_m = 1.f / (float)M;
-  for (long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y; row < n; row += (long long)gridDim.x * blockDim.y) {
-    const T* xr = x + row * M;
-    float v[VPT][W];
-    float s[1] = {0.f};
+  const long long stride = (long long)gridDim.x * blockDim.y;
+  Pack<T, W> raw[VPT];
+  auto fetch = [&](long long row) {
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int p = i * blockDim.x + threadIdx.x;
-      if (p < packs) {
-        load_pack<T, W>(xr + (long long)p * W, v[i]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < W; ++j) v[i][j] = 0.f;
-      }
+      if (whole || p < packs) raw[i].load_once(x + row * M + p * W);
     }
+  };
+  float gm[NV], bt[NV];
+  auto params = [&](int i) {
+    const int p = i * blockDim.x + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i)
+    for (int j = 0; j < W; ++j) gm[i * W + j] = bt[i * W + j] = 0.f;
+    if (whole || p < packs) {
+      load_param<W>(gamma + p * W, gm + i * W);
+      if (beta) load_param<W>(beta + p * W, bt + i * W);
+    }
+  };
+  if (KEEP) {
 #pragma unroll
-      for (int j = 0; j < W; ++j) s[0] += v[i][j];
+    for (int i = 0; i < VPT; ++i) params(i);
+  }
+  long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  if (AHEAD && row < n) fetch(row);
+  for (; row < n; row += stride) {
+    if (!AHEAD) fetch(row);
+    float v[NV], a[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      v[j] = whole || j / W * (int)blockDim.x + (int)threadIdx.x < packs ? raw[j / W].get(j % W) : 0.f;
+      a[j & 1] += v[j];
+    }
+    if (AHEAD && row + stride < n) fetch(row + stride);
+    float s[1] = {a[0] + a[1]};
     team_sum<1>(s, buf[0]);
     const float mu = s[0] * inv_m;
-    float q[1] = {0.f};
+    a[0] = a[1] = 0.f;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      if (i * (int)blockDim.x + (int)threadIdx.x < packs) {
-#pragma unroll
-        for (int j = 0; j < W; ++j) { v[i][j] -= mu; q[0] = fmaf(v[i][j], v[i][j], q[0]); }
-      }
+    for (int j = 0; j < NV; ++j) {
+      v[j] -= mu;
+      if (!whole && j / W * (int)blockDim.x + (int)threadIdx.x >= packs) v[j] = 0.f;     // padding stays out of the variance
+      a[j & 1] = fmaf(v[j], v[j], a[j & 1]);
     }
-    team_sum<1>(q, buf[1]);
-    const float r = 1.f / sqrtf(q[0] * inv_m + eps);
+    s[0] = a[0] + a[1];
+    team_sum<1>(s, buf[1]);
+    const float r = 1.f / sqrtf(s[0] * inv_m + eps);
     if (threadIdx.x == 0) {
       if (mean) mean[row] = mu;
       if (rstd) rstd[row] = r;
@@ -102,18 +131,12 @@ __global__ void __launch_bounds__(NT) ln_fwd_kernel(const T* __restrict__ x, con
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int p = i * blockDim.x + threadIdx.x;
-      if (p < packs) {
-        float gm[W], o[W];
-        load_param<W>(gamma + (long long)p * W, gm);
+      if (!KEEP) params(i);
+      if (whole || p < packs) {
+        float o[W];
 #pragma unroll
-        for (int j = 0; j < W; ++j) o[j] = v[i][j] * r * gm[j];
-        if (beta) {
-          float bt[W];
-          load_param<W>(beta + (long long)p * W, bt);
-#pragma unroll
-          for (int j = 0; j < W; ++j) o[j] += bt[j];
-        }
-        store_pack<T, W>(yr + (long long)p * W, o);
+        for (int j = 0; j < W; ++j) o[j] = fmaf(v[i * W + j] * r, gm[i * W + j], bt[i * W + j]);
+        store_pack<T, W>(yr + p * W, o);
       }
     }
   }
@@ -121,98 +144,138 @@ __global__ void __launch_bounds__(NT) ln_fwd_kernel(const T* __restrict__ x, con
 
 // Block b's share of the weight gradients goes to partial[b][0..M) (dgamma) and partial[b][M..2M) (dbeta).
 // A thread's columns are summed in registers, or (SUMS_IN_SMEM, rows beyond 8192 elements, where the
-// register file does not hold a row and its sums) in its own words of shared memory.
-template <typename T, int W, int VPT, int NT, bool SUMS_IN_SMEM>
-__global__ void __launch_bounds__(NT) ln_bwd_kernel(const T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ mean,
-                              const float* __restrict__ rstd, const T* dy, const T* dskip, T* dx, float* __restrict__ partial,
-                              long long n, int M) {
+// register file does not hold a row and its sums) in its own words of shared memory.  AHEAD: a team's next row
+// is loaded while it works on the current one.  WHOLE: the row fills the team's packs exactly.
+template <typename T, int W, int VPT, int NT, int MINB, bool AHEAD, bool SUMS_IN_SMEM, bool WHOLE>
+__global__ void __launch_bounds__(NT, MINB) ln_bwd_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
+                                                    const float* __restrict__ mean, const float* __restrict__ rstd, const T* dy,
+                                                    const T* dskip, T* dx, float* __restrict__ partial, long long n, int M) {
+  constexpr int NV = W * VPT;
   extern __shared__ float sums[];              // 2 M floats: several teams in the block, or SUMS_IN_SMEM
   __shared__ float buf[2][64];
+  constexpr bool whole = WHOLE;
   const int packs = M / W;
   const float inv_m = 1.f / (float)M;
-  float ag[SUMS_IN_SMEM ? 1 : VPT][W], ab[SUMS_IN_SMEM ? 1 : VPT][W];
+  f32x2 ag[SUMS_IN_SMEM ? 1 : NV / 2], ab[SUMS_IN_SMEM ? 1 : NV / 2];
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int p = i * blockDim.x + threadIdx.x;
-#pragma unroll
-    for (int j = 0; j < W; ++j) {
-      if (!SUMS_IN_SMEM) { ag[i][j] = 0.f; ab[i][j] = 0.f; }
-      else if (partial && p < packs) { sums[j * packs + p] = 0.f; sums[M + j * packs + p] = 0.f; }
-    }
+  for (int j = 0; j < NV; ++j) {
+    const int p = j / W * blockDim.x + threadIdx.x;
+    if (!SUMS_IN_SMEM) { ag[SUMS_IN_SMEM ? 0 : j / 2] = both(0.f); ab[SUMS_IN_SMEM ? 0 : j / 2] = both(0.f); }
+    else if (partial && p < packs) { sums[j % W * packs + p] = 0.f; sums[M + j % W * packs + p] = 0.f; }
   }
   int flip = 0;
-  for (long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y; row < n; row += (long long)gridDim.x * blockDim.y) {
-    const T* xr = x + row * M;
-    const T* dyr = dy + row * M;
-    const float mu = mean[row], r = rstd[row];
-    float z[VPT][W], g[VPT][W];
-    float s[2] = {0.f, 0.f};
+  const long long stride = (long long)gridDim.x * blockDim.y;
+  Pack<T, W> vx[VPT], vd[VPT], vk[VPT];
+  float mu = 0.f, rs = 0.f;
+  auto fetch = [&](long long row, bool skip_too) {
+    mu = mean[row]; rs = rstd[row];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int p = i * blockDim.x + threadIdx.x;
-      if (p < packs) {
-        load_pack<T, W>(xr + (long long)p * W, z[i]);
-        load_pack<T, W>(dyr + (long long)p * W, g[i]);
+      const long long at = row * M + p * W;
+      if (whole || p < packs) {
+        vx[i].load_once(x + at);
+        vd[i].load_once(dy + at);
+        if (skip_too) vk[i].load_once(dskip + at);
       }
     }
+  };
+  long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  if (AHEAD && row < n) fetch(row, false);
+  for (; row < n; row += stride) {
+    if (!AHEAD) fetch(row, dskip != nullptr);
+    f32x2 z[NV / 2], g[NV / 2];
+    const float m = mu, r = rs;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int p = i * blockDim.x + threadIdx.x;
-      if (p < packs) {
-        float gm[W];
-        load_param<W>(gamma + (long long)p * W, gm);
+    for (int j = 0; j < NV; j += 2) {
+      const bool in0 = whole || j / W * (int)blockDim.x + (int)threadIdx.x < packs;
+      const bool in1 = whole || (j + 1) / W * (int)blockDim.x + (int)threadIdx.x < packs;
+      const f32x2 xx = pair(in0 ? vx[j / W].get(j % W) : m, in1 ? vx[(j + 1) / W].get((j + 1) % W) : m);
+      z[j / 2] = mul2(add2(xx, both(-m)), both(r));
+      g[j / 2] = pair(in0 ? vd[j / W].get(j % W) : 0.f, in1 ? vd[(j + 1) / W].get((j + 1) % W) : 0.f);
+    }
+    if (AHEAD) {
+      if (dskip) {                               // used last: loaded now, for this row
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-          z[i][j] = (z[i][j] - mu) * r;
-          if (SUMS_IN_SMEM) {
-            if (partial) {
-              sums[j * packs + p] = fmaf(g[i][j], z[i][j], sums[j * packs + p]);
-              sums[M + j * packs + p] += g[i][j];
-            }
-          } else {
-            ab[i][j] += g[i][j];
-            ag[i][j] = fmaf(g[i][j], z[i][j], ag[i][j]);
-          }
-          g[i][j] *= gm[j];
-          s[0] += g[i][j];
-          s[1] = fmaf(g[i][j], z[i][j], s[1]);
+        for (int i = 0; i < VPT; ++i) {
+          const int p = i * blockDim.x + threadIdx.x;
+          if (whole || p < packs) vk[i].load_once(dskip + row * M + p * W);
         }
       }
+      if (row + stride < n) fetch(row + stride, false);
     }
+    f32x2 s0 = both(0.f), s1 = both(0.f);
+    float gm[NV];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int p = i * blockDim.x + threadIdx.x;
+#pragma unroll
+      for (int j = 0; j < W; ++j) gm[i * W + j] = 0.f;
+      if (whole || p < packs) load_param<W>(gamma + p * W, gm + i * W);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; j += 2) {
+      const f32x2 zz = z[j / 2], d = g[j / 2];
+      if (SUMS_IN_SMEM) {
+        if (partial) {
+          const float2 zf = unpair(zz), df = unpair(d);
+          const int p0 = j / W * blockDim.x + threadIdx.x, p1 = (j + 1) / W * blockDim.x + threadIdx.x;
+          if (p0 < packs) {
+            sums[j % W * packs + p0] = fmaf(df.x, zf.x, sums[j % W * packs + p0]);
+            sums[M + j % W * packs + p0] += df.x;
+          }
+          if (p1 < packs) {
+            sums[(j + 1) % W * packs + p1] = fmaf(df.y, zf.y, sums[(j + 1) % W * packs + p1]);
+            sums[M + (j + 1) % W * packs + p1] += df.y;
+          }
+        }
+      } else {
+        ag[SUMS_IN_SMEM ? 0 : j / 2] = fma2(d, zz, ag[SUMS_IN_SMEM ? 0 : j / 2]);
+        ab[SUMS_IN_SMEM ? 0 : j / 2] = add2(d, ab[SUMS_IN_SMEM ? 0 : j / 2]);
+      }
+      g[j / 2] = mul2(d, pair(gm[j], gm[j + 1]));
+      s0 = add2(s0, g[j / 2]);
+      s1 = fma2(g[j / 2], zz, s1);
+    }
+    const float2 t0 = unpair(s0), t1 = unpair(s1);
+    float s[2] = {t0.x + t0.y, t1.x + t1.y};
     team_sum<2>(s, buf[flip]);
     flip ^= 1;
-    const float c0 = s[0] * inv_m, c1 = s[1] * inv_m;
-    T* dxr = dx + row * M;
+    const float c0 = -s[0] * inv_m, c1 = -s[1] * inv_m;
+    float dxv[NV];
+#pragma unroll
+    for (int j = 0; j < NV; j += 2) {
+      const f32x2 t = add2(fma2(z[j / 2], both(c1), g[j / 2]), both(c0));
+      const f32x2 k = dskip ? pair(vk[j / W].get(j % W), vk[(j + 1) / W].get((j + 1) % W)) : both(0.f);
+      const float2 o = unpair(fma2(t, both(r), k));
+      dxv[j] = o.x; dxv[j + 1] = o.y;
+    }
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int p = i * blockDim.x + threadIdx.x;
-      if (p < packs) {
-        float o[W];
-#pragma unroll
-        for (int j = 0; j < W; ++j) o[j] = r * (g[i][j] - c0 - z[i][j] * c1);
-        if (dskip) {
-          float k[W];
-          load_pack<T, W>(dskip + row * M + (long long)p * W, k);
-#pragma unroll
-          for (int j = 0; j < W; ++j) o[j] += k[j];
-        }
-        store_pack<T, W>(dxr + (long long)p * W, o);
-      }
+      if (whole || p < packs) store_pack<T, W>(dx + row * M + p * W, dxv + i * W);
     }
   }
   if (!partial) return;
   float* out = partial + (long long)blockIdx.x * 2 * M;
-  if (SUMS_IN_SMEM || blockDim.y == 1) {                 // one team in the block
+  float fg[NV], fb[NV];                          // this thread's sums, element by element
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int p = i * blockDim.x + threadIdx.x;
-      if (p < packs) {
+  for (int j = 0; j < NV; ++j) {
+    const int p = j / W * blockDim.x + threadIdx.x;
+    if (SUMS_IN_SMEM) {
+      fg[j] = p < packs ? sums[j % W * packs + p] : 0.f;
+      fb[j] = p < packs ? sums[M + j % W * packs + p] : 0.f;
+    } else {
+      const float2 u = unpair(ag[SUMS_IN_SMEM ? 0 : j / 2]), w = unpair(ab[SUMS_IN_SMEM ? 0 : j / 2]);
+      fg[j] = j & 1 ? u.y : u.x;
+      fb[j] = j & 1 ? w.y : w.x;
+    }
+  }
+  if (SUMS_IN_SMEM || blockDim.y == 1) {         // one team in the block
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-          out[p * W + j] = SUMS_IN_SMEM ? sums[j * packs + p] : ag[SUMS_IN_SMEM ? 0 : i][j];
-          out[M + p * W + j] = SUMS_IN_SMEM ? sums[M + j * packs + p] : ab[SUMS_IN_SMEM ? 0 : i][j];
-        }
-      }
+    for (int j = 0; j < NV; ++j) {
+      const int p = j / W * blockDim.x + threadIdx.x;
+      if (p < packs) { out[p * W + j % W] = fg[j]; out[M + p * W + j % W] = fb[j]; }
     }
     return;
   }
@@ -220,14 +283,12 @@ __global__ void __launch_bounds__(NT) ln_bwd_kernel(const T* __restrict__ x, con
     for (int t = 0; t < (int)blockDim.y; ++t) {          // the block's teams add up in order
       if ((int)threadIdx.y == t) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-          const int p = i * blockDim.x + threadIdx.x;
+        for (int j = 0; j < NV; ++j) {
+          const int p = j / W * blockDim.x + threadIdx.x;
           if (p < packs) {
-#pragma unroll
-            for (int j = 0; j < W; ++j) {
-              sums[p * W + j] = (t ? sums[p * W + j] : 0.f) + ag[i][j];
-              sums[M + p * W + j] = (t ? sums[M + p * W + j] : 0.f) + ab[i][j];
-            }
+            const int c = p * W + j % W;
+            sums[c] = (t ? sums[c] : 0.f) + fg[j];
+            sums[M + c] = (t ? sums[M + c] : 0.f) + fb[j];
           }
         }
       }
@@ -237,23 +298,32 @@ __global__ void __launch_bounds__(NT) ln_bwd_kernel(const T* __restrict__ x, con
   }
 }
 
-// dgamma / dbeta = sum over the partial rows, in order within each of 32 interleaved strands.
-__global__ void __launch_bounds__(1024) ln_bwd_finish_kernel(const float* __restrict__ partial, int rows, int M,
-                                                             float* __restrict__ dgamma, float* __restrict__ dbeta) {
-  __shared__ float part[32][33];
-  const int c = blockIdx.x * 32 + threadIdx.x;        // column of [dgamma | dbeta]
-  float s = 0.f;
-  if (c < 2 * M)
-    for (int b = threadIdx.y; b < rows; b += 32) s += partial[(long long)b * 2 * M + c];
-  part[threadIdx.y][threadIdx.x] = s;
+// dgamma / dbeta = sum over the partial rows: 32 strands of rows in order, then the strands.  8 columns per
+// block, so that the pass spreads over the multiprocessors.
+__global__ void __launch_bounds__(256) ln_bwd_finish_kernel(const float* __restrict__ partial, int rows, int M,
+                                                            float* __restrict__ dgamma, float* __restrict__ dbeta) {
+  __shared__ float part[32][9];
+  const int cx = threadIdx.x & 7, strand = threadIdx.x >> 3;
+  const int c = blockIdx.x * 8 + cx;                  // column of [dgamma | dbeta]
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c < 2 * M) {
+    const float* p = partial + c;
+    int b = strand;
+    for (; b + 96 < rows; b += 128)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[k] += p[(long long)(b + 32 * k) * 2 * M];
+    for (; b < rows; b += 32) s[0] += p[(long long)b * 2 * M];
+  }
+  part[strand][cx] = (s[0] + s[1]) + (s[2] + s[3]);
   __syncthreads();
-  float t = part[threadIdx.x][threadIdx.y];           // strand threadIdx.x of column threadIdx.y
+  const int col = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float t = part[lane][col];
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
-  const int col = blockIdx.x * 32 + threadIdx.y;
-  if (threadIdx.x == 0 && col < 2 * M) {
-    if (col < M) { if (dgamma) dgamma[col] = t; }
-    else if (dbeta) dbeta[col - M] = t;
+  const int g = blockIdx.x * 8 + col;
+  if (lane == 0 && g < 2 * M) {
+    if (g < M) { if (dgamma) dgamma[g] = t; }
+    else if (dbeta) dbeta[g - M] = t;
   }
 }
 
@@ -264,46 +334,58 @@ int ln_width(int M, int esize) {
   return w;
 }
 
-struct LnShape { int team, teams, nv; };   // threads per row, rows per block, values per thread
+struct LnShape { int team, teams, nv; };   // threads per row, rows side by side in a block, values per thread
 
-// Rows of at most 1024 elements, and many of them: one warp per row, which needs no block barrier, and 8, 16
-// or 32 values per thread, eight rows per block.  Otherwise a block per row with 8 values per thread (16
-// beyond 8192 elements).
-LnShape ln_shape(long long n, int M) {
-  LnShape s;
-  if (M <= 1024 && (n >= kLnSms * 8 || M <= 256)) {
-    s.nv = M <= 256 ? 8 : M <= 512 ? 16 : 32;
-    s.team = 32;
-    s.teams = 8;
-  } else {
-    s.nv = M <= 8192 ? 8 : 16;
-    s.team = 32 * ceil_div(M, 32 * s.nv);
-    s.teams = 1;
+// Forward: one warp per row up to 1024 elements, with 8, 16 or 32 values per thread and no barrier; else a block
+// per row with 16 (8 for few rows, where the latency of one row counts).
+LnShape ln_fwd_shape(long long n, int M) {
+  if (M <= 256) return {32, n < kLnSms * 8 ? 1 : 4, 8};
+  if (n < kLnSms * 4) {
+    const int nv = M <= 8192 ? 8 : 16;
+    return {32 * ceil_div(M, 32 * nv), 1, nv};
   }
-  return s;
+  if (M <= 1024) return {32, 4, M <= 512 ? 16 : 32};
+  return {32 * ceil_div(M, 512), 1, 16};
 }
-
-int ln_bwd_blocks(long long n, const LnShape& s) {
-  const int per_sm = s.teams > 1 ? 2 : std::max(1, std::min(8, 1024 / s.team));
-  const long long blocks = (n + s.teams - 1) / s.teams;
-  return (int)std::min<long long>(blocks, (long long)kLnSms * per_sm);
+// Backward: a thread also holds its columns' sums and its next row, so 16 values (8 of fp32, whose next row
+// waits unpacked) per thread while that fits the registers.
+LnShape ln_bwd_shape(int M, int esize) {
+  if (M <= 256) return {32, 4, 8};
+  const int nv = esize == 2 && M <= 8192 ? 16 : M <= 8192 ? 8 : 16;
+  return {32 * ceil_div(M, 32 * nv), 1, nv};
+}
+// The backward's grid, resident as a whole: 512 threads of a multiprocessor at 128 registers each, 640 at 96.
+int ln_bwd_blocks(long long n, int M, int esize) {
+  const LnShape s = ln_bwd_shape(M, esize);
+  const int per_sm = std::max(1, (s.nv == 16 ? 512 : 640) / (s.team * s.teams));
+  return (int)std::min<long long>((n + s.teams - 1) / s.teams, (long long)kLnSms * per_sm);
 }
 
 template <typename T, int W>
 int ln_fwd_launch(long long n, int M, float eps, const T* x, const float* gamma, const float* beta, T* y, float* mean,
                   float* rstd, cudaStream_t st) {
-  const LnShape s = ln_shape(n, M);
+  const LnShape s = ln_fwd_shape(n, M);
   const dim3 block(s.team, s.teams);
-  const int grid = (int)std::min<long long>((n + s.teams - 1) / s.teams, 1ll << 30);
-#define GSHARD_LN(NV, NT) ln_fwd_kernel<T, W, NV / W, NT><<<grid, block, 0, st>>>(x, gamma, beta, y, mean, rstd, n, M, eps)
-  if (s.teams > 1) {
-    if (s.nv == 32) GSHARD_LN(32, 256);
-    else if (s.nv == 16) GSHARD_LN(16, 256);
-    else GSHARD_LN(8, 256);
-  } else {
-    if (s.nv == 16) GSHARD_LN(16, 1024);
-    else GSHARD_LN(8, 1024);
-  }
+  const long long all = (n + s.teams - 1) / s.teams;
+  const int threads = s.team * s.teams;
+  const bool ahead = threads <= 768 && s.nv < 32 && all > kLnSms * 4;
+  const int grid = (int)std::min<long long>(all, ahead ? kLnSms * std::max(1, 768 / threads) : 1ll << 30);
+  const bool whole = M == s.team * s.nv;
+#define GSHARD_LN(NV, NT, MINB, AHEAD)                                                                              \
+  do {                                                                                                              \
+    if constexpr (W >= 4) {                                                                                         \
+      if (whole) {                                                                                                  \
+        ln_fwd_kernel<T, W, NV / W, NT, MINB, AHEAD, true><<<grid, block, 0, st>>>(x, gamma, beta, y, mean, rstd, n, M, eps); \
+        break;                                                                                                      \
+      }                                                                                                             \
+    }                                                                                                               \
+    ln_fwd_kernel<T, W, NV / W, NT, MINB, AHEAD, false><<<grid, block, 0, st>>>(x, gamma, beta, y, mean, rstd, n, M, eps); \
+  } while (0)
+  if (ahead && threads <= 128) { if (s.nv == 16) GSHARD_LN(16, 128, 6, true); else GSHARD_LN(8, 128, 6, true); }
+  else if (ahead) GSHARD_LN(16, 768, 1, true);
+  else if (s.nv == 32) GSHARD_LN(32, 128, 8, false);
+  else if (s.nv == 16) GSHARD_LN(16, 1024, 1, false);
+  else GSHARD_LN(8, 1024, 1, false);
 #undef GSHARD_LN
   count_launch();
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
@@ -312,23 +394,39 @@ int ln_fwd_launch(long long n, int M, float eps, const T* x, const float* gamma,
 template <typename T, int W>
 int ln_bwd_launch(long long n, int M, const T* x, const float* gamma, const float* mean, const float* rstd, const T* dy,
                   const T* dskip, T* dx, float* dgamma, float* dbeta, float* partial, cudaStream_t st) {
-  const LnShape s = ln_shape(n, M);
+  const LnShape s = ln_bwd_shape(M, (int)sizeof(T));
   const dim3 block(s.team, s.teams);
-  const int grid = ln_bwd_blocks(n, s);
-  const int smem = partial && (s.teams > 1 || s.nv == 16) ? 2 * M * (int)sizeof(float) : 0;
-#define GSHARD_LN(NV, NT, SMEM)                                                                                         do {                                                                                                                    auto kern = ln_bwd_kernel<T, W, NV / W, NT, SMEM>;                                                                    if (smem > 48 * 1024 &&                                                                                                   cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {                     cudaGetLastError();                                                                                                   return GSHARD_ERR_CUDA;                                                                                             }                                                                                                                     kern<<<grid, block, smem, st>>>(x, gamma, mean, rstd, dy, dskip, dx, partial, n, M);                                } while (0)
-  if (s.teams > 1) {
-    if (s.nv == 32) GSHARD_LN(32, 256, false);
-    else if (s.nv == 16) GSHARD_LN(16, 256, false);
-    else GSHARD_LN(8, 256, false);
-  } else {
-    if (s.nv == 16) GSHARD_LN(16, 1024, true);
-    else GSHARD_LN(8, 1024, false);
-  }
+  const int grid = ln_bwd_blocks(n, M, (int)sizeof(T));
+  const bool sums_in_smem = M > 8192;
+  const int smem = partial && (s.teams > 1 || sums_in_smem) ? 2 * M * (int)sizeof(float) : 0;
+  const bool whole = M == s.team * s.nv;
+#define GSHARD_LN_W(NV, NT, MINB, AHEAD, SMEM, WHOLE)                                                                 \
+  do {                                                                                                                \
+    auto kern = ln_bwd_kernel<T, W, NV / W, NT, MINB, AHEAD, SMEM, WHOLE>;                                            \
+    if (smem > 48 * 1024 &&                                                                                           \
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {               \
+      cudaGetLastError();                                                                                             \
+      return GSHARD_ERR_CUDA;                                                                                         \
+    }                                                                                                                 \
+    kern<<<grid, block, smem, st>>>(x, gamma, mean, rstd, dy, dskip, dx, partial, n, M);                              \
+  } while (0)
+#define GSHARD_LN(NV, NT, MINB, AHEAD, SMEM)                                                                          \
+  do {                                                                                                                \
+    if constexpr (W * sizeof(T) == 16) {                                                                              \
+      if (whole) { GSHARD_LN_W(NV, NT, MINB, AHEAD, SMEM, true); break; }                                             \
+    }                                                                                                                 \
+    GSHARD_LN_W(NV, NT, MINB, AHEAD, SMEM, false);                                                                    \
+  } while (0)
+  if (sums_in_smem) GSHARD_LN(16, 1024, 1, false, true);
+  else if (s.nv == 16) { if constexpr (sizeof(T) == 2) GSHARD_LN(16, 512, 1, true, false); }
+  else if (s.team * s.teams <= 128) GSHARD_LN(8, 128, 5, true, false);
+  else if (s.team <= 640) GSHARD_LN(8, 640, 1, true, false);
+  else GSHARD_LN(8, 1024, 1, false, false);
+#undef GSHARD_LN_W
 #undef GSHARD_LN
   count_launch();
   if (partial) {
-    ln_bwd_finish_kernel<<<ceil_div(2 * M, 32), dim3(32, 32), 0, st>>>(partial, grid, M, dgamma, dbeta);
+    ln_bwd_finish_kernel<<<ceil_div(2 * M, 8), 256, 0, st>>>(partial, grid, M, dgamma, dbeta);
     count_launch();
   }
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
@@ -352,7 +450,9 @@ extern "C" {
 size_t gshard_layer_norm_workspace_bytes(int64_t n_rows, int32_t M) {
   if (ln_validate(n_rows, M, GSHARD_F32) != GSHARD_OK) return 0;
   if (n_rows == 0) return kAlign;
-  return align_up((size_t)ln_bwd_blocks(n_rows, ln_shape(n_rows, M)) * 2 * M * sizeof(float));
+  // the type is not known here: the larger of the two grids
+  const int rows = std::max(ln_bwd_blocks(n_rows, M, 2), ln_bwd_blocks(n_rows, M, 4));
+  return align_up((size_t)rows * 2 * M * sizeof(float));
 }
 
 int gshard_layer_norm_forward(int64_t n_rows, int32_t M, int32_t dtype, float eps, const void* x, const float* gamma,
@@ -366,7 +466,11 @@ int gshard_layer_norm_forward(int64_t n_rows, int32_t M, int32_t dtype, float ep
   GS_CHECK(check_device());
   NvtxRange range("gshard.layer_norm");
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int w = ln_width(M, dtype == GSHARD_BF16 ? 2 : 4);
+  int w = ln_width(M, dtype == GSHARD_BF16 ? 2 : 4);
+  // With 32 values per thread gamma and beta are read again for every row, four times the bytes of a bf16 row: at
+  // 4 columns per lane their loads are whole 512-byte lines of L1, at 8 they take twice the passes (106 us
+  // at 131072 x 1024, L1 90 % busy).
+  if (ln_fwd_shape(n_rows, M).nv == 32) w = std::min(w, 4);
 #define GSHARD_LN_FWD(T, W) ln_fwd_launch<T, W>(n_rows, M, eps, static_cast<const T*>(x), gamma, beta, static_cast<T*>(y), mean, rstd, st)
   if (dtype == GSHARD_BF16)
     return w == 8 ? GSHARD_LN_FWD(__nv_bfloat16, 8) : w == 4 ? GSHARD_LN_FWD(__nv_bfloat16, 4)

@@ -32,22 +32,6 @@ __device__ __forceinline__ float sigmoid_fast(float l) {
   return y;
 }
 
-// two fp32 operations per instruction
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
-      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
-      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-
 template <int LPR> __device__ __forceinline__ float seg_max(float v) {
 #pragma unroll
   for (int off = LPR / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, off));
@@ -165,17 +149,17 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
   }
   // f * s[0..4) of an active token to the sums i .. i + 3
   auto accumulate = [&](int i, const float* s, float f) {
-    const float2 ff = make_float2(f, f);
+    const f32x2 ff = both(f);
     if (ACC_SMEM) {
       float4* at = reinterpret_cast<float4*>(sacc + (i / 4 * 32 + lane) * 4);
       const float4 o = *at;
-      const float2 lo = fma2(make_float2(s[0], s[1]), ff, make_float2(o.x, o.y));
-      const float2 hi = fma2(make_float2(s[2], s[3]), ff, make_float2(o.z, o.w));
+      const float2 lo = unpair(fma2(pair(s[0], s[1]), ff, pair(o.x, o.y)));
+      const float2 hi = unpair(fma2(pair(s[2], s[3]), ff, pair(o.z, o.w)));
       *at = make_float4(lo.x, lo.y, hi.x, hi.y);
     } else {
 #pragma unroll
       for (int w = 0; w < 4; w += 2) {
-        const float2 o = fma2(make_float2(s[w], s[w + 1]), ff, make_float2(acc[ACC_SMEM ? 0 : i + w], acc[ACC_SMEM ? 1 : i + w + 1]));
+        const float2 o = unpair(fma2(pair(s[w], s[w + 1]), ff, pair(acc[ACC_SMEM ? 0 : i + w], acc[ACC_SMEM ? 1 : i + w + 1])));
         acc[ACC_SMEM ? 0 : i + w] = o.x; acc[ACC_SMEM ? 1 : i + w + 1] = o.y;
       }
     }
@@ -217,15 +201,15 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
       if (need_sum) {
         mx = seg_max<LPR>(mx);
         const float shift = -mx * kLog2e;      // its rounding is a factor that the sum shares
-        float2 sum2x[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        f32x2 sum2x[2] = {both(0.f), both(0.f)};
 #pragma unroll
         for (int i = 0; i < V; i += 2) {
-          const float2 e = fma2(make_float2(v[i], v[i + 1]), make_float2(kLog2e, kLog2e), make_float2(shift, shift));
+          const float2 e = unpair(fma2(pair(v[i], v[i + 1]), both(kLog2e), both(shift)));
           v[i] = exp2_approx(e.x); v[i + 1] = exp2_approx(e.y);
-          sum2x[i / 2 % 2] = add2(sum2x[i / 2 % 2], make_float2(v[i], v[i + 1]));
+          sum2x[i / 2 % 2] = add2(sum2x[i / 2 % 2], pair(v[i], v[i + 1]));
         }
-        sum2x[0] = add2(sum2x[0], sum2x[1]);
-        float sum = seg_sum<LPR>(sum2x[0].x + sum2x[0].y);
+        const float2 sums2 = unpair(add2(sum2x[0], sum2x[1]));
+        float sum = seg_sum<LPR>(sums2.x + sums2.y);
         const bool odd = !(fabsf(mx) <= 0x1p20f) || !(sum < INFINITY);
         if (__any_sync(kAll, odd)) {           // NaN, infinite or huge logits, or no expert at all
           float u[8], m2 = -INFINITY, sum2 = 0.f;
