@@ -15,6 +15,7 @@
 #include "activation.cuh"
 #include "checks.cuh"
 #include "gemm_dispatch.cuh"
+#include "pack.cuh"
 #include "plan.cuh"
 
 namespace gshard {
@@ -46,10 +47,14 @@ __global__ void __launch_bounds__(256) linear_finish_kernel(const float* __restr
 }
 
 // dpre = dy act'(pre) rounded to TD (where wanted), and the chunk's column sums of dpre before the rounding.
-// A block covers 32 x 8 columns and one chunk of rows; a thread owns 8 columns and every 8th row.
-template <typename TY, typename TD>
+// A block covers 32 x 8 columns and one chunk of rows; a thread owns 8 columns and every 8th row, four of
+// them in flight: the pass is bound by HBM (dy and pre in, dpre out).
+template <typename TY, typename TD, int ACT>
 __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__ dy, const TY* __restrict__ pre, TD* dpre,
-                                                          float* __restrict__ partial, long long n, int cols, int chunk, int act) {
+                                                          float* __restrict__ partial, long long n, int cols, int chunk) {
+  constexpr bool FAST = sizeof(TD) == 2;
+  constexpr int U = sizeof(TY) == 2 ? 4 : 2;              // rows in flight
+  constexpr int PW = 16 / (int)sizeof(TY), PN = 8 / PW;    // packs of 16 bytes per 8 columns
   __shared__ float part[8][256 + 8];
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
   const int col = blockIdx.x * 256 + tx * 8;
@@ -58,24 +63,39 @@ __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum[j] = 0.f;
   if (col < cols) {
-    for (long long r = (long long)blockIdx.y * chunk + ty; r < r1; r += 8) {
-      const long long off = r * cols + col;
-      float g[8], v[8];
-      constexpr int n16 = Vec16<TY>::n;
+    for (long long r0 = (long long)blockIdx.y * chunk + ty; r0 < r1; r0 += 8 * U) {
+      Pack<TY, PW> g[U][PN], v[U][PN];
 #pragma unroll
-      for (int h = 0; h < 8 / n16; ++h) Vec16<TY>::load(__ldg(reinterpret_cast<const uint4*>(dy + off) + h), g + h * n16);
-      if (act != GSHARD_ACT_NONE) {
+      for (int u = 0; u < U; ++u) {
+        if (r0 + 8 * u < r1) {
+          const long long off = (r0 + 8 * u) * cols + col;
 #pragma unroll
-        for (int h = 0; h < 8 / n16; ++h) Vec16<TY>::load(__ldg(reinterpret_cast<const uint4*>(pre + off) + h), v + h * n16);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] *= activation_slope(v[j], act);
+          for (int h = 0; h < PN; ++h) {
+            g[u][h].load_once(dy + off + h * PW);
+            if (ACT != GSHARD_ACT_NONE) v[u][h].load_once(pre + off + h * PW);
+          }
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] += g[j];
-      if (dpre) {
-        constexpr int d16 = Vec16<TD>::n;
+      for (int u = 0; u < U; ++u) {
+        if (r0 + 8 * u < r1) {
+          float d[8];
 #pragma unroll
-        for (int h = 0; h < 8 / d16; ++h) reinterpret_cast<uint4*>(dpre + off)[h] = Vec16<TD>::store(g + h * d16);
+          for (int j = 0; j < 8; ++j) {
+            d[j] = g[u][j / PW].get(j % PW);
+            if (ACT != GSHARD_ACT_NONE) {
+              const float a = v[u][j / PW].get(j % PW);
+              // rounded before it is summed, whether or not it is also stored: the same bits for any set of outputs
+              d[j] = __fmul_rn(d[j], FAST ? activation_slope_fast(a, ACT) : activation_slope(a, ACT));
+            }
+            sum[j] += d[j];
+          }
+          if (dpre) {
+            const long long off = (r0 + 8 * u) * cols + col;
+#pragma unroll
+            for (int h = 0; h < 8; h += 16 / (int)sizeof(TD)) store_pack<TD, 16 / (int)sizeof(TD)>(dpre + off + h, d + h);
+          }
+        }
       }
     }
   }
@@ -92,14 +112,43 @@ __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__
   }
 }
 
-// out[c] = sum over `rows` partial rows, in order.
-__global__ void __launch_bounds__(128) linear_dbias_kernel(const float* __restrict__ partial, float* __restrict__ out, int rows,
+template <typename TY, typename TD>
+void launch_dpre(const void* dy, const void* pre, void* dpre, float* partial, long long n, int cols, int chunk, int chunks, int act,
+                 cudaStream_t st) {
+  const dim3 grid(ceil_div(cols, 256), chunks);
+#define GSHARD_DPRE(A)                                                                                                   \
+  case A:                                                                                                                \
+    linear_dpre_kernel<TY, TD, A><<<grid, 256, 0, st>>>(static_cast<const TY*>(dy), static_cast<const TY*>(pre),         \
+                                                        static_cast<TD*>(dpre), partial, n, cols, chunk);                \
+    break;
+  switch (act) {
+    GSHARD_DPRE(GSHARD_ACT_NONE)
+    GSHARD_DPRE(GSHARD_ACT_RELU)
+    GSHARD_DPRE(GSHARD_ACT_GELU)
+    GSHARD_DPRE(GSHARD_ACT_GELU_TANH)
+    GSHARD_DPRE(GSHARD_ACT_SILU)
+  }
+#undef GSHARD_DPRE
+  count_launch();
+}
+
+// out[c] = sum over the partial rows: 8 strands of rows in order, then the strands.
+__global__ void __launch_bounds__(256) linear_dbias_kernel(const float* __restrict__ partial, float* __restrict__ out, int rows,
                                                            int cols) {
-  const int c = blockIdx.x * 128 + threadIdx.x;
-  if (c >= cols) return;
+  __shared__ float part[8][33];
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const int c = blockIdx.x * 32 + tx;
   float s = 0.f;
-  for (int r = 0; r < rows; ++r) s += partial[(long long)r * cols + c];
-  out[c] = s;
+  if (c < cols)
+    for (int r = ty; r < rows; r += 8) s += partial[(long long)r * cols + c];
+  part[ty][tx] = s;
+  __syncthreads();
+  if (ty == 0 && c < cols) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += part[i][tx];
+    out[c] = s;
+  }
 }
 
 // out = sum of `splits` fp32 partial products of n4 float4 each, in order, rounded to bf16.
@@ -276,17 +325,11 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
   void* buf = convert && (dx || dw) ? ws + pl.dpre : nullptr;
   float* colsum = dbias ? reinterpret_cast<float*>(ws + pl.colsum) : nullptr;
   if (buf || colsum) {
-    const dim3 grid(ceil_div(cols, 256), pl.chunks);
-#define GSHARD_DPRE(TY, TD)                                                                                        \
-  linear_dpre_kernel<TY, TD><<<grid, 256, 0, st>>>(static_cast<const TY*>(dy), static_cast<const TY*>(pre),        \
-                                                   static_cast<TD*>(buf), colsum, n_rows, cols, pl.chunk, activation)
-    if (dtype == GSHARD_F32) GSHARD_DPRE(float, float);
-    else if (out_dtype == GSHARD_F32) GSHARD_DPRE(float, __nv_bfloat16);
-    else GSHARD_DPRE(__nv_bfloat16, __nv_bfloat16);
-#undef GSHARD_DPRE
-    count_launch();
+    if (dtype == GSHARD_F32) launch_dpre<float, float>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
+    else if (out_dtype == GSHARD_F32) launch_dpre<float, __nv_bfloat16>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
+    else launch_dpre<__nv_bfloat16, __nv_bfloat16>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
     if (dbias) {
-      linear_dbias_kernel<<<ceil_div(cols, 128), 128, 0, st>>>(colsum, dbias, pl.chunks, cols);
+      linear_dbias_kernel<<<ceil_div(cols, 32), 256, 0, st>>>(colsum, dbias, pl.chunks, cols);
       count_launch();
     }
   }

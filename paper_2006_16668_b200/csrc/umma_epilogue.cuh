@@ -241,7 +241,8 @@ __device__ __forceinline__ void epilogue_linear_tile(const P& p, const CUtensorM
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      activate<32>(r[h], p.lin.act);
+      if (p.out_f32) activate<32, false>(r[h], p.lin.act);
+      else activate<32, true>(r[h], p.lin.act);
       if (has_res) {
         if (p.out_f32) {
           const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(p.lin.residual) + off + 32 * h);
