@@ -103,6 +103,8 @@ struct UmmaGemm {
                              // multiprocessors to a kernel running beside this one on another stream
   int splits;                // > 1: the contraction is cut into `splits` runs of whole k-blocks (batch 1); run i writes
                              // its partial product to C + i * c_bs (fp32), and the caller adds them
+  int planes;                // A and B are three bf16 planes each (batch strides a_bs, b_bs) whose sum is the fp32 operand:
+                             // the six products of planes that reach 2^-16 are added up, small ones first
   const LinearEpilogue* linear;   // a_kmajor, !b_kmajor, batch 1: the linear operator's epilogue instead of relu / masks
 };
 int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st);

@@ -9,12 +9,17 @@
 // dpre is rounded to bf16 once, as the operand of both gradient products; dbias sums it before the rounding.
 // A product with too few output tiles for the multiprocessors is cut along the contraction into runs whose
 // fp32 partial products a second kernel adds in order.
-// fp32: CUDA cores, fp32 FMA.
+// fp32: an fp32 value is the exact sum of three bf16 values (8 bits of its 24 each), so x . w is six bf16 products
+// of such planes on the same GEMMs, accumulated in fp32, smallest first; the three products left out lie below 2^-24.
+// That is six times the tensor work and three times the operand bytes, and still several times faster than fp32 FMA
+// on the CUDA cores (4100 x 1024 x 4096: 1172 us there).  Infinities and NaN in x, w or dy give NaN.
+// A few rows stream w through the CUDA cores instead (linear_few.cu).
 #include <algorithm>
 
 #include "activation.cuh"
 #include "checks.cuh"
 #include "gemm_dispatch.cuh"
+#include "linear.cuh"
 #include "pack.cuh"
 #include "plan.cuh"
 
@@ -24,35 +29,50 @@ namespace {
 
 constexpr int kSms = 148;                    // multiprocessors of a B200: sizes the work split, not the grids
 
-// The rest of the operator on the fp32 product x . w.
-__global__ void __launch_bounds__(256) linear_finish_kernel(const float* __restrict__ product, float* y,
-                                                            const float* __restrict__ bias, const float* residual,
-                                                            float* pre, long long n4, int cols4, int act) {
+// The operator's epilogue on `splits` fp32 partial products of n4 float4 each, added in order.
+template <typename TY>
+__global__ void __launch_bounds__(256) linear_finish_kernel(const float4* __restrict__ partial, int splits, LinearEpilogue lin,
+                                                            void* y, long long n4, int cols4) {
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n4; i += (long long)gridDim.x * 256) {
-    const float4 v = reinterpret_cast<const float4*>(product)[i];
-    float f[4] = {v.x, v.y, v.z, v.w};
-    if (bias) {
-      const float4 b = __ldg(reinterpret_cast<const float4*>(bias) + i % cols4);
-      f[0] += b.x; f[1] += b.y; f[2] += b.z; f[3] += b.w;
+    float4 s = partial[i];
+    for (int k = 1; k < splits; ++k) {
+      const float4 v = partial[(long long)k * n4 + i];
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
-    if (pre) reinterpret_cast<float4*>(pre)[i] = make_float4(f[0], f[1], f[2], f[3]);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = activation_value(f[j], act);
-    if (residual) {
-      const float4 r = reinterpret_cast<const float4*>(residual)[i];
-      f[0] += r.x; f[1] += r.y; f[2] += r.z; f[3] += r.w;
-    }
-    reinterpret_cast<float4*>(y)[i] = make_float4(f[0], f[1], f[2], f[3]);
+    linear_epilogue4<TY>(lin, y, 4 * i, (int)(i % cols4) * 4, s);
   }
 }
 
-// dpre = dy act'(pre) rounded to TD (where wanted), and the chunk's column sums of dpre before the rounding.
+// The three bf16 planes of fp32 values: hi takes the top 8 bits of the significand, mid the next 8, lo the last 8,
+// each by truncation, so that hi + mid + lo is the value exactly and nothing overflows.
+__device__ __forceinline__ void split3(const float* f, float* hi, float* mid, float* lo, int n) {
+#pragma unroll
+  for (int j = 0; j < n; ++j) {
+    hi[j] = __uint_as_float(__float_as_uint(f[j]) & 0xffff0000u);
+    const float r = f[j] - hi[j];
+    mid[j] = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+    lo[j] = r - mid[j];
+  }
+}
+__global__ void __launch_bounds__(256) linear_split_kernel(const float* __restrict__ src, __nv_bfloat16* __restrict__ dst, long long n8) {
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n8; i += (long long)gridDim.x * 256) {
+    float f[8], hi[8], mid[8], lo[8];
+    load_pack<float, 4>(src + 8 * i, f);
+    load_pack<float, 4>(src + 8 * i + 4, f + 4);
+    split3(f, hi, mid, lo, 8);
+    store_pack<__nv_bfloat16, 8>(dst + 8 * i, hi);
+    store_pack<__nv_bfloat16, 8>(dst + 8 * (n8 + i), mid);
+    store_pack<__nv_bfloat16, 8>(dst + 8 * (2 * n8 + i), lo);
+  }
+}
+
+// dpre = dy act'(pre) rounded to bf16 (where wanted), and the chunk's column sums of dpre before the rounding.
 // A block covers 32 x 8 columns and one chunk of rows; a thread owns 8 columns and every 8th row, four of
-// them in flight: the pass is bound by HBM (dy and pre in, dpre out).
-template <typename TY, typename TD, int ACT>
-__global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__ dy, const TY* __restrict__ pre, TD* dpre,
+// them in flight: the pass is bound by HBM (dy and pre in, dpre out).  PLANES: dpre as three bf16 planes.
+template <typename TY, bool PLANES, int ACT>
+__global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__ dy, const TY* __restrict__ pre, __nv_bfloat16* dpre,
                                                           float* __restrict__ partial, long long n, int cols, int chunk) {
-  constexpr bool FAST = sizeof(TD) == 2;
+  constexpr bool FAST = !PLANES;
   constexpr int U = sizeof(TY) == 2 ? 4 : 2;              // rows in flight
   constexpr int PW = 16 / (int)sizeof(TY), PN = 8 / PW;    // packs of 16 bytes per 8 columns
   __shared__ float part[8][256 + 8];
@@ -92,8 +112,15 @@ __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__
           }
           if (dpre) {
             const long long off = (r0 + 8 * u) * cols + col;
-#pragma unroll
-            for (int h = 0; h < 8; h += 16 / (int)sizeof(TD)) store_pack<TD, 16 / (int)sizeof(TD)>(dpre + off + h, d + h);
+            if (PLANES) {
+              float hi[8], mid[8], lo[8];
+              split3(d, hi, mid, lo, 8);
+              store_pack<__nv_bfloat16, 8>(dpre + off, hi);
+              store_pack<__nv_bfloat16, 8>(dpre + n * cols + off, mid);
+              store_pack<__nv_bfloat16, 8>(dpre + 2 * n * cols + off, lo);
+            } else {
+              store_pack<__nv_bfloat16, 8>(dpre + off, d);
+            }
           }
         }
       }
@@ -112,14 +139,14 @@ __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__
   }
 }
 
-template <typename TY, typename TD>
+template <typename TY, bool PLANES>
 void launch_dpre(const void* dy, const void* pre, void* dpre, float* partial, long long n, int cols, int chunk, int chunks, int act,
                  cudaStream_t st) {
   const dim3 grid(ceil_div(cols, 256), chunks);
 #define GSHARD_DPRE(A)                                                                                                   \
   case A:                                                                                                                \
-    linear_dpre_kernel<TY, TD, A><<<grid, 256, 0, st>>>(static_cast<const TY*>(dy), static_cast<const TY*>(pre),         \
-                                                        static_cast<TD*>(dpre), partial, n, cols, chunk);                \
+    linear_dpre_kernel<TY, PLANES, A><<<grid, 256, 0, st>>>(static_cast<const TY*>(dy), static_cast<const TY*>(pre),     \
+                                                            static_cast<__nv_bfloat16*>(dpre), partial, n, cols, chunk); \
     break;
   switch (act) {
     GSHARD_DPRE(GSHARD_ACT_NONE)
@@ -151,20 +178,6 @@ __global__ void __launch_bounds__(256) linear_dbias_kernel(const float* __restri
   }
 }
 
-// out = sum of `splits` fp32 partial products of n4 float4 each, in order, rounded to bf16.
-__global__ void __launch_bounds__(256) linear_join_kernel(const float4* __restrict__ partial, uint2* __restrict__ out,
-                                                          long long n4, int splits) {
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n4; i += (long long)gridDim.x * 256) {
-    float4 s = partial[i];
-    for (int k = 1; k < splits; ++k) {
-      const float4 v = partial[(long long)k * n4 + i];
-      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-    }
-    const __nv_bfloat162 a = __floats2bfloat162_rn(s.x, s.y), b = __floats2bfloat162_rn(s.z, s.w);
-    out[i] = make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b));
-  }
-}
-
 int stride_grid(long long items) {
   return (int)std::max<long long>(1, std::min<long long>((items + 255) / 256, (long long)kSms * 16));
 }
@@ -182,23 +195,33 @@ int splits_for(long long rows, int cols, long long depth) {
   return (int)((k_blocks + per - 1) / per);      // no empty run at the end
 }
 
-struct LinearPlan { size_t status, dpre, colsum, join, total; int chunks, chunk, dx_splits, dw_splits; };
+// Rows up to which w streams through the CUDA cores (linear_few.cu) instead of the tensor cores.
+bool few_rows(int64_t n) { return n <= 8; }
+
+struct LinearPlan { size_t status, xp, wp, dpre, colsum, join, total; int chunks, chunk, splits, dx_splits, dw_splits; };
 
 LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, bool backward) {
   Carver c;
   LinearPlan p{};
   const bool bf16 = dtype == GSHARD_BF16;
   p.status = c.take(256);
-  if (!backward && !bf16) p.join = c.take((size_t)n * cols * 4);           // the product before its epilogue
-  if (!backward || n == 0) { p.total = c.off; return p; }
-  p.dpre = c.take((size_t)n * cols * (bf16 ? 2 : 4));
+  if (n == 0 || (!backward && few_rows(n))) { p.total = c.off; return p; }
+  p.xp = c.take(bf16 ? 0 : (size_t)n * K * 6);             // planes of fp32 operands
+  p.wp = c.take(bf16 ? 0 : (size_t)K * cols * 6);
+  if (!backward) {
+    p.splits = splits_for(n, cols, K);
+    if (p.splits > 1) p.join = c.take((size_t)p.splits * n * cols * 4);
+    p.total = c.off;
+    return p;
+  }
+  p.dpre = c.take((size_t)n * cols * (bf16 ? 2 : 6));
   const int col_blocks = ceil_div(cols, 256);
   const long long want = std::max(1, kSms * 8 / col_blocks);                // row chunks that give every multiprocessor 8 blocks
   p.chunk = (int)std::max<long long>(32, (n + want - 1) / want);
   p.chunks = (int)((n + p.chunk - 1) / p.chunk);
   p.colsum = c.take((size_t)p.chunks * cols * 4);
-  p.dx_splits = bf16 ? splits_for(n, K, cols) : 1;
-  p.dw_splits = bf16 ? splits_for(K, cols, n) : 1;
+  p.dx_splits = splits_for(n, K, cols);
+  p.dw_splits = splits_for(K, cols, n);
   p.join = c.take(std::max(p.dx_splits > 1 ? (size_t)p.dx_splits * n * K * 4 : 0,
                            p.dw_splits > 1 ? (size_t)p.dw_splits * K * cols * 4 : 0));
   p.total = c.off;
@@ -210,27 +233,35 @@ int linear_validate(int64_t n, int32_t K, int32_t cols, int32_t dtype, int32_t o
   if (dtype != GSHARD_F32 && dtype != GSHARD_BF16) return GSHARD_ERR_INVALID_ARG;
   if (out_dtype != GSHARD_F32 && out_dtype != dtype) return GSHARD_ERR_INVALID_ARG;
   if (K % 8 || cols % 8 || K > (1 << 24) || cols > (1 << 24)) return GSHARD_ERR_UNSUPPORTED_SHAPE;
-  // 64-row tiles of the CUDA-core GEMM in a grid's y extent; a tensor map's strides; tile counts in 31 bits
-  if (dtype == GSHARD_F32 && ((n + 63) / 64 > 65535 || (K + 63) / 64 > 65535)) return GSHARD_ERR_UNSUPPORTED_SHAPE;
+  // a tensor map's strides; tile counts in 31 bits
   if (n > (1ll << 30) || n * std::max(K, cols) >= (1ll << 37)) return GSHARD_ERR_UNSUPPORTED_SHAPE;
   if (((n + 127) / 128) * ((long long)(std::max(K, cols) + 127) / 128) >= (1ll << 30)) return GSHARD_ERR_UNSUPPORTED_SHAPE;
   return GSHARD_OK;
 }
 
-Dims linear_dims(int K, int cols, int dtype) {
+// the tensor-core GEMMs, whose operands are bf16 (or planes of it)
+Dims linear_dims(int K, int cols) {
   gshard_moe_shape one{};
-  one.G = 1; one.S = 1; one.C = 1; one.E = 2; one.M = K; one.H = cols; one.dtype = dtype;
+  one.G = 1; one.S = 1; one.C = 1; one.E = 2; one.M = K; one.H = cols; one.dtype = GSHARD_BF16;
   return make_dims(one);
 }
+void split_planes(const void* src, void* dst, long long n, cudaStream_t st) {
+  linear_split_kernel<<<stride_grid(n / 8), 256, 0, st>>>(static_cast<const float*>(src), static_cast<__nv_bfloat16*>(dst), n / 8);
+  count_launch();
+}
 
-// C = A . B (bf16 out) cut into `splits` runs through the fp32 partial products in `join`
+// C = A . B, cut into `splits` runs through the fp32 partial products in `join`
 int gemm_joined(const Dims& d, UmmaGemm g, int splits, float* join, int* status, cudaStream_t st) {
   if (splits <= 1) return run_gemm(d, g, status, st);
   void* out = g.C;
+  const bool out_f32 = g.out_f32 != 0;
   const long long n4 = (long long)g.rows * g.cols / 4;
   g.C = join; g.out_f32 = 1; g.splits = splits; g.c_bs = (long long)g.rows * g.cols;
   GS_CHECK(run_gemm(d, g, status, st));
-  linear_join_kernel<<<stride_grid(n4), 256, 0, st>>>(reinterpret_cast<const float4*>(join), static_cast<uint2*>(out), n4, splits);
+  const LinearEpilogue none{};
+  const float4* partial = reinterpret_cast<const float4*>(join);
+  if (out_f32) linear_finish_kernel<float><<<stride_grid(n4), 256, 0, st>>>(partial, splits, none, out, n4, g.cols / 4);
+  else linear_finish_kernel<__nv_bfloat16><<<stride_grid(n4), 256, 0, st>>>(partial, splits, none, out, n4, g.cols / 4);
   count_launch();
   return GSHARD_OK;
 }
@@ -270,24 +301,34 @@ int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype
   NvtxRange range("gshard.linear");
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   int* status = static_cast<int*>(workspace);
+  const LinearEpilogue lin{bias, residual, pre, activation};
+  const bool out_f32 = out_dtype == GSHARD_F32;
+  if (few_rows(n_rows)) {
+    GS_CHECK(launch_linear_few((int)n_rows, K, cols, dtype == GSHARD_BF16, out_f32, x, w, y, lin, status, st));
+    return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
+  }
   GS_CHECK(zero(status, sizeof(int), st));
-  const Dims d = linear_dims(K, cols, dtype);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  const Dims d = linear_dims(K, cols);
   UmmaGemm g{};
   g.A = x; g.B = w; g.C = y; g.rows = (int)n_rows; g.cols = cols; g.K = K; g.batch = 1;
   g.a_kmajor = true; g.b_kmajor = false; g.a_ld = K; g.b_ld = cols; g.c_ld = cols;
-  g.a_stream = 1; g.prefer_two_sm = 1; g.out_f32 = out_dtype == GSHARD_F32;
-  LinearEpilogue lin{bias, residual, pre, activation};
-  if (dtype == GSHARD_BF16) {
+  g.a_stream = 1; g.prefer_two_sm = 1; g.out_f32 = out_f32;
+  if (dtype == GSHARD_F32) {
+    split_planes(x, ws + pl.xp, n_rows * K, st);
+    split_planes(w, ws + pl.wp, (long long)K * cols, st);
+    g.A = ws + pl.xp; g.B = ws + pl.wp; g.planes = 1; g.a_bs = n_rows * K; g.b_bs = (long long)K * cols; g.a_stream = 0;
+  }
+  if (pl.splits == 1) {
     g.linear = &lin;
     GS_CHECK(run_gemm(d, g, status, st));
   } else {
-    float* product = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + pl.join);
-    g.C = product;
-    GS_CHECK(run_gemm(d, g, status, st));
     const long long n4 = n_rows * cols / 4;
-    linear_finish_kernel<<<stride_grid(n4), 256, 0, st>>>(product, static_cast<float*>(y), bias,
-                                                          static_cast<const float*>(residual), static_cast<float*>(pre), n4,
-                                                          cols / 4, activation);
+    g.C = ws + pl.join; g.out_f32 = 1; g.splits = pl.splits; g.c_bs = n_rows * cols;
+    GS_CHECK(run_gemm(d, g, status, st));
+    const float4* partial = reinterpret_cast<const float4*>(ws + pl.join);
+    if (out_f32) linear_finish_kernel<float><<<stride_grid(n4), 256, 0, st>>>(partial, pl.splits, lin, y, n4, cols / 4);
+    else linear_finish_kernel<__nv_bfloat16><<<stride_grid(n4), 256, 0, st>>>(partial, pl.splits, lin, y, n4, cols / 4);
     count_launch();
   }
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
@@ -321,33 +362,42 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   int* status = reinterpret_cast<int*>(ws);
   GS_CHECK(zero(status, sizeof(int), st));
-  const bool convert = activation != GSHARD_ACT_NONE || out_dtype != dtype;    // else dpre is dy itself
+  const bool fp32 = dtype == GSHARD_F32;
+  const bool convert = fp32 || activation != GSHARD_ACT_NONE || out_dtype != dtype;    // else dpre is dy itself
   void* buf = convert && (dx || dw) ? ws + pl.dpre : nullptr;
   float* colsum = dbias ? reinterpret_cast<float*>(ws + pl.colsum) : nullptr;
   if (buf || colsum) {
-    if (dtype == GSHARD_F32) launch_dpre<float, float>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
-    else if (out_dtype == GSHARD_F32) launch_dpre<float, __nv_bfloat16>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
-    else launch_dpre<__nv_bfloat16, __nv_bfloat16>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
+    if (fp32) launch_dpre<float, true>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
+    else if (out_dtype == GSHARD_F32) launch_dpre<float, false>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
+    else launch_dpre<__nv_bfloat16, false>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
     if (dbias) {
       linear_dbias_kernel<<<ceil_div(cols, 32), 256, 0, st>>>(colsum, dbias, pl.chunks, cols);
       count_launch();
     }
   }
   const void* dpre = convert ? buf : dy;
-  const Dims d = linear_dims(K, cols, dtype);
+  const Dims d = linear_dims(K, cols);
   float* join = reinterpret_cast<float*>(ws + pl.join);
   if (dx) {                                       // [n, K] = dpre [n, cols] . w^T, both contiguous along cols
     UmmaGemm g{};
     g.A = dpre; g.B = w; g.C = dx; g.rows = (int)n_rows; g.cols = K; g.K = cols; g.batch = 1;
     g.a_kmajor = true; g.b_kmajor = true; g.a_ld = cols; g.b_ld = cols; g.c_ld = K;
-    g.prefer_two_sm = 1;
+    g.prefer_two_sm = 1; g.out_f32 = fp32;
+    if (fp32) {
+      split_planes(w, ws + pl.wp, (long long)K * cols, st);
+      g.B = ws + pl.wp; g.planes = 1; g.a_bs = n_rows * cols; g.b_bs = (long long)K * cols;
+    }
     GS_CHECK(gemm_joined(d, g, pl.dx_splits, join, status, st));
   }
   if (dw) {                                       // [K, cols] = x^T . dpre, both stored row by row of the contraction
     UmmaGemm g{};
     g.A = x; g.B = dpre; g.C = dw; g.rows = K; g.cols = cols; g.K = (int)n_rows; g.batch = 1;
     g.a_kmajor = false; g.b_kmajor = false; g.a_ld = K; g.b_ld = cols; g.c_ld = cols;
-    g.prefer_two_sm = 1;
+    g.prefer_two_sm = 1; g.out_f32 = fp32;
+    if (fp32) {
+      split_planes(x, ws + pl.xp, n_rows * K, st);
+      g.A = ws + pl.xp; g.planes = 1; g.a_bs = n_rows * K; g.b_bs = n_rows * cols;
+    }
     GS_CHECK(gemm_joined(d, g, pl.dw_splits, join, status, st));
   }
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;

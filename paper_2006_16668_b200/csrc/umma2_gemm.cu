@@ -61,6 +61,7 @@ struct Params2 {
   int* status;
   int tma_store;   // epilogue rows leave by bulk tensor stores through map_c
   int split;       // batch index = run of k_blocks k-blocks of the one problem (operands have no batch)
+  int passes;      // 1, or 6 with planes: every tile runs its k-blocks once per product of planes
   LinearEpilogue lin;   // LIN instantiations only
   // Ragged batches (compacted expert rows): problem b owns the 256-row tiles [tile_base[b], tile_base[b+1])
   // of a device-side prefix array with batch + 1 entries; nullptr = every problem has m_tiles row tiles.
@@ -133,7 +134,9 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         const int row0 = t.mt * 2 * BM + (int)rank * BM;      // this CTA's 128 rows of the 256-row tile
         const int col0 = t.nt * BN + (int)rank * BNH;         // this CTA's half of the B columns
         const int kfirst = p.split ? t.b * p.k_blocks : 0, ob = p.split ? 0 : t.b;
-        for (int kb = 0; kb < p.k_blocks; ++kb) {
+        const int iters = p.k_blocks * p.passes;
+        for (int it = 0, kb = 0, pass = 0; it < iters; ++it) {
+          const int oa = p.passes > 1 ? plane_of_a(pass) : ob, obb = p.passes > 1 ? plane_of_b(pass) : ob;
           if (!ptx::mbar_wait(empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
           unsigned char* sa = smem + stage * kStageBytes;
           unsigned char* sb = sa + kABytes;
@@ -141,19 +144,20 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
           if (rank == 0) ptx::mbar_arrive_expect_tx(full + stage, (uint32_t)(2 * kStageBytes));
           const int k0 = (kfirst + kb) * BK;
           if (A_K) {
-            ptx::tma_load_3d_pair(sa, &map_a, bar, k0, row0, ob, pol_a);
+            ptx::tma_load_3d_pair(sa, &map_a, bar, k0, row0, oa, pol_a);
           } else {
 #pragma unroll
             for (int j = 0; j < BM / 64; ++j)
-              ptx::tma_load_3d_pair(sa + j * kBoxBytes, &map_a, bar, row0 + j * 64, k0, ob, pol_a);
+              ptx::tma_load_3d_pair(sa + j * kBoxBytes, &map_a, bar, row0 + j * 64, k0, oa, pol_a);
           }
           if (B_K) {
-            ptx::tma_load_3d_pair(sb, &map_b, bar, k0, col0, ob, pol_b);
+            ptx::tma_load_3d_pair(sb, &map_b, bar, k0, col0, obb, pol_b);
           } else {
 #pragma unroll
             for (int j = 0; j < BNH / 64; ++j)
-              ptx::tma_load_3d_pair(sb + j * kBoxBytes, &map_b, bar, col0 + j * 64, k0, ob, pol_b);
+              ptx::tma_load_3d_pair(sb + j * kBoxBytes, &map_b, bar, col0 + j * 64, k0, obb, pol_b);
           }
+          if (++kb == p.k_blocks) { kb = 0; ++pass; }
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -169,7 +173,7 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         if (!ptx::mbar_wait(acc_empty + acc, acc_phase ^ 1u, abort_flag)) { ok = false; break; }
         ptx::tc_fence_after_sync();
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
-        for (int kb = 0; kb < p.k_blocks; ++kb) {
+        for (int kb = 0; kb < p.k_blocks * p.passes; ++kb) {
           if (!ptx::mbar_wait(full + stage, phase, abort_flag)) { ok = false; break; }
           ptx::tc_fence_after_sync();
           const uint32_t sa = ptx::smem_u32(smem + stage * kStageBytes);
@@ -485,10 +489,11 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   if ((g.mask_bits || g.mask_bits_out) && g.cols % 32) return GSHARD_ERR_INTERNAL;   // one word per 32 columns
   CUtensorMap ma, mb;
   bool okm;
-  if (g.a_kmajor) okm = make_map(&ma, g.A, g.K, g.rows, g.batch, g.a_ld, g.a_bs, BK, BM);
-  else            okm = make_map(&ma, g.A, g.rows, g.K, g.batch, g.a_ld, g.a_bs, 64, BK);
-  if (g.b_kmajor) okm = okm && make_map(&mb, g.B, g.K, g.cols, g.batch, g.b_ld, g.b_bs, BK, BNH);
-  else            okm = okm && make_map(&mb, g.B, g.cols, g.K, g.batch, g.b_ld, g.b_bs, 64, BK);
+  const int problems = g.planes ? 3 : g.batch;
+  if (g.a_kmajor) okm = make_map(&ma, g.A, g.K, g.rows, problems, g.a_ld, g.a_bs, BK, BM);
+  else            okm = make_map(&ma, g.A, g.rows, g.K, problems, g.a_ld, g.a_bs, 64, BK);
+  if (g.b_kmajor) okm = okm && make_map(&mb, g.B, g.K, g.cols, problems, g.b_ld, g.b_bs, BK, BNH);
+  else            okm = okm && make_map(&mb, g.B, g.cols, g.K, problems, g.b_ld, g.b_bs, 64, BK);
   if (!okm) return GSHARD_ERR_CUDA;
   CUtensorMap mc;
   const bool tma_store = store_map_for(g, &mc);
@@ -500,6 +505,8 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   p.total_tiles = p.m_tiles * p.n_tiles * g.batch;
   p.k_blocks = ceil_div(g.K, BK);
   p.split = 0;
+  p.passes = g.planes ? 6 : 1;
+  if (g.planes && (g.batch != 1 || g.tile_base || !g.out_f32 || g.mask_bits || g.mask_bits_out)) return GSHARD_ERR_INTERNAL;
   if (g.splits > 1) {
     if (g.batch != 1 || !g.out_f32 || g.tile_base || g.linear || g.mask_bits || g.mask_bits_out) return GSHARD_ERR_INTERNAL;
     p.split = 1; p.batch = g.splits; p.total_tiles = p.m_tiles * p.n_tiles * g.splits; p.k_blocks = ceil_div(p.k_blocks, g.splits);

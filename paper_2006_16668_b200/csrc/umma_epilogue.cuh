@@ -31,6 +31,12 @@ __device__ __forceinline__ TileCoord decode_ragged(const P& p, int tile) {
   return t;
 }
 
+// Products of three-plane operands (hi + mid + lo, each the next 8 bits of an fp32 value) in the order they are added:
+// the smallest first, so that the tensor core's truncation of the running sum acts on small sums until the
+// last pass.  Products below 2^-24 are left out.
+__device__ __forceinline__ int plane_of_a(int pass) { return (0x001012 >> (4 * pass)) & 0xf; }   // lo mid hi mid hi hi
+__device__ __forceinline__ int plane_of_b(int pass) { return (0x010210 >> (4 * pass)) & 0xf; }   // hi mid lo hi mid hi
+
 // Writes a warp's staged 32 rows x 128 bytes to C: lane l handles 16-byte piece (l & 7) of rows
 // 4*i + (l >> 3); pieces beyond the matrix edge are skipped (cols is a multiple of the piece width).
 // Whether the output rows should be kept in L2 (they are re-read soon by the same launch).  A kernel

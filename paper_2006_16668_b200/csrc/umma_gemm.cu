@@ -65,6 +65,7 @@ struct Params {
   const int* pair_base;
   int tma_store;   // epilogue rows leave by bulk tensor stores through map_c
   int split;       // batch index = run of k_blocks k-blocks of the one problem (operands have no batch)
+  int passes;      // 1, or 6 with planes: every tile runs its k-blocks once per product of planes
   LinearEpilogue lin;   // LIN instantiations only
 };
 
@@ -141,26 +142,29 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         const TileCoord cur = t;
         if (tile + (int)gridDim.x < total_tiles) t = decode(p, tile + gridDim.x);   // the next tile's coordinates load meanwhile
         const int kfirst = p.split ? cur.b * p.k_blocks : 0, ob = p.split ? 0 : cur.b;
-        for (int kb = 0; kb < p.k_blocks; ++kb) {
+        const int iters = p.k_blocks * p.passes;
+        for (int it = 0, kb = 0, pass = 0; it < iters; ++it) {
+          const int oa = p.passes > 1 ? plane_of_a(pass) : ob, obb = p.passes > 1 ? plane_of_b(pass) : ob;
           if (!ptx::mbar_wait(empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
           unsigned char* sa = smem + stage * C_::stage_bytes;
           unsigned char* sb = sa + kABytes;
           ptx::mbar_arrive_expect_tx(full + stage, (uint32_t)C_::stage_bytes);
           const int k0 = (kfirst + kb) * BKE;
           if (A_K) {
-            ptx::tma_load_3d(sa, &map_a, full + stage, k0, cur.mt * BM, ob, pol_a);
+            ptx::tma_load_3d(sa, &map_a, full + stage, k0, cur.mt * BM, oa, pol_a);
           } else {
 #pragma unroll
             for (int j = 0; j < BM / kBoxMN; ++j)
-              ptx::tma_load_3d(sa + j * kBoxB, &map_a, full + stage, cur.mt * BM + j * kBoxMN, k0, ob, pol_a);
+              ptx::tma_load_3d(sa + j * kBoxB, &map_a, full + stage, cur.mt * BM + j * kBoxMN, k0, oa, pol_a);
           }
           if (B_K) {
-            ptx::tma_load_3d(sb, &map_b, full + stage, k0, cur.nt * BN, ob, pol_b);
+            ptx::tma_load_3d(sb, &map_b, full + stage, k0, cur.nt * BN, obb, pol_b);
           } else {
 #pragma unroll
             for (int j = 0; j < BN / kBoxMN; ++j)
-              ptx::tma_load_3d(sb + j * kBoxB, &map_b, full + stage, cur.nt * BN + j * kBoxMN, k0, ob, pol_b);
+              ptx::tma_load_3d(sb + j * kBoxB, &map_b, full + stage, cur.nt * BN + j * kBoxMN, k0, obb, pol_b);
           }
+          if (++kb == p.k_blocks) { kb = 0; ++pass; }
           if (++stage == C_::stages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -176,7 +180,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         if (!ptx::mbar_wait(acc_empty + acc, acc_phase ^ 1u, abort_flag)) { ok = false; break; }
         ptx::tc_fence_after_sync();
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
-        for (int kb = 0; kb < p.k_blocks; ++kb) {
+        for (int kb = 0; kb < p.k_blocks * p.passes; ++kb) {
           if (!ptx::mbar_wait(full + stage, phase, abort_flag)) { ok = false; break; }
           ptx::tc_fence_after_sync();
           const uint32_t sa = ptx::smem_u32(smem + stage * C_::stage_bytes);
@@ -431,10 +435,11 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   const int bke = 128 / esz;                     // elements per 128-byte k-block row
   CUtensorMap ma, mb;
   bool okm;
-  if (g.a_kmajor) okm = make_map(&ma, g.A, g.K, g.rows, g.batch, g.a_ld, g.a_bs, bke, BM, esz);
-  else            okm = make_map(&ma, g.A, g.rows, g.K, g.batch, g.a_ld, g.a_bs, bke, bke, esz);
-  if (g.b_kmajor) okm = okm && make_map(&mb, g.B, g.K, g.cols, g.batch, g.b_ld, g.b_bs, bke, BN, esz);
-  else            okm = okm && make_map(&mb, g.B, g.cols, g.K, g.batch, g.b_ld, g.b_bs, bke, bke, esz);
+  const int problems = g.planes ? 3 : g.batch;
+  if (g.a_kmajor) okm = make_map(&ma, g.A, g.K, g.rows, problems, g.a_ld, g.a_bs, bke, BM, esz);
+  else            okm = make_map(&ma, g.A, g.rows, g.K, problems, g.a_ld, g.a_bs, bke, bke, esz);
+  if (g.b_kmajor) okm = okm && make_map(&mb, g.B, g.K, g.cols, problems, g.b_ld, g.b_bs, bke, BN, esz);
+  else            okm = okm && make_map(&mb, g.B, g.cols, g.K, problems, g.b_ld, g.b_bs, bke, bke, esz);
   if (!okm) return GSHARD_ERR_CUDA;
   CUtensorMap mc;
   const bool tma_store = store_map_for(g, &mc);
@@ -446,6 +451,8 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   p.total_tiles = p.m_tiles * p.n_tiles * g.batch;
   p.k_blocks = ceil_div(g.K, bke);
   p.split = 0;
+  p.passes = g.planes ? 6 : 1;
+  if (g.planes && (g.batch != 1 || g.tile_base || !g.out_f32 || g.mask_bits || g.mask_bits_out)) return GSHARD_ERR_INTERNAL;
   if (g.splits > 1) {
     if (g.batch != 1 || !g.out_f32 || g.tile_base || g.linear || g.mask_bits || g.mask_bits_out) return GSHARD_ERR_INTERNAL;
     p.split = 1; p.batch = g.splits; p.total_tiles = p.m_tiles * p.n_tiles * g.splits; p.k_blocks = ceil_div(p.k_blocks, g.splits);
@@ -462,7 +469,7 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   if (g.tile_base) p.n_fastest = 0;            // ragged lists are walked with the row tiles fastest
   int sms = device_sms();
   if (g.max_ctas > 0 && sms > g.max_ctas) sms = g.max_ctas;
-  if (!g.tf32 && !p.split && !g.tile_base && !g.a_kmajor && !g.b_kmajor && !g.mask_bits && BN == 256 && p.k_blocks <= resb::kMaxKBlocks && p.m_tiles >= 4) {
+  if (!g.tf32 && !p.split && !g.planes && !g.tile_base && !g.a_kmajor && !g.b_kmajor && !g.mask_bits && BN == 256 && p.k_blocks <= resb::kMaxKBlocks && p.m_tiles >= 4) {
     // short contraction, several row tiles per column block: keep the B tile resident
     const int n_groups = p.n_tiles * g.batch;
     if (cudaFuncSetAttribute(umma_gemm_resident_b_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
