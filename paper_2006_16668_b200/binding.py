@@ -435,33 +435,44 @@ def _code_of(dtype, what):
 
 
 def _arg(t, name, shape, dtype, device):
-    """Pointer of a tensor argument after checking it (None stays None)."""
+    """Pointer of a tensor argument after checking it (None stays None); device: index of the call's GPU."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got "
-                         f"{t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous"))
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on the device of the first "
+                         f"tensor, got {t.dtype} {tuple(t.shape)} on {t.device}"
+                         + ("" if t.is_contiguous() else ", not contiguous"))
     return t.data_ptr()
 
 
 def _workspace(ws, device):
     if ws is None:
         return None, 0
-    if ws.device != device or not ws.is_contiguous():
-        raise ValueError(f"workspace: expected a contiguous tensor on {device}, got {ws.device}")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on the device of the first tensor, got {ws.device}")
+    return ws.data_ptr(), ws.nbytes
 
 
 def _call(name, device, stream, *args):
-    """Call library function `name` with `device` current, on its current stream or on the one given."""
-    fn = getattr(load(), name)
-    if device.type != "cuda":
-        raise ValueError(f"{name}: tensors must be on a CUDA device, got {device}")
-    if torch.cuda.current_device() == device.index:
-        _check(fn(*args, _stream(stream)), name)
+    """Call library function `name` with GPU `device` current, on its current stream or on the one given."""
+    if device < 0:
+        raise ValueError(f"{name}: tensors must be on a CUDA device")
+    fn = getattr(_lib or load(), name)
+    if torch.cuda.current_device() == device:
+        _check(fn(*args, _stream_of(device, stream)), name)
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, _stream(stream)), name)
+            _check(fn(*args, _stream_of(device, stream)), name)
+
+
+# the handle of a device's current stream without a Stream object around it (a few microseconds less per call)
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(device, stream):
+    if stream is None and _current_raw_stream is not None:
+        return _current_raw_stream(device)
+    return _stream(stream)
 
 
 def gshard_layer_norm_workspace_bytes(n_rows, M) -> int:
@@ -470,7 +481,7 @@ def gshard_layer_norm_workspace_bytes(n_rows, M) -> int:
 
 def gshard_layer_norm_forward(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5, stream=None):
     """y = gamma (x - mean) rstd + beta over the last dimension of x [n, M]; beta, mean, rstd optional."""
-    code, dev, f32 = _code_of(x.dtype, "x"), x.device, torch.float32
+    code, dev, f32 = _code_of(x.dtype, "x"), x.get_device(), torch.float32
     n, M = x.shape
     args = [_arg(x, "x", (n, M), x.dtype, dev), _arg(gamma, "gamma", (M,), f32, dev), _arg(beta, "beta", (M,), f32, dev),
             _arg(y, "y", (n, M), x.dtype, dev), _arg(mean, "mean", (n,), f32, dev), _arg(rstd, "rstd", (n,), f32, dev)]
@@ -480,7 +491,7 @@ def gshard_layer_norm_forward(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5,
 def gshard_layer_norm_backward(x, gamma, mean, rstd, dy, dx, dgamma=None, dbeta=None, dskip=None, workspace=None,
                                stream=None):
     """dx (+ dskip), dgamma and dbeta of the layer norm; workspace is needed with dgamma or dbeta."""
-    code, dev, f32 = _code_of(x.dtype, "x"), x.device, torch.float32
+    code, dev, f32 = _code_of(x.dtype, "x"), x.get_device(), torch.float32
     n, M = x.shape
     args = [_arg(x, "x", (n, M), x.dtype, dev), _arg(gamma, "gamma", (M,), f32, dev), _arg(mean, "mean", (n,), f32, dev),
             _arg(rstd, "rstd", (n,), f32, dev), _arg(dy, "dy", (n, M), x.dtype, dev),
@@ -498,7 +509,7 @@ def gshard_linear_workspace_bytes(n_rows, K, cols, dtype, out_dtype=None, for_ba
 
 def gshard_linear_forward(x, w, y, bias=None, residual=None, pre=None, activation="none", workspace=None, stream=None):
     """y = activation(x . w + bias) + residual for x [n, K], w [K, cols]; pre receives x . w + bias."""
-    code, out, dev = _code_of(x.dtype, "x"), _code_of(y.dtype, "y"), x.device
+    code, out, dev = _code_of(x.dtype, "x"), _code_of(y.dtype, "y"), x.get_device()
     (n, K), cols = x.shape, w.shape[-1]
     args = [_arg(x, "x", (n, K), x.dtype, dev), _arg(w, "w", (K, cols), x.dtype, dev),
             _arg(bias, "bias", (cols,), torch.float32, dev), _arg(residual, "residual", (n, cols), y.dtype, dev),
@@ -509,7 +520,7 @@ def gshard_linear_forward(x, w, y, bias=None, residual=None, pre=None, activatio
 def gshard_linear_backward(x, w, dy, dx=None, dw=None, dbias=None, pre=None, activation="none", workspace=None,
                            stream=None):
     """dx, dw, dbias (each optional) of the linear operator; pre as the forward kept it."""
-    code, out, dev = _code_of(x.dtype, "x"), _code_of(dy.dtype, "dy"), x.device
+    code, out, dev = _code_of(x.dtype, "x"), _code_of(dy.dtype, "dy"), x.get_device()
     (n, K), cols = x.shape, w.shape[-1]
     args = [_arg(x, "x", (n, K), x.dtype, dev), _arg(w, "w", (K, cols), x.dtype, dev),
             _arg(pre, "pre", (n, cols), dy.dtype, dev), _arg(dy, "dy", (n, cols), dy.dtype, dev),
@@ -532,7 +543,7 @@ def gshard_moe_route_workspace_bytes(route) -> int:
 
 def gshard_moe_route(route, logits, expert_idx, weight, bias=None, m=None, load=None, workspace=None, stream=None):
     """Chooses route.k experts per token of logits [G, S, E]; workspace is needed with m."""
-    G, S, E, k, dev, f32 = route.G, route.S, route.E, route.k, logits.device, torch.float32
+    G, S, E, k, dev, f32 = route.G, route.S, route.E, route.k, logits.get_device(), torch.float32
     dt = torch.bfloat16 if route.dtype == GSHARD_BF16 else f32
     args = [_arg(logits, "logits", (G, S, E), dt, dev), _arg(bias, "bias", (E,), f32, dev),
             _arg(expert_idx, "expert_idx", (G, S, k), torch.int32, dev), _arg(weight, "weight", (G, S, k), f32, dev),
@@ -542,7 +553,7 @@ def gshard_moe_route(route, logits, expert_idx, weight, bias=None, m=None, load=
 
 def gshard_moe_route_backward(route, logits, expert_idx, dweight, dlogits, dm=None, stream=None):
     """dlogits of <dweight, weight> + <dm, m> with the choice held constant."""
-    G, S, E, k, dev, f32 = route.G, route.S, route.E, route.k, logits.device, torch.float32
+    G, S, E, k, dev, f32 = route.G, route.S, route.E, route.k, logits.get_device(), torch.float32
     dt = torch.bfloat16 if route.dtype == GSHARD_BF16 else f32
     args = [_arg(logits, "logits", (G, S, E), dt, dev), _arg(expert_idx, "expert_idx", (G, S, k), torch.int32, dev),
             _arg(dweight, "dweight", (G, S, k), f32, dev), _arg(dm, "dm", (G, E), f32, dev),
