@@ -21,7 +21,7 @@ namespace gshard {
 namespace {
 
 template <typename T>
-__global__ void __launch_bounds__(256) route_fwd_kernel(const RouteArgs a) {
+__global__ void __launch_bounds__(256) route_fwd_kernel(const __grid_constant__ RouteArgs a) {
   const int lane = threadIdx.x & 31;
   const long long nwarps = ((long long)gridDim.x * blockDim.x) >> 5;
   for (long long t = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5; t < a.n; t += nwarps) {

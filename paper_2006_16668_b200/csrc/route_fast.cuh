@@ -5,10 +5,11 @@
 // the choice with many (8 of 512 in 4 of 8 groups: see the figures at the launcher).  Reductions and
 // the bookkeeping of a pick cost about the same however many tokens the warp holds, which is why eight
 // lanes per token are taken where the experts fit.
-// Layout: with groups, LPR / groups lanes own a group, else all lanes own the whole row; the owners take
-// turns of W consecutive experts, so that loads are whole 16-byte words (W = 1 for rows that are not).  The values
-// that decide the choice lie in shared memory as well, in chunks of 8 per lane with the chunk's maximum in a
-// register: a pick then looks at one chunk of one lane instead of at all its values.
+// Layout: lanes take turns of W consecutive experts, so that loads are whole 16-byte words (W = 1 for rows that are
+// not).  The values that decide the choice lie in shared memory, in chunks of 8 per lane with the chunk's maximum in a
+// register: a pick then looks at one chunk of one lane instead of at all its values.  With groups LPR / groups
+// lanes own a group, and the values change lanes on their way through shared memory (loading each group by
+// its owners costs four times the L1 passes).
 #pragma once
 #include "route.cuh"
 
@@ -92,16 +93,17 @@ template <int V> __device__ __forceinline__ void clean(float (&v)[V]) {
   for (int i = 0; i < V; ++i) v[i] = fminf(fmaxf(v[i], -INFINITY), FLT_MAX);
 }
 
-// 8 consecutive values of a lane (chunk c) out of shared memory.
-__device__ __forceinline__ void chunk_values(const float* st, int lane, int c, float (&x)[8]) {
+// Shared memory of a warp: V / 4 units of 32 x 16 bytes; a lane's values i .. i + 3 (i a multiple of 4) are unit i / 4.
+// The lane is XORed with the unit (per vector of W), which spreads the stores of values that change lanes over the banks.
+template <int W> __device__ __forceinline__ int unit_at(int unit, int lane) {
+  return (unit * 32 + (lane ^ ((W >= 4 ? unit / (W / 4) : unit) & 7))) * 4;
+}
+template <int W> __device__ __forceinline__ void chunk_values(const float* st, int lane, int c, float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; i += 4) {
-    const float4 f = *reinterpret_cast<const float4*>(st + ((c * 2 + i / 4) * 32 + lane) * 4);
+    const float4 f = *reinterpret_cast<const float4*>(st + unit_at<W>(c * 2 + i / 4, lane));
     x[i] = f.x; x[i + 1] = f.y; x[i + 2] = f.z; x[i + 3] = f.w;
   }
-}
-__device__ __forceinline__ void chunk_store(float* st, int lane, int i, const float* x) {      // i a multiple of 4
-  *reinterpret_cast<float4*>(st + (i / 4 * 32 + lane) * 4) = make_float4(x[0], x[1], x[2], x[3]);
 }
 
 // A score in 64 bits; norm: the 64-bit sum of exp(l - mx) over the row (softmax).
@@ -119,25 +121,59 @@ __device__ __noinline__ double softmax_norm64(const T* row, const RouteLane<W>& 
   return s > 0.0 ? s : 1.0;
 }
 
-// BIASED: a bias or sums of group scores decide, so that scores are needed before the choice; else logits do.
+// What decides the choice: the logits; a softmax's scores plus bias; logits, with groups valued by sums of scores; or a
+// sigmoid's scores plus bias, which need no sum over the row, so that its logits pass through the registers in pieces.
+enum RouteMode { kByLogits = 0, kBySoftmaxBias = 1, kBySums = 2, kBySigmoidBias = 3 };
+
 // MEAN: sums of the scores over the block's tokens, in registers, or (64 values per lane) in shared memory, where
 // they leave the registers to more warps.
-template <typename T, int W, int LPR, int V, bool BIASED, bool MEAN>
-__global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BIASED ? 3 : 4) : 1) route_fwd_fast_kernel(const RouteArgs a, float* __restrict__ sums) {
+template <typename T, int W, int LPR, int V, int MODE, bool MEAN>
+__global__ void __launch_bounds__(kRouteThreads, V < 64 || W == 1 ? 1 : MODE == kBySigmoidBias ? (MEAN ? 3 : 4) : MEAN && MODE == kByLogits ? 3 : 4)
+route_fwd_fast_kernel(const __grid_constant__ RouteArgs a, float* __restrict__ sums) {
   constexpr int RPW = 32 / LPR;               // tokens per warp
   constexpr int NC = V / 8;
-  constexpr bool ACC_SMEM = MEAN && V == 64;
+  constexpr bool ACC_SMEM = MEAN && V == 64, BIASED = MODE != kByLogits, STREAM = MODE == kBySigmoidBias;
+  constexpr bool by_bias = MODE == kBySoftmaxBias || STREAM;
   extern __shared__ __align__(16) float route_smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int slot = lane / LPR, p = lane % LPR;
   float* st = route_smem + warp * V * 32;                       // the values that decide; at the end the sums
   float* sacc = route_smem + (warp + kRouteWarps) * V * 32;     // ACC_SMEM
-  RouteLane<W> ln;
+  const RouteLane<W> lin{0, p, LPR, a.E};     // as loaded
+  RouteLane<W> ln;                            // as owned for the choice: the same without groups
   ln.P = LPR / a.groups; ln.q = p % ln.P; ln.size = a.E / a.groups; ln.base = p / ln.P * ln.size;
-  const bool by_bias = BIASED && a.bias != nullptr;
-  const bool need_sum = !a.sigmoid && (MEAN || !a.renorm || BIASED);
+  const bool grouped = a.groups > 1;
+  const bool full = a.E == V * LPR, owns_all = ln.size == V * ln.P;
+  const bool need_sum = !STREAM && !a.sigmoid && (MEAN || !a.renorm || BIASED);
   const int t0 = blockIdx.x * kRouteTile, t1 = min(a.S, t0 + kRouteTile);
   const long long first = (long long)blockIdx.y * a.S;
+  const int per_group = ln.size / W;          // vectors of a group; g = vi / per_group by a reciprocal, exact for vi < 2^10
+  const int recip = ((1 << 20) + per_group - 1) / per_group, lg = __ffs(ln.P) - 1;
+  // a vector of this lane to where its owner looks for it
+  auto stage = [&](int j, const float* x, bool moves) {
+    int unit = j * W / 4, to = lane, comp = j * W % 4;
+    if (moves) {
+      const int vi = j * LPR + p, g = (vi * recip) >> 20, r = vi - g * per_group;
+      to = slot * LPR + (g << lg) + (r & (ln.P - 1));
+      const int i = (r >> lg) * W;
+      unit = i / 4; comp = i % 4;
+      if (vi * W >= a.E) return;
+    }
+    if constexpr (W >= 4) {
+#pragma unroll
+      for (int w = 0; w < W; w += 4)
+        *reinterpret_cast<float4*>(st + unit_at<W>(unit + w / 4, to)) = make_float4(x[w], x[w + 1], x[w + 2], x[w + 3]);
+    } else {
+      st[unit_at<W>(unit, to) + comp] = x[0];
+    }
+  };
+  auto blank = [&]() {                        // places beyond a group's end: nothing is ever staged there
+    if (grouped && !owns_all) {
+#pragma unroll
+      for (int u = 0; u < V / 4; ++u) *reinterpret_cast<float4*>(st + unit_at<W>(u, lane)) = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    }
+  };
+  blank();
   float acc[MEAN && !ACC_SMEM ? V : 4];
   if (MEAN && !ACC_SMEM) {
 #pragma unroll
@@ -165,13 +201,12 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
     }
   };
 
-  const bool full = ln.size == V * ln.P;
   for (int s0 = t0 + warp * RPW; s0 < t1; s0 += kRouteWarps * RPW) {
     const bool active = s0 + slot < t1;
     const long long t = first + min(s0 + slot, t1 - 1);
     const T* row = static_cast<const T*>(a.logits) + t * a.E;
-    float v[V];
-    load_logits<T, W, V>(row, ln, full, v);
+    float v[STREAM ? W : V];
+    if constexpr (!STREAM) load_logits<T, W, V>(row, lin, full, v);
     {                                          // the warp's next tokens on their way into L2 meanwhile
       const int s1 = s0 + kRouteWarps * RPW;
       const char* ahead = reinterpret_cast<const char*>(static_cast<const T*>(a.logits) + (first + s1) * a.E);
@@ -184,20 +219,34 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
     // Errors of fp32 scores: of a softmax, (V + 32) roundings of its sum and its exponentials; of a sigmoid,
     // under 2^-20; the sum with the bias half a step.  Values closer than twice that are compared in 64 bits.
     float slack = 0x1p-20f;
-    if (!BIASED) {
-      // fmaxf passes over NaN, so that the choice needs no clean-up; exponentials of NaN or of infinite
-      // logits are caught by the two tests below
-      __syncwarp();                            // the previous tokens' values have been read
+    __syncwarp();                              // the previous tokens' values have been read
+    if constexpr (MODE == kBySums) clean<V>(v);
+    if constexpr (!by_bias) {
+      auto maxima = [&]() {
+        mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < V; i += 4) chunk_store(st, lane, i, v + i);
+        for (int c = 0; c < NC; ++c) {
+          float m = v[c * 8];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float m = v[c * 8];
+          for (int i = 1; i < 8; ++i) m = fmaxf(m, v[c * 8 + i]);
+          cm[c] = fmaxf(m, -INFINITY);
+          mx = fmaxf(mx, cm[c]);
+        }
+      };
+      maxima();
+      // fmaxf passes over NaN, so that logits need no clean-up for the choice, except that +inf and the largest float
+      // are the same
+      if (MODE == kByLogits && __any_sync(kAll, mx == INFINITY)) { clean<V>(v); maxima(); }
+      if (grouped) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) m = fmaxf(m, v[c * 8 + i]);
-        cm[c] = fmaxf(m, -INFINITY);
-        mx = fmaxf(mx, cm[c]);
+        for (int j = 0; j < V / W; ++j) stage(j, v + j * W, true);
+      } else {
+#pragma unroll
+        for (int j = 0; j < V / W; ++j) stage(j, v + j * W, false);
       }
+    }
+    if constexpr (MODE == kByLogits) {
+      // exponentials of NaN or of infinite logits are caught by the two tests below
       if (need_sum) {
         mx = seg_max<LPR>(mx);
         const float shift = -mx * kLog2e;      // its rounding is a factor that the sum shares
@@ -211,24 +260,19 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
         const float2 sums2 = unpair(add2(sum2x[0], sum2x[1]));
         float sum = seg_sum<LPR>(sums2.x + sums2.y);
         const bool odd = !(fabsf(mx) <= 0x1p20f) || !(sum < INFINITY);
-        if (__any_sync(kAll, odd)) {           // NaN, infinite or huge logits, or no expert at all
-          float u[8], m2 = -INFINITY, sum2 = 0.f;
+        if (__any_sync(kAll, odd)) {           // NaN, infinite or huge logits, or no expert at all: once more, cleaned up
+          float m2 = -INFINITY, sum2 = 0.f;
 #pragma unroll 1
-          for (int c = 0; c < NC; ++c) {
-            chunk_values(st, lane, c, u);
-            for (int i = 0; i < 8; ++i) m2 = fmaxf(m2, u[i]);
-          }
-          m2 = fminf(seg_max<LPR>(m2), FLT_MAX);
+          for (int i = 0; i < V; ++i)
+            if (lin.offset(i) < a.E) m2 = fmaxf(m2, usable(row[lin.expert(i)]));
+          m2 = seg_max<LPR>(m2);
           if (m2 == -INFINITY) m2 = 0.f;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            chunk_values(st, lane, c, u);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float e = exp2_approx((fminf(fmaxf(u[i], -INFINITY), FLT_MAX) - m2) * kLog2e);
-              sum2 += e;
-              if (odd) v[c * 8 + i] = e;
-            }
+          for (int i = 0; i < V; ++i) {
+            const float l = lin.offset(i) < a.E ? usable(row[lin.expert(i)]) : -INFINITY;
+            const float e = exp2_approx((l - m2) * kLog2e);
+            sum2 += e;
+            if (odd) v[i] = e;
           }
           sum2 = seg_sum<LPR>(sum2);
           if (odd) { mx = m2; sum = sum2; }
@@ -243,9 +287,58 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
 #pragma unroll
         for (int i = 0; i < V; i += 4) accumulate(i, v + i, a.sigmoid ? 1.f : inv);
       }
+    } else if constexpr (STREAM) {
+      constexpr int Q = V / W < 4 ? V / W : 4;               // vectors on their way at a time
+#pragma unroll
+      for (int jb = 0; jb < V / W; jb += Q) {
+        Pack<T, W> q[Q];
+#pragma unroll
+        for (int u = 0; u < Q; ++u) {
+          const int off = ((jb + u) * LPR + p) * W;
+          if (full || off < a.E) q[u].load(row + off);
+        }
+#pragma unroll
+        for (int u = 0; u < Q; ++u) {
+          constexpr int C = W < 4 ? W : 4;
+          const int j = jb + u, off = (j * LPR + p) * W;
+          float b[W], s[W], x[W];
+          if (full || off < a.E) {
+#pragma unroll
+            for (int w = 0; w < W; w += C) load_pack<float, C>(a.bias + off + w, b + w);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+              const float l = q[u].get(w);
+              s[w] = sigmoid_fast(l);                        // NaN logits and biases: barred by the maximum
+              x[w] = l == -INFINITY ? -INFINITY : fmaxf(s[w] + b[w], -INFINITY);
+            }
+          } else {
+#pragma unroll
+            for (int w = 0; w < W; ++w) { s[w] = 0.f; x[w] = -INFINITY; }
+          }
+          stage(j, x, grouped);
+          if constexpr (MEAN) {
+            static_assert(!MEAN || W >= 4 || W == 1, "");
+#pragma unroll
+            for (int w = 0; w < W; ++w) s[w] = active ? fmaxf(s[w], 0.f) : 0.f;
+            if constexpr (W >= 4) {
+#pragma unroll
+              for (int w = 0; w < W; w += 4) accumulate(j * W + w, s + w, 1.f);
+            } else {
+              float one[4] = {0.f, 0.f, 0.f, 0.f};
+              one[j % 4] = s[0];
+              accumulate(j / 4 * 4, one, 1.f);
+            }
+          }
+          if (!grouped) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) cm[(j * W + w) / 8] = (j * W + w) % 8 == 0 ? x[w] : fmaxf(cm[(j * W + w) / 8], x[w]);
+          }
+        }
+      }
     } else {
-      clean<V>(v);
       if (need_sum) {
+        if (by_bias) clean<V>(v);
+        mx = -INFINITY;
 #pragma unroll
         for (int i = 0; i < V; ++i) mx = fmaxf(mx, v[i]);
         mx = seg_max<LPR>(mx);
@@ -257,36 +350,60 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
         inv = sum > 0.f ? 1.f / sum : 0.f;
         slack = (V + 32) * 0x1p-24f * inv;
       }
-      __syncwarp();                            // the previous tokens' values have been read
+      if (by_bias || MEAN) {
+        // scores into v; then the values that decide
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float best = -INFINITY;
+        for (int j = 0; j < V / W; ++j) {
+          float s[W], x[W];
+          if (MODE == kBySums && a.sigmoid) {
 #pragma unroll
-        for (int h = 0; h < 8; h += 4) {
-          float b[4] = {0.f, 0.f, 0.f, 0.f}, s[4], x[4];
+            for (int w = 0; w < W; ++w) s[w] = sigmoid_fast(v[j * W + w]);
+          } else {
+#pragma unroll
+            for (int w = 0; w < W; ++w) s[w] = exp2_approx((v[j * W + w] - mx) * kLog2e) * inv;
+          }
           if (by_bias) {
             constexpr int C = W < 4 ? W : 4;
+            float b[W];
+            const int off = (j * LPR + p) * W;
 #pragma unroll
-            for (int w = 0; w < 4; w += C) {
-              const int off = ln.offset(c * 8 + h + w);
-              if (off < ln.size) load_pack<float, C>(a.bias + ln.base + off, b + w);
+            for (int w = 0; w < W; ++w) b[w] = 0.f;
+            if (full || off < a.E) {
+#pragma unroll
+              for (int w = 0; w < W; w += C) load_pack<float, C>(a.bias + off + w, b + w);
             }
+#pragma unroll
+            for (int w = 0; w < W; ++w) x[w] = v[j * W + w] == -INFINITY ? -INFINITY : fmaxf(s[w] + b[w], -INFINITY);
+            stage(j, x, grouped);
           }
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float l = v[c * 8 + h + w];
-            s[w] = a.sigmoid ? sigmoid_fast(l) : exp2_approx((l - mx) * kLog2e) * inv;
-            // a NaN bias bars; without a bias the logits decide, and the scores only value the groups
-            x[w] = l == -INFINITY ? -INFINITY : by_bias ? fmaxf(s[w] + b[w], -INFINITY) : l;
-            best = fmaxf(best, x[w]);
-          }
-          chunk_store(st, lane, c * 8 + h, x);
-          if (MEAN && active) accumulate(c * 8 + h, s, 1.f);
+          for (int w = 0; w < W; ++w) v[j * W + w] = MEAN ? s[w] : x[w];
         }
-        cm[c] = best;
+        if (MEAN && active) {
+#pragma unroll
+          for (int i = 0; i < V; i += 4) accumulate(i, v + i, 1.f);
+        }
       }
     }
-    if (a.groups > 1) {
+    if (grouped || (MEAN && MODE == kBySoftmaxBias)) {        // maxima of the chunks as they are owned
+      __syncwarp();
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float x[8];
+        chunk_values<W>(st, lane, c, x);
+        cm[c] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) cm[c] = fmaxf(cm[c], x[i]);
+      }
+    } else if constexpr (MODE == kBySoftmaxBias) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        cm[c] = v[c * 8];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) cm[c] = fmaxf(cm[c], v[c * 8 + i]);
+      }
+    }
+    if (grouped) {
       float top1 = -INFINITY, top2 = -INFINITY;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
@@ -299,7 +416,7 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
         for (int c = NC - 1; c >= 0; --c)
           if (cm[c] == top1) bc = c;
         float x[8], x1 = -INFINITY, x2 = -INFINITY;
-        chunk_values(st, lane, bc, x);
+        chunk_values<W>(st, lane, bc, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) { x2 = fmaxf(x2, fminf(x1, x[i])); x1 = fmaxf(x1, x[i]); }
         top2 = fmaxf(top2, x2);
@@ -310,15 +427,15 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
         top1 = fmaxf(top1, o1);
       }
       const float floor2 = a.group_top == 2 ? top2 : top1;
-      if (BIASED && !by_bias) {                // logits so far: scores grow with them
-        top1 = top1 == -INFINITY ? top1 : a.sigmoid ? sigmoid_fast(top1) : exp2_approx((top1 - mx) * kLog2e) * inv;
-        top2 = top2 == -INFINITY ? top2 : a.sigmoid ? sigmoid_fast(top2) : exp2_approx((top2 - mx) * kLog2e) * inv;
+      if (MODE == kBySums) {                   // logits so far: scores grow with them
+        top1 = top1 == -INFINITY ? top1 : a.sigmoid ? sigmoid_fast(top1) : exp2_approx((fminf(top1, FLT_MAX) - mx) * kLog2e) * inv;
+        top2 = top2 == -INFINITY ? top2 : a.sigmoid ? sigmoid_fast(top2) : exp2_approx((fminf(top2, FLT_MAX) - mx) * kLog2e) * inv;
       }
       const float mine = BIASED && a.group_top == 2 && top2 != -INFINITY ? top1 + top2 : top1;
-      const int group = p / ln.P;
+      const int group = p >> lg;
       int better = 0;
       for (int g = 0; g < a.groups; ++g) {
-        const float other = __shfl_sync(kAll, mine, slot * LPR + g * ln.P);
+        const float other = __shfl_sync(kAll, mine, slot * LPR + (g << lg));
         better += (other > mine || (other == mine && g < group)) ? 1 : 0;
       }
       bool keep = better < a.kept;
@@ -329,15 +446,15 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
                           worst_kept - best_left <= 4.f * slack + 0x1p-20f * fmaxf(fabsf(worst_kept), fabsf(best_left));
         if (__any_sync(kAll, near)) {
           // the groups' values again in 64 bits, from the few entries that can be among a group's best
-          if (!a.sigmoid && norm64 == 0.0) norm64 = softmax_norm64<LPR, V>(row, ln, mx);
+          if (!a.sigmoid && norm64 == 0.0) norm64 = softmax_norm64<LPR, V>(row, lin, mx);
           const float from = floor2 - (by_bias ? 2.f * slack + 0x1p-21f * fabsf(floor2) : 0.f);
           double d1 = -INFINITY, d2 = -INFINITY;
 #pragma unroll 1
           for (int c = 0; c < NC; ++c) {
             float x[8];
-            chunk_values(st, lane, c, x);
+            chunk_values<W>(st, lane, c, x);
             for (int i = 0; i < 8; ++i) {
-              if (x[i] == -INFINITY || !(x[i] >= from || floor2 == -INFINITY)) continue;
+              if (!(x[i] > -INFINITY) || !(x[i] >= from || floor2 == -INFINITY)) continue;
               const int e = ln.expert(c * 8 + i);
               const double d = score64(usable(row[e]), a.sigmoid, mx, norm64) + (by_bias ? (double)a.bias[e] : 0.0);
               if (d > d1) { d2 = d1; d1 = d; } else if (d > d2) d2 = d;
@@ -351,7 +468,7 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
           const double mine64 = a.group_top == 2 && d2 != -INFINITY ? d1 + d2 : d1;
           better = 0;
           for (int g = 0; g < a.groups; ++g) {
-            const double other = __shfl_sync(kAll, mine64, slot * LPR + g * ln.P);
+            const double other = __shfl_sync(kAll, mine64, slot * LPR + (g << lg));
             better += (other > mine64 || (other == mine64 && g < group)) ? 1 : 0;
           }
           keep = better < a.kept;
@@ -362,37 +479,33 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
         for (int c = 0; c < NC; ++c) cm[c] = -INFINITY;
       }
     }
-    // Picks.  The lanes whose best value is the token's best look up which one it is (the lowest index wins) and
-    // the winner takes it out of its chunk; values above (lastv, lasti) in the order of choice are taken.
-    float bv = cm[0], lastv = INFINITY;
-#pragma unroll
-    for (int c = 1; c < NC; ++c) bv = fmaxf(bv, cm[c]);
+    // Picks.  The lanes whose best value is the token's best look up which one it is (the lowest index wins); the
+    // winner blots it out and takes its chunk's maximum again.
     // With a bias fp32 values that are too close to call are looked at again: the picks go on behind the k-th as
     // long as its value is not clearly larger, and lane p also holds the (p + LPR)-th of them.
-    int lasti = -1, picked = -1, extra = -1, held = a.k;
+    float bv = cm[0];
+#pragma unroll
+    for (int c = 1; c < NC; ++c) bv = fmaxf(bv, cm[c]);
+    int picked = -1, extra = -1, held = a.k;
     float value = -INFINITY, before = INFINITY, kth = INFINITY;
     bool near = false, more = by_bias;
-    for (int j = 0; j < a.k || (j < 2 * LPR && __any_sync(kAll, more)); ++j) {
+    for (int j = 0; j < a.k || (by_bias && j < 2 * LPR && __any_sync(kAll, more)); ++j) {
       const float gv = seg_max<LPR>(bv);
       int e = INT_MAX, bi = 0, bc = 0;
-      float left = -INFINITY;
       const bool mine = bv == gv && gv != -INFINITY;
       if (mine) {
 #pragma unroll
         for (int c = NC - 1; c >= 0; --c)
           if (cm[c] == bv) bc = c;
         float x[8];
-        chunk_values(st, lane, bc, x);
-        // taken values of the chunk lie above (lastv, lasti); the first of the rest that equals bv is the pick
+        chunk_values<W>(st, lane, bc, x);
 #pragma unroll
         for (int i = 7; i >= 0; --i)
-          if (x[i] == bv && !(x[i] == lastv && bc * 8 + i <= lasti)) bi = bc * 8 + i;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (x[i] < bv || (x[i] == bv && bc * 8 + i > bi)) left = fmaxf(left, x[i]);
+          if (x[i] == bv) bi = i;
+        bi += bc * 8;
         e = ln.expert(bi);
       }
-      int ge = seg_min<LPR>(e);
+      const int ge = seg_min<LPR>(e);
       if (by_bias) {
         const float top = j < a.k ? before : kth;
         const bool tight = gv != -INFINITY && top - gv <= 2.f * slack + 0x1p-22f * fmaxf(fabsf(top), fabsf(gv));
@@ -405,11 +518,15 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
         before = gv;
         if (j == a.k - 1) kth = gv;
       }
-      const int got = ge == INT_MAX || (j >= a.k && !more) ? -1 : ge;
+      const int got = ge == INT_MAX || (by_bias && j >= a.k && !more) ? -1 : ge;
       if (p == j) { picked = got; value = gv; }
-      if (p + LPR == j) extra = got;
+      if (by_bias && p + LPR == j) extra = got;
       if (mine && e == ge) {
-        lastv = bv; lasti = bi;
+        st[unit_at<W>(bi / 4, lane) + bi % 4] = -INFINITY;
+        float x[8], left = -INFINITY;
+        chunk_values<W>(st, lane, bc, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) left = fmaxf(left, x[i]);
         bv = -INFINITY;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -418,8 +535,8 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
         }
       }
     }
-    if (BIASED && __any_sync(kAll, near)) {
-      if (!a.sigmoid && norm64 == 0.0) norm64 = softmax_norm64<LPR, V>(row, ln, mx);
+    if (by_bias && __any_sync(kAll, near)) {
+      if (!a.sigmoid && norm64 == 0.0) norm64 = softmax_norm64<LPR, V>(row, lin, mx);
       // held picks by their 64-bit values; lane p's two are picks p and p + LPR
       auto value64 = [&](int e) -> double {
         return e < 0 ? -INFINITY : score64(usable(row[e]), a.sigmoid, mx, norm64) + (double)a.bias[e];
@@ -447,6 +564,7 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
       if (near) picked = sorted;
       // more near ties than the lanes hold: the whole row in 64 bits
       unsigned open = __ballot_sync(kAll, more && active && p == 0);
+      const bool reuse = open != 0;
       while (open) {
         const int src = __ffs(open) - 1;
         open &= open - 1;
@@ -456,6 +574,7 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
         const int ep = __shfl_sync(kAll, e, p);
         if (slot == src / LPR) picked = p < a.k ? ep : -1;
       }
+      if (reuse) blank();
     }
     if (p >= a.k) picked = -1;
     // without a bias the value that was compared is the logit
@@ -489,9 +608,8 @@ __global__ void __launch_bounds__(kRouteThreads, V == 64 && W > 1 ? (MEAN && !BI
     float* out = sums + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * a.E;
     for (int c = threadIdx.x; c < V * LPR; c += kRouteThreads) {
       const int i = c / (LPR * 4) * 4 + c % 4, pp = c / 4 % LPR;
-      RouteLane<W> o = ln;
-      o.q = pp % o.P; o.base = pp / o.P * o.size;
-      if (o.offset(i) < o.size) {
+      const RouteLane<W> o{0, pp, LPR, a.E};
+      if (o.offset(i) < a.E) {
         float s = 0.f;
 #pragma unroll
         for (int w = 0; w < kRouteWarps; ++w)
@@ -621,11 +739,11 @@ __global__ void __launch_bounds__(kRouteThreads) route_bwd_fast_kernel(const Rou
   }
 }
 
-template <typename T, int W, int LPR, int V, bool BIASED, bool MEAN>
+template <typename T, int W, int LPR, int V, int MODE, bool MEAN>
 bool launch_fwd_m(const RouteArgs& a, int G, float* sums, cudaStream_t st) {
   constexpr int regions = MEAN && V == 64 ? 2 : 1;
   constexpr int smem = regions * kRouteWarps * V * 32 * (int)sizeof(float);
-  auto kern = route_fwd_fast_kernel<T, W, LPR, V, BIASED, MEAN>;
+  auto kern = route_fwd_fast_kernel<T, W, LPR, V, MODE, MEAN>;
   if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
     cudaGetLastError();
     return false;
@@ -636,9 +754,12 @@ bool launch_fwd_m(const RouteArgs& a, int G, float* sums, cudaStream_t st) {
 }
 template <typename T, int W, int LPR, int V>
 bool launch_fwd(const RouteArgs& a, int G, float* sums, cudaStream_t st) {
-  const bool biased = a.bias || (a.groups > 1 && a.group_top == 2);
-  return biased ? (sums ? launch_fwd_m<T, W, LPR, V, true, true>(a, G, sums, st) : launch_fwd_m<T, W, LPR, V, true, false>(a, G, sums, st))
-                : (sums ? launch_fwd_m<T, W, LPR, V, false, true>(a, G, sums, st) : launch_fwd_m<T, W, LPR, V, false, false>(a, G, sums, st));
+#define GSHARD_ROUTE_MODE(MODE) \
+  (sums ? launch_fwd_m<T, W, LPR, V, MODE, true>(a, G, sums, st) : launch_fwd_m<T, W, LPR, V, MODE, false>(a, G, sums, st))
+  if (a.bias) return a.sigmoid ? GSHARD_ROUTE_MODE(kBySigmoidBias) : GSHARD_ROUTE_MODE(kBySoftmaxBias);
+  if (a.groups > 1 && a.group_top == 2) return GSHARD_ROUTE_MODE(kBySums);
+  return GSHARD_ROUTE_MODE(kByLogits);
+#undef GSHARD_ROUTE_MODE
 }
 template <typename T, int W, int LPR, int V>
 void launch_bwd(const RouteGradArgs& a, cudaStream_t st) {

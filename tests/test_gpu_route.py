@@ -336,3 +336,18 @@ def test_refusals():
     assert e.value.code == B.GSHARD_ERR_INVALID_ARG
     with pytest.raises(B.GshardError):
         B.gshard_moe_route_backward(cfg, l, idx, w, l)
+
+
+@pytest.mark.parametrize("kw", [{}, dict(groups=4, groups_kept=2), dict(score="sigmoid", groups=4, groups_kept=2, group_top=2)])
+def test_infinity_and_the_largest_float_are_equal(kw):
+    """+inf counts as the largest float, so the lower index wins between the two; NaN never does."""
+    logits = _logits(1, 64, 32, F32, seed=21)
+    logits[0, :, 5], logits[0, :, 9], logits[0, :, 2] = torch.finfo(torch.float32).max, math.inf, math.nan
+    logits[0, ::2, 13] = math.inf
+    for with_bias in (False, True):
+        bias = torch.zeros(32, device="cuda") if with_bias else None
+        cfg = B.make_route(G=1, S=64, E=32, k=3, **kw)
+        out = _route(cfg, logits, bias)
+        if kw.get("group_top", 1) == 1:                  # with sums a better pair may shut 5's group out
+            assert (out[0][..., 0] == 5).all() and (out[0][..., 1] == 9).all()
+        _check_forward(cfg, kw, logits, bias, out)
