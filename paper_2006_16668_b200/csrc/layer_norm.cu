@@ -63,17 +63,21 @@ __device__ __forceinline__ void team_sum(float (&s)[K], float* buf) {
   }
 }
 
+// How the row fills the team's packs: each thread's last pack and others may be missing; none is; only last ones are.
+// Knowing it saves a third of the instructions (selects and branches per element).
+enum LnFill { kLnAny = 0, kLnWhole = 1, kLnLast = 2 };
+#define GSHARD_LN_IN(I) (FILL == kLnWhole || (FILL == kLnLast && (I) < VPT - 1) || (I) * (int)blockDim.x + (int)threadIdx.x < packs)
+
 // The row's values stay in registers in fp32.  AHEAD: the grid is resident, and the next row is loaded (packed)
 // while the current one is worked on; up to 16 values per thread, a thread also keeps its columns' gamma and beta in
-// registers over all its rows.  WHOLE: the row fills the team's packs exactly, which saves a third of the
-// instructions (selects and branches per element).
-template <typename T, int W, int VPT, int NT, int MINB, bool AHEAD, bool WHOLE>
+// registers over all its rows.
+template <typename T, int W, int VPT, int NT, int MINB, bool AHEAD, int FILL>
 __global__ void __launch_bounds__(NT, MINB) ln_fwd_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
                                                           const float* __restrict__ beta, T* y, float* __restrict__ mean,
                                                           float* __restrict__ rstd, long long n, int M, float eps) {
   constexpr int NV = W * VPT;
   __shared__ float buf[2][32];
-  constexpr bool whole = WHOLE, KEEP = AHEAD && NV <= 16;
+  constexpr bool KEEP = AHEAD && NV <= 16;
   const int packs = M / W;
   const float inv_m = 1.f / (float)M;
   const long long stride = (long long)gridDim.x * blockDim.y;
@@ -82,7 +86,7 @@ __global__ void __launch_bounds__(NT, MINB) ln_fwd_kernel(const T* __restrict__ 
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int p = i * blockDim.x + threadIdx.x;
-      if (whole || p < packs) raw[i].load_once(x + row * M + p * W);
+      if (GSHARD_LN_IN(i)) raw[i].load_once(x + row * M + p * W);
     }
   };
   float gm[NV], bt[NV];
@@ -90,7 +94,7 @@ __global__ void __launch_bounds__(NT, MINB) ln_fwd_kernel(const T* __restrict__ 
     const int p = i * blockDim.x + threadIdx.x;
 #pragma unroll
     for (int j = 0; j < W; ++j) gm[i * W + j] = bt[i * W + j] = 0.f;
-    if (whole || p < packs) {
+    if (GSHARD_LN_IN(i)) {
       load_param<W>(gamma + p * W, gm + i * W);
       if (beta) load_param<W>(beta + p * W, bt + i * W);
     }
@@ -106,7 +110,7 @@ __global__ void __launch_bounds__(NT, MINB) ln_fwd_kernel(const T* __restrict__ 
     float v[NV], a[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      v[j] = whole || j / W * (int)blockDim.x + (int)threadIdx.x < packs ? raw[j / W].get(j % W) : 0.f;
+      v[j] = GSHARD_LN_IN(j / W) ? raw[j / W].get(j % W) : 0.f;
       a[j & 1] += v[j];
     }
     if (AHEAD && row + stride < n) fetch(row + stride);
@@ -117,7 +121,7 @@ __global__ void __launch_bounds__(NT, MINB) ln_fwd_kernel(const T* __restrict__ 
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       v[j] -= mu;
-      if (!whole && j / W * (int)blockDim.x + (int)threadIdx.x >= packs) v[j] = 0.f;     // padding stays out of the variance
+      if (!GSHARD_LN_IN(j / W)) v[j] = 0.f;     // padding stays out of the variance
       a[j & 1] = fmaf(v[j], v[j], a[j & 1]);
     }
     s[0] = a[0] + a[1];
@@ -132,7 +136,7 @@ __global__ void __launch_bounds__(NT, MINB) ln_fwd_kernel(const T* __restrict__ 
     for (int i = 0; i < VPT; ++i) {
       const int p = i * blockDim.x + threadIdx.x;
       if (!KEEP) params(i);
-      if (whole || p < packs) {
+      if (GSHARD_LN_IN(i)) {
         float o[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) o[j] = fmaf(v[i * W + j] * r, gm[i * W + j], bt[i * W + j]);
@@ -145,15 +149,14 @@ __global__ void __launch_bounds__(NT, MINB) ln_fwd_kernel(const T* __restrict__ 
 // Block b's share of the weight gradients goes to partial[b][0..M) (dgamma) and partial[b][M..2M) (dbeta).
 // A thread's columns are summed in registers, or (SUMS_IN_SMEM, rows beyond 8192 elements, where the
 // register file does not hold a row and its sums) in its own words of shared memory.  AHEAD: a team's next row
-// is loaded while it works on the current one.  WHOLE: the row fills the team's packs exactly.
-template <typename T, int W, int VPT, int NT, int MINB, bool AHEAD, bool SUMS_IN_SMEM, bool WHOLE>
+// is loaded while it works on the current one.
+template <typename T, int W, int VPT, int NT, int MINB, bool AHEAD, bool SUMS_IN_SMEM, int FILL>
 __global__ void __launch_bounds__(NT, MINB) ln_bwd_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
                                                     const float* __restrict__ mean, const float* __restrict__ rstd, const T* dy,
                                                     const T* dskip, T* dx, float* __restrict__ partial, long long n, int M) {
   constexpr int NV = W * VPT;
   extern __shared__ float sums[];              // 2 M floats: several teams in the block, or SUMS_IN_SMEM
   __shared__ float buf[2][64];
-  constexpr bool whole = WHOLE;
   const int packs = M / W;
   const float inv_m = 1.f / (float)M;
   f32x2 ag[SUMS_IN_SMEM ? 1 : NV / 2], ab[SUMS_IN_SMEM ? 1 : NV / 2];
@@ -173,7 +176,7 @@ __global__ void __launch_bounds__(NT, MINB) ln_bwd_kernel(const T* __restrict__ 
     for (int i = 0; i < VPT; ++i) {
       const int p = i * blockDim.x + threadIdx.x;
       const long long at = row * M + p * W;
-      if (whole || p < packs) {
+      if (GSHARD_LN_IN(i)) {
         vx[i].load_once(x + at);
         vd[i].load_once(dy + at);
         if (skip_too) vk[i].load_once(dskip + at);
@@ -188,8 +191,8 @@ __global__ void __launch_bounds__(NT, MINB) ln_bwd_kernel(const T* __restrict__ 
     const float m = mu, r = rs;
 #pragma unroll
     for (int j = 0; j < NV; j += 2) {
-      const bool in0 = whole || j / W * (int)blockDim.x + (int)threadIdx.x < packs;
-      const bool in1 = whole || (j + 1) / W * (int)blockDim.x + (int)threadIdx.x < packs;
+      const bool in0 = GSHARD_LN_IN(j / W);
+      const bool in1 = GSHARD_LN_IN((j + 1) / W);
       const f32x2 xx = pair(in0 ? vx[j / W].get(j % W) : m, in1 ? vx[(j + 1) / W].get((j + 1) % W) : m);
       z[j / 2] = mul2(add2(xx, both(-m)), both(r));
       g[j / 2] = pair(in0 ? vd[j / W].get(j % W) : 0.f, in1 ? vd[(j + 1) / W].get((j + 1) % W) : 0.f);
@@ -199,7 +202,7 @@ __global__ void __launch_bounds__(NT, MINB) ln_bwd_kernel(const T* __restrict__ 
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
           const int p = i * blockDim.x + threadIdx.x;
-          if (whole || p < packs) vk[i].load_once(dskip + row * M + p * W);
+          if (GSHARD_LN_IN(i)) vk[i].load_once(dskip + row * M + p * W);
         }
       }
       if (row + stride < n) fetch(row + stride, false);
@@ -211,7 +214,7 @@ __global__ void __launch_bounds__(NT, MINB) ln_bwd_kernel(const T* __restrict__ 
       const int p = i * blockDim.x + threadIdx.x;
 #pragma unroll
       for (int j = 0; j < W; ++j) gm[i * W + j] = 0.f;
-      if (whole || p < packs) load_param<W>(gamma + p * W, gm + i * W);
+      if (GSHARD_LN_IN(i)) load_param<W>(gamma + p * W, gm + i * W);
     }
 #pragma unroll
     for (int j = 0; j < NV; j += 2) {
@@ -253,7 +256,7 @@ __global__ void __launch_bounds__(NT, MINB) ln_bwd_kernel(const T* __restrict__ 
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int p = i * blockDim.x + threadIdx.x;
-      if (whole || p < packs) store_pack<T, W>(dx + row * M + p * W, dxv + i * W);
+      if (GSHARD_LN_IN(i)) store_pack<T, W>(dx + row * M + p * W, dxv + i * W);
     }
   }
   if (!partial) return;
@@ -334,6 +337,10 @@ int ln_width(int M, int esize) {
   return w;
 }
 
+int ln_fill(int packs, int team, int vpt) {
+  return packs == team * vpt ? kLnWhole : packs >= team * (vpt - 1) ? kLnLast : kLnAny;
+}
+
 struct LnShape { int team, teams, nv; };   // threads per row, rows side by side in a block, values per thread
 
 // Forward: one warp per row up to 1024 elements, with 8, 16 or 32 values per thread and no barrier; else a block
@@ -370,16 +377,14 @@ int ln_fwd_launch(long long n, int M, float eps, const T* x, const float* gamma,
   const int threads = s.team * s.teams;
   const bool ahead = threads <= 768 && s.nv < 32 && all > kLnSms * 4;
   const int grid = (int)std::min<long long>(all, ahead ? kLnSms * std::max(1, 768 / threads) : 1ll << 30);
-  const bool whole = M == s.team * s.nv;
-#define GSHARD_LN(NV, NT, MINB, AHEAD)                                                                              \
-  do {                                                                                                              \
-    if constexpr (W >= 4) {                                                                                         \
-      if (whole) {                                                                                                  \
-        ln_fwd_kernel<T, W, NV / W, NT, MINB, AHEAD, true><<<grid, block, 0, st>>>(x, gamma, beta, y, mean, rstd, n, M, eps); \
-        break;                                                                                                      \
-      }                                                                                                             \
-    }                                                                                                               \
-    ln_fwd_kernel<T, W, NV / W, NT, MINB, AHEAD, false><<<grid, block, 0, st>>>(x, gamma, beta, y, mean, rstd, n, M, eps); \
+  const int fill = ln_fill(M / W, s.team, s.nv / W);
+#define GSHARD_LN_F(NV, NT, MINB, AHEAD, FILL) \
+  ln_fwd_kernel<T, W, NV / W, NT, MINB, AHEAD, FILL><<<grid, block, 0, st>>>(x, gamma, beta, y, mean, rstd, n, M, eps)
+#define GSHARD_LN(NV, NT, MINB, AHEAD)                                                  \
+  do {                                                                                  \
+    if (W >= 4 && fill == kLnWhole) GSHARD_LN_F(NV, NT, MINB, AHEAD, (W >= 4 ? kLnWhole : kLnAny)); \
+    else if (fill != kLnAny) GSHARD_LN_F(NV, NT, MINB, AHEAD, kLnLast);                 \
+    else GSHARD_LN_F(NV, NT, MINB, AHEAD, kLnAny);                                      \
   } while (0)
   if (ahead && threads <= 128) { if (s.nv == 16) GSHARD_LN(16, 128, 6, true); else GSHARD_LN(8, 128, 6, true); }
   else if (ahead) GSHARD_LN(16, 768, 1, true);
@@ -387,6 +392,7 @@ int ln_fwd_launch(long long n, int M, float eps, const T* x, const float* gamma,
   else if (s.nv == 16) GSHARD_LN(16, 1024, 1, false);
   else GSHARD_LN(8, 1024, 1, false);
 #undef GSHARD_LN
+#undef GSHARD_LN_F
   count_launch();
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
 }
@@ -399,10 +405,10 @@ int ln_bwd_launch(long long n, int M, const T* x, const float* gamma, const floa
   const int grid = ln_bwd_blocks(n, M, (int)sizeof(T));
   const bool sums_in_smem = M > 8192;
   const int smem = partial && (s.teams > 1 || sums_in_smem) ? 2 * M * (int)sizeof(float) : 0;
-  const bool whole = M == s.team * s.nv;
-#define GSHARD_LN_W(NV, NT, MINB, AHEAD, SMEM, WHOLE)                                                                 \
+  const int fill = ln_fill(M / W, s.team, s.nv / W);
+#define GSHARD_LN_F(NV, NT, MINB, AHEAD, SMEM, FILL)                                                                  \
   do {                                                                                                                \
-    auto kern = ln_bwd_kernel<T, W, NV / W, NT, MINB, AHEAD, SMEM, WHOLE>;                                            \
+    auto kern = ln_bwd_kernel<T, W, NV / W, NT, MINB, AHEAD, SMEM, FILL>;                                             \
     if (smem > 48 * 1024 &&                                                                                           \
         cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {               \
       cudaGetLastError();                                                                                             \
@@ -412,18 +418,17 @@ int ln_bwd_launch(long long n, int M, const T* x, const float* gamma, const floa
   } while (0)
 #define GSHARD_LN(NV, NT, MINB, AHEAD, SMEM)                                                                          \
   do {                                                                                                                \
-    if constexpr (W * sizeof(T) == 16) {                                                                              \
-      if (whole) { GSHARD_LN_W(NV, NT, MINB, AHEAD, SMEM, true); break; }                                             \
-    }                                                                                                                 \
-    GSHARD_LN_W(NV, NT, MINB, AHEAD, SMEM, false);                                                                    \
+    if (W >= 4 && fill == kLnWhole) GSHARD_LN_F(NV, NT, MINB, AHEAD, SMEM, (W >= 4 ? kLnWhole : kLnAny));             \
+    else if (fill != kLnAny) GSHARD_LN_F(NV, NT, MINB, AHEAD, SMEM, kLnLast);                                         \
+    else GSHARD_LN_F(NV, NT, MINB, AHEAD, SMEM, kLnAny);                                                              \
   } while (0)
   if (sums_in_smem) GSHARD_LN(16, 1024, 1, false, true);
   else if (s.nv == 16) { if constexpr (sizeof(T) == 2) GSHARD_LN(16, 512, 1, true, false); }
   else if (s.team * s.teams <= 128) GSHARD_LN(8, 128, 5, true, false);
   else if (s.team <= 640) GSHARD_LN(8, 640, 1, true, false);
   else GSHARD_LN(8, 1024, 1, false, false);
-#undef GSHARD_LN_W
 #undef GSHARD_LN
+#undef GSHARD_LN_F
   count_launch();
   if (partial) {
     ln_bwd_finish_kernel<<<ceil_div(2 * M, 8), 256, 0, st>>>(partial, grid, M, dgamma, dbeta);
