@@ -69,15 +69,15 @@ enum LnFill { kLnAny = 0, kLnWhole = 1, kLnLast = 2 };
 #define GSHARD_LN_IN(I) (FILL == kLnWhole || (FILL == kLnLast && (I) < VPT - 1) || (I) * (int)blockDim.x + (int)threadIdx.x < packs)
 
 // The row's values stay in registers in fp32.  AHEAD: the grid is resident, and the next row is loaded (packed)
-// while the current one is worked on; up to 16 values per thread, a thread also keeps its columns' gamma and beta in
-// registers over all its rows.
+// while the current one is worked on; in blocks of less than 1024 threads a thread also keeps its columns' gamma and
+// beta in registers over all its rows (NT = 1024: 64 registers, so that two rows' blocks share a multiprocessor).
 template <typename T, int W, int VPT, int NT, int MINB, bool AHEAD, int FILL>
 __global__ void __launch_bounds__(NT, MINB) ln_fwd_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
                                                           const float* __restrict__ beta, T* y, float* __restrict__ mean,
                                                           float* __restrict__ rstd, long long n, int M, float eps) {
   constexpr int NV = W * VPT;
   __shared__ float buf[2][32];
-  constexpr bool KEEP = AHEAD && NV <= 16;
+  constexpr bool KEEP = AHEAD && NV <= 16 && NT < 1024;
   const int packs = M / W;
   const float inv_m = 1.f / (float)M;
   const long long stride = (long long)gridDim.x * blockDim.y;
@@ -375,8 +375,8 @@ int ln_fwd_launch(long long n, int M, float eps, const T* x, const float* gamma,
   const dim3 block(s.team, s.teams);
   const long long all = (n + s.teams - 1) / s.teams;
   const int threads = s.team * s.teams;
-  const bool ahead = threads <= 768 && s.nv < 32 && all > kLnSms * 4;
-  const int grid = (int)std::min<long long>(all, ahead ? kLnSms * std::max(1, 768 / threads) : 1ll << 30);
+  const bool ahead = s.nv < 32 && all > kLnSms * 4, wide = threads > 384;
+  const int grid = (int)std::min<long long>(all, ahead ? kLnSms * std::max(1, (wide ? 1024 : 768) / threads) : 1ll << 30);
   const int fill = ln_fill(M / W, s.team, s.nv / W);
 #define GSHARD_LN_F(NV, NT, MINB, AHEAD, FILL) \
   ln_fwd_kernel<T, W, NV / W, NT, MINB, AHEAD, FILL><<<grid, block, 0, st>>>(x, gamma, beta, y, mean, rstd, n, M, eps)
@@ -387,7 +387,8 @@ int ln_fwd_launch(long long n, int M, float eps, const T* x, const float* gamma,
     else GSHARD_LN_F(NV, NT, MINB, AHEAD, kLnAny);                                      \
   } while (0)
   if (ahead && threads <= 128) { if (s.nv == 16) GSHARD_LN(16, 128, 6, true); else GSHARD_LN(8, 128, 6, true); }
-  else if (ahead) GSHARD_LN(16, 768, 1, true);
+  else if (ahead && !wide) GSHARD_LN(16, 384, 2, true);
+  else if (ahead) GSHARD_LN(16, 1024, 1, true);
   else if (s.nv == 32) GSHARD_LN(32, 128, 8, false);
   else if (s.nv == 16) GSHARD_LN(16, 1024, 1, false);
   else GSHARD_LN(8, 1024, 1, false);
@@ -472,10 +473,11 @@ int gshard_layer_norm_forward(int64_t n_rows, int32_t M, int32_t dtype, float ep
   NvtxRange range("gshard.layer_norm");
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   int w = ln_width(M, dtype == GSHARD_BF16 ? 2 : 4);
-  // With 32 values per thread gamma and beta are read again for every row, four times the bytes of a bf16 row: at
-  // 4 columns per lane their loads are whole 512-byte lines of L1, at 8 they take twice the passes (106 us
-  // at 131072 x 1024, L1 90 % busy).
-  if (ln_fwd_shape(n_rows, M).nv == 32) w = std::min(w, 4);
+  // Where gamma and beta are read again for every row (32 values per thread, or blocks too large to keep them in
+  // registers), they are four times the bytes of a bf16 row: at 4 columns per lane their loads are whole 512-byte
+  // passes of L1, at 8 they take twice as many (131072 x 1024: 106 against 97 us, L1 90 % busy).
+  const LnShape shape = ln_fwd_shape(n_rows, M);
+  if (shape.nv == 32 || shape.team > 384) w = std::min(w, 4);
 #define GSHARD_LN_FWD(T, W) ln_fwd_launch<T, W>(n_rows, M, eps, static_cast<const T*>(x), gamma, beta, static_cast<T*>(y), mean, rstd, st)
   if (dtype == GSHARD_BF16)
     return w == 8 ? GSHARD_LN_FWD(__nv_bfloat16, 8) : w == 4 ? GSHARD_LN_FWD(__nv_bfloat16, 4)

@@ -234,8 +234,8 @@ int linear_validate(int64_t n, int32_t K, int32_t cols, int32_t dtype, int32_t o
   if (out_dtype != GSHARD_F32 && out_dtype != dtype) return GSHARD_ERR_INVALID_ARG;
   if (K % 8 || cols % 8 || K > (1 << 24) || cols > (1 << 24)) return GSHARD_ERR_UNSUPPORTED_SHAPE;
   // a tensor map's strides; tile counts in 31 bits
-  if (n > (1ll << 30) || n * std::max(K, cols) >= (1ll << 37)) return GSHARD_ERR_UNSUPPORTED_SHAPE;
-  if (((n + 127) / 128) * ((long long)(std::max(K, cols) + 127) / 128) >= (1ll << 30)) return GSHARD_ERR_UNSUPPORTED_SHAPE;
+  if (n > (1ll << 30) || n * std::max(K, cols) >= (1ll << 37) || (long long)K * cols >= (1ll << 37)) return GSHARD_ERR_UNSUPPORTED_SHAPE;
+  if (((std::max<long long>(n, K) + 127) / 128) * ((long long)(std::max(K, cols) + 127) / 128) >= (1ll << 30)) return GSHARD_ERR_UNSUPPORTED_SHAPE;
   return GSHARD_OK;
 }
 

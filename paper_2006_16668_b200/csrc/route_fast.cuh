@@ -147,13 +147,14 @@ route_fwd_fast_kernel(const __grid_constant__ RouteArgs a, float* __restrict__ s
   const bool need_sum = !STREAM && !a.sigmoid && (MEAN || !a.renorm || BIASED);
   const int t0 = blockIdx.x * kRouteTile, t1 = min(a.S, t0 + kRouteTile);
   const long long first = (long long)blockIdx.y * a.S;
-  const int per_group = ln.size / W;          // vectors of a group; g = vi / per_group by a reciprocal, exact for vi < 2^10
-  const int recip = ((1 << 20) + per_group - 1) / per_group, lg = __ffs(ln.P) - 1;
+  // group of vector vi: vi / per_group by a 32-bit reciprocal (exact while vi * per_group < 2^32; 1 divides nothing)
+  const unsigned per_group = ln.size / W, recip = 0xffffffffu / per_group + 1u;
+  const int lg = __ffs(ln.P) - 1;
   // a vector of this lane to where its owner looks for it
   auto stage = [&](int j, const float* x, bool moves) {
     int unit = j * W / 4, to = lane, comp = j * W % 4;
     if (moves) {
-      const int vi = j * LPR + p, g = (vi * recip) >> 20, r = vi - g * per_group;
+      const int vi = j * LPR + p, g = per_group == 1 ? vi : (int)__umulhi((unsigned)vi, recip), r = vi - g * (int)per_group;
       to = slot * LPR + (g << lg) + (r & (ln.P - 1));
       const int i = (r >> lg) * W;
       unit = i / 4; comp = i % 4;

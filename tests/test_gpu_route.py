@@ -110,6 +110,10 @@ CASES = [
     (2, 30, 513, 32, {}), (1, 40, 1024, 16, dict(score="sigmoid", groups=32, groups_kept=7, group_top=2)),
     (2, 40, 2048, 2, dict(renormalise=False)), (1, 12, 2046, 9, dict(groups=31, groups_kept=30)),
     (1, 9, 3000, 4, {}), (1, 5, 16384, 8, dict(score="sigmoid")), (1, 30, 32, 32, {}), (1, 30, 32, 32, dict(score="sigmoid")),
+    (1, 20, 2046, 5, dict(groups=2, groups_kept=1)), (2, 9, 2044, 3, dict(groups=2, groups_kept=1, group_top=2)),
+    (1, 30, 1022, 4, dict(score="sigmoid", groups=2, groups_kept=1)), (1, 33, 128, 6, dict(groups=16, groups_kept=5)),
+    (1, 2400, 64, 4, dict(groups=8, groups_kept=3)), (1, 2400, 60, 3, dict(score="sigmoid", groups=4, groups_kept=2, group_top=2)),
+    (1, 2500, 200, 7, dict(groups=2, groups_kept=1)), (1, 2370, 24, 5, dict(score="sigmoid")),
     (1, 700, 64, 1, {}), (4, 300, 32, 4, dict(groups=16, groups_kept=9, group_top=2)), (1, 50, 64, 5, dict(groups=32, groups_kept=16)),
 ]
 
