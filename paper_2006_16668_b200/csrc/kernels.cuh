@@ -103,9 +103,12 @@ struct UmmaGemm {
                              // multiprocessors to a kernel running beside this one on another stream
   int splits;                // > 1: the contraction is cut into `splits` runs of whole k-blocks (batch 1); run i writes
                              // its partial product to C + i * c_bs (fp32), and the caller adds them
-  int planes;                // A and B are three bf16 planes each (batch strides a_bs, b_bs) whose sum is the fp32 operand:
-                             // the six products of planes that reach 2^-16 are added up, small ones first
-  const LinearEpilogue* linear;   // a_kmajor, !b_kmajor, batch 1: the linear operator's epilogue instead of relu / masks
+  int planes_a, planes_b;    // 0 (plain operands), or the operands are sums of so many bf16 planes (batch strides a_bs, b_bs):
+                             // 2 and 1, 1 and 2, or 3 and 3 (fp32 values; fp32 output; takes `linear`)
+  int runs;                  // fp32 accuracy: accumulate in short runs (three planes always; plain operands with `linear` and
+                             // fp32 output)
+  const LinearEpilogue* linear;   // batch 1; a_kmajor, !b_kmajor unless 3 planes: the linear operator's epilogue instead of
+                             // relu / masks
 };
 int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st);
 // umma2_gemm.cu: the same contraction with the two-SM MMA (CTA pairs, 256 x 256 tiles).

@@ -6,7 +6,9 @@
 //
 // bf16: the matrix products run on the tcgen05 GEMMs of the expert FFN (CTA pairs from 129 rows on); the
 // forward's epilogue adds the bias, keeps pre, activates and adds the residual on the fp32 accumulator.
-// dpre is rounded to bf16 once, as the operand of both gradient products; dbias sums it before the rounding.
+// dpre is rounded to bf16 once, as the operand of both gradient products (exact with no activation or relu on 16-bit
+// dy); dbias sums it before the rounding.  Small products, whose time is launches, take what the rounding left as a
+// second plane and a second pass, which halves the error of dx and dw to that of their own rounding.
 // A product with too few output tiles for the multiprocessors is cut along the contraction into runs whose
 // fp32 partial products a second kernel adds in order.
 // fp32: an fp32 value is the exact sum of three bf16 values (8 bits of its 24 each), so x . w is six bf16 products
@@ -68,11 +70,12 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const float* __restri
 
 // dpre = dy act'(pre) rounded to bf16 (where wanted), and the chunk's column sums of dpre before the rounding.
 // A block covers 32 x 8 columns and one chunk of rows; a thread owns 8 columns and every 8th row, four of
-// them in flight: the pass is bound by HBM (dy and pre in, dpre out).  PLANES: dpre as three bf16 planes.
-template <typename TY, bool PLANES, int ACT>
+// them in flight: the pass is bound by HBM (dy and pre in, dpre out).  PLANES: bf16 planes that dpre is
+// written as: 3 (fp32), 2 (rounded, and what the rounding left) or 1.
+template <typename TY, int PLANES, int ACT>
 __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__ dy, const TY* __restrict__ pre, __nv_bfloat16* dpre,
                                                           float* __restrict__ partial, long long n, int cols, int chunk) {
-  constexpr bool FAST = !PLANES;
+  constexpr bool FAST = PLANES < 3;
   constexpr int U = sizeof(TY) == 2 ? 4 : 2;              // rows in flight
   constexpr int PW = 16 / (int)sizeof(TY), PN = 8 / PW;    // packs of 16 bytes per 8 columns
   __shared__ float part[8][256 + 8];
@@ -112,7 +115,13 @@ __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__
           }
           if (dpre) {
             const long long off = (r0 + 8 * u) * cols + col;
-            if (PLANES) {
+            if (PLANES == 2) {
+              float hi[8], lo[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) { hi[j] = __bfloat162float(__float2bfloat16_rn(d[j])); lo[j] = d[j] - hi[j]; }
+              store_pack<__nv_bfloat16, 8>(dpre + off, hi);
+              store_pack<__nv_bfloat16, 8>(dpre + n * cols + off, lo);
+            } else if (PLANES == 3) {
               float hi[8], mid[8], lo[8];
               split3(d, hi, mid, lo, 8);
               store_pack<__nv_bfloat16, 8>(dpre + off, hi);
@@ -139,7 +148,7 @@ __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__
   }
 }
 
-template <typename TY, bool PLANES>
+template <typename TY, int PLANES>
 void launch_dpre(const void* dy, const void* pre, void* dpre, float* partial, long long n, int cols, int chunk, int chunks, int act,
                  cudaStream_t st) {
   const dim3 grid(ceil_div(cols, 256), chunks);
@@ -198,7 +207,7 @@ int splits_for(long long rows, int cols, long long depth) {
 // Rows up to which w streams through the CUDA cores (linear_few.cu) instead of the tensor cores.
 bool few_rows(int64_t n) { return n <= 8; }
 
-struct LinearPlan { size_t status, xp, wp, dpre, colsum, join, total; int chunks, chunk, splits, dx_splits, dw_splits; };
+struct LinearPlan { size_t status, xp, wp, dpre, colsum, join, total; int planes, chunks, chunk, splits, dx_splits, dw_splits; };
 
 LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, bool backward) {
   Carver c;
@@ -214,7 +223,9 @@ LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, bool backward) {
     p.total = c.off;
     return p;
   }
-  p.dpre = c.take((size_t)n * cols * (bf16 ? 2 : 6));
+  // a second pass of a product below 2^32 operations takes at most about 3 us
+  p.planes = !bf16 ? 3 : 2.0 * n * K * cols <= 4294967296.0 ? 2 : 1;
+  p.dpre = c.take((size_t)n * cols * 2 * p.planes);
   const int col_blocks = ceil_div(cols, 256);
   const long long want = std::max(1, kSms * 8 / col_blocks);                // row chunks that give every multiprocessor 8 blocks
   p.chunk = (int)std::max<long long>(32, (n + want - 1) / want);
@@ -252,13 +263,14 @@ void split_planes(const void* src, void* dst, long long n, cudaStream_t st) {
 
 // C = A . B, cut into `splits` runs through the fp32 partial products in `join`
 int gemm_joined(const Dims& d, UmmaGemm g, int splits, float* join, int* status, cudaStream_t st) {
+  const LinearEpilogue none{};
+  if (g.planes_a == 3) { g.linear = &none; g.runs = 1; }
   if (splits <= 1) return run_gemm(d, g, status, st);
   void* out = g.C;
   const bool out_f32 = g.out_f32 != 0;
   const long long n4 = (long long)g.rows * g.cols / 4;
   g.C = join; g.out_f32 = 1; g.splits = splits; g.c_bs = (long long)g.rows * g.cols;
   GS_CHECK(run_gemm(d, g, status, st));
-  const LinearEpilogue none{};
   const float4* partial = reinterpret_cast<const float4*>(join);
   if (out_f32) linear_finish_kernel<float><<<stride_grid(n4), 256, 0, st>>>(partial, splits, none, out, n4, g.cols / 4);
   else linear_finish_kernel<__nv_bfloat16><<<stride_grid(n4), 256, 0, st>>>(partial, splits, none, out, n4, g.cols / 4);
@@ -317,13 +329,16 @@ int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype
   if (dtype == GSHARD_F32) {
     split_planes(x, ws + pl.xp, n_rows * K, st);
     split_planes(w, ws + pl.wp, (long long)K * cols, st);
-    g.A = ws + pl.xp; g.B = ws + pl.wp; g.planes = 1; g.a_bs = n_rows * K; g.b_bs = (long long)K * cols; g.a_stream = 0;
+    g.A = ws + pl.xp; g.B = ws + pl.wp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * K; g.b_bs = (long long)K * cols; g.a_stream = 0;
   }
+  g.runs = out_f32;
   if (pl.splits == 1) {
     g.linear = &lin;
     GS_CHECK(run_gemm(d, g, status, st));
   } else {
     const long long n4 = n_rows * cols / 4;
+    const LinearEpilogue none{};
+    if (g.runs) g.linear = &none;
     g.C = ws + pl.join; g.out_f32 = 1; g.splits = pl.splits; g.c_bs = n_rows * cols;
     GS_CHECK(run_gemm(d, g, status, st));
     const float4* partial = reinterpret_cast<const float4*>(ws + pl.join);
@@ -364,12 +379,17 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
   GS_CHECK(zero(status, sizeof(int), st));
   const bool fp32 = dtype == GSHARD_F32;
   const bool convert = fp32 || activation != GSHARD_ACT_NONE || out_dtype != dtype;    // else dpre is dy itself
+  // dy times 0 or 1 needs no second plane
+  const bool exact = out_dtype == dtype && (activation == GSHARD_ACT_NONE || activation == GSHARD_ACT_RELU);
+  const int planes = !fp32 && exact ? 1 : pl.planes;
   void* buf = convert && (dx || dw) ? ws + pl.dpre : nullptr;
   float* colsum = dbias ? reinterpret_cast<float*>(ws + pl.colsum) : nullptr;
   if (buf || colsum) {
-    if (fp32) launch_dpre<float, true>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
-    else if (out_dtype == GSHARD_F32) launch_dpre<float, false>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
-    else launch_dpre<__nv_bfloat16, false>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st);
+#define GSHARD_DPRE(TY, P) launch_dpre<TY, P>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st)
+    if (planes == 3) GSHARD_DPRE(float, 3);
+    else if (out_dtype == GSHARD_F32) { if (planes == 2) GSHARD_DPRE(float, 2); else GSHARD_DPRE(float, 1); }
+    else { if (planes == 2) GSHARD_DPRE(__nv_bfloat16, 2); else GSHARD_DPRE(__nv_bfloat16, 1); }
+#undef GSHARD_DPRE
     if (dbias) {
       linear_dbias_kernel<<<ceil_div(cols, 32), 256, 0, st>>>(colsum, dbias, pl.chunks, cols);
       count_launch();
@@ -385,7 +405,9 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
     g.prefer_two_sm = 1; g.out_f32 = fp32;
     if (fp32) {
       split_planes(w, ws + pl.wp, (long long)K * cols, st);
-      g.B = ws + pl.wp; g.planes = 1; g.a_bs = n_rows * cols; g.b_bs = (long long)K * cols;
+      g.B = ws + pl.wp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * cols; g.b_bs = (long long)K * cols;
+    } else if (planes == 2) {
+      g.planes_a = 2; g.planes_b = 1; g.a_bs = n_rows * cols;
     }
     GS_CHECK(gemm_joined(d, g, pl.dx_splits, join, status, st));
   }
@@ -396,7 +418,9 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
     g.prefer_two_sm = 1; g.out_f32 = fp32;
     if (fp32) {
       split_planes(x, ws + pl.xp, n_rows * K, st);
-      g.A = ws + pl.xp; g.planes = 1; g.a_bs = n_rows * K; g.b_bs = n_rows * cols;
+      g.A = ws + pl.xp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * K; g.b_bs = n_rows * cols;
+    } else if (planes == 2) {
+      g.planes_a = 1; g.planes_b = 2; g.b_bs = n_rows * cols;
     }
     GS_CHECK(gemm_joined(d, g, pl.dw_splits, join, status, st));
   }

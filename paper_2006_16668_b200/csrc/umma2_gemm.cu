@@ -61,7 +61,7 @@ struct Params2 {
   int* status;
   int tma_store;   // epilogue rows leave by bulk tensor stores through map_c
   int split;       // batch index = run of k_blocks k-blocks of the one problem (operands have no batch)
-  int passes;      // 1, or 6 with planes: every tile runs its k-blocks once per product of planes
+  int passes, pass_a, pass_b;   // operands in planes: every tile runs its k-blocks once per product (plane numbers in nibbles)
   LinearEpilogue lin;   // LIN instantiations only
   // Ragged batches (compacted expert rows): problem b owns the 256-row tiles [tile_base[b], tile_base[b+1])
   // of a device-side prefix array with batch + 1 entries; nullptr = every problem has m_tiles row tiles.
@@ -82,8 +82,9 @@ __device__ __forceinline__ TileCoord decode(const Params2& p, int tile) {
   return t;
 }
 
-// LIN: the linear operator's epilogue (map_pre: tensor map of the kept pre-activations).
-template <bool A_K, bool B_K, bool MASK, bool LIN = false>
+// LIN: the linear operator's epilogue (map_pre: tensor map of the kept pre-activations).  RUNS: accumulated run by
+// run into the epilogue warps' registers (umma_epilogue.cuh), with fp32 operands in three planes each.
+template <bool A_K, bool B_K, bool MASK, bool LIN = false, bool RUNS = false>
 __global__ void __launch_bounds__(kThreads, 1)
 umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                   const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_pre, const Params2 p) {
@@ -136,7 +137,7 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         const int kfirst = p.split ? t.b * p.k_blocks : 0, ob = p.split ? 0 : t.b;
         const int iters = p.k_blocks * p.passes;
         for (int it = 0, kb = 0, pass = 0; it < iters; ++it) {
-          const int oa = p.passes > 1 ? plane_of_a(pass) : ob, obb = p.passes > 1 ? plane_of_b(pass) : ob;
+          const int oa = p.passes > 1 ? plane_of(p.pass_a, pass) : ob, obb = p.passes > 1 ? plane_of(p.pass_b, pass) : ob;
           if (!ptx::mbar_wait(empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
           unsigned char* sa = smem + stage * kStageBytes;
           unsigned char* sb = sa + kABytes;
@@ -170,28 +171,32 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
       int acc = 0; uint32_t acc_phase = 0;
       const int total_tiles = total_tiles_of(p);
       for (int tile = pair; tile < total_tiles && ok; tile += n_pairs) {
-        if (!ptx::mbar_wait(acc_empty + acc, acc_phase ^ 1u, abort_flag)) { ok = false; break; }
-        ptx::tc_fence_after_sync();
-        const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
-        for (int kb = 0; kb < p.k_blocks * p.passes; ++kb) {
-          if (!ptx::mbar_wait(full + stage, phase, abort_flag)) { ok = false; break; }
+        const int runs = RUNS ? all_runs(p.k_blocks, p.passes) : 1;
+        for (int run = 0; run < runs && ok; ++run) {
+          if (!ptx::mbar_wait(acc_empty + acc, acc_phase ^ 1u, abort_flag)) { ok = false; break; }
           ptx::tc_fence_after_sync();
-          const uint32_t sa = ptx::smem_u32(smem + stage * kStageBytes);
-          const uint32_t sb = sa + kABytes;
-#pragma unroll
-          for (int k = 0; k < BK / 16; ++k) {
-            const uint64_t da = A_K ? ptx::make_smem_desc(sa + k * 32, 16, 1024)
-                                    : ptx::make_smem_desc(sa + k * 2048, kBoxBytes, 1024);
-            const uint64_t db = B_K ? ptx::make_smem_desc(sb + k * 32, 16, 1024)
-                                    : ptx::make_smem_desc(sb + k * 2048, kBoxBytes, 1024);
-            ptx::umma_bf16_pair(d_tmem, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
+          const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
+          const int len = RUNS ? run_length(run, p.k_blocks, p.passes) : p.k_blocks * p.passes;
+          for (int kb = 0; kb < len; ++kb) {
+            if (!ptx::mbar_wait(full + stage, phase, abort_flag)) { ok = false; break; }
+            ptx::tc_fence_after_sync();
+            const uint32_t sa = ptx::smem_u32(smem + stage * kStageBytes);
+            const uint32_t sb = sa + kABytes;
+  #pragma unroll
+            for (int k = 0; k < BK / 16; ++k) {
+              const uint64_t da = A_K ? ptx::make_smem_desc(sa + k * 32, 16, 1024)
+                                      : ptx::make_smem_desc(sa + k * 2048, kBoxBytes, 1024);
+              const uint64_t db = B_K ? ptx::make_smem_desc(sb + k * 32, 16, 1024)
+                                      : ptx::make_smem_desc(sb + k * 2048, kBoxBytes, 1024);
+              ptx::umma_bf16_pair(d_tmem, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
+            }
+            ptx::umma_commit_pair(empty + stage);             // stage free in both CTAs
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
-          ptx::umma_commit_pair(empty + stage);             // stage free in both CTAs
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          if (!ok) break;
+          ptx::umma_commit_pair(acc_full + acc);              // accumulator complete in both CTAs
+          if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         }
-        if (!ok) break;
-        ptx::umma_commit_pair(acc_full + acc);              // accumulator complete in both CTAs
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
     }
   } else {
@@ -207,6 +212,22 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
       const TileCoord t = tn;
       if (tile + n_pairs < total_tiles) tn = decode(p, tile + n_pairs);
       const int tile_row0 = t.mt * 2 * BM + (int)rank * BM;     // this CTA's 128 rows of the 256-row tile
+      if constexpr (RUNS) {
+        uint32_t sums[BN / 64][32];
+        const int runs = all_runs(p.k_blocks, p.passes);
+        for (int run = 0; run < runs; ++run) {
+          if (!ptx::mbar_wait_warp(acc_full + acc, acc_phase, abort_flag, lane)) { ok = false; break; }
+          ptx::tc_fence_after_sync();
+          add_run<BN>(sums, tmem_base + (uint32_t)(acc * BN), q, half, run == 0);
+          ptx::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive_remote_relaxed(ptx::map_to_cta(ptx::smem_u32(acc_empty + acc), 0));
+          if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+        if (!ok) break;
+        epilogue_linear_sums<BN>(p, &map_c, &map_pre, t, tile_row0, sums, q, half, stg, lane);
+        continue;
+      }
       if (!ptx::mbar_wait_warp(acc_full + acc, acc_phase, abort_flag, lane)) { ok = false; break; }
       ptx::tc_fence_after_sync();
       if constexpr (LIN)
@@ -457,10 +478,10 @@ int launch2_resident_b(const CUtensorMap& ma, const CUtensorMap& mb, const CUten
   return GSHARD_OK;
 }
 
-template <bool A_K, bool B_K, bool MASK, bool LIN = false>
+template <bool A_K, bool B_K, bool MASK, bool LIN = false, bool RUNS = false>
 int launch2_t(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const Params2& p, int pairs,
               cudaStream_t st, const CUtensorMap* mp = nullptr) {
-  auto kern = umma2_gemm_kernel<A_K, B_K, MASK, LIN>;
+  auto kern = umma2_gemm_kernel<A_K, B_K, MASK, LIN, RUNS>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
     return GSHARD_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
@@ -489,11 +510,11 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   if ((g.mask_bits || g.mask_bits_out) && g.cols % 32) return GSHARD_ERR_INTERNAL;   // one word per 32 columns
   CUtensorMap ma, mb;
   bool okm;
-  const int problems = g.planes ? 3 : g.batch;
-  if (g.a_kmajor) okm = make_map(&ma, g.A, g.K, g.rows, problems, g.a_ld, g.a_bs, BK, BM);
-  else            okm = make_map(&ma, g.A, g.rows, g.K, problems, g.a_ld, g.a_bs, 64, BK);
-  if (g.b_kmajor) okm = okm && make_map(&mb, g.B, g.K, g.cols, problems, g.b_ld, g.b_bs, BK, BNH);
-  else            okm = okm && make_map(&mb, g.B, g.cols, g.K, problems, g.b_ld, g.b_bs, 64, BK);
+  const int a_maps = g.planes_a > 0 ? g.planes_a : g.batch, b_maps = g.planes_b > 0 ? g.planes_b : g.batch;
+  if (g.a_kmajor) okm = make_map(&ma, g.A, g.K, g.rows, a_maps, g.a_ld, g.a_bs, BK, BM);
+  else            okm = make_map(&ma, g.A, g.rows, g.K, a_maps, g.a_ld, g.a_bs, 64, BK);
+  if (g.b_kmajor) okm = okm && make_map(&mb, g.B, g.K, g.cols, b_maps, g.b_ld, g.b_bs, BK, BNH);
+  else            okm = okm && make_map(&mb, g.B, g.cols, g.K, b_maps, g.b_ld, g.b_bs, 64, BK);
   if (!okm) return GSHARD_ERR_CUDA;
   CUtensorMap mc;
   const bool tma_store = store_map_for(g, &mc);
@@ -505,10 +526,15 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   p.total_tiles = p.m_tiles * p.n_tiles * g.batch;
   p.k_blocks = ceil_div(g.K, BK);
   p.split = 0;
-  p.passes = g.planes ? 6 : 1;
-  if (g.planes && (g.batch != 1 || g.tile_base || !g.out_f32 || g.mask_bits || g.mask_bits_out)) return GSHARD_ERR_INTERNAL;
+  const bool planes = g.planes_a > 0, planes3 = g.planes_a == 3, in_runs = planes3 || g.runs;
+  p.passes = planes3 ? kPasses3 : planes ? 2 : 1;
+  p.pass_a = planes3 ? kPassA3 : g.planes_a == 2 ? 0x01 : 0;       // two planes: the low one first
+  p.pass_b = planes3 ? kPassB3 : g.planes_b == 2 ? 0x01 : 0;
+  if (planes && (g.batch != 1 || g.tile_base || g.mask_bits || g.mask_bits_out)) return GSHARD_ERR_INTERNAL;
+  if (planes3 && g.planes_b != 3) return GSHARD_ERR_INTERNAL;
+  if (in_runs && (!g.out_f32 || !g.linear || (planes && !planes3))) return GSHARD_ERR_INTERNAL;
   if (g.splits > 1) {
-    if (g.batch != 1 || !g.out_f32 || g.tile_base || g.linear || g.mask_bits || g.mask_bits_out) return GSHARD_ERR_INTERNAL;
+    if (g.batch != 1 || !g.out_f32 || g.tile_base || (g.linear && !in_runs) || g.mask_bits || g.mask_bits_out) return GSHARD_ERR_INTERNAL;
     p.split = 1; p.batch = g.splits; p.total_tiles = p.m_tiles * p.n_tiles * g.splits; p.k_blocks = ceil_div(p.k_blocks, g.splits);
   }
   p.out_f32 = g.out_f32; p.relu = g.relu; p.a_stream = g.a_stream; p.b_stream = g.b_stream;
@@ -521,7 +547,7 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   const int sms = device_sms();
   int pairs = sms / 2;
   if (g.max_ctas > 0 && pairs > g.max_ctas / 2) pairs = g.max_ctas / 2 > 0 ? g.max_ctas / 2 : 1;
-  if (!g.a_kmajor && !g.b_kmajor && !g.mask_bits && !g.mask_bits_out && !p.tile_base && !g.out_f32 && !p.split &&
+  if (!g.a_kmajor && !g.b_kmajor && !g.mask_bits && !g.mask_bits_out && !p.tile_base && !g.out_f32 && !p.split && !planes &&
       p.k_blocks <= resb2::kMaxKBlocks && p.m_tiles >= 2) {
     // short contraction, several row tiles per column block: B slice resident, deep A ring
     const int n_groups = p.n_tiles * g.batch;
@@ -532,9 +558,15 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   if (pairs > p.total_tiles && !p.tile_base) pairs = p.total_tiles;   // ragged: count known on the device only
   if (g.linear) {
     CUtensorMap mp = mc;
-    if (!g.a_kmajor || g.b_kmajor || g.batch != 1 || p.tile_base || !tma_store) return GSHARD_ERR_INTERNAL;
+    if (g.batch != 1 || p.tile_base || !tma_store) return GSHARD_ERR_INTERNAL;
     if (g.linear->pre && !pre_map_for(g, &mp)) return GSHARD_ERR_CUDA;
     p.lin = *g.linear;
+    if (in_runs) {
+      if (g.a_kmajor && g.b_kmajor) return launch2_t<true, true, false, true, true>(ma, mb, mc, p, pairs, st, &mp);
+      if (g.a_kmajor) return launch2_t<true, false, false, true, true>(ma, mb, mc, p, pairs, st, &mp);
+      return g.b_kmajor ? GSHARD_ERR_INTERNAL : launch2_t<false, false, false, true, true>(ma, mb, mc, p, pairs, st, &mp);
+    }
+    if (!g.a_kmajor || g.b_kmajor) return GSHARD_ERR_INTERNAL;
     return launch2_t<true, false, false, true>(ma, mb, mc, p, pairs, st, &mp);
   }
 #define GSHARD_DISPATCH2(AK, BKM) \

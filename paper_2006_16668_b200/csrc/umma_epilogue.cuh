@@ -31,11 +31,25 @@ __device__ __forceinline__ TileCoord decode_ragged(const P& p, int tile) {
   return t;
 }
 
-// Products of three-plane operands (hi + mid + lo, each the next 8 bits of an fp32 value) in the order they are added:
-// the smallest first, so that the tensor core's truncation of the running sum acts on small sums until the
-// last pass.  Products below 2^-24 are left out.
-__device__ __forceinline__ int plane_of_a(int pass) { return (0x001012 >> (4 * pass)) & 0xf; }   // lo mid hi mid hi hi
-__device__ __forceinline__ int plane_of_b(int pass) { return (0x010210 >> (4 * pass)) & 0xf; }   // hi mid lo hi mid hi
+// Products of operands that are sums of bf16 planes.  An fp32 value is hi + mid + lo, each the next 8 bits; of the nine
+// products the six that reach 2^-16 of the largest are added, small ones first, plane numbers in nibbles per pass.
+constexpr int kPasses3 = 6, kPassA3 = 0x001012, kPassB3 = 0x010210;      // lo hi, mid mid, hi lo, mid hi, hi mid, hi hi
+__host__ __device__ __forceinline__ int plane_of(int table, int pass) { return (table >> (4 * pass)) & 0xf; }
+
+// The tensor core truncates its running sum at every step (16 products), so an fp32-accurate product must not stay in
+// it for long: a run of at most 4 k-blocks (256 deep) of the hi hi pass, after which the epilogue warps add the run to
+// fp32 sums in their registers, rounding to nearest; the other passes, 2^-8 of it, in runs of 64 k-blocks.  16-bit
+// operands with fp32 output have the one pass.  (One
+// accumulation over 1024: 1e-6 relative error, over 8192: 8e-6; in runs 3e-7 at any length.)
+constexpr int kHiRun = 4, kLowRun = 64;
+__device__ __forceinline__ int low_runs(int k_blocks, int passes) { return ((passes - 1) * k_blocks + kLowRun - 1) / kLowRun; }
+__device__ __forceinline__ int all_runs(int k_blocks, int passes) {
+  return low_runs(k_blocks, passes) + (k_blocks + kHiRun - 1) / kHiRun;
+}
+__device__ __forceinline__ int run_length(int run, int k_blocks, int passes) {
+  const int low = low_runs(k_blocks, passes);
+  return run < low ? min(kLowRun, (passes - 1) * k_blocks - run * kLowRun) : min(kHiRun, k_blocks - (run - low) * kHiRun);
+}
 
 // Writes a warp's staged 32 rows x 128 bytes to C: lane l handles 16-byte piece (l & 7) of rows
 // 4*i + (l >> 3); pieces beyond the matrix edge are skipped (cols is a multiple of the piece width).
@@ -188,19 +202,100 @@ __device__ __forceinline__ void epilogue_tile(const P& p, const CUtensorMap* map
 
 // The linear operator's epilogue: pre = acc + bias, C = act(pre) + residual, and pre itself where the caller
 // keeps it.  Same share of the tile and same bulk tensor stores as above.  64 columns per round stay in
-// registers (two TMEM loads), so that pre and C can leave one after the other through the one staging
-// block; the residual's 64 columns of the thread's row are fetched while the accumulator load is in flight.
-// All of it in fp32, rounded once per output.
+// registers, so that pre and C can leave one after the other through the one staging block; the residual's 64
+// columns of the thread's row are fetched ahead.  All of it in fp32, rounded once per output.
+// One round: 64 columns from col0 of this thread's row, in r.  WAIT: tensor-memory loads into r are still in flight.
+// F32: the output is known to be fp32.
+template <bool WAIT, bool F32, typename P>
+__device__ __forceinline__ void linear_round(const P& p, const CUtensorMap* map_c, const CUtensorMap* map_pre, int b, int row0,
+                                             int col0, uint32_t (*r)[32], unsigned char* stg, int lane) {
+  unsigned char* srow = stg + lane * kStgRowBytes;
+  const int row = row0 + lane;
+  const bool f32 = F32 || p.out_f32;
+  struct Plain { int relu, out_f32; } plain{0, f32};
+  uint4 res[8];                                  // bf16 residual: 64 columns (an fp32 one is read below)
+  const bool has_res = p.lin.residual != nullptr && row < p.rows;
+  const long long off = (long long)row * p.c_ld + col0;
+  if (has_res && !f32) {
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.lin.residual) + off);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) res[i] = col0 + 8 * i < p.cols ? src[i] : make_uint4(0, 0, 0, 0);
+  }
+  store_wait(lane);                              // the previous bulk store has read the staging block
+  if (WAIT) ptx::tmem_ld_wait();
+  if (p.lin.bias) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) {
+        const int col = col0 + 32 * h + i;
+        if (col < p.cols) {                    // cols is a multiple of 8
+          const float4 b = __ldg(reinterpret_cast<const float4*>(p.lin.bias + col));
+          r[h][i] = __float_as_uint(__uint_as_float(r[h][i]) + b.x);
+          r[h][i + 1] = __float_as_uint(__uint_as_float(r[h][i + 1]) + b.y);
+          r[h][i + 2] = __float_as_uint(__uint_as_float(r[h][i + 2]) + b.z);
+          r[h][i + 3] = __float_as_uint(__uint_as_float(r[h][i + 3]) + b.w);
+        }
+      }
+  }
+  if (p.lin.pre) {
+    process_chunk<false>(r[0], plain, srow, lane, 0, 0);
+    if (f32) {
+      flush_rows_tma(stg, map_pre, b, row0, col0, lane);
+      store_wait(lane);
+      process_chunk<false>(r[1], plain, srow, lane, 0, 0);
+      if (col0 + 32 < p.cols) flush_rows_tma(stg, map_pre, b, row0, col0 + 32, lane);
+    } else {
+      process_chunk<false>(r[1], plain, srow, lane, 4, 0);
+      flush_rows_tma(stg, map_pre, b, row0, col0, lane);
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (f32) activate<32, false>(r[h], p.lin.act);
+    else activate<32, true>(r[h], p.lin.act);
+    if (has_res) {
+      if (f32) {
+        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(p.lin.residual) + off + 32 * h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (col0 + 32 * h + 4 * i < p.cols) {
+            const float4 f = src[i];
+            r[h][4 * i] = __float_as_uint(__uint_as_float(r[h][4 * i]) + f.x);
+            r[h][4 * i + 1] = __float_as_uint(__uint_as_float(r[h][4 * i + 1]) + f.y);
+            r[h][4 * i + 2] = __float_as_uint(__uint_as_float(r[h][4 * i + 2]) + f.z);
+            r[h][4 * i + 3] = __float_as_uint(__uint_as_float(r[h][4 * i + 3]) + f.w);
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float f[8];
+          Vec16<__nv_bfloat16>::load(res[4 * h + i], f);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) r[h][8 * i + j] = __float_as_uint(__uint_as_float(r[h][8 * i + j]) + f[j]);
+        }
+      }
+    }
+  }
+  if (p.lin.pre) store_wait(lane);
+  process_chunk<false>(r[0], plain, srow, lane, 0, 0);
+  if (f32) {
+    flush_rows_tma(stg, map_c, b, row0, col0, lane);
+    store_wait(lane);
+    process_chunk<false>(r[1], plain, srow, lane, 0, 0);
+    if (col0 + 32 < p.cols) flush_rows_tma(stg, map_c, b, row0, col0 + 32, lane);
+  } else {
+    process_chunk<false>(r[1], plain, srow, lane, 4, 0);
+    flush_rows_tma(stg, map_c, b, row0, col0, lane);
+  }
+}
+
 template <int BN, typename P>
 __device__ __forceinline__ void epilogue_linear_tile(const P& p, const CUtensorMap* map_c, const CUtensorMap* map_pre,
                                                      const TileCoord& t, int tile_row0, uint32_t tmem_acc, int q, int half,
                                                      unsigned char* stg, int lane) {
   constexpr int kHalfCols = BN / 2;
-  unsigned char* srow = stg + lane * kStgRowBytes;
-  const int row0 = tile_row0 + q * 32;
-  const int row = row0 + lane;
   const uint32_t t_acc = tmem_acc + (uint32_t)(half * kHalfCols) + ((uint32_t)(q * 32) << 16);
-  struct Plain { int relu, out_f32; } plain{0, p.out_f32};
 #pragma unroll 1
   for (int c = 0; c < kHalfCols / 64; ++c) {
     const int col0 = round_col0<BN>(t, half, c);
@@ -208,81 +303,32 @@ __device__ __forceinline__ void epilogue_linear_tile(const P& p, const CUtensorM
     uint32_t r[2][32];
     ptx::tmem_ld_32x32(t_acc + (uint32_t)(c * 64), r[0]);
     ptx::tmem_ld_32x32(t_acc + (uint32_t)(c * 64 + 32), r[1]);
-    uint4 res[8];                                // bf16 residual: 64 columns (an fp32 one is read below)
-    const bool has_res = p.lin.residual != nullptr && row < p.rows;
-    const long long off = (long long)row * p.c_ld + col0;
-    if (has_res && !p.out_f32) {
-      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.lin.residual) + off);
+    linear_round<true, false>(p, map_c, map_pre, t.b, tile_row0 + q * 32, col0, r, stg, lane);
+  }
+}
+
+// sums (+)= this warp's share of a finished run: 32 rows x BN / 2 columns, one row per lane, as fp32 bits.
+template <int BN>
+__device__ __forceinline__ void add_run(uint32_t (*sums)[32], uint32_t tmem_acc, int q, int half, bool first) {
+  const uint32_t t_acc = tmem_acc + (uint32_t)(half * (BN / 2)) + ((uint32_t)(q * 32) << 16);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) res[i] = col0 + 8 * i < p.cols ? src[i] : make_uint4(0, 0, 0, 0);
-    }
-    store_wait(lane);                            // the previous bulk store has read the staging block
+  for (int c = 0; c < BN / 32; ++c) {              // 16 columns at a time: the sums take most of the registers
+    uint32_t r[16];
+    ptx::tmem_ld_32x16(t_acc + (uint32_t)(c * 16), r);
     ptx::tmem_ld_wait();
-    if (p.lin.bias) {
+    uint32_t* s = &sums[c / 2][c % 2 * 16];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+    for (int i = 0; i < 16; ++i) s[i] = __float_as_uint(__uint_as_float(r[i]) + (first ? 0.f : __uint_as_float(s[i])));
+  }
+}
+template <int BN, typename P>
+__device__ __forceinline__ void epilogue_linear_sums(const P& p, const CUtensorMap* map_c, const CUtensorMap* map_pre,
+                                                     const TileCoord& t, int tile_row0, uint32_t (*sums)[32], int q, int half,
+                                                     unsigned char* stg, int lane) {
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          const int col = col0 + 32 * h + i;
-          if (col < p.cols) {                    // cols is a multiple of 8
-            const float4 b = __ldg(reinterpret_cast<const float4*>(p.lin.bias + col));
-            r[h][i] = __float_as_uint(__uint_as_float(r[h][i]) + b.x);
-            r[h][i + 1] = __float_as_uint(__uint_as_float(r[h][i + 1]) + b.y);
-            r[h][i + 2] = __float_as_uint(__uint_as_float(r[h][i + 2]) + b.z);
-            r[h][i + 3] = __float_as_uint(__uint_as_float(r[h][i + 3]) + b.w);
-          }
-        }
-    }
-    if (p.lin.pre) {
-      process_chunk<false>(r[0], plain, srow, lane, 0, 0);
-      if (p.out_f32) {
-        flush_rows_tma(stg, map_pre, t.b, row0, col0, lane);
-        store_wait(lane);
-        process_chunk<false>(r[1], plain, srow, lane, 0, 0);
-        if (col0 + 32 < p.cols) flush_rows_tma(stg, map_pre, t.b, row0, col0 + 32, lane);
-      } else {
-        process_chunk<false>(r[1], plain, srow, lane, 4, 0);
-        flush_rows_tma(stg, map_pre, t.b, row0, col0, lane);
-      }
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (p.out_f32) activate<32, false>(r[h], p.lin.act);
-      else activate<32, true>(r[h], p.lin.act);
-      if (has_res) {
-        if (p.out_f32) {
-          const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(p.lin.residual) + off + 32 * h);
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (col0 + 32 * h + 4 * i < p.cols) {
-              const float4 f = src[i];
-              r[h][4 * i] = __float_as_uint(__uint_as_float(r[h][4 * i]) + f.x);
-              r[h][4 * i + 1] = __float_as_uint(__uint_as_float(r[h][4 * i + 1]) + f.y);
-              r[h][4 * i + 2] = __float_as_uint(__uint_as_float(r[h][4 * i + 2]) + f.z);
-              r[h][4 * i + 3] = __float_as_uint(__uint_as_float(r[h][4 * i + 3]) + f.w);
-            }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float f[8];
-            Vec16<__nv_bfloat16>::load(res[4 * h + i], f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) r[h][8 * i + j] = __float_as_uint(__uint_as_float(r[h][8 * i + j]) + f[j]);
-          }
-        }
-      }
-    }
-    if (p.lin.pre) store_wait(lane);
-    process_chunk<false>(r[0], plain, srow, lane, 0, 0);
-    if (p.out_f32) {
-      flush_rows_tma(stg, map_c, t.b, row0, col0, lane);
-      store_wait(lane);
-      process_chunk<false>(r[1], plain, srow, lane, 0, 0);
-      if (col0 + 32 < p.cols) flush_rows_tma(stg, map_c, t.b, row0, col0 + 32, lane);
-    } else {
-      process_chunk<false>(r[1], plain, srow, lane, 4, 0);
-      flush_rows_tma(stg, map_c, t.b, row0, col0, lane);
-    }
+  for (int c = 0; c < BN / 128; ++c) {
+    const int col0 = round_col0<BN>(t, half, c);
+    if (col0 < p.cols) linear_round<false, true>(p, map_c, map_pre, t.b, tile_row0 + q * 32, col0, sums + 2 * c, stg, lane);
   }
 }
 

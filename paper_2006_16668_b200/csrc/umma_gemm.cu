@@ -65,7 +65,7 @@ struct Params {
   const int* pair_base;
   int tma_store;   // epilogue rows leave by bulk tensor stores through map_c
   int split;       // batch index = run of k_blocks k-blocks of the one problem (operands have no batch)
-  int passes;      // 1, or 6 with planes: every tile runs its k-blocks once per product of planes
+  int passes, pass_a, pass_b;   // operands in planes: every tile runs its k-blocks once per product (plane numbers in nibbles)
   LinearEpilogue lin;   // LIN instantiations only
 };
 
@@ -90,8 +90,9 @@ __device__ __forceinline__ TileCoord decode(const Params& p, int tile) {
 // 32-bit MN-major operand the instruction returns zeros).  A shared-memory row is still 128 bytes,
 // i.e. 32 elements: a k-block is 32 deep and an MMA contracts 8; stage sizes in bytes are those of
 // the bf16 form.
-// LIN: the linear operator's epilogue (map_pre: tensor map of the kept pre-activations).
-template <bool A_K, bool B_K, int BN, bool MASK, bool TF32 = false, bool LIN = false>
+// LIN: the linear operator's epilogue (map_pre: tensor map of the kept pre-activations).  RUNS: accumulated run by
+// run into the epilogue warps' registers (umma_epilogue.cuh), with fp32 operands in three planes each.
+template <bool A_K, bool B_K, int BN, bool MASK, bool TF32 = false, bool LIN = false, bool RUNS = false>
 __global__ void __launch_bounds__(kThreads, 1)
 umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                  const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_pre, const Params p) {
@@ -144,7 +145,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         const int kfirst = p.split ? cur.b * p.k_blocks : 0, ob = p.split ? 0 : cur.b;
         const int iters = p.k_blocks * p.passes;
         for (int it = 0, kb = 0, pass = 0; it < iters; ++it) {
-          const int oa = p.passes > 1 ? plane_of_a(pass) : ob, obb = p.passes > 1 ? plane_of_b(pass) : ob;
+          const int oa = p.passes > 1 ? plane_of(p.pass_a, pass) : ob, obb = p.passes > 1 ? plane_of(p.pass_b, pass) : ob;
           if (!ptx::mbar_wait(empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
           unsigned char* sa = smem + stage * C_::stage_bytes;
           unsigned char* sb = sa + kABytes;
@@ -177,29 +178,33 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
       int acc = 0; uint32_t acc_phase = 0;
       const int total_tiles = total_tiles_of(p);
       for (int tile = blockIdx.x; tile < total_tiles && ok; tile += gridDim.x) {
-        if (!ptx::mbar_wait(acc_empty + acc, acc_phase ^ 1u, abort_flag)) { ok = false; break; }
-        ptx::tc_fence_after_sync();
-        const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
-        for (int kb = 0; kb < p.k_blocks * p.passes; ++kb) {
-          if (!ptx::mbar_wait(full + stage, phase, abort_flag)) { ok = false; break; }
+        const int runs = RUNS ? all_runs(p.k_blocks, p.passes) : 1;
+        for (int run = 0; run < runs && ok; ++run) {
+          if (!ptx::mbar_wait(acc_empty + acc, acc_phase ^ 1u, abort_flag)) { ok = false; break; }
           ptx::tc_fence_after_sync();
-          const uint32_t sa = ptx::smem_u32(smem + stage * C_::stage_bytes);
-          const uint32_t sb = sa + kABytes;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {              // 4 MMAs per k-block: 4 x 16 bf16 or 4 x 8 tf32
-            const uint64_t da = A_K ? ptx::make_smem_desc(sa + k * 32, 16, 1024)
-                                    : ptx::make_smem_desc(sa + k * kStepMN, kBoxB, 1024);
-            const uint64_t db = B_K ? ptx::make_smem_desc(sb + k * 32, 16, 1024)
-                                    : ptx::make_smem_desc(sb + k * kStepMN, kBoxB, 1024);
-            if (TF32) ptx::umma_tf32(d_tmem, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
-            else ptx::umma_bf16(d_tmem, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
+          const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
+          const int len = RUNS ? run_length(run, p.k_blocks, p.passes) : p.k_blocks * p.passes;
+          for (int kb = 0; kb < len; ++kb) {
+            if (!ptx::mbar_wait(full + stage, phase, abort_flag)) { ok = false; break; }
+            ptx::tc_fence_after_sync();
+            const uint32_t sa = ptx::smem_u32(smem + stage * C_::stage_bytes);
+            const uint32_t sb = sa + kABytes;
+  #pragma unroll
+            for (int k = 0; k < 4; ++k) {              // 4 MMAs per k-block: 4 x 16 bf16 or 4 x 8 tf32
+              const uint64_t da = A_K ? ptx::make_smem_desc(sa + k * 32, 16, 1024)
+                                      : ptx::make_smem_desc(sa + k * kStepMN, kBoxB, 1024);
+              const uint64_t db = B_K ? ptx::make_smem_desc(sb + k * 32, 16, 1024)
+                                      : ptx::make_smem_desc(sb + k * kStepMN, kBoxB, 1024);
+              if (TF32) ptx::umma_tf32(d_tmem, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
+              else ptx::umma_bf16(d_tmem, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
+            }
+            ptx::umma_commit(empty + stage);           // stage reusable once these MMAs have read it
+            if (++stage == C_::stages) { stage = 0; phase ^= 1u; }
           }
-          ptx::umma_commit(empty + stage);           // stage reusable once these MMAs have read it
-          if (++stage == C_::stages) { stage = 0; phase ^= 1u; }
+          if (!ok) break;
+          ptx::umma_commit(acc_full + acc);            // accumulator complete
+          if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         }
-        if (!ok) break;
-        ptx::umma_commit(acc_full + acc);            // accumulator complete
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
     }
   } else {
@@ -214,6 +219,22 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     for (int tile = blockIdx.x; tile < total_tiles && ok; tile += gridDim.x) {
       const TileCoord t = tn;
       if (tile + (int)gridDim.x < total_tiles) tn = decode(p, tile + gridDim.x);
+      if constexpr (RUNS) {
+        uint32_t sums[BN / 64][32];
+        const int runs = all_runs(p.k_blocks, p.passes);
+        for (int run = 0; run < runs; ++run) {
+          if (!ptx::mbar_wait_warp(acc_full + acc, acc_phase, abort_flag, lane)) { ok = false; break; }
+          ptx::tc_fence_after_sync();
+          add_run<BN>(sums, tmem_base + (uint32_t)(acc * BN), q, half, run == 0);
+          ptx::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive_relaxed(acc_empty + acc);
+          if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+        if (!ok) break;
+        epilogue_linear_sums<BN>(p, &map_c, &map_pre, t, t.mt * BM, sums, q, half, stg, lane);
+        continue;
+      }
       if (!ptx::mbar_wait_warp(acc_full + acc, acc_phase, abort_flag, lane)) { ok = false; break; }
       ptx::tc_fence_after_sync();
       if constexpr (LIN)
@@ -411,10 +432,10 @@ umma_gemm_resident_b_kernel(const __grid_constant__ CUtensorMap map_a, const __g
 
 // ---- host side ------------------------------------------------------------------------------
 
-template <bool A_K, bool B_K, int BN, bool MASK, bool TF32 = false, bool LIN = false>
+template <bool A_K, bool B_K, int BN, bool MASK, bool TF32 = false, bool LIN = false, bool RUNS = false>
 int launch_t(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const Params& p, int grid,
              cudaStream_t st, const CUtensorMap* mp = nullptr) {
-  auto kern = umma_gemm_kernel<A_K, B_K, BN, MASK, TF32, LIN>;
+  auto kern = umma_gemm_kernel<A_K, B_K, BN, MASK, TF32, LIN, RUNS>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN>::smem_bytes) != cudaSuccess)
     return GSHARD_ERR_CUDA;
   kern<<<grid, kThreads, Cfg<BN>::smem_bytes, st>>>(ma, mb, mc, mp ? *mp : mc, p);
@@ -435,11 +456,11 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   const int bke = 128 / esz;                     // elements per 128-byte k-block row
   CUtensorMap ma, mb;
   bool okm;
-  const int problems = g.planes ? 3 : g.batch;
-  if (g.a_kmajor) okm = make_map(&ma, g.A, g.K, g.rows, problems, g.a_ld, g.a_bs, bke, BM, esz);
-  else            okm = make_map(&ma, g.A, g.rows, g.K, problems, g.a_ld, g.a_bs, bke, bke, esz);
-  if (g.b_kmajor) okm = okm && make_map(&mb, g.B, g.K, g.cols, problems, g.b_ld, g.b_bs, bke, BN, esz);
-  else            okm = okm && make_map(&mb, g.B, g.cols, g.K, problems, g.b_ld, g.b_bs, bke, bke, esz);
+  const int a_maps = g.planes_a > 0 ? g.planes_a : g.batch, b_maps = g.planes_b > 0 ? g.planes_b : g.batch;
+  if (g.a_kmajor) okm = make_map(&ma, g.A, g.K, g.rows, a_maps, g.a_ld, g.a_bs, bke, BM, esz);
+  else            okm = make_map(&ma, g.A, g.rows, g.K, a_maps, g.a_ld, g.a_bs, bke, bke, esz);
+  if (g.b_kmajor) okm = okm && make_map(&mb, g.B, g.K, g.cols, b_maps, g.b_ld, g.b_bs, bke, BN, esz);
+  else            okm = okm && make_map(&mb, g.B, g.cols, g.K, b_maps, g.b_ld, g.b_bs, bke, bke, esz);
   if (!okm) return GSHARD_ERR_CUDA;
   CUtensorMap mc;
   const bool tma_store = store_map_for(g, &mc);
@@ -451,10 +472,15 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   p.total_tiles = p.m_tiles * p.n_tiles * g.batch;
   p.k_blocks = ceil_div(g.K, bke);
   p.split = 0;
-  p.passes = g.planes ? 6 : 1;
-  if (g.planes && (g.batch != 1 || g.tile_base || !g.out_f32 || g.mask_bits || g.mask_bits_out)) return GSHARD_ERR_INTERNAL;
+  const bool planes = g.planes_a > 0, planes3 = g.planes_a == 3, in_runs = planes3 || g.runs;
+  p.passes = planes3 ? kPasses3 : planes ? 2 : 1;
+  p.pass_a = planes3 ? kPassA3 : g.planes_a == 2 ? 0x01 : 0;       // two planes: the low one first
+  p.pass_b = planes3 ? kPassB3 : g.planes_b == 2 ? 0x01 : 0;
+  if (planes && (g.batch != 1 || g.tile_base || g.mask_bits || g.mask_bits_out)) return GSHARD_ERR_INTERNAL;
+  if (planes3 && g.planes_b != 3) return GSHARD_ERR_INTERNAL;
+  if (in_runs && (!g.out_f32 || !g.linear || (planes && !planes3))) return GSHARD_ERR_INTERNAL;
   if (g.splits > 1) {
-    if (g.batch != 1 || !g.out_f32 || g.tile_base || g.linear || g.mask_bits || g.mask_bits_out) return GSHARD_ERR_INTERNAL;
+    if (g.batch != 1 || !g.out_f32 || g.tile_base || (g.linear && !in_runs) || g.mask_bits || g.mask_bits_out) return GSHARD_ERR_INTERNAL;
     p.split = 1; p.batch = g.splits; p.total_tiles = p.m_tiles * p.n_tiles * g.splits; p.k_blocks = ceil_div(p.k_blocks, g.splits);
   }
   p.out_f32 = g.out_f32; p.relu = g.relu; p.a_stream = g.a_stream; p.b_stream = g.b_stream;
@@ -469,7 +495,7 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   if (g.tile_base) p.n_fastest = 0;            // ragged lists are walked with the row tiles fastest
   int sms = device_sms();
   if (g.max_ctas > 0 && sms > g.max_ctas) sms = g.max_ctas;
-  if (!g.tf32 && !p.split && !g.planes && !g.tile_base && !g.a_kmajor && !g.b_kmajor && !g.mask_bits && BN == 256 && p.k_blocks <= resb::kMaxKBlocks && p.m_tiles >= 4) {
+  if (!g.tf32 && !p.split && !planes && !g.tile_base && !g.a_kmajor && !g.b_kmajor && !g.mask_bits && BN == 256 && p.k_blocks <= resb::kMaxKBlocks && p.m_tiles >= 4) {
     // short contraction, several row tiles per column block: keep the B tile resident
     const int n_groups = p.n_tiles * g.batch;
     if (cudaFuncSetAttribute(umma_gemm_resident_b_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -482,9 +508,18 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   const int grid = (p.total_tiles < sms && !g.tile_base) ? p.total_tiles : sms;   // ragged: count known on the device only
   if (g.linear) {
     CUtensorMap mp = mc;
-    if (!g.a_kmajor || g.b_kmajor || g.batch != 1 || g.tf32 || g.tile_base || !tma_store) return GSHARD_ERR_INTERNAL;
+    if (g.batch != 1 || g.tf32 || g.tile_base || !tma_store) return GSHARD_ERR_INTERNAL;
     if (g.linear->pre && !pre_map_for(g, &mp)) return GSHARD_ERR_CUDA;
     p.lin = *g.linear;
+#define GSHARD_RUNS(AK, BKM)                                                                                     \
+  (BN == 256 ? launch_t<AK, BKM, 256, false, false, true, true>(ma, mb, mc, p, grid, st, &mp)                    \
+             : launch_t<AK, BKM, 128, false, false, true, true>(ma, mb, mc, p, grid, st, &mp))
+    if (in_runs) {
+      if (g.a_kmajor) return g.b_kmajor ? GSHARD_RUNS(true, true) : GSHARD_RUNS(true, false);
+      return g.b_kmajor ? GSHARD_ERR_INTERNAL : GSHARD_RUNS(false, false);
+    }
+#undef GSHARD_RUNS
+    if (!g.a_kmajor || g.b_kmajor) return GSHARD_ERR_INTERNAL;
     return BN == 256 ? launch_t<true, false, 256, false, false, true>(ma, mb, mc, p, grid, st, &mp)
                      : launch_t<true, false, 128, false, false, true>(ma, mb, mc, p, grid, st, &mp);
   }
