@@ -639,6 +639,8 @@ __global__ void __launch_bounds__(kRouteThreads) route_bwd_fast_kernel(const Rou
     const T* row = static_cast<const T*>(a.logits) + t * a.E;
     T* out = static_cast<T*>(a.dlogits) + t * a.E;
     const float* dm = a.dm ? a.dm + t / a.S * a.E : nullptr;
+    float v[V];
+    if (dense) load_logits<T, W, V>(row, ln, a.E == V * LPR, v);    // in flight while the picks' own loads follow one another
     int e = -1;
     float l = -INFINITY, dw = 0.f;
     if (p < a.k) {
@@ -647,10 +649,8 @@ __global__ void __launch_bounds__(kRouteThreads) route_bwd_fast_kernel(const Rou
       if (e >= 0) { l = usable(row[e]); dw = a.dweight[t * a.k + p]; }
       if (l == -INFINITY) e = -1;
     }
-    float v[V];
     float mx = 0.f, inv = 0.f;
     if (dense) {
-      load_logits<T, W, V>(row, ln, a.E == V * LPR, v);
       clean<V>(v);
       if (soft_stats) {
         mx = -INFINITY;
