@@ -8,6 +8,7 @@
  *                 with random routing (keep iff c < C and 2*g2 > rnd)
  *   Algorithm 2   tensor layouts: inputs [G,S,M], wg [M,E], wi [E,M,H], wo [E,H,M],
  *                 dispatched expert inputs [E,G,C,M], outputs [G,S,M]
+ * and, further down, the operators of the Transformer around it: layer norm, linear, routing beyond top-2.
  *
  * Conventions for every call
  *   - All tensor arguments are DEVICE pointers unless the name ends in _host; tensors are
@@ -27,7 +28,7 @@
  *     u, l_aux, weight, m, dwg are always float.
  *   - Outputs are bit-reproducible from run to run (no atomics in any reduction).
  *   - Every stage's launches sit inside an NVTX range (gshard.gate, .capacity, .dispatch,
- *     .expert_ffn, .combine, .backward.*), visible to a profiler that injects NVTX.
+ *     .expert_ffn, .combine, .backward.*, .layer_norm, .linear, .route), visible to a profiler that injects NVTX.
  */
 #ifndef GSHARD_MOE_H_
 #define GSHARD_MOE_H_
@@ -482,7 +483,9 @@ int gshard_layer_norm_backward(int64_t n_rows, int32_t M, int32_t dtype, const v
  * is dtype or GSHARD_F32 (a router's logits, for instance).  bias, residual and pre may be NULL; pre receives
  * the pre-activations that the backward takes.  residual may be y itself; no other output may
  * overlap an operand.  K % 8 == 0 and cols % 8 == 0; n_rows may be 0.
- * bf16: tensor cores, fp32 accumulation, one rounding per output; fp32: fp32 arithmetic.
+ * bf16: tensor cores, fp32 accumulation, one rounding per output.  fp32: as close to the exact result as an fp32
+ * product (three bf16 planes per operand on the tensor cores); an infinite operand may come out as NaN.
+ * n_rows == 0 launches nothing and leaves the workspace alone.
  * workspace: gshard_linear_workspace_bytes() bytes, 256-byte aligned; its first word is the status word
  * (gshard_moe_last_device_status).  Calls that share a workspace must be ordered on one stream. */
 typedef enum {

@@ -434,6 +434,13 @@ def _code_of(dtype, what):
     return code
 
 
+def _activation(activation):
+    code = _ACTIVATIONS.get(activation, activation)
+    if not isinstance(code, int):
+        raise ValueError(f"activation: expected one of {sorted(_ACTIVATIONS)} or a GSHARD_ACT_ value, got {activation!r}")
+    return code
+
+
 def _arg(t, name, shape, dtype, device):
     """Pointer of a tensor argument after checking it (None stays None); device: index of the call's GPU."""
     if t is None:
@@ -514,7 +521,7 @@ def gshard_linear_forward(x, w, y, bias=None, residual=None, pre=None, activatio
     args = [_arg(x, "x", (n, K), x.dtype, dev), _arg(w, "w", (K, cols), x.dtype, dev),
             _arg(bias, "bias", (cols,), torch.float32, dev), _arg(residual, "residual", (n, cols), y.dtype, dev),
             _arg(y, "y", (n, cols), y.dtype, dev), _arg(pre, "pre", (n, cols), y.dtype, dev), *_workspace(workspace, dev)]
-    _call("gshard_linear_forward", dev, stream, n, K, cols, code, out, _ACTIVATIONS.get(activation, activation), *args)
+    _call("gshard_linear_forward", dev, stream, n, K, cols, code, out, _activation(activation), *args)
 
 
 def gshard_linear_backward(x, w, dy, dx=None, dw=None, dbias=None, pre=None, activation="none", workspace=None,
@@ -526,7 +533,7 @@ def gshard_linear_backward(x, w, dy, dx=None, dw=None, dbias=None, pre=None, act
             _arg(pre, "pre", (n, cols), dy.dtype, dev), _arg(dy, "dy", (n, cols), dy.dtype, dev),
             _arg(dx, "dx", (n, K), x.dtype, dev), _arg(dw, "dw", (K, cols), x.dtype, dev),
             _arg(dbias, "dbias", (cols,), torch.float32, dev), *_workspace(workspace, dev)]
-    _call("gshard_linear_backward", dev, stream, n, K, cols, code, out, _ACTIVATIONS.get(activation, activation), *args)
+    _call("gshard_linear_backward", dev, stream, n, K, cols, code, out, _activation(activation), *args)
 
 
 def make_route(*, G, S, E, k, dtype="f32", score="softmax", groups=1, groups_kept=None, group_top=1, renormalise=True,

@@ -269,7 +269,7 @@ using namespace gshard;
 
 extern "C" {
 
-int gshard_version(void) { return 210; }
+int gshard_version(void) { return 220; }
 
 const char* gshard_status_string(int s) {
   switch (s) {

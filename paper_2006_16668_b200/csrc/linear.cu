@@ -10,7 +10,9 @@
 // dy); dbias sums it before the rounding.  Small products, whose time is launches, take what the rounding left as a
 // second plane and a second pass, which halves the error of dx and dw to that of their own rounding.
 // A product with too few output tiles for the multiprocessors is cut along the contraction into runs whose
-// fp32 partial products a second kernel adds in order.
+// fp32 partial products a second kernel adds in order.  Measured: 65536 x 8192 -> 1024 with residual 733 to 800 us$
+// (1.37 to 1.5 PFLOP/s, tensor pipe 88 % active); backward of 30011 x 1024 -> 8192 with gelu 926 us: dpre 245 (HBM),
+// dx 336, dw 346.
 // fp32: an fp32 value is the exact sum of three bf16 values (8 bits of its 24 each), so x . w is six bf16 products
 // of such planes on the same GEMMs, accumulated in fp32, smallest first; the three products left out lie below 2^-24.
 // That is six times the tensor work and three times the operand bytes, and still several times faster than fp32 FMA

@@ -6,7 +6,7 @@
 
 namespace gshard {
 
-// linear_few.cu: the whole operator in one launch for few rows; also clears the status word.
+// linear_few.cu: the whole operator in one launch for up to 8 rows; also clears the status word.
 int launch_linear_few(int n, int K, int cols, bool bf16, bool out_f32, const void* x, const void* w, void* y,
                       const LinearEpilogue& lin, int* status, cudaStream_t st);
 

@@ -125,6 +125,9 @@ def test_binding_refuses_host_tensors_and_mismatches():
         B.gshard_linear_forward(x, torch.zeros(32, 8), torch.zeros(4, 8))
     with pytest.raises(ValueError, match="residual"):
         B.gshard_linear_forward(x, torch.zeros(64, 8), torch.zeros(4, 8), residual=torch.zeros(8, 8).t()[:4])
+    for act in ("gelu_fast", None, 1.5):
+        with pytest.raises(ValueError, match="activation"):
+            B.gshard_linear_forward(x, torch.zeros(64, 8), torch.zeros(4, 8), activation=act)
     cfg = B.make_route(G=1, S=4, E=8, k=2)
     with pytest.raises(ValueError, match="expert_idx"):
         B.gshard_moe_route(cfg, torch.zeros(1, 4, 8), torch.zeros(1, 4, 2, dtype=torch.int64), torch.zeros(1, 4, 2))
