@@ -107,6 +107,8 @@ struct UmmaGemm {
                              // 2 and 1, 1 and 2, or 3 and 3 (fp32 values; fp32 output; takes `linear`)
   int runs;                  // fp32 accuracy: accumulate in short runs (three planes always; plain operands with `linear` and
                              // fp32 output)
+  int clear_status;          // *status = 0 at the start, by the first CTA (all CTAs run at once, and a CTA reports only after a
+                             // wait of two seconds): for callers without a memset before the launch
   const LinearEpilogue* linear;   // batch 1; a_kmajor, !b_kmajor unless 3 planes: the linear operator's epilogue instead of
                              // relu / masks
 };

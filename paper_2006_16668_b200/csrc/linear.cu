@@ -9,14 +9,15 @@
 // dpre is rounded to bf16 once, as the operand of both gradient products (exact with no activation or relu on 16-bit
 // dy); dbias sums it before the rounding.  Small products, whose time is launches, take what the rounding left as a
 // second plane and a second pass, which halves the error of dx and dw to that of their own rounding.
-// A product with too few output tiles for the multiprocessors is cut along the contraction into runs whose
-// fp32 partial products a second kernel adds in order.  Measured: 65536 x 8192 -> 1024 with residual 733 to 800 us$
+// A product whose output tiles run at once is one launch (linear_mid.cu); another one (fp32 output, deep contractions) with
+// too few tiles for the multiprocessors is cut along the contraction into runs whose fp32 partial products a second
+// kernel adds in order.  Measured: 65536 x 8192 -> 1024 with residual 733 to 800 us
 // (1.37 to 1.5 PFLOP/s, tensor pipe 88 % active); backward of 30011 x 1024 -> 8192 with gelu 926 us: dpre 245 (HBM),
 // dx 336, dw 346.
 // fp32: an fp32 value is the exact sum of three bf16 values (8 bits of its 24 each), so x . w is six bf16 products
 // of such planes on the same GEMMs, accumulated in fp32, smallest first; the three products left out lie below 2^-24.
 // That is six times the tensor work and three times the operand bytes, and still several times faster than fp32 FMA
-// on the CUDA cores (4100 x 1024 x 4096: 1172 us there).  Infinities and NaN in x, w or dy give NaN.
+// on the CUDA cores (4100 x 1024 x 4096: 170 us against 1172 there).  Infinities and NaN in x, w or dy give NaN.
 // A few rows stream w through the CUDA cores instead (linear_few.cu).
 #include <algorithm>
 
@@ -39,6 +40,7 @@ __global__ void __launch_bounds__(256) linear_finish_kernel(const float4* __rest
                                                             void* y, long long n4, int cols4) {
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n4; i += (long long)gridDim.x * 256) {
     float4 s = partial[i];
+#pragma unroll 8
     for (int k = 1; k < splits; ++k) {
       const float4 v = partial[(long long)k * n4 + i];
       s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -73,15 +75,16 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const float* __restri
 // dpre = dy act'(pre) rounded to bf16 (where wanted), and the chunk's column sums of dpre before the rounding.
 // A block covers 32 x 8 columns and one chunk of rows; a thread owns 8 columns and every 8th row, four of
 // them in flight: the pass is bound by HBM (dy and pre in, dpre out).  PLANES: bf16 planes that dpre is
-// written as: 3 (fp32), 2 (rounded, and what the rounding left) or 1.
+// written as: 3 (fp32), 2 (rounded, and what the rounding left) or 1.  Also clears the status word for the products that follow.
 template <typename TY, int PLANES, int ACT>
 __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__ dy, const TY* __restrict__ pre, __nv_bfloat16* dpre,
-                                                          float* __restrict__ partial, long long n, int cols, int chunk) {
+                                                          float* __restrict__ partial, int* status, long long n, int cols, int chunk) {
   constexpr bool FAST = PLANES < 3;
   constexpr int U = sizeof(TY) == 2 ? 4 : 2;              // rows in flight
   constexpr int PW = 16 / (int)sizeof(TY), PN = 8 / PW;    // packs of 16 bytes per 8 columns
   __shared__ float part[8][256 + 8];
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) *status = 0;
   const int col = blockIdx.x * 256 + tx * 8;
   const long long r1 = min(n, (long long)(blockIdx.y + 1) * chunk);
   float sum[8];
@@ -151,13 +154,13 @@ __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__
 }
 
 template <typename TY, int PLANES>
-void launch_dpre(const void* dy, const void* pre, void* dpre, float* partial, long long n, int cols, int chunk, int chunks, int act,
+void launch_dpre(const void* dy, const void* pre, void* dpre, float* partial, int* status, long long n, int cols, int chunk, int chunks, int act,
                  cudaStream_t st) {
   const dim3 grid(ceil_div(cols, 256), chunks);
 #define GSHARD_DPRE(A)                                                                                                   \
   case A:                                                                                                                \
     linear_dpre_kernel<TY, PLANES, A><<<grid, 256, 0, st>>>(static_cast<const TY*>(dy), static_cast<const TY*>(pre),     \
-                                                            static_cast<__nv_bfloat16*>(dpre), partial, n, cols, chunk); \
+                                                            static_cast<__nv_bfloat16*>(dpre), partial, status, n, cols, chunk); \
     break;
   switch (act) {
     GSHARD_DPRE(GSHARD_ACT_NONE)
@@ -206,21 +209,28 @@ int splits_for(long long rows, int cols, long long depth) {
   return (int)((k_blocks + per - 1) / per);      // no empty run at the end
 }
 
-// Rows up to which w streams through the CUDA cores (linear_few.cu) instead of the tensor cores.
-bool few_rows(int64_t n) { return n <= 8; }
+// Whether w streams through the CUDA cores (linear_few.cu): up to 2 rows, and up to 8 where a product is not one launch of
+// linear_mid.cu.  Measured, us, few to mid: 1024 -> 8192 6.8 to 7.5 for two rows, 8.2 to 7.6 for three, 10.5 to 7.5 for
+// eight; 2048 -> 2048 5.9 to 6.5, 6.6 to 6.5, 8.8 to 6.5; 8192 -> 1024 8.0 to 9.8, 9.2 to 9.8, 11.6 to 9.8.
+bool few_rows(int64_t n, MidShape mid) { return n <= 2 || (n <= 8 && !mid.bn); }
 
-struct LinearPlan { size_t status, xp, wp, dpre, colsum, join, total; int planes, chunks, chunk, splits, dx_splits, dw_splits; };
+struct LinearPlan {
+  size_t status, xp, wp, dpre, colsum, join, total;
+  int planes, chunks, chunk, splits, dx_splits, dw_splits;
+  MidShape mid, dx_mid, dw_mid;          // bn > 0: the product goes to linear_mid.cu
+};
 
-LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, bool backward) {
+LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, int out_dtype, bool backward) {
   Carver c;
   LinearPlan p{};
   const bool bf16 = dtype == GSHARD_BF16;
   p.status = c.take(256);
-  if (n == 0 || (!backward && few_rows(n))) { p.total = c.off; return p; }
+  if (!backward && bf16 && out_dtype == dtype) p.mid = linear_mid_shape(n, cols, K, 1);
+  if (n == 0 || (!backward && few_rows(n, p.mid))) { p.total = c.off; return p; }
   p.xp = c.take(bf16 ? 0 : (size_t)n * K * 6);             // planes of fp32 operands
   p.wp = c.take(bf16 ? 0 : (size_t)K * cols * 6);
   if (!backward) {
-    p.splits = splits_for(n, cols, K);
+    p.splits = p.mid.bn ? 1 : splits_for(n, cols, K);
     if (p.splits > 1) p.join = c.take((size_t)p.splits * n * cols * 4);
     p.total = c.off;
     return p;
@@ -233,8 +243,12 @@ LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, bool backward) {
   p.chunk = (int)std::max<long long>(32, (n + want - 1) / want);
   p.chunks = (int)((n + p.chunk - 1) / p.chunk);
   p.colsum = c.take((size_t)p.chunks * cols * 4);
-  p.dx_splits = splits_for(n, K, cols);
-  p.dw_splits = splits_for(K, cols, n);
+  if (bf16) {
+    p.dx_mid = linear_mid_shape(n, K, cols, p.planes);
+    p.dw_mid = linear_mid_shape(K, cols, n, p.planes);
+  }
+  p.dx_splits = p.dx_mid.bn ? 1 : splits_for(n, K, cols);
+  p.dw_splits = p.dw_mid.bn ? 1 : splits_for(K, cols, n);
   p.join = c.take(std::max(p.dx_splits > 1 ? (size_t)p.dx_splits * n * K * 4 : 0,
                            p.dw_splits > 1 ? (size_t)p.dw_splits * K * cols * 4 : 0));
   p.total = c.off;
@@ -263,9 +277,10 @@ void split_planes(const void* src, void* dst, long long n, cudaStream_t st) {
   count_launch();
 }
 
-// C = A . B, cut into `splits` runs through the fp32 partial products in `join`
-int gemm_joined(const Dims& d, UmmaGemm g, int splits, float* join, int* status, cudaStream_t st) {
+// C = A . B: in one launch of linear_mid.cu, or cut into `splits` runs through the fp32 partial products in `join`
+int gemm_joined(const Dims& d, UmmaGemm g, MidShape mid, int splits, float* join, int* status, cudaStream_t st) {
   const LinearEpilogue none{};
+  if (mid.bn) return launch_linear_mid(g, none, mid, g.clear_status != 0, status, st);
   if (g.planes_a == 3) { g.linear = &none; g.runs = 1; }
   if (splits <= 1) return run_gemm(d, g, status, st);
   void* out = g.C;
@@ -296,7 +311,7 @@ extern "C" {
 
 size_t gshard_linear_workspace_bytes(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype, int for_backward) {
   if (linear_validate(n_rows, K, cols, dtype, out_dtype) != GSHARD_OK) return 0;
-  return linear_plan(n_rows, K, cols, dtype, for_backward != 0).total;
+  return linear_plan(n_rows, K, cols, dtype, out_dtype, for_backward != 0).total;
 }
 
 int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype, int32_t activation,
@@ -309,7 +324,7 @@ int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype
   GS_CHECK_PTR(x); GS_CHECK_PTR(w); GS_CHECK_PTR(y);
   GS_CHECK_OPTIONAL_PTR(bias); GS_CHECK_OPTIONAL_PTR(residual); GS_CHECK_OPTIONAL_PTR(pre);
   if (y == x || y == w || pre == x || pre == w || (pre && (pre == y || pre == residual))) return GSHARD_ERR_INVALID_ARG;
-  const LinearPlan pl = linear_plan(n_rows, K, cols, dtype, false);
+  const LinearPlan pl = linear_plan(n_rows, K, cols, dtype, out_dtype, false);
   GS_CHECK_WORKSPACE(workspace, workspace_bytes, pl.total);
   GS_CHECK(check_device());
   NvtxRange range("gshard.linear");
@@ -317,16 +332,17 @@ int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype
   int* status = static_cast<int*>(workspace);
   const LinearEpilogue lin{bias, residual, pre, activation};
   const bool out_f32 = out_dtype == GSHARD_F32;
-  if (few_rows(n_rows)) {
+  if (few_rows(n_rows, pl.mid)) {
     GS_CHECK(launch_linear_few((int)n_rows, K, cols, dtype == GSHARD_BF16, out_f32, x, w, y, lin, status, st));
     return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
   }
-  GS_CHECK(zero(status, sizeof(int), st));
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   const Dims d = linear_dims(K, cols);
   UmmaGemm g{};
   g.A = x; g.B = w; g.C = y; g.rows = (int)n_rows; g.cols = cols; g.K = K; g.batch = 1;
   g.a_kmajor = true; g.b_kmajor = false; g.a_ld = K; g.b_ld = cols; g.c_ld = cols;
+  if (pl.mid.bn) return launch_linear_mid(g, lin, pl.mid, true, status, st);
+  g.clear_status = 1;
   g.a_stream = 1; g.prefer_two_sm = 1; g.out_f32 = out_f32;
   if (dtype == GSHARD_F32) {
     split_planes(x, ws + pl.xp, n_rows * K, st);
@@ -372,13 +388,13 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
   if (activation != GSHARD_ACT_NONE) GS_CHECK_PTR(pre);
   if (dx && (dx == dy || dx == x || dx == w || dx == pre)) return GSHARD_ERR_INVALID_ARG;
   if (dw && (dw == dy || dw == x || dw == w || dw == pre)) return GSHARD_ERR_INVALID_ARG;
-  const LinearPlan pl = linear_plan(n_rows, K, cols, dtype, true);
+  const LinearPlan pl = linear_plan(n_rows, K, cols, dtype, out_dtype, true);
   GS_CHECK_WORKSPACE(workspace, workspace_bytes, pl.total);
   GS_CHECK(check_device());
   NvtxRange range("gshard.linear.backward");
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   int* status = reinterpret_cast<int*>(ws);
-  GS_CHECK(zero(status, sizeof(int), st));
+  if (!dx && !dw && !dbias) return zero(status, sizeof(int), st);
   const bool fp32 = dtype == GSHARD_F32;
   const bool convert = fp32 || activation != GSHARD_ACT_NONE || out_dtype != dtype;    // else dpre is dy itself
   // dy times 0 or 1 needs no second plane
@@ -387,7 +403,7 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
   void* buf = convert && (dx || dw) ? ws + pl.dpre : nullptr;
   float* colsum = dbias ? reinterpret_cast<float*>(ws + pl.colsum) : nullptr;
   if (buf || colsum) {
-#define GSHARD_DPRE(TY, P) launch_dpre<TY, P>(dy, pre, buf, colsum, n_rows, cols, pl.chunk, pl.chunks, activation, st)
+#define GSHARD_DPRE(TY, P) launch_dpre<TY, P>(dy, pre, buf, colsum, status, n_rows, cols, pl.chunk, pl.chunks, activation, st)
     if (planes == 3) GSHARD_DPRE(float, 3);
     else if (out_dtype == GSHARD_F32) { if (planes == 2) GSHARD_DPRE(float, 2); else GSHARD_DPRE(float, 1); }
     else { if (planes == 2) GSHARD_DPRE(__nv_bfloat16, 2); else GSHARD_DPRE(__nv_bfloat16, 1); }
@@ -398,33 +414,35 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
     }
   }
   const void* dpre = convert ? buf : dy;
+  bool cleared = buf || colsum;                   // the status word, by the first kernel of the call
   const Dims d = linear_dims(K, cols);
   float* join = reinterpret_cast<float*>(ws + pl.join);
   if (dx) {                                       // [n, K] = dpre [n, cols] . w^T, both contiguous along cols
     UmmaGemm g{};
     g.A = dpre; g.B = w; g.C = dx; g.rows = (int)n_rows; g.cols = K; g.K = cols; g.batch = 1;
     g.a_kmajor = true; g.b_kmajor = true; g.a_ld = cols; g.b_ld = cols; g.c_ld = K;
-    g.prefer_two_sm = 1; g.out_f32 = fp32;
+    g.prefer_two_sm = 1; g.out_f32 = fp32; g.clear_status = !cleared;
+    cleared = true;
     if (fp32) {
       split_planes(w, ws + pl.wp, (long long)K * cols, st);
       g.B = ws + pl.wp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * cols; g.b_bs = (long long)K * cols;
     } else if (planes == 2) {
       g.planes_a = 2; g.planes_b = 1; g.a_bs = n_rows * cols;
     }
-    GS_CHECK(gemm_joined(d, g, pl.dx_splits, join, status, st));
+    GS_CHECK(gemm_joined(d, g, pl.dx_mid, pl.dx_splits, join, status, st));
   }
   if (dw) {                                       // [K, cols] = x^T . dpre, both stored row by row of the contraction
     UmmaGemm g{};
     g.A = x; g.B = dpre; g.C = dw; g.rows = K; g.cols = cols; g.K = (int)n_rows; g.batch = 1;
     g.a_kmajor = false; g.b_kmajor = false; g.a_ld = K; g.b_ld = cols; g.c_ld = cols;
-    g.prefer_two_sm = 1; g.out_f32 = fp32;
+    g.prefer_two_sm = 1; g.out_f32 = fp32; g.clear_status = !cleared;
     if (fp32) {
       split_planes(x, ws + pl.xp, n_rows * K, st);
       g.A = ws + pl.xp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * K; g.b_bs = n_rows * cols;
     } else if (planes == 2) {
       g.planes_a = 1; g.planes_b = 2; g.b_bs = n_rows * cols;
     }
-    GS_CHECK(gemm_joined(d, g, pl.dw_splits, join, status, st));
+    GS_CHECK(gemm_joined(d, g, pl.dw_mid, pl.dw_splits, join, status, st));
   }
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
 }

@@ -7,8 +7,8 @@
 // result has the same bits from run to run.  A second wave of blocks would double the time (each has some 3 us of
 // its own: launch, staging of x, the joins), so the launcher aims just below two blocks per multiprocessor, with
 // narrow column blocks (LC = 4) before runs that need a cluster.
-// Measured (back to back, w from HBM): 1024 -> 8192 bf16 6.2 us for one row, 10 us for eight; 8192 -> 1024 7.4 us.  From
-// nine rows on the tensor-core path, cut along the contraction, is as fast.
+// Measured (back to back, w from HBM): 1024 -> 8192 bf16 6.2 us for one row, 10 us for eight; 8192 -> 1024 7.6 us.  From
+// three rows on (linear.cu) the tensor cores are as fast where one launch of theirs covers the product.
 #include <algorithm>
 
 #include "activation.cuh"

@@ -59,6 +59,7 @@ struct Params2 {
   int a_stream, b_stream;
   int n_fastest;
   int* status;
+  int clear_status;
   int tma_store;   // epilogue rows leave by bulk tensor stores through map_c
   int split;       // batch index = run of k_blocks k-blocks of the one problem (operands have no batch)
   int passes, pass_a, pass_b;   // operands in planes: every tile runs its k-blocks once per product (plane numbers in nibbles)
@@ -106,6 +107,7 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     for (int s = 0; s < kStages; ++s) { ptx::mbar_init(full + s, 1); ptx::mbar_init(empty + s, 1); }
     for (int a = 0; a < 2; ++a) { ptx::mbar_init(acc_full + a, 1); ptx::mbar_init(acc_empty + a, 2 * kEpiWarps); }
     *abort_flag = 0;
+    if (p.clear_status && blockIdx.x == 0) *p.status = 0;
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&map_a);
     ptx::prefetch_tensormap(&map_b);
@@ -318,6 +320,7 @@ umma2_gemm_resident_b_kernel(const __grid_constant__ CUtensorMap map_a, const __
     for (int s = 0; s < kBBars; ++s) { ptx::mbar_init(b_full + s, 1); ptx::mbar_init(b_empty + s, 1); }
     for (int a = 0; a < 2; ++a) { ptx::mbar_init(acc_full + a, 1); ptx::mbar_init(acc_empty + a, 2 * kEpiWarps); }
     *abort_flag = 0;
+    if (p.clear_status && blockIdx.x == 0) *p.status = 0;
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&map_a);
     ptx::prefetch_tensormap(&map_b);
@@ -539,7 +542,7 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   }
   p.out_f32 = g.out_f32; p.relu = g.relu; p.a_stream = g.a_stream; p.b_stream = g.b_stream;
   p.n_fastest = (g.rows > g.cols) ? 1 : 0;
-  p.status = status;
+  p.status = status; p.clear_status = g.clear_status;
   p.tile_base = g.ragged_on_pairs ? g.tile_base : nullptr;
   p.tile_problem = g.tile_problem;
   if (p.tile_base && !p.tile_problem) return GSHARD_ERR_INTERNAL;

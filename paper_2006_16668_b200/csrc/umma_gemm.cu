@@ -56,6 +56,7 @@ struct Params {
   int a_stream, b_stream;
   int n_fastest;   // tile order: column tiles fastest (A is the larger operand) instead of row tiles
   int* status;
+  int clear_status;
   // Ragged batches (compacted expert rows): problem b owns the row tiles [tile_base[b], tile_base[b+1])
   // of a device-side prefix array with batch + 1 entries; nullptr = every problem has m_tiles row tiles.
   const int* tile_base;
@@ -117,6 +118,7 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     for (int s = 0; s < C_::stages; ++s) { ptx::mbar_init(full + s, 1); ptx::mbar_init(empty + s, 1); }
     for (int a = 0; a < 2; ++a) { ptx::mbar_init(acc_full + a, 1); ptx::mbar_init(acc_empty + a, kEpiWarps); }
     *abort_flag = 0;
+    if (p.clear_status && blockIdx.x == 0) *p.status = 0;
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&map_a);
     ptx::prefetch_tensormap(&map_b);
@@ -315,6 +317,7 @@ umma_gemm_resident_b_kernel(const __grid_constant__ CUtensorMap map_a, const __g
     for (int s = 0; s < kMaxKBlocks; ++s) { ptx::mbar_init(b_full + s, 1); ptx::mbar_init(b_empty + s, 1); }
     for (int a = 0; a < 2; ++a) { ptx::mbar_init(acc_full + a, 1); ptx::mbar_init(acc_empty + a, kEpiWarps); }
     *abort_flag = 0;
+    if (p.clear_status && blockIdx.x == 0) *p.status = 0;
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&map_a);
     ptx::prefetch_tensormap(&map_b);
@@ -486,7 +489,7 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   p.out_f32 = g.out_f32; p.relu = g.relu; p.a_stream = g.a_stream; p.b_stream = g.b_stream;
   // stream the larger operand once: walk the tiles that share it back to back
   p.n_fastest = (g.rows > g.cols) ? 1 : 0;
-  p.status = status;
+  p.status = status; p.clear_status = g.clear_status;
   p.tile_base = g.tile_base;
   p.pair_base = g.tile_base ? g.pair_base : nullptr;
   p.tile_problem = g.tile_problem;

@@ -263,3 +263,54 @@ def test_refusals():
     square = _make(64, 64, 64, BF)
     with pytest.raises(B.GshardError):                       # an output over an operand
         B.gshard_linear_forward(square["x"], square["w"], square["x"], workspace=_ws(square, False))
+
+
+# Products whose tiles of 128 x 64 or 128 x 128 run at once take one launch: one CTA, or 2 or 4 sharing the contraction.
+ONE_LAUNCH = [(3, 1024, 72), (9, 8, 8), (17, 128, 64), (40, 136, 9472), (65, 256, 8), (100, 512, 1000), (127, 1160, 200),
+              (128, 2048, 264), (129, 3840, 72), (130, 1024, 4744), (255, 640, 136), (513, 1096, 520), (1025, 776, 1160),
+              (2049, 264, 640), (64, 8200, 1024), (31, 16392, 40)]
+
+
+@pytest.mark.parametrize("n,K,cols", ONE_LAUNCH)
+def test_products_of_one_launch(n, K, cols):
+    t = _make(n, K, cols, BF)
+    act = ACTS[(n + cols) % 5]
+    guard = torch.full((n + 2, cols), 7.0, dtype=BF, device="cuda")
+    y, kept = _forward(t, act, residual=True, pre=True, y=guard[1:n + 1])
+    _check_forward(t, y, kept, act, residual=True)
+    assert (guard[0] == 7).all() and (guard[-1] == 7).all()
+    again, _ = _forward(t, act, residual=True)
+    assert torch.equal(again, y)
+    plain, _ = _forward(t, bias=False)
+    _check_forward(t, plain, None, "none", bias=False)
+    _check_backward(t, act, *_backward(t, act))
+
+
+@pytest.mark.parametrize("out", [BF, F32])
+@pytest.mark.parametrize("n", [1, 8, 9, 200, 3000])
+def test_status_word_is_cleared(n, out):
+    """A workspace full of ones, as another call may have left it, reads as success afterwards."""
+    t = _make(n, 256, 512, BF, out)
+    y = torch.empty_like(t["dy"])
+    ws = _ws(t, False).fill_(255)
+    B.gshard_linear_forward(t["x"], t["w"], y, workspace=ws)
+    assert B.gshard_moe_last_device_status(ws) == B.GSHARD_OK
+    for act in ("none", "gelu"):
+        for wanted in ((1, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1), (0, 0, 0)):
+            g = [torch.empty_like(v) if on else None for on, v in zip(wanted, (t["x"], t["w"], t["bias"]))]
+            ws = _ws(t, True).fill_(255)
+            B.gshard_linear_backward(t["x"], t["w"], t["dy"], *g, pre=None if act == "none" else t["pre"], activation=act,
+                                     workspace=ws)
+            assert B.gshard_moe_last_device_status(ws) == B.GSHARD_OK
+
+
+def test_rows_of_one_launch_do_not_touch_each_other():
+    """Infinities and NaN in a row of x stay in its row of y, whatever the rows that a tile does not have."""
+    for n in (5, 60, 130):
+        t = _make(n, 1024, 256, BF)
+        y0, _ = _forward(t)
+        t["x"][n - 1, 7] = float("nan")
+        t["x"][0, 9] = float("inf")
+        y, _ = _forward(t)
+        assert torch.isnan(y[n - 1]).all() and not torch.isfinite(y[0]).any()
+        assert torch.equal(y[1:n - 1], y0[1:n - 1])
