@@ -9,7 +9,7 @@
 // dpre is rounded to bf16 once, as the operand of both gradient products (exact with no activation or relu on 16-bit
 // dy); dbias sums it before the rounding.  Small products, whose time is launches, take what the rounding left as a
 // second plane and a second pass, which halves the error of dx and dw to that of their own rounding.
-// A product whose output tiles run at once is one launch (linear_mid.cu); another one (fp32 output, deep contractions) with
+// A product whose output tiles run at once is one launch (linear_mid.cu); another one (deep contractions) with
 // too few tiles for the multiprocessors is cut along the contraction into runs whose fp32 partial products a second
 // kernel adds in order.  Measured: 65536 x 8192 -> 1024 with residual 733 to 800 us
 // (1.37 to 1.5 PFLOP/s, tensor pipe 88 % active); backward of 30011 x 1024 -> 8192 with gelu 926 us: dpre 245 (HBM),
@@ -27,11 +27,13 @@
 #include "linear.cuh"
 #include "pack.cuh"
 #include "plan.cuh"
+#include "umma_epilogue.cuh"
 
 namespace gshard {
 
 namespace {
 
+using umma_epi::kPasses3;
 constexpr int kSms = 148;                    // multiprocessors of a B200: sizes the work split, not the grids
 
 // The operator's epilogue on `splits` fp32 partial products of n4 float4 each, added in order.
@@ -60,8 +62,14 @@ __device__ __forceinline__ void split3(const float* f, float* hi, float* mid, fl
     lo[j] = r - mid[j];
   }
 }
-__global__ void __launch_bounds__(256) linear_split_kernel(const float* __restrict__ src, __nv_bfloat16* __restrict__ dst, long long n8) {
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n8; i += (long long)gridDim.x * 256) {
+// Two tensors in one launch (the second may have no elements), n8 packs of 8 values each.
+__global__ void __launch_bounds__(256) linear_split_kernel(const float* __restrict__ src0, __nv_bfloat16* __restrict__ dst0, long long n0,
+                                                           const float* __restrict__ src1, __nv_bfloat16* __restrict__ dst1, long long n1) {
+  for (long long at = (long long)blockIdx.x * 256 + threadIdx.x; at < n0 + n1; at += (long long)gridDim.x * 256) {
+    const bool second = at >= n0;
+    const float* src = second ? src1 : src0;
+    __nv_bfloat16* dst = second ? dst1 : dst0;
+    const long long n8 = second ? n1 : n0, i = second ? at - n0 : at;
     float f[8], hi[8], mid[8], lo[8];
     load_pack<float, 4>(src + 8 * i, f);
     load_pack<float, 4>(src + 8 * i + 4, f + 4);
@@ -209,10 +217,10 @@ int splits_for(long long rows, int cols, long long depth) {
   return (int)((k_blocks + per - 1) / per);      // no empty run at the end
 }
 
-// Whether w streams through the CUDA cores (linear_few.cu): up to 2 rows, and up to 8 where a product is not one launch of
-// linear_mid.cu.  Measured, us, few to mid: 1024 -> 8192 6.8 to 7.5 for two rows, 8.2 to 7.6 for three, 10.5 to 7.5 for
+// Whether w streams through the CUDA cores (linear_few.cu): up to 2 rows, and up to 8 of fp32 (whose planes would
+// first be written) or where a product is not one launch of linear_mid.cu.  Measured, us, few to mid: 1024 -> 8192 6.8 to 7.5 for two rows, 8.2 to 7.6 for three, 10.5 to 7.5 for
 // eight; 2048 -> 2048 5.9 to 6.5, 6.6 to 6.5, 8.8 to 6.5; 8192 -> 1024 8.0 to 9.8, 9.2 to 9.8, 11.6 to 9.8.
-bool few_rows(int64_t n, MidShape mid) { return n <= 2 || (n <= 8 && !mid.bn); }
+bool few_rows(int64_t n, bool bf16, MidShape mid) { return n <= 2 || (n <= 8 && !(bf16 && mid.bn)); }
 
 struct LinearPlan {
   size_t status, xp, wp, dpre, colsum, join, total;
@@ -225,8 +233,8 @@ LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, int out_dtype, boo
   LinearPlan p{};
   const bool bf16 = dtype == GSHARD_BF16;
   p.status = c.take(256);
-  if (!backward && bf16 && out_dtype == dtype) p.mid = linear_mid_shape(n, cols, K, 1);
-  if (n == 0 || (!backward && few_rows(n, p.mid))) { p.total = c.off; return p; }
+  if (!backward) p.mid = linear_mid_shape(n, cols, K, bf16 ? 1 : kPasses3, out_dtype == GSHARD_F32);
+  if (n == 0 || (!backward && few_rows(n, bf16, p.mid))) { p.total = c.off; return p; }
   p.xp = c.take(bf16 ? 0 : (size_t)n * K * 6);             // planes of fp32 operands
   p.wp = c.take(bf16 ? 0 : (size_t)K * cols * 6);
   if (!backward) {
@@ -243,10 +251,8 @@ LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, int out_dtype, boo
   p.chunk = (int)std::max<long long>(32, (n + want - 1) / want);
   p.chunks = (int)((n + p.chunk - 1) / p.chunk);
   p.colsum = c.take((size_t)p.chunks * cols * 4);
-  if (bf16) {
-    p.dx_mid = linear_mid_shape(n, K, cols, p.planes);
-    p.dw_mid = linear_mid_shape(K, cols, n, p.planes);
-  }
+  p.dx_mid = linear_mid_shape(n, K, cols, bf16 ? p.planes : kPasses3, !bf16);
+  p.dw_mid = linear_mid_shape(K, cols, n, bf16 ? p.planes : kPasses3, !bf16);
   p.dx_splits = p.dx_mid.bn ? 1 : splits_for(n, K, cols);
   p.dw_splits = p.dw_mid.bn ? 1 : splits_for(K, cols, n);
   p.join = c.take(std::max(p.dx_splits > 1 ? (size_t)p.dx_splits * n * K * 4 : 0,
@@ -272,8 +278,9 @@ Dims linear_dims(int K, int cols) {
   one.G = 1; one.S = 1; one.C = 1; one.E = 2; one.M = K; one.H = cols; one.dtype = GSHARD_BF16;
   return make_dims(one);
 }
-void split_planes(const void* src, void* dst, long long n, cudaStream_t st) {
-  linear_split_kernel<<<stride_grid(n / 8), 256, 0, st>>>(static_cast<const float*>(src), static_cast<__nv_bfloat16*>(dst), n / 8);
+void split_planes(const void* src0, void* dst0, long long n0, const void* src1, void* dst1, long long n1, cudaStream_t st) {
+  linear_split_kernel<<<stride_grid((n0 + n1) / 8), 256, 0, st>>>(static_cast<const float*>(src0), static_cast<__nv_bfloat16*>(dst0), n0 / 8,
+                                                                  static_cast<const float*>(src1), static_cast<__nv_bfloat16*>(dst1), n1 / 8);
   count_launch();
 }
 
@@ -332,7 +339,7 @@ int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype
   int* status = static_cast<int*>(workspace);
   const LinearEpilogue lin{bias, residual, pre, activation};
   const bool out_f32 = out_dtype == GSHARD_F32;
-  if (few_rows(n_rows, pl.mid)) {
+  if (few_rows(n_rows, dtype == GSHARD_BF16, pl.mid)) {
     GS_CHECK(launch_linear_few((int)n_rows, K, cols, dtype == GSHARD_BF16, out_f32, x, w, y, lin, status, st));
     return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
   }
@@ -341,14 +348,13 @@ int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype
   UmmaGemm g{};
   g.A = x; g.B = w; g.C = y; g.rows = (int)n_rows; g.cols = cols; g.K = K; g.batch = 1;
   g.a_kmajor = true; g.b_kmajor = false; g.a_ld = K; g.b_ld = cols; g.c_ld = cols;
-  if (pl.mid.bn) return launch_linear_mid(g, lin, pl.mid, true, status, st);
   g.clear_status = 1;
   g.a_stream = 1; g.prefer_two_sm = 1; g.out_f32 = out_f32;
   if (dtype == GSHARD_F32) {
-    split_planes(x, ws + pl.xp, n_rows * K, st);
-    split_planes(w, ws + pl.wp, (long long)K * cols, st);
+    split_planes(x, ws + pl.xp, n_rows * K, w, ws + pl.wp, (long long)K * cols, st);
     g.A = ws + pl.xp; g.B = ws + pl.wp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * K; g.b_bs = (long long)K * cols; g.a_stream = 0;
   }
+  if (pl.mid.bn) return launch_linear_mid(g, lin, pl.mid, true, status, st);
   g.runs = out_f32;
   if (pl.splits == 1) {
     g.linear = &lin;
@@ -417,6 +423,8 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
   bool cleared = buf || colsum;                   // the status word, by the first kernel of the call
   const Dims d = linear_dims(K, cols);
   float* join = reinterpret_cast<float*>(ws + pl.join);
+  if (fp32 && (dx || dw))
+    split_planes(w, ws + pl.wp, dx ? (long long)K * cols : 0, x, ws + pl.xp, dw ? n_rows * K : 0, st);
   if (dx) {                                       // [n, K] = dpre [n, cols] . w^T, both contiguous along cols
     UmmaGemm g{};
     g.A = dpre; g.B = w; g.C = dx; g.rows = (int)n_rows; g.cols = K; g.K = cols; g.batch = 1;
@@ -424,7 +432,6 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
     g.prefer_two_sm = 1; g.out_f32 = fp32; g.clear_status = !cleared;
     cleared = true;
     if (fp32) {
-      split_planes(w, ws + pl.wp, (long long)K * cols, st);
       g.B = ws + pl.wp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * cols; g.b_bs = (long long)K * cols;
     } else if (planes == 2) {
       g.planes_a = 2; g.planes_b = 1; g.a_bs = n_rows * cols;
@@ -437,7 +444,6 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
     g.a_kmajor = false; g.b_kmajor = false; g.a_ld = K; g.b_ld = cols; g.c_ld = cols;
     g.prefer_two_sm = 1; g.out_f32 = fp32; g.clear_status = !cleared;
     if (fp32) {
-      split_planes(x, ws + pl.xp, n_rows * K, st);
       g.A = ws + pl.xp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * K; g.b_bs = n_rows * cols;
     } else if (planes == 2) {
       g.planes_a = 1; g.planes_b = 2; g.b_bs = n_rows * cols;

@@ -10,10 +10,10 @@ namespace gshard {
 int launch_linear_few(int n, int K, int cols, bool bf16, bool out_f32, const void* x, const void* w, void* y,
                       const LinearEpilogue& lin, int* status, cudaStream_t st);
 
-// linear_mid.cu: a product whose output tiles run at once, with the operator's epilogue, in one launch (bf16 output; operands
-// as in UmmaGemm, in at most two planes together).  bn == 0: too many tiles, or too deep for them.
+// linear_mid.cu: a product whose output tiles run at once, with the operator's epilogue, in one launch (operands
+// as in UmmaGemm: bf16 output with at most two planes together, fp32 output with one or three each).  bn == 0: too many tiles, or too deep for them.
 struct MidShape { int bn, splits; };
-MidShape linear_mid_shape(long long rows, int cols, long long depth, int passes);
+MidShape linear_mid_shape(long long rows, int cols, long long depth, int passes, bool out_f32);
 int launch_linear_mid(const UmmaGemm& g, const LinearEpilogue& lin, MidShape shape, bool clear_status, int* status, cudaStream_t st);
 
 // The operator's epilogue on four neighbouring sums at element `off` (column `col`) of the output.

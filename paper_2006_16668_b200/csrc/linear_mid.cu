@@ -11,7 +11,7 @@
 //     holds, and each MMA 35;
 //   * the status word is cleared by the first CTA instead of a memset before the launch (3 us less).  A CTA reports only
 //     after a wait of two seconds ran out, long after the first CTA of a grid whose CTAs all run at once began.
-// Warp 0 feeds TMA loads, warp 1 issues the MMAs, then all eight warps take the accumulator out of tensor memory.
+// fp32 operands come as three bf16 planes (linear.cu).  Warp 0 feeds TMA loads, warp 1 issues the MMAs, then all eight warps take the accumulator out of tensor memory.
 #include <cuda.h>
 
 #include <algorithm>
@@ -33,6 +33,7 @@ constexpr int kMidBox = 64 * kMidDepth * 2;            // one box of an MN-major
 constexpr int kMidMaxStages = 12;
 constexpr int kMidBarBytes = 1024;                     // barriers, before the stages
 constexpr int kMidSmem = 226 * 1024;                   // used at most
+constexpr int kMidAlone = 120 * 1024;                  // asked for at least: more than half of a multiprocessor's
 constexpr int kMidSms = 148;
 
 struct MidArgs {
@@ -46,15 +47,34 @@ struct MidArgs {
   int a_half, stages;                   // bytes of A's rows in half a stage
 };
 
+// fp32 output: the tensor core truncates its running sum at every step, so the leading product stays in an accumulator for
+// two k-blocks (256 deep) only and the epilogue adds the accumulators, rounding to nearest.  With operands in three planes
+// the five small products (2^-8 of it) come first, in two accumulators.  All of it lies in tensor memory at once.
+constexpr int kMidRunAccs = 8, kMidRun = 2;
+__device__ __forceinline__ int run_of(int it, int blocks, int passes) {
+  const int low = (passes - 1) * blocks;
+  if (it < low) return 2 * it >= low ? 1 : 0;
+  return (low ? 2 : 0) + (it - low) / kMidRun;
+}
+// K-blocks per CTA up to which this is the faster path.  Three planes are six products of each k-block: 512 rows of
+// 1024 -> 1024 (4 k-blocks) 22.1 to 18.0 us, 256 rows of 3000 -> 1024 (6) 26.9 to 28.7, 64 of 4096 -> 1024 (8) equal.  One
+// product with fp32 output: what tensor memory holds (16), 256 rows of 3000 -> 1024 13.9 to 9.6.
+int most_k_blocks(int passes, bool out_f32) {
+  if (out_f32) return passes > 1 ? 4 : kMidRunAccs * kMidRun;
+  return 64 / passes;
+}
+
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void st_peer(uint32_t addr, float a, float b, float c, float d) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
 }
 
-template <bool A_K, bool B_K, int BN, int SPLITS>
+template <bool A_K, bool B_K, int BN, int SPLITS, typename TY>
 __global__ void __launch_bounds__(kMidThreads, 1)
 linear_mid_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MidArgs p) {
+  constexpr bool RUNS = sizeof(TY) == 4;
+  constexpr int kAccs = RUNS ? kMidRunAccs : 1;
   constexpr int kBBytes = BN * kMidDepth * 2, kLd = BN + 4;      // floats per row of sums: rows start in different banks
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -81,7 +101,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     ptx::fence_mbar_init();
   }
   if (warp == 1) {
-    ptx::tmem_alloc(tmem_slot, BN);
+    ptx::tmem_alloc(tmem_slot, kAccs * BN);
     ptx::tmem_relinquish();
   }
   // what the epilogue adds to every row of this thread's four columns
@@ -131,7 +151,11 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     if (ptx::elect_one()) {
       constexpr uint32_t idesc = ptx::make_idesc_bf16(kMidRows, BN, !A_K, !B_K);
       int stage = 0; uint32_t phase = 0;
+      int prev = -1;
       for (int it = 0; it < iters; ++it) {
+        const int acc = RUNS ? run_of(it, blocks, p.passes) : 0;
+        const bool more = acc == prev;                 // than the accumulator's first k-block
+        prev = acc;
         if (!ptx::mbar_wait(full + stage, phase, abort_flag)) { ok = false; break; }
         ptx::tc_fence_after_sync();
         const uint32_t sa = ptx::smem_u32(smem + stage * stage_bytes), sb = sa + 2 * p.a_half;
@@ -141,7 +165,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                                   : ptx::make_smem_desc(sa + k * 2048, kMidBox, 1024);
           const uint64_t db = B_K ? ptx::make_smem_desc(sb + k / 4 * (kBBytes / 2) + k % 4 * 32, 16, 1024)
                                   : ptx::make_smem_desc(sb + k * 2048, kMidBox, 1024);
-          ptx::umma_bf16(tmem, da, db, idesc, (it | k) != 0 ? 1u : 0u);
+          ptx::umma_bf16(tmem + (uint32_t)(acc * BN), da, db, idesc, more || k != 0 ? 1u : 0u);
         }
         ptx::umma_commit(empty + stage);
         if (++stage == stages) { stage = 0; phase ^= 1u; }
@@ -175,6 +199,17 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         uint32_t v[32];
         ptx::tmem_ld_32x32(src + (uint32_t)c, v);
         ptx::tmem_ld_wait();
+        if (RUNS) {
+          const int accs = run_of(iters - 1, blocks, p.passes) + 1;
+#pragma unroll 1
+          for (int a = 1; a < accs; ++a) {             // small terms first
+            uint32_t more[32];
+            ptx::tmem_ld_32x32(src + (uint32_t)(a * BN + c), more);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(more[i]));
+          }
+        }
         if (r < valid) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4)
@@ -189,7 +224,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
   else __syncthreads();
   if (warp == 1) {
     ptx::tc_fence_after_sync();
-    ptx::tmem_dealloc(tmem, BN);
+    ptx::tmem_dealloc(tmem, kAccs * BN);
   }
   if (failed || !in) return;
   constexpr int kStep = kMidThreads / kQuads, U = 4;   // rows between a thread's, rows in flight
@@ -197,11 +232,11 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
   const long long top = (long long)(row0 + rank * share) * p.cols + col;
   for (int first = tid / kQuads; first < own; first += U * kStep) {
     float4 s[U];
-    Pack<__nv_bfloat16, 4> res[U];
+    Pack<TY, 4> res[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int r = first + u * kStep;
-      if (p.lin.residual && r < own) res[u].load(static_cast<const __nv_bfloat16*>(p.lin.residual) + top + (long long)r * p.cols);
+      if (p.lin.residual && r < own) res[u].load(static_cast<const TY*>(p.lin.residual) + top + (long long)r * p.cols);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -219,7 +254,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
       for (int u = 0; u < U; ++u) {
         const int r = first + u * kStep;
         const float f[4] = {s[u].x, s[u].y, s[u].z, s[u].w};
-        if (r < own) store_pack<__nv_bfloat16, 4>(static_cast<__nv_bfloat16*>(p.lin.pre) + top + (long long)r * p.cols, f);
+        if (r < own) store_pack<TY, 4>(static_cast<TY*>(p.lin.pre) + top + (long long)r * p.cols, f);
       }
     }
     uint32_t v[4 * U];
@@ -228,7 +263,7 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
       v[4 * u] = __float_as_uint(s[u].x); v[4 * u + 1] = __float_as_uint(s[u].y);
       v[4 * u + 2] = __float_as_uint(s[u].z); v[4 * u + 3] = __float_as_uint(s[u].w);
     }
-    activate<4 * U, true>(v, p.lin.act);
+    activate<4 * U, sizeof(TY) == 2>(v, p.lin.act);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int r = first + u * kStep;
@@ -238,21 +273,23 @@ linear_mid_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         f[j] = __uint_as_float(v[4 * u + j]);
         if (p.lin.residual) f[j] += res[u].get(j);
       }
-      if (r < own) store_pack<__nv_bfloat16, 4>(static_cast<__nv_bfloat16*>(p.y) + top + (long long)r * p.cols, f);
+      if (r < own) store_pack<TY, 4>(static_cast<TY*>(p.y) + top + (long long)r * p.cols, f);
     }
   }
 }
 
-template <bool A_K, bool B_K, int BN, int SPLITS>
+template <bool A_K, bool B_K, int BN, int SPLITS, typename TY>
 int launch_mid_t(const CUtensorMap& ma, const CUtensorMap& mb, const MidArgs& p_in, cudaStream_t st) {
-  auto kern = linear_mid_kernel<A_K, B_K, BN, SPLITS>;
+  auto kern = linear_mid_kernel<A_K, B_K, BN, SPLITS, TY>;
   MidArgs p = p_in;
   const int stage = 2 * p.a_half + BN * kMidDepth * 2;
   const int valid = std::min(kMidRows, p.rows);
   const int sums = (valid + SPLITS - 1) / SPLITS * SPLITS * (BN + 4) * 4;
   const int room = kMidSmem - 1024 /*alignment*/ - kMidBarBytes - (SPLITS > 1 ? sums : 0);
   p.stages = std::min({kMidMaxStages, room / stage, std::max(2, p.run * p.passes)});
-  const int smem = 1024 + kMidBarBytes + (SPLITS > 1 ? p.stages * stage + sums : std::max(p.stages * stage, sums));
+  // At least kMidAlone, which keeps any other kernel that allocates tensor memory off the multiprocessor: CTAs of two
+  // clusters that waited for each other's tensor memory would never meet at their barriers.
+  const int smem = std::max(kMidAlone, 1024 + kMidBarBytes + (SPLITS > 1 ? p.stages * stage + sums : std::max(p.stages * stage, sums)));
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
     cudaGetLastError();
     return GSHARD_ERR_CUDA;
@@ -275,9 +312,12 @@ int launch_mid_t(const CUtensorMap& ma, const CUtensorMap& mb, const MidArgs& p_
 }
 
 template <bool A_K, bool B_K>
-int launch_mid(const CUtensorMap& ma, const CUtensorMap& mb, const MidArgs& p, MidShape s, cudaStream_t st) {
-#define GSHARD_MID(S)                                                                              \
-  case S: return s.bn == 64 ? launch_mid_t<A_K, B_K, 64, S>(ma, mb, p, st) : launch_mid_t<A_K, B_K, 128, S>(ma, mb, p, st);
+int launch_mid(const CUtensorMap& ma, const CUtensorMap& mb, const MidArgs& p, MidShape s, bool out_f32, cudaStream_t st) {
+#define GSHARD_MID(S)                                                                      \
+  case S:                                                                                  \
+    if (out_f32) return launch_mid_t<A_K, B_K, 64, S, float>(ma, mb, p, st);               \
+    return s.bn == 64 ? launch_mid_t<A_K, B_K, 64, S, __nv_bfloat16>(ma, mb, p, st)        \
+                      : launch_mid_t<A_K, B_K, 128, S, __nv_bfloat16>(ma, mb, p, st);
   switch (s.splits) {
     GSHARD_MID(1)
     GSHARD_MID(2)
@@ -294,24 +334,25 @@ int launch_mid(const CUtensorMap& ma, const CUtensorMap& mb, const MidArgs& p, M
 // 4096 -> 4096 21.5 to 26.9.  Equal at 64 k-blocks per CTA (1024 rows of 8192 -> 1024: 26.0 to 26.8), and
 // worse beyond.  Eight CTAs per cluster are no gain: 16 such clusters do not run at once (8192 -> 1024: 13 to 18), nor are
 // more than 128 CTAs in clusters certain to.
-MidShape linear_mid_shape(long long rows, int cols, long long depth, int passes) {
+MidShape linear_mid_shape(long long rows, int cols, long long depth, int passes, bool out_f32) {
   MidShape s{0, 1};
   const long long m_tiles = (rows + kMidRows - 1) / kMidRows, k_blocks = (depth + kMidDepth - 1) / kMidDepth;
-  for (int bn = 64; bn <= 128 && !s.bn; bn *= 2)
+  for (int bn = 64; bn <= (out_f32 ? 64 : 128) && !s.bn; bn *= 2)
     if (m_tiles * ceil_div(cols, bn) <= kMidSms) s.bn = bn;
   if (!s.bn) return s;
   const long long tiles = m_tiles * ceil_div(cols, s.bn);
   while (s.splits < 4 && 2 * s.splits * tiles <= 128 && k_blocks >= 4 * s.splits) s.splits *= 2;
   // no empty run at the end
   while (s.splits > 1 && (s.splits - 1) * ((k_blocks + s.splits - 1) / s.splits) >= k_blocks) s.splits /= 2;
-  if ((k_blocks + s.splits - 1) / s.splits * passes > 64) s.bn = 0;
+  if ((k_blocks + s.splits - 1) / s.splits > most_k_blocks(passes, out_f32)) s.bn = 0;
   return s;
 }
 
 int launch_linear_mid(const UmmaGemm& g, const LinearEpilogue& lin, MidShape s, bool clear_status, int* status, cudaStream_t st) {
-  if (g.out_f32 || g.batch != 1 || g.c_ld != g.cols || (!g.a_kmajor && g.b_kmajor)) return GSHARD_ERR_INTERNAL;
+  if (g.batch != 1 || g.c_ld != g.cols || (!g.a_kmajor && g.b_kmajor)) return GSHARD_ERR_INTERNAL;
   const int pa = std::max(1, g.planes_a), pb = std::max(1, g.planes_b);
-  if (pa * pb > 2) return GSHARD_ERR_INTERNAL;
+  const bool planes3 = pa == 3;
+  if (planes3 ? pb != 3 || !g.out_f32 : pa * pb > 2 || (pa * pb == 2 && g.out_f32)) return GSHARD_ERR_INTERNAL;
   // Rows of A that are loaded: whole swizzle atoms of 8.  The MMA reads 128; what it finds behind the loaded ones goes
   // to accumulator rows that no one reads.
   const int a_rows = g.a_kmajor ? std::min(kMidRows, (g.rows + 7) / 8 * 8) : kMidRows;
@@ -325,14 +366,15 @@ int launch_linear_mid(const UmmaGemm& g, const LinearEpilogue& lin, MidShape s, 
   p.y = g.C; p.lin = lin; p.status = status; p.clear_status = clear_status; p.rows = g.rows; p.cols = g.cols;
   p.k_blocks = ceil_div(g.K, kMidDepth);
   p.run = ceil_div(p.k_blocks, s.splits);
-  p.passes = pa * pb;
-  p.pass_a = pa == 2 ? 0x01 : 0;                       // two planes: the low one first
-  p.pass_b = pb == 2 ? 0x01 : 0;
+  p.passes = planes3 ? umma_epi::kPasses3 : pa * pb;
+  p.pass_a = planes3 ? umma_epi::kPassA3 : pa == 2 ? 0x01 : 0;     // two planes: the low one first
+  p.pass_b = planes3 ? umma_epi::kPassB3 : pb == 2 ? 0x01 : 0;
   p.a_half = a_rows * 128;
   p.a_once = g.cols <= s.bn;
   p.b_once = g.rows <= kMidRows;
-  if (!g.a_kmajor) return launch_mid<false, false>(ma, mb, p, s, st);
-  return g.b_kmajor ? launch_mid<true, true>(ma, mb, p, s, st) : launch_mid<true, false>(ma, mb, p, s, st);
+  const bool out_f32 = g.out_f32 != 0;
+  if (!g.a_kmajor) return launch_mid<false, false>(ma, mb, p, s, out_f32, st);
+  return g.b_kmajor ? launch_mid<true, true>(ma, mb, p, s, out_f32, st) : launch_mid<true, false>(ma, mb, p, s, out_f32, st);
 }
 
 }  // namespace gshard

@@ -314,3 +314,26 @@ def test_rows_of_one_launch_do_not_touch_each_other():
         y, _ = _forward(t)
         assert torch.isnan(y[n - 1]).all() and not torch.isfinite(y[0]).any()
         assert torch.equal(y[1:n - 1], y0[1:n - 1])
+
+
+@pytest.mark.parametrize("dtype,n,K,cols", [
+    (BF, 9, 8, 8), (BF, 33, 264, 200), (BF, 100, 2048, 9000), (BF, 130, 8192, 40), (BF, 64, 2056, 4000), (BF, 1000, 1408, 712),
+    (F32, 9, 8, 8), (F32, 33, 264, 200), (F32, 100, 2048, 1000), (F32, 60, 512, 9000), (F32, 130, 1024, 1032), (F32, 1025, 392, 648)])
+def test_fp32_products_of_one_launch(dtype, n, K, cols):
+    """fp32 results are accumulated in runs of 256, so their error does not grow with the depth."""
+    t = _make(n, K, cols, dtype, F32)
+    act = ACTS[(n + cols) % 5]
+    guard = torch.full((n + 2, cols), 7.0, device="cuda")
+    y, kept = _forward(t, act, residual=True, pre=True, y=guard[1:n + 1])
+    _check_forward(t, y, kept, act, residual=True)
+    assert (guard[0] == 7).all() and (guard[-1] == 7).all()
+    again, _ = _forward(t, act, residual=True)
+    assert torch.equal(again, y)
+    # a run is 16 truncated steps of at most 2^-23 of the absolute sum; the small products, up to 240 steps at 2^-8 of it,
+    # count as one, the sums of at most 64 runs and of the cluster, 2^-24 of a partial sum each, as fewer than 8, and the
+    # three products left out as one: 32 covers them
+    plain, _ = _forward(t, bias=False)
+    want = t["x"].double() @ t["w"].double()
+    total = t["x"].double().abs() @ t["w"].double().abs()
+    within(plain, want, 32 * 2 * U32 * total + 1e-30, "product")
+    _check_backward(t, act, *_backward(t, act))
