@@ -290,7 +290,8 @@ int launch_mid_t(const CUtensorMap& ma, const CUtensorMap& mb, const MidArgs& p_
   // At least kMidAlone, which keeps any other kernel that allocates tensor memory off the multiprocessor: CTAs of two
   // clusters that waited for each other's tensor memory would never meet at their barriers.
   const int smem = std::max(kMidAlone, 1024 + kMidBarBytes + (SPLITS > 1 ? p.stages * stage + sums : std::max(p.stages * stage, sums)));
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+  // the same limit from every call: another thread may be between its own call of this and its launch
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMidSmem) != cudaSuccess) {
     cudaGetLastError();
     return GSHARD_ERR_CUDA;
   }

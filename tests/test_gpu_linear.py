@@ -337,3 +337,35 @@ def test_fp32_products_of_one_launch(dtype, n, K, cols):
     total = t["x"].double().abs() @ t["w"].double().abs()
     within(plain, want, 32 * 2 * U32 * total + 1e-30, "product")
     _check_backward(t, act, *_backward(t, act))
+
+
+def test_two_threads_at_once():
+    """Calls of different sizes from two threads, each with its own stream and workspace, do not disturb each other."""
+    import threading
+    sizes = ([(3, 1024, 72), (128, 2048, 264)], [(100, 512, 1000), (700, 1096, 520)])
+    cases = [[(t, _forward(t, "gelu", residual=True)[0], torch.empty_like(t["dy"]), _ws(t, False))
+              for t in (_make(*s, BF) for s in group)] for group in sizes]
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(group):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for i in range(200):
+                    t, want, y, ws = group[i % 2]
+                    B.gshard_linear_forward(t["x"], t["w"], y, bias=t["bias"], residual=t["residual"], activation="gelu",
+                                            workspace=ws)
+                stream.synchronize()
+        except Exception as e:                               # noqa: BLE001 - reported by the main thread
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(g,)) for g in cases]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not failed, failed
+    for group in cases:
+        for _, want, y, ws in group:
+            assert torch.equal(y, want) and B.gshard_moe_last_device_status(ws) == B.GSHARD_OK
