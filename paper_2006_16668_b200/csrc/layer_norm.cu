@@ -409,11 +409,13 @@ int ln_bwd_launch(long long n, int M, const T* x, const float* gamma, const floa
   const bool sums_in_smem = M > 8192;
   const int smem = partial && (s.teams > 1 || sums_in_smem) ? 2 * M * (int)sizeof(float) : 0;
   const int fill = ln_fill(M / W, s.team, s.nv / W);
+  // the same limit from every call (rows have at most 16384 elements): another thread may be between its own call and launch
+  constexpr int kLnBwdSmem = 2 * 16384 * (int)sizeof(float);
 #define GSHARD_LN_F(NV, NT, MINB, AHEAD, SMEM, FILL)                                                                  \
   do {                                                                                                                \
     auto kern = ln_bwd_kernel<T, W, NV / W, NT, MINB, AHEAD, SMEM, FILL>;                                             \
     if (smem > 48 * 1024 &&                                                                                           \
-        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {               \
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kLnBwdSmem) != cudaSuccess) {         \
       cudaGetLastError();                                                                                             \
       return GSHARD_ERR_CUDA;                                                                                         \
     }                                                                                                                 \

@@ -241,3 +241,32 @@ def test_refusals():
     with pytest.raises(B.GshardError) as e:
         B.gshard_layer_norm_backward(t["x"], t["gamma"], mean, rstd, t["dy"], y, torch.empty(64, device="cuda"), workspace=small)
     assert e.value.code in (B.GSHARD_ERR_WORKSPACE_TOO_SMALL, B.GSHARD_ERR_INVALID_ARG)
+
+
+def test_long_rows_from_two_threads_at_once():
+    """Backward passes over rows of two lengths, whose blocks share different amounts of memory, from two threads."""
+    import threading
+    cases = []
+    for M in (9000, 16384):
+        t = _make(40, M, torch.float32)
+        _, mean, rstd = _forward(t)
+        cases.append((t, mean, rstd, _backward(t, mean, rstd)))
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(t, mean, rstd, want):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(100):
+                    got = _backward(t, mean, rstd)
+                torch.cuda.current_stream().synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+        except Exception as e:                               # noqa: BLE001 - reported by the main thread
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=c) for c in cases]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not failed, failed
