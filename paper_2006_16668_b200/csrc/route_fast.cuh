@@ -34,6 +34,13 @@ __device__ __forceinline__ float sigmoid_fast(float l) {
   return y;
 }
 
+// exp(l - mx), up to a factor close to 1 that is the same for the whole row: below 2^20 the shift -mx log2(e) is rounded
+// before the logits' products with log2(e) are added to it exactly.  So a sum of these may be divided into these only: the
+// factor is 2^(half a step of the shift), 5e-6 at logits near 100 and 4 % near 10^6.
+__device__ __forceinline__ float row_exp(float l, float mx) {
+  return exp2_approx(fabsf(mx) <= 0x1p20f ? fmaf(l, kLog2e, -mx * kLog2e) : (l - mx) * kLog2e);
+}
+
 template <int LPR> __device__ __forceinline__ float seg_max(float v) {
 #pragma unroll
   for (int off = LPR / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, off));
@@ -251,7 +258,7 @@ route_fwd_fast_kernel(const __grid_constant__ RouteArgs a, float* __restrict__ s
       // exponentials of NaN or of infinite logits are caught by the two tests below
       if (need_sum) {
         mx = seg_max<LPR>(mx);
-        const float shift = -mx * kLog2e;      // its rounding is a factor that the sum shares
+        const float shift = -mx * kLog2e;      // row_exp of all values, two at a time
         f32x2 sum2x[2] = {both(0.f), both(0.f)};
 #pragma unroll
         for (int i = 0; i < V; i += 2) {
@@ -272,7 +279,7 @@ route_fwd_fast_kernel(const __grid_constant__ RouteArgs a, float* __restrict__ s
 #pragma unroll
           for (int i = 0; i < V; ++i) {
             const float l = lin.offset(i) < a.E ? usable(row[lin.expert(i)]) : -INFINITY;
-            const float e = exp2_approx((l - m2) * kLog2e);
+            const float e = row_exp(l, m2);
             sum2 += e;
             if (odd) v[i] = e;
           }
@@ -587,7 +594,8 @@ route_fwd_fast_kernel(const __grid_constant__ RouteArgs a, float* __restrict__ s
       w = seg_ratio<LPR>(l, a.sigmoid, total);
       w = total > 0.f ? a.scale * (w / total) : 0.f;
     } else {
-      w = picked < 0 ? 0.f : a.scale * (a.sigmoid ? sigmoid_f(l) : expf(l - mx) * inv);
+      // by logits the sum was taken over row_exp, otherwise over exponentials of differences
+      w = picked < 0 ? 0.f : a.scale * (a.sigmoid ? sigmoid_f(l) : (MODE == kByLogits ? row_exp(l, mx) : expf(l - mx)) * inv);
     }
     if (active && p < a.k) {
       a.expert_idx[t * a.k + p] = picked;

@@ -1,0 +1,79 @@
+"""Routing of logits far from zero and far from one another, against the definition in 64 bits.
+
+A softmax depends on differences of logits only, so its weights, means and gradients are held to a bound in the
+largest difference of a row, whatever the row's offset.  The exponent of a score is a difference of logits times
+log2(e), rounded once: its error, times ln 2, is the difference times U; some 24 U are left to exp2, the division and the
+scale.  A sigmoid's exponent is the logit itself."""
+import math
+
+import pytest
+import torch
+
+import test_gpu_route as R
+from paper_2006_16668_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = R.BF, R.F32
+OFFSETS = (0.0, 100.0, -100.0, 1e3, -1e3, 1e4, -1e4, 1e5, -1e5, 5e5, -5e5, 9e5)
+
+
+@pytest.fixture
+def bounds_in_differences(monkeypatch):
+    def spread(l):
+        there = torch.isfinite(l) & (l.abs() < 1e30)
+        top = l.masked_fill(~there, -math.inf).amax(-1, keepdim=True)
+        low = l.masked_fill(~there, math.inf).amin(-1, keepdim=True)
+        return 24 + torch.where(top >= low, top - low, torch.zeros_like(top))
+    monkeypatch.setattr(R, "_spread", spread)
+
+
+def _offset_logits(G, S, E, dtype, std, seed, offsets=OFFSETS):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    l = torch.randn(G, S, E, generator=gen, device="cuda") * std
+    at = torch.randint(0, len(offsets), (G, S, 1), generator=gen, device="cuda")
+    return (l + torch.tensor(offsets, device="cuda")[at]).to(dtype)
+
+
+def _both_ways(kw, logits, bias, k, m=True):
+    G, S, E = logits.shape
+    cfg = B.make_route(G=G, S=S, E=E, k=k, dtype="bf16" if logits.dtype == BF else "f32", **kw)
+    out = R._route(cfg, logits, bias, m=m, load=m)
+    R._check_forward(cfg, kw, logits, bias, out)
+    gen = torch.Generator(device="cuda").manual_seed(E + k)
+    dweight = torch.randn(G, S, k, generator=gen, device="cuda")
+    dm = torch.randn(G, E, generator=gen, device="cuda")
+    for d in (None, dm):
+        R._check_backward(cfg, kw, logits, out[0], dweight, d, R._backward(cfg, logits, out[0], dweight, d))
+
+
+# 8 or 32 lanes per token, single-element loads, and the kernel of every other shape
+SHAPES = [(2, 70, 64, 4), (1, 2400, 64, 2), (1, 2400, 256, 8), (1, 70, 100, 3), (1, 40, 602, 2), (2, 30, 2048, 2), (1, 9, 3000, 4)]
+
+
+@pytest.mark.parametrize("m", [False, True])
+@pytest.mark.parametrize("std", [1.0, 8.0])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("G,S,E,k", SHAPES)
+def test_raw_softmax_weights_ignore_a_common_offset(G, S, E, k, dtype, std, m, bounds_in_differences):
+    logits = _offset_logits(G, S, E, dtype, std, seed=E + S)
+    _both_ways(dict(renormalise=False), logits, None, k, m=m)
+
+
+@pytest.mark.parametrize("kw", [{}, dict(renormalise=False, groups=4, groups_kept=2),
+                                dict(renormalise=False, groups=4, groups_kept=2, group_top=2)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("G,S,E,k", [(1, 2400, 64, 4), (2, 70, 256, 8), (1, 60, 100, 3)])
+def test_offsets_with_groups_and_renormalised(G, S, E, k, dtype, kw, bounds_in_differences):
+    # with sums of scores, offsets at which a step of either type leaves the scores far above 2^-53 of one another
+    logits = _offset_logits(G, S, E, dtype, 2.0, seed=E + S + 1, offsets=OFFSETS[:3] if kw.get("group_top") == 2 else OFFSETS)
+    _both_ways(kw, logits, None, k)
+
+
+def test_barred_experts_beside_an_offset(bounds_in_differences):
+    """NaN, infinities and empty rows among rows with offsets: the clean-up of one token leaves its neighbours alone."""
+    for E in (64, 100, 2048):
+        logits = _offset_logits(1, 300, E, F32, 1.0, seed=E)
+        logits[0, ::5, 3], logits[0, 1::7, 9], logits[0, 2::11] = math.nan, -math.inf, -math.inf
+        logits[0, 3::13, 5] = math.inf
+        _both_ways(dict(renormalise=False), logits, None, 3)
