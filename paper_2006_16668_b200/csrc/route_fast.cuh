@@ -41,6 +41,15 @@ __device__ __forceinline__ float row_exp(float l, float mx) {
   return exp2_approx(fabsf(mx) <= 0x1p20f ? fmaf(l, kLog2e, -mx * kLog2e) : (l - mx) * kLog2e);
 }
 
+// s (1 - s) of s = sigmoid(l): with e = exp(-|l|) it is e / (1 + e)^2, which loses nothing where s is close to 1 (s times
+// the difference 1 - s is 0.2 % off at l = 10 and 0 from 17 on)
+__device__ __forceinline__ float sigmoid_slope_fast(float l) {
+  const float e = exp2_approx(-fabsf(l) * kLog2e);
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return e * r * r;
+}
+
 template <int LPR> __device__ __forceinline__ float seg_max(float v) {
 #pragma unroll
   for (int off = LPR / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, off));
@@ -737,7 +746,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_bwd_fast_kernel(const Rou
 #pragma unroll
           for (int w = 0; w < W; ++w) {
             const float x = v[j * W + w];
-            if (a.sigmoid) { const float s = sigmoid_fast(x); o[w] = d[w] * inv_s * s * (1.f - s); }
+            if (a.sigmoid) o[w] = d[w] * inv_s * sigmoid_slope_fast(x);
             else o[w] = x * inv * (d[w] * inv_s - dot);
           }
         }

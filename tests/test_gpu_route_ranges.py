@@ -77,3 +77,27 @@ def test_barred_experts_beside_an_offset(bounds_in_differences):
         logits[0, ::5, 3], logits[0, 1::7, 9], logits[0, 2::11] = math.nan, -math.inf, -math.inf
         logits[0, 3::13, 5] = math.inf
         _both_ways(dict(renormalise=False), logits, None, 3)
+
+
+@pytest.mark.parametrize("renormalise", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("G,S,E,k", SHAPES)
+def test_sigmoid_of_wide_logits(G, S, E, k, dtype, renormalise):
+    """Standard deviation 8: scores near 0 and 1, whose gradient s (1 - s) is small but not zero."""
+    logits = R._logits(G, S, E, dtype, seed=3, std=8.0)
+    _both_ways(dict(score="sigmoid", renormalise=renormalise), logits, None, k)
+
+
+@pytest.mark.parametrize("E", [32, 100, 512, 3000])
+def test_sigmoid_gradient_at_given_logits(E):
+    """d m / d l = s (1 - s) / S from -90 to 90: relative error as at zero."""
+    logits = torch.linspace(-90, 90, E, device="cuda").reshape(1, 1, E).contiguous()
+    logits[0, 0, 0], logits[0, 0, 1] = -math.inf, math.nan
+    cfg = B.make_route(G=1, S=1, E=E, k=2, score="sigmoid")
+    idx = torch.full((1, 1, 2), -1, dtype=torch.int32, device="cuda")
+    got = R._backward(cfg, logits, idx, torch.zeros(1, 1, 2, device="cuda"), torch.ones(1, E, device="cuda")).double()
+    l = logits.double()
+    want = torch.sigmoid(l) * torch.sigmoid(-l)
+    assert (got[..., :2] == 0).all()
+    err = (got - want).abs()[..., 2:]
+    assert (err <= (24 + l[..., 2:].abs()) * 4 * R.U32 * want[..., 2:] + 1e-37).all(), float((err / want[..., 2:]).max())
