@@ -65,7 +65,8 @@ __device__ __forceinline__ float activation_value_fast(float v, int act) {
     case GSHARD_ACT_GELU: {
       float e;
       const float q = normal_tail(v, e);
-      return fmaf(-fabsf(v), q, fmaxf(v, 0.f));          // v (1 - q) or v q
+      // v (1 - q) or v q; q is 0 from 14 on, and the product stays 0 for an infinite v
+      return fmaf(-fabsf(fminf(v, 16.f)), q, fmaxf(v, 0.f));
     }
     case GSHARD_ACT_GELU_TANH: {
       const float d = 1.f + approx_exp2(-2.3022082f * v * fmaf(0.044715f * v, v, 1.f));

@@ -1,0 +1,43 @@
+"""Infinities, NaN and very large values under the linear operator's activations and in its gradient, against the
+definition in 64 bits.  They are put into the pre-activations through the bias (one of each per column), so that every
+type and every kernel meets them."""
+import math
+
+import pytest
+import torch
+
+import test_gpu_linear as L
+from operator_reference import HALF, activation
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = L.BF, L.F32
+ODD = (math.inf, -math.inf, math.nan, 1e20, -1e20, 1e30, -1e30, 3e38, -3e38)
+
+# one or two rows, up to 8 of fp32, one launch, pairs of CTAs, one CTA per tile, runs of a cut contraction
+SIZES = [(1, 256, 512), (8, 256, 512), (300, 256, 512), (3000, 256, 512), (100, 264, 37888), (130, 40000, 64)]
+
+
+@pytest.mark.parametrize("dtype,out", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("act", [a for a in L.ACTS if a != "relu"])
+@pytest.mark.parametrize("n,K,cols", SIZES)
+def test_activation_of_infinity_nan_and_huge_values(n, K, cols, act, dtype, out):
+    t = L._make(n, K, cols, dtype, out)
+    t["bias"][:len(ODD)] = torch.tensor(ODD, device="cuda")
+    t["bias"][-len(ODD):] = torch.tensor(ODD, device="cuda")
+    y, kept = L._forward(t, act, pre=True)
+    pre = t["x"].double() @ t["w"].double() + t["bias"].double()
+    for what, got, want in (("pre", kept, pre), ("y", y, activation(pre, act))):
+        got = got.double()
+        assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+        assert torch.equal(torch.isinf(got), torch.isinf(want)), what
+        assert torch.equal(got[torch.isinf(got)], want[torch.isinf(want)]), what
+        there = torch.isfinite(want)
+        # x . w is about 1, far from its neighbours in size: the columns of huge values have two roundings and the exp
+        # of an activation, the others are held by the general tests
+        huge = there & (pre.abs() > 1e10)
+        bound = (HALF[out] * 1.01 + 8 * L.U32) * want.abs() + 1e-30
+        assert ((got - want).abs() <= bound)[huge].all(), what
+    rest = slice(len(ODD), cols - len(ODD))
+    u = {k: (v[..., rest].contiguous() if k in ("w", "bias", "dy") else v) for k, v in t.items()}
+    L._check_forward(u, y[:, rest], kept[:, rest], act)
