@@ -4,11 +4,18 @@
 
 namespace gshard {
 
+// max(v, 0), where NaN stays NaN (fmaxf would answer 0)
+__device__ __forceinline__ float relu(float v) {
+  float y;
+  asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(v));
+  return y;
+}
+
 // relu(v), v Phi(v) (erf form), its tanh approximation 0.5 v (1 + tanh(u)) = v / (1 + exp(-2u)) with
 // u = sqrt(2/pi) (v + 0.044715 v^3), and v / (1 + exp(-v)).  exp may overflow to infinity: the quotient is then 0.
 __device__ __forceinline__ float activation_value(float v, int act) {
   switch (act) {
-    case GSHARD_ACT_RELU: return fmaxf(v, 0.f);
+    case GSHARD_ACT_RELU: return relu(v);
     case GSHARD_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
     case GSHARD_ACT_GELU_TANH: return v / (1.f + expf(-1.5957691216057308f * v * fmaf(0.044715f * v, v, 1.f)));
     case GSHARD_ACT_SILU: return v / (1.f + expf(-v));
@@ -61,7 +68,7 @@ __device__ __forceinline__ float normal_tail(float v, float& e) {
 }
 __device__ __forceinline__ float activation_value_fast(float v, int act) {
   switch (act) {
-    case GSHARD_ACT_RELU: return fmaxf(v, 0.f);
+    case GSHARD_ACT_RELU: return relu(v);
     case GSHARD_ACT_GELU: {
       float e;
       const float q = normal_tail(v, e);
