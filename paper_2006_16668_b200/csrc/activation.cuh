@@ -29,9 +29,10 @@ __device__ __forceinline__ float activation_slope(float v, int act) {
     case GSHARD_ACT_GELU:
       return fmaf(v * 0.39894228040143268f, expf(-0.5f * v * v), 0.5f * (1.f + erff(v * 0.70710678118654752f)));
     case GSHARD_ACT_GELU_TANH: {
-      // with s = 1 / (1 + exp(-2u)): d(v s)/dv = s + v s (1 - s) d(2u)/dv
+      // with s = 1 / (1 + exp(-2u)): d(v s)/dv = s + v s (1 - s) d(2u)/dv.  s (1 - s) is 0 long before v^2 overflows,
+      // and d(2u)/dv is held to a finite value so that the product stays 0.
       const float s = 1.f / (1.f + expf(-1.5957691216057308f * v * fmaf(0.044715f * v, v, 1.f)));
-      return fmaf(v * s * (1.f - s), 1.5957691216057308f * fmaf(0.134145f * v, v, 1.f), s);
+      return fmaf(v * s * (1.f - s), 1.5957691216057308f * fminf(fmaf(0.134145f * v, v, 1.f), 1e30f), s);
     }
     case GSHARD_ACT_SILU: {
       const float s = 1.f / (1.f + expf(-v));
@@ -93,7 +94,7 @@ __device__ __forceinline__ float activation_slope_fast(float v, int act) {
     }
     case GSHARD_ACT_GELU_TANH: {
       const float s = approx_rcp(1.f + approx_exp2(-2.3022082f * v * fmaf(0.044715f * v, v, 1.f)));
-      return fmaf(v * s * (1.f - s), 1.5957691216057308f * fmaf(0.134145f * v, v, 1.f), s);
+      return fmaf(v * s * (1.f - s), 1.5957691216057308f * fminf(fmaf(0.134145f * v, v, 1.f), 1e30f), s);
     }
     case GSHARD_ACT_SILU: {
       const float s = approx_rcp(1.f + approx_exp2(-1.4426950408889634f * v));

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import test_gpu_linear as L
-from operator_reference import HALF, activation
+from operator_reference import HALF, activation, slope
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +41,18 @@ def test_activation_of_infinity_nan_and_huge_values(n, K, cols, act, dtype, out)
     rest = slice(len(ODD), cols - len(ODD))
     u = {k: (v[..., rest].contiguous() if k in ("w", "bias", "dy") else v) for k, v in t.items()}
     L._check_forward(u, y[:, rest], kept[:, rest], act)
+
+
+@pytest.mark.parametrize("dtype,out", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("act", L.ACTS[1:])
+def test_slope_far_from_zero(act, dtype, out):
+    """dbias of a single row is dy times the slope: 0 or 1 however large the pre-activation is."""
+    far = [s * v for v in (100.0, 1e4, 1e10, 1e19, 2e19, 1e25, 1e30, 3e38) for s in (1, -1)]
+    cols = len(far)
+    t = L._make(1, 64, cols, dtype, out)
+    t["pre"] = torch.tensor([far], device="cuda").to(out)
+    gx, gw, gb = L._backward(t, act)
+    want = t["dy"].double()[0] * slope(t["pre"].double(), act)[0]
+    assert torch.isfinite(want).all()
+    assert ((gb.double() - want).abs() <= 8 * L.U32 * t["dy"].double()[0].abs()).all(), gb
+    assert torch.isfinite(gx).all() and torch.isfinite(gw).all()
