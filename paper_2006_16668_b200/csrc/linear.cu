@@ -131,7 +131,10 @@ __global__ void __launch_bounds__(256) linear_dpre_kernel(const TY* __restrict__
             if (PLANES == 2) {
               float hi[8], lo[8];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) { hi[j] = __bfloat162float(__float2bfloat16_rn(d[j])); lo[j] = d[j] - hi[j]; }
+              for (int j = 0; j < 8; ++j) {
+                hi[j] = __bfloat162float(__float2bfloat16_rn(d[j]));
+                lo[j] = fabsf(hi[j]) == INFINITY ? 0.f : d[j] - hi[j];     // an infinity is all in the first plane
+              }
               store_pack<__nv_bfloat16, 8>(dpre + off, hi);
               store_pack<__nv_bfloat16, 8>(dpre + n * cols + off, lo);
             } else if (PLANES == 3) {

@@ -56,3 +56,28 @@ def test_slope_far_from_zero(act, dtype, out):
     assert torch.isfinite(want).all()
     assert ((gb.double() - want).abs() <= 8 * L.U32 * t["dy"].double()[0].abs()).all(), gb
     assert torch.isfinite(gx).all() and torch.isfinite(gw).all()
+
+
+@pytest.mark.parametrize("n,K,cols", [(5, 64, 64), (300, 264, 520), (2100, 1024, 1032)])
+@pytest.mark.parametrize("act", L.ACTS)
+@pytest.mark.parametrize("out", [BF, F32])
+def test_infinite_gradient(out, act, n, K, cols):
+    """An infinite dy reaches its row of dx, its column of dw and its dbias as an infinity, in products of every size."""
+    t = L._make(n, K, cols, BF, out)
+    t["pre"][2, 3] = 1.0
+    t["dy"][2, 3], t["dy"][4, 5] = math.inf, -math.inf
+    t["pre"][4, 5] = 2.0
+    t["w"][:, 3] = torch.where(t["w"][:, 3].abs() < 1e-3, torch.full_like(t["w"][:, 3], 0.5), t["w"][:, 3])
+    t["w"][:, 5] = t["w"][:, 3]
+    t["x"][2] = torch.where(t["x"][2].abs() < 1e-3, torch.full_like(t["x"][2], 0.5), t["x"][2])
+    t["x"][4] = t["x"][2]
+    gx, gw, gb = L._backward(t, act)
+    inf = torch.full((), math.inf, device="cuda")
+    assert torch.equal(gx[2].float(), torch.sign(t["w"][:, 3].float()) * inf)
+    assert torch.equal(gx[4].float(), -torch.sign(t["w"][:, 5].float()) * inf)
+    assert torch.equal(gw[:, 3].float(), torch.sign(t["x"][2].float()) * inf)
+    assert torch.equal(gw[:, 5].float(), -torch.sign(t["x"][4].float()) * inf)
+    assert gb[3] == math.inf and gb[5] == -math.inf
+    keep_rows = [i for i in range(n) if i not in (2, 4)]
+    keep_cols = [i for i in range(cols) if i not in (3, 5)]
+    assert torch.isfinite(gx[keep_rows]).all() and torch.isfinite(gw[:, keep_cols]).all() and torch.isfinite(gb[keep_cols]).all()
