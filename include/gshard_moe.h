@@ -505,8 +505,8 @@ int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype
 
 /* Backward of the linear operator: dpre = dy activation'(pre), dx = dpre . w^T, dw = x^T . dpre (dtype),
  * dbias = sum over rows of dpre (float); the residual's gradient is dy itself.  dy and pre: out_dtype; pre
- * is not read with GSHARD_ACT_NONE.  dx, dw, dbias: overwritten, each may be NULL; dx and dw may not
- * overlap an operand.  With dtype bf16 dpre is rounded to bf16 once, as an operand of both products (small
+ * is not read with GSHARD_ACT_NONE.  dx, dw, dbias: overwritten, each may be NULL; they may not
+ * overlap one another or an operand.  With dtype bf16 dpre is rounded to bf16 once, as an operand of both products (small
  * products take it to 16 bits).
  * n_rows == 0 gives zero weight gradients. */
 int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype,

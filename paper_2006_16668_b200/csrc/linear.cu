@@ -385,6 +385,8 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
   const size_t es = dtype == GSHARD_BF16 ? 2 : 4;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   GS_CHECK_OPTIONAL_PTR(dx); GS_CHECK_OPTIONAL_PTR(dw); GS_CHECK_OPTIONAL_PTR(dbias);
+  // two gradients in one place (n_rows == K, K == cols or a single row make their sizes agree)
+  if ((dx && dx == dw) || (dbias && (dbias == dx || dbias == dw))) return GSHARD_ERR_INVALID_ARG;
   if (n_rows == 0) {                              // no rows: the weight gradients are empty sums
     if (!dw && !dbias) return GSHARD_OK;
     GS_CHECK(check_device());
