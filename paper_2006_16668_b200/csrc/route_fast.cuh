@@ -458,10 +458,13 @@ route_fwd_fast_kernel(const __grid_constant__ RouteArgs a, float* __restrict__ s
       }
       bool keep = better < a.kept;
       if (BIASED) {
-        const float worst_kept = -seg_max<LPR>(keep ? -mine : -INFINITY);
-        const float best_left = seg_max<LPR>(keep ? -INFINITY : mine);
-        const bool near = best_left != -INFINITY &&
-                          worst_kept - best_left <= 4.f * slack + 0x1p-20f * fmaxf(fabsf(worst_kept), fabsf(best_left));
+        // What this group's value may be off by: its entries' scores, and half a step of each entry and of their sum, which
+        // may be far smaller than either (a score plus a large bias and a score minus it).
+        const float second = a.group_top == 2 && top2 != -INFINITY ? top2 : 0.f;
+        const float off = 2.f * slack + 0x1p-21f * fmaxf(top1 == -INFINITY ? 0.f : fabsf(top1), fabsf(second));
+        const float worst_kept = -seg_max<LPR>(keep ? off - mine : -INFINITY);
+        const float best_left = seg_max<LPR>(keep ? -INFINITY : mine + off);
+        const bool near = best_left != -INFINITY && worst_kept <= best_left;
         if (__any_sync(kAll, near)) {
           // the groups' values again in 64 bits, from the few entries that can be among a group's best
           if (!a.sigmoid && norm64 == 0.0) norm64 = softmax_norm64<LPR, V>(row, lin, mx);

@@ -101,3 +101,31 @@ def test_sigmoid_gradient_at_given_logits(E):
     assert (got[..., :2] == 0).all()
     err = (got - want).abs()[..., 2:]
     assert (err <= (24 + l[..., 2:].abs()) * 4 * R.U32 * want[..., 2:] + 1e-37).all(), float((err / want[..., 2:]).max())
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,groups,S", [(32, 8, 500), (64, 8, 2500), (96, 3, 90)])
+@pytest.mark.parametrize("size", [1e3, 1e6])
+def test_groups_whose_best_values_cancel(size, E, groups, S, score):
+    """Each group's two best are a score plus a large bias and a score minus it: the sum is small, its error in fp32 is
+    that of the large values."""
+    logits = R._logits(1, S, E, F32, seed=11)
+    bias = torch.full((groups, E // groups), -4 * size, device="cuda")
+    bias[:, 1], bias[:, 2] = size, -size
+    kw = dict(score=score, groups=groups, groups_kept=max(1, groups // 3), group_top=2)
+    cfg = B.make_route(G=1, S=S, E=E, k=2, **kw)
+    bias = bias.reshape(E).contiguous()
+    R._check_forward(cfg, kw, logits, bias, R._route(cfg, logits, bias))
+
+
+def test_group_with_one_expert_left():
+    """The lowest float as a bias for experts that are switched off, all but one of some groups."""
+    E, groups, S = 64, 8, 600
+    for score in ("softmax", "sigmoid"):
+        logits = R._logits(1, S, E, F32, seed=12)
+        bias = torch.zeros(groups, E // groups, device="cuda")
+        bias[2, 1:] = torch.finfo(torch.float32).min
+        bias[5] = torch.finfo(torch.float32).min
+        kw = dict(score=score, groups=groups, groups_kept=3, group_top=2)
+        cfg = B.make_route(G=1, S=S, E=E, k=6, **kw)
+        R._check_forward(cfg, kw, logits, bias.reshape(E), R._route(cfg, logits, bias.reshape(E)))
