@@ -452,6 +452,12 @@ def _arg(t, name, shape, dtype, device):
     return t.data_ptr()
 
 
+def _distinct(a, b, names):
+    """Two outputs of one call, as pointers, may not be one (None and empty tensors are no clash)."""
+    if a and a == b:
+        raise ValueError(f"{names}: two outputs in one place")
+
+
 def _workspace(ws, device):
     if ws is None:
         return None, 0
@@ -492,6 +498,7 @@ def gshard_layer_norm_forward(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5,
     n, M = x.shape
     args = [_arg(x, "x", (n, M), x.dtype, dev), _arg(gamma, "gamma", (M,), f32, dev), _arg(beta, "beta", (M,), f32, dev),
             _arg(y, "y", (n, M), x.dtype, dev), _arg(mean, "mean", (n,), f32, dev), _arg(rstd, "rstd", (n,), f32, dev)]
+    _distinct(args[4], args[5], "mean and rstd")
     _call("gshard_layer_norm_forward", dev, stream, n, M, code, float(eps), *args)
 
 
@@ -504,6 +511,7 @@ def gshard_layer_norm_backward(x, gamma, mean, rstd, dy, dx, dgamma=None, dbeta=
             _arg(rstd, "rstd", (n,), f32, dev), _arg(dy, "dy", (n, M), x.dtype, dev),
             _arg(dskip, "dskip", (n, M), x.dtype, dev), _arg(dx, "dx", (n, M), x.dtype, dev),
             _arg(dgamma, "dgamma", (M,), f32, dev), _arg(dbeta, "dbeta", (M,), f32, dev), *_workspace(workspace, dev)]
+    _distinct(args[7], args[8], "dgamma and dbeta")
     _call("gshard_layer_norm_backward", dev, stream, n, M, code, *args)
 
 

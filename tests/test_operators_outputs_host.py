@@ -27,3 +27,11 @@ def test_linear_backward_refuses_one_address_for_two_gradients(dtype):
     if not torch.cuda.is_available():                        # absent gradients are no clash
         for kw in ({}, dict(dx=None, dw=None), dict(dw=None, db=None), dict(dx=None, db=None), dict(dx=None, dw=None, db=None)):
             assert _linear_backward(dtype=dtype, **kw) in (B.GSHARD_ERR_CUDA, B.GSHARD_ERR_ARCH), kw
+
+
+def test_layer_norm_refuses_one_tensor_for_two_outputs():
+    x, g, s, y = torch.zeros(4, 64), torch.zeros(64), torch.zeros(4), torch.zeros(4, 64)
+    with pytest.raises(ValueError, match="mean and rstd"):
+        B.gshard_layer_norm_forward(x, g, None, y, s, s)
+    with pytest.raises(ValueError, match="dgamma and dbeta"):
+        B.gshard_layer_norm_backward(x, g, s, torch.ones(4), y, torch.zeros(4, 64), g, g)
