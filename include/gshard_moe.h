@@ -457,8 +457,8 @@ int gshard_dense_ffn_forward(int64_t n_tokens, int32_t M, int32_t H, int32_t dty
  * dimension of x [n_rows, M]:
  *   mean = sum x / M, rstd = 1 / sqrt(sum (x - mean)^2 / M + eps), y = gamma (x - mean) rstd + beta
  * x, y: dtype; gamma, beta [M], mean, rstd [n_rows]: float.  beta, mean and rstd may be NULL (no shift;
- * statistics not kept).  y may be x itself; mean and rstd may not share memory.  M <= 16384, any M >= 1 (rows that are whole 16-byte words
- * move fastest); n_rows may be 0.  No workspace. */
+ * statistics not kept).  y may be x itself; mean and rstd may not share memory.  M <= 16384, any M >= 1
+ * (rows that are whole 16-byte words move fastest); n_rows may be 0.  No workspace. */
 int gshard_layer_norm_forward(int64_t n_rows, int32_t M, int32_t dtype, float eps, const void* x,
                               const float* gamma, const float* beta, void* y, float* mean, float* rstd,
                               void* cuda_stream);
@@ -467,7 +467,8 @@ int gshard_layer_norm_forward(int64_t n_rows, int32_t M, int32_t dtype, float ep
  *   dx = rstd (g - sum g / M - z sum (g z) / M) + dskip  with z = (x - mean) rstd, g = gamma dy;
  *   dgamma = sum over rows of dy z, dbeta = sum over rows of dy: float [M], overwritten, either may be
  *   NULL.  dskip [n_rows, M] (dtype, may be NULL): the gradient that reaches x past the layer norm, along
- *   a residual connection.  dx may be dy or dskip itself; dgamma and dbeta may not share memory.  n_rows == 0 gives zero weight gradients.
+ *   a residual connection.  dx may be dy or dskip itself; dgamma and dbeta may not share memory.
+ *   n_rows == 0 gives zero weight gradients.
  *   workspace: gshard_layer_norm_workspace_bytes() bytes, 256-byte aligned; needed only with dgamma or
  *   dbeta.  Its contents are scratch, so calls that share one must be ordered on one stream. */
 size_t gshard_layer_norm_workspace_bytes(int64_t n_rows, int32_t M);

@@ -441,6 +441,13 @@ def _activation(activation):
     return code
 
 
+def _size32(**sizes):
+    """Sizes that the library takes as 32-bit integers; ctypes would cut larger ones off without a word."""
+    for name, v in sizes.items():
+        if not -(1 << 31) <= v < 1 << 31:
+            raise ValueError(f"{name}: {v} is not below 2**31")
+
+
 def _arg(t, name, shape, dtype, device):
     """Pointer of a tensor argument after checking it (None stays None); device: index of the call's GPU."""
     if t is None:
@@ -489,6 +496,7 @@ def _stream_of(device, stream):
 
 
 def gshard_layer_norm_workspace_bytes(n_rows, M) -> int:
+    _size32(M=M)
     return int(load().gshard_layer_norm_workspace_bytes(int(n_rows), int(M)))
 
 
@@ -498,6 +506,8 @@ def gshard_layer_norm_forward(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5,
     n, M = x.shape
     args = [_arg(x, "x", (n, M), x.dtype, dev), _arg(gamma, "gamma", (M,), f32, dev), _arg(beta, "beta", (M,), f32, dev),
             _arg(y, "y", (n, M), x.dtype, dev), _arg(mean, "mean", (n,), f32, dev), _arg(rstd, "rstd", (n,), f32, dev)]
+    if M >> 31:
+        _size32(M=M)
     _distinct(args[4], args[5], "mean and rstd")
     _call("gshard_layer_norm_forward", dev, stream, n, M, code, float(eps), *args)
 
@@ -511,6 +521,8 @@ def gshard_layer_norm_backward(x, gamma, mean, rstd, dy, dx, dgamma=None, dbeta=
             _arg(rstd, "rstd", (n,), f32, dev), _arg(dy, "dy", (n, M), x.dtype, dev),
             _arg(dskip, "dskip", (n, M), x.dtype, dev), _arg(dx, "dx", (n, M), x.dtype, dev),
             _arg(dgamma, "dgamma", (M,), f32, dev), _arg(dbeta, "dbeta", (M,), f32, dev), *_workspace(workspace, dev)]
+    if M >> 31:
+        _size32(M=M)
     _distinct(args[7], args[8], "dgamma and dbeta")
     _call("gshard_layer_norm_backward", dev, stream, n, M, code, *args)
 
@@ -519,6 +531,7 @@ def gshard_linear_workspace_bytes(n_rows, K, cols, dtype, out_dtype=None, for_ba
     """dtype, out_dtype: torch.float32 or torch.bfloat16 (out_dtype: that of y, dtype where not given)."""
     code = _code_of(dtype, "dtype")
     out = code if out_dtype is None else _code_of(out_dtype, "out_dtype")
+    _size32(K=K, cols=cols)
     return int(load().gshard_linear_workspace_bytes(int(n_rows), int(K), int(cols), code, out, int(bool(for_backward))))
 
 
@@ -529,6 +542,8 @@ def gshard_linear_forward(x, w, y, bias=None, residual=None, pre=None, activatio
     args = [_arg(x, "x", (n, K), x.dtype, dev), _arg(w, "w", (K, cols), x.dtype, dev),
             _arg(bias, "bias", (cols,), torch.float32, dev), _arg(residual, "residual", (n, cols), y.dtype, dev),
             _arg(y, "y", (n, cols), y.dtype, dev), _arg(pre, "pre", (n, cols), y.dtype, dev), *_workspace(workspace, dev)]
+    if (K | cols) >> 31:
+        _size32(K=K, cols=cols)
     _call("gshard_linear_forward", dev, stream, n, K, cols, code, out, _activation(activation), *args)
 
 
@@ -541,14 +556,18 @@ def gshard_linear_backward(x, w, dy, dx=None, dw=None, dbias=None, pre=None, act
             _arg(pre, "pre", (n, cols), dy.dtype, dev), _arg(dy, "dy", (n, cols), dy.dtype, dev),
             _arg(dx, "dx", (n, K), x.dtype, dev), _arg(dw, "dw", (K, cols), x.dtype, dev),
             _arg(dbias, "dbias", (cols,), torch.float32, dev), *_workspace(workspace, dev)]
+    if (K | cols) >> 31:
+        _size32(K=K, cols=cols)
     _call("gshard_linear_backward", dev, stream, n, K, cols, code, out, _activation(activation), *args)
 
 
 def make_route(*, G, S, E, k, dtype="f32", score="softmax", groups=1, groups_kept=None, group_top=1, renormalise=True,
                scale=1.0) -> gshard_route_config:
     """Routing description; dtype is "f32" | "bf16", score "softmax" | "sigmoid"; groups_kept: all by default."""
+    groups_kept = groups if groups_kept is None else groups_kept
+    _size32(G=G, S=S, E=E, k=k, groups=groups, groups_kept=groups_kept, group_top=group_top)
     return gshard_route_config(G, S, E, k, {"f32": GSHARD_F32, "bf16": GSHARD_BF16}[dtype], _SCORES[score], groups,
-                               groups if groups_kept is None else groups_kept, group_top, int(bool(renormalise)),
+                               groups_kept, group_top, int(bool(renormalise)),
                                float(scale))
 
 

@@ -1,4 +1,4 @@
-"""Outputs that share memory are refused: no GPU needed."""
+"""Outputs that share memory, and sizes that the library's 32-bit arguments cannot hold, are refused: no GPU needed."""
 import pytest
 import torch
 
@@ -35,3 +35,25 @@ def test_layer_norm_refuses_one_tensor_for_two_outputs():
         B.gshard_layer_norm_forward(x, g, None, y, s, s)
     with pytest.raises(ValueError, match="dgamma and dbeta"):
         B.gshard_layer_norm_backward(x, g, s, torch.ones(4), y, torch.zeros(4, 64), g, g)
+
+
+def test_sizes_beyond_31_bits_are_refused():
+    """A size of 2^32 + 1024 must not be taken for 1024."""
+    big = (1 << 32) + 1024
+    bf, f32 = torch.bfloat16, torch.float32
+    e = lambda *s, dtype=bf: torch.empty(*s, dtype=dtype, device="meta")
+    with pytest.raises(ValueError, match="2\\*\\*31"):
+        B.gshard_layer_norm_forward(e(1, big), e(big, dtype=f32), None, e(1, big))
+    with pytest.raises(ValueError, match="2\\*\\*31"):
+        B.gshard_layer_norm_backward(e(1, big), e(big, dtype=f32), e(1, dtype=f32), e(1, dtype=f32), e(1, big), e(1, big))
+    with pytest.raises(ValueError, match="2\\*\\*31"):
+        B.gshard_linear_forward(e(1, big), e(big, 8), e(1, 8))
+    with pytest.raises(ValueError, match="2\\*\\*31"):
+        B.gshard_linear_forward(e(1, 8), e(8, big), e(1, big))
+    with pytest.raises(ValueError, match="2\\*\\*31"):
+        B.gshard_linear_backward(e(1, big), e(big, 8), e(1, 8), e(1, big))
+    for call in (lambda: B.gshard_layer_norm_workspace_bytes(4, big), lambda: B.gshard_linear_workspace_bytes(4, big, 64, bf),
+                 lambda: B.gshard_linear_workspace_bytes(4, 64, big, bf), lambda: B.make_route(G=1, S=big, E=8, k=2),
+                 lambda: B.make_route(G=1, S=8, E=8, k=(1 << 32) + 2)):
+        with pytest.raises(ValueError, match="2\\*\\*31"):
+            call()
