@@ -26,7 +26,7 @@
  *     fp32 on CUDA cores.  dtype GSHARD_BF16: they are bfloat16; contractions run on the
  *     tcgen05 tensor cores with fp32 accumulation; softmax, top-2, weights, l_aux are fp32.
  *     u, l_aux, weight, m, dwg are always float.
- *   - Outputs are bit-reproducible from run to run (no atomics in any reduction).
+ *   - Outputs are bit-reproducible from run to run (no atomics in any floating-point reduction).
  *   - Every stage's launches sit inside an NVTX range (gshard.gate, .capacity, .dispatch,
  *     .expert_ffn, .combine, .backward.*, .layer_norm, .linear, .route), visible to a profiler that injects NVTX.
  */
@@ -485,7 +485,8 @@ int gshard_layer_norm_backward(int64_t n_rows, int32_t M, int32_t dtype, const v
  * the pre-activations that the backward takes.  residual may be y itself; no other output may
  * overlap an operand.  K % 8 == 0 and cols % 8 == 0; n_rows may be 0.
  * bf16: tensor cores, fp32 accumulation, one rounding per output.  fp32: as close to the exact result as an fp32
- * product (three bf16 planes per operand on the tensor cores); an infinite operand may come out as NaN.
+ * product (three bf16 planes per operand on the tensor cores), where entries below 2^-110 (8e-34) may count to a
+ * multiple of 2^-133 only; an infinite operand may come out as NaN.
  * n_rows == 0 launches nothing and leaves the workspace alone.
  * workspace: gshard_linear_workspace_bytes() bytes, 256-byte aligned; its first word is the status word
  * (gshard_moe_last_device_status).  Calls that share a workspace must be ordered on one stream. */

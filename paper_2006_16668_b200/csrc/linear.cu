@@ -14,7 +14,8 @@
 // kernel adds in order.  Measured: 65536 x 8192 -> 1024 with residual 733 to 800 us
 // (1.37 to 1.5 PFLOP/s, tensor pipe 88 % active); backward of 30011 x 1024 -> 8192 with gelu 926 us: dpre 245 (HBM),
 // dx 336, dw 346.
-// fp32: an fp32 value is the exact sum of three bf16 values (8 bits of its 24 each), so x . w is six bf16 products
+// fp32: an fp32 value is the exact sum of three bf16 values (8 bits of its 24 each; from 2^-110 on, below it what bf16's
+// smallest step 2^-133 leaves), so x . w is six bf16 products
 // of such planes on the same GEMMs, accumulated in fp32, smallest first; the three products left out lie below 2^-24.
 // That is six times the tensor work and three times the operand bytes, and still several times faster than fp32 FMA
 // on the CUDA cores (4100 x 1024 x 4096: 170 us against 1172 there).  Infinities and NaN in x, w or dy give NaN.
@@ -52,7 +53,7 @@ __global__ void __launch_bounds__(256) linear_finish_kernel(const float4* __rest
 }
 
 // The three bf16 planes of fp32 values: hi takes the top 8 bits of the significand, mid the next 8, lo the last 8,
-// each by truncation, so that hi + mid + lo is the value exactly and nothing overflows.
+// each by truncation, so that hi + mid + lo is the value exactly (below 2^-110 to half a step of 2^-133) and nothing overflows.
 __device__ __forceinline__ void split3(const float* f, float* hi, float* mid, float* lo, int n) {
 #pragma unroll
   for (int j = 0; j < n; ++j) {

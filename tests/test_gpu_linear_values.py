@@ -81,3 +81,38 @@ def test_infinite_gradient(out, act, n, K, cols):
     keep_rows = [i for i in range(n) if i not in (2, 4)]
     keep_cols = [i for i in range(cols) if i not in (3, 5)]
     assert torch.isfinite(gx[keep_rows]).all() and torch.isfinite(gw[:, keep_cols]).all() and torch.isfinite(gb[keep_cols]).all()
+
+
+@pytest.mark.parametrize("dtype,act", [(BF, "gelu"), (F32, "silu")])
+def test_offsets_beyond_32_bits(dtype, act):
+    """More than 2^31 elements in y, pre, dy and the residual: rows and columns at both ends against the formula."""
+    n, K, cols = 65600, 64, 32800
+    t = {"x": torch.empty(n, K, dtype=dtype, device="cuda").normal_(),
+         "w": torch.empty(K, cols, dtype=dtype, device="cuda").normal_(std=K ** -0.5),
+         "bias": torch.randn(cols, device="cuda")}
+    t["dy"], t["residual"] = (torch.empty(n, cols, dtype=dtype, device="cuda").normal_() for _ in range(2))
+    y, kept = L._forward(t, act, residual=True, pre=True)
+    rows = torch.cat([torch.arange(0, 64), torch.arange(n - 200, n)]).cuda()
+    u = {k: (v[rows] if v.shape[0] == n else v) for k, v in t.items()}
+    L._check_forward(u, y[rows], kept[rows], act, residual=True)
+    del y
+    t["pre"] = kept
+    gx, gw, gb = L._backward(t, act)
+    u["pre"] = kept[rows]
+    L._check_backward(u, act, gx[rows], None, None)
+    at = torch.cat([torch.arange(0, 16), torch.arange(cols - 24, cols)]).cuda()
+    v = {k: (t[k][:, at] if k in ("w", "dy", "pre") else t[k]) for k in ("x", "w", "dy", "pre")}
+    L._check_backward(v, act, None, gw[:, at], gb[at])
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-33, 1e-36, 1e-38])
+@pytest.mark.parametrize("n", [4, 64, 3000])
+def test_fp32_operands_near_the_smallest_float(n, scale):
+    """The three bf16 planes of an entry end at 2^-133: below 2^-110 that, and not 24 bits, bounds what is lost of it, half
+    a step of 2^-133."""
+    t = L._make(n, 512, 256, F32)
+    t["x"] *= scale
+    y, _ = L._forward(t, bias=False)
+    x, w = t["x"].double(), t["w"].double()
+    bound = L._steps(t, 512) * (x.abs() @ w.abs()) + 2.0 ** -134 * w.abs().sum(0) + 512 * 2.0 ** -149
+    assert ((y.double() - x @ w).abs() <= bound).all()
