@@ -11,14 +11,14 @@
 // second plane and a second pass, which halves the error of dx and dw to that of their own rounding.
 // A product whose output tiles run at once is one launch (linear_mid.cu); another one (deep contractions) with
 // too few tiles for the multiprocessors is cut along the contraction into runs whose fp32 partial products a second
-// kernel adds in order.  Measured: 65536 x 8192 -> 1024 with residual 733 to 800 us
-// (1.37 to 1.5 PFLOP/s, tensor pipe 88 % active); backward of 30011 x 1024 -> 8192 with gelu 926 us: dpre 245 (HBM),
-// dx 336, dw 346.
+// kernel adds in order.  Measured under the power cap, as a program that keeps the GPU busy has it: 65536 x 8192 -> 1024
+// with residual 915 to 1000 us (1.1 to 1.2 PFLOP/s, tensor pipe 88 % active; a short burst 733 to 800); backward of
+// 30011 x 1024 -> 8192 with gelu 1080 to 1110 us (burst 926: dpre 245, bound by HBM, dx 336, dw 346).
 // fp32: an fp32 value is the exact sum of three bf16 values (8 bits of its 24 each; from 2^-110 on, below it what bf16's
-// smallest step 2^-133 leaves), so x . w is six bf16 products
-// of such planes on the same GEMMs, accumulated in fp32, smallest first; the three products left out lie below 2^-24.
+// smallest step 2^-133 leaves), so x . w is six bf16 products of such planes on the same GEMMs, accumulated in fp32,
+// smallest first; the three products left out lie below 2^-24.
 // That is six times the tensor work and three times the operand bytes, and still several times faster than fp32 FMA
-// on the CUDA cores (4100 x 1024 x 4096: 170 us against 1172 there).  Infinities and NaN in x, w or dy give NaN.
+// on the CUDA cores (4100 x 1024 x 4096: 195 to 200 us, 160 to 170 in a burst, against 1172 there).  Infinities and NaN in x, w or dy give NaN.
 // A few rows stream w through the CUDA cores instead (linear_few.cu).
 #include <algorithm>
 

@@ -3,7 +3,7 @@
 //
 // What bounds the pass: the logits are read once, so HBM while few experts are chosen, the arithmetic of
 // the choice with many.  Measured: 131072 tokens, top-2 of 2048 fp32 190 us (5.7 TB/s), with mean gates 264; 65536
-// tokens, sigmoid + bias, 4 of 8 groups, top-8 of 512 bf16 99 us, of which the nine picks 29, the groups 16.  Reductions and
+// tokens, sigmoid + bias, 4 of 8 groups, top-8 of 512 bf16 97 us, of which the nine picks 29, the groups 16.  Reductions and
 // the bookkeeping of a pick cost about the same however many tokens the warp holds, which is why eight
 // lanes per token are taken where the experts fit.
 // Layout: lanes take turns of W consecutive experts, so that loads are whole 16-byte words (W = 1 for rows that are
