@@ -18,7 +18,8 @@
 // smallest step 2^-133 leaves), so x . w is six bf16 products of such planes on the same GEMMs, accumulated in fp32,
 // smallest first; the three products left out lie below 2^-24.
 // That is six times the tensor work and three times the operand bytes, and still several times faster than fp32 FMA
-// on the CUDA cores (4100 x 1024 x 4096: 195 to 200 us, 160 to 170 in a burst, against 1172 there).  Infinities and NaN in x, w or dy give NaN.
+// on the CUDA cores (4100 x 1024 x 4096: 195 to 200 us, 160 to 170 in a burst, against 1172 there).  Infinities and NaN
+// in x, w or dy give NaN.
 // A few rows stream w through the CUDA cores instead (linear_few.cu).
 #include <algorithm>
 
