@@ -8,7 +8,8 @@
  *                 with random routing (keep iff c < C and 2*g2 > rnd)
  *   Algorithm 2   tensor layouts: inputs [G,S,M], wg [M,E], wi [E,M,H], wo [E,H,M],
  *                 dispatched expert inputs [E,G,C,M], outputs [G,S,M]
- * and, further down, the operators of the Transformer around it: layer norm, linear, routing beyond top-2.
+ * and, further down, the operators of the Transformer around it: layer norm, linear, routing beyond top-2, cross
+ * attention, gated linear, gradient norm and clipping.
  *
  * Conventions for every call
  *   - All tensor arguments are DEVICE pointers unless the name ends in _host; tensors are
@@ -28,7 +29,7 @@
  *     u, l_aux, weight, m, dwg are always float.
  *   - Outputs are bit-reproducible from run to run (no atomics in any floating-point reduction).
  *   - Every stage's launches sit inside an NVTX range (gshard.gate, .capacity, .dispatch,
- *     .expert_ffn, .combine, .backward.*, .layer_norm, .linear, .route), visible to a profiler that injects NVTX.
+ *     .expert_ffn, .combine, .backward.*, .layer_norm, .linear, .route, .attention, .gated_linear, .grad_norm, .grad_clip), visible to a profiler that injects NVTX.
  */
 #ifndef GSHARD_MOE_H_
 #define GSHARD_MOE_H_
@@ -561,6 +562,91 @@ int gshard_moe_route(const gshard_route_config* config, const void* logits, cons
 int gshard_moe_route_backward(const gshard_route_config* config, const void* logits,
                               const int32_t* expert_idx, const float* dweight, const float* dm,
                               void* dlogits, void* cuda_stream);
+
+/* ---- cross attention -----------------------------------------------------------------------------
+ * A decoder layer's attention to the states of the encoder, whose sequences have another length (the paper's
+ * model is an encoder-decoder Transformer with 16 heads of 128), without the projections around it:
+ *   s = scale q.k over the keys below the source's length, p = softmax(s), o = p v, lse = log sum exp(s)
+ * q [batch, q_len, heads, head_dim], k, v [batch, k_len, kv_heads, head_dim]: dtype; query heads
+ * h * heads / kv_heads and following share key head h.  q_stride, k_stride, v_stride: elements from one token
+ * to the next, so that q, k, v may be parts of wider rows (one projection's output); a batch element
+ * follows the last token of the one before it.  k_lengths [batch] int32 (NULL: all k_len): keys from there on are
+ * neither used nor read as values, whatever they hold; values are taken into [0, k_len].  A source without keys
+ * gives o = 0 and lse = -inf.
+ *   o [batch, q_len, heads, head_dim] packed, dtype; lse [batch, heads, q_len] float, may be NULL.
+ * bf16: tensor cores, fp32 accumulation and softmax, the weights p rounded to bf16 as an operand of p v.  fp32: all
+ * arithmetic in fp32.
+ * Limits: head_dim a multiple of 8 up to 128, strides multiples of 16 bytes, scale > 0; batch, q_len and
+ * k_len may be 0.  workspace: gshard_cross_attention_workspace_bytes() bytes, 256-byte aligned; its first word
+ * is the status word (gshard_moe_last_device_status).  Calls that share a workspace must be ordered on one stream. */
+typedef struct {
+  int32_t batch, q_len, k_len, heads, kv_heads, head_dim;
+  int32_t dtype;         /* gshard_dtype */
+  float scale;
+  int64_t q_stride, k_stride, v_stride;
+} gshard_attention_config;
+
+size_t gshard_cross_attention_workspace_bytes(const gshard_attention_config* config, int for_backward);
+int gshard_cross_attention_forward(const gshard_attention_config* config, const void* q, const void* k,
+                                   const void* v, const int32_t* k_lengths, void* o, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Backward of the cross attention.  o, lse: as the forward returned them; dout: laid out like o.  With
+ * P = exp(s - lse), delta = sum over d of dout o and dS = scale P (dout.v - delta):
+ *   dq = dS k, dk = dS^T q, dv = P^T dout, the last two summed over the heads that share a key head.
+ * dq, dk, dv: laid out like q, k, v (same strides), overwritten; what lies between their rows is left as it is.  Keys
+ * from the source's length on get zero.  No output may overlap an operand or another output (parts of one wider
+ * row do not).  With bf16 P and dS are rounded to bf16 once, as operands. */
+int gshard_cross_attention_backward(const gshard_attention_config* config, const void* q, const void* k,
+                                    const void* v, const int32_t* k_lengths, const void* o, const float* lse,
+                                    const void* dout, void* dq, void* dk, void* dv, void* workspace,
+                                    size_t workspace_bytes, void* cuda_stream);
+
+/* ---- gated linear -----------------------------------------------------------------------------------
+ * The first half of a gated feed-forward block; the second is gshard_linear_forward.  No bias, as in eq. (2):
+ *   pre = x . w, h = activation(pre[:, :cols]) * pre[:, cols:]
+ * x [n_rows, K], w [K, 2 cols] (the gate's columns, then the other factor's), h [n_rows, cols]: dtype; pre
+ * [n_rows, 2 cols] (dtype, may be NULL) is kept for the backward.  activation: gshard_activation.  No output may
+ * overlap an operand or the other output.  K % 8 == 0 and cols % 8 == 0; n_rows may be 0.  Accuracy, workspace and
+ * status word as for the linear operator; h is rounded once, from fp32 projections. */
+size_t gshard_gated_linear_workspace_bytes(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int for_backward);
+int gshard_gated_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t activation,
+                                const void* x, const void* w, void* h, void* pre, void* workspace,
+                                size_t workspace_bytes, void* cuda_stream);
+
+/* Backward of the gated linear operator: with g and u the two halves of pre,
+ *   dpre = [dh u activation'(g), dh activation(g)], dx = dpre . w^T, dw = x^T . dpre (dtype)
+ * dx, dw: overwritten, each may be NULL; they may not overlap one another or an operand.  Rounding of dpre as in the linear
+ * operator.  n_rows == 0 gives a zero dw. */
+int gshard_gated_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t activation,
+                                 const void* x, const void* w, const void* pre, const void* dh, void* dx,
+                                 void* dw, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ---- gradient norm and clipping ---------------------------------------------------------------------
+ * The norm of all gradients of a training step together, and their scaling down to a bound.  A list names n
+ * tensors by HOST arrays: device pointers (element-aligned; parts of one buffer are fine), element counts (may be
+ * 0) and gshard_dtype.  outs: where the clipped gradients go, grads itself for in place; a pair of tensors whose
+ * addresses agree modulo 16 moves fastest.  The arrays are read during the call only.
+ *   gshard_grad_norm: *sumsq = sum over all tensors of g^2 (double, device memory).
+ *   gshard_grad_clip: norm = sqrt(*sumsq); outs = grads * (norm > max_norm ? max_norm / norm : 1), the factor in fp32,
+ *   products rounded to the tensor's type; *norm (float, device memory, may be NULL).  A norm that is infinite or NaN
+ *   leaves the gradients as they are (outs: copies), so that a caller can look at *norm and skip the step.
+ * Several ranks (the experts' gradients of the expert-parallel form): add the ranks' *sumsq between the two calls.
+ * outs may not overlap grads other than by being the same tensor.
+ * workspace: gshard_grad_norm_workspace_bytes() bytes, 256-byte aligned; scratch. */
+typedef struct {
+  int32_t n;
+  const void* const* grads;
+  void* const* outs;
+  const int64_t* counts;
+  const int32_t* dtypes;
+} gshard_grad_list;
+
+size_t gshard_grad_norm_workspace_bytes(const gshard_grad_list* list);
+int gshard_grad_norm(const gshard_grad_list* list, double* sumsq, void* workspace, size_t workspace_bytes,
+                     void* cuda_stream);
+int gshard_grad_clip(const gshard_grad_list* list, const double* sumsq, float max_norm, float* norm,
+                     void* cuda_stream);
 
 /* The check that GSHARD_FLAG_DEBUG_CHECKS runs inside the forward, callable on its own: verifies
  * the invariants Algorithm 1 implies for routing->expert_idx, slot, weight, flags and slot_token

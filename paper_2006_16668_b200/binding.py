@@ -92,6 +92,16 @@ class gshard_route_config(Structure):
                                        "renormalise")] + [("scale", c_float)]
 
 
+class gshard_attention_config(Structure):
+    _fields_ = [(n, c_int32) for n in ("batch", "q_len", "k_len", "heads", "kv_heads", "head_dim", "dtype")] + \
+               [("scale", c_float)] + [(n, c_int64) for n in ("q_stride", "k_stride", "v_stride")]
+
+
+class gshard_grad_list(Structure):
+    _fields_ = [("n", c_int32), ("grads", POINTER(c_void_p)), ("outs", POINTER(c_void_p)), ("counts", POINTER(c_int64)),
+                ("dtypes", POINTER(c_int32))]
+
+
 EXPORTS = {
     # name: (restype, argtypes)
     "gshard_version": (c_int, []),
@@ -143,6 +153,15 @@ EXPORTS = {
     "gshard_moe_route_workspace_bytes": (c_size_t, [POINTER(gshard_route_config)]),
     "gshard_moe_route": (c_int, [POINTER(gshard_route_config)] + [c_void_p] * 7 + [c_size_t, c_void_p]),
     "gshard_moe_route_backward": (c_int, [POINTER(gshard_route_config)] + [c_void_p] * 6),
+    "gshard_cross_attention_workspace_bytes": (c_size_t, [POINTER(gshard_attention_config), c_int]),
+    "gshard_cross_attention_forward": (c_int, [POINTER(gshard_attention_config)] + [c_void_p] * 7 + [c_size_t, c_void_p]),
+    "gshard_cross_attention_backward": (c_int, [POINTER(gshard_attention_config)] + [c_void_p] * 11 + [c_size_t, c_void_p]),
+    "gshard_gated_linear_workspace_bytes": (c_size_t, [c_int64] + [c_int32] * 3 + [c_int]),
+    "gshard_gated_linear_forward": (c_int, [c_int64] + [c_int32] * 4 + [c_void_p] * 5 + [c_size_t, c_void_p]),
+    "gshard_gated_linear_backward": (c_int, [c_int64] + [c_int32] * 4 + [c_void_p] * 7 + [c_size_t, c_void_p]),
+    "gshard_grad_norm_workspace_bytes": (c_size_t, [POINTER(gshard_grad_list)]),
+    "gshard_grad_norm": (c_int, [POINTER(gshard_grad_list)] + [c_void_p] * 2 + [c_size_t, c_void_p]),
+    "gshard_grad_clip": (c_int, [POINTER(gshard_grad_list), c_void_p, c_float, c_void_p, c_void_p]),
     "gshard_moe_debug_wait_timeout": (c_int, [c_void_p, c_uint32, c_void_p]),
     "gshard_moe_check_routing": (c_int, [POINTER(gshard_moe_shape), POINTER(gshard_moe_routing), c_void_p, c_void_p]),
     "gshard_moe_last_device_status": (c_int, [c_void_p, c_void_p]),
@@ -593,6 +612,140 @@ def gshard_moe_route_backward(route, logits, expert_idx, dweight, dlogits, dm=No
             _arg(dweight, "dweight", (G, S, k), f32, dev), _arg(dm, "dm", (G, E), f32, dev),
             _arg(dlogits, "dlogits", (G, S, E), dt, dev)]
     _call("gshard_moe_route_backward", dev, stream, ctypes.byref(route), *args)
+
+
+# ---- cross attention, gated linear, gradient norm ---------------------------------------------------
+# Checked like the operators above.
+
+def _tokens(t, name, shape, dtype, device):
+    """(pointer, token stride) of a [batch, tokens, heads, head_dim] tensor whose rows of heads are dense and may lie apart."""
+    st = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the device of the first tensor, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    B, T, H, D = shape
+    row = st[1] if T > 1 else (st[0] if B > 1 else H * D)
+    if t.numel() and ((st[3] != 1 and D > 1) or (st[2] != D and H > 1) or (B > 1 and st[0] != T * row)):
+        raise ValueError(f"{name}: strides {st}; heads of a token must be dense, and batch elements follow one another")
+    return t.data_ptr(), row
+
+
+def _attention(q, k, v, scale):
+    code, dev = _code_of(q.dtype, "q"), q.get_device()
+    (B, Tq, H, D), (Tk, Hkv) = q.shape, k.shape[1:3]
+    (pq, sq), (pk, sk), (pv, sv) = (_tokens(q, "q", q.shape, q.dtype, dev), _tokens(k, "k", (B, Tk, Hkv, D), q.dtype, dev),
+                                    _tokens(v, "v", (B, Tk, Hkv, D), q.dtype, dev))
+    if (Tq | Tk | B | H) >> 31:
+        _size32(batch=B, q_len=Tq, k_len=Tk, heads=H)
+    return (gshard_attention_config(B, Tq, Tk, H, Hkv, D, code, D ** -0.5 if scale is None else scale, sq, sk, sv), dev,
+            (pq, pk, pv))
+
+
+def gshard_cross_attention_workspace_bytes(batch, q_len, k_len, heads, kv_heads, head_dim, dtype, for_backward=False) -> int:
+    """dtype: torch.float32 or torch.bfloat16."""
+    _size32(batch=batch, q_len=q_len, k_len=k_len, heads=heads, kv_heads=kv_heads, head_dim=head_dim)
+    c = gshard_attention_config(batch, q_len, k_len, heads, kv_heads, head_dim, _code_of(dtype, "dtype"), 1.0,
+                                heads * head_dim, kv_heads * head_dim, kv_heads * head_dim)
+    return int(load().gshard_cross_attention_workspace_bytes(ctypes.byref(c), int(bool(for_backward))))
+
+
+def gshard_cross_attention_forward(q, k, v, o, lse=None, k_lengths=None, scale=None, workspace=None, stream=None):
+    """o = softmax(scale q k^T) v for q [B, Tq, H, D], k, v [B, Tk, Hkv, D] (tokens may lie apart, as parts of one projection's
+    output); k_lengths [B] int32: keys of each source; scale: 1 / sqrt(D) where not given; lse [B, H, Tq] for the backward."""
+    cfg, dev, (pq, pk, pv) = _attention(q, k, v, scale)
+    B, Tq, H, D = q.shape
+    args = [pq, pk, pv, _arg(k_lengths, "k_lengths", (B,), torch.int32, dev), _arg(o, "o", (B, Tq, H, D), q.dtype, dev),
+            _arg(lse, "lse", (B, H, Tq), torch.float32, dev), *_workspace(workspace, dev)]
+    _call("gshard_cross_attention_forward", dev, stream, ctypes.byref(cfg), *args)
+
+
+def gshard_cross_attention_backward(q, k, v, o, lse, dout, dq, dk, dv, k_lengths=None, scale=None, workspace=None, stream=None):
+    """dq, dk, dv (laid out like q, k, v) of the cross attention; o, lse as the forward returned them, with the same scale."""
+    cfg, dev, (pq, pk, pv) = _attention(q, k, v, scale)
+    B, Tq, H, D = q.shape
+    grads = []
+    for t, name, like, stride in ((dq, "dq", q, cfg.q_stride), (dk, "dk", k, cfg.k_stride), (dv, "dv", v, cfg.v_stride)):
+        p, s = _tokens(t, name, like.shape, q.dtype, dev)
+        if s != stride and t.numel():
+            raise ValueError(f"{name}: tokens lie {s} elements apart, those of {name[1:]} {stride}")
+        grads.append(p)
+    args = [pq, pk, pv, _arg(k_lengths, "k_lengths", (B,), torch.int32, dev), _arg(o, "o", (B, Tq, H, D), q.dtype, dev),
+            _arg(lse, "lse", (B, H, Tq), torch.float32, dev), _arg(dout, "dout", (B, Tq, H, D), q.dtype, dev), *grads,
+            *_workspace(workspace, dev)]
+    _call("gshard_cross_attention_backward", dev, stream, ctypes.byref(cfg), *args)
+
+
+def gshard_gated_linear_workspace_bytes(n_rows, K, cols, dtype, for_backward=False) -> int:
+    """dtype: torch.float32 or torch.bfloat16."""
+    _size32(K=K, cols=cols)
+    return int(load().gshard_gated_linear_workspace_bytes(int(n_rows), int(K), int(cols), _code_of(dtype, "dtype"),
+                                                          int(bool(for_backward))))
+
+
+def gshard_gated_linear_forward(x, w, h, pre=None, activation="silu", workspace=None, stream=None):
+    """h = activation(x . w[:, :cols]) * (x . w[:, cols:]) for x [n, K], w [K, 2 cols]; pre [n, 2 cols] receives x . w."""
+    code, dev = _code_of(x.dtype, "x"), x.get_device()
+    (n, K), cols = x.shape, h.shape[-1]
+    args = [_arg(x, "x", (n, K), x.dtype, dev), _arg(w, "w", (K, 2 * cols), x.dtype, dev), _arg(h, "h", (n, cols), x.dtype, dev),
+            _arg(pre, "pre", (n, 2 * cols), x.dtype, dev), *_workspace(workspace, dev)]
+    if (K | 2 * cols) >> 31:
+        _size32(K=K, cols=2 * cols)
+    _call("gshard_gated_linear_forward", dev, stream, n, K, cols, code, _activation(activation), *args)
+
+
+def gshard_gated_linear_backward(x, w, pre, dh, dx=None, dw=None, activation="silu", workspace=None, stream=None):
+    """dx, dw (each optional) of the gated linear operator; pre as the forward kept it."""
+    code, dev = _code_of(x.dtype, "x"), x.get_device()
+    (n, K), cols = x.shape, dh.shape[-1]
+    args = [_arg(x, "x", (n, K), x.dtype, dev), _arg(w, "w", (K, 2 * cols), x.dtype, dev),
+            _arg(pre, "pre", (n, 2 * cols), x.dtype, dev), _arg(dh, "dh", (n, cols), x.dtype, dev),
+            _arg(dx, "dx", (n, K), x.dtype, dev), _arg(dw, "dw", (K, 2 * cols), x.dtype, dev), *_workspace(workspace, dev)]
+    if (K | 2 * cols) >> 31:
+        _size32(K=K, cols=2 * cols)
+    _call("gshard_gated_linear_backward", dev, stream, n, K, cols, code, _activation(activation), *args)
+
+
+class GradList:
+    """Gradients of one training program, and where their clipped values go: the arrays of addresses, counts and types that
+    the library reads on every call.  It holds the tensors, whose storage must stay where it is."""
+
+    def __init__(self, grads, outs):
+        if len(grads) != len(outs):
+            raise ValueError(f"outs: {len(outs)} tensors for {len(grads)} gradients")
+        self.tensors, self.device = (list(grads), list(outs)), grads[0].get_device() if grads else torch.cuda.current_device()
+        n, codes = len(grads), []
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            codes.append(_code_of(g.dtype, f"grads[{i}]"))
+            _arg(g, f"grads[{i}]", g.shape, g.dtype, self.device)
+            _arg(o, f"outs[{i}]", g.shape, g.dtype, self.device)
+        self._arrays = ((c_void_p * n)(*[g.data_ptr() for g in grads]), (c_void_p * n)(*[o.data_ptr() for o in outs]),
+                        (c_int64 * n)(*[g.numel() for g in grads]), (c_int32 * n)(*codes))
+        self.struct = gshard_grad_list(n, *[ctypes.cast(a, t) for a, t in zip(
+            self._arrays, (POINTER(c_void_p), POINTER(c_void_p), POINTER(c_int64), POINTER(c_int32)))])
+
+
+def make_grad_list(grads, outs=None) -> GradList:
+    """List of contiguous gradient tensors (float32 or bfloat16) of one GPU; outs: like grads, by default grads themselves (in place)."""
+    grads = list(grads)
+    return GradList(grads, grads if outs is None else list(outs))
+
+
+def gshard_grad_norm_workspace_bytes(grads) -> int:
+    return int(load().gshard_grad_norm_workspace_bytes(ctypes.byref(grads.struct)))
+
+
+def gshard_grad_norm(grads, sumsq, workspace=None, stream=None):
+    """sumsq [1] (float64): the sum of squares of all gradients of a list."""
+    dev = grads.device
+    _call("gshard_grad_norm", dev, stream, ctypes.byref(grads.struct), _arg(sumsq, "sumsq", (1,), torch.float64, dev),
+          *_workspace(workspace, dev))
+
+
+def gshard_grad_clip(grads, sumsq, max_norm, norm=None, stream=None):
+    """Scales the list's gradients by max_norm / sqrt(sumsq) where that is below 1; norm [1] (float32) receives sqrt(sumsq)."""
+    dev = grads.device
+    _call("gshard_grad_clip", dev, stream, ctypes.byref(grads.struct), _arg(sumsq, "sumsq", (1,), torch.float64, dev),
+          float(max_norm), _arg(norm, "norm", (1,), torch.float32, dev))
 
 
 def gshard_moe_debug_wait_timeout(workspace, limit_us=200, stream=None):

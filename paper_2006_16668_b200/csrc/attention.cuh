@@ -1,0 +1,33 @@
+// Shared by the cross-attention kernels.
+//
+//   s = scale q.k over the keys below the source's length, p = softmax(s), o = p v, lse = log sum exp(s)
+//   backward, with o and lse as the forward kept them: P = exp(s - lse), delta = sum over d of dout o,
+//   dS = scale P (dout v^T - delta), dq = dS k, dk = dS^T q, dv = P^T dout; heads that share a key head add up.
+#pragma once
+#include "common.cuh"
+
+namespace gshard {
+
+struct AttentionArgs {
+  const void* q; const void* k; const void* v;       // [B, Tq, H, D], [B, Tk, Hkv, D]: tokens at the strides below
+  const int32_t* lengths;                            // [B] keys of each source, or nullptr: Tk
+  void* o; float* lse;                               // [B, Tq, H, D] packed, [B, H, Tq]; lse may be nullptr in the forward
+  const void* dout; const float* delta;              // like o, like lse
+  void* dq; void* dk; void* dv;                      // laid out like q, k, v
+  int B, Tq, Tk, H, Hkv, D;
+  float scale;
+  long long q_stride, k_stride, v_stride;            // elements from one token to the next; batches are dense
+  int* status;
+};
+
+__device__ __forceinline__ int source_length(const AttentionArgs& a, int b) {
+  return a.lengths ? min(max(__ldg(a.lengths + b), 0), a.Tk) : a.Tk;
+}
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// attention_simt.cu: CUDA cores
+int launch_attention_simt_forward(const AttentionArgs& a, bool bf16, cudaStream_t st);
+int launch_attention_simt_backward(const AttentionArgs& a, bool bf16, cudaStream_t st);
+
+}  // namespace gshard

@@ -1,0 +1,329 @@
+// Cross attention on the CUDA cores (fp32), forward and backward: tiles of 64 queries by 64 keys, one pass over the
+// keys with the running maximum and sum of the softmax, fp32 throughout.
+//
+// 256 threads as 16 x 16; a thread owns rows ty + 16 i and columns tx + 16 j of a score tile, or four neighbouring
+// columns of an output tile.  All tiles lie in shared memory row by row with a pitch of D + 4 floats, so that the 16-byte
+// reads of eight neighbouring rows fall into different banks; products take two fp32 values per instruction, along the
+// head dimension for the scores and along the columns for the outputs.
+// The backward runs over the scores twice, once per block of keys (dk, dv) and once per block of queries (dq): seven
+// products instead of five, but every gradient is summed by one block in a fixed order, without atomics.
+#include "attention.cuh"
+#include "pack.cuh"
+
+namespace gshard {
+
+namespace {
+
+constexpr int BT = 64;                  // rows of a tile
+constexpr int PP = BT + 4;              // pitch of a score tile
+constexpr int kThreads = 256;
+
+template <int DP> constexpr int kPitch = DP + 4;
+
+// 64 rows from `src` (pitch `stride` elements) as floats; rows from `rows` on and columns from D on are zero
+template <typename T, int DP>
+__device__ __forceinline__ void load_tile(float* dst, const T* src, long long stride, int rows, int D) {
+  for (int i = threadIdx.x; i < BT * DP / 4; i += kThreads) {
+    const int r = i / (DP / 4), c = i % (DP / 4) * 4;
+    float f[4] = {0.f, 0.f, 0.f, 0.f};
+    if (r < rows && c < D) load_pack<T, 4>(src + r * stride + c, f);
+    *reinterpret_cast<float4*>(dst + r * kPitch<DP> + c) = make_float4(f[0], f[1], f[2], f[3]);
+  }
+}
+
+// s[i][j] = <row ty + 16 i of A, row tx + 16 j of B>
+template <int DP>
+__device__ __forceinline__ void rows_by_rows(const float* A, const float* B, float (*s)[4], int tx, int ty) {
+  f32x2 acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0;
+#pragma unroll 4
+  for (int d = 0; d < DP; d += 4) {
+    ulonglong2 a[4], b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const ulonglong2*>(A + (ty + 16 * i) * kPitch<DP> + d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const ulonglong2*>(B + (tx + 16 * j) * kPitch<DP> + d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = fma2(a[i].y, b[j].y, fma2(a[i].x, b[j].x, acc[i][j]));
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = unpair(acc[i][j]);
+      s[i][j] = f.x + f.y;
+    }
+}
+
+// acc[i][c] += sum over k of P[ty + 16 i][k] V[k][4 tx + 64 c ...]
+template <int DP>
+__device__ __forceinline__ void scores_by_rows(const float* P, const float* V, f32x2 (*acc)[DP / 64][2], int tx, int ty) {
+#pragma unroll 2
+  for (int k = 0; k < BT; k += 4) {
+    float p[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 f = *reinterpret_cast<const float4*>(P + (ty + 16 * i) * PP + k);
+      p[i][0] = f.x; p[i][1] = f.y; p[i][2] = f.z; p[i][3] = f.w;
+    }
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int c = 0; c < DP / 64; ++c) {
+        const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(V + (k + kk) * kPitch<DP> + 4 * tx + 64 * c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          acc[i][c][0] = fma2(both(p[i][kk]), v.x, acc[i][c][0]);
+          acc[i][c][1] = fma2(both(p[i][kk]), v.y, acc[i][c][1]);
+        }
+      }
+  }
+}
+
+template <int DP>
+__device__ __forceinline__ void clear(f32x2 (*acc)[DP / 64][2]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c) acc[i][c][0] = acc[i][c][1] = 0;
+}
+
+// rows ty + 16 i below `rows` of an output tile, each times factor[i]
+template <typename T, int DP>
+__device__ __forceinline__ void store_tile(T* dst, long long stride, int rows, int D, f32x2 (*acc)[DP / 64][2], const float* factor, int tx,
+                                           int ty) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c) {
+      const int r = ty + 16 * i, col = 4 * tx + 64 * c;
+      if (r >= rows || col >= D) continue;
+      const float2 lo = unpair(acc[i][c][0]), hi = unpair(acc[i][c][1]);
+      const float f[4] = {lo.x * factor[i], lo.y * factor[i], hi.x * factor[i], hi.y * factor[i]};
+      store_pack<T, 4>(dst + r * stride + col, f);
+    }
+}
+
+template <typename F>
+__device__ __forceinline__ float over_columns(float v, F f) {       // over the 16 threads of a row
+#pragma unroll
+  for (int off = 8; off; off >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, off));
+  return v;
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) attention_simt_forward_kernel(const AttentionArgs a) {
+  extern __shared__ __align__(16) float smem[];
+  float *sq = smem, *sk = sq + BT * kPitch<DP>, *sv = sk + BT * kPitch<DP>, *sp = sv + BT * kPitch<DP>;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int tiles = ceil_div(a.Tq, BT);
+  const int q0 = blockIdx.x % tiles * BT, h = blockIdx.x / tiles % a.H, b = blockIdx.x / tiles / a.H;
+  const int kh = h / (a.H / a.Hkv), len = source_length(a, b), rows = min(BT, a.Tq - q0);
+  const T* q = static_cast<const T*>(a.q) + ((long long)b * a.Tq + q0) * a.q_stride + (long long)h * a.D;
+  const T* k = static_cast<const T*>(a.k) + (long long)b * a.Tk * a.k_stride + (long long)kh * a.D;
+  const T* v = static_cast<const T*>(a.v) + (long long)b * a.Tk * a.v_stride + (long long)kh * a.D;
+  load_tile<T, DP>(sq, q, a.q_stride, rows, a.D);
+  f32x2 acc[4][DP / 64][2];
+  clear<DP>(acc);
+  float top[4], sum[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { top[i] = -INFINITY; sum[i] = 0.f; }
+  const float c = a.scale * kLog2e;
+  for (int k0 = 0; k0 < len; k0 += BT) {
+    __syncthreads();                                  // the previous tiles have been read
+    load_tile<T, DP>(sk, k + k0 * a.k_stride, a.k_stride, len - k0, a.D);
+    load_tile<T, DP>(sv, v + k0 * a.v_stride, a.v_stride, len - k0, a.D);
+    __syncthreads();
+    float s[4][4];
+    rows_by_rows<DP>(sq, sk, s, tx, ty);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (k0 + tx + 16 * j >= len) s[i][j] = -INFINITY;
+        m = fmaxf(m, s[i][j]);
+      }
+      m = fmaxf(top[i], over_columns(m, [](float x, float y) { return fmaxf(x, y); }));
+      const float ref = m == -INFINITY ? 0.f : m;
+      const float shrink = exp2f((top[i] - ref) * c);
+      top[i] = m;
+      float t = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = exp2f((s[i][j] - ref) * c);
+        sp[(ty + 16 * i) * PP + tx + 16 * j] = p;
+        t += p;
+      }
+      sum[i] = fmaf(sum[i], shrink, t);
+#pragma unroll
+      for (int d = 0; d < DP / 64; ++d) {
+        acc[i][d][0] = mul2(acc[i][d][0], both(shrink));
+        acc[i][d][1] = mul2(acc[i][d][1], both(shrink));
+      }
+    }
+    __syncthreads();
+    scores_by_rows<DP>(sp, sv, acc, tx, ty);
+  }
+  float factor[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float total = over_columns(sum[i], [](float x, float y) { return x + y; });
+    factor[i] = len ? 1.f / total : 0.f;
+    if (a.lse && tx == 0 && ty + 16 * i < rows)
+      a.lse[((long long)b * a.H + h) * a.Tq + q0 + ty + 16 * i] = len ? top[i] * a.scale + logf(total) : -INFINITY;
+  }
+  store_tile<T, DP>(static_cast<T*>(a.o) + (((long long)b * a.Tq + q0) * a.H + h) * a.D, (long long)a.H * a.D, rows, a.D, acc, factor, tx,
+                    ty);
+}
+
+// dk and dv of 64 keys: the score tiles are computed key by query, over the queries of every head that shares the keys.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const AttentionArgs a) {
+  extern __shared__ __align__(16) float smem[];
+  float *sk = smem, *sv = sk + BT * kPitch<DP>, *sq = sv + BT * kPitch<DP>, *sd = sq + BT * kPitch<DP>, *sp = sd + BT * kPitch<DP>;
+  float *slse = sp + BT * PP, *sdelta = slse + BT;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int tiles = ceil_div(a.Tk, BT);
+  const int k0 = blockIdx.x % tiles * BT, kh = blockIdx.x / tiles % a.Hkv, b = blockIdx.x / tiles / a.Hkv;
+  const int len = source_length(a, b), rows = min(BT, a.Tk - k0), group = a.H / a.Hkv;
+  const long long koff = ((long long)b * a.Tk + k0) * a.k_stride + (long long)kh * a.D;
+  const long long voff = ((long long)b * a.Tk + k0) * a.v_stride + (long long)kh * a.D;
+  f32x2 dk[4][DP / 64][2], dv[4][DP / 64][2];
+  clear<DP>(dk);
+  clear<DP>(dv);
+  const float c = a.scale * kLog2e;
+  if (k0 < len) {
+    load_tile<T, DP>(sk, static_cast<const T*>(a.k) + koff, a.k_stride, len - k0, a.D);
+    load_tile<T, DP>(sv, static_cast<const T*>(a.v) + voff, a.v_stride, len - k0, a.D);
+    for (int h = kh * group; h < (kh + 1) * group; ++h) {
+      const T* q = static_cast<const T*>(a.q) + (long long)b * a.Tq * a.q_stride + (long long)h * a.D;
+      const T* dout = static_cast<const T*>(a.dout) + ((long long)b * a.Tq * a.H + h) * a.D;
+      const long long row = ((long long)b * a.H + h) * a.Tq;
+      for (int q0 = 0; q0 < a.Tq; q0 += BT) {
+        __syncthreads();
+        load_tile<T, DP>(sq, q + q0 * a.q_stride, a.q_stride, a.Tq - q0, a.D);
+        load_tile<T, DP>(sd, dout + (long long)q0 * a.H * a.D, (long long)a.H * a.D, a.Tq - q0, a.D);
+        if (threadIdx.x < BT) {
+          const bool in = q0 + threadIdx.x < a.Tq;                // queries behind the last one: P = exp(-inf) = 0
+          slse[threadIdx.x] = in ? a.lse[row + q0 + threadIdx.x] * kLog2e : INFINITY;
+          sdelta[threadIdx.x] = in ? a.delta[row + q0 + threadIdx.x] : 0.f;
+        }
+        __syncthreads();
+        float s[4][4], dp[4][4];
+        rows_by_rows<DP>(sk, sq, s, tx, ty);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            s[i][j] = k0 + ty + 16 * i < len ? exp2f(fmaf(s[i][j], c, -slse[tx + 16 * j])) : 0.f;
+            sp[(ty + 16 * i) * PP + tx + 16 * j] = s[i][j];
+          }
+        rows_by_rows<DP>(sv, sd, dp, tx, ty);
+        __syncthreads();
+        scores_by_rows<DP>(sp, sd, dv, tx, ty);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sp[(ty + 16 * i) * PP + tx + 16 * j] = s[i][j] * (dp[i][j] - sdelta[tx + 16 * j]);
+        __syncthreads();
+        scores_by_rows<DP>(sp, sq, dk, tx, ty);
+      }
+    }
+  }
+  // keys behind the length have gradient zero: their scores were zero throughout
+  const float one[4] = {1.f, 1.f, 1.f, 1.f}, scale[4] = {a.scale, a.scale, a.scale, a.scale};
+  store_tile<T, DP>(static_cast<T*>(a.dk) + koff, a.k_stride, rows, a.D, dk, scale, tx, ty);
+  store_tile<T, DP>(static_cast<T*>(a.dv) + voff, a.v_stride, rows, a.D, dv, one, tx, ty);
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const AttentionArgs a) {
+  extern __shared__ __align__(16) float smem[];
+  float *sq = smem, *sd = sq + BT * kPitch<DP>, *sk = sd + BT * kPitch<DP>, *sv = sk + BT * kPitch<DP>, *sp = sv + BT * kPitch<DP>;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int tiles = ceil_div(a.Tq, BT);
+  const int q0 = blockIdx.x % tiles * BT, h = blockIdx.x / tiles % a.H, b = blockIdx.x / tiles / a.H;
+  const int kh = h / (a.H / a.Hkv), len = source_length(a, b), rows = min(BT, a.Tq - q0);
+  const long long qoff = ((long long)b * a.Tq + q0) * a.q_stride + (long long)h * a.D;
+  const T* k = static_cast<const T*>(a.k) + (long long)b * a.Tk * a.k_stride + (long long)kh * a.D;
+  const T* v = static_cast<const T*>(a.v) + (long long)b * a.Tk * a.v_stride + (long long)kh * a.D;
+  f32x2 dq[4][DP / 64][2];
+  clear<DP>(dq);
+  const float c = a.scale * kLog2e;
+  if (len) {
+    load_tile<T, DP>(sq, static_cast<const T*>(a.q) + qoff, a.q_stride, rows, a.D);
+    load_tile<T, DP>(sd, static_cast<const T*>(a.dout) + (((long long)b * a.Tq + q0) * a.H + h) * a.D, (long long)a.H * a.D, rows, a.D);
+    float lse[4], delta[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const long long row = ((long long)b * a.H + h) * a.Tq + q0 + ty + 16 * i;
+      lse[i] = ty + 16 * i < rows ? a.lse[row] * kLog2e : INFINITY;
+      delta[i] = ty + 16 * i < rows ? a.delta[row] : 0.f;
+    }
+    for (int k0 = 0; k0 < len; k0 += BT) {
+      __syncthreads();
+      load_tile<T, DP>(sk, k + k0 * a.k_stride, a.k_stride, len - k0, a.D);
+      load_tile<T, DP>(sv, v + k0 * a.v_stride, a.v_stride, len - k0, a.D);
+      __syncthreads();
+      float s[4][4], dp[4][4];
+      rows_by_rows<DP>(sq, sk, s, tx, ty);
+      rows_by_rows<DP>(sd, sv, dp, tx, ty);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          sp[(ty + 16 * i) * PP + tx + 16 * j] =
+              k0 + tx + 16 * j < len ? exp2f(fmaf(s[i][j], c, -lse[i])) * (dp[i][j] - delta[i]) : 0.f;
+      __syncthreads();
+      scores_by_rows<DP>(sp, sk, dq, tx, ty);
+    }
+  }
+  const float scale[4] = {a.scale, a.scale, a.scale, a.scale};
+  store_tile<T, DP>(static_cast<T*>(a.dq) + qoff, a.q_stride, rows, a.D, dq, scale, tx, ty);
+}
+
+template <typename K>
+int launch(K kernel, long long blocks, int floats, const AttentionArgs& a, cudaStream_t st) {
+  const int bytes = floats * 4;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+    cudaGetLastError();
+    return GSHARD_ERR_CUDA;
+  }
+  kernel<<<(unsigned)blocks, kThreads, bytes, st>>>(a);
+  count_launch();
+  return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
+}
+
+template <typename T, int DP>
+int backward(const AttentionArgs& a, cudaStream_t st) {
+  const int floats = 4 * BT * kPitch<DP> + BT * PP + 2 * BT;
+  const int rc = a.Tk ? launch(attention_simt_dkv_kernel<T, DP>, (long long)ceil_div(a.Tk, BT) * a.Hkv * a.B, floats, a, st) : GSHARD_OK;
+  if (rc != GSHARD_OK || !a.Tq) return rc;
+  return launch(attention_simt_dq_kernel<T, DP>, (long long)ceil_div(a.Tq, BT) * a.H * a.B, floats, a, st);
+}
+
+template <typename T, int DP>
+int forward(const AttentionArgs& a, cudaStream_t st) {
+  return launch(attention_simt_forward_kernel<T, DP>, (long long)ceil_div(a.Tq, BT) * a.H * a.B, 3 * BT * kPitch<DP> + BT * PP, a, st);
+}
+
+}  // namespace
+
+int launch_attention_simt_forward(const AttentionArgs& a, bool bf16, cudaStream_t st) {
+  if (bf16) return a.D <= 64 ? forward<__nv_bfloat16, 64>(a, st) : forward<__nv_bfloat16, 128>(a, st);
+  return a.D <= 64 ? forward<float, 64>(a, st) : forward<float, 128>(a, st);
+}
+
+int launch_attention_simt_backward(const AttentionArgs& a, bool bf16, cudaStream_t st) {
+  if (bf16) return a.D <= 64 ? backward<__nv_bfloat16, 64>(a, st) : backward<__nv_bfloat16, 128>(a, st);
+  return a.D <= 64 ? backward<float, 64>(a, st) : backward<float, 128>(a, st);
+}
+
+}  // namespace gshard

@@ -53,17 +53,6 @@ __global__ void __launch_bounds__(256) linear_finish_kernel(const float4* __rest
   }
 }
 
-// The three bf16 planes of fp32 values: hi takes the top 8 bits of the significand, mid the next 8, lo the last 8,
-// each by truncation, so that hi + mid + lo is the value exactly (below 2^-110 to half a step of 2^-133) and nothing overflows.
-__device__ __forceinline__ void split3(const float* f, float* hi, float* mid, float* lo, int n) {
-#pragma unroll
-  for (int j = 0; j < n; ++j) {
-    hi[j] = __uint_as_float(__float_as_uint(f[j]) & 0xffff0000u);
-    const float r = f[j] - hi[j];
-    mid[j] = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
-    lo[j] = r - mid[j];
-  }
-}
 // Two tensors in one launch (the second may have no elements), n8 packs of 8 values each.
 __global__ void __launch_bounds__(256) linear_split_kernel(const float* __restrict__ src0, __nv_bfloat16* __restrict__ dst0, long long n0,
                                                            const float* __restrict__ src1, __nv_bfloat16* __restrict__ dst1, long long n1) {
@@ -227,11 +216,7 @@ int splits_for(long long rows, int cols, long long depth) {
 // eight; 2048 -> 2048 5.9 to 6.5, 6.6 to 6.5, 8.8 to 6.5; 8192 -> 1024 8.0 to 9.8, 9.2 to 9.8, 11.6 to 9.8.
 bool few_rows(int64_t n, bool bf16, MidShape mid) { return n <= 2 || (n <= 8 && !(bf16 && mid.bn)); }
 
-struct LinearPlan {
-  size_t status, xp, wp, dpre, colsum, join, total;
-  int planes, chunks, chunk, splits, dx_splits, dw_splits;
-  MidShape mid, dx_mid, dw_mid;          // bn > 0: the product goes to linear_mid.cu
-};
+}  // namespace
 
 LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, int out_dtype, bool backward) {
   Carver c;
@@ -277,6 +262,8 @@ int linear_validate(int64_t n, int32_t K, int32_t cols, int32_t dtype, int32_t o
   return GSHARD_OK;
 }
 
+namespace {
+
 // the tensor-core GEMMs, whose operands are bf16 (or planes of it)
 Dims linear_dims(int K, int cols) {
   gshard_moe_shape one{};
@@ -315,40 +302,14 @@ int zero(void* p, size_t bytes, cudaStream_t st) {
 
 }  // namespace
 
-}  // namespace gshard
-
-using namespace gshard;
-
-extern "C" {
-
-size_t gshard_linear_workspace_bytes(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype, int for_backward) {
-  if (linear_validate(n_rows, K, cols, dtype, out_dtype) != GSHARD_OK) return 0;
-  return linear_plan(n_rows, K, cols, dtype, out_dtype, for_backward != 0).total;
-}
-
-int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype, int32_t activation,
-                          const void* x, const void* w, const float* bias, const void* residual, void* y, void* pre,
-                          void* workspace, size_t workspace_bytes, void* cuda_stream) {
-  launch_counter().n = 0;
-  GS_CHECK(linear_validate(n_rows, K, cols, dtype, out_dtype));
-  if (activation < GSHARD_ACT_NONE || activation > GSHARD_ACT_SILU) return GSHARD_ERR_INVALID_ARG;
-  if (n_rows == 0) return GSHARD_OK;
-  GS_CHECK_PTR(x); GS_CHECK_PTR(w); GS_CHECK_PTR(y);
-  GS_CHECK_OPTIONAL_PTR(bias); GS_CHECK_OPTIONAL_PTR(residual); GS_CHECK_OPTIONAL_PTR(pre);
-  if (y == x || y == w || pre == x || pre == w || (pre && (pre == y || pre == residual))) return GSHARD_ERR_INVALID_ARG;
-  const LinearPlan pl = linear_plan(n_rows, K, cols, dtype, out_dtype, false);
-  GS_CHECK_WORKSPACE(workspace, workspace_bytes, pl.total);
-  GS_CHECK(check_device());
-  NvtxRange range("gshard.linear");
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  int* status = static_cast<int*>(workspace);
-  const LinearEpilogue lin{bias, residual, pre, activation};
+int linear_run_forward(int64_t n_rows, int K, int cols, int dtype, int out_dtype, const LinearEpilogue& lin, const void* x,
+                       const void* w, void* y, const LinearPlan& pl, unsigned char* ws, cudaStream_t st) {
+  int* status = reinterpret_cast<int*>(ws);
   const bool out_f32 = out_dtype == GSHARD_F32;
   if (few_rows(n_rows, dtype == GSHARD_BF16, pl.mid)) {
     GS_CHECK(launch_linear_few((int)n_rows, K, cols, dtype == GSHARD_BF16, out_f32, x, w, y, lin, status, st));
     return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
   }
-  unsigned char* ws = static_cast<unsigned char*>(workspace);
   const Dims d = linear_dims(K, cols);
   UmmaGemm g{};
   g.A = x; g.B = w; g.C = y; g.rows = (int)n_rows; g.cols = cols; g.K = K; g.batch = 1;
@@ -376,6 +337,71 @@ int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype
     count_launch();
   }
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
+}
+
+int linear_run_gradients(int64_t n_rows, int K, int cols, bool fp32, int planes, const void* x, const void* w, const void* dpre, void* dx,
+                         void* dw, const LinearPlan& pl, unsigned char* ws, bool cleared, cudaStream_t st) {
+  int* status = reinterpret_cast<int*>(ws);
+  const Dims d = linear_dims(K, cols);
+  float* join = reinterpret_cast<float*>(ws + pl.join);
+  if (fp32 && (dx || dw))
+    split_planes(w, ws + pl.wp, dx ? (long long)K * cols : 0, x, ws + pl.xp, dw ? n_rows * K : 0, st);
+  if (dx) {                                       // [n, K] = dpre [n, cols] . w^T, both contiguous along cols
+    UmmaGemm g{};
+    g.A = dpre; g.B = w; g.C = dx; g.rows = (int)n_rows; g.cols = K; g.K = cols; g.batch = 1;
+    g.a_kmajor = true; g.b_kmajor = true; g.a_ld = cols; g.b_ld = cols; g.c_ld = K;
+    g.prefer_two_sm = 1; g.out_f32 = fp32; g.clear_status = !cleared;
+    cleared = true;
+    if (fp32) {
+      g.B = ws + pl.wp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * cols; g.b_bs = (long long)K * cols;
+    } else if (planes == 2) {
+      g.planes_a = 2; g.planes_b = 1; g.a_bs = n_rows * cols;
+    }
+    GS_CHECK(gemm_joined(d, g, pl.dx_mid, pl.dx_splits, join, status, st));
+  }
+  if (dw) {                                       // [K, cols] = x^T . dpre, both stored row by row of the contraction
+    UmmaGemm g{};
+    g.A = x; g.B = dpre; g.C = dw; g.rows = K; g.cols = cols; g.K = (int)n_rows; g.batch = 1;
+    g.a_kmajor = false; g.b_kmajor = false; g.a_ld = K; g.b_ld = cols; g.c_ld = cols;
+    g.prefer_two_sm = 1; g.out_f32 = fp32; g.clear_status = !cleared;
+    if (fp32) {
+      g.A = ws + pl.xp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * K; g.b_bs = n_rows * cols;
+    } else if (planes == 2) {
+      g.planes_a = 1; g.planes_b = 2; g.b_bs = n_rows * cols;
+    }
+    GS_CHECK(gemm_joined(d, g, pl.dw_mid, pl.dw_splits, join, status, st));
+  }
+  return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
+}
+
+}  // namespace gshard
+
+using namespace gshard;
+
+extern "C" {
+
+size_t gshard_linear_workspace_bytes(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype, int for_backward) {
+  if (linear_validate(n_rows, K, cols, dtype, out_dtype) != GSHARD_OK) return 0;
+  return linear_plan(n_rows, K, cols, dtype, out_dtype, for_backward != 0).total;
+}
+
+int gshard_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype, int32_t activation,
+                          const void* x, const void* w, const float* bias, const void* residual, void* y, void* pre,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  launch_counter().n = 0;
+  GS_CHECK(linear_validate(n_rows, K, cols, dtype, out_dtype));
+  if (activation < GSHARD_ACT_NONE || activation > GSHARD_ACT_SILU) return GSHARD_ERR_INVALID_ARG;
+  if (n_rows == 0) return GSHARD_OK;
+  GS_CHECK_PTR(x); GS_CHECK_PTR(w); GS_CHECK_PTR(y);
+  GS_CHECK_OPTIONAL_PTR(bias); GS_CHECK_OPTIONAL_PTR(residual); GS_CHECK_OPTIONAL_PTR(pre);
+  if (y == x || y == w || pre == x || pre == w || (pre && (pre == y || pre == residual))) return GSHARD_ERR_INVALID_ARG;
+  const LinearPlan pl = linear_plan(n_rows, K, cols, dtype, out_dtype, false);
+  GS_CHECK_WORKSPACE(workspace, workspace_bytes, pl.total);
+  GS_CHECK(check_device());
+  NvtxRange range("gshard.linear");
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return linear_run_forward(n_rows, K, cols, dtype, out_dtype, LinearEpilogue{bias, residual, pre, activation}, x, w, y, pl,
+                            static_cast<unsigned char*>(workspace), st);
 }
 
 int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype, int32_t activation,
@@ -427,37 +453,8 @@ int gshard_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_t dtyp
     }
   }
   const void* dpre = convert ? buf : dy;
-  bool cleared = buf || colsum;                   // the status word, by the first kernel of the call
-  const Dims d = linear_dims(K, cols);
-  float* join = reinterpret_cast<float*>(ws + pl.join);
-  if (fp32 && (dx || dw))
-    split_planes(w, ws + pl.wp, dx ? (long long)K * cols : 0, x, ws + pl.xp, dw ? n_rows * K : 0, st);
-  if (dx) {                                       // [n, K] = dpre [n, cols] . w^T, both contiguous along cols
-    UmmaGemm g{};
-    g.A = dpre; g.B = w; g.C = dx; g.rows = (int)n_rows; g.cols = K; g.K = cols; g.batch = 1;
-    g.a_kmajor = true; g.b_kmajor = true; g.a_ld = cols; g.b_ld = cols; g.c_ld = K;
-    g.prefer_two_sm = 1; g.out_f32 = fp32; g.clear_status = !cleared;
-    cleared = true;
-    if (fp32) {
-      g.B = ws + pl.wp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * cols; g.b_bs = (long long)K * cols;
-    } else if (planes == 2) {
-      g.planes_a = 2; g.planes_b = 1; g.a_bs = n_rows * cols;
-    }
-    GS_CHECK(gemm_joined(d, g, pl.dx_mid, pl.dx_splits, join, status, st));
-  }
-  if (dw) {                                       // [K, cols] = x^T . dpre, both stored row by row of the contraction
-    UmmaGemm g{};
-    g.A = x; g.B = dpre; g.C = dw; g.rows = K; g.cols = cols; g.K = (int)n_rows; g.batch = 1;
-    g.a_kmajor = false; g.b_kmajor = false; g.a_ld = K; g.b_ld = cols; g.c_ld = cols;
-    g.prefer_two_sm = 1; g.out_f32 = fp32; g.clear_status = !cleared;
-    if (fp32) {
-      g.A = ws + pl.xp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * K; g.b_bs = n_rows * cols;
-    } else if (planes == 2) {
-      g.planes_a = 1; g.planes_b = 2; g.b_bs = n_rows * cols;
-    }
-    GS_CHECK(gemm_joined(d, g, pl.dw_mid, pl.dw_splits, join, status, st));
-  }
-  return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
+  const bool cleared = buf || colsum;             // the status word, by the first kernel of the call
+  return linear_run_gradients(n_rows, K, cols, fp32, planes, x, w, dpre, dx, dw, pl, ws, cleared, st);
 }
 
 }  // extern "C"

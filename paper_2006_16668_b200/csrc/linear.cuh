@@ -16,6 +16,34 @@ struct MidShape { int bn, splits; };
 MidShape linear_mid_shape(long long rows, int cols, long long depth, int passes, bool out_f32);
 int launch_linear_mid(const UmmaGemm& g, const LinearEpilogue& lin, MidShape shape, bool clear_status, int* status, cudaStream_t st);
 
+// linear.cu: regions of the workspace and how the products are run.
+struct LinearPlan {
+  size_t status, xp, wp, dpre, colsum, join, total;
+  int planes, chunks, chunk, splits, dx_splits, dw_splits;
+  MidShape mid, dx_mid, dw_mid;          // bn > 0: the product goes to linear_mid.cu
+};
+
+LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, int out_dtype, bool backward);
+int linear_validate(int64_t n, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype);
+// y = act(x . w + bias) + residual on checked arguments.
+int linear_run_forward(int64_t n_rows, int K, int cols, int dtype, int out_dtype, const LinearEpilogue& lin, const void* x,
+                       const void* w, void* y, const LinearPlan& pl, unsigned char* ws, cudaStream_t st);
+// dx = dpre . w^T and dw = x^T . dpre (either may be nullptr) from `planes` bf16 planes of dpre [n_rows, cols] (3: fp32).
+// cleared: an earlier kernel of the call has cleared the status word.
+int linear_run_gradients(int64_t n_rows, int K, int cols, bool fp32, int planes, const void* x, const void* w, const void* dpre,
+                         void* dx, void* dw, const LinearPlan& pl, unsigned char* ws, bool cleared, cudaStream_t st);
+
+// The three bf16 planes of fp32 values: hi takes the top 8 bits of the significand, mid the next 8, lo the last 8,
+// each by truncation, so that hi + mid + lo is the value exactly (below 2^-110 to half a step of 2^-133) and nothing overflows.
+__device__ __forceinline__ void split3(const float* f, float* hi, float* mid, float* lo, int n) {
+#pragma unroll
+  for (int j = 0; j < n; ++j) {
+    hi[j] = __uint_as_float(__float_as_uint(f[j]) & 0xffff0000u);
+    const float r = f[j] - hi[j];
+    mid[j] = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+    lo[j] = r - mid[j];
+  }
+}
 // The operator's epilogue on four neighbouring sums at element `off` (column `col`) of the output.
 template <typename TY>
 __device__ __forceinline__ void linear_epilogue4(const LinearEpilogue& lin, void* y, long long off, int col, float4 s) {
