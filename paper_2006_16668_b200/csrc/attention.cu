@@ -112,7 +112,7 @@ int gshard_cross_attention_forward(const gshard_attention_config* config, const 
   AttentionArgs a = attention_args(c, q, k, v, k_lengths);
   a.o = o; a.lse = lse; a.status = static_cast<int*>(workspace);
   GS_CHECK(clear_status(workspace, st));
-  return launch_attention_simt_forward(a, c.dtype == GSHARD_BF16, st);
+  return c.dtype == GSHARD_BF16 ? launch_attention_umma_forward(a, st) : launch_attention_simt_forward(a, false, st);
 }
 
 int gshard_cross_attention_backward(const gshard_attention_config* config, const void* q, const void* k, const void* v,

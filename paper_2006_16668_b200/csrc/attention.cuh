@@ -30,4 +30,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 int launch_attention_simt_forward(const AttentionArgs& a, bool bf16, cudaStream_t st);
 int launch_attention_simt_backward(const AttentionArgs& a, bool bf16, cudaStream_t st);
 
+// attention_umma.cu: bf16 on the tensor cores
+int launch_attention_umma_forward(const AttentionArgs& a, cudaStream_t st);
+
 }  // namespace gshard

@@ -1,0 +1,395 @@
+// Cross attention forward in bf16 on the tensor cores (tcgen05, accumulators in tensor memory), one pass over the keys.
+//
+// A CTA owns two tiles of 128 query rows that share a key head (neighbouring tiles of one head, or tiles of heads in the
+// same group) and walks the source in blocks of 128 keys.  Per block and tile: S = Q K^T into 128 columns of tensor memory; one
+// thread per row reads its scores, takes the block's maximum, writes p = 2^(c (s - m)) as bf16 over the scores, and the
+// second product O += P V reads P from tensor memory.  While the four warps of one tile work on their scores, the
+// tensor core runs the other tile's products.  The issue order S0 | S1, then PV0, S0', PV1, S1' ... makes every hand-over of a
+// buffer a consequence of the in-order execution of MMAs:
+//   scores of block j+1 overwrite P of block j behind the PV product that read it;
+//   "scores complete" of block j+1 also says that PV of block j is complete, so that O may be rescaled.
+// O is rescaled only when a row's maximum has grown by more than 2^8 since the last time (the weights then stay below
+// 2^8, and their sums far from overflow); that is rare after the first blocks.
+// Persistent grid, one CTA per multiprocessor; while a tile's rows are written out, the next tile's scores are computed.
+//
+// Rows behind the source's length: scores are masked before the maximum; rows of V that hold something else are zeroed in
+// shared memory up to the next multiple of 16, where the last block's product ends.
+#include <algorithm>
+
+#include "attention.cuh"
+#include "pack.cuh"
+#include "sm100_ptx.cuh"
+#include "tensor_map.cuh"
+
+namespace gshard {
+
+namespace {
+
+constexpr int kRows = 128;                    // query rows of a tile, keys of a block
+constexpr int kThreads = 384;                 // 2 x 4 softmax warps; TMA, MMA and two idle warps
+// registers per thread: 168 at launch, moved to where the scores live (2 x 128 x 216 + 128 x 72 = 384 x 168)
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+constexpr float kSlack = 8.f;                 // growth of a row's maximum (powers of two) that O is not rescaled for
+
+template <int DP> struct Layout {
+  static constexpr int tile = kRows * DP * 2;
+  static constexpr int stages = DP == 128 ? 4 : 6;
+  static constexpr int kv_off = 2 * tile;
+  static constexpr int bar_off = kv_off + stages * tile;
+  static constexpr int bytes = bar_off + 256 + 1024;
+  static_assert(bytes <= 232448, "shared memory budget");
+};
+
+struct Tile { int h, q0, rows; };             // a 128-row tile of one head
+
+struct Item {
+  int b, kh, first, tiles, len;               // the tiles first, first + 1 (or only the first) of the key head's list
+};
+
+struct ForwardParams {
+  AttentionArgs a;
+  int q_tiles;                                // tiles per head
+  int list;                                   // tiles per key head
+  int pairs;                                  // items per key head
+  int items;
+};
+
+__device__ __forceinline__ Item item_of(const ForwardParams& p, int i) {
+  Item t;
+  t.first = i % p.pairs * 2;
+  t.kh = i / p.pairs % p.a.Hkv;
+  t.b = i / p.pairs / p.a.Hkv;
+  t.tiles = min(2, p.list - t.first);
+  t.len = source_length(p.a, t.b);
+  return t;
+}
+__device__ __forceinline__ Tile tile_of(const ForwardParams& p, const Item& t, int half) {
+  const int i = t.first + half;
+  Tile r;
+  r.h = t.kh * (p.a.H / p.a.Hkv) + i / p.q_tiles;
+  r.q0 = i % p.q_tiles * kRows;
+  r.rows = min(kRows, p.a.Tq - r.q0);
+  return r;
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                              const __grid_constant__ CUtensorMap map_v, const ForwardParams p) {
+  using L = Layout<DP>;
+  constexpr int kStages = L::stages;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  unsigned char* ring = smem + L::kv_off;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bar_off);
+  uint64_t* kv_full = bars;                   // [kStages]
+  uint64_t* kv_empty = kv_full + kStages;     // [kStages]
+  uint64_t* q_full = kv_empty + kStages;      // [2] a tile's queries landed
+  uint64_t* q_empty = q_full + 2;             // [2] ... and have been read for the last time
+  uint64_t* s_full = q_empty + 2;             // [2] scores complete
+  uint64_t* p_full = s_full + 2;              // [2] weights written (4 warps)
+  uint64_t* o_full = p_full + 2;              // [2] output complete
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) { ptx::mbar_init(kv_full + s, 1); ptx::mbar_init(kv_empty + s, 1); }
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(q_full + i, 1); ptx::mbar_init(q_empty + i, 1);
+      ptx::mbar_init(s_full + i, 1); ptx::mbar_init(p_full + i, 4); ptx::mbar_init(o_full + i, 1);
+    }
+    *abort_flag = 0;
+    ptx::fence_mbar_init();
+    ptx::prefetch_tensormap(&map_q);
+    ptx::prefetch_tensormap(&map_k);
+    ptx::prefetch_tensormap(&map_v);
+  }
+  if (warp == 9) {
+    ptx::tmem_alloc(tmem_slot, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;           // S0, S1 (128 columns each), O0, O1 (DP each)
+  const uint32_t tmem_o = tmem + 256;
+
+  bool ok = true;
+  if (warp >= 8) {
+    ptx::registers_down<kOtherRegs>();
+    if (warp == 8) {
+      // ------------------------------ TMA producer -----------------------------------------------
+      if (lane == 0) {
+        const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_last();
+        int stage = 0; uint32_t phase = 0;
+        uint32_t q_phase[2] = {0, 0};
+        auto load = [&](const CUtensorMap* map, int kh, int k0, int b) {
+          if (!ptx::mbar_wait(kv_empty + stage, phase ^ 1u, abort_flag)) { ok = false; return; }
+          ptx::mbar_arrive_expect_tx(kv_full + stage, L::tile);
+  #pragma unroll
+          for (int j = 0; j < DP / 64; ++j)
+            ptx::tma_load_4d(ring + stage * L::tile + j * (kRows * 128), map, kv_full + stage, j * 64, kh, k0, b, again);
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        };
+        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+          const Item t = item_of(p, i);
+          if (t.len == 0) continue;
+          for (int half = 0; half < t.tiles && ok; ++half) {
+            const Tile q = tile_of(p, t, half);
+            if (!ptx::mbar_wait(q_empty + half, q_phase[half] ^ 1u, abort_flag)) { ok = false; break; }
+            q_phase[half] ^= 1u;
+            ptx::mbar_arrive_expect_tx(q_full + half, L::tile);
+  #pragma unroll
+            for (int j = 0; j < DP / 64; ++j)
+              ptx::tma_load_4d(smem + half * L::tile + j * (kRows * 128), &map_q, q_full + half, j * 64, q.h, q.q0, t.b, once);
+            if (half == 0) load(&map_k, t.kh, 0, t.b);
+          }
+          for (int k0 = 0; k0 < t.len && ok; k0 += kRows) {
+            load(&map_v, t.kh, k0, t.b);
+            if (ok && k0 + kRows < t.len) load(&map_k, t.kh, k0 + kRows, t.b);
+          }
+        }
+      }
+    } else if (warp == 9) {
+      // ------------------------------ MMA issuer (whole warp waits, lane 0 issues) ------------------
+      constexpr uint32_t idesc_s = ptx::make_idesc_bf16(kRows, kRows, false, false);
+      constexpr uint32_t idesc_o = ptx::make_idesc_bf16(kRows, DP, false, true);
+      int stage = 0; uint32_t phase = 0;
+      uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (ok && !__all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag))) ok = false;
+        ptx::tc_fence_after_sync();
+        return ok;
+      };
+      auto next = [&] { if (++stage == kStages) { stage = 0; phase ^= 1u; } };
+      // scores of tile `half` against the keys in the ring's stage
+      auto scores = [&](int half) {
+        if (lane) return;
+        const uint32_t sq = ptx::smem_u32(smem + half * L::tile), sk = ptx::smem_u32(ring + stage * L::tile);
+  #pragma unroll
+        for (int k = 0; k < DP / 16; ++k) {
+          const uint32_t off = (uint32_t)(k / 4 * (kRows * 128) + k % 4 * 32);
+          ptx::umma_bf16(tmem + half * kRows, ptx::make_smem_desc(sq + off, 16, 1024), ptx::make_smem_desc(sk + off, 16, 1024), idesc_s,
+                         k != 0 ? 1u : 0u);
+        }
+        ptx::umma_commit(s_full + half);
+      };
+      for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+        const Item t = item_of(p, i);
+        if (t.len == 0) continue;
+        const int blocks = ceil_div(t.len, kRows);
+        for (int half = 0; half < t.tiles; ++half) {
+          if (!wait(q_full + half, q_phase[half])) break;
+          q_phase[half] ^= 1u;
+          if (half == 0 && !wait(kv_full + stage, phase)) break;
+          scores(half);
+          if (blocks == 1 && lane == 0) ptx::umma_commit(q_empty + half);
+        }
+        if (!ok) break;
+        if (lane == 0) ptx::umma_commit(kv_empty + stage);
+        next();
+        for (int j = 0; j < blocks && ok; ++j) {
+          const int left = t.len - j * kRows;
+          const int steps = min(kRows, (left + 15) & ~15) / 16;        // 16 keys each
+          if (!wait(kv_full + stage, phase)) break;
+          const int v_stage = stage;
+          unsigned char* sv = ring + v_stage * L::tile;
+          if (left < kRows && j * kRows + left < p.a.Tk && steps * 16 != left) {     // what lies behind the last key
+            const int bad = steps * 16 - left;
+            for (int x = lane; x < bad * (DP / 8); x += 32) {
+              const int row = left + x / (DP / 8), c = x % (DP / 8);
+              *reinterpret_cast<uint4*>(sv + c / 8 * (kRows * 128) + row * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+            }
+            ptx::fence_proxy_async();
+            __syncwarp();
+          }
+          next();
+          for (int half = 0; half < t.tiles; ++half) {
+            if (!wait(p_full + half, p_phase[half])) break;
+            p_phase[half] ^= 1u;
+            if (lane == 0) {
+              const uint32_t b0 = ptx::smem_u32(sv);
+              for (int k = 0; k < steps; ++k)
+                ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, ptx::make_smem_desc(b0 + k * 2048, kRows * 128, 1024), idesc_o,
+                                  (j | k) != 0 ? 1u : 0u);
+              if (half == t.tiles - 1) ptx::umma_commit(kv_empty + v_stage);
+              if (j == blocks - 1) ptx::umma_commit(o_full + half);
+            }
+            if (j + 1 < blocks) {
+              if (half == 0 && !wait(kv_full + stage, phase)) break;
+              scores(half);
+              if (lane == 0) {
+                if (j + 2 == blocks) ptx::umma_commit(q_empty + half);
+                if (half == t.tiles - 1) ptx::umma_commit(kv_empty + stage);
+              }
+            }
+          }
+          if (j + 1 < blocks) next();
+        }
+      }
+    }
+  } else {
+    // ------------------------------ softmax: one thread per row ----------------------------------
+    ptx::registers_up<kSoftmaxRegs>();
+    const int half = warp >> 2;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + half * kRows + lanes, t_o = tmem_o + half * DP + lanes;
+    const int r = threadIdx.x & 127;
+    const float c = p.a.scale * kLog2e;
+    uint32_t s_phase = 0, o_phase = 0;
+    for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+      const Item t = item_of(p, i);
+      if (half >= t.tiles) continue;
+      const Tile q = tile_of(p, t, half);
+      const bool in = r < q.rows;
+      const long long token = (long long)t.b * p.a.Tq + q.q0 + r;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.a.o) + (token * p.a.H + q.h) * p.a.D;
+      float* lse = p.a.lse ? p.a.lse + ((long long)t.b * p.a.H + q.h) * p.a.Tq + q.q0 + r : nullptr;
+      if (t.len == 0) {
+        if (in) {
+          for (int d = 0; d < p.a.D; d += 8) *reinterpret_cast<uint4*>(out + d) = make_uint4(0, 0, 0, 0);
+          if (lse) *lse = -INFINITY;
+        }
+        continue;
+      }
+      float top = -INFINITY, sum = 0.f;        // the maximum that the weights so far refer to, and their sum
+      for (int k0 = 0; k0 < t.len; k0 += kRows) {
+        if (!__all_sync(0xffffffffu, ptx::mbar_wait(s_full + half, s_phase, abort_flag))) { ok = false; break; }
+        s_phase ^= 1u;
+        ptx::tc_fence_after_sync();
+        uint32_t s[kRows];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ptx::tmem_ld_32x32(t_s + j * 32, s + j * 32);
+        ptx::tmem_ld_wait();
+        const int left = t.len - k0;
+        if (left < kRows) {
+#pragma unroll
+          for (int j = 0; j < kRows; ++j)
+            if (j >= left) s[j] = 0xff800000u;
+        }
+        float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) m[j & 3] = fmaxf(m[j & 3], __uint_as_float(s[j]));
+        const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+        if (k0 == 0) {
+          top = fmaxf(most, -1e30f);
+        } else {
+          const bool grown = (most - top) * c > kSlack;
+          if (__any_sync(0xffffffffu, grown)) {
+            const float shrink = grown ? exp2_approx((top - most) * c) : 1.f;
+            if (grown) top = most;
+            sum *= shrink;
+#pragma unroll
+            for (int j = 0; j < DP / 16; ++j) {
+              uint32_t o[16];
+              ptx::tmem_ld_32x16(t_o + j * 16, o);
+              ptx::tmem_ld_wait();
+#pragma unroll
+              for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * shrink);
+              ptx::tmem_st_32x16(t_o + j * 16, o);
+            }
+          }
+        }
+        const f32x2 c2 = both(c), m2 = both(-top * c);
+        f32x2 sum2[2] = {0, 0};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const int at = h * 64 + 2 * j;
+            const float2 x = unpair(fma2(pair(__uint_as_float(s[at]), __uint_as_float(s[at + 1])), c2, m2));
+            const float e0 = exp2_approx(x.x), e1 = exp2_approx(x.y);
+            sum2[j & 1] = add2(sum2[j & 1], pair(e0, e1));
+            const __nv_bfloat162 b = __floats2bfloat162_rn(e0, e1);
+            w[j] = *reinterpret_cast<const uint32_t*>(&b);
+          }
+          ptx::tmem_st_32x32(t_s + h * 32, w);
+        }
+        const float2 part = unpair(add2(sum2[0], sum2[1]));
+        sum += part.x + part.y;
+        ptx::tmem_st_wait();
+        ptx::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(p_full + half);
+      }
+      if (!ok) break;
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(o_full + half, o_phase, abort_flag))) { ok = false; break; }
+      o_phase ^= 1u;
+      ptx::tc_fence_after_sync();
+      const float factor = 1.f / sum;
+#pragma unroll
+      for (int j = 0; j < DP / 32; ++j) {
+        uint32_t o[32];
+        ptx::tmem_ld_32x32(t_o + j * 32, o);
+        ptx::tmem_ld_wait();
+        if (in) {
+#pragma unroll
+          for (int d = 0; d < 32; d += 8) {
+            float f[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) f[x] = __uint_as_float(o[d + x]) * factor;
+            if (j * 32 + d < p.a.D) store_pack<__nv_bfloat16, 8>(out + j * 32 + d, f);
+          }
+        }
+      }
+      if (lse && in) *lse = top * p.a.scale + logf(sum);
+      ptx::tc_fence_before_sync();
+    }
+  }
+
+  // ------------------------------ teardown -------------------------------------------------------
+  if (!ok) {
+    *abort_flag = 1;
+    set_device_status(p.a.status, GSHARD_ERR_TIMEOUT);
+    const uint64_t t0 = ptx::globaltimer_ns();
+    while (ptx::globaltimer_ns() - t0 < 2000000ull) { __nanosleep(1000); }
+  }
+  __syncwarp();
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 9) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int DP>
+int forward(const AttentionArgs& a, cudaStream_t st) {
+  ForwardParams p;
+  p.a = a;
+  p.q_tiles = ceil_div(a.Tq, kRows);
+  p.list = p.q_tiles * (a.H / a.Hkv);
+  p.pairs = ceil_div(p.list, 2);
+  p.items = p.pairs * a.Hkv * a.B;
+  CUtensorMap mq, mk, mv;
+  // a source of no tokens: the maps are not used
+  const int tokens = a.Tk > 0 ? a.Tk : 1;
+  if (!make_token_map(&mq, a.q, a.D, a.H, a.Tq, a.B, a.q_stride, kRows) ||
+      !make_token_map(&mk, a.Tk > 0 ? a.k : a.q, a.D, a.Tk > 0 ? a.Hkv : 1, tokens, a.Tk > 0 ? a.B : 1, a.k_stride, kRows) ||
+      !make_token_map(&mv, a.Tk > 0 ? a.v : a.q, a.D, a.Tk > 0 ? a.Hkv : 1, tokens, a.Tk > 0 ? a.B : 1, a.v_stride, kRows))
+    return GSHARD_ERR_CUDA;
+  auto kernel = attention_umma_forward_kernel<DP>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<DP>::bytes) != cudaSuccess) {
+    cudaGetLastError();
+    return GSHARD_ERR_CUDA;
+  }
+  kernel<<<std::min(p.items, device_sms()), kThreads, Layout<DP>::bytes, st>>>(mq, mk, mv, p);
+  count_launch();
+  return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
+}
+
+}  // namespace
+
+int launch_attention_umma_forward(const AttentionArgs& a, cudaStream_t st) {
+  return a.D <= 64 ? forward<64>(a, st) : forward<128>(a, st);
+}
+
+}  // namespace gshard

@@ -48,6 +48,25 @@ inline bool make_map(CUtensorMap* map, const void* base, long long inner, long l
   return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess && encode();
 }
 
+// 4-D bf16 tensor map {head_dim, heads, tokens, batch} of a [batch, tokens, heads, head_dim] tensor whose tokens lie `stride`
+// elements apart, with boxes of 64 head dimensions by `box_tokens` tokens of one head, 128-byte swizzle; outside reads as zero.
+inline bool make_token_map(CUtensorMap* map, const void* base, int head_dim, int heads, long long tokens, long long batch, long long stride,
+                           int box_tokens) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)batch};
+  cuuint64_t strides[3] = {(cuuint64_t)head_dim * 2, (cuuint64_t)stride * 2, (cuuint64_t)(tokens * stride) * 2};
+  cuuint32_t box[4] = {64, 1, (cuuint32_t)box_tokens, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  auto encode = [&] {
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  if (encode()) return true;
+  int device = 0;                              // a thread without a current context, as above
+  return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess && encode();
+}
+
 // Tensor map of an output matrix batch C [batch][rows][cols] (row pitch c_ld, batch pitch c_bs elements)
 // for the epilogue's 32-row x 128-byte stores.
 inline bool make_store_map(CUtensorMap* map, void* base, long long cols, long long rows, long long batch,
