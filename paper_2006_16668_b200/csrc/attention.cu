@@ -8,21 +8,20 @@ namespace gshard {
 
 namespace {
 
-// delta[b, h, t] = sum over d of dout o, one warp per row
-template <typename T>
+// delta[b, h, t] = sum over d of dout o in fp32, one warp per row
 __global__ void __launch_bounds__(256) attention_delta_kernel(const AttentionArgs a, float* delta, long long rows) {
-  constexpr int W = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & 31;
   for (long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += (long long)gridDim.x * 8) {
-    const T* o = static_cast<const T*>(a.o) + r * a.D;
-    const T* g = static_cast<const T*>(a.dout) + r * a.D;
+    const float* o = static_cast<const float*>(a.o) + r * a.D;
+    const float* g = static_cast<const float*>(a.dout) + r * a.D;
     float s = 0.f;
-    for (int c = lane * W; c < a.D; c += 32 * W) {
-      float x[W], y[W];
-      load_pack<T, W>(o + c, x);
-      load_pack<T, W>(g + c, y);
+    const int c = lane * 4;
+    if (c < a.D) {
+      float x[4], y[4];
+      load_pack<float, 4>(o + c, x);
+      load_pack<float, 4>(g + c, y);
 #pragma unroll
-      for (int j = 0; j < W; ++j) s = fmaf(x[j], y[j], s);
+      for (int j = 0; j < 4; ++j) s = fmaf(x[j], y[j], s);
     }
 #pragma unroll
     for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
@@ -40,7 +39,8 @@ AttentionPlan attention_plan(const gshard_attention_config& c, bool backward) {
   Carver w;
   AttentionPlan p{};
   p.status = w.take(256);
-  if (backward) p.delta = w.take((size_t)c.batch * c.heads * c.q_len * 4);
+  if (backward)
+    p.delta = w.take(4 * (c.dtype == GSHARD_BF16 ? attention_stats_floats(c.batch, c.q_len, c.heads) : (size_t)c.batch * c.heads * c.q_len));
   p.total = w.off;
   return p;
 }
@@ -112,7 +112,7 @@ int gshard_cross_attention_forward(const gshard_attention_config* config, const 
   AttentionArgs a = attention_args(c, q, k, v, k_lengths);
   a.o = o; a.lse = lse; a.status = static_cast<int*>(workspace);
   GS_CHECK(clear_status(workspace, st));
-  return c.dtype == GSHARD_BF16 ? launch_attention_umma_forward(a, st) : launch_attention_simt_forward(a, false, st);
+  return c.dtype == GSHARD_BF16 ? launch_attention_umma_forward(a, st) : launch_attention_simt_forward(a, st);
 }
 
 int gshard_cross_attention_backward(const gshard_attention_config* config, const void* q, const void* k, const void* v,
@@ -143,14 +143,13 @@ int gshard_cross_attention_backward(const gshard_attention_config* config, const
   a.o = const_cast<void*>(o); a.lse = const_cast<float*>(lse); a.dout = dout; a.delta = delta;
   a.dq = dq; a.dk = dk; a.dv = dv; a.status = static_cast<int*>(workspace);
   GS_CHECK(clear_status(workspace, st));
-  const bool bf16 = c.dtype == GSHARD_BF16;
+  if (c.dtype == GSHARD_BF16) return launch_attention_umma_backward(a, delta, st);
   const long long rows = (long long)c.batch * c.q_len * c.heads;
   if (rows) {
-    if (bf16) attention_delta_kernel<__nv_bfloat16><<<grid_for_rows(rows), 256, 0, st>>>(a, delta, rows);
-    else attention_delta_kernel<float><<<grid_for_rows(rows), 256, 0, st>>>(a, delta, rows);
+    attention_delta_kernel<<<grid_for_rows(rows), 256, 0, st>>>(a, delta, rows);
     count_launch();
   }
-  return launch_attention_simt_backward(a, bf16, st);
+  return launch_attention_simt_backward(a, st);
 }
 
 }  // extern "C"

@@ -5,6 +5,7 @@
 //   dS = scale P (dout v^T - delta), dq = dS k, dk = dS^T q, dv = P^T dout; heads that share a key head add up.
 #pragma once
 #include "common.cuh"
+#include "tensor_map.cuh"
 
 namespace gshard {
 
@@ -26,11 +27,19 @@ __device__ __forceinline__ int source_length(const AttentionArgs& a, int b) {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// attention_simt.cu: CUDA cores
-int launch_attention_simt_forward(const AttentionArgs& a, bool bf16, cudaStream_t st);
-int launch_attention_simt_backward(const AttentionArgs& a, bool bf16, cudaStream_t st);
+// attention_simt.cu: fp32 on the CUDA cores
+int launch_attention_simt_forward(const AttentionArgs& a, cudaStream_t st);
+int launch_attention_simt_backward(const AttentionArgs& a, cudaStream_t st);
 
-// attention_umma.cu: bf16 on the tensor cores
+// attention_umma.cu, attention_backward.cu: bf16 on the tensor cores.  stats: attention_stats_floats() floats of scratch
 int launch_attention_umma_forward(const AttentionArgs& a, cudaStream_t st);
+size_t attention_stats_floats(int B, int Tq, int H);
+int launch_attention_umma_backward(const AttentionArgs& a, float* stats, cudaStream_t st);
+
+// Tensor map of k or v.  A batch of sources without tokens gets a valid map that nothing reads through.
+inline bool make_source_map(CUtensorMap* map, const AttentionArgs& a, const void* base, long long stride, int box_tokens) {
+  return a.Tk > 0 ? make_token_map(map, base, a.D, a.Hkv, a.Tk, a.B, stride, box_tokens)
+                  : make_token_map(map, a.q, a.D, 1, 1, 1, stride, box_tokens);
+}
 
 }  // namespace gshard

@@ -21,12 +21,12 @@ constexpr int kThreads = 256;
 template <int DP> constexpr int kPitch = DP + 4;
 
 // 64 rows from `src` (pitch `stride` elements) as floats; rows from `rows` on and columns from D on are zero
-template <typename T, int DP>
-__device__ __forceinline__ void load_tile(float* dst, const T* src, long long stride, int rows, int D) {
+template <int DP>
+__device__ __forceinline__ void load_tile(float* dst, const float* src, long long stride, int rows, int D) {
   for (int i = threadIdx.x; i < BT * DP / 4; i += kThreads) {
     const int r = i / (DP / 4), c = i % (DP / 4) * 4;
     float f[4] = {0.f, 0.f, 0.f, 0.f};
-    if (r < rows && c < D) load_pack<T, 4>(src + r * stride + c, f);
+    if (r < rows && c < D) load_pack<float, 4>(src + r * stride + c, f);
     *reinterpret_cast<float4*>(dst + r * kPitch<DP> + c) = make_float4(f[0], f[1], f[2], f[3]);
   }
 }
@@ -94,8 +94,8 @@ __device__ __forceinline__ void clear(f32x2 (*acc)[DP / 64][2]) {
 }
 
 // rows ty + 16 i below `rows` of an output tile, each times factor[i]
-template <typename T, int DP>
-__device__ __forceinline__ void store_tile(T* dst, long long stride, int rows, int D, f32x2 (*acc)[DP / 64][2], const float* factor, int tx,
+template <int DP>
+__device__ __forceinline__ void store_tile(float* dst, long long stride, int rows, int D, f32x2 (*acc)[DP / 64][2], const float* factor, int tx,
                                            int ty) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -105,7 +105,7 @@ __device__ __forceinline__ void store_tile(T* dst, long long stride, int rows, i
       if (r >= rows || col >= D) continue;
       const float2 lo = unpair(acc[i][c][0]), hi = unpair(acc[i][c][1]);
       const float f[4] = {lo.x * factor[i], lo.y * factor[i], hi.x * factor[i], hi.y * factor[i]};
-      store_pack<T, 4>(dst + r * stride + col, f);
+      store_pack<float, 4>(dst + r * stride + col, f);
     }
 }
 
@@ -116,7 +116,7 @@ __device__ __forceinline__ float over_columns(float v, F f) {       // over the 
   return v;
 }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads) attention_simt_forward_kernel(const AttentionArgs a) {
   extern __shared__ __align__(16) float smem[];
   float *sq = smem, *sk = sq + BT * kPitch<DP>, *sv = sk + BT * kPitch<DP>, *sp = sv + BT * kPitch<DP>;
@@ -124,10 +124,10 @@ __global__ void __launch_bounds__(kThreads) attention_simt_forward_kernel(const 
   const int tiles = ceil_div(a.Tq, BT);
   const int q0 = blockIdx.x % tiles * BT, h = blockIdx.x / tiles % a.H, b = blockIdx.x / tiles / a.H;
   const int kh = h / (a.H / a.Hkv), len = source_length(a, b), rows = min(BT, a.Tq - q0);
-  const T* q = static_cast<const T*>(a.q) + ((long long)b * a.Tq + q0) * a.q_stride + (long long)h * a.D;
-  const T* k = static_cast<const T*>(a.k) + (long long)b * a.Tk * a.k_stride + (long long)kh * a.D;
-  const T* v = static_cast<const T*>(a.v) + (long long)b * a.Tk * a.v_stride + (long long)kh * a.D;
-  load_tile<T, DP>(sq, q, a.q_stride, rows, a.D);
+  const float* q = static_cast<const float*>(a.q) + ((long long)b * a.Tq + q0) * a.q_stride + (long long)h * a.D;
+  const float* k = static_cast<const float*>(a.k) + (long long)b * a.Tk * a.k_stride + (long long)kh * a.D;
+  const float* v = static_cast<const float*>(a.v) + (long long)b * a.Tk * a.v_stride + (long long)kh * a.D;
+  load_tile<DP>(sq, q, a.q_stride, rows, a.D);
   f32x2 acc[4][DP / 64][2];
   clear<DP>(acc);
   float top[4], sum[4];
@@ -136,8 +136,8 @@ __global__ void __launch_bounds__(kThreads) attention_simt_forward_kernel(const 
   const float c = a.scale * kLog2e;
   for (int k0 = 0; k0 < len; k0 += BT) {
     __syncthreads();                                  // the previous tiles have been read
-    load_tile<T, DP>(sk, k + k0 * a.k_stride, a.k_stride, len - k0, a.D);
-    load_tile<T, DP>(sv, v + k0 * a.v_stride, a.v_stride, len - k0, a.D);
+    load_tile<DP>(sk, k + k0 * a.k_stride, a.k_stride, len - k0, a.D);
+    load_tile<DP>(sv, v + k0 * a.v_stride, a.v_stride, len - k0, a.D);
     __syncthreads();
     float s[4][4];
     rows_by_rows<DP>(sq, sk, s, tx, ty);
@@ -178,12 +178,12 @@ __global__ void __launch_bounds__(kThreads) attention_simt_forward_kernel(const 
     if (a.lse && tx == 0 && ty + 16 * i < rows)
       a.lse[((long long)b * a.H + h) * a.Tq + q0 + ty + 16 * i] = len ? top[i] * a.scale + logf(total) : -INFINITY;
   }
-  store_tile<T, DP>(static_cast<T*>(a.o) + (((long long)b * a.Tq + q0) * a.H + h) * a.D, (long long)a.H * a.D, rows, a.D, acc, factor, tx,
+  store_tile<DP>(static_cast<float*>(a.o) + (((long long)b * a.Tq + q0) * a.H + h) * a.D, (long long)a.H * a.D, rows, a.D, acc, factor, tx,
                     ty);
 }
 
 // dk and dv of 64 keys: the score tiles are computed key by query, over the queries of every head that shares the keys.
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const AttentionArgs a) {
   extern __shared__ __align__(16) float smem[];
   float *sk = smem, *sv = sk + BT * kPitch<DP>, *sq = sv + BT * kPitch<DP>, *sd = sq + BT * kPitch<DP>, *sp = sd + BT * kPitch<DP>;
@@ -199,16 +199,16 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const Atte
   clear<DP>(dv);
   const float c = a.scale * kLog2e;
   if (k0 < len) {
-    load_tile<T, DP>(sk, static_cast<const T*>(a.k) + koff, a.k_stride, len - k0, a.D);
-    load_tile<T, DP>(sv, static_cast<const T*>(a.v) + voff, a.v_stride, len - k0, a.D);
+    load_tile<DP>(sk, static_cast<const float*>(a.k) + koff, a.k_stride, len - k0, a.D);
+    load_tile<DP>(sv, static_cast<const float*>(a.v) + voff, a.v_stride, len - k0, a.D);
     for (int h = kh * group; h < (kh + 1) * group; ++h) {
-      const T* q = static_cast<const T*>(a.q) + (long long)b * a.Tq * a.q_stride + (long long)h * a.D;
-      const T* dout = static_cast<const T*>(a.dout) + ((long long)b * a.Tq * a.H + h) * a.D;
+      const float* q = static_cast<const float*>(a.q) + (long long)b * a.Tq * a.q_stride + (long long)h * a.D;
+      const float* dout = static_cast<const float*>(a.dout) + ((long long)b * a.Tq * a.H + h) * a.D;
       const long long row = ((long long)b * a.H + h) * a.Tq;
       for (int q0 = 0; q0 < a.Tq; q0 += BT) {
         __syncthreads();
-        load_tile<T, DP>(sq, q + q0 * a.q_stride, a.q_stride, a.Tq - q0, a.D);
-        load_tile<T, DP>(sd, dout + (long long)q0 * a.H * a.D, (long long)a.H * a.D, a.Tq - q0, a.D);
+        load_tile<DP>(sq, q + q0 * a.q_stride, a.q_stride, a.Tq - q0, a.D);
+        load_tile<DP>(sd, dout + (long long)q0 * a.H * a.D, (long long)a.H * a.D, a.Tq - q0, a.D);
         if (threadIdx.x < BT) {
           const bool in = q0 + threadIdx.x < a.Tq;                // queries behind the last one: P = exp(-inf) = 0
           slse[threadIdx.x] = in ? a.lse[row + q0 + threadIdx.x] * kLog2e : INFINITY;
@@ -239,11 +239,11 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const Atte
   }
   // keys behind the length have gradient zero: their scores were zero throughout
   const float one[4] = {1.f, 1.f, 1.f, 1.f}, scale[4] = {a.scale, a.scale, a.scale, a.scale};
-  store_tile<T, DP>(static_cast<T*>(a.dk) + koff, a.k_stride, rows, a.D, dk, scale, tx, ty);
-  store_tile<T, DP>(static_cast<T*>(a.dv) + voff, a.v_stride, rows, a.D, dv, one, tx, ty);
+  store_tile<DP>(static_cast<float*>(a.dk) + koff, a.k_stride, rows, a.D, dk, scale, tx, ty);
+  store_tile<DP>(static_cast<float*>(a.dv) + voff, a.v_stride, rows, a.D, dv, one, tx, ty);
 }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const AttentionArgs a) {
   extern __shared__ __align__(16) float smem[];
   float *sq = smem, *sd = sq + BT * kPitch<DP>, *sk = sd + BT * kPitch<DP>, *sv = sk + BT * kPitch<DP>, *sp = sv + BT * kPitch<DP>;
@@ -252,14 +252,14 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const Atten
   const int q0 = blockIdx.x % tiles * BT, h = blockIdx.x / tiles % a.H, b = blockIdx.x / tiles / a.H;
   const int kh = h / (a.H / a.Hkv), len = source_length(a, b), rows = min(BT, a.Tq - q0);
   const long long qoff = ((long long)b * a.Tq + q0) * a.q_stride + (long long)h * a.D;
-  const T* k = static_cast<const T*>(a.k) + (long long)b * a.Tk * a.k_stride + (long long)kh * a.D;
-  const T* v = static_cast<const T*>(a.v) + (long long)b * a.Tk * a.v_stride + (long long)kh * a.D;
+  const float* k = static_cast<const float*>(a.k) + (long long)b * a.Tk * a.k_stride + (long long)kh * a.D;
+  const float* v = static_cast<const float*>(a.v) + (long long)b * a.Tk * a.v_stride + (long long)kh * a.D;
   f32x2 dq[4][DP / 64][2];
   clear<DP>(dq);
   const float c = a.scale * kLog2e;
   if (len) {
-    load_tile<T, DP>(sq, static_cast<const T*>(a.q) + qoff, a.q_stride, rows, a.D);
-    load_tile<T, DP>(sd, static_cast<const T*>(a.dout) + (((long long)b * a.Tq + q0) * a.H + h) * a.D, (long long)a.H * a.D, rows, a.D);
+    load_tile<DP>(sq, static_cast<const float*>(a.q) + qoff, a.q_stride, rows, a.D);
+    load_tile<DP>(sd, static_cast<const float*>(a.dout) + (((long long)b * a.Tq + q0) * a.H + h) * a.D, (long long)a.H * a.D, rows, a.D);
     float lse[4], delta[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -269,8 +269,8 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const Atten
     }
     for (int k0 = 0; k0 < len; k0 += BT) {
       __syncthreads();
-      load_tile<T, DP>(sk, k + k0 * a.k_stride, a.k_stride, len - k0, a.D);
-      load_tile<T, DP>(sv, v + k0 * a.v_stride, a.v_stride, len - k0, a.D);
+      load_tile<DP>(sk, k + k0 * a.k_stride, a.k_stride, len - k0, a.D);
+      load_tile<DP>(sv, v + k0 * a.v_stride, a.v_stride, len - k0, a.D);
       __syncthreads();
       float s[4][4], dp[4][4];
       rows_by_rows<DP>(sq, sk, s, tx, ty);
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const Atten
     }
   }
   const float scale[4] = {a.scale, a.scale, a.scale, a.scale};
-  store_tile<T, DP>(static_cast<T*>(a.dq) + qoff, a.q_stride, rows, a.D, dq, scale, tx, ty);
+  store_tile<DP>(static_cast<float*>(a.dq) + qoff, a.q_stride, rows, a.D, dq, scale, tx, ty);
 }
 
 template <typename K>
@@ -301,29 +301,23 @@ int launch(K kernel, long long blocks, int floats, const AttentionArgs& a, cudaS
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
 }
 
-template <typename T, int DP>
+template <int DP>
 int backward(const AttentionArgs& a, cudaStream_t st) {
   const int floats = 4 * BT * kPitch<DP> + BT * PP + 2 * BT;
-  const int rc = a.Tk ? launch(attention_simt_dkv_kernel<T, DP>, (long long)ceil_div(a.Tk, BT) * a.Hkv * a.B, floats, a, st) : GSHARD_OK;
+  const int rc = a.Tk ? launch(attention_simt_dkv_kernel<DP>, (long long)ceil_div(a.Tk, BT) * a.Hkv * a.B, floats, a, st) : GSHARD_OK;
   if (rc != GSHARD_OK || !a.Tq) return rc;
-  return launch(attention_simt_dq_kernel<T, DP>, (long long)ceil_div(a.Tq, BT) * a.H * a.B, floats, a, st);
+  return launch(attention_simt_dq_kernel<DP>, (long long)ceil_div(a.Tq, BT) * a.H * a.B, floats, a, st);
 }
 
-template <typename T, int DP>
+template <int DP>
 int forward(const AttentionArgs& a, cudaStream_t st) {
-  return launch(attention_simt_forward_kernel<T, DP>, (long long)ceil_div(a.Tq, BT) * a.H * a.B, 3 * BT * kPitch<DP> + BT * PP, a, st);
+  return launch(attention_simt_forward_kernel<DP>, (long long)ceil_div(a.Tq, BT) * a.H * a.B, 3 * BT * kPitch<DP> + BT * PP, a, st);
 }
 
 }  // namespace
 
-int launch_attention_simt_forward(const AttentionArgs& a, bool bf16, cudaStream_t st) {
-  if (bf16) return a.D <= 64 ? forward<__nv_bfloat16, 64>(a, st) : forward<__nv_bfloat16, 128>(a, st);
-  return a.D <= 64 ? forward<float, 64>(a, st) : forward<float, 128>(a, st);
-}
+int launch_attention_simt_forward(const AttentionArgs& a, cudaStream_t st) { return a.D <= 64 ? forward<64>(a, st) : forward<128>(a, st); }
 
-int launch_attention_simt_backward(const AttentionArgs& a, bool bf16, cudaStream_t st) {
-  if (bf16) return a.D <= 64 ? backward<__nv_bfloat16, 64>(a, st) : backward<__nv_bfloat16, 128>(a, st);
-  return a.D <= 64 ? backward<float, 64>(a, st) : backward<float, 128>(a, st);
-}
+int launch_attention_simt_backward(const AttentionArgs& a, cudaStream_t st) { return a.D <= 64 ? backward<64>(a, st) : backward<128>(a, st); }
 
 }  // namespace gshard

@@ -19,7 +19,6 @@
 #include "attention.cuh"
 #include "pack.cuh"
 #include "sm100_ptx.cuh"
-#include "tensor_map.cuh"
 
 namespace gshard {
 
@@ -370,11 +369,8 @@ int forward(const AttentionArgs& a, cudaStream_t st) {
   p.pairs = ceil_div(p.list, 2);
   p.items = p.pairs * a.Hkv * a.B;
   CUtensorMap mq, mk, mv;
-  // a source of no tokens: the maps are not used
-  const int tokens = a.Tk > 0 ? a.Tk : 1;
-  if (!make_token_map(&mq, a.q, a.D, a.H, a.Tq, a.B, a.q_stride, kRows) ||
-      !make_token_map(&mk, a.Tk > 0 ? a.k : a.q, a.D, a.Tk > 0 ? a.Hkv : 1, tokens, a.Tk > 0 ? a.B : 1, a.k_stride, kRows) ||
-      !make_token_map(&mv, a.Tk > 0 ? a.v : a.q, a.D, a.Tk > 0 ? a.Hkv : 1, tokens, a.Tk > 0 ? a.B : 1, a.v_stride, kRows))
+  if (!make_token_map(&mq, a.q, a.D, a.H, a.Tq, a.B, a.q_stride, kRows) || !make_source_map(&mk, a, a.k, a.k_stride, kRows) ||
+      !make_source_map(&mv, a, a.v, a.v_stride, kRows))
     return GSHARD_ERR_CUDA;
   auto kernel = attention_umma_forward_kernel<DP>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<DP>::bytes) != cudaSuccess) {
