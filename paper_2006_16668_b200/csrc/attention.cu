@@ -111,8 +111,10 @@ int gshard_cross_attention_forward(const gshard_attention_config* config, const 
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   AttentionArgs a = attention_args(c, q, k, v, k_lengths);
   a.o = o; a.lse = lse; a.status = static_cast<int*>(workspace);
+  const bool bf16 = c.dtype == GSHARD_BF16;
+  if (attention_is_few(a.Tq, a.H, a.Hkv)) return launch_attention_few(a, bf16, st);
   GS_CHECK(clear_status(workspace, st));
-  return c.dtype == GSHARD_BF16 ? launch_attention_umma_forward(a, st) : launch_attention_simt_forward(a, st);
+  return bf16 ? launch_attention_umma_forward(a, st) : launch_attention_simt_forward(a, st);
 }
 
 int gshard_cross_attention_backward(const gshard_attention_config* config, const void* q, const void* k, const void* v,

@@ -27,6 +27,10 @@ __device__ __forceinline__ int source_length(const AttentionArgs& a, int b) {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// attention_few.cu: up to 8 rows (queries x heads) per key head, in one launch
+bool attention_is_few(int q_len, int heads, int kv_heads);
+int launch_attention_few(const AttentionArgs& a, bool bf16, cudaStream_t st);
+
 // attention_simt.cu: fp32 on the CUDA cores
 int launch_attention_simt_forward(const AttentionArgs& a, cudaStream_t st);
 int launch_attention_simt_backward(const AttentionArgs& a, cudaStream_t st);

@@ -10,6 +10,7 @@
 #include "linear.cuh"
 #include "pack.cuh"
 #include "plan.cuh"
+#include "umma_epilogue.cuh"
 
 namespace gshard {
 
@@ -138,14 +139,50 @@ int gated_validate(int64_t n, int32_t K, int32_t cols, int32_t dtype) {
   return linear_validate(n, K, 2 * cols, dtype, dtype);
 }
 
-struct GatedPlan { LinearPlan lin; size_t acc, total; };
+// How a forward runs.
+//   FEW      w streams through the CUDA cores in one launch (linear_few.cu): up to 4 rows, 8 of fp32, whose planes would first be
+//            written.  1024 -> 4096, bf16, us, few / tiles / project: 1 row 6.7 / 14.2 / 7.5, 4 rows 8.7 / 12.6 / 9.7, 8 rows
+//            11.0 / 12.6 / 9.8; fp32, 8 rows 12.4 / 58.8 / 14.3.
+//   TILES    one launch on CTA pairs, both factors of a tile side by side in tensor memory (umma2_gemm.cu).  One tile takes
+//            about 8.6 us + 4.3 us per 1024 of the contraction (fp32 22 + 29), so it wants enough tiles to fill the pairs.
+//   PROJECT  the product in the linear operator's forms, which cut the contraction, and the projections meet in a second launch.
+//            Better where that product is one launch (linear_mid.cu; 4096 -> 1024, bf16: 64 rows 25.9 / 10.7), or the tiles
+//            are few: 4096 -> 1024, 512 rows (16 tiles) 26.3 / 21.9, 1024 rows (32 tiles) 27.0 / 28.6; 2048 -> 2048, 512 rows (32 tiles)
+//            18.0 / 23.0; fp32: 32 tiles 81.5 / 63.1, 64 tiles 88.9 / 94.4.
+enum class GatedForm { FEW, TILES, PROJECT };
+GatedForm gated_form(int64_t n, int K, int cols, bool bf16) {
+  if (n <= (bf16 ? 4 : 8)) return GatedForm::FEW;
+  if (linear_mid_shape(n, 2 * cols, K, bf16 ? 1 : umma_epi::kPasses3, true).bn) return GatedForm::PROJECT;
+  const int64_t tiles = (n + 255) / 256 * ((cols + 127) / 128);
+  return tiles >= (bf16 ? 24 : 48) ? GatedForm::TILES : GatedForm::PROJECT;
+}
+
+struct GatedPlan {
+  GatedForm form;
+  LinearPlan lin;            // backward, PROJECT
+  size_t xp, wp, acc, total;
+};
 
 GatedPlan gated_plan(int64_t n, int K, int cols, int dtype, bool backward) {
   GatedPlan p{};
-  p.lin = linear_plan(n, K, 2 * cols, dtype, backward ? dtype : GSHARD_F32, backward);
   Carver w;
-  w.take(p.lin.total);
-  if (!backward) p.acc = w.take((size_t)n * 2 * cols * 4);
+  if (backward) {
+    p.lin = linear_plan(n, K, 2 * cols, dtype, dtype, true);
+    p.total = p.lin.total;
+    return p;
+  }
+  p.form = gated_form(n, K, cols, dtype == GSHARD_BF16);
+  if (p.form == GatedForm::PROJECT) {
+    p.lin = linear_plan(n, K, 2 * cols, dtype, GSHARD_F32, false);
+    w.take(p.lin.total);
+    p.acc = w.take((size_t)n * 2 * cols * 4);
+  } else {
+    w.take(256);             // status word
+    if (p.form == GatedForm::TILES && dtype == GSHARD_F32) {
+      p.xp = w.take((size_t)n * K * 6);
+      p.wp = w.take((size_t)K * 2 * cols * 6);
+    }
+  }
   p.total = w.off;
   return p;
 }
@@ -177,10 +214,24 @@ int gshard_gated_linear_forward(int64_t n_rows, int32_t K, int32_t cols, int32_t
   NvtxRange range("gshard.gated_linear");
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
-  float* acc = reinterpret_cast<float*>(ws + pl.acc);
-  GS_CHECK(linear_run_forward(n_rows, K, 2 * cols, dtype, GSHARD_F32, LinearEpilogue{}, x, w, acc, pl.lin, ws, st));
-  if (dtype == GSHARD_BF16) launch_value<__nv_bfloat16>(acc, h, pre, n_rows, cols, activation, st);
-  else launch_value<float>(acc, h, pre, n_rows, cols, activation, st);
+  int* status = reinterpret_cast<int*>(ws);
+  const bool bf16 = dtype == GSHARD_BF16;
+  if (pl.form == GatedForm::FEW) {
+    const LinearEpilogue lin{nullptr, nullptr, pre, activation};
+    GS_CHECK(launch_linear_few((int)n_rows, K, 2 * cols, bf16, !bf16, x, w, h, lin, status, st, true));
+  } else if (pl.form == GatedForm::TILES) {
+    GatedGemm g{x, w, h, pre, (int)n_rows, cols, K, 1, activation};
+    if (!bf16) {
+      linear_split_planes(x, ws + pl.xp, n_rows * K, w, ws + pl.wp, (long long)K * 2 * cols, st);
+      g.A = ws + pl.xp; g.B = ws + pl.wp; g.planes = 3;
+    }
+    GS_CHECK(launch_umma2_gated(g, status, st));
+  } else {
+    float* acc = reinterpret_cast<float*>(ws + pl.acc);
+    GS_CHECK(linear_run_forward(n_rows, K, 2 * cols, dtype, GSHARD_F32, LinearEpilogue{}, x, w, acc, pl.lin, ws, st));
+    if (bf16) launch_value<__nv_bfloat16>(acc, h, pre, n_rows, cols, activation, st);
+    else launch_value<float>(acc, h, pre, n_rows, cols, activation, st);
+  }
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
 }
 

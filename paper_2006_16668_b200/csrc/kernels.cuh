@@ -116,6 +116,14 @@ int launch_umma_gemm(const UmmaGemm& g, int* status, cudaStream_t st);
 // umma2_gemm.cu: the same contraction with the two-SM MMA (CTA pairs, 256 x 256 tiles).
 int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st);
 
+// The gated linear operator on CTA pairs: A [rows, K], B [K, 2 cols] (planes of them: 1, or 3 with float C and pre), C [rows, cols],
+// pre [rows, 2 cols] or nullptr.
+struct GatedGemm {
+  const void* A; const void* B; void* C; void* pre;
+  int rows, cols, K, planes, act;
+};
+int launch_umma2_gated(const GatedGemm& g, int* status, cudaStream_t st);
+
 // ffn_fused.cu: both expert GEMMs in one persistent launch; groups of four CTAs exchange 256-column
 // chunks of the hidden activations through a small L2-resident scratch ring.
 bool ffn_fused_supported(const Dims& d);

@@ -262,6 +262,12 @@ int linear_validate(int64_t n, int32_t K, int32_t cols, int32_t dtype, int32_t o
   return GSHARD_OK;
 }
 
+void linear_split_planes(const void* src0, void* dst0, long long n0, const void* src1, void* dst1, long long n1, cudaStream_t st) {
+  linear_split_kernel<<<stride_grid((n0 + n1) / 8), 256, 0, st>>>(static_cast<const float*>(src0), static_cast<__nv_bfloat16*>(dst0), n0 / 8,
+                                                                  static_cast<const float*>(src1), static_cast<__nv_bfloat16*>(dst1), n1 / 8);
+  count_launch();
+}
+
 namespace {
 
 // the tensor-core GEMMs, whose operands are bf16 (or planes of it)
@@ -270,12 +276,6 @@ Dims linear_dims(int K, int cols) {
   one.G = 1; one.S = 1; one.C = 1; one.E = 2; one.M = K; one.H = cols; one.dtype = GSHARD_BF16;
   return make_dims(one);
 }
-void split_planes(const void* src0, void* dst0, long long n0, const void* src1, void* dst1, long long n1, cudaStream_t st) {
-  linear_split_kernel<<<stride_grid((n0 + n1) / 8), 256, 0, st>>>(static_cast<const float*>(src0), static_cast<__nv_bfloat16*>(dst0), n0 / 8,
-                                                                  static_cast<const float*>(src1), static_cast<__nv_bfloat16*>(dst1), n1 / 8);
-  count_launch();
-}
-
 // C = A . B: in one launch of linear_mid.cu, or cut into `splits` runs through the fp32 partial products in `join`
 int gemm_joined(const Dims& d, UmmaGemm g, MidShape mid, int splits, float* join, int* status, cudaStream_t st) {
   const LinearEpilogue none{};
@@ -317,7 +317,7 @@ int linear_run_forward(int64_t n_rows, int K, int cols, int dtype, int out_dtype
   g.clear_status = 1;
   g.a_stream = 1; g.prefer_two_sm = 1; g.out_f32 = out_f32;
   if (dtype == GSHARD_F32) {
-    split_planes(x, ws + pl.xp, n_rows * K, w, ws + pl.wp, (long long)K * cols, st);
+    linear_split_planes(x, ws + pl.xp, n_rows * K, w, ws + pl.wp, (long long)K * cols, st);
     g.A = ws + pl.xp; g.B = ws + pl.wp; g.planes_a = g.planes_b = 3; g.a_bs = n_rows * K; g.b_bs = (long long)K * cols; g.a_stream = 0;
   }
   if (pl.mid.bn) return launch_linear_mid(g, lin, pl.mid, true, status, st);
@@ -345,7 +345,7 @@ int linear_run_gradients(int64_t n_rows, int K, int cols, bool fp32, int planes,
   const Dims d = linear_dims(K, cols);
   float* join = reinterpret_cast<float*>(ws + pl.join);
   if (fp32 && (dx || dw))
-    split_planes(w, ws + pl.wp, dx ? (long long)K * cols : 0, x, ws + pl.xp, dw ? n_rows * K : 0, st);
+    linear_split_planes(w, ws + pl.wp, dx ? (long long)K * cols : 0, x, ws + pl.xp, dw ? n_rows * K : 0, st);
   if (dx) {                                       // [n, K] = dpre [n, cols] . w^T, both contiguous along cols
     UmmaGemm g{};
     g.A = dpre; g.B = w; g.C = dx; g.rows = (int)n_rows; g.cols = K; g.K = cols; g.batch = 1;

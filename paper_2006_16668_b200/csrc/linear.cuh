@@ -6,9 +6,10 @@
 
 namespace gshard {
 
-// linear_few.cu: the whole operator in one launch for up to 8 rows; also clears the status word.
+// linear_few.cu: the whole operator in one launch for up to 8 rows; also clears the status word.  gated: the gated linear operator
+// with cols columns of w, cols / 2 of y (typed like x).
 int launch_linear_few(int n, int K, int cols, bool bf16, bool out_f32, const void* x, const void* w, void* y,
-                      const LinearEpilogue& lin, int* status, cudaStream_t st);
+                      const LinearEpilogue& lin, int* status, cudaStream_t st, bool gated = false);
 
 // linear_mid.cu: a product whose output tiles run at once, with the operator's epilogue, in one launch (operands
 // as in UmmaGemm: bf16 output with at most two planes together, fp32 output with one or three each).  bn == 0: too many tiles, or too deep for them.
@@ -25,6 +26,8 @@ struct LinearPlan {
 
 LinearPlan linear_plan(int64_t n, int K, int cols, int dtype, int out_dtype, bool backward);
 int linear_validate(int64_t n, int32_t K, int32_t cols, int32_t dtype, int32_t out_dtype);
+// Three bf16 planes of one or two fp32 tensors (the second may have no elements), one behind the other.
+void linear_split_planes(const void* src0, void* dst0, long long n0, const void* src1, void* dst1, long long n1, cudaStream_t st);
 // y = act(x . w + bias) + residual on checked arguments.
 int linear_run_forward(int64_t n_rows, int K, int cols, int dtype, int out_dtype, const LinearEpilogue& lin, const void* x,
                        const void* w, void* y, const LinearPlan& pl, unsigned char* ws, cudaStream_t st);
@@ -62,6 +65,21 @@ __device__ __forceinline__ void linear_epilogue4(const LinearEpilogue& lin, void
     for (int j = 0; j < 4; ++j) f[j] += r[j];
   }
   store_pack<TY, 4>(static_cast<TY*>(y) + off, f);
+}
+
+// The gated linear operator's epilogue on four neighbouring sums of both factors, column `col` of row `row` of h [n, cols].
+template <typename TY>
+__device__ __forceinline__ void gated_epilogue4(const LinearEpilogue& lin, void* h, long long row, int cols, int col, float4 gate, float4 up) {
+  const float g[4] = {gate.x, gate.y, gate.z, gate.w}, u[4] = {up.x, up.y, up.z, up.w};
+  if (lin.pre) {
+    TY* pre = static_cast<TY*>(lin.pre) + row * 2 * cols + col;
+    store_pack<TY, 4>(pre, g);
+    store_pack<TY, 4>(pre + cols, u);
+  }
+  float f[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f[j] = (sizeof(TY) == 2 ? activation_value_fast(g[j], lin.act) : activation_value(g[j], lin.act)) * u[j];
+  store_pack<TY, 4>(static_cast<TY*>(h) + row * cols + col, f);
 }
 
 }  // namespace gshard

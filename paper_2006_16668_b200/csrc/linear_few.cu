@@ -37,7 +37,9 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
   return v;
 }
 
-template <typename T, typename TY, int N, int LC>
+// GATED: w holds the gate's columns and then the other factor's; the first half of a block's columns are gate columns, the second half
+// the same columns of the other factor, and lin.act(gate) times that is the result.
+template <typename T, typename TY, int N, int LC, bool GATED>
 __global__ void __launch_bounds__(kFewThreads, 2) linear_few_kernel(const FewArgs a) {
   constexpr int W = 16 / (int)sizeof(T);            // columns per thread
   constexpr int CT = LC * W;                        // columns per block
@@ -48,7 +50,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) linear_few_kernel(const FewArg
   __shared__ __align__(16) float sums[N][CT];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int splits = gridDim.y, rank = blockIdx.y;  // the cluster spans grid.y
-  const int col = blockIdx.x * CT + lane % LC * W;
+  const int half_cols = a.cols / 2;
+  const int lc = lane % LC;
+  const int col = !GATED ? blockIdx.x * CT + lc * W : (lc < LC / 2 ? 0 : half_cols) + blockIdx.x * (CT / 2) + lc % (LC / 2) * W;
   const int k_row = warp * RW + lane / LC;
   const int k0 = rank * a.run, k1 = min(a.K, k0 + a.run);
   if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) *a.status = 0;
@@ -59,7 +63,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) linear_few_kernel(const FewArg
   for (int r = 0; r < N; ++r)
 #pragma unroll
     for (int j = 0; j < W; ++j) acc[r][j] = 0.f;
-  const bool in = col < a.cols;
+  const bool in = !GATED ? col < a.cols : blockIdx.x * (CT / 2) + lc % (LC / 2) * W < half_cols;
   for (int kc = k0; kc < k1; kc += kFewChunk) {
     const int len = min(kFewChunk, k1 - kc);
     // the chunk's first rows of w are on their way before x is staged
@@ -131,26 +135,30 @@ __global__ void __launch_bounds__(kFewThreads, 2) linear_few_kernel(const FewArg
   if (splits > 1) ptx::cluster_sync_all();
   else __syncthreads();
   // every block of the cluster finishes its share of the outputs, four columns at a time
-  for (int i = rank * kFewThreads + tid; i < N * CT / 4; i += splits * kFewThreads) {
-    const int r = i / (CT / 4), c = i % (CT / 4) * 4;
-    const int out_col = blockIdx.x * CT + c;
-    if (r >= a.n || out_col >= a.cols) continue;
+  auto total = [&](int r, int c) {
+    if (splits == 1) return *reinterpret_cast<const float4*>(&sums[r][c]);
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (splits == 1) {
-      s = *reinterpret_cast<const float4*>(&sums[r][c]);
-    } else {
-      const uint32_t at = ptx::smem_u32(&sums[r][c]);
-      for (int k = 0; k < splits; ++k) {
-        const float4 v = ld_cluster(ptx::map_to_cta(at, k));
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-      }
+    const uint32_t at = ptx::smem_u32(&sums[r][c]);
+    for (int k = 0; k < splits; ++k) {
+      const float4 v = ld_cluster(ptx::map_to_cta(at, k));
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
-    linear_epilogue4<TY>(a.lin, a.y, (long long)r * a.cols + out_col, out_col, s);
+    return s;
+  };
+  constexpr int CO = GATED ? CT / 2 : CT;
+  const int out_cols = GATED ? half_cols : a.cols;
+  for (int i = rank * kFewThreads + tid; i < N * CO / 4; i += splits * kFewThreads) {
+    const int r = i / (CO / 4), c = i % (CO / 4) * 4;
+    const int out_col = blockIdx.x * CO + c;
+    if (r >= a.n || out_col >= out_cols) continue;
+    const float4 s = total(r, c);
+    if constexpr (GATED) gated_epilogue4<TY>(a.lin, a.y, r, half_cols, out_col, s, total(r, CO + c));
+    else linear_epilogue4<TY>(a.lin, a.y, (long long)r * a.cols + out_col, out_col, s);
   }
   if (splits > 1) ptx::cluster_sync_all();           // no block leaves while another may still read its sums
 }
 
-template <typename T, typename TY, int N, int LC>
+template <typename T, typename TY, int N, int LC, bool GATED>
 int launch_few_t(const FewArgs& a, int blocks, int splits, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(blocks, splits, 1);
@@ -163,38 +171,39 @@ int launch_few_t(const FewArgs& a, int blocks, int splits, cudaStream_t st) {
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = splits > 1 ? 1 : 0;
-  if (cudaLaunchKernelEx(&cfg, linear_few_kernel<T, TY, N, LC>, a) != cudaSuccess) { cudaGetLastError(); return GSHARD_ERR_CUDA; }
+  if (cudaLaunchKernelEx(&cfg, linear_few_kernel<T, TY, N, LC, GATED>, a) != cudaSuccess) { cudaGetLastError(); return GSHARD_ERR_CUDA; }
   count_launch();
   return GSHARD_OK;
 }
 
-template <typename T, typename TY, int N>
+template <typename T, typename TY, int N, bool GATED>
 int launch_few_n(const FewArgs& a, int lc, int splits, cudaStream_t st) {
   const int blocks = ceil_div(a.cols, lc * 16 / (int)sizeof(T));
-  return lc == 8 ? launch_few_t<T, TY, N, 8>(a, blocks, splits, st) : launch_few_t<T, TY, N, 4>(a, blocks, splits, st);
+  return lc == 8 ? launch_few_t<T, TY, N, 8, GATED>(a, blocks, splits, st) : launch_few_t<T, TY, N, 4, GATED>(a, blocks, splits, st);
 }
 
-template <typename T, typename TY>
+template <typename T, typename TY, bool GATED>
 int launch_few(const FewArgs& a, int lc, int splits, cudaStream_t st) {
-  if (a.n == 1) return launch_few_n<T, TY, 1>(a, lc, splits, st);
-  if (a.n == 2) return launch_few_n<T, TY, 2>(a, lc, splits, st);
-  if (a.n <= 4) return launch_few_n<T, TY, 4>(a, lc, splits, st);
-  return launch_few_n<T, TY, 8>(a, lc, splits, st);
+  if (a.n == 1) return launch_few_n<T, TY, 1, GATED>(a, lc, splits, st);
+  if (a.n == 2) return launch_few_n<T, TY, 2, GATED>(a, lc, splits, st);
+  if (a.n <= 4) return launch_few_n<T, TY, 4, GATED>(a, lc, splits, st);
+  return launch_few_n<T, TY, 8, GATED>(a, lc, splits, st);
 }
 
 }  // namespace
 
 int launch_linear_few(int n, int K, int cols, bool bf16, bool out_f32, const void* x, const void* w, void* y,
-                      const LinearEpilogue& lin, int* status, cudaStream_t st) {
+                      const LinearEpilogue& lin, int* status, cudaStream_t st, bool gated) {
   const int wide = ceil_div(cols, bf16 ? 64 : 32), room = 2 * 148;
   const int lc = 2 * wide <= room ? 4 : 8;
   const int blocks = lc == 4 ? 2 * wide : wide;
   int splits = 1;
   while (splits < 8 && 2 * blocks * splits <= room && K / (2 * splits) >= 128) splits *= 2;
   FewArgs a{x, w, y, lin, status, n, K, cols, ceil_div(ceil_div(K, splits), 32) * 32};
-  if (bf16) return out_f32 ? launch_few<__nv_bfloat16, float>(a, lc, splits, st)
-                           : launch_few<__nv_bfloat16, __nv_bfloat16>(a, lc, splits, st);
-  return launch_few<float, float>(a, lc, splits, st);
+  if (gated) return bf16 ? launch_few<__nv_bfloat16, __nv_bfloat16, true>(a, lc, splits, st) : launch_few<float, float, true>(a, lc, splits, st);
+  if (bf16) return out_f32 ? launch_few<__nv_bfloat16, float, false>(a, lc, splits, st)
+                           : launch_few<__nv_bfloat16, __nv_bfloat16, false>(a, lc, splits, st);
+  return launch_few<float, float, false>(a, lc, splits, st);
 }
 
 }  // namespace gshard

@@ -48,16 +48,14 @@ inline bool make_map(CUtensorMap* map, const void* base, long long inner, long l
   return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess && encode();
 }
 
-// 4-D bf16 tensor map {head_dim, heads, tokens, batch} of a [batch, tokens, heads, head_dim] tensor whose tokens lie `stride`
-// elements apart, with boxes of 64 head dimensions by `box_tokens` tokens of one head, 128-byte swizzle; outside reads as zero.
-inline bool make_token_map(CUtensorMap* map, const void* base, int head_dim, int heads, long long tokens, long long batch, long long stride,
-                           int box_tokens) {
+// 4-D bf16 tensor map, 128-byte swizzle, strides (of the outer dimensions) in elements; outside reads as zero.
+inline bool make_map_4d(CUtensorMap* map, const void* base, const long long* dims_, const long long* strides_, const int* box_) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
-  cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)batch};
-  cuuint64_t strides[3] = {(cuuint64_t)head_dim * 2, (cuuint64_t)stride * 2, (cuuint64_t)(tokens * stride) * 2};
-  cuuint32_t box[4] = {64, 1, (cuuint32_t)box_tokens, 1};
-  cuuint32_t estr[4] = {1, 1, 1, 1};
+  cuuint64_t dims[4], strides[3];
+  cuuint32_t box[4], estr[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 4; ++i) { dims[i] = (cuuint64_t)dims_[i]; box[i] = (cuuint32_t)box_[i]; }
+  for (int i = 0; i < 3; ++i) strides[i] = (cuuint64_t)strides_[i] * 2;
   auto encode = [&] {
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -65,6 +63,23 @@ inline bool make_token_map(CUtensorMap* map, const void* base, int head_dim, int
   if (encode()) return true;
   int device = 0;                              // a thread without a current context, as above
   return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess && encode();
+}
+
+// 4-D bf16 tensor map {cols, 2, K, planes} of `planes` matrices [K, 2 cols], one behind the other, with boxes of 64 columns of one half by
+// 64 rows, 128-byte swizzle.
+inline bool make_gated_map(CUtensorMap* map, const void* base, long long cols, long long K, int planes) {
+  const long long dims[4] = {cols, 2, K, planes}, strides[3] = {cols, 2 * cols, 2 * cols * K};
+  const int box[4] = {64, 1, 64, 1};
+  return make_map_4d(map, base, dims, strides, box);
+}
+
+// 4-D bf16 tensor map {head_dim, heads, tokens, batch} of a [batch, tokens, heads, head_dim] tensor whose tokens lie `stride`
+// elements apart, with boxes of 64 head dimensions by `box_tokens` tokens of one head, 128-byte swizzle; outside reads as zero.
+inline bool make_token_map(CUtensorMap* map, const void* base, int head_dim, int heads, long long tokens, long long batch, long long stride,
+                           int box_tokens) {
+  const long long dims[4] = {head_dim, heads, tokens, batch}, strides[3] = {head_dim, stride, tokens * stride};
+  const int box[4] = {64, 1, box_tokens, 1};
+  return make_map_4d(map, base, dims, strides, box);
 }
 
 // Tensor map of an output matrix batch C [batch][rows][cols] (row pitch c_ld, batch pitch c_bs elements)

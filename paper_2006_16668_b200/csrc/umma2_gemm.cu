@@ -24,6 +24,8 @@
 // the row tiles of that column block.
 #include <cuda.h>
 
+#include <algorithm>
+
 #include "kernels.cuh"
 #include "sm100_ptx.cuh"
 #include "tensor_map.cuh"
@@ -85,7 +87,9 @@ __device__ __forceinline__ TileCoord decode(const Params2& p, int tile) {
 
 // LIN: the linear operator's epilogue (map_pre: tensor map of the kept pre-activations).  RUNS: accumulated run by
 // run into the epilogue warps' registers (umma_epilogue.cuh), with fp32 operands in three planes each.
-template <bool A_K, bool B_K, bool MASK, bool LIN = false, bool RUNS = false>
+// GATED: the gated linear operator; B's tile is 128 columns of the gate (leader) and the same columns of the other factor (peer),
+// through a 4-D map {cols, factor, K, plane}; t.nt counts 128 columns of C.
+template <bool A_K, bool B_K, bool MASK, bool LIN = false, bool RUNS = false, bool GATED = false>
 __global__ void __launch_bounds__(kThreads, 1)
 umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                   const __grid_constant__ CUtensorMap map_c, const __grid_constant__ CUtensorMap map_pre, const Params2 p) {
@@ -158,7 +162,8 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
           } else {
 #pragma unroll
             for (int j = 0; j < BNH / 64; ++j)
-              ptx::tma_load_3d_pair(sb + j * kBoxBytes, &map_b, bar, col0 + j * 64, k0, obb, pol_b);
+              if (GATED) ptx::tma_load_4d_pair(sb + j * kBoxBytes, &map_b, bar, t.nt * BNH + j * 64, (int)rank, k0, obb, pol_b);
+              else ptx::tma_load_3d_pair(sb + j * kBoxBytes, &map_b, bar, col0 + j * 64, k0, obb, pol_b);
           }
           if (++kb == p.k_blocks) { kb = 0; ++pass; }
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
@@ -220,19 +225,26 @@ umma2_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         for (int run = 0; run < runs; ++run) {
           if (!ptx::mbar_wait_warp(acc_full + acc, acc_phase, abort_flag, lane)) { ok = false; break; }
           ptx::tc_fence_after_sync();
-          add_run<BN>(sums, tmem_base + (uint32_t)(acc * BN), q, half, run == 0);
+          add_run<BN, GATED>(sums, tmem_base + (uint32_t)(acc * BN), q, half, run == 0);
           ptx::tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive_remote_relaxed(ptx::map_to_cta(ptx::smem_u32(acc_empty + acc), 0));
           if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         }
         if (!ok) break;
-        epilogue_linear_sums<BN>(p, &map_c, &map_pre, t, tile_row0, sums, q, half, stg, lane);
+        if constexpr (GATED) {
+          const int gcol0 = t.nt * BNH + half * 64;
+          if (gcol0 < p.cols) gated_round<true>(p, &map_c, &map_pre, tile_row0 + q * 32, gcol0, sums, sums + 2, stg, lane);
+        } else {
+          epilogue_linear_sums<BN>(p, &map_c, &map_pre, t, tile_row0, sums, q, half, stg, lane);
+        }
         continue;
       }
       if (!ptx::mbar_wait_warp(acc_full + acc, acc_phase, abort_flag, lane)) { ok = false; break; }
       ptx::tc_fence_after_sync();
-      if constexpr (LIN)
+      if constexpr (GATED)
+        epilogue_gated_tile<BN>(p, &map_c, &map_pre, t, tile_row0, tmem_base + (uint32_t)(acc * BN), q, half, stg, lane);
+      else if constexpr (LIN)
         epilogue_linear_tile<BN>(p, &map_c, &map_pre, t, tile_row0, tmem_base + (uint32_t)(acc * BN), q, half, stg, lane);
       else
         epilogue_tile<BN, MASK>(p, p.tma_store ? &map_c : nullptr, t, tile_row0, tmem_base + (uint32_t)(acc * BN), q, half,
@@ -481,10 +493,10 @@ int launch2_resident_b(const CUtensorMap& ma, const CUtensorMap& mb, const CUten
   return GSHARD_OK;
 }
 
-template <bool A_K, bool B_K, bool MASK, bool LIN = false, bool RUNS = false>
+template <bool A_K, bool B_K, bool MASK, bool LIN = false, bool RUNS = false, bool GATED = false>
 int launch2_t(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const Params2& p, int pairs,
               cudaStream_t st, const CUtensorMap* mp = nullptr) {
-  auto kern = umma2_gemm_kernel<A_K, B_K, MASK, LIN, RUNS>;
+  auto kern = umma2_gemm_kernel<A_K, B_K, MASK, LIN, RUNS, GATED>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
     return GSHARD_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
@@ -579,6 +591,34 @@ int launch_umma2_gemm(const UmmaGemm& g, int* status, cudaStream_t st) {
   if (!g.a_kmajor && g.b_kmajor) return GSHARD_DISPATCH2(false, true);
   return GSHARD_DISPATCH2(false, false);
 #undef GSHARD_DISPATCH2
+}
+
+// The gated linear operator on pairs: C = act(A . B[:, :cols]) (A . B[:, cols:]) with 256 x 128 tiles of C.
+int launch_umma2_gated(const GatedGemm& g, int* status, cudaStream_t st) {
+  const bool planes3 = g.planes == 3;
+  const int esize = planes3 ? 4 : 2;
+  CUtensorMap ma, mb, mc, mp;
+  if (!make_map(&ma, g.A, g.K, g.rows, g.planes, g.K, (long long)g.rows * g.K, BK, BM) ||
+      !make_gated_map(&mb, g.B, g.cols, g.K, g.planes) || !make_store_map(&mc, g.C, g.cols, g.rows, 1, g.cols, 0, esize))
+    return GSHARD_ERR_CUDA;
+  if (!g.pre) mp = mc;
+  else if (!make_store_map(&mp, g.pre, g.cols, g.rows, 2, 2ll * g.cols, g.cols, esize)) return GSHARD_ERR_CUDA;
+  Params2 p{};
+  p.C = g.C; p.rows = g.rows; p.cols = g.cols; p.K = g.K; p.batch = 1;
+  p.m_tiles = ceil_div(g.rows, 2 * BM); p.n_tiles = ceil_div(g.cols, BNH);
+  p.total_tiles = p.m_tiles * p.n_tiles;
+  p.k_blocks = ceil_div(g.K, BK);
+  p.passes = planes3 ? kPasses3 : 1;
+  p.pass_a = planes3 ? kPassA3 : 0;
+  p.pass_b = planes3 ? kPassB3 : 0;
+  p.out_f32 = planes3; p.a_stream = 0; p.b_stream = 0;
+  p.n_fastest = g.rows > 2 * g.cols ? 1 : 0;
+  p.status = status; p.clear_status = 1;
+  p.tma_store = 1;
+  p.lin.pre = g.pre; p.lin.act = g.act;
+  const int pairs = std::min(device_sms() / 2, p.total_tiles);
+  return planes3 ? launch2_t<true, false, false, true, true, true>(ma, mb, mc, p, pairs, st, &mp)
+                 : launch2_t<true, false, false, true, false, true>(ma, mb, mc, p, pairs, st, &mp);
 }
 
 }  // namespace gshard

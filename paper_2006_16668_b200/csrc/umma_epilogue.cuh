@@ -308,13 +308,14 @@ __device__ __forceinline__ void epilogue_linear_tile(const P& p, const CUtensorM
 }
 
 // sums (+)= this warp's share of a finished run: 32 rows x BN / 2 columns, one row per lane, as fp32 bits.
-template <int BN>
+// GATED: a quarter of the columns of either factor instead.
+template <int BN, bool GATED = false>
 __device__ __forceinline__ void add_run(uint32_t (*sums)[32], uint32_t tmem_acc, int q, int half, bool first) {
-  const uint32_t t_acc = tmem_acc + (uint32_t)(half * (BN / 2)) + ((uint32_t)(q * 32) << 16);
+  const uint32_t t_acc = tmem_acc + (uint32_t)(half * (GATED ? BN / 4 : BN / 2)) + ((uint32_t)(q * 32) << 16);
 #pragma unroll
   for (int c = 0; c < BN / 32; ++c) {              // 16 columns at a time: the sums take most of the registers
     uint32_t r[16];
-    ptx::tmem_ld_32x16(t_acc + (uint32_t)(c * 16), r);
+    ptx::tmem_ld_32x16(t_acc + (uint32_t)(c * 16 + (GATED && c >= BN / 64 ? BN / 4 : 0)), r);
     ptx::tmem_ld_wait();
     uint32_t* s = &sums[c / 2][c % 2 * 16];
 #pragma unroll
@@ -330,6 +331,58 @@ __device__ __forceinline__ void epilogue_linear_sums(const P& p, const CUtensorM
     const int col0 = round_col0<BN>(t, half, c);
     if (col0 < p.cols) linear_round<false, true>(p, map_c, map_pre, t.b, tile_row0 + q * 32, col0, sums + 2 * c, stg, lane);
   }
+}
+
+// The gated linear operator's epilogue: the accumulator's first half of columns are gate columns, its second half the
+// same columns of the other factor; h = act(gate) up, and both factors themselves where the caller keeps them (map_pre: batch 0
+// the gates, 1 the other factors).  A round is 64 columns of a warp's 32 rows.
+template <bool F32, typename P>
+__device__ __forceinline__ void gated_round(const P& p, const CUtensorMap* map_c, const CUtensorMap* map_pre, int row0, int col0,
+                                            uint32_t (*g)[32], uint32_t (*u)[32], unsigned char* stg, int lane) {
+  unsigned char* srow = stg + lane * kStgRowBytes;
+  struct Plain { int relu, out_f32; } plain{0, F32};
+  auto put = [&](uint32_t (*r)[32], const CUtensorMap* map, int b) {       // 64 columns through the staging rows
+    store_wait(lane);                            // the previous bulk store has read them
+    process_chunk<false>(r[0], plain, srow, lane, 0, 0);
+    if (F32) {
+      flush_rows_tma(stg, map, b, row0, col0, lane);
+      store_wait(lane);
+      process_chunk<false>(r[1], plain, srow, lane, 0, 0);
+      if (col0 + 32 < p.cols) flush_rows_tma(stg, map, b, row0, col0 + 32, lane);
+    } else {
+      process_chunk<false>(r[1], plain, srow, lane, 4, 0);
+      flush_rows_tma(stg, map, b, row0, col0, lane);
+    }
+  };
+  if (p.lin.pre) {
+    put(g, map_pre, 0);
+    put(u, map_pre, 1);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    activate<32, !F32>(g[h], p.lin.act);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) g[h][i] = __float_as_uint(__uint_as_float(g[h][i]) * __uint_as_float(u[h][i]));
+  }
+  put(g, map_c, 0);
+}
+
+// One epilogue warp's share of a finished tile: column half `half` of both factors.
+template <int BN, typename P>
+__device__ __forceinline__ void epilogue_gated_tile(const P& p, const CUtensorMap* map_c, const CUtensorMap* map_pre, const TileCoord& t,
+                                                    int tile_row0, uint32_t tmem_acc, int q, int half, unsigned char* stg, int lane) {
+  const int col0 = t.nt * (BN / 2) + half * (BN / 4);
+  static_assert(BN / 4 == 64, "one round per warp");
+  if (col0 >= p.cols) return;                    // uniform over the warp
+  const uint32_t t_acc = tmem_acc + (uint32_t)(half * (BN / 4)) + ((uint32_t)(q * 32) << 16);
+  uint32_t g[2][32], u[2][32];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    ptx::tmem_ld_32x32(t_acc + h * 32, g[h]);
+    ptx::tmem_ld_32x32(t_acc + BN / 2 + h * 32, u[h]);
+  }
+  ptx::tmem_ld_wait();
+  gated_round<false>(p, map_c, map_pre, tile_row0 + q * 32, col0, g, u, stg, lane);
 }
 
 // After a warp's last tile: its bulk stores have left shared memory and reached global memory.
