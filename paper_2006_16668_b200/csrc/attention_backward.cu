@@ -87,26 +87,35 @@ __device__ __forceinline__ void load_rows(unsigned char* dst, const CUtensorMap*
   for (int j = 0; j < DP / 64; ++j) ptx::tma_load_4d(dst + j * (kRows * 128), map, bar, j * 64, h, t, b, policy);
 }
 
+// The two products, called by one elected thread.  (Branches on elect.sync, not on the lane: the compiler then knows that one
+// thread issues; with lane 0 an MMA took about 170 cycles to issue instead of its 64 in the tensor core.  The same thread is
+// elected every time.)
 // D = A B^T of two tiles in shared memory (rows by rows, along the head dimension)
 template <int DP>
 __device__ __forceinline__ void mma_rows(uint32_t d, const unsigned char* a, const unsigned char* b) {
   constexpr uint32_t idesc = ptx::make_idesc_bf16(kRows, kRows, false, false);
-  const uint32_t sa = ptx::smem_u32(a), sb = ptx::smem_u32(b);
+  const uint64_t da = ptx::make_smem_desc(ptx::smem_u32(a), 16, 1024), db = ptx::make_smem_desc(ptx::smem_u32(b), 16, 1024);
 #pragma unroll
   for (int k = 0; k < DP / 16; ++k) {
-    const uint32_t off = (uint32_t)(k / 4 * (kRows * 128) + k % 4 * 32);
-    ptx::umma_bf16(d, ptx::make_smem_desc(sa + off, 16, 1024), ptx::make_smem_desc(sb + off, 16, 1024), idesc, k != 0 ? 1u : 0u);
+    const uint64_t off = (uint64_t)(k / 4 * (kRows * 128) + k % 4 * 32) >> 4;
+    ptx::umma_bf16(d, da + off, db + off, idesc, k != 0 ? 1u : 0u);
   }
 }
-// D (+)= A B: A is 128 x (16 steps) bf16 in tensor memory, its second 64 columns `gap` tensor-memory columns behind the first;
+// D (+)= A B: A is 128 x (16 steps) bf16 in tensor memory, its second 64 columns 64 tensor-memory columns behind the first;
 // B a tile in shared memory whose rows are the contraction
 template <int DP>
-__device__ __forceinline__ void mma_weights(uint32_t d, uint32_t a, uint32_t gap, const unsigned char* b, int steps, bool add) {
+__device__ __forceinline__ void mma_weights(uint32_t d, uint32_t a, const unsigned char* b, int steps, bool add) {
   constexpr uint32_t idesc = ptx::make_idesc_bf16(kRows, DP, false, true);
-  const uint32_t sb = ptx::smem_u32(b);
-  for (int k = 0; k < steps; ++k)
-    ptx::umma_bf16_ta(d, a + (k >> 2) * gap + (k & 3) * 8, ptx::make_smem_desc(sb + k * 2048, kRows * 128, 1024), idesc,
-                      add || k != 0 ? 1u : 0u);
+  const uint64_t db = ptx::make_smem_desc(ptx::smem_u32(b), kRows * 128, 1024);
+  auto step = [&](int k) {
+    ptx::umma_bf16_ta(d, a + (k >> 2) * 64 + (k & 3) * 8, db + (uint64_t)(k * 2048 >> 4), idesc, add || k != 0 ? 1u : 0u);
+  };
+  if (steps == kRows / 16) {
+#pragma unroll
+    for (int k = 0; k < kRows / 16; ++k) step(k);
+  } else {
+    for (int k = 0; k < steps; ++k) step(k);
+  }
 }
 
 __device__ __forceinline__ uint32_t pack2(float x, float y) {
@@ -224,44 +233,48 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
       }
     } else if (warp == 9) {
-      // ------------------------------ MMA issuer ---------------------------------------------------
-      if (lane == 0) {
-        auto wait = [&](uint64_t* bar, uint32_t parity) {
-          if (ok && !ptx::mbar_wait(bar, parity, abort_flag)) ok = false;
-          ptx::tc_fence_after_sync();
-          return ok;
-        };
-        int stage = 0, ahead = 0;             // of query tile i, and of the tile whose scores are computed next
-        uint32_t ahead_phase = 0;
-        auto step = [&](int& s) { return ++s == kStages ? (s = 0, true) : false; };
-        if (wait(kv_full, 0) && wait(full, 0)) {
-          mma_rows<DP>(t_s, sk, ring);
-          ptx::umma_commit(s_full);
-          mma_rows<DP>(t_dp, sv, ring + L::tile);
-          ptx::umma_commit(dp_full);
-        }
-        if (step(ahead)) ahead_phase ^= 1u;
-        for (int i = 0; i < n && ok; ++i) {
-          const unsigned char *q = ring + stage * L::stage, *d = q + L::tile;
-          const unsigned char *q1 = ring + ahead * L::stage, *d1 = q1 + L::tile;
-          if (!wait(p_full, i & 1)) break;
-          mma_weights<DP>(t_dv, t_s, 64, d, 8, i != 0);
-          if (i + 1 < n) {
-            if (!wait(full + ahead, ahead_phase)) break;
+      // ------------------------------ MMA issuer (whole warp waits, one thread issues) --------------
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (ok && !__all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag))) ok = false;
+        ptx::tc_fence_after_sync();
+        return ok;
+      };
+      int stage = 0, ahead = 0;               // of query tile i, and of the tile whose scores are computed next
+      uint32_t ahead_phase = 0;
+      auto step = [&](int& s) { return ++s == kStages ? (s = 0, true) : false; };
+      if (wait(kv_full, 0) && wait(full, 0) && ptx::elect_one()) {
+        mma_rows<DP>(t_s, sk, ring);
+        ptx::umma_commit(s_full);
+        mma_rows<DP>(t_dp, sv, ring + L::tile);
+        ptx::umma_commit(dp_full);
+      }
+      if (step(ahead)) ahead_phase ^= 1u;
+      for (int i = 0; i < n && ok; ++i) {
+        const unsigned char *q = ring + stage * L::stage, *d = q + L::tile;
+        const unsigned char *q1 = ring + ahead * L::stage, *d1 = q1 + L::tile;
+        const bool more = i + 1 < n;
+        if (!wait(p_full, i & 1)) break;
+        if (ptx::elect_one()) mma_weights<DP>(t_dv, t_s, d, kRows / 16, i != 0);
+        if (more) {
+          if (!wait(full + ahead, ahead_phase)) break;
+          if (ptx::elect_one()) {
             mma_rows<DP>(t_s, sk, q1);
             ptx::umma_commit(s_full);
           }
-          if (!wait(ds_full, i & 1)) break;
-          mma_weights<DP>(t_dk, t_dp, 64, q, 8, i != 0);
+        }
+        if (!wait(ds_full, i & 1)) break;
+        if (ptx::elect_one()) {
+          mma_weights<DP>(t_dk, t_dp, q, kRows / 16, i != 0);
           ptx::umma_commit(empty + stage);
-          if (i + 1 < n) {
+          if (more) {
             mma_rows<DP>(t_dp, sv, d1);
             ptx::umma_commit(dp_full);
+          } else {
+            ptx::umma_commit(o_full);
           }
-          step(stage);
-          if (step(ahead)) ahead_phase ^= 1u;
         }
-        ptx::umma_commit(o_full);
+        step(stage);
+        if (step(ahead)) ahead_phase ^= 1u;
       }
     }
   } else {
@@ -441,7 +454,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         }
       }
     } else if (warp == 9) {
-      // ------------------------------ MMA issuer (whole warp waits, lane 0 issues) ------------------
+      // ------------------------------ MMA issuer (whole warp waits, one thread issues) ------------------
       int ks = 0, vs = 0, ds = 0;             // ring positions of the next S, the next dP and the next dq
       uint32_t k_phase = 0, v_phase = 0, q_phase = 0, ds_phase = 0;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -458,7 +471,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           unsigned char* k = sk + ks * L::tile;
           const int left = len - j * kRows;
           if (left < kRows && (left & 15) && len < p.a.Tk) zero_rows<DP>(k, left, (left + 15) & ~15, lane);
-          if (lane == 0) {
+          if (ptx::elect_one()) {
             mma_rows<DP>(tmem + (j & 1) * kRows, sq, k);
             ptx::umma_commit(s_full + (j & 1));
           }
@@ -466,7 +479,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         };
         auto grads = [&](int j) {             // dP of block j
           if (!wait(v_full + vs, v_phase)) return;
-          if (lane == 0) {
+          if (ptx::elect_one()) {
             mma_rows<DP>(t_dp, sd, sv + vs * L::tile);
             ptx::umma_commit(dp_full);
             ptx::umma_commit(v_empty + vs);
@@ -486,8 +499,8 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           const int steps = min(kRows, (len - j * kRows + 15) & ~15) / 16;
           if (j + 1 < blocks) grads(j + 1);     // first: the threads are about to wait for it
           if (!ok) break;
-          if (lane == 0) {
-            mma_weights<DP>(t_dq, tmem + (j & 1) * kRows, 64, sk + ds * L::tile, steps, j != 0);
+          if (ptx::elect_one()) {
+            mma_weights<DP>(t_dq, tmem + (j & 1) * kRows, sk + ds * L::tile, steps, j != 0);
             ptx::umma_commit(k_empty + ds);
             if (j == blocks - 1) ptx::umma_commit(o_full);
           }

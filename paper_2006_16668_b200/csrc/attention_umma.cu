@@ -157,7 +157,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         }
       }
     } else if (warp == 9) {
-      // ------------------------------ MMA issuer (whole warp waits, lane 0 issues) ------------------
+      // ------------------------------ MMA issuer (whole warp waits, one thread issues) ------------------
       constexpr uint32_t idesc_s = ptx::make_idesc_bf16(kRows, kRows, false, false);
       constexpr uint32_t idesc_o = ptx::make_idesc_bf16(kRows, DP, false, true);
       int stage = 0; uint32_t phase = 0;
@@ -168,15 +168,17 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         return ok;
       };
       auto next = [&] { if (++stage == kStages) { stage = 0; phase ^= 1u; } };
+      // Branches on elect.sync, not on the lane: the compiler then knows that one thread issues (with lane 0 an MMA took about
+      // 170 cycles to issue instead of its 64 in the tensor core).  The same thread is elected every time.
       // scores of tile `half` against the keys in the ring's stage
       auto scores = [&](int half) {
-        if (lane) return;
-        const uint32_t sq = ptx::smem_u32(smem + half * L::tile), sk = ptx::smem_u32(ring + stage * L::tile);
-  #pragma unroll
+        if (!ptx::elect_one()) return;
+        const uint64_t dq = ptx::make_smem_desc(ptx::smem_u32(smem + half * L::tile), 16, 1024);
+        const uint64_t dk = ptx::make_smem_desc(ptx::smem_u32(ring + stage * L::tile), 16, 1024);
+#pragma unroll
         for (int k = 0; k < DP / 16; ++k) {
-          const uint32_t off = (uint32_t)(k / 4 * (kRows * 128) + k % 4 * 32);
-          ptx::umma_bf16(tmem + half * kRows, ptx::make_smem_desc(sq + off, 16, 1024), ptx::make_smem_desc(sk + off, 16, 1024), idesc_s,
-                         k != 0 ? 1u : 0u);
+          const uint64_t off = (uint64_t)(k / 4 * (kRows * 128) + k % 4 * 32) >> 4;
+          ptx::umma_bf16(tmem + half * kRows, dq + off, dk + off, idesc_s, k != 0 ? 1u : 0u);
         }
         ptx::umma_commit(s_full + half);
       };
@@ -189,10 +191,10 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
           q_phase[half] ^= 1u;
           if (half == 0 && !wait(kv_full + stage, phase)) break;
           scores(half);
-          if (blocks == 1 && lane == 0) ptx::umma_commit(q_empty + half);
+          if (blocks == 1 && ptx::elect_one()) ptx::umma_commit(q_empty + half);
         }
         if (!ok) break;
-        if (lane == 0) ptx::umma_commit(kv_empty + stage);
+        if (ptx::elect_one()) ptx::umma_commit(kv_empty + stage);
         next();
         for (int j = 0; j < blocks && ok; ++j) {
           const int left = t.len - j * kRows;
@@ -213,18 +215,23 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
           for (int half = 0; half < t.tiles; ++half) {
             if (!wait(p_full + half, p_phase[half])) break;
             p_phase[half] ^= 1u;
-            if (lane == 0) {
-              const uint32_t b0 = ptx::smem_u32(sv);
-              for (int k = 0; k < steps; ++k)
-                ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, ptx::make_smem_desc(b0 + k * 2048, kRows * 128, 1024), idesc_o,
-                                  (j | k) != 0 ? 1u : 0u);
+            if (ptx::elect_one()) {
+              const uint64_t dv = ptx::make_smem_desc(ptx::smem_u32(sv), kRows * 128, 1024);
+              if (steps == kRows / 16) {
+#pragma unroll
+                for (int k = 0; k < kRows / 16; ++k)
+                  ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, dv + (uint64_t)(k * 2048 >> 4), idesc_o, (j | k) != 0 ? 1u : 0u);
+              } else {
+                for (int k = 0; k < steps; ++k)
+                  ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, dv + (uint64_t)(k * 2048 >> 4), idesc_o, (j | k) != 0 ? 1u : 0u);
+              }
               if (half == t.tiles - 1) ptx::umma_commit(kv_empty + v_stage);
               if (j == blocks - 1) ptx::umma_commit(o_full + half);
             }
             if (j + 1 < blocks) {
               if (half == 0 && !wait(kv_full + stage, phase)) break;
               scores(half);
-              if (lane == 0) {
+              if (ptx::elect_one()) {
                 if (j + 2 == blocks) ptx::umma_commit(q_empty + half);
                 if (half == t.tiles - 1) ptx::umma_commit(kv_empty + stage);
               }
