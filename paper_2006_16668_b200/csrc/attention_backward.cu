@@ -94,11 +94,11 @@ __device__ __forceinline__ void load_rows(unsigned char* dst, const CUtensorMap*
 template <int DP>
 __device__ __forceinline__ void mma_rows(uint32_t d, const unsigned char* a, const unsigned char* b) {
   constexpr uint32_t idesc = ptx::make_idesc_bf16(kRows, kRows, false, false);
-  const uint64_t da = ptx::make_smem_desc(ptx::smem_u32(a), 16, 1024), db = ptx::make_smem_desc(ptx::smem_u32(b), 16, 1024);
+  const uint32_t da = ptx::smem_desc_low(a, 16), db = ptx::smem_desc_low(b, 16);
 #pragma unroll
   for (int k = 0; k < DP / 16; ++k) {
-    const uint64_t off = (uint64_t)(k / 4 * (kRows * 128) + k % 4 * 32) >> 4;
-    ptx::umma_bf16(d, da + off, db + off, idesc, k != 0 ? 1u : 0u);
+    const uint32_t off = (uint32_t)(k / 4 * (kRows * 128) + k % 4 * 32) >> 4;
+    ptx::umma_bf16_low(d, da + off, db + off, idesc, k != 0 ? 1u : 0u);
   }
 }
 // D (+)= A B: A is 128 x (16 steps) bf16 in tensor memory, its second 64 columns 64 tensor-memory columns behind the first;
@@ -106,9 +106,9 @@ __device__ __forceinline__ void mma_rows(uint32_t d, const unsigned char* a, con
 template <int DP>
 __device__ __forceinline__ void mma_weights(uint32_t d, uint32_t a, const unsigned char* b, int steps, bool add) {
   constexpr uint32_t idesc = ptx::make_idesc_bf16(kRows, DP, false, true);
-  const uint64_t db = ptx::make_smem_desc(ptx::smem_u32(b), kRows * 128, 1024);
+  const uint32_t db = ptx::smem_desc_low(b, kRows * 128);
   auto step = [&](int k) {
-    ptx::umma_bf16_ta(d, a + (k >> 2) * 64 + (k & 3) * 8, db + (uint64_t)(k * 2048 >> 4), idesc, add || k != 0 ? 1u : 0u);
+    ptx::umma_bf16_ta(d, a + (k >> 2) * 64 + (k & 3) * 8, db + (uint32_t)(k * 2048 >> 4), idesc, add || k != 0 ? 1u : 0u);
   };
   if (steps == kRows / 16) {
 #pragma unroll

@@ -10,7 +10,9 @@
 //   "scores complete" of block j+1 also says that PV of block j is complete, so that O may be rescaled.
 // O is rescaled only when a row's maximum has grown by more than 2^8 since the last time (the weights then stay below
 // 2^8, and their sums far from overflow); that is rare after the first blocks.
-// Persistent grid, one CTA per multiprocessor; while a tile's rows are written out, the next tile's scores are computed.
+// Persistent grid, one CTA per multiprocessor, and the stream of products does not stop between two items: the scores of the
+// next item follow the last block's, and a fourth warpgroup takes the finished output from tensor memory, divides it by its sums
+// and sends it off through shared memory (bulk tensor stores) while the next item's first block is being worked on.
 //
 // Rows behind the source's length: scores are masked before the maximum; rows of V that hold something else are zeroed in
 // shared memory up to the next multiple of 16, where the last block's product ends.
@@ -25,16 +27,18 @@ namespace gshard {
 namespace {
 
 constexpr int kRows = 128;                    // query rows of a tile, keys of a block
-constexpr int kThreads = 384;                 // 2 x 4 softmax warps; TMA, MMA and two idle warps
-// registers per thread: 168 at launch, moved to where the scores live (2 x 128 x 216 + 128 x 72 = 384 x 168)
-constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+constexpr int kThreads = 512;                 // 2 x 4 softmax warps; 4 output warps; TMA, MMA and two idle warps
+// registers per thread: 128 at launch, moved to where the scores live (128 x (2 x 184 + 80 + 64) = 512 x 128)
+constexpr int kSoftmaxRegs = 184, kOutputRegs = 80, kOtherRegs = 64;
 constexpr float kSlack = 8.f;                 // growth of a row's maximum (powers of two) that O is not rescaled for
 
 template <int DP> struct Layout {
   static constexpr int tile = kRows * DP * 2;
   static constexpr int stages = DP == 128 ? 4 : 6;
   static constexpr int kv_off = 2 * tile;
-  static constexpr int bar_off = kv_off + stages * tile;
+  static constexpr int out_off = kv_off + stages * tile;      // 32 rows x 128 bytes per output warp
+  static constexpr int stat_off = out_off + 4 * 32 * 128;      // sum and maximum of every row of both tiles
+  static constexpr int bar_off = stat_off + 2 * 2 * kRows * 4;
   static constexpr int bytes = bar_off + 256 + 1024;
   static_assert(bytes <= 232448, "shared memory budget");
 };
@@ -80,12 +84,13 @@ __device__ __forceinline__ float exp2_approx(float x) {
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                              const __grid_constant__ CUtensorMap map_v, const ForwardParams p) {
+                              const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const ForwardParams p) {
   using L = Layout<DP>;
   constexpr int kStages = L::stages;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   unsigned char* ring = smem + L::kv_off;
+  float* stat = reinterpret_cast<float*>(smem + L::stat_off);     // [tile][sum, maximum][row]
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bar_off);
   uint64_t* kv_full = bars;                   // [kStages]
   uint64_t* kv_empty = kv_full + kStages;     // [kStages]
@@ -94,7 +99,9 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
   uint64_t* s_full = q_empty + 2;             // [2] scores complete
   uint64_t* p_full = s_full + 2;              // [2] weights written (4 warps)
   uint64_t* o_full = p_full + 2;              // [2] output complete
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 2);
+  uint64_t* o_empty = o_full + 2;             // [2] output and statistics read (4 warps)
+  uint64_t* stat_full = o_empty + 2;          // [2] statistics written (4 warps)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(stat_full + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -102,15 +109,17 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
     for (int s = 0; s < kStages; ++s) { ptx::mbar_init(kv_full + s, 1); ptx::mbar_init(kv_empty + s, 1); }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(q_full + i, 1); ptx::mbar_init(q_empty + i, 1);
-      ptx::mbar_init(s_full + i, 1); ptx::mbar_init(p_full + i, 4); ptx::mbar_init(o_full + i, 1);
+      ptx::mbar_init(s_full + i, 1); ptx::mbar_init(p_full + i, 4);
+      ptx::mbar_init(o_full + i, 1); ptx::mbar_init(o_empty + i, 4); ptx::mbar_init(stat_full + i, 4);
     }
     *abort_flag = 0;
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&map_q);
     ptx::prefetch_tensormap(&map_k);
     ptx::prefetch_tensormap(&map_v);
+    ptx::prefetch_tensormap(&map_o);
   }
-  if (warp == 9) {
+  if (warp == 13) {
     ptx::tmem_alloc(tmem_slot, 512);
     ptx::tmem_relinquish();
   }
@@ -121,9 +130,17 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
   const uint32_t tmem_o = tmem + 256;
 
   bool ok = true;
-  if (warp >= 8) {
+  // the next item from i on whose source has keys
+  auto with_keys = [&](int i, Item& t) {
+    for (; i < p.items; i += gridDim.x) {
+      t = item_of(p, i);
+      if (t.len > 0) break;
+    }
+    return i;
+  };
+  if (warp >= 12) {
     ptx::registers_down<kOtherRegs>();
-    if (warp == 8) {
+    if (warp == 12) {
       // ------------------------------ TMA producer -----------------------------------------------
       if (lane == 0) {
         const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_last();
@@ -132,20 +149,19 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         auto load = [&](const CUtensorMap* map, int kh, int k0, int b) {
           if (!ptx::mbar_wait(kv_empty + stage, phase ^ 1u, abort_flag)) { ok = false; return; }
           ptx::mbar_arrive_expect_tx(kv_full + stage, L::tile);
-  #pragma unroll
+#pragma unroll
           for (int j = 0; j < DP / 64; ++j)
             ptx::tma_load_4d(ring + stage * L::tile + j * (kRows * 128), map, kv_full + stage, j * 64, kh, k0, b, again);
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         };
-        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-          const Item t = item_of(p, i);
-          if (t.len == 0) continue;
+        Item t;
+        for (int i = with_keys(blockIdx.x, t); i < p.items && ok; i = with_keys(i + gridDim.x, t)) {
           for (int half = 0; half < t.tiles && ok; ++half) {
             const Tile q = tile_of(p, t, half);
             if (!ptx::mbar_wait(q_empty + half, q_phase[half] ^ 1u, abort_flag)) { ok = false; break; }
             q_phase[half] ^= 1u;
             ptx::mbar_arrive_expect_tx(q_full + half, L::tile);
-  #pragma unroll
+#pragma unroll
             for (int j = 0; j < DP / 64; ++j)
               ptx::tma_load_4d(smem + half * L::tile + j * (kRows * 128), &map_q, q_full + half, j * 64, q.h, q.q0, t.b, once);
             if (half == 0) load(&map_k, t.kh, 0, t.b);
@@ -156,49 +172,51 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
           }
         }
       }
-    } else if (warp == 9) {
-      // ------------------------------ MMA issuer (whole warp waits, one thread issues) ------------------
+    } else if (warp == 13) {
+      // ------------------------------ MMA issuer (whole warp waits, one thread issues) ---------------
       constexpr uint32_t idesc_s = ptx::make_idesc_bf16(kRows, kRows, false, false);
       constexpr uint32_t idesc_o = ptx::make_idesc_bf16(kRows, DP, false, true);
       int stage = 0; uint32_t phase = 0;
-      uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+      uint32_t q_phase = 0, p_phase = 0, o_phase = 0;           // bit `half`
       auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok && !__all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag))) ok = false;
+        if (ok && !__all_sync(0xffffffffu, ptx::mbar_wait(bar, parity & 1u, abort_flag))) ok = false;
         ptx::tc_fence_after_sync();
         return ok;
       };
-      auto next = [&] { if (++stage == kStages) { stage = 0; phase ^= 1u; } };
+      auto next_stage = [&] { if (++stage == kStages) { stage = 0; phase ^= 1u; } };
       // Branches on elect.sync, not on the lane: the compiler then knows that one thread issues (with lane 0 an MMA took about
       // 170 cycles to issue instead of its 64 in the tensor core).  The same thread is elected every time.
-      // scores of tile `half` against the keys in the ring's stage
-      auto scores = [&](int half) {
+      // Scores of tile `half` against the keys in the ring's stage; `fresh`: the first of an item; `last`: the item's last; `release`:
+      // the last use of these keys.
+      auto scores = [&](int half, bool fresh, bool last, bool release) {
+        if (fresh) {
+          if (!wait(q_full + half, q_phase >> half)) return;
+          q_phase ^= 1u << half;
+        }
         if (!ptx::elect_one()) return;
-        const uint64_t dq = ptx::make_smem_desc(ptx::smem_u32(smem + half * L::tile), 16, 1024);
-        const uint64_t dk = ptx::make_smem_desc(ptx::smem_u32(ring + stage * L::tile), 16, 1024);
+        const uint32_t dq = ptx::smem_desc_low(smem + half * L::tile, 16), dk = ptx::smem_desc_low(ring + stage * L::tile, 16);
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k) {
-          const uint64_t off = (uint64_t)(k / 4 * (kRows * 128) + k % 4 * 32) >> 4;
-          ptx::umma_bf16(tmem + half * kRows, dq + off, dk + off, idesc_s, k != 0 ? 1u : 0u);
+          const uint32_t off = (uint32_t)(k / 4 * (kRows * 128) + k % 4 * 32) >> 4;
+          ptx::umma_bf16_low(tmem + half * kRows, dq + off, dk + off, idesc_s, k != 0 ? 1u : 0u);
         }
         ptx::umma_commit(s_full + half);
+        if (last) ptx::umma_commit(q_empty + half);
+        if (release) ptx::umma_commit(kv_empty + stage);
       };
-      for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-        const Item t = item_of(p, i);
-        if (t.len == 0) continue;
+      Item t, n;
+      int i = with_keys(blockIdx.x, t);
+      if (i < p.items && wait(kv_full + stage, phase)) {
+        for (int half = 0; half < t.tiles && ok; ++half) scores(half, true, t.len <= kRows, half == t.tiles - 1);
+        next_stage();
+      }
+      while (i < p.items && ok) {
+        const int ni = with_keys(i + gridDim.x, n);
+        const bool more = ni < p.items;
         const int blocks = ceil_div(t.len, kRows);
-        for (int half = 0; half < t.tiles; ++half) {
-          if (!wait(q_full + half, q_phase[half])) break;
-          q_phase[half] ^= 1u;
-          if (half == 0 && !wait(kv_full + stage, phase)) break;
-          scores(half);
-          if (blocks == 1 && ptx::elect_one()) ptx::umma_commit(q_empty + half);
-        }
-        if (!ok) break;
-        if (ptx::elect_one()) ptx::umma_commit(kv_empty + stage);
-        next();
         for (int j = 0; j < blocks && ok; ++j) {
           const int left = t.len - j * kRows;
-          const int steps = min(kRows, (left + 15) & ~15) / 16;        // 16 keys each
+          const int steps = min(kRows, (left + 15) & ~15) / 16;      // 16 keys each
           if (!wait(kv_full + stage, phase)) break;
           const int v_stage = stage;
           unsigned char* sv = ring + v_stage * L::tile;
@@ -211,62 +229,127 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
             ptx::fence_proxy_async();
             __syncwarp();
           }
-          next();
-          for (int half = 0; half < t.tiles; ++half) {
-            if (!wait(p_full + half, p_phase[half])) break;
-            p_phase[half] ^= 1u;
-            if (ptx::elect_one()) {
-              const uint64_t dv = ptx::make_smem_desc(ptx::smem_u32(sv), kRows * 128, 1024);
-              if (steps == kRows / 16) {
-#pragma unroll
-                for (int k = 0; k < kRows / 16; ++k)
-                  ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, dv + (uint64_t)(k * 2048 >> 4), idesc_o, (j | k) != 0 ? 1u : 0u);
-              } else {
-                for (int k = 0; k < steps; ++k)
-                  ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, dv + (uint64_t)(k * 2048 >> 4), idesc_o, (j | k) != 0 ? 1u : 0u);
+          next_stage();
+          // the scores that follow: the next block's, or the next item's first
+          const bool inner = j + 1 < blocks, ahead = inner || more;
+          const int s_tiles = inner ? t.tiles : more ? n.tiles : 0;
+          const bool s_last = inner ? j + 2 == blocks : n.len <= kRows;
+          for (int half = 0; half < 2 && ok; ++half) {
+            if (half < t.tiles) {
+              if (!wait(p_full + half, p_phase >> half)) break;
+              p_phase ^= 1u << half;
+              if (j == 0) {                          // the output before this one has left tensor memory
+                if (!wait(o_empty + half, (o_phase >> half) ^ 1u)) break;
+                o_phase ^= 1u << half;
               }
-              if (half == t.tiles - 1) ptx::umma_commit(kv_empty + v_stage);
-              if (j == blocks - 1) ptx::umma_commit(o_full + half);
-            }
-            if (j + 1 < blocks) {
-              if (half == 0 && !wait(kv_full + stage, phase)) break;
-              scores(half);
               if (ptx::elect_one()) {
-                if (j + 2 == blocks) ptx::umma_commit(q_empty + half);
-                if (half == t.tiles - 1) ptx::umma_commit(kv_empty + stage);
+                const uint32_t dv = ptx::smem_desc_low(sv, kRows * 128);
+                if (steps == kRows / 16) {
+#pragma unroll
+                  for (int k = 0; k < kRows / 16; ++k)
+                    ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, dv + (uint32_t)(k * 2048 >> 4), idesc_o, (j | k) != 0 ? 1u : 0u);
+                } else {
+                  for (int k = 0; k < steps; ++k)
+                    ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, dv + (uint32_t)(k * 2048 >> 4), idesc_o, (j | k) != 0 ? 1u : 0u);
+                }
+                if (half == t.tiles - 1) ptx::umma_commit(kv_empty + v_stage);
+                if (j == blocks - 1) ptx::umma_commit(o_full + half);
               }
+            }
+            if (half < s_tiles) {
+              if (half == 0 && !wait(kv_full + stage, phase)) break;
+              scores(half, !inner, s_last, half == s_tiles - 1);
             }
           }
-          if (j + 1 < blocks) next();
+          if (ahead) next_stage();
+        }
+        t = n;
+        i = ni;
+      }
+    }
+  } else if (warp >= 8) {
+    // ------------------------------ output: one thread per row ---------------------------------------
+    ptx::registers_down<kOutputRegs>();
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    unsigned char* stage = smem + L::out_off + (warp & 3) * 32 * 128;
+    unsigned char* srow = stage + lane * 128;
+    uint32_t phase = 0;                        // bit `half`
+    for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+      const Item t = item_of(p, i);
+      for (int half = 0; half < t.tiles && ok; ++half) {
+        const Tile q = tile_of(p, t, half);
+        const int r = (warp & 3) * 32 + lane;
+        float* lse = p.a.lse && r < q.rows ? p.a.lse + ((long long)t.b * p.a.H + q.h) * p.a.Tq + q.q0 + r : nullptr;
+        float factor = 0.f;
+        if (t.len > 0) {
+          bool here = ptx::mbar_wait(stat_full + half, (phase >> half) & 1u, abort_flag) &&
+                      ptx::mbar_wait(o_full + half, (phase >> half) & 1u, abort_flag);
+          if (!__all_sync(0xffffffffu, here)) { ok = false; break; }
+          phase ^= 1u << half;
+          ptx::tc_fence_after_sync();
+          const float sum = stat[half * 2 * kRows + r], top = stat[half * 2 * kRows + kRows + r];
+          factor = 1.f / sum;
+          if (lse) *lse = top * p.a.scale + logf(sum);
+        } else if (lse) {
+          *lse = -INFINITY;
+        }
+        // 64 columns at a time through the warp's staging rows
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c) {
+          uint32_t w[32];
+#pragma unroll
+          for (int x = 0; x < 32; ++x) w[x] = 0;
+          if (t.len > 0) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              uint32_t o[32];
+              ptx::tmem_ld_32x32(tmem_o + half * DP + c * 64 + y * 32 + lanes, o);
+              ptx::tmem_ld_wait();
+#pragma unroll
+              for (int x = 0; x < 16; ++x) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(o[2 * x]) * factor, __uint_as_float(o[2 * x + 1]) * factor);
+                w[y * 16 + x] = *reinterpret_cast<const uint32_t*>(&b);
+              }
+            }
+            if (c == DP / 64 - 1) {
+              ptx::tc_fence_before_sync();
+              __syncwarp();
+              if (lane == 0) ptx::mbar_arrive(o_empty + half);
+            }
+          }
+          if (lane == 0) ptx::tma_store_wait_read();            // the store before has read the staging rows
+          __syncwarp();
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            *reinterpret_cast<uint4*>(srow + ((x ^ (lane & 7)) * 16)) = make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]);
+          ptx::fence_proxy_async();
+          __syncwarp();
+          const int row0 = q.q0 + (warp & 3) * 32;
+          if (lane == 0 && row0 < p.a.Tq && c * 64 < p.a.D) {
+            ptx::tma_store_4d(&map_o, stage, c * 64, q.h, row0, t.b);
+            ptx::tma_store_commit();
+          }
         }
       }
     }
+    if (lane == 0) ptx::tma_store_wait_all();
   } else {
     // ------------------------------ softmax: one thread per row ----------------------------------
     ptx::registers_up<kSoftmaxRegs>();
     const int half = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + half * kRows + lanes, t_o = tmem_o + half * DP + lanes;
-    const int r = threadIdx.x & 127;
     const float c = p.a.scale * kLog2e;
     uint32_t s_phase = 0, o_phase = 0;
     for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-      const Item t = item_of(p, i);
-      if (half >= t.tiles) continue;
-      const Tile q = tile_of(p, t, half);
-      const bool in = r < q.rows;
-      const long long token = (long long)t.b * p.a.Tq + q.q0 + r;
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.a.o) + (token * p.a.H + q.h) * p.a.D;
-      float* lse = p.a.lse ? p.a.lse + ((long long)t.b * p.a.H + q.h) * p.a.Tq + q.q0 + r : nullptr;
-      if (t.len == 0) {
-        if (in) {
-          for (int d = 0; d < p.a.D; d += 8) *reinterpret_cast<uint4*>(out + d) = make_uint4(0, 0, 0, 0);
-          if (lse) *lse = -INFINITY;
-        }
-        continue;
+      int len;
+      {
+        const Item t = item_of(p, i);
+        len = half < t.tiles ? t.len : 0;
       }
+      if (len == 0) continue;
       float top = -INFINITY, sum = 0.f;        // the maximum that the weights so far refer to, and their sum
-      for (int k0 = 0; k0 < t.len; k0 += kRows) {
+      for (int k0 = 0; k0 < len; k0 += kRows) {
         if (!__all_sync(0xffffffffu, ptx::mbar_wait(s_full + half, s_phase, abort_flag))) { ok = false; break; }
         s_phase ^= 1u;
         ptx::tc_fence_after_sync();
@@ -274,7 +357,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
 #pragma unroll
         for (int j = 0; j < 4; ++j) ptx::tmem_ld_32x32(t_s + j * 32, s + j * 32);
         ptx::tmem_ld_wait();
-        const int left = t.len - k0;
+        const int left = len - k0;
         if (left < kRows) {
 #pragma unroll
           for (int j = 0; j < kRows; ++j)
@@ -327,27 +410,14 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         if (lane == 0) ptx::mbar_arrive(p_full + half);
       }
       if (!ok) break;
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(o_full + half, o_phase, abort_flag))) { ok = false; break; }
+      // the statistics of the item before have been read together with its output
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(o_empty + half, o_phase ^ 1u, abort_flag))) { ok = false; break; }
       o_phase ^= 1u;
-      ptx::tc_fence_after_sync();
-      const float factor = 1.f / sum;
-#pragma unroll
-      for (int j = 0; j < DP / 32; ++j) {
-        uint32_t o[32];
-        ptx::tmem_ld_32x32(t_o + j * 32, o);
-        ptx::tmem_ld_wait();
-        if (in) {
-#pragma unroll
-          for (int d = 0; d < 32; d += 8) {
-            float f[8];
-#pragma unroll
-            for (int x = 0; x < 8; ++x) f[x] = __uint_as_float(o[d + x]) * factor;
-            if (j * 32 + d < p.a.D) store_pack<__nv_bfloat16, 8>(out + j * 32 + d, f);
-          }
-        }
-      }
-      if (lse && in) *lse = top * p.a.scale + logf(sum);
-      ptx::tc_fence_before_sync();
+      const int r = threadIdx.x & 127;
+      stat[half * 2 * kRows + r] = sum;
+      stat[half * 2 * kRows + kRows + r] = top;
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(stat_full + half);
     }
   }
 
@@ -361,7 +431,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
   __syncwarp();
   ptx::tc_fence_before_sync();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == 13) {
     ptx::tc_fence_after_sync();
     ptx::tmem_dealloc(tmem, 512);
   }
@@ -375,16 +445,16 @@ int forward(const AttentionArgs& a, cudaStream_t st) {
   p.list = p.q_tiles * (a.H / a.Hkv);
   p.pairs = ceil_div(p.list, 2);
   p.items = p.pairs * a.Hkv * a.B;
-  CUtensorMap mq, mk, mv;
+  CUtensorMap mq, mk, mv, mo;
   if (!make_token_map(&mq, a.q, a.D, a.H, a.Tq, a.B, a.q_stride, kRows) || !make_source_map(&mk, a, a.k, a.k_stride, kRows) ||
-      !make_source_map(&mv, a, a.v, a.v_stride, kRows))
+      !make_source_map(&mv, a, a.v, a.v_stride, kRows) || !make_token_map(&mo, a.o, a.D, a.H, a.Tq, a.B, (long long)a.H * a.D, 32))
     return GSHARD_ERR_CUDA;
   auto kernel = attention_umma_forward_kernel<DP>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<DP>::bytes) != cudaSuccess) {
     cudaGetLastError();
     return GSHARD_ERR_CUDA;
   }
-  kernel<<<std::min(p.items, device_sms()), kThreads, Layout<DP>::bytes, st>>>(mq, mk, mv, p);
+  kernel<<<std::min(p.items, device_sms()), kThreads, Layout<DP>::bytes, st>>>(mq, mk, mv, mo, p);
   count_launch();
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
 }
