@@ -33,32 +33,40 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
-// stats[b, h, tile][0]: lse log2(e), [1]: delta; one warp per row
-__global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArgs a, float* stats, int q_tiles, long long rows) {
-  const int lane = threadIdx.x & 31;
-  for (long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += (long long)gridDim.x * 8) {
-    const int i = (int)(r % kRows);
-    const long long tile = r / kRows;
-    const int t = (int)(tile % q_tiles) * kRows + i;
-    const long long head = tile / q_tiles;            // b * H + h
-    float lse = INFINITY, delta = 0.f;
-    if (t < a.Tq) {
-      const long long at = ((head / a.H * a.Tq + t) * a.H + head % a.H) * a.D;
-      const int c = lane * 4;
-      if (c < a.D) {
-        float x[4], y[4];
-        load_pack<__nv_bfloat16, 4>(static_cast<const __nv_bfloat16*>(a.o) + at + c, x);
-        load_pack<__nv_bfloat16, 4>(static_cast<const __nv_bfloat16*>(a.dout) + at + c, y);
+// stats[b, h, tile][0]: lse log2(e), [1]: delta.  A block takes 64 (query, head) rows of a tile, 16 lanes a row and four rows of
+// a group in flight; neighbouring rows are the heads of a token, which lie together in o and dout.
+constexpr int kStatRows = 64;
+__global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArgs a, float* stats, int q_tiles) {
+  constexpr int U = kStatRows / 16;
+  const int part = threadIdx.x & 15, grp = threadIdx.x >> 4, c = part * 8;
+  const int parts = ceil_div(kRows * a.H, kStatRows);
+  const long long tile = blockIdx.x / parts;            // b * q_tiles + tile of the sequence
+  const int b = (int)(tile / q_tiles), t0 = (int)(tile % q_tiles) * kRows;
+  const int r0 = (int)(blockIdx.x % parts) * kStatRows + grp;
+  Pack<__nv_bfloat16, 8> x[U], y[U];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) delta = fmaf(x[j], y[j], delta);
-      }
-#pragma unroll
-      for (int off = 16; off; off >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, off);
-      lse = a.lse[head * a.Tq + t] * kLog2e;
+  for (int u = 0; u < U; ++u) {
+    const int r = r0 + u * 16, t = t0 + r / a.H, h = r % a.H;
+    x[u].raw = y[u].raw = make_uint4(0, 0, 0, 0);
+    if (r < kRows * a.H && t < a.Tq && c < a.D) {
+      const long long off = (((long long)b * a.Tq + t) * a.H + h) * a.D + c;
+      x[u].load_once(static_cast<const __nv_bfloat16*>(a.o) + off);
+      y[u].load_once(static_cast<const __nv_bfloat16*>(a.dout) + off);
     }
-    if (lane == 0) {
-      stats[tile * 2 * kRows + i] = lse;
-      stats[tile * 2 * kRows + kRows + i] = delta;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int r = r0 + u * 16, t = t0 + r / a.H, h = r % a.H;
+    float delta = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) delta = fmaf(x[u].get(j), y[u].get(j), delta);
+#pragma unroll
+    for (int off = 8; off; off >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, off);
+    if (part == 0 && r < kRows * a.H) {
+      const long long head = (long long)b * a.H + h;
+      float* out = stats + (head * q_tiles + t0 / kRows) * (2 * kRows) + r / a.H;
+      out[0] = t < a.Tq ? a.lse[head * a.Tq + t] * kLog2e : INFINITY;
+      out[kRows] = delta;
     }
   }
 }
@@ -609,9 +617,8 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   p.q_tiles = ceil_div(a.Tq, kRows);
   p.k_tiles = ceil_div(a.Tk, kRows);
   p.items = p.q_tiles * a.H * a.B;
-  const long long rows = (long long)p.items * kRows;
-  if (rows) {
-    attention_stats_kernel<<<grid_for_rows(rows), 256, 0, st>>>(a, stats, p.q_tiles, rows);
+  if (p.items) {
+    attention_stats_kernel<<<(unsigned)((long long)a.B * p.q_tiles * ceil_div(kRows * a.H, kStatRows)), 256, 0, st>>>(a, stats, p.q_tiles);
     count_launch();
   }
   CUtensorMap m[4] = {};

@@ -31,6 +31,18 @@ template <int N> struct GradTable {
   int n;
 };
 
+// Elements that p lies behind a 16-byte boundary.
+template <typename T>
+__host__ __device__ __forceinline__ int skew(const T* p) { return (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T)); }
+
+// A tensor's chunks are cut at 16-byte boundaries of its memory, so that single elements occur at its ends only.
+struct Range { long long begin, end; };
+template <typename T>
+__device__ __forceinline__ Range range_of(const T* p, int chunk, long long count) {
+  const long long at = (long long)chunk * kChunk - skew(p);
+  return {max(0ll, at), min(count, at + kChunk)};
+}
+
 // the tensor that owns a chunk
 template <int N>
 __device__ __forceinline__ int owner_of(const GradTable<N>& t, int chunk) {
@@ -68,11 +80,11 @@ template <typename T, typename FP, typename FE>
 __device__ __forceinline__ void walk(const T* p, const void* other, long long begin, long long end, FP on_pack, FE on_element) {
   constexpr int W = 16 / (int)sizeof(T);
   const bool packs = ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(other)) & 15u) == 0;
-  const long long skew = (reinterpret_cast<uintptr_t>(p + begin) & 15u) / sizeof(T);
-  const long long head = packs ? min(end, begin + (skew ? W - skew : 0)) : end;
+  const int off = skew(p + begin);
+  const long long head = packs ? min(end, begin + (off ? W - off : 0)) : end;
   const long long tail = head + (end - head) / W * W;
   for (long long i = begin + threadIdx.x; i < head; i += kThreads) on_element(i);
-  constexpr int U = 4;                         // packs in flight
+  constexpr int U = 8;                         // packs in flight
   for (long long i = head + (long long)threadIdx.x * W; i < tail; i += (long long)kThreads * W * U) {
     Pack<T, W> v[U];
 #pragma unroll
@@ -86,10 +98,11 @@ __device__ __forceinline__ void walk(const T* p, const void* other, long long be
 }
 
 template <typename T>
-__device__ __forceinline__ double sum_chunk(const T* p, long long begin, long long end) {
+__device__ __forceinline__ double sum_chunk(const T* p, int chunk, long long count) {
   constexpr int W = 16 / (int)sizeof(T);
+  const Range r = range_of(p, chunk, count);
   double s = 0.0;
-  walk(p, p, begin, end, [&](const Pack<T, W>& v, long long) { s += squares<T, W>(v); }, [&](long long i) { s += square(to_f32(p[i])); });
+  walk(p, p, r.begin, r.end, [&](const Pack<T, W>& v, long long) { s += squares<T, W>(v); }, [&](long long i) { s += square(to_f32(p[i])); });
   return s;
 }
 
@@ -111,9 +124,8 @@ __global__ void __launch_bounds__(kThreads) grad_sum_kernel(const __grid_constan
   double s = 0.0;
   for (int chunk = blockIdx.x; chunk < t.first[t.n]; chunk += gridDim.x) {
     const int i = owner_of(t, chunk);
-    const long long count = t.count[i] >> 1, begin = (long long)(chunk - t.first[i]) * kChunk, end = min(count, begin + kChunk);
-    s += t.count[i] & 1 ? sum_chunk(static_cast<const __nv_bfloat16*>(t.in[i]), begin, end)
-                        : sum_chunk(static_cast<const float*>(t.in[i]), begin, end);
+    s += t.count[i] & 1 ? sum_chunk(static_cast<const __nv_bfloat16*>(t.in[i]), chunk - t.first[i], t.count[i] >> 1)
+                        : sum_chunk(static_cast<const float*>(t.in[i]), chunk - t.first[i], t.count[i] >> 1);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -127,9 +139,10 @@ __global__ void __launch_bounds__(kThreads) grad_sum_finish_kernel(const double*
 }
 
 template <typename T>
-__device__ __forceinline__ void scale_chunk(const T* p, T* q, long long begin, long long end, float factor) {
+__device__ __forceinline__ void scale_chunk(const T* p, T* q, int chunk, long long count, float factor) {
   constexpr int W = 16 / (int)sizeof(T);
-  walk(p, q, begin, end,
+  const Range r = range_of(p, chunk, count);
+  walk(p, q, r.begin, r.end,
        [&](const Pack<T, W>& v, long long i) {
          if (factor == 1.f) {                    // a copy, bit by bit: also of what is no number
            *reinterpret_cast<uint4*>(q + i) = v.raw;
@@ -150,12 +163,14 @@ __global__ void __launch_bounds__(kThreads) grad_clip_kernel(const __grid_consta
   // a norm that is no number says nothing about the factor: the gradients pass unchanged
   const float factor = norm > (double)max_norm && norm < (double)INFINITY ? (float)((double)max_norm / norm) : 1.f;
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
-  for (int chunk = blockIdx.x; chunk < t.first[t.n]; chunk += gridDim.x) {
+  // from the end: the norm has read the last chunks last, and L2 still holds them
+  for (int chunk = t.first[t.n] - 1 - (int)blockIdx.x; chunk >= 0; chunk -= gridDim.x) {
     const int i = owner_of(t, chunk);
     if (factor == 1.f && t.in[i] == t.out[i]) continue;
-    const long long count = t.count[i] >> 1, begin = (long long)(chunk - t.first[i]) * kChunk, end = min(count, begin + kChunk);
-    if (t.count[i] & 1) scale_chunk(static_cast<const __nv_bfloat16*>(t.in[i]), static_cast<__nv_bfloat16*>(t.out[i]), begin, end, factor);
-    else scale_chunk(static_cast<const float*>(t.in[i]), static_cast<float*>(t.out[i]), begin, end, factor);
+    if (t.count[i] & 1)
+      scale_chunk(static_cast<const __nv_bfloat16*>(t.in[i]), static_cast<__nv_bfloat16*>(t.out[i]), chunk - t.first[i], t.count[i] >> 1, factor);
+    else
+      scale_chunk(static_cast<const float*>(t.in[i]), static_cast<float*>(t.out[i]), chunk - t.first[i], t.count[i] >> 1, factor);
   }
 }
 
@@ -184,7 +199,8 @@ void for_tables(const gshard_grad_list& l, bool clip, F f) {
     long long chunks = 0;
     for (; i < l.n && t.n < N; ++i) {
       if (!l.counts[i]) continue;
-      const long long more = (l.counts[i] + kChunk - 1) / kChunk;
+      const long long off = l.dtypes[i] == GSHARD_BF16 ? skew(static_cast<const __nv_bfloat16*>(l.grads[i])) : skew(static_cast<const float*>(l.grads[i]));
+      const long long more = (l.counts[i] + off + kChunk - 1) / kChunk;
       if (t.n && chunks + more >= (1 << 30)) break;
       t.in[t.n] = l.grads[i];
       t.out[t.n] = clip ? l.outs[i] : nullptr;
