@@ -34,9 +34,10 @@ constexpr float kSlack = 8.f;                 // growth of a row's maximum (powe
 
 template <int DP> struct Layout {
   static constexpr int tile = kRows * DP * 2;
-  static constexpr int stages = DP == 128 ? 4 : 6;
+  static constexpr int stage = 2 * tile;                       // values of a block, and the keys that come after it
+  static constexpr int stages = DP == 128 ? 2 : 3;
   static constexpr int kv_off = 2 * tile;
-  static constexpr int out_off = kv_off + stages * tile;      // 32 rows x 128 bytes per output warp
+  static constexpr int out_off = kv_off + stages * stage;      // 32 rows x 128 bytes per output warp
   static constexpr int stat_off = out_off + 4 * 32 * 128;      // sum and maximum of every row of both tiles
   static constexpr int bar_off = stat_off + 2 * 2 * kRows * 4;
   static constexpr int bytes = bar_off + 256 + 1024;
@@ -75,6 +76,11 @@ __device__ __forceinline__ Tile tile_of(const ForwardParams& p, const Item& t, i
   return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -93,7 +99,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
   float* stat = reinterpret_cast<float*>(smem + L::stat_off);     // [tile][sum, maximum][row]
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bar_off);
   uint64_t* kv_full = bars;                   // [kStages]
-  uint64_t* kv_empty = kv_full + kStages;     // [kStages]
+  uint64_t* kv_empty = kv_full + kStages;     // [kStages] (MMA, cleaning warp)
   uint64_t* q_full = kv_empty + kStages;      // [2] a tile's queries landed
   uint64_t* q_empty = q_full + 2;             // [2] ... and have been read for the last time
   uint64_t* s_full = q_empty + 2;             // [2] scores complete
@@ -101,12 +107,14 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
   uint64_t* o_full = p_full + 2;              // [2] output complete
   uint64_t* o_empty = o_full + 2;             // [2] output and statistics read (4 warps)
   uint64_t* stat_full = o_empty + 2;          // [2] statistics written (4 warps)
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(stat_full + 2);
+  uint64_t* v_clean = stat_full + 2;          // rows behind the last key zeroed
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(v_clean + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { ptx::mbar_init(kv_full + s, 1); ptx::mbar_init(kv_empty + s, 1); }
+    for (int s = 0; s < kStages; ++s) { ptx::mbar_init(kv_full + s, 1); ptx::mbar_init(kv_empty + s, 2); }
+    ptx::mbar_init(v_clean, 1);
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(q_full + i, 1); ptx::mbar_init(q_empty + i, 1);
       ptx::mbar_init(s_full + i, 1); ptx::mbar_init(p_full + i, 4);
@@ -138,134 +146,173 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
     }
     return i;
   };
+  // Whether the last block of an item has rows between its last key and the next multiple of 16, where its product ends, that TMA
+  // has not zeroed.
+  auto ragged = [&](const Item& t) { return (t.len & 15) != 0 && t.len < p.a.Tk; };
   if (warp >= 12) {
     ptx::registers_down<kOtherRegs>();
     if (warp == 12) {
       // ------------------------------ TMA producer -----------------------------------------------
+      // The ring's first stage holds keys only; from then on values of a block and the keys of the next (or of the next item).
       if (lane == 0) {
         const uint64_t once = ptx::policy_evict_first(), again = ptx::policy_evict_last();
         int stage = 0; uint32_t phase = 0;
         uint32_t q_phase[2] = {0, 0};
-        auto load = [&](const CUtensorMap* map, int kh, int k0, int b) {
-          if (!ptx::mbar_wait(kv_empty + stage, phase ^ 1u, abort_flag)) { ok = false; return; }
-          ptx::mbar_arrive_expect_tx(kv_full + stage, L::tile);
+        auto load = [&](const CUtensorMap* map, int off, int kh, int k0, int b) {
 #pragma unroll
           for (int j = 0; j < DP / 64; ++j)
-            ptx::tma_load_4d(ring + stage * L::tile + j * (kRows * 128), map, kv_full + stage, j * 64, kh, k0, b, again);
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            ptx::tma_load_4d(ring + stage * L::stage + off + j * (kRows * 128), map, kv_full + stage, j * 64, kh, k0, b, again);
         };
-        Item t;
-        for (int i = with_keys(blockIdx.x, t); i < p.items && ok; i = with_keys(i + gridDim.x, t)) {
-          for (int half = 0; half < t.tiles && ok; ++half) {
-            const Tile q = tile_of(p, t, half);
-            if (!ptx::mbar_wait(q_empty + half, q_phase[half] ^ 1u, abort_flag)) { ok = false; break; }
-            q_phase[half] ^= 1u;
-            ptx::mbar_arrive_expect_tx(q_full + half, L::tile);
+        auto load_queries = [&](const Item& t, int half) {
+          const Tile q = tile_of(p, t, half);
+          if (!ptx::mbar_wait(q_empty + half, q_phase[half] ^ 1u, abort_flag)) { ok = false; return; }
+          q_phase[half] ^= 1u;
+          ptx::mbar_arrive_expect_tx(q_full + half, L::tile);
 #pragma unroll
-            for (int j = 0; j < DP / 64; ++j)
-              ptx::tma_load_4d(smem + half * L::tile + j * (kRows * 128), &map_q, q_full + half, j * 64, q.h, q.q0, t.b, once);
-            if (half == 0) load(&map_k, t.kh, 0, t.b);
+          for (int j = 0; j < DP / 64; ++j)
+            ptx::tma_load_4d(smem + half * L::tile + j * (kRows * 128), &map_q, q_full + half, j * 64, q.h, q.q0, t.b, once);
+        };
+        Item t, n;
+        int i = with_keys(blockIdx.x, t);
+        if (i < p.items) {
+          ptx::mbar_arrive_expect_tx(kv_full, L::tile);
+          load(&map_k, L::tile, t.kh, 0, t.b);
+          stage = 1;
+          for (int half = 0; half < t.tiles && ok; ++half) load_queries(t, half);
+        }
+        while (i < p.items && ok) {
+          const int ni = with_keys(i + gridDim.x, n);
+          const bool more = ni < p.items;
+          if (more)                            // the next item's queries are loaded only when this one's have been read for the last time
+            for (int half = 0; half < n.tiles; ++half) {
+              const Tile q = tile_of(p, n, half);
+#pragma unroll
+              for (int j = 0; j < DP / 64; ++j) ptx::tma_prefetch_4d(&map_q, j * 64, q.h, q.q0, n.b);
+            }
+          for (int k0 = 0; k0 < t.len; k0 += kRows) {
+            const bool inner = k0 + kRows < t.len, keys = inner || more;
+            if (!ptx::mbar_wait(kv_empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
+            ptx::mbar_arrive_expect_tx(kv_full + stage, keys ? L::stage : L::tile);
+            load(&map_v, 0, t.kh, k0, t.b);
+            if (inner) load(&map_k, L::tile, t.kh, k0 + kRows, t.b);
+            else if (more) load(&map_k, L::tile, n.kh, 0, n.b);
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
-          for (int k0 = 0; k0 < t.len && ok; k0 += kRows) {
-            load(&map_v, t.kh, k0, t.b);
-            if (ok && k0 + kRows < t.len) load(&map_k, t.kh, k0 + kRows, t.b);
-          }
+          if (more)
+            for (int half = 0; half < n.tiles && ok; ++half) load_queries(n, half);
+          t = n;
+          i = ni;
         }
       }
     } else if (warp == 13) {
-      // ------------------------------ MMA issuer (whole warp waits, one thread issues) ---------------
-      constexpr uint32_t idesc_s = ptx::make_idesc_bf16(kRows, kRows, false, false);
-      constexpr uint32_t idesc_o = ptx::make_idesc_bf16(kRows, DP, false, true);
-      int stage = 0; uint32_t phase = 0;
-      uint32_t q_phase = 0, p_phase = 0, o_phase = 0;           // bit `half`
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok && !__all_sync(0xffffffffu, ptx::mbar_wait(bar, parity & 1u, abort_flag))) ok = false;
-        ptx::tc_fence_after_sync();
-        return ok;
-      };
-      auto next_stage = [&] { if (++stage == kStages) { stage = 0; phase ^= 1u; } };
-      // Branches on elect.sync, not on the lane: the compiler then knows that one thread issues (with lane 0 an MMA took about
-      // 170 cycles to issue instead of its 64 in the tensor core).  The same thread is elected every time.
-      // Scores of tile `half` against the keys in the ring's stage; `fresh`: the first of an item; `last`: the item's last; `release`:
-      // the last use of these keys.
-      auto scores = [&](int half, bool fresh, bool last, bool release) {
-        if (fresh) {
-          if (!wait(q_full + half, q_phase >> half)) return;
-          q_phase ^= 1u << half;
-        }
-        if (!ptx::elect_one()) return;
-        const uint32_t dq = ptx::smem_desc_low(smem + half * L::tile, 16), dk = ptx::smem_desc_low(ring + stage * L::tile, 16);
-#pragma unroll
-        for (int k = 0; k < DP / 16; ++k) {
-          const uint32_t off = (uint32_t)(k / 4 * (kRows * 128) + k % 4 * 32) >> 4;
-          ptx::umma_bf16_low(tmem + half * kRows, dq + off, dk + off, idesc_s, k != 0 ? 1u : 0u);
-        }
-        ptx::umma_commit(s_full + half);
-        if (last) ptx::umma_commit(q_empty + half);
-        if (release) ptx::umma_commit(kv_empty + stage);
-      };
-      Item t, n;
-      int i = with_keys(blockIdx.x, t);
-      if (i < p.items && wait(kv_full + stage, phase)) {
-        for (int half = 0; half < t.tiles && ok; ++half) scores(half, true, t.len <= kRows, half == t.tiles - 1);
-        next_stage();
-      }
-      while (i < p.items && ok) {
-        const int ni = with_keys(i + gridDim.x, n);
-        const bool more = ni < p.items;
-        const int blocks = ceil_div(t.len, kRows);
-        for (int j = 0; j < blocks && ok; ++j) {
-          const int left = t.len - j * kRows;
-          const int steps = min(kRows, (left + 15) & ~15) / 16;      // 16 keys each
-          if (!wait(kv_full + stage, phase)) break;
-          const int v_stage = stage;
-          unsigned char* sv = ring + v_stage * L::tile;
-          if (left < kRows && j * kRows + left < p.a.Tk && steps * 16 != left) {     // what lies behind the last key
-            const int bad = steps * 16 - left;
-            for (int x = lane; x < bad * (DP / 8); x += 32) {
-              const int row = left + x / (DP / 8), c = x % (DP / 8);
-              *reinterpret_cast<uint4*>(sv + c / 8 * (kRows * 128) + row * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
-            }
-            ptx::fence_proxy_async();
-            __syncwarp();
+      // ------------------------------ MMA issuer ---------------------------------------------------
+      // One elected thread runs all of it.  Few MMAs queue up behind one another, so whatever this thread does between two of them
+      // costs the tensor core: with a branch on lane 0 instead of elect.sync an MMA took 170 cycles to issue (64 in the tensor
+      // core), whole-warp waits and a wait for each of keys and values cost a tenth of the kernel.
+      if (ptx::elect_one()) {
+        constexpr uint32_t idesc_s = ptx::make_idesc_bf16(kRows, kRows, false, false);
+        constexpr uint32_t idesc_o = ptx::make_idesc_bf16(kRows, DP, false, true);
+        int stage = 0; uint32_t phase = 0;
+        uint32_t q_phase = 0, p_phase = 0, o_phase = 0, clean_phase = 0;           // bit `half`
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+          if (ok) ok = ptx::mbar_wait(bar, parity & 1u, abort_flag);
+          return ok;
+        };
+        // Scores of tile `half` against the keys in the ring's stage; `fresh`: the first of an item; `last`: the item's last.
+        auto scores = [&](int half, bool fresh, bool last) {
+          if (fresh) {
+            if (!wait(q_full + half, q_phase >> half)) return;
+            q_phase ^= 1u << half;
           }
-          next_stage();
-          // the scores that follow: the next block's, or the next item's first
-          const bool inner = j + 1 < blocks, ahead = inner || more;
-          const int s_tiles = inner ? t.tiles : more ? n.tiles : 0;
-          const bool s_last = inner ? j + 2 == blocks : n.len <= kRows;
-          for (int half = 0; half < 2 && ok; ++half) {
-            if (half < t.tiles) {
-              if (!wait(p_full + half, p_phase >> half)) break;
-              p_phase ^= 1u << half;
-              if (j == 0) {                          // the output before this one has left tensor memory
-                if (!wait(o_empty + half, (o_phase >> half) ^ 1u)) break;
-                o_phase ^= 1u << half;
-              }
-              if (ptx::elect_one()) {
-                const uint32_t dv = ptx::smem_desc_low(sv, kRows * 128);
+          const uint32_t dq = ptx::smem_desc_low(smem + half * L::tile, 16), dk = ptx::smem_desc_low(ring + stage * L::stage + L::tile, 16);
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k) {
+            const uint32_t off = (uint32_t)(k / 4 * (kRows * 128) + k % 4 * 32) >> 4;
+            ptx::umma_bf16_low(tmem + half * kRows, dq + off, dk + off, idesc_s, k != 0 ? 1u : 0u);
+          }
+          ptx::umma_commit(s_full + half);
+          if (last) ptx::umma_commit(q_empty + half);
+        };
+        Item t, n;
+        int i = with_keys(blockIdx.x, t);
+        if (i < p.items && wait(kv_full, 0)) {
+          for (int half = 0; half < t.tiles && ok; ++half) scores(half, true, t.len <= kRows);
+          ptx::umma_commit(kv_empty);
+          stage = 1;
+        }
+        while (i < p.items && ok) {
+          const int ni = with_keys(i + gridDim.x, n);
+          const bool more = ni < p.items;
+          const int blocks = ceil_div(t.len, kRows);
+          for (int j = 0; j < blocks; ++j) {
+            const int steps = min(kRows, (t.len - j * kRows + 15) & ~15) / 16;      // 16 keys each
+            // the scores that follow: the next block's, or the next item's first
+            const bool inner = j + 1 < blocks;
+            const int s_tiles = inner ? t.tiles : more ? n.tiles : 0;
+            const bool s_last = inner ? j + 2 == blocks : n.len <= kRows;
+            if (!wait(kv_full + stage, phase)) break;
+            if (!inner && ragged(t)) {
+              if (!wait(v_clean, clean_phase)) break;
+              clean_phase ^= 1u;
+            }
+            const uint32_t dv = ptx::smem_desc_low(ring + stage * L::stage, kRows * 128);
+            for (int half = 0; half < 2 && ok; ++half) {
+              if (half < t.tiles) {
+                if (j == 0) {                        // the output before this one has left tensor memory
+                  if (!wait(o_empty + half, (o_phase >> half) ^ 1u)) break;
+                  o_phase ^= 1u << half;
+                }
+                if (!wait(p_full + half, p_phase >> half)) break;
+                ptx::tc_fence_after_sync();
+                p_phase ^= 1u << half;
+                auto product = [&](int k) {
+                  ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, dv + (uint32_t)(k * 2048 >> 4), idesc_o, (j | k) != 0 ? 1u : 0u);
+                };
                 if (steps == kRows / 16) {
 #pragma unroll
-                  for (int k = 0; k < kRows / 16; ++k)
-                    ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, dv + (uint32_t)(k * 2048 >> 4), idesc_o, (j | k) != 0 ? 1u : 0u);
+                  for (int k = 0; k < kRows / 16; ++k) product(k);
                 } else {
-                  for (int k = 0; k < steps; ++k)
-                    ptx::umma_bf16_ta(tmem_o + half * DP, tmem + half * kRows + k * 8, dv + (uint32_t)(k * 2048 >> 4), idesc_o, (j | k) != 0 ? 1u : 0u);
+                  for (int k = 0; k < steps; ++k) product(k);
                 }
-                if (half == t.tiles - 1) ptx::umma_commit(kv_empty + v_stage);
-                if (j == blocks - 1) ptx::umma_commit(o_full + half);
+                if (!inner) ptx::umma_commit(o_full + half);
               }
+              if (half < s_tiles) scores(half, !inner, s_last);
             }
-            if (half < s_tiles) {
-              if (half == 0 && !wait(kv_full + stage, phase)) break;
-              scores(half, !inner, s_last, half == s_tiles - 1);
-            }
+            ptx::umma_commit(kv_empty + stage);
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
-          if (ahead) next_stage();
+          t = n;
+          i = ni;
         }
-        t = n;
-        i = ni;
       }
+    } else if (warp == 14) {
+      // ------------------------------ zeroes what lies behind a source's last key ----------------------
+      // It follows every stage, so that no phase of the barriers passes by unseen.
+      int stage = 0; uint32_t phase = 0;
+      auto follow = [&](int from, int to) {    // rows of V to zero
+        if (!ptx::mbar_wait_all(kv_full + stage, phase, abort_flag)) { ok = false; return; }
+        if (from < to) {
+          unsigned char* sv = ring + stage * L::stage;
+          for (int x = lane; x < (to - from) * (DP / 8); x += 32) {
+            const int row = from + x / (DP / 8), c = x % (DP / 8);
+            *reinterpret_cast<uint4*>(sv + c / 8 * (kRows * 128) + row * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+          }
+          ptx::fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(v_clean);
+        }
+        if (lane == 0) ptx::mbar_arrive(kv_empty + stage);
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      };
+      Item t;
+      int i = with_keys(blockIdx.x, t);
+      if (i < p.items) follow(0, 0);
+      for (; i < p.items && ok; i = with_keys(i + gridDim.x, t))
+        for (int k0 = 0; k0 < t.len && ok; k0 += kRows) {
+          const int left = t.len - k0;
+          const bool fix = left <= kRows && ragged(t);
+          follow(fix ? left : 0, fix ? (left + 15) & ~15 : 0);
+        }
     }
   } else if (warp >= 8) {
     // ------------------------------ output: one thread per row ---------------------------------------
@@ -350,7 +397,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
       if (len == 0) continue;
       float top = -INFINITY, sum = 0.f;        // the maximum that the weights so far refer to, and their sum
       for (int k0 = 0; k0 < len; k0 += kRows) {
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait(s_full + half, s_phase, abort_flag))) { ok = false; break; }
+        if (!ptx::mbar_wait_all(s_full + half, s_phase, abort_flag)) { ok = false; break; }
         s_phase ^= 1u;
         ptx::tc_fence_after_sync();
         uint32_t s[kRows];
@@ -365,7 +412,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         }
         float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) m[j & 3] = fmaxf(m[j & 3], __uint_as_float(s[j]));
+        for (int j = 0; j < kRows; j += 2) m[j >> 1 & 3] = max3(m[j >> 1 & 3], __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
         const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
         if (k0 == 0) {
           top = fmaxf(most, -1e30f);
@@ -389,18 +436,18 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         const f32x2 c2 = both(c), m2 = both(-top * c);
         f32x2 sum2[2] = {0, 0};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[32];
+        for (int h = 0; h < 4; ++h) {
+          uint32_t w[16];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const int at = h * 64 + 2 * j;
+          for (int j = 0; j < 16; ++j) {
+            const int at = h * 32 + 2 * j;
             const float2 x = unpair(fma2(pair(__uint_as_float(s[at]), __uint_as_float(s[at + 1])), c2, m2));
             const float e0 = exp2_approx(x.x), e1 = exp2_approx(x.y);
             sum2[j & 1] = add2(sum2[j & 1], pair(e0, e1));
             const __nv_bfloat162 b = __floats2bfloat162_rn(e0, e1);
             w[j] = *reinterpret_cast<const uint32_t*>(&b);
           }
-          ptx::tmem_st_32x32(t_s + h * 32, w);
+          ptx::tmem_st_32x16(t_s + h * 16, w);
         }
         const float2 part = unpair(add2(sum2[0], sum2[1]));
         sum += part.x + part.y;
@@ -411,7 +458,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
       }
       if (!ok) break;
       // the statistics of the item before have been read together with its output
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(o_empty + half, o_phase ^ 1u, abort_flag))) { ok = false; break; }
+      if (!ptx::mbar_wait_all(o_empty + half, o_phase ^ 1u, abort_flag)) { ok = false; break; }
       o_phase ^= 1u;
       const int r = threadIdx.x & 127;
       stat[half * 2 * kRows + r] = sum;

@@ -89,6 +89,11 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
   }
 }
 
+// Every lane waits; the answer is the warp's (a lane that gave up makes all of them).
+__device__ __forceinline__ bool mbar_wait_all(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)) != 0;
+}
+
 // Whole-warp wait: lane 0 polls (sleeping between polls, the waits of an epilogue warp last
 // microseconds) while the other lanes park at the shuffle instead of all 32 spinning on the
 // barrier; the shuffle also orders the other lanes' later reads after lane 0's acquire.
@@ -149,6 +154,13 @@ __device__ __forceinline__ void tma_load_4d(void* smem_dst, const CUtensorMap* m
       : "r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3),
         "l"(policy)
       : "memory");
+}
+
+// the tile into L2 only
+__device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0),
+               "r"(c1), "r"(c2), "r"(c3)
+               : "memory");
 }
 
 // 3-D tiled store shared -> global (bulk async-group completion); elements outside the tensor are
