@@ -95,9 +95,8 @@ __device__ __forceinline__ void load_rows(unsigned char* dst, const CUtensorMap*
   for (int j = 0; j < DP / 64; ++j) ptx::tma_load_4d(dst + j * (kRows * 128), map, bar, j * 64, h, t, b, policy);
 }
 
-// The two products, called by one elected thread.  (Branches on elect.sync, not on the lane: the compiler then knows that one
-// thread issues; with lane 0 an MMA took about 170 cycles to issue instead of its 64 in the tensor core.  The same thread is
-// elected every time.)
+// The two products, called by one elected thread.  (A branch on elect.sync, not on the lane: the compiler then knows that one
+// thread issues; with lane 0 an MMA took about 170 cycles to issue instead of its 64 in the tensor core.)
 // D = A B^T of two tiles in shared memory (rows by rows, along the head dimension)
 template <int DP>
 __device__ __forceinline__ void mma_rows(uint32_t d, const unsigned char* a, const unsigned char* b) {
@@ -241,37 +240,36 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
       }
     } else if (warp == 9) {
-      // ------------------------------ MMA issuer (whole warp waits, one thread issues) --------------
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok && !__all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag))) ok = false;
-        ptx::tc_fence_after_sync();
-        return ok;
-      };
-      int stage = 0, ahead = 0;               // of query tile i, and of the tile whose scores are computed next
-      uint32_t ahead_phase = 0;
-      auto step = [&](int& s) { return ++s == kStages ? (s = 0, true) : false; };
-      if (wait(kv_full, 0) && wait(full, 0) && ptx::elect_one()) {
-        mma_rows<DP>(t_s, sk, ring);
-        ptx::umma_commit(s_full);
-        mma_rows<DP>(t_dp, sv, ring + L::tile);
-        ptx::umma_commit(dp_full);
-      }
-      if (step(ahead)) ahead_phase ^= 1u;
-      for (int i = 0; i < n && ok; ++i) {
-        const unsigned char *q = ring + stage * L::stage, *d = q + L::tile;
-        const unsigned char *q1 = ring + ahead * L::stage, *d1 = q1 + L::tile;
-        const bool more = i + 1 < n;
-        if (!wait(p_full, i & 1)) break;
-        if (ptx::elect_one()) mma_weights<DP>(t_dv, t_s, d, kRows / 16, i != 0);
-        if (more) {
-          if (!wait(full + ahead, ahead_phase)) break;
-          if (ptx::elect_one()) {
+      // ------------------------------ MMA issuer (one elected thread runs all of it) ------------------
+      if (ptx::elect_one()) {
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+          if (ok) ok = ptx::mbar_wait(bar, parity, abort_flag);
+          return ok;
+        };
+        int stage = 0, ahead = 0;             // of query tile i, and of the tile whose scores are computed next
+        uint32_t ahead_phase = 0;
+        auto step = [&](int& s) { return ++s == kStages ? (s = 0, true) : false; };
+        if (wait(kv_full, 0) && wait(full, 0)) {
+          mma_rows<DP>(t_s, sk, ring);
+          ptx::umma_commit(s_full);
+          mma_rows<DP>(t_dp, sv, ring + L::tile);
+          ptx::umma_commit(dp_full);
+        }
+        if (step(ahead)) ahead_phase ^= 1u;
+        for (int i = 0; i < n && ok; ++i) {
+          const unsigned char *q = ring + stage * L::stage, *d = q + L::tile;
+          const unsigned char *q1 = ring + ahead * L::stage, *d1 = q1 + L::tile;
+          const bool more = i + 1 < n;
+          if (more && !wait(full + ahead, ahead_phase)) break;
+          if (!wait(p_full, i & 1)) break;
+          ptx::tc_fence_after_sync();
+          mma_weights<DP>(t_dv, t_s, d, kRows / 16, i != 0);
+          if (more) {
             mma_rows<DP>(t_s, sk, q1);
             ptx::umma_commit(s_full);
           }
-        }
-        if (!wait(ds_full, i & 1)) break;
-        if (ptx::elect_one()) {
+          if (!wait(ds_full, i & 1)) break;
+          ptx::tc_fence_after_sync();
           mma_weights<DP>(t_dk, t_dp, q, kRows / 16, i != 0);
           ptx::umma_commit(empty + stage);
           if (more) {
@@ -280,9 +278,9 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           } else {
             ptx::umma_commit(o_full);
           }
+          step(stage);
+          if (step(ahead)) ahead_phase ^= 1u;
         }
-        step(stage);
-        if (step(ahead)) ahead_phase ^= 1u;
       }
     }
   } else {
@@ -388,7 +386,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   unsigned char *sq = smem, *sd = smem + L::tile, *sk = smem + L::k_off, *sv = smem + L::v_off;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bar_off);
   uint64_t* k_full = bars;
-  uint64_t* k_empty = k_full + kK;
+  uint64_t* k_empty = k_full + kK;            // MMA, cleaning warp
   uint64_t* v_full = k_empty + kK;
   uint64_t* v_empty = v_full + kV;
   uint64_t* q_full = v_empty + kV;            // queries and dO landed
@@ -397,13 +395,15 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   uint64_t* dp_full = s_full + 2;
   uint64_t* ds_full = dp_full + 1;            // 8 warps: dS written, dP read
   uint64_t* o_full = ds_full + 1;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 1);
+  uint64_t* k_clean = o_full + 1;             // rows behind the last key zeroed
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(k_clean + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int group = p.a.H / p.a.Hkv;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kK; ++s) { ptx::mbar_init(k_full + s, 1); ptx::mbar_init(k_empty + s, 1); }
+    for (int s = 0; s < kK; ++s) { ptx::mbar_init(k_full + s, 1); ptx::mbar_init(k_empty + s, 2); }
+    ptx::mbar_init(k_clean, 1);
     for (int s = 0; s < kV; ++s) { ptx::mbar_init(v_full + s, 1); ptx::mbar_init(v_empty + s, 1); }
     ptx::mbar_init(q_full, 1); ptx::mbar_init(q_empty, 1);
     ptx::mbar_init(s_full, 1); ptx::mbar_init(s_full + 1, 1); ptx::mbar_init(dp_full, 1);
@@ -428,6 +428,8 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   // item: query tile (fastest), head, batch
   auto head_of = [&](int i) { return i / p.q_tiles % p.a.H; };
   auto batch_of = [&](int i) { return i / p.q_tiles / p.a.H; };
+  // whether the last block has rows between its last key and the next multiple of 16, where its product ends, that TMA has not zeroed
+  auto ragged = [&](int len) { return (len & 15) != 0 && len < p.a.Tk; };
 
   bool ok = true;
   if (warp >= 8) {
@@ -462,58 +464,72 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         }
       }
     } else if (warp == 9) {
-      // ------------------------------ MMA issuer (whole warp waits, one thread issues) ------------------
-      int ks = 0, vs = 0, ds = 0;             // ring positions of the next S, the next dP and the next dq
-      uint32_t k_phase = 0, v_phase = 0, q_phase = 0, ds_phase = 0;
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok && !__all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag))) ok = false;
-        ptx::tc_fence_after_sync();
-        return ok;
-      };
-      for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-        const int len = source_length(p.a, batch_of(i));
-        if (len == 0) continue;
-        const int blocks = ceil_div(len, kRows);
-        auto scores = [&](int j) {
-          if (!wait(k_full + ks, k_phase)) return;
-          unsigned char* k = sk + ks * L::tile;
-          const int left = len - j * kRows;
-          if (left < kRows && (left & 15) && len < p.a.Tk) zero_rows<DP>(k, left, (left + 15) & ~15, lane);
-          if (ptx::elect_one()) {
-            mma_rows<DP>(tmem + (j & 1) * kRows, sq, k);
-            ptx::umma_commit(s_full + (j & 1));
-          }
-          if (++ks == kK) { ks = 0; k_phase ^= 1u; }
+      // ------------------------------ MMA issuer (one elected thread runs all of it) ------------------
+      if (ptx::elect_one()) {
+        int ks = 0, vs = 0, ds = 0;           // ring positions of the next S, the next dP and the next dq
+        uint32_t k_phase = 0, v_phase = 0, q_phase = 0, ds_phase = 0, clean_phase = 0;
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+          if (ok) ok = ptx::mbar_wait(bar, parity, abort_flag);
+          return ok;
         };
-        auto grads = [&](int j) {             // dP of block j
-          if (!wait(v_full + vs, v_phase)) return;
-          if (ptx::elect_one()) {
+        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+          const int len = source_length(p.a, batch_of(i));
+          if (len == 0) continue;
+          const int blocks = ceil_div(len, kRows);
+          auto scores = [&](int j) {
+            if (!wait(k_full + ks, k_phase)) return;
+            if (j == blocks - 1 && ragged(len)) {
+              if (!wait(k_clean, clean_phase)) return;
+              clean_phase ^= 1u;
+            }
+            mma_rows<DP>(tmem + (j & 1) * kRows, sq, sk + ks * L::tile);
+            ptx::umma_commit(s_full + (j & 1));
+            if (++ks == kK) { ks = 0; k_phase ^= 1u; }
+          };
+          auto grads = [&](int j) {           // dP of block j
+            if (!wait(v_full + vs, v_phase)) return;
             mma_rows<DP>(t_dp, sd, sv + vs * L::tile);
             ptx::umma_commit(dp_full);
             ptx::umma_commit(v_empty + vs);
             if (j == blocks - 1) ptx::umma_commit(q_empty);
-          }
-          if (++vs == kV) { vs = 0; v_phase ^= 1u; }
-        };
-        if (!wait(q_full, q_phase)) break;
-        q_phase ^= 1u;
-        scores(0);
-        // a block's scores always go before its dP, so that "queries read" may follow the last dP
-        if (ok && blocks > 1) scores(1);
-        if (ok) grads(0);
-        for (int j = 0; j < blocks && ok; ++j) {
-          if (!wait(ds_full, ds_phase)) break;
-          ds_phase ^= 1u;
-          const int steps = min(kRows, (len - j * kRows + 15) & ~15) / 16;
-          if (j + 1 < blocks) grads(j + 1);     // first: the threads are about to wait for it
-          if (!ok) break;
-          if (ptx::elect_one()) {
+            if (++vs == kV) { vs = 0; v_phase ^= 1u; }
+          };
+          if (!wait(q_full, q_phase)) break;
+          q_phase ^= 1u;
+          scores(0);
+          // a block's scores always go before its dP, so that "queries read" may follow the last dP
+          if (ok && blocks > 1) scores(1);
+          if (ok) grads(0);
+          for (int j = 0; j < blocks && ok; ++j) {
+            if (!wait(ds_full, ds_phase)) break;
+            ptx::tc_fence_after_sync();
+            ds_phase ^= 1u;
+            const int steps = min(kRows, (len - j * kRows + 15) & ~15) / 16;
+            if (j + 1 < blocks) grads(j + 1);   // first: the threads are about to wait for it
+            if (!ok) break;
             mma_weights<DP>(t_dq, tmem + (j & 1) * kRows, sk + ds * L::tile, steps, j != 0);
             ptx::umma_commit(k_empty + ds);
             if (j == blocks - 1) ptx::umma_commit(o_full);
+            if (++ds == kK) ds = 0;
+            if (j + 2 < blocks) scores(j + 2);
           }
-          if (++ds == kK) ds = 0;
-          if (j + 2 < blocks) scores(j + 2);
+        }
+      }
+    } else if (warp == 10) {
+      // ------------------------------ zeroes what lies behind a source's last key ----------------------
+      // It follows every stage, so that no phase of the barriers passes by unseen.
+      int ks = 0; uint32_t k_phase = 0;
+      for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+        const int len = source_length(p.a, batch_of(i));
+        for (int k0 = 0; k0 < len; k0 += kRows) {
+          if (!ptx::mbar_wait_all(k_full + ks, k_phase, abort_flag)) { ok = false; break; }
+          const int left = len - k0;
+          if (left <= kRows && ragged(len)) {
+            zero_rows<DP>(sk + ks * L::tile, left, (left + 15) & ~15, lane);
+            if (lane == 0) ptx::mbar_arrive(k_clean);
+          }
+          if (lane == 0) ptx::mbar_arrive(k_empty + ks);
+          if (++ks == kK) { ks = 0; k_phase ^= 1u; }
         }
       }
     }
@@ -575,7 +591,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         if (lane == 0) ptx::mbar_arrive(ds_full);
       }
       if (!ok) break;
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(o_full, o_phase, abort_flag))) { ok = false; break; }
+      if (!ptx::mbar_wait_all(o_full, o_phase, abort_flag)) { ok = false; break; }
       o_phase ^= 1u;
       ptx::tc_fence_after_sync();
       store_row<DP / 2>(t_dq + half * (DP / 2) + lanes, dq, half * (DP / 2), p.a.D, p.a.scale, in, false);
