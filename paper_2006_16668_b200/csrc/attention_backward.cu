@@ -2,19 +2,24 @@
 // and once per tile of queries (dq): seven products instead of five, and every gradient is accumulated in one place
 // of tensor memory in a fixed order, without atomics and without partial sums in HBM.
 //
-// Row statistics.  A first kernel writes lse log2(e) and delta = sum over d of dout o per tile of 128 queries, padded with
-// lse = +inf, so that P = 2^(c s - lse) of a row behind the last query is 0 and nothing else needs a mask there.
+// Row statistics.  A first kernel writes, per tile of 128 queries, lse log2(e) and delta = sum over d of dout o in fp32, and both once
+// more as three bf16 terms each, laid out as the B operand of one MMA step: with ones as A that step adds -lse / scale to the scores
+// and -delta to dP (24 bits, as exact as fp32), for which the threads would have to read shared memory that the tensor core keeps
+// busy (32 16-byte loads per thread and tile, 900 of 3800 cycles).  Rows behind the last query are padded with -1e30 for the former, so
+// that their P is 0 and nothing else needs a mask there.
 //
-// dk, dv: a CTA owns 128 keys of one key head and walks the query tiles of all heads of its group.
+// dk, dv: persistent CTAs; an item is 128 keys of one key head and walks the query tiles of all heads of its group.
 //   S^T = K Q^T and dP^T = V dO^T into tensor memory (a thread holds 64 of a key's 128 queries), P^T over S^T, dv += P^T dO,
 //   dS^T = P^T (dP^T - delta) over dP^T, dk += dS^T Q; P stays in fp32 registers between the two.  While the threads
-//   work on P the tensor core runs dk of the tile before and dP^T, while they work on dS it runs dv and the next S^T.
+//   work on P the tensor core runs dk of the tile before and dP^T, while they work on dS it runs dv and the next S^T; the next
+//   item's first products are under way while an item's dk and dv leave tensor memory.
 //   Keys behind the source's length only make rows of their own; these are written as zero.
 // dq: a CTA owns 128 queries of one head and walks the source: S = Q K^T (two buffers), dP = dO V^T, dS over S,
 //   dq += dS K.  Keys behind the length: dS is zero, and rows of K that hold something else are zeroed in shared memory.
 #include <algorithm>
 
 #include "attention.cuh"
+#include "checks.cuh"
 #include "pack.cuh"
 #include "sm100_ptx.cuh"
 
@@ -25,7 +30,8 @@ namespace {
 constexpr int kRows = 128;
 constexpr int kThreads = 384;                 // 8 warps on the scores; TMA, MMA and two idle warps
 constexpr int kScoreRegs = 216, kOtherRegs = 72;      // 2 x 128 x 216 + 128 x 72 = 384 x 168
-constexpr int kStatBytes = 2 * kRows * 4;     // lse log2(e) and delta of a query tile
+// statistics of a query tile: lse log2(e) [128], delta [128], and the operand [128 x 16] of their terms
+constexpr int kTermBytes = kRows * 16 * 2, kStatFloats = 2 * kRows + kTermBytes / 4;
 
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
@@ -33,7 +39,17 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
-// stats[b, h, tile][0]: lse log2(e), [1]: delta.  A block takes 64 (query, head) rows of a tile, 16 lanes a row and four rows of
+// v as three bf16 terms, 16 bits of a word each from `at` on
+__device__ __forceinline__ void put_terms(float v, unsigned short* out) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const __nv_bfloat16 t = __float2bfloat16_rn(v);
+    out[i] = *reinterpret_cast<const unsigned short*>(&t);
+    v -= __bfloat162float(t);
+  }
+}
+
+// A block takes 64 (query, head) rows of a tile, 16 lanes a row and four rows of
 // a group in flight; neighbouring rows are the heads of a token, which lie together in o and dout.
 constexpr int kStatRows = 64;
 __global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArgs a, float* stats, int q_tiles) {
@@ -64,9 +80,17 @@ __global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArg
     for (int off = 8; off; off >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, off);
     if (part == 0 && r < kRows * a.H) {
       const long long head = (long long)b * a.H + h;
-      float* out = stats + (head * q_tiles + t0 / kRows) * (2 * kRows) + r / a.H;
-      out[0] = t < a.Tq ? a.lse[head * a.Tq + t] * kLog2e : INFINITY;
-      out[kRows] = delta;
+      float* out = stats + (head * q_tiles + t0 / kRows) * kStatFloats;
+      const int row = r / a.H;
+      const float lse = t < a.Tq ? a.lse[head * a.Tq + t] : 0.f;
+      out[row] = t < a.Tq ? lse * kLog2e : INFINITY;
+      out[kRows + row] = delta;
+      alignas(16) unsigned short terms[8] = {};
+      put_terms(t < a.Tq ? -lse / a.scale : -1e30f, terms);
+      put_terms(-delta, terms + 3);
+      uint4* step = reinterpret_cast<uint4*>(out + 2 * kRows) + row / 8 * 16 + row % 8;
+      step[0] = *reinterpret_cast<const uint4*>(terms);
+      step[8] = make_uint4(0, 0, 0, 0);
     }
   }
 }
@@ -75,7 +99,7 @@ struct BackwardParams {
   AttentionArgs a;
   const float* stats;
   int q_tiles, k_tiles;
-  int items;                                  // dq
+  int items, kv_items;                        // of dq, of dk and dv
 };
 
 // zeroes the rows [from, to) of a tile of 128 rows x DP bf16 in two or one swizzled halves (zeros need no swizzle); whole warp
@@ -151,62 +175,76 @@ __device__ __forceinline__ void store_row(uint32_t taddr, __nv_bfloat16* out, in
 
 template <int DP> struct KvLayout {
   static constexpr int tile = kRows * DP * 2;
-  static constexpr int stages = 2;
-  static constexpr int stage = 2 * tile;
+  static constexpr int stages = DP == 128 ? 2 : 4;
+  static constexpr int stage = 2 * tile + kTermBytes;          // Q, dO, the terms of their statistics
   static constexpr int ring_off = 2 * tile;
-  static constexpr int stat_off = ring_off + stages * stage;
-  static constexpr int bar_off = stat_off + stages * kStatBytes;
+  static constexpr int ones_off = ring_off + stages * stage;   // [2] A operands of the terms' step: ones for lse's, for delta's
+  static constexpr int out_off = ones_off + 2 * kTermBytes;    // 32 rows x 64 bytes per warp
+  static constexpr int bar_off = out_off + 8 * 32 * 64;
   static constexpr int bytes = bar_off + 256 + 1024;
   static_assert(bytes <= 232448, "shared memory budget");
 };
 
+struct KvItem { int b, kh, k0, n, len; };      // n: query tiles to walk
+
+__device__ __forceinline__ KvItem kv_item_of(const BackwardParams& p, int i) {
+  KvItem t;
+  t.k0 = i % p.k_tiles * kRows;
+  t.kh = i / p.k_tiles % p.a.Hkv;
+  t.b = i / p.k_tiles / p.a.Hkv;
+  t.len = source_length(p.a, t.b);
+  t.n = t.k0 < t.len ? p.a.H / p.a.Hkv * p.q_tiles : 0;
+  return t;
+}
+
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                     const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const BackwardParams p) {
+                     const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
+                     const __grid_constant__ CUtensorMap map_dk, const __grid_constant__ CUtensorMap map_dv, const BackwardParams p) {
   using L = KvLayout<DP>;
   constexpr int kStages = L::stages;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  unsigned char *sk = smem, *sv = smem + L::tile, *ring = smem + L::ring_off;
-  const float* stat = reinterpret_cast<const float*>(smem + L::stat_off);
+  unsigned char *sk = smem, *sv = smem + L::tile, *ring = smem + L::ring_off, *ones = smem + L::ones_off;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bar_off);
-  uint64_t* full = bars;                      // [kStages] Q, dO and their statistics landed
+  uint64_t* full = bars;                      // [kStages] Q, dO and their terms landed
   uint64_t* empty = full + kStages;           // [kStages]
-  uint64_t* kv_full = empty + kStages;
-  uint64_t* s_full = kv_full + 1;
+  uint64_t* k_full = empty + kStages;
+  uint64_t* k_empty = k_full + 1;
+  uint64_t* v_full = k_empty + 1;
+  uint64_t* v_empty = v_full + 1;
+  uint64_t* s_full = v_empty + 1;
   uint64_t* dp_full = s_full + 1;
   uint64_t* p_full = dp_full + 1;             // 8 warps
   uint64_t* ds_full = p_full + 1;             // 8 warps
   uint64_t* o_full = ds_full + 1;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 1);
+  uint64_t* o_empty = o_full + 1;             // 8 warps: dk and dv have left tensor memory
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_empty + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-
   const int group = p.a.H / p.a.Hkv;
-  const int k0 = blockIdx.x % p.k_tiles * kRows, kh = blockIdx.x / p.k_tiles % p.a.Hkv, b = blockIdx.x / p.k_tiles / p.a.Hkv;
-  const int len = source_length(p.a, b), rows = min(kRows, p.a.Tk - k0);
-  const int n = k0 < len ? group * p.q_tiles : 0;      // query tiles to walk
-  __nv_bfloat16* dk = static_cast<__nv_bfloat16*>(p.a.dk) + ((long long)b * p.a.Tk + k0) * p.a.k_stride + (long long)kh * p.a.D;
-  __nv_bfloat16* dv = static_cast<__nv_bfloat16*>(p.a.dv) + ((long long)b * p.a.Tk + k0) * p.a.v_stride + (long long)kh * p.a.D;
-  if (n == 0) {                               // no key of this block counts, or there is no query
-    for (int x = threadIdx.x; x < rows * (p.a.D / 8); x += kThreads) {
-      const int r = x / (p.a.D / 8), c = x % (p.a.D / 8) * 8;
-      *reinterpret_cast<uint4*>(dk + r * p.a.k_stride + c) = make_uint4(0, 0, 0, 0);
-      *reinterpret_cast<uint4*>(dv + r * p.a.v_stride + c) = make_uint4(0, 0, 0, 0);
-    }
-    return;
-  }
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { ptx::mbar_init(full + s, 1); ptx::mbar_init(empty + s, 1); }
-    ptx::mbar_init(kv_full, 1); ptx::mbar_init(s_full, 1); ptx::mbar_init(dp_full, 1);
-    ptx::mbar_init(p_full, 8); ptx::mbar_init(ds_full, 8); ptx::mbar_init(o_full, 1);
+    ptx::mbar_init(k_full, 1); ptx::mbar_init(k_empty, 1); ptx::mbar_init(v_full, 1); ptx::mbar_init(v_empty, 1);
+    ptx::mbar_init(s_full, 1); ptx::mbar_init(dp_full, 1);
+    ptx::mbar_init(p_full, 8); ptx::mbar_init(ds_full, 8); ptx::mbar_init(o_full, 1); ptx::mbar_init(o_empty, 8);
     *abort_flag = 0;
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&map_q);
     ptx::prefetch_tensormap(&map_do);
+    ptx::prefetch_tensormap(&map_k);
+    ptx::prefetch_tensormap(&map_v);
   }
+  // ones in columns 0 to 2 (the first operand) or 3 to 5 (the second) of every row
+  for (int x = threadIdx.x; x < 2 * kRows; x += kThreads) {
+    const int row = x % kRows;
+    uint4* step = reinterpret_cast<uint4*>(ones + x / kRows * kTermBytes) + row / 8 * 16 + row % 8;
+    step[0] = x < kRows ? make_uint4(0x3f803f80u, 0x3f80u, 0, 0) : make_uint4(0, 0x3f800000u, 0x3f803f80u, 0);
+    step[8] = make_uint4(0, 0, 0, 0);
+  }
+  ptx::fence_proxy_async();
   if (warp == 9) {
     ptx::tmem_alloc(tmem_slot, 512);
     ptx::tmem_relinquish();
@@ -217,6 +255,14 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
   const uint32_t tmem = *tmem_slot;
   const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DP;
 
+  // the next item from i on that has query tiles to walk
+  auto with_work = [&](int i, KvItem& t) {
+    for (; i < p.kv_items; i += gridDim.x) {
+      t = kv_item_of(p, i);
+      if (t.n > 0) break;
+    }
+    return i;
+  };
   bool ok = true;
   if (warp >= 8) {
     ptx::registers_down<kOtherRegs>();
@@ -224,130 +270,188 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       // ------------------------------ TMA producer -----------------------------------------------
       if (lane == 0) {
         const uint64_t again = ptx::policy_evict_last(), once = ptx::policy_evict_first();
-        ptx::mbar_arrive_expect_tx(kv_full, 2 * L::tile);
-        load_rows<DP>(sk, &map_k, kv_full, kh, k0, b, once);
-        load_rows<DP>(sv, &map_v, kv_full, kh, k0, b, once);
-        int stage = 0; uint32_t phase = 0;
-        for (int i = 0; i < n; ++i) {
-          if (!ptx::mbar_wait(empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
-          const int h = kh * group + i / p.q_tiles, tile = i % p.q_tiles;
-          ptx::mbar_arrive_expect_tx(full + stage, L::stage + kStatBytes);
-          load_rows<DP>(ring + stage * L::stage, &map_q, full + stage, h, tile * kRows, b, again);
-          load_rows<DP>(ring + stage * L::stage + L::tile, &map_do, full + stage, h, tile * kRows, b, again);
-          ptx::bulk_load(smem + L::stat_off + stage * kStatBytes, p.stats + (((long long)b * p.a.H + h) * p.q_tiles + tile) * 2 * kRows,
-                         kStatBytes, full + stage);
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        int stage = 0; uint32_t phase = 0, kv_phase = 0;
+        KvItem t;
+        for (int it = with_work(blockIdx.x, t); it < p.kv_items && ok; it = with_work(it + gridDim.x, t)) {
+          if (!ptx::mbar_wait(k_empty, kv_phase ^ 1u, abort_flag)) { ok = false; break; }
+          ptx::mbar_arrive_expect_tx(k_full, L::tile);
+          load_rows<DP>(sk, &map_k, k_full, t.kh, t.k0, t.b, once);
+          if (!ptx::mbar_wait(v_empty, kv_phase ^ 1u, abort_flag)) { ok = false; break; }
+          ptx::mbar_arrive_expect_tx(v_full, L::tile);
+          load_rows<DP>(sv, &map_v, v_full, t.kh, t.k0, t.b, once);
+          kv_phase ^= 1u;
+          for (int i = 0; i < t.n; ++i) {
+            if (!ptx::mbar_wait(empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
+            const int h = t.kh * group + i / p.q_tiles, tile = i % p.q_tiles;
+            unsigned char* q = ring + stage * L::stage;
+            ptx::mbar_arrive_expect_tx(full + stage, L::stage);
+            load_rows<DP>(q, &map_q, full + stage, h, tile * kRows, t.b, again);
+            load_rows<DP>(q + L::tile, &map_do, full + stage, h, tile * kRows, t.b, again);
+            ptx::bulk_load(q + 2 * L::tile, p.stats + (((long long)t.b * p.a.H + h) * p.q_tiles + tile) * kStatFloats + 2 * kRows, kTermBytes,
+                           full + stage);
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          }
         }
       }
     } else if (warp == 9) {
       // ------------------------------ MMA issuer (one elected thread runs all of it) ------------------
       if (ptx::elect_one()) {
+        constexpr uint32_t idesc = ptx::make_idesc_bf16(kRows, kRows, false, false);
+        const uint32_t one_l = ptx::plain_desc_low(ones), one_d = ptx::plain_desc_low(ones + kTermBytes);
         auto wait = [&](uint64_t* bar, uint32_t parity) {
-          if (ok) ok = ptx::mbar_wait(bar, parity, abort_flag);
+          if (ok) ok = ptx::mbar_wait(bar, parity & 1u, abort_flag);
           return ok;
         };
-        int stage = 0, ahead = 0;             // of query tile i, and of the tile whose scores are computed next
-        uint32_t ahead_phase = 0;
-        auto step = [&](int& s) { return ++s == kStages ? (s = 0, true) : false; };
-        if (wait(kv_full, 0) && wait(full, 0)) {
-          mma_rows<DP>(t_s, sk, ring);
+        int stage = 0, ahead = 0;             // of the query tile at hand, and of the tile whose scores are computed next
+        uint32_t ahead_phase = 0, turn = 0, item_phase = 0, k_phase = 0, v_phase = 0;
+        // scores and dP of the tile in stage `ahead`; `fresh`: the first of an item, `last`: its last
+        auto scores = [&](bool fresh, bool last) {
+          if (fresh) { if (!wait(k_full, k_phase)) return; k_phase ^= 1u; }
+          if (!wait(full + ahead, ahead_phase)) return;
+          const unsigned char* q = ring + ahead * L::stage;
+          mma_rows<DP>(t_s, sk, q);
+          ptx::umma_bf16_plain(t_s, one_l, ptx::plain_desc_low(q + 2 * L::tile), idesc, 1u);
           ptx::umma_commit(s_full);
-          mma_rows<DP>(t_dp, sv, ring + L::tile);
+          if (last) ptx::umma_commit(k_empty);
+        };
+        auto grads = [&](bool fresh, bool last) {
+          if (fresh) { if (!wait(v_full, v_phase)) return; v_phase ^= 1u; }
+          const unsigned char* q = ring + ahead * L::stage;
+          mma_rows<DP>(t_dp, sv, q + L::tile);
+          ptx::umma_bf16_plain(t_dp, one_d, ptx::plain_desc_low(q + 2 * L::tile), idesc, 1u);
           ptx::umma_commit(dp_full);
+          if (last) ptx::umma_commit(v_empty);
+        };
+        auto step = [&] { if (++ahead == kStages) { ahead = 0; ahead_phase ^= 1u; } };
+        KvItem t, next;
+        int it = with_work(blockIdx.x, t);
+        if (it < p.kv_items) {
+          scores(true, t.n == 1);
+          if (ok) grads(true, t.n == 1);
+          step();
         }
-        if (step(ahead)) ahead_phase ^= 1u;
-        for (int i = 0; i < n && ok; ++i) {
-          const unsigned char *q = ring + stage * L::stage, *d = q + L::tile;
-          const unsigned char *q1 = ring + ahead * L::stage, *d1 = q1 + L::tile;
-          const bool more = i + 1 < n;
-          if (more && !wait(full + ahead, ahead_phase)) break;
-          if (!wait(p_full, i & 1)) break;
-          ptx::tc_fence_after_sync();
-          mma_weights<DP>(t_dv, t_s, d, kRows / 16, i != 0);
-          if (more) {
-            mma_rows<DP>(t_s, sk, q1);
-            ptx::umma_commit(s_full);
+        while (it < p.kv_items && ok) {
+          const int nit = with_work(it + gridDim.x, next);
+          const bool more = nit < p.kv_items;
+          for (int i = 0; i < t.n && ok; ++i) {
+            const unsigned char *q = ring + stage * L::stage, *d = q + L::tile;
+            const bool inner = i + 1 < t.n, fresh = !inner, last = inner ? i + 2 == t.n : next.n == 1;
+            if (i == 0 && !wait(o_empty, item_phase ^ 1u)) break;       // the item before has left tensor memory
+            if (!wait(p_full, turn)) break;
+            ptx::tc_fence_after_sync();
+            mma_weights<DP>(t_dv, t_s, d, kRows / 16, i != 0);
+            if (inner || more) scores(fresh, last);
+            if (!wait(ds_full, turn)) break;
+            ptx::tc_fence_after_sync();
+            mma_weights<DP>(t_dk, t_dp, q, kRows / 16, i != 0);
+            ptx::umma_commit(empty + stage);
+            if (!inner) ptx::umma_commit(o_full);
+            if (inner || more) {
+              grads(fresh, last);
+              step();
+            }
+            if (++stage == kStages) stage = 0;
+            turn ^= 1u;
           }
-          if (!wait(ds_full, i & 1)) break;
-          ptx::tc_fence_after_sync();
-          mma_weights<DP>(t_dk, t_dp, q, kRows / 16, i != 0);
-          ptx::umma_commit(empty + stage);
-          if (more) {
-            mma_rows<DP>(t_dp, sv, d1);
-            ptx::umma_commit(dp_full);
-          } else {
-            ptx::umma_commit(o_full);
-          }
-          step(stage);
-          if (step(ahead)) ahead_phase ^= 1u;
+          item_phase ^= 1u;
+          t = next;
+          it = nit;
         }
       }
     }
   } else {
-    // ------------------------------ scores: a thread per key, two threads' worth of queries -----------
+    // ------------------------------ scores: two threads per key, 64 queries each -----------------------
     ptx::registers_up<kScoreRegs>();
-    const int half = warp >> 2;               // queries [64 half, 64 half + 64) of a tile
+    const int half = warp >> 2;               // queries [64 half, 64 half + 64) of a tile; later dv (0) or dk (1)
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t my_s = t_s + half * 64 + lanes, my_dp = t_dp + half * 64 + lanes;
-    const float c = p.a.scale * kLog2e;
-    int stage = 0; uint32_t phase = 0;
-    for (int i = 0; i < n; ++i) {
-      const float4* lse4 = reinterpret_cast<const float4*>(stat + stage * 2 * kRows + half * 64);
-      const float4* delta4 = lse4 + kRows / 4;
-      bool here = ptx::mbar_wait(full + stage, phase, abort_flag) && ptx::mbar_wait(s_full, i & 1, abort_flag);
-      if (!__all_sync(0xffffffffu, here)) { ok = false; break; }
-      ptx::tc_fence_after_sync();
-      uint32_t s[64];
-      ptx::tmem_ld_32x32(my_s, s);
-      ptx::tmem_ld_32x32(my_s + 32, s + 32);
-      ptx::tmem_ld_wait();
-      uint32_t w[32];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float4 l = lse4[j];
-        const float m[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[4 * j + x] = __float_as_uint(exp2_approx(fmaf(__uint_as_float(s[4 * j + x]), c, -m[x])));
-        w[2 * j] = pack2(__uint_as_float(s[4 * j]), __uint_as_float(s[4 * j + 1]));
-        w[2 * j + 1] = pack2(__uint_as_float(s[4 * j + 2]), __uint_as_float(s[4 * j + 3]));
+    const f32x2 c2 = both(p.a.scale * kLog2e);
+    uint32_t turn = 0, item_phase = 0;
+    for (int it = blockIdx.x; it < p.kv_items && ok; it += gridDim.x) {
+      const KvItem t = kv_item_of(p, it);
+      if (t.n == 0) {                         // no key of this block counts, or there is no query
+        const int rows = min(kRows, p.a.Tk - t.k0);
+        __nv_bfloat16* dk = static_cast<__nv_bfloat16*>(p.a.dk) + ((long long)t.b * p.a.Tk + t.k0) * p.a.k_stride + (long long)t.kh * p.a.D;
+        __nv_bfloat16* dv = static_cast<__nv_bfloat16*>(p.a.dv) + ((long long)t.b * p.a.Tk + t.k0) * p.a.v_stride + (long long)t.kh * p.a.D;
+        for (int x = threadIdx.x; x < rows * (p.a.D / 8); x += 256) {
+          const int r = x / (p.a.D / 8), c = x % (p.a.D / 8) * 8;
+          *reinterpret_cast<uint4*>(dk + r * p.a.k_stride + c) = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(dv + r * p.a.v_stride + c) = make_uint4(0, 0, 0, 0);
+        }
+        continue;
       }
-      ptx::tmem_st_32x32(my_s, w);
-      ptx::tmem_st_wait();
+      for (int i = 0; i < t.n; ++i) {
+        if (!ptx::mbar_wait_all(s_full, turn, abort_flag)) { ok = false; break; }
+        ptx::tc_fence_after_sync();
+        uint32_t s[64];
+        ptx::tmem_ld_32x32(my_s, s);
+        ptx::tmem_ld_32x32(my_s + 32, s + 32);
+        ptx::tmem_ld_wait();
+        f32x2 pr[32];
+        uint32_t w[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float2 x = unpair(mul2(pair(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1])), c2));
+          const float e0 = exp2_approx(x.x), e1 = exp2_approx(x.y);
+          pr[j] = pair(e0, e1);
+          w[j] = pack2(e0, e1);
+        }
+        ptx::tmem_st_32x32(my_s, w);
+        ptx::tmem_st_wait();
+        ptx::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(p_full);
+        if (!ptx::mbar_wait_all(dp_full, turn, abort_flag)) { ok = false; break; }
+        ptx::tc_fence_after_sync();
+        ptx::tmem_ld_32x32(my_dp, s);
+        ptx::tmem_ld_32x32(my_dp + 32, s + 32);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float2 x = unpair(mul2(pr[j], pair(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1]))));
+          w[j] = pack2(x.x, x.y);
+        }
+        ptx::tmem_st_32x32(my_dp, w);
+        ptx::tmem_st_wait();
+        ptx::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(ds_full);
+        turn ^= 1u;
+      }
+      if (!ok || !ptx::mbar_wait_all(o_full, item_phase, abort_flag)) { ok = false; break; }
+      item_phase ^= 1u;
+      ptx::tc_fence_after_sync();
+      // rows of dv (the first four warps) or dk through the warp's staging rows, 32 columns at a time
+      const int row0 = t.k0 + (warp & 3) * 32;
+      const float factor = half == 0 ? 1.f : p.a.scale;
+      const bool zero = row0 + lane >= t.len;
+      unsigned char* stg = smem + L::out_off + warp * 32 * 64;
+      uint32_t o[DP];
+#pragma unroll
+      for (int j = 0; j < DP / 32; ++j) ptx::tmem_ld_32x32((half == 0 ? t_dv : t_dk) + lanes + j * 32, o + j * 32);
+      ptx::tmem_ld_wait();
       ptx::tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(p_full);
-      here = ptx::mbar_wait(dp_full, i & 1, abort_flag);
-      if (!__all_sync(0xffffffffu, here)) { ok = false; break; }
-      ptx::tc_fence_after_sync();
-      uint32_t g[64];
-      ptx::tmem_ld_32x32(my_dp, g);
-      ptx::tmem_ld_32x32(my_dp + 32, g + 32);
-      ptx::tmem_ld_wait();
+      if (lane == 0) ptx::mbar_arrive(o_empty);
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float4 l = delta4[j];
-        const float m[4] = {l.x, l.y, l.z, l.w};
-        float f[4];
+      for (int j = 0; j < DP / 32; ++j) {
+        uint32_t w[16];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) f[x] = __uint_as_float(s[4 * j + x]) * (__uint_as_float(g[4 * j + x]) - m[x]);
-        w[2 * j] = pack2(f[0], f[1]);
-        w[2 * j + 1] = pack2(f[2], f[3]);
+        for (int x = 0; x < 16; ++x)
+          w[x] = zero ? 0u : pack2(__uint_as_float(o[j * 32 + 2 * x]) * factor, __uint_as_float(o[j * 32 + 2 * x + 1]) * factor);
+        if (lane == 0) ptx::tma_store_wait_read();              // the store before has read the staging rows
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < 4; ++x) *reinterpret_cast<uint4*>(stg + lane * 64 + x * 16) = make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]);
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0 && row0 < p.a.Tk && j * 32 < p.a.D) {
+          ptx::tma_store_4d(half == 0 ? &map_dv : &map_dk, stg, j * 32, t.kh, row0, t.b);
+          ptx::tma_store_commit();
+        }
       }
-      ptx::tmem_st_32x32(my_dp, w);
-      ptx::tmem_st_wait();
-      ptx::tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(ds_full);
-      if (++stage == kStages) { stage = 0; phase ^= 1u; }
     }
-    if (ok && !__all_sync(0xffffffffu, ptx::mbar_wait(o_full, 0, abort_flag))) ok = false;
-    if (ok) {
-      ptx::tc_fence_after_sync();
-      const int r = threadIdx.x & 127;
-      const bool zero = k0 + r >= len;
-      if (half == 0) store_row<DP>(t_dv + lanes, dv + r * p.a.v_stride, 0, p.a.D, 1.f, r < rows, zero);
-      else store_row<DP>(t_dk + lanes, dk + r * p.a.k_stride, 0, p.a.D, p.a.scale, r < rows, zero);
-    }
+    if (lane == 0) ptx::tma_store_wait_all();
   }
 
   if (!ok) {
@@ -551,7 +655,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           for (int d = 0; d < p.a.D; d += 8) *reinterpret_cast<uint4*>(dq + d) = make_uint4(0, 0, 0, 0);
         continue;
       }
-      const float* stat = p.stats + (long long)i * 2 * kRows;
+      const float* stat = p.stats + (long long)i * kStatFloats;
       const float lse = __ldg(stat + r), delta = __ldg(stat + kRows + r);
       for (int j = 0; j * kRows < len; ++j) {
         const uint32_t my_s = tmem + (j & 1) * kRows + half * 64 + lanes, my_dp = t_dp + half * 64 + lanes;
@@ -615,14 +719,10 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 }
 
 template <typename K>
-int launch(K kernel, int blocks, int bytes, const CUtensorMap* m, const BackwardParams& p, cudaStream_t st) {
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
-    cudaGetLastError();
-    return GSHARD_ERR_CUDA;
-  }
-  kernel<<<blocks, kThreads, bytes, st>>>(m[0], m[1], m[2], m[3], p);
-  count_launch();
-  return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
+int allow_shared(K kernel, int bytes) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess) return GSHARD_OK;
+  cudaGetLastError();
+  return GSHARD_ERR_CUDA;
 }
 
 template <int DP>
@@ -633,27 +733,41 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   p.q_tiles = ceil_div(a.Tq, kRows);
   p.k_tiles = ceil_div(a.Tk, kRows);
   p.items = p.q_tiles * a.H * a.B;
+  p.kv_items = p.k_tiles * a.Hkv * a.B;
   if (p.items) {
     attention_stats_kernel<<<(unsigned)((long long)a.B * p.q_tiles * ceil_div(kRows * a.H, kStatRows)), 256, 0, st>>>(a, stats, p.q_tiles);
     count_launch();
   }
-  CUtensorMap m[4] = {};
-  // without queries no kernel looks at a map
-  if (a.Tq && (!make_token_map(&m[0], a.q, a.D, a.H, a.Tq, a.B, a.q_stride, kRows) || !make_source_map(&m[1], a, a.k, a.k_stride, kRows) ||
-               !make_source_map(&m[2], a, a.v, a.v_stride, kRows) ||
-               !make_token_map(&m[3], a.dout, a.D, a.H, a.Tq, a.B, (long long)a.H * a.D, kRows)))
+  CUtensorMap q, k, v, dout, dk, dv;
+  // Without queries or without keys the kernels write zeros and look through no map; they get valid ones all the same.
+  const AttentionArgs& s = a;
+  const bool both_there = a.Tq && a.Tk;
+  const long long o_stride = (long long)a.H * a.D;
+  const void* any = a.Tq ? a.q : a.k;
+  auto map = [&](CUtensorMap* m, const void* base, int heads, int tokens, long long stride, int box_tokens, int box_dims) {
+    return both_there ? make_token_map(m, base, s.D, heads, tokens, s.B, stride, box_tokens, box_dims)
+                      : make_token_map(m, any, s.D, 1, 1, 1, stride, box_tokens, box_dims);
+  };
+  if (!map(&q, a.q, a.H, a.Tq, a.q_stride, kRows, 64) || !map(&dout, a.dout, a.H, a.Tq, o_stride, kRows, 64) ||
+      !map(&k, a.k, a.Hkv, a.Tk, a.k_stride, kRows, 64) || !map(&v, a.v, a.Hkv, a.Tk, a.v_stride, kRows, 64) ||
+      !map(&dk, a.dk, a.Hkv, a.Tk, a.k_stride, 32, 32) || !map(&dv, a.dv, a.Hkv, a.Tk, a.v_stride, 32, 32))
     return GSHARD_ERR_CUDA;
-  if (a.Tk) {
-    const int rc = launch(attention_dkv_kernel<DP>, p.k_tiles * a.Hkv * a.B, KvLayout<DP>::bytes, m, p, st);
-    if (rc != GSHARD_OK) return rc;
+  if (p.kv_items) {
+    GS_CHECK(allow_shared(attention_dkv_kernel<DP>, KvLayout<DP>::bytes));
+    attention_dkv_kernel<DP><<<std::min(p.kv_items, device_sms()), kThreads, KvLayout<DP>::bytes, st>>>(q, k, v, dout, dk, dv, p);
+    count_launch();
   }
-  if (!a.Tq) return GSHARD_OK;
-  return launch(attention_dq_kernel<DP>, std::min(p.items, device_sms()), QLayout<DP>::bytes, m, p, st);
+  if (p.items) {
+    GS_CHECK(allow_shared(attention_dq_kernel<DP>, QLayout<DP>::bytes));
+    attention_dq_kernel<DP><<<std::min(p.items, device_sms()), kThreads, QLayout<DP>::bytes, st>>>(q, k, v, dout, p);
+    count_launch();
+  }
+  return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
 }
 
 }  // namespace
 
-size_t attention_stats_floats(int B, int Tq, int H) { return (size_t)ceil_div(Tq, kRows) * 2 * kRows * H * B; }
+size_t attention_stats_floats(int B, int Tq, int H) { return (size_t)ceil_div(Tq, kRows) * kStatFloats * H * B; }
 
 int launch_attention_umma_backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   return a.D <= 64 ? backward<64>(a, stats, st) : backward<128>(a, stats, st);

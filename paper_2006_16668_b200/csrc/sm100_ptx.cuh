@@ -252,6 +252,24 @@ __device__ __forceinline__ void umma_bf16_low(uint32_t d_tmem, uint32_t a_low, u
       : "r"(d_tmem), "r"(a_low), "r"(b_low), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
       : "memory");
 }
+// One K = 16 step of operands without swizzle, K-major: 8 x 8 elements (128 bytes) lie together, the two halves of K next to one
+// another, 8-row groups 256 bytes apart.
+constexpr uint32_t kPlainDescHigh = (256u >> 4) | (1u << 14);
+__device__ __forceinline__ uint32_t plain_desc_low(const void* p) { return (smem_u32(p) >> 4) | (128u >> 4) << 16; }
+__device__ __forceinline__ void umma_bf16_plain(uint32_t d_tmem, uint32_t a_low, uint32_t b_low, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      ".reg .b64 a, b;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 a, {%1, %5};\n\t"
+      "mov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t"
+      "}"
+      :
+      : "r"(d_tmem), "r"(a_low), "r"(b_low), "r"(idesc), "r"(accumulate), "n"(kPlainDescHigh)
+      : "memory");
+}
 // The same with A in tensor memory: lane = row, two consecutive k per 32-bit column.
 __device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_low, uint32_t idesc, uint32_t accumulate) {
   asm volatile(

@@ -48,7 +48,8 @@ inline bool make_map(CUtensorMap* map, const void* base, long long inner, long l
   return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess && encode();
 }
 
-// 4-D bf16 tensor map, 128-byte swizzle, strides (of the outer dimensions) in elements; outside reads as zero.
+// 4-D bf16 tensor map, 128-byte swizzle for boxes of 64 elements, else none; strides (of the outer dimensions) in elements; outside
+// reads as zero.
 inline bool make_map_4d(CUtensorMap* map, const void* base, const long long* dims_, const long long* strides_, const int* box_) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
@@ -58,7 +59,7 @@ inline bool make_map_4d(CUtensorMap* map, const void* base, const long long* dim
   for (int i = 0; i < 3; ++i) strides[i] = (cuuint64_t)strides_[i] * 2;
   auto encode = [&] {
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+              box_[0] == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   };
   if (encode()) return true;
   int device = 0;                              // a thread without a current context, as above
@@ -74,11 +75,11 @@ inline bool make_gated_map(CUtensorMap* map, const void* base, long long cols, l
 }
 
 // 4-D bf16 tensor map {head_dim, heads, tokens, batch} of a [batch, tokens, heads, head_dim] tensor whose tokens lie `stride`
-// elements apart, with boxes of 64 head dimensions by `box_tokens` tokens of one head, 128-byte swizzle; outside reads as zero.
+// elements apart, with boxes of `box_dims` head dimensions by `box_tokens` tokens of one head; outside reads as zero.
 inline bool make_token_map(CUtensorMap* map, const void* base, int head_dim, int heads, long long tokens, long long batch, long long stride,
-                           int box_tokens) {
+                           int box_tokens, int box_dims = 64) {
   const long long dims[4] = {head_dim, heads, tokens, batch}, strides[3] = {head_dim, stride, tokens * stride};
-  const int box[4] = {64, 1, box_tokens, 1};
+  const int box[4] = {box_dims, 1, box_tokens, 1};
   return make_map_4d(map, base, dims, strides, box);
 }
 
