@@ -49,10 +49,43 @@ __device__ __forceinline__ void put_terms(float v, unsigned short* out) {
   }
 }
 
+// Exclusive prefix over the sources of the blocks of 128 keys that dk and dv have work for ([B + 1]; none without queries); one block.
+__device__ void count_blocks(const AttentionArgs& a, int* prefix) {
+  __shared__ int warp_sum[8];
+  __shared__ int base;
+  if (threadIdx.x == 0) base = 0;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int b0 = 0; b0 < a.B; b0 += 256) {
+    const int b = b0 + threadIdx.x;
+    const int own = b < a.B && a.Tq > 0 ? ceil_div(source_length(a, b), kRows) : 0;
+    int v = own;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, v, off);
+      if (lane >= off) v += o;
+    }
+    __syncthreads();
+    if (lane == 31) warp_sum[warp] = v;
+    __syncthreads();
+    int before = base;
+    for (int w = 0; w < warp; ++w) before += warp_sum[w];
+    if (b < a.B) prefix[b] = before + v - own;
+    __syncthreads();
+    if (threadIdx.x == 255) base = before + v;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) prefix[a.B] = base;
+}
+
 // A block takes 64 (query, head) rows of a tile, 16 lanes a row and four rows of
 // a group in flight; neighbouring rows are the heads of a token, which lie together in o and dout.
 constexpr int kStatRows = 64;
-__global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArgs a, float* stats, int q_tiles) {
+// The last block counts the sources' blocks.
+__global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArgs a, float* stats, int* prefix, int q_tiles) {
+  if (blockIdx.x == gridDim.x - 1) {
+    count_blocks(a, prefix);
+    return;
+  }
   constexpr int U = kStatRows / 16;
   const int part = threadIdx.x & 15, grp = threadIdx.x >> 4, c = part * 8;
   const int parts = ceil_div(kRows * a.H, kStatRows);
@@ -99,7 +132,8 @@ struct BackwardParams {
   AttentionArgs a;
   const float* stats;
   int q_tiles, k_tiles;
-  int items, kv_items;                        // of dq, of dk and dv
+  int items;                                  // of dq
+  const int* prefix;                          // see count_blocks
 };
 
 // zeroes the rows [from, to) of a tile of 128 rows x DP bf16 in two or one swizzled halves (zeros need no swizzle); whole warp
@@ -187,14 +221,40 @@ template <int DP> struct KvLayout {
 
 struct KvItem { int b, kh, k0, n, len; };      // n: query tiles to walk
 
+// The i-th block of keys that has work: by source, key head, block, so that the blocks that walk the same queries run together and
+// every CTA gets its share whatever the lengths are.
 __device__ __forceinline__ KvItem kv_item_of(const BackwardParams& p, int i) {
+  int lo = 0, hi = p.a.B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (__ldg(p.prefix + mid) * p.a.Hkv <= i) lo = mid; else hi = mid - 1;
+  }
   KvItem t;
-  t.k0 = i % p.k_tiles * kRows;
-  t.kh = i / p.k_tiles % p.a.Hkv;
-  t.b = i / p.k_tiles / p.a.Hkv;
-  t.len = source_length(p.a, t.b);
-  t.n = t.k0 < t.len ? p.a.H / p.a.Hkv * p.q_tiles : 0;
+  t.b = lo;
+  const int first = __ldg(p.prefix + lo), count = __ldg(p.prefix + lo + 1) - first, r = i - first * p.a.Hkv;
+  t.kh = r / count;
+  t.k0 = r % count * kRows;
+  t.len = source_length(p.a, lo);
+  t.n = p.a.H / p.a.Hkv * p.q_tiles;
   return t;
+}
+// The blocks of keys that have none are zero: the z-th of them.
+__device__ __forceinline__ void zero_block(const BackwardParams& p, int z) {
+  int lo = 0, hi = p.a.B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if ((mid * p.k_tiles - __ldg(p.prefix + mid)) * p.a.Hkv <= z) lo = mid; else hi = mid - 1;
+  }
+  const int first = lo * p.k_tiles - __ldg(p.prefix + lo), worked = __ldg(p.prefix + lo + 1) - __ldg(p.prefix + lo);
+  const int r = z - first * p.a.Hkv, kh = r / (p.k_tiles - worked), k0 = (worked + r % (p.k_tiles - worked)) * kRows;
+  const int rows = min(kRows, p.a.Tk - k0);
+  __nv_bfloat16* dk = static_cast<__nv_bfloat16*>(p.a.dk) + ((long long)lo * p.a.Tk + k0) * p.a.k_stride + (long long)kh * p.a.D;
+  __nv_bfloat16* dv = static_cast<__nv_bfloat16*>(p.a.dv) + ((long long)lo * p.a.Tk + k0) * p.a.v_stride + (long long)kh * p.a.D;
+  for (int x = threadIdx.x; x < rows * (p.a.D / 8); x += kThreads) {
+    const int row = x / (p.a.D / 8), c = x % (p.a.D / 8) * 8;
+    *reinterpret_cast<uint4*>(dk + row * p.a.k_stride + c) = make_uint4(0, 0, 0, 0);
+    *reinterpret_cast<uint4*>(dv + row * p.a.v_stride + c) = make_uint4(0, 0, 0, 0);
+  }
 }
 
 template <int DP>
@@ -255,14 +315,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
   const uint32_t tmem = *tmem_slot;
   const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DP;
 
-  // the next item from i on that has query tiles to walk
-  auto with_work = [&](int i, KvItem& t) {
-    for (; i < p.kv_items; i += gridDim.x) {
-      t = kv_item_of(p, i);
-      if (t.n > 0) break;
-    }
-    return i;
-  };
+  const int items = __ldg(p.prefix + p.a.B) * p.a.Hkv, zeros = p.k_tiles * p.a.B * p.a.Hkv - items;
+  for (int z = blockIdx.x; z < zeros; z += gridDim.x) zero_block(p, z);
   bool ok = true;
   if (warp >= 8) {
     ptx::registers_down<kOtherRegs>();
@@ -271,8 +325,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       if (lane == 0) {
         const uint64_t again = ptx::policy_evict_last(), once = ptx::policy_evict_first();
         int stage = 0; uint32_t phase = 0, kv_phase = 0;
-        KvItem t;
-        for (int it = with_work(blockIdx.x, t); it < p.kv_items && ok; it = with_work(it + gridDim.x, t)) {
+        for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+          const KvItem t = kv_item_of(p, it);
           if (!ptx::mbar_wait(k_empty, kv_phase ^ 1u, abort_flag)) { ok = false; break; }
           ptx::mbar_arrive_expect_tx(k_full, L::tile);
           load_rows<DP>(sk, &map_k, k_full, t.kh, t.k0, t.b, once);
@@ -323,19 +377,17 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           if (last) ptx::umma_commit(v_empty);
         };
         auto step = [&] { if (++ahead == kStages) { ahead = 0; ahead_phase ^= 1u; } };
-        KvItem t, next;
-        int it = with_work(blockIdx.x, t);
-        if (it < p.kv_items) {
-          scores(true, t.n == 1);
-          if (ok) grads(true, t.n == 1);
+        const int n = group * p.q_tiles;
+        if ((int)blockIdx.x < items) {
+          scores(true, n == 1);
+          if (ok) grads(true, n == 1);
           step();
         }
-        while (it < p.kv_items && ok) {
-          const int nit = with_work(it + gridDim.x, next);
-          const bool more = nit < p.kv_items;
-          for (int i = 0; i < t.n && ok; ++i) {
+        for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+          const bool more = it + (int)gridDim.x < items;
+          for (int i = 0; i < n && ok; ++i) {
             const unsigned char *q = ring + stage * L::stage, *d = q + L::tile;
-            const bool inner = i + 1 < t.n, fresh = !inner, last = inner ? i + 2 == t.n : next.n == 1;
+            const bool inner = i + 1 < n, fresh = !inner, last = inner ? i + 2 == n : n == 1;
             if (i == 0 && !wait(o_empty, item_phase ^ 1u)) break;       // the item before has left tensor memory
             if (!wait(p_full, turn)) break;
             ptx::tc_fence_after_sync();
@@ -354,8 +406,6 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             turn ^= 1u;
           }
           item_phase ^= 1u;
-          t = next;
-          it = nit;
         }
       }
     }
@@ -367,19 +417,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const uint32_t my_s = t_s + half * 64 + lanes, my_dp = t_dp + half * 64 + lanes;
     const f32x2 c2 = both(p.a.scale * kLog2e);
     uint32_t turn = 0, item_phase = 0;
-    for (int it = blockIdx.x; it < p.kv_items && ok; it += gridDim.x) {
+    for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
       const KvItem t = kv_item_of(p, it);
-      if (t.n == 0) {                         // no key of this block counts, or there is no query
-        const int rows = min(kRows, p.a.Tk - t.k0);
-        __nv_bfloat16* dk = static_cast<__nv_bfloat16*>(p.a.dk) + ((long long)t.b * p.a.Tk + t.k0) * p.a.k_stride + (long long)t.kh * p.a.D;
-        __nv_bfloat16* dv = static_cast<__nv_bfloat16*>(p.a.dv) + ((long long)t.b * p.a.Tk + t.k0) * p.a.v_stride + (long long)t.kh * p.a.D;
-        for (int x = threadIdx.x; x < rows * (p.a.D / 8); x += 256) {
-          const int r = x / (p.a.D / 8), c = x % (p.a.D / 8) * 8;
-          *reinterpret_cast<uint4*>(dk + r * p.a.k_stride + c) = make_uint4(0, 0, 0, 0);
-          *reinterpret_cast<uint4*>(dv + r * p.a.v_stride + c) = make_uint4(0, 0, 0, 0);
-        }
-        continue;
-      }
       for (int i = 0; i < t.n; ++i) {
         if (!ptx::mbar_wait_all(s_full, turn, abort_flag)) { ok = false; break; }
         ptx::tc_fence_after_sync();
@@ -733,11 +772,11 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   p.q_tiles = ceil_div(a.Tq, kRows);
   p.k_tiles = ceil_div(a.Tk, kRows);
   p.items = p.q_tiles * a.H * a.B;
-  p.kv_items = p.k_tiles * a.Hkv * a.B;
-  if (p.items) {
-    attention_stats_kernel<<<(unsigned)((long long)a.B * p.q_tiles * ceil_div(kRows * a.H, kStatRows)), 256, 0, st>>>(a, stats, p.q_tiles);
-    count_launch();
-  }
+  const int kv_items = p.k_tiles * a.Hkv * a.B;
+  int* prefix = reinterpret_cast<int*>(stats + (size_t)p.items * kStatFloats);
+  p.prefix = prefix;
+  attention_stats_kernel<<<(unsigned)((long long)a.B * p.q_tiles * ceil_div(kRows * a.H, kStatRows) + 1), 256, 0, st>>>(a, stats, prefix, p.q_tiles);
+  count_launch();
   CUtensorMap q, k, v, dout, dk, dv;
   // Without queries or without keys the kernels write zeros and look through no map; they get valid ones all the same.
   const AttentionArgs& s = a;
@@ -752,9 +791,9 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
       !map(&k, a.k, a.Hkv, a.Tk, a.k_stride, kRows, 64) || !map(&v, a.v, a.Hkv, a.Tk, a.v_stride, kRows, 64) ||
       !map(&dk, a.dk, a.Hkv, a.Tk, a.k_stride, 32, 32) || !map(&dv, a.dv, a.Hkv, a.Tk, a.v_stride, 32, 32))
     return GSHARD_ERR_CUDA;
-  if (p.kv_items) {
+  if (kv_items) {
     GS_CHECK(allow_shared(attention_dkv_kernel<DP>, KvLayout<DP>::bytes));
-    attention_dkv_kernel<DP><<<std::min(p.kv_items, device_sms()), kThreads, KvLayout<DP>::bytes, st>>>(q, k, v, dout, dk, dv, p);
+    attention_dkv_kernel<DP><<<std::min(kv_items, device_sms()), kThreads, KvLayout<DP>::bytes, st>>>(q, k, v, dout, dk, dv, p);
     count_launch();
   }
   if (p.items) {
@@ -767,7 +806,7 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
 
 }  // namespace
 
-size_t attention_stats_floats(int B, int Tq, int H) { return (size_t)ceil_div(Tq, kRows) * kStatFloats * H * B; }
+size_t attention_stats_floats(int B, int Tq, int H) { return (size_t)ceil_div(Tq, kRows) * kStatFloats * H * B + B + 1; }
 
 int launch_attention_umma_backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   return a.D <= 64 ? backward<64>(a, stats, st) : backward<128>(a, stats, st);
