@@ -93,9 +93,11 @@ __global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArg
   const int b = (int)(tile / q_tiles), t0 = (int)(tile % q_tiles) * kRows;
   const int r0 = (int)(blockIdx.x % parts) * kStatRows + grp;
   Pack<__nv_bfloat16, 8> x[U], y[U];
+  float lse[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int r = r0 + u * 16, t = t0 + r / a.H, h = r % a.H;
+    lse[u] = part == 0 && r < kRows * a.H && t < a.Tq ? a.lse[((long long)b * a.H + h) * a.Tq + t] : 0.f;
     x[u].raw = y[u].raw = make_uint4(0, 0, 0, 0);
     if (r < kRows * a.H && t < a.Tq && c < a.D) {
       const long long off = (((long long)b * a.Tq + t) * a.H + h) * a.D + c;
@@ -115,11 +117,10 @@ __global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArg
       const long long head = (long long)b * a.H + h;
       float* out = stats + (head * q_tiles + t0 / kRows) * kStatFloats;
       const int row = r / a.H;
-      const float lse = t < a.Tq ? a.lse[head * a.Tq + t] : 0.f;
-      out[row] = t < a.Tq ? lse * kLog2e : INFINITY;
+      out[row] = t < a.Tq ? lse[u] * kLog2e : INFINITY;
       out[kRows + row] = delta;
       alignas(16) unsigned short terms[8] = {};
-      put_terms(t < a.Tq ? -lse / a.scale : -1e30f, terms);
+      put_terms(t < a.Tq ? -lse[u] / a.scale : -1e30f, terms);
       put_terms(-delta, terms + 3);
       uint4* step = reinterpret_cast<uint4*>(out + 2 * kRows) + row / 8 * 16 + row % 8;
       step[0] = *reinterpret_cast<const uint4*>(terms);
@@ -538,15 +539,14 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   uint64_t* dp_full = s_full + 2;
   uint64_t* ds_full = dp_full + 1;            // 8 warps: dS written, dP read
   uint64_t* o_full = ds_full + 1;
-  uint64_t* k_clean = o_full + 1;             // rows behind the last key zeroed
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(k_clean + 1);
+  uint64_t* k_clean = o_full + 1;             // [kK] looked through for rows behind the last key
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(k_clean + kK);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int group = p.a.H / p.a.Hkv;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kK; ++s) { ptx::mbar_init(k_full + s, 1); ptx::mbar_init(k_empty + s, 2); }
-    ptx::mbar_init(k_clean, 1);
+    for (int s = 0; s < kK; ++s) { ptx::mbar_init(k_full + s, 1); ptx::mbar_init(k_empty + s, 2); ptx::mbar_init(k_clean + s, 1); }
     for (int s = 0; s < kV; ++s) { ptx::mbar_init(v_full + s, 1); ptx::mbar_init(v_empty + s, 1); }
     ptx::mbar_init(q_full, 1); ptx::mbar_init(q_empty, 1);
     ptx::mbar_init(s_full, 1); ptx::mbar_init(s_full + 1, 1); ptx::mbar_init(dp_full, 1);
@@ -597,6 +597,13 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           ptx::mbar_arrive_expect_tx(q_full, 2 * L::tile);
           load_rows<DP>(sq, &map_q, q_full, h, i % p.q_tiles * kRows, b, once);
           load_rows<DP>(sd, &map_do, q_full, h, i % p.q_tiles * kRows, b, once);
+          if (const int n = i + gridDim.x; n < p.items) {         // the next item's rows into L2: they are loaded only when these have been read
+#pragma unroll
+            for (int j = 0; j < DP / 64; ++j) {
+              ptx::tma_prefetch_4d(&map_q, j * 64, head_of(n), n % p.q_tiles * kRows, batch_of(n));
+              ptx::tma_prefetch_4d(&map_do, j * 64, head_of(n), n % p.q_tiles * kRows, batch_of(n));
+            }
+          }
           for (int k0 = 0; k0 < len && ok; k0 += kRows) {
             if (!ptx::mbar_wait(v_empty + vs, v_phase ^ 1u, abort_flag)) { ok = false; break; }
             ptx::mbar_arrive_expect_tx(v_full + vs, L::tile);
@@ -610,7 +617,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       // ------------------------------ MMA issuer (one elected thread runs all of it) ------------------
       if (ptx::elect_one()) {
         int ks = 0, vs = 0, ds = 0;           // ring positions of the next S, the next dP and the next dq
-        uint32_t k_phase = 0, v_phase = 0, q_phase = 0, ds_phase = 0, clean_phase = 0;
+        uint32_t k_phase = 0, v_phase = 0, q_phase = 0, ds_phase = 0;
         auto wait = [&](uint64_t* bar, uint32_t parity) {
           if (ok) ok = ptx::mbar_wait(bar, parity, abort_flag);
           return ok;
@@ -621,10 +628,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           const int blocks = ceil_div(len, kRows);
           auto scores = [&](int j) {
             if (!wait(k_full + ks, k_phase)) return;
-            if (j == blocks - 1 && ragged(len)) {
-              if (!wait(k_clean, clean_phase)) return;
-              clean_phase ^= 1u;
-            }
+            if (j == blocks - 1 && ragged(len) && !wait(k_clean + ks, k_phase)) return;
             mma_rows<DP>(tmem + (j & 1) * kRows, sq, sk + ks * L::tile);
             ptx::umma_commit(s_full + (j & 1));
             if (++ks == kK) { ks = 0; k_phase ^= 1u; }
@@ -667,11 +671,11 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         for (int k0 = 0; k0 < len; k0 += kRows) {
           if (!ptx::mbar_wait_all(k_full + ks, k_phase, abort_flag)) { ok = false; break; }
           const int left = len - k0;
-          if (left <= kRows && ragged(len)) {
-            zero_rows<DP>(sk + ks * L::tile, left, (left + 15) & ~15, lane);
-            if (lane == 0) ptx::mbar_arrive(k_clean);
+          if (left <= kRows && ragged(len)) zero_rows<DP>(sk + ks * L::tile, left, (left + 15) & ~15, lane);
+          if (lane == 0) {
+            ptx::mbar_arrive(k_clean + ks);
+            ptx::mbar_arrive(k_empty + ks);
           }
-          if (lane == 0) ptx::mbar_arrive(k_empty + ks);
           if (++ks == kK) { ks = 0; k_phase ^= 1u; }
         }
       }

@@ -107,14 +107,13 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
   uint64_t* o_full = p_full + 2;              // [2] output complete
   uint64_t* o_empty = o_full + 2;             // [2] output and statistics read (4 warps)
   uint64_t* stat_full = o_empty + 2;          // [2] statistics written (4 warps)
-  uint64_t* v_clean = stat_full + 2;          // rows behind the last key zeroed
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(v_clean + 1);
+  uint64_t* v_clean = stat_full + 2;          // [kStages] looked through for rows behind the last key
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(v_clean + kStages);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { ptx::mbar_init(kv_full + s, 1); ptx::mbar_init(kv_empty + s, 2); }
-    ptx::mbar_init(v_clean, 1);
+    for (int s = 0; s < kStages; ++s) { ptx::mbar_init(kv_full + s, 1); ptx::mbar_init(kv_empty + s, 2); ptx::mbar_init(v_clean + s, 1); }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(q_full + i, 1); ptx::mbar_init(q_empty + i, 1);
       ptx::mbar_init(s_full + i, 1); ptx::mbar_init(p_full + i, 4);
@@ -213,7 +212,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         constexpr uint32_t idesc_s = ptx::make_idesc_bf16(kRows, kRows, false, false);
         constexpr uint32_t idesc_o = ptx::make_idesc_bf16(kRows, DP, false, true);
         int stage = 0; uint32_t phase = 0;
-        uint32_t q_phase = 0, p_phase = 0, o_phase = 0, clean_phase = 0;           // bit `half`
+        uint32_t q_phase = 0, p_phase = 0, o_phase = 0;           // bit `half`
         auto wait = [&](uint64_t* bar, uint32_t parity) {
           if (ok) ok = ptx::mbar_wait(bar, parity & 1u, abort_flag);
           return ok;
@@ -251,10 +250,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
             const int s_tiles = inner ? t.tiles : more ? n.tiles : 0;
             const bool s_last = inner ? j + 2 == blocks : n.len <= kRows;
             if (!wait(kv_full + stage, phase)) break;
-            if (!inner && ragged(t)) {
-              if (!wait(v_clean, clean_phase)) break;
-              clean_phase ^= 1u;
-            }
+            if (!inner && ragged(t) && !wait(v_clean + stage, phase)) break;
             const uint32_t dv = ptx::smem_desc_low(ring + stage * L::stage, kRows * 128);
             for (int half = 0; half < 2 && ok; ++half) {
               if (half < t.tiles) {
@@ -299,9 +295,11 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
           }
           ptx::fence_proxy_async();
           __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(v_clean);
         }
-        if (lane == 0) ptx::mbar_arrive(kv_empty + stage);
+        if (lane == 0) {
+          ptx::mbar_arrive(v_clean + stage);
+          ptx::mbar_arrive(kv_empty + stage);
+        }
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       };
       Item t;
