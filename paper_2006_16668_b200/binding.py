@@ -619,22 +619,30 @@ def gshard_moe_route_backward(route, logits, expert_idx, dweight, dlogits, dm=No
 
 def _tokens(t, name, shape, dtype, device):
     """(pointer, token stride) of a [batch, tokens, heads, head_dim] tensor whose rows of heads are dense and may lie apart."""
-    st = t.stride()
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
         raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the device of the first tensor, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}")
     B, T, H, D = shape
-    row = st[1] if T > 1 else (st[0] if B > 1 else H * D)
-    if t.numel() and ((st[3] != 1 and D > 1) or (st[2] != D and H > 1) or (B > 1 and st[0] != T * row)):
-        raise ValueError(f"{name}: strides {st}; heads of a token must be dense, and batch elements follow one another")
+    if t.is_contiguous():
+        return t.data_ptr(), H * D
+    b, row, h, d = t.stride()
+    if T == 1:
+        row = b if B > 1 else H * D
+    if (d != 1 and D > 1) or (h != D and H > 1) or (B > 1 and b != T * row):
+        raise ValueError(f"{name}: strides {t.stride()}; heads of a token must be dense, and batch elements follow one another")
     return t.data_ptr(), row
 
 
 def _attention(q, k, v, scale):
-    code, dev = _code_of(q.dtype, "q"), q.get_device()
-    (B, Tq, H, D), (Tk, Hkv) = q.shape, k.shape[1:3]
-    (pq, sq), (pk, sk), (pv, sv) = (_tokens(q, "q", q.shape, q.dtype, dev), _tokens(k, "k", (B, Tk, Hkv, D), q.dtype, dev),
-                                    _tokens(v, "v", (B, Tk, Hkv, D), q.dtype, dev))
+    dtype, dev, q_shape, k_shape = q.dtype, q.get_device(), q.shape, k.shape
+    code = _code_of(dtype, "q")
+    if len(q_shape) != 4 or len(k_shape) != 4:
+        raise ValueError(f"q, k: expected [batch, tokens, heads, head_dim], got {tuple(q_shape)} and {tuple(k_shape)}")
+    B, Tq, H, D = q_shape
+    _, Tk, Hkv, _ = k_shape
+    pq, sq = _tokens(q, "q", q_shape, dtype, dev)
+    pk, sk = _tokens(k, "k", (B, Tk, Hkv, D), dtype, dev)
+    pv, sv = _tokens(v, "v", (B, Tk, Hkv, D), dtype, dev)
     if (Tq | Tk | B | H) >> 31:
         _size32(batch=B, q_len=Tq, k_len=Tk, heads=H)
     return (gshard_attention_config(B, Tq, Tk, H, Hkv, D, code, D ** -0.5 if scale is None else scale, sq, sk, sv), dev,

@@ -33,12 +33,14 @@ __global__ void __launch_bounds__(256) attention_delta_kernel(const AttentionArg
   }
 }
 
-struct AttentionPlan { size_t status, delta, total; };
+struct AttentionPlan { size_t status, parts, delta, total; };
 
 AttentionPlan attention_plan(const gshard_attention_config& c, bool backward) {
   Carver w;
   AttentionPlan p{};
   p.status = w.take(256);
+  if (!backward && c.dtype == GSHARD_BF16 && !attention_is_few(c.q_len, c.heads, c.kv_heads))
+    p.parts = w.take(4 * attention_parts_floats(c.batch, c.q_len, c.k_len, c.heads, c.kv_heads, c.head_dim));
   if (backward)
     p.delta = w.take(4 * (c.dtype == GSHARD_BF16 ? attention_stats_floats(c.batch, c.q_len, c.heads) : (size_t)c.batch * c.heads * c.q_len));
   p.total = w.off;
@@ -105,7 +107,8 @@ int gshard_cross_attention_forward(const gshard_attention_config* config, const 
   if (c.k_len) { GS_CHECK_PTR(k); GS_CHECK_PTR(v); }
   if (reinterpret_cast<uintptr_t>(k_lengths) % 4) return GSHARD_ERR_INVALID_ARG;
   if (o == q || o == k || o == v || o == lse) return GSHARD_ERR_INVALID_ARG;
-  GS_CHECK_WORKSPACE(workspace, workspace_bytes, attention_plan(c, false).total);
+  const AttentionPlan pl = attention_plan(c, false);
+  GS_CHECK_WORKSPACE(workspace, workspace_bytes, pl.total);
   GS_CHECK(check_device());
   NvtxRange range("gshard.attention");
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -114,7 +117,8 @@ int gshard_cross_attention_forward(const gshard_attention_config* config, const 
   const bool bf16 = c.dtype == GSHARD_BF16;
   if (attention_is_few(a.Tq, a.H, a.Hkv)) return launch_attention_few(a, bf16, st);
   GS_CHECK(clear_status(workspace, st));
-  return bf16 ? launch_attention_umma_forward(a, st) : launch_attention_simt_forward(a, st);
+  return bf16 ? launch_attention_umma_forward(a, reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + pl.parts), st)
+              : launch_attention_simt_forward(a, st);
 }
 
 int gshard_cross_attention_backward(const gshard_attention_config* config, const void* q, const void* k, const void* v,

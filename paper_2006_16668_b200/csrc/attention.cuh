@@ -35,8 +35,10 @@ int launch_attention_few(const AttentionArgs& a, bool bf16, cudaStream_t st);
 int launch_attention_simt_forward(const AttentionArgs& a, cudaStream_t st);
 int launch_attention_simt_backward(const AttentionArgs& a, cudaStream_t st);
 
-// attention_umma.cu, attention_backward.cu: bf16 on the tensor cores.  stats: attention_stats_floats() floats of scratch
-int launch_attention_umma_forward(const AttentionArgs& a, cudaStream_t st);
+// attention_umma.cu, attention_backward.cu: bf16 on the tensor cores.  scratch, stats: attention_parts_floats() and
+// attention_stats_floats() floats
+size_t attention_parts_floats(int B, int Tq, int Tk, int H, int Hkv, int D);
+int launch_attention_umma_forward(const AttentionArgs& a, float* scratch, cudaStream_t st);
 size_t attention_stats_floats(int B, int Tq, int H);
 int launch_attention_umma_backward(const AttentionArgs& a, float* stats, cudaStream_t st);
 

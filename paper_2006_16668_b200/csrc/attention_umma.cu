@@ -14,6 +14,9 @@
 // next item follow the last block's, and a fourth warpgroup takes the finished output from tensor memory, divides it by its sums
 // and sends it off through shared memory (bulk tensor stores) while the next item's first block is being worked on.
 //
+// Where the items do not fill the GPU and the source is long, an item is one of several parts of the source: it leaves its output in fp32
+// and the logarithm of its sums, and a second launch joins them in order (one head, 64 queries, 32768 keys: SPLIT_FIGURES us).
+//
 // Rows behind the source's length: scores are masked before the maximum; rows of V that hold something else are zeroed in
 // shared memory up to the next multiple of 16, where the last block's product ends.
 #include <algorithm>
@@ -47,24 +50,30 @@ template <int DP> struct Layout {
 struct Tile { int h, q0, rows; };             // a 128-row tile of one head
 
 struct Item {
-  int b, kh, first, tiles, len;               // the tiles first, first + 1 (or only the first) of the key head's list
+  int b, kh, first, tiles;                    // the tiles first, first + 1 (or only the first) of the key head's list
+  int part, k0, len;                          // keys [k0, k0 + len)
 };
 
 struct ForwardParams {
   AttentionArgs a;
   int q_tiles;                                // tiles per head
   int list;                                   // tiles per key head
-  int pairs;                                  // items per key head
+  int pairs;                                  // items per key head and part
   int items;
+  int parts, part_keys;                       // parts of a source, a multiple of 128 keys each
+  float* part_o; float* part_lse;             // parts > 1: [parts][B, Tq, H, D] and (powers of two) [parts][B, Tq, H]
 };
 
 __device__ __forceinline__ Item item_of(const ForwardParams& p, int i) {
   Item t;
+  t.part = i % p.parts;
+  i /= p.parts;
   t.first = i % p.pairs * 2;
   t.kh = i / p.pairs % p.a.Hkv;
   t.b = i / p.pairs / p.a.Hkv;
   t.tiles = min(2, p.list - t.first);
-  t.len = source_length(p.a, t.b);
+  t.k0 = t.part * p.part_keys;
+  t.len = min(max(source_length(p.a, t.b) - t.k0, 0), p.part_keys);
   return t;
 }
 __device__ __forceinline__ Tile tile_of(const ForwardParams& p, const Item& t, int half) {
@@ -147,7 +156,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
   };
   // Whether the last block of an item has rows between its last key and the next multiple of 16, where its product ends, that TMA
   // has not zeroed.
-  auto ragged = [&](const Item& t) { return (t.len & 15) != 0 && t.len < p.a.Tk; };
+  auto ragged = [&](const Item& t) { return (t.len & 15) != 0 && t.k0 + t.len < p.a.Tk; };
   if (warp >= 12) {
     ptx::registers_down<kOtherRegs>();
     if (warp == 12) {
@@ -175,7 +184,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         int i = with_keys(blockIdx.x, t);
         if (i < p.items) {
           ptx::mbar_arrive_expect_tx(kv_full, L::tile);
-          load(&map_k, L::tile, t.kh, 0, t.b);
+          load(&map_k, L::tile, t.kh, t.k0, t.b);
           stage = 1;
           for (int half = 0; half < t.tiles && ok; ++half) load_queries(t, half);
         }
@@ -192,9 +201,9 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
             const bool inner = k0 + kRows < t.len, keys = inner || more;
             if (!ptx::mbar_wait(kv_empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
             ptx::mbar_arrive_expect_tx(kv_full + stage, keys ? L::stage : L::tile);
-            load(&map_v, 0, t.kh, k0, t.b);
-            if (inner) load(&map_k, L::tile, t.kh, k0 + kRows, t.b);
-            else if (more) load(&map_k, L::tile, n.kh, 0, n.b);
+            load(&map_v, 0, t.kh, t.k0 + k0, t.b);
+            if (inner) load(&map_k, L::tile, t.kh, t.k0 + k0 + kRows, t.b);
+            else if (more) load(&map_k, L::tile, n.kh, n.k0, n.b);
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
           if (more)
@@ -324,7 +333,9 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
       for (int half = 0; half < t.tiles && ok; ++half) {
         const Tile q = tile_of(p, t, half);
         const int r = (warp & 3) * 32 + lane;
-        float* lse = p.a.lse && r < q.rows ? p.a.lse + ((long long)t.b * p.a.H + q.h) * p.a.Tq + q.q0 + r : nullptr;
+        const bool in = r < q.rows, whole = p.parts == 1;
+        float* lse = p.a.lse && in && whole ? p.a.lse + ((long long)t.b * p.a.H + q.h) * p.a.Tq + q.q0 + r : nullptr;
+        const long long part_row = whole ? 0 : (((long long)t.part * p.a.B + t.b) * p.a.Tq + q.q0 + r) * p.a.H + q.h;
         float factor = 0.f;
         if (t.len > 0) {
           bool here = ptx::mbar_wait(stat_full + half, (phase >> half) & 1u, abort_flag) &&
@@ -335,8 +346,31 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
           const float sum = stat[half * 2 * kRows + r], top = stat[half * 2 * kRows + kRows + r];
           factor = 1.f / sum;
           if (lse) *lse = top * p.a.scale + logf(sum);
-        } else if (lse) {
-          *lse = -INFINITY;
+          if (!whole && in) p.part_lse[part_row] = fmaf(top, p.a.scale * kLog2e, log2f(sum));
+        } else {
+          if (lse) *lse = -INFINITY;
+          if (!whole && in) p.part_lse[part_row] = -INFINITY;
+        }
+        if (!whole) {                          // a part's output, in fp32; nothing where it had no key
+          if (t.len == 0) continue;
+#pragma unroll
+          for (int c = 0; c < DP / 32; ++c) {
+            uint32_t o[32];
+            ptx::tmem_ld_32x32(tmem_o + half * DP + c * 32 + lanes, o);
+            ptx::tmem_ld_wait();
+            if (c == DP / 32 - 1) {
+              ptx::tc_fence_before_sync();
+              __syncwarp();
+              if (lane == 0) ptx::mbar_arrive(o_empty + half);
+            }
+#pragma unroll
+            for (int x = 0; x < 32; x += 4)
+              if (in && c * 32 + x < p.a.D)
+                *reinterpret_cast<float4*>(p.part_o + part_row * p.a.D + c * 32 + x) =
+                    make_float4(__uint_as_float(o[x]) * factor, __uint_as_float(o[x + 1]) * factor, __uint_as_float(o[x + 2]) * factor,
+                                __uint_as_float(o[x + 3]) * factor);
+          }
+          continue;
         }
         // 64 columns at a time through the warp's staging rows
 #pragma unroll
@@ -482,14 +516,58 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
   }
 }
 
+// Joins the parts of a source: o = sum of w_p o_p with w_p = 2^(lse_p) over their sum; one warp per (token, head).
+__global__ void __launch_bounds__(256) attention_join_kernel(const ForwardParams p, long long rows) {
+  const int lane = threadIdx.x & 31, c = lane * 4;
+  for (long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += (long long)gridDim.x * 8) {
+    float top = -INFINITY;
+    for (int i = 0; i < p.parts; ++i) top = fmaxf(top, p.part_lse[i * rows + r]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < p.parts; ++i) {
+      const float lse = p.part_lse[i * rows + r];
+      if (lse == -INFINITY) continue;          // no key in this part
+      const float w = exp2f(lse - ref);
+      sum += w;
+      if (c < p.a.D) {
+        const float4 x = *reinterpret_cast<const float4*>(p.part_o + (i * rows + r) * p.a.D + c);
+        o[0] = fmaf(w, x.x, o[0]); o[1] = fmaf(w, x.y, o[1]); o[2] = fmaf(w, x.z, o[2]); o[3] = fmaf(w, x.w, o[3]);
+      }
+    }
+    const float factor = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] *= factor;
+    if (c < p.a.D) store_pack<__nv_bfloat16, 4>(static_cast<__nv_bfloat16*>(p.a.o) + r * p.a.D + c, o);
+    if (p.a.lse && lane == 0) {
+      const long long token = r / p.a.H;
+      p.a.lse[((token / p.a.Tq) * p.a.H + r % p.a.H) * p.a.Tq + token % p.a.Tq] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+    }
+  }
+}
+
+// Parts of the sources: as many as fill the multiprocessors where the items do not, with four blocks of keys in each at least.
+int parts_of(int items, int Tk) {
+  if (items == 0) return 1;
+  return std::max(1, std::min(148 / items, ceil_div(Tk, kRows) / 4));
+}
+
+int items_of(int B, int Tq, int H, int Hkv) { return ceil_div(ceil_div(Tq, kRows) * (H / Hkv), 2) * Hkv * B; }
+
 template <int DP>
-int forward(const AttentionArgs& a, cudaStream_t st) {
+int forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
   ForwardParams p;
   p.a = a;
   p.q_tiles = ceil_div(a.Tq, kRows);
   p.list = p.q_tiles * (a.H / a.Hkv);
   p.pairs = ceil_div(p.list, 2);
-  p.items = p.pairs * a.Hkv * a.B;
+  const int items = p.pairs * a.Hkv * a.B, blocks = std::max(1, ceil_div(a.Tk, kRows));
+  p.parts = parts_of(items, a.Tk);
+  p.part_keys = ceil_div(blocks, p.parts) * kRows;
+  p.parts = ceil_div(blocks * kRows, p.part_keys);      // none without a block
+  p.items = items * p.parts;
+  const long long rows = (long long)a.B * a.Tq * a.H;
+  p.part_o = scratch;
+  p.part_lse = scratch + p.parts * rows * a.D;
   CUtensorMap mq, mk, mv, mo;
   if (!make_token_map(&mq, a.q, a.D, a.H, a.Tq, a.B, a.q_stride, kRows) || !make_source_map(&mk, a, a.k, a.k_stride, kRows) ||
       !make_source_map(&mv, a, a.v, a.v_stride, kRows) || !make_token_map(&mo, a.o, a.D, a.H, a.Tq, a.B, (long long)a.H * a.D, 32))
@@ -501,13 +579,22 @@ int forward(const AttentionArgs& a, cudaStream_t st) {
   }
   kernel<<<std::min(p.items, device_sms()), kThreads, Layout<DP>::bytes, st>>>(mq, mk, mv, mo, p);
   count_launch();
+  if (p.parts > 1) {
+    attention_join_kernel<<<grid_for_rows(rows), 256, 0, st>>>(p, rows);
+    count_launch();
+  }
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
 }
 
 }  // namespace
 
-int launch_attention_umma_forward(const AttentionArgs& a, cudaStream_t st) {
-  return a.D <= 64 ? forward<64>(a, st) : forward<128>(a, st);
+size_t attention_parts_floats(int B, int Tq, int Tk, int H, int Hkv, int D) {
+  const int parts = parts_of(items_of(B, Tq, H, Hkv), Tk);
+  return parts > 1 ? (size_t)parts * B * Tq * H * (D + 1) : 0;
+}
+
+int launch_attention_umma_forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
+  return a.D <= 64 ? forward<64>(a, scratch, st) : forward<128>(a, scratch, st);
 }
 
 }  // namespace gshard

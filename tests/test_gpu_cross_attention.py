@@ -104,6 +104,11 @@ SIZES = [  # B, Tq, Tk, H, Hkv, D, lengths, k and v in one buffer
     (2, 257, 1, 2, 2, 128, [1, 0], True),
     (1, 520, 1025, 2, 2, 72, None, True),
     (2, 700, 650, 4, 2, 64, [-5, 9000], False),
+    # few rows and a long source: parts of it, some of them empty
+    (1, 9, 1024, 1, 1, 128, None, False),
+    (2, 20, 5000, 2, 1, 64, [4999, 700], True),
+    (3, 13, 2500, 4, 2, 128, [2500, 0, 513], True),
+    (1, 300, 4100, 1, 1, 40, [3000], False),
 ]
 
 
@@ -116,6 +121,17 @@ def test_against_the_formula(size, dtype):
     check_forward(t, o, lse)
     only, none = forward(t, lse=False)
     assert torch.equal(only, o)
+    check_backward(t, o, lse, backward(t, o, lse))
+
+
+@pytest.mark.parametrize("Tq", [9, 100, 130, 300])
+def test_many_short_ragged_sources(Tq):
+    """More sources than multiprocessors, each of one block or two that end inside 16 keys: whatever a kernel does for the last keys of
+    a source it does many times in a row."""
+    lengths = [(37 * i) % 200 for i in range(160)]
+    t = make(160, Tq, 200, 4, 2, 64, BF, lengths)
+    o, lse = forward(t)
+    check_forward(t, o, lse)
     check_backward(t, o, lse, backward(t, o, lse))
 
 
