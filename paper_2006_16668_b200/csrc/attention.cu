@@ -39,7 +39,7 @@ AttentionPlan attention_plan(const gshard_attention_config& c, bool backward) {
   Carver w;
   AttentionPlan p{};
   p.status = w.take(256);
-  if (!backward && c.dtype == GSHARD_BF16 && !attention_is_few(c.q_len, c.heads, c.kv_heads))
+  if (!backward && c.dtype == GSHARD_BF16 && !attention_is_few(true, c.batch, c.q_len, c.k_len, c.heads, c.kv_heads))
     p.parts = w.take(4 * attention_parts_floats(c.batch, c.q_len, c.k_len, c.heads, c.kv_heads, c.head_dim));
   if (backward)
     p.delta = w.take(4 * (c.dtype == GSHARD_BF16 ? attention_stats_floats(c.batch, c.q_len, c.heads) : (size_t)c.batch * c.heads * c.q_len));
@@ -115,7 +115,7 @@ int gshard_cross_attention_forward(const gshard_attention_config* config, const 
   AttentionArgs a = attention_args(c, q, k, v, k_lengths);
   a.o = o; a.lse = lse; a.status = static_cast<int*>(workspace);
   const bool bf16 = c.dtype == GSHARD_BF16;
-  if (attention_is_few(a.Tq, a.H, a.Hkv)) return launch_attention_few(a, bf16, st);
+  if (attention_is_few(bf16, a.B, a.Tq, a.Tk, a.H, a.Hkv)) return launch_attention_few(a, bf16, st);
   GS_CHECK(clear_status(workspace, st));
   return bf16 ? launch_attention_umma_forward(a, reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + pl.parts), st)
               : launch_attention_simt_forward(a, st);

@@ -28,7 +28,7 @@ __device__ __forceinline__ int source_length(const AttentionArgs& a, int b) {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // attention_few.cu: up to 8 rows (queries x heads) per key head, in one launch
-bool attention_is_few(int q_len, int heads, int kv_heads);
+bool attention_is_few(bool bf16, int B, int Tq, int Tk, int H, int Hkv);
 int launch_attention_few(const AttentionArgs& a, bool bf16, cudaStream_t st);
 
 // attention_simt.cu: fp32 on the CUDA cores

@@ -210,7 +210,20 @@ int launch_few(const AttentionArgs& a, int rows, int splits, cudaStream_t st) {
 
 }  // namespace
 
-bool attention_is_few(int q_len, int heads, int kv_heads) { return (long long)q_len * (heads / kv_heads) <= 8; }
+// Whether this kernel takes the call.  fp32: up to 8 rows (the other kernel pads them to 64).  bf16: by what it measured beside the
+// tensor cores' (which take any number of rows alike, and parts of the source), us, key heads of 128 x keys:
+//   rows                 1           2           4           8
+//   16 x 512         5.8 / 14.9  6.7 / 15    9.3 / 15   20.8 / 15
+//   128 x 512        9.4 / 16.5 15.6 / 17   21.8 / 17   51.7 / 17
+//   1024 x 2048      157 / 203   173 / 205   329 / 205   702 / 205
+//   16 x 32768        87 / 68    104 / 68    176 / 68    389 / 68
+bool attention_is_few(bool bf16, int B, int Tq, int Tk, int H, int Hkv) {
+  const long long rows = (long long)Tq * (H / Hkv), heads = (long long)B * Hkv;
+  if (rows > 8) return false;
+  if (!bf16) return true;
+  if (rows <= 2) return Tk <= 16384 || heads >= 64;
+  return heads <= 32 && Tk * rows <= (rows <= 4 ? 8192 : 2048);
+}
 
 int launch_attention_few(const AttentionArgs& a, bool bf16, cudaStream_t st) {
   const int rows = a.Tq * (a.H / a.Hkv);

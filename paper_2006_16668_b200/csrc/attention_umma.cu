@@ -1,7 +1,6 @@
 // Cross attention forward in bf16 on the tensor cores (tcgen05, accumulators in tensor memory), one pass over the keys.
 //
-// A CTA owns two tiles of 128 query rows that share a key head (neighbouring tiles of one head, or tiles of heads in the
-// same group) and walks the source in blocks of 128 keys.  Per block and tile: S = Q K^T into 128 columns of tensor memory; one
+// A CTA owns two tiles of 128 query rows that share a key head and walks the source in blocks of 128 keys.  Per block and tile: S = Q K^T into 128 columns of tensor memory; one
 // thread per row reads its scores, takes the block's maximum, writes p = 2^(c (s - m)) as bf16 over the scores, and the
 // second product O += P V reads P from tensor memory.  While the four warps of one tile work on their scores, the
 // tensor core runs the other tile's products.  The issue order S0 | S1, then PV0, S0', PV1, S1' ... makes every hand-over of a
@@ -47,7 +46,7 @@ template <int DP> struct Layout {
   static_assert(bytes <= 232448, "shared memory budget");
 };
 
-struct Tile { int h, q0, rows; };             // a 128-row tile of one head
+struct Tile { int h, q0, rows; };             // rows: (token from q0 on, one of the tile's heads from h on), heads fastest
 
 struct Item {
   int b, kh, first, tiles;                    // the tiles first, first + 1 (or only the first) of the key head's list
@@ -56,7 +55,8 @@ struct Item {
 
 struct ForwardParams {
   AttentionArgs a;
-  int q_tiles;                                // tiles per head
+  int heads, tokens;                          // of a tile: all heads of a group where they are 1, 2, 4, .. 32, else one; 128 / heads
+  int q_tiles;                                // tiles of a sequence
   int list;                                   // tiles per key head
   int pairs;                                  // items per key head and part
   int items;
@@ -79,9 +79,9 @@ __device__ __forceinline__ Item item_of(const ForwardParams& p, int i) {
 __device__ __forceinline__ Tile tile_of(const ForwardParams& p, const Item& t, int half) {
   const int i = t.first + half;
   Tile r;
-  r.h = t.kh * (p.a.H / p.a.Hkv) + i / p.q_tiles;
-  r.q0 = i % p.q_tiles * kRows;
-  r.rows = min(kRows, p.a.Tq - r.q0);
+  r.h = t.kh * (p.a.H / p.a.Hkv) + i / p.q_tiles * p.heads;
+  r.q0 = i % p.q_tiles * p.tokens;
+  r.rows = min(p.tokens, p.a.Tq - r.q0) * p.heads;
   return r;
 }
 
@@ -334,8 +334,9 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         const Tile q = tile_of(p, t, half);
         const int r = (warp & 3) * 32 + lane;
         const bool in = r < q.rows, whole = p.parts == 1;
-        float* lse = p.a.lse && in && whole ? p.a.lse + ((long long)t.b * p.a.H + q.h) * p.a.Tq + q.q0 + r : nullptr;
-        const long long part_row = whole ? 0 : (((long long)t.part * p.a.B + t.b) * p.a.Tq + q.q0 + r) * p.a.H + q.h;
+        const int token = q.q0 + r / p.heads, head = q.h + r % p.heads;
+        float* lse = p.a.lse && in && whole ? p.a.lse + ((long long)t.b * p.a.H + head) * p.a.Tq + token : nullptr;
+        const long long part_row = whole ? 0 : (((long long)t.part * p.a.B + t.b) * p.a.Tq + token) * p.a.H + head;
         float factor = 0.f;
         if (t.len > 0) {
           bool here = ptx::mbar_wait(stat_full + half, (phase >> half) & 1u, abort_flag) &&
@@ -403,9 +404,9 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
             *reinterpret_cast<uint4*>(srow + ((x ^ (lane & 7)) * 16)) = make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]);
           ptx::fence_proxy_async();
           __syncwarp();
-          const int row0 = q.q0 + (warp & 3) * 32;
-          if (lane == 0 && row0 < p.a.Tq && c * 64 < p.a.D) {
-            ptx::tma_store_4d(&map_o, stage, c * 64, q.h, row0, t.b);
+          const int token0 = q.q0 + (warp & 3) * 32 / p.heads;
+          if (lane == 0 && token0 < p.a.Tq && c * 64 < p.a.D) {
+            ptx::tma_store_4d(&map_o, stage, c * 64, q.h, token0, t.b);
             ptx::tma_store_commit();
           }
         }
@@ -551,14 +552,19 @@ int parts_of(int items, int Tk) {
   return std::max(1, std::min(148 / items, ceil_div(Tk, kRows) / 4));
 }
 
-int items_of(int B, int Tq, int H, int Hkv) { return ceil_div(ceil_div(Tq, kRows) * (H / Hkv), 2) * Hkv * B; }
+// Heads of a tile: with all of a group's heads in it the keys are read once for them; the output warps' 32 rows are whole tokens.
+int tile_heads(int group) { return 32 % group == 0 ? group : 1; }
+int tiles_of(int Tq, int group) { return ceil_div(Tq, kRows / tile_heads(group)) * (group / tile_heads(group)); }
+int items_of(int B, int Tq, int H, int Hkv) { return ceil_div(tiles_of(Tq, H / Hkv), 2) * Hkv * B; }
 
 template <int DP>
 int forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
   ForwardParams p;
   p.a = a;
-  p.q_tiles = ceil_div(a.Tq, kRows);
-  p.list = p.q_tiles * (a.H / a.Hkv);
+  p.heads = tile_heads(a.H / a.Hkv);
+  p.tokens = kRows / p.heads;
+  p.q_tiles = ceil_div(a.Tq, p.tokens);
+  p.list = tiles_of(a.Tq, a.H / a.Hkv);
   p.pairs = ceil_div(p.list, 2);
   const int items = p.pairs * a.Hkv * a.B, blocks = std::max(1, ceil_div(a.Tk, kRows));
   p.parts = parts_of(items, a.Tk);
@@ -569,8 +575,8 @@ int forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
   p.part_o = scratch;
   p.part_lse = scratch + p.parts * rows * a.D;
   CUtensorMap mq, mk, mv, mo;
-  if (!make_token_map(&mq, a.q, a.D, a.H, a.Tq, a.B, a.q_stride, kRows) || !make_source_map(&mk, a, a.k, a.k_stride, kRows) ||
-      !make_source_map(&mv, a, a.v, a.v_stride, kRows) || !make_token_map(&mo, a.o, a.D, a.H, a.Tq, a.B, (long long)a.H * a.D, 32))
+  if (!make_token_map(&mq, a.q, a.D, a.H, a.Tq, a.B, a.q_stride, p.tokens, 64, p.heads) || !make_source_map(&mk, a, a.k, a.k_stride, kRows) ||
+      !make_source_map(&mv, a, a.v, a.v_stride, kRows) || !make_token_map(&mo, a.o, a.D, a.H, a.Tq, a.B, (long long)a.H * a.D, 32 / p.heads, 64, p.heads))
     return GSHARD_ERR_CUDA;
   auto kernel = attention_umma_forward_kernel<DP>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<DP>::bytes) != cudaSuccess) {

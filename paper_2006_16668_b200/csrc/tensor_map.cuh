@@ -75,11 +75,11 @@ inline bool make_gated_map(CUtensorMap* map, const void* base, long long cols, l
 }
 
 // 4-D bf16 tensor map {head_dim, heads, tokens, batch} of a [batch, tokens, heads, head_dim] tensor whose tokens lie `stride`
-// elements apart, with boxes of `box_dims` head dimensions by `box_tokens` tokens of one head; outside reads as zero.
+// elements apart, with boxes of `box_dims` head dimensions by `box_heads` heads by `box_tokens` tokens; outside reads as zero.
 inline bool make_token_map(CUtensorMap* map, const void* base, int head_dim, int heads, long long tokens, long long batch, long long stride,
-                           int box_tokens, int box_dims = 64) {
+                           int box_tokens, int box_dims = 64, int box_heads = 1) {
   const long long dims[4] = {head_dim, heads, tokens, batch}, strides[3] = {head_dim, stride, tokens * stride};
-  const int box[4] = {box_dims, 1, box_tokens, 1};
+  const int box[4] = {box_dims, box_heads, box_tokens, 1};
   return make_map_4d(map, base, dims, strides, box);
 }
 

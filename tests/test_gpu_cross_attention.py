@@ -104,6 +104,11 @@ SIZES = [  # B, Tq, Tk, H, Hkv, D, lengths, k and v in one buffer
     (2, 257, 1, 2, 2, 128, [1, 0], True),
     (1, 520, 1025, 2, 2, 72, None, True),
     (2, 700, 650, 4, 2, 64, [-5, 9000], False),
+    # groups of heads that share a tile, and some that do not fit one
+    (2, 37, 300, 32, 1, 64, [300, 17], True),
+    (2, 70, 260, 8, 1, 128, [259, 128], False),
+    (1, 50, 200, 12, 2, 72, [131], False),
+    (1, 3, 400, 64, 1, 64, None, False),
     # few rows and a long source: parts of it, some of them empty
     (1, 9, 1024, 1, 1, 128, None, False),
     (2, 20, 5000, 2, 1, 64, [4999, 700], True),
