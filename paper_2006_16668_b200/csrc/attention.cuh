@@ -25,6 +25,24 @@ __device__ __forceinline__ int source_length(const AttentionArgs& a, int b) {
   return a.lengths ? min(max(__ldg(a.lengths + b), 0), a.Tk) : a.Tk;
 }
 
+// Division of 31-bit numbers by a divisor known at launch: a multiplication and a shift (Granlund and Montgomery, 1994) where the
+// hardware's takes some twenty instructions, which in the thread that issues MMAs cost the tensor core.
+struct Divisor {
+  uint32_t d, mul, shift;
+  Divisor() = default;
+  explicit Divisor(int divisor) : d((uint32_t)divisor), shift(0) {
+    while ((1ull << shift) < d) ++shift;
+    mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+  }
+  __device__ __forceinline__ int quotient(int n) const { return (int)((__umulhi(mul, (uint32_t)n) + (uint32_t)n) >> shift); }
+  // quotient; n becomes the remainder
+  __device__ __forceinline__ int split(int& n) const {
+    const int q = quotient(n);
+    n -= q * (int)d;
+    return q;
+  }
+};
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // attention_few.cu: up to 8 rows (queries x heads) per key head, in one launch

@@ -134,6 +134,7 @@ struct BackwardParams {
   const float* stats;
   int q_tiles, k_tiles;
   int items;                                  // of dq
+  Divisor by_tiles, by_heads, by_group;       // of q_tiles, a.H, the heads of a key head
   const int* prefix;                          // see count_blocks
 };
 
@@ -337,7 +338,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           kv_phase ^= 1u;
           for (int i = 0; i < t.n; ++i) {
             if (!ptx::mbar_wait(empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
-            const int h = t.kh * group + i / p.q_tiles, tile = i % p.q_tiles;
+            int tile = i;
+            const int h = t.kh * group + p.by_tiles.split(tile);
             unsigned char* q = ring + stage * L::stage;
             ptx::mbar_arrive_expect_tx(full + stage, L::stage);
             load_rows<DP>(q, &map_q, full + stage, h, tile * kRows, t.b, again);
@@ -543,7 +545,6 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(k_clean + kK);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int group = p.a.H / p.a.Hkv;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kK; ++s) { ptx::mbar_init(k_full + s, 1); ptx::mbar_init(k_empty + s, 2); ptx::mbar_init(k_clean + s, 1); }
@@ -569,8 +570,9 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   const uint32_t t_dp = tmem + 256, t_dq = tmem + 384;
 
   // item: query tile (fastest), head, batch
-  auto head_of = [&](int i) { return i / p.q_tiles % p.a.H; };
-  auto batch_of = [&](int i) { return i / p.q_tiles / p.a.H; };
+  auto tile_of = [&](int i) { p.by_tiles.split(i); return i; };
+  auto head_of = [&](int i) { int h = p.by_tiles.quotient(i); p.by_heads.split(h); return h; };
+  auto batch_of = [&](int i) { return p.by_heads.quotient(p.by_tiles.quotient(i)); };
   // whether the last block has rows between its last key and the next multiple of 16, where its product ends, that TMA has not zeroed
   auto ragged = [&](int len) { return (len & 15) != 0 && len < p.a.Tk; };
 
@@ -583,7 +585,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         const uint64_t again = ptx::policy_evict_last(), once = ptx::policy_evict_first();
         int ks = 0, vs = 0; uint32_t k_phase = 0, v_phase = 0, q_phase = 0;
         for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-          const int h = head_of(i), b = batch_of(i), kh = h / group, len = source_length(p.a, b);
+          const int h = head_of(i), b = batch_of(i), kh = p.by_group.quotient(h), len = source_length(p.a, b);
           if (len == 0) continue;
           auto load_k = [&](int k0) {
             if (!ptx::mbar_wait(k_empty + ks, k_phase ^ 1u, abort_flag)) { ok = false; return; }
@@ -595,13 +597,13 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           if (!ok || !ptx::mbar_wait(q_empty, q_phase ^ 1u, abort_flag)) { ok = false; break; }
           q_phase ^= 1u;
           ptx::mbar_arrive_expect_tx(q_full, 2 * L::tile);
-          load_rows<DP>(sq, &map_q, q_full, h, i % p.q_tiles * kRows, b, once);
-          load_rows<DP>(sd, &map_do, q_full, h, i % p.q_tiles * kRows, b, once);
+          load_rows<DP>(sq, &map_q, q_full, h, tile_of(i) * kRows, b, once);
+          load_rows<DP>(sd, &map_do, q_full, h, tile_of(i) * kRows, b, once);
           if (const int n = i + gridDim.x; n < p.items) {         // the next item's rows into L2: they are loaded only when these have been read
 #pragma unroll
             for (int j = 0; j < DP / 64; ++j) {
-              ptx::tma_prefetch_4d(&map_q, j * 64, head_of(n), n % p.q_tiles * kRows, batch_of(n));
-              ptx::tma_prefetch_4d(&map_do, j * 64, head_of(n), n % p.q_tiles * kRows, batch_of(n));
+              ptx::tma_prefetch_4d(&map_q, j * 64, head_of(n), tile_of(n) * kRows, batch_of(n));
+              ptx::tma_prefetch_4d(&map_do, j * 64, head_of(n), tile_of(n) * kRows, batch_of(n));
             }
           }
           for (int k0 = 0; k0 < len && ok; k0 += kRows) {
@@ -690,7 +692,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     uint32_t s_phase[2] = {0, 0}, dp_phase = 0, o_phase = 0;
     for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
       const int h = head_of(i), b = batch_of(i), len = source_length(p.a, b);
-      const int q0 = i % p.q_tiles * kRows;
+      const int q0 = tile_of(i) * kRows;
       const bool in = q0 + r < p.a.Tq;
       __nv_bfloat16* dq = static_cast<__nv_bfloat16*>(p.a.dq) + ((long long)b * p.a.Tq + q0 + r) * p.a.q_stride + (long long)h * p.a.D;
       if (len == 0) {
@@ -776,6 +778,9 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   p.q_tiles = ceil_div(a.Tq, kRows);
   p.k_tiles = ceil_div(a.Tk, kRows);
   p.items = p.q_tiles * a.H * a.B;
+  p.by_tiles = Divisor(std::max(1, p.q_tiles));
+  p.by_heads = Divisor(a.H);
+  p.by_group = Divisor(a.H / a.Hkv);
   const int kv_items = p.k_tiles * a.Hkv * a.B;
   int* prefix = reinterpret_cast<int*>(stats + (size_t)p.items * kStatFloats);
   p.prefix = prefix;

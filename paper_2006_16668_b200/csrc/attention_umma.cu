@@ -55,32 +55,35 @@ struct Item {
 
 struct ForwardParams {
   AttentionArgs a;
+  int group;                                  // heads of a key head
   int heads, tokens;                          // of a tile: all heads of a group where they are 1, 2, 4, .. 32, else one; 128 / heads
   int q_tiles;                                // tiles of a sequence
   int list;                                   // tiles per key head
   int pairs;                                  // items per key head and part
   int items;
+  Divisor by_parts, by_pairs, by_kv_heads, by_tiles, by_heads;      // of parts, pairs, a.Hkv, q_tiles, heads
   int parts, part_keys;                       // parts of a source, a multiple of 128 keys each
   float* part_o; float* part_lse;             // parts > 1: [parts][B, Tq, H, D] and (powers of two) [parts][B, Tq, H]
 };
 
 __device__ __forceinline__ Item item_of(const ForwardParams& p, int i) {
   Item t;
-  t.part = i % p.parts;
-  i /= p.parts;
-  t.first = i % p.pairs * 2;
-  t.kh = i / p.pairs % p.a.Hkv;
-  t.b = i / p.pairs / p.a.Hkv;
+  t.part = i;                                  // fastest, then the pair of tiles, the key head, the source
+  t.first = p.by_parts.split(t.part);
+  t.kh = p.by_pairs.split(t.first);
+  t.b = p.by_kv_heads.split(t.kh);
+  t.first *= 2;
   t.tiles = min(2, p.list - t.first);
   t.k0 = t.part * p.part_keys;
   t.len = min(max(source_length(p.a, t.b) - t.k0, 0), p.part_keys);
   return t;
 }
 __device__ __forceinline__ Tile tile_of(const ForwardParams& p, const Item& t, int half) {
-  const int i = t.first + half;
+  int i = t.first + half;
+  const int heads = p.by_tiles.split(i);
   Tile r;
-  r.h = t.kh * (p.a.H / p.a.Hkv) + i / p.q_tiles * p.heads;
-  r.q0 = i % p.q_tiles * p.tokens;
+  r.h = t.kh * p.group + heads * p.heads;
+  r.q0 = i * p.tokens;
   r.rows = min(p.tokens, p.a.Tq - r.q0) * p.heads;
   return r;
 }
@@ -334,7 +337,9 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         const Tile q = tile_of(p, t, half);
         const int r = (warp & 3) * 32 + lane;
         const bool in = r < q.rows, whole = p.parts == 1;
-        const int token = q.q0 + r / p.heads, head = q.h + r % p.heads;
+        int head = r;
+        const int token = q.q0 + p.by_heads.split(head);
+        head += q.h;
         float* lse = p.a.lse && in && whole ? p.a.lse + ((long long)t.b * p.a.H + head) * p.a.Tq + token : nullptr;
         const long long part_row = whole ? 0 : (((long long)t.part * p.a.B + t.b) * p.a.Tq + token) * p.a.H + head;
         float factor = 0.f;
@@ -404,7 +409,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
             *reinterpret_cast<uint4*>(srow + ((x ^ (lane & 7)) * 16)) = make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]);
           ptx::fence_proxy_async();
           __syncwarp();
-          const int token0 = q.q0 + (warp & 3) * 32 / p.heads;
+          const int token0 = q.q0 + p.by_heads.quotient((warp & 3) * 32);
           if (lane == 0 && token0 < p.a.Tq && c * 64 < p.a.D) {
             ptx::tma_store_4d(&map_o, stage, c * 64, q.h, token0, t.b);
             ptx::tma_store_commit();
@@ -561,7 +566,8 @@ template <int DP>
 int forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
   ForwardParams p;
   p.a = a;
-  p.heads = tile_heads(a.H / a.Hkv);
+  p.group = a.H / a.Hkv;
+  p.heads = tile_heads(p.group);
   p.tokens = kRows / p.heads;
   p.q_tiles = ceil_div(a.Tq, p.tokens);
   p.list = tiles_of(a.Tq, a.H / a.Hkv);
@@ -571,6 +577,11 @@ int forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
   p.part_keys = ceil_div(blocks, p.parts) * kRows;
   p.parts = ceil_div(blocks * kRows, p.part_keys);      // none without a block
   p.items = items * p.parts;
+  p.by_parts = Divisor(p.parts);
+  p.by_pairs = Divisor(p.pairs);
+  p.by_kv_heads = Divisor(a.Hkv);
+  p.by_tiles = Divisor(p.q_tiles);
+  p.by_heads = Divisor(p.heads);
   const long long rows = (long long)a.B * a.Tq * a.H;
   p.part_o = scratch;
   p.part_lse = scratch + p.parts * rows * a.D;
