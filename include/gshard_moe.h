@@ -576,8 +576,8 @@ int gshard_moe_route_backward(const gshard_route_config* config, const void* log
  *   o [batch, q_len, heads, head_dim] packed, dtype; lse [batch, heads, q_len] float, may be NULL.
  * bf16: tensor cores, fp32 accumulation and softmax, the weights p rounded to bf16 as an operand of p v.  fp32: all
  * arithmetic in fp32.
- * Limits: head_dim a multiple of 8 up to 128, strides multiples of 16 bytes, scale > 0; batch, q_len and
- * k_len may be 0.  workspace: gshard_cross_attention_workspace_bytes() bytes, 256-byte aligned; its first word
+ * Limits: head_dim a multiple of 8 up to 128, strides multiples of 16 bytes, scale from 1e-20 to 1e20; batch,
+ * q_len and k_len may be 0.  workspace: gshard_cross_attention_workspace_bytes() bytes, 256-byte aligned; its first word
  * is the status word (gshard_moe_last_device_status).  Calls that share a workspace must be ordered on one stream. */
 typedef struct {
   int32_t batch, q_len, k_len, heads, kv_heads, head_dim;
@@ -632,7 +632,8 @@ int gshard_gated_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_
  *   products rounded to the tensor's type; *norm (float, device memory, may be NULL).  A norm that is infinite or NaN
  *   leaves the gradients as they are (outs: copies), so that a caller can look at *norm and skip the step.
  * Several ranks (the experts' gradients of the expert-parallel form): add the ranks' *sumsq between the two calls.
- * outs may not overlap grads other than by being the same tensor.
+ * An output may be its own gradient, and shares memory with no other tensor of the list (a tensor that is listed twice
+ * counts twice, and would be scaled twice).
  * workspace: gshard_grad_norm_workspace_bytes() bytes, 256-byte aligned; scratch. */
 typedef struct {
   int32_t n;

@@ -713,6 +713,23 @@ def gshard_gated_linear_backward(x, w, pre, dh, dx=None, dw=None, activation="si
     _call("gshard_gated_linear_backward", dev, stream, n, K, cols, code, _activation(activation), *args)
 
 
+def _no_overlap(grads, outs):
+    """An output may be its own gradient, but share memory with no other tensor (it would be scaled twice, or read after)."""
+    spans = []
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        if g.numel():
+            spans.append((o.data_ptr(), o.data_ptr() + o.nbytes, True, i))
+            if o.data_ptr() != g.data_ptr():
+                spans.append((g.data_ptr(), g.data_ptr() + g.nbytes, False, i))
+    end_out = end_any = 0                      # of the spans that start before this one
+    for start, end, written, i in sorted(spans):
+        if start < (end_any if written else end_out):
+            raise ValueError(f"outs: the memory of tensor {i} is that of another tensor too")
+        end_any = max(end_any, end)
+        if written:
+            end_out = max(end_out, end)
+
+
 class GradList:
     """Gradients of one training program, and where their clipped values go: the arrays of addresses, counts and types that
     the library reads on every call.  It holds the tensors, whose storage must stay where it is."""
@@ -726,6 +743,7 @@ class GradList:
             codes.append(_code_of(g.dtype, f"grads[{i}]"))
             _arg(g, f"grads[{i}]", g.shape, g.dtype, self.device)
             _arg(o, f"outs[{i}]", g.shape, g.dtype, self.device)
+        _no_overlap(self.tensors[0], self.tensors[1])
         self._arrays = ((c_void_p * n)(*[g.data_ptr() for g in grads]), (c_void_p * n)(*[o.data_ptr() for o in outs]),
                         (c_int64 * n)(*[g.numel() for g in grads]), (c_int32 * n)(*codes))
         self.struct = gshard_grad_list(n, *[ctypes.cast(a, t) for a, t in zip(

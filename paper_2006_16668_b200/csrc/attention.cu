@@ -51,7 +51,7 @@ int attention_validate(const gshard_attention_config* c) {
   if (!c || c->batch < 0 || c->q_len < 0 || c->k_len < 0 || c->heads <= 0 || c->kv_heads <= 0 || c->head_dim <= 0)
     return GSHARD_ERR_INVALID_ARG;
   if (c->dtype != GSHARD_F32 && c->dtype != GSHARD_BF16) return GSHARD_ERR_INVALID_ARG;
-  if (!(c->scale > 0.f) || c->scale > 3e38f) return GSHARD_ERR_INVALID_ARG;
+  if (!(c->scale >= 1e-20f && c->scale <= 1e20f)) return GSHARD_ERR_INVALID_ARG;     // lse / scale is a finite number
   if (c->heads % c->kv_heads) return GSHARD_ERR_INVALID_ARG;
   if (c->head_dim % 8 || c->head_dim > 128) return GSHARD_ERR_UNSUPPORTED_SHAPE;
   const int64_t q_row = (int64_t)c->heads * c->head_dim, k_row = (int64_t)c->kv_heads * c->head_dim;

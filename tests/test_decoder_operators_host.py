@@ -37,7 +37,7 @@ def _att_bwd(q=P[0], k=P[1], v=P[2], lengths=P[3], o=P[4], lse=P[5], dout=P[7], 
 CONFIGS = [(dict(batch=-1), INVALID), (dict(q_len=-1), INVALID), (dict(k_len=-3), INVALID), (dict(heads=0), INVALID), (dict(kv_heads=0), INVALID),
            (dict(kv_heads=3), INVALID), (dict(kv_heads=8), INVALID), (dict(head_dim=60), SHAPE), (dict(head_dim=136), SHAPE),
            (dict(head_dim=0), INVALID), (dict(dtype=2), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID),
-           (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID), (dict(q_stride=255), INVALID), (dict(q_stride=260), INVALID),
+           (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID), (dict(scale=1e-21), INVALID), (dict(scale=2e20), INVALID), (dict(q_stride=255), INVALID), (dict(q_stride=260), INVALID),
            (dict(k_stride=120), INVALID), (dict(v_stride=132), INVALID), (dict(k_stride=1 << 36), SHAPE),
            (dict(heads=65536, kv_heads=2), SHAPE), (dict(batch=1 << 30, k_len=1 << 20), SHAPE), (dict(k_len=(1 << 30) + 1), SHAPE)]
 
@@ -156,6 +156,15 @@ def test_grad_list_checks_its_tensors():
                         ([torch.zeros(4, 8)[:, ::2]], [torch.zeros(4, 4)])):
         with pytest.raises(ValueError):
             B.make_grad_list(grads, outs)
+    flat = torch.zeros(100)
+    a, b = flat[:60], flat[60:]
+    for grads, outs in (([a, a], [a, a]), ([a, flat[59:]], [a, flat[59:]]), ([a, b], [b.new_zeros(60), a[:40]]), ([a, b], [b.new_zeros(60), a[20:]]),
+                        ([a[:40], b], [b, a[:40]]), ([a, b], [flat.new_zeros(60), flat[59:99]])):
+        with pytest.raises(ValueError, match="another tensor"):
+            B.make_grad_list(grads, outs)
+    for grads, outs in (([a, b], [a, b]), ([a, a], [flat.new_zeros(60), flat.new_zeros(60)]), ([a, b], [a, flat.new_zeros(40)]), ([b, a], [b, a]),
+                        ([flat[:0], a], [flat[:0], a])):
+        B.make_grad_list(grads, outs)
     lst = B.make_grad_list(g)
     assert lst.struct.n == 2 and lst.struct.counts[1] == 16 and lst.struct.grads[0] == lst.struct.outs[0] == g[0].data_ptr()
     with pytest.raises(ValueError, match="CUDA"):
