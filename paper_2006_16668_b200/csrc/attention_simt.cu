@@ -9,6 +9,7 @@
 // products instead of five, but every gradient is summed by one block in a fixed order, without atomics.
 #include "attention.cuh"
 #include "pack.cuh"
+#include "sm100_ptx.cuh"
 
 namespace gshard {
 
@@ -20,16 +21,22 @@ constexpr int kThreads = 256;
 
 template <int DP> constexpr int kPitch = DP + 4;
 
-// 64 rows from `src` (pitch `stride` elements) as floats; rows from `rows` on and columns from D on are zero
+// 64 rows from `src` (pitch `stride` elements), asynchronously; rows from `rows` on and columns from D on are zero (nothing
+// is loaded where there is no row)
 template <int DP>
 __device__ __forceinline__ void load_tile(float* dst, const float* src, long long stride, int rows, int D) {
-  for (int i = threadIdx.x; i < BT * DP / 4; i += kThreads) {
+  for (int i = threadIdx.x; rows > 0 && i < BT * DP / 4; i += kThreads) {
     const int r = i / (DP / 4), c = i % (DP / 4) * 4;
-    float f[4] = {0.f, 0.f, 0.f, 0.f};
-    if (r < rows && c < D) load_pack<float, 4>(src + r * stride + c, f);
-    *reinterpret_cast<float4*>(dst + r * kPitch<DP> + c) = make_float4(f[0], f[1], f[2], f[3]);
+    const bool in = r < rows && c < D;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst + r * kPitch<DP> + c)), "l"(in ? src + r * stride + c : src),
+                 "r"(in ? 16 : 0)
+                 : "memory");
   }
+  asm volatile("cp.async.commit_group;" ::: "memory");
 }
+// all but the last N tiles of this thread's have landed (for everyone behind the next barrier)
+template <int N>
+__device__ __forceinline__ void landed() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // s[i][j] = <row ty + 16 i of A, row tx + 16 j of B>
 template <int DP>
@@ -134,13 +141,18 @@ __global__ void __launch_bounds__(kThreads) attention_simt_forward_kernel(const 
 #pragma unroll
   for (int i = 0; i < 4; ++i) { top[i] = -INFINITY; sum[i] = 0.f; }
   const float c = a.scale * kLog2e;
+  if (len) {
+    load_tile<DP>(sk, k, a.k_stride, len, a.D);
+    load_tile<DP>(sv, v, a.v_stride, len, a.D);
+  }
+  // the next keys are on their way while the softmax and the second product run, the next values while the next scores do
   for (int k0 = 0; k0 < len; k0 += BT) {
-    __syncthreads();                                  // the previous tiles have been read
-    load_tile<DP>(sk, k + k0 * a.k_stride, a.k_stride, len - k0, a.D);
-    load_tile<DP>(sv, v + k0 * a.v_stride, a.v_stride, len - k0, a.D);
+    landed<1>();                                      // queries and keys
     __syncthreads();
     float s[4][4];
     rows_by_rows<DP>(sq, sk, s, tx, ty);
+    __syncthreads();                                  // the keys have been read
+    load_tile<DP>(sk, k + (k0 + BT) * a.k_stride, a.k_stride, len - k0 - BT, a.D);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float m = -INFINITY;
@@ -167,9 +179,13 @@ __global__ void __launch_bounds__(kThreads) attention_simt_forward_kernel(const 
         acc[i][d][1] = mul2(acc[i][d][1], both(shrink));
       }
     }
+    landed<1>();                                      // values
     __syncthreads();
     scores_by_rows<DP>(sp, sv, acc, tx, ty);
+    __syncthreads();
+    load_tile<DP>(sv, v + (k0 + BT) * a.v_stride, a.v_stride, len - k0 - BT, a.D);
   }
+  landed<0>();
   float factor[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -201,41 +217,59 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const Atte
   if (k0 < len) {
     load_tile<DP>(sk, static_cast<const float*>(a.k) + koff, a.k_stride, len - k0, a.D);
     load_tile<DP>(sv, static_cast<const float*>(a.v) + voff, a.v_stride, len - k0, a.D);
-    for (int h = kh * group; h < (kh + 1) * group; ++h) {
-      const float* q = static_cast<const float*>(a.q) + (long long)b * a.Tq * a.q_stride + (long long)h * a.D;
-      const float* dout = static_cast<const float*>(a.dout) + ((long long)b * a.Tq * a.H + h) * a.D;
-      const long long row = ((long long)b * a.H + h) * a.Tq;
-      for (int q0 = 0; q0 < a.Tq; q0 += BT) {
-        __syncthreads();
-        load_tile<DP>(sq, q + q0 * a.q_stride, a.q_stride, a.Tq - q0, a.D);
-        load_tile<DP>(sd, dout + (long long)q0 * a.H * a.D, (long long)a.H * a.D, a.Tq - q0, a.D);
-        if (threadIdx.x < BT) {
-          const bool in = q0 + threadIdx.x < a.Tq;                // queries behind the last one: P = exp(-inf) = 0
-          slse[threadIdx.x] = in ? a.lse[row + q0 + threadIdx.x] * kLog2e : INFINITY;
-          sdelta[threadIdx.x] = in ? a.delta[row + q0 + threadIdx.x] : 0.f;
-        }
-        __syncthreads();
-        float s[4][4], dp[4][4];
-        rows_by_rows<DP>(sk, sq, s, tx, ty);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            s[i][j] = k0 + ty + 16 * i < len ? exp2f(fmaf(s[i][j], c, -slse[tx + 16 * j])) : 0.f;
-            sp[(ty + 16 * i) * PP + tx + 16 * j] = s[i][j];
-          }
-        rows_by_rows<DP>(sv, sd, dp, tx, ty);
-        __syncthreads();
-        scores_by_rows<DP>(sp, sd, dv, tx, ty);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sp[(ty + 16 * i) * PP + tx + 16 * j] = s[i][j] * (dp[i][j] - sdelta[tx + 16 * j]);
-        __syncthreads();
-        scores_by_rows<DP>(sp, sq, dk, tx, ty);
+    const int n = group * ceil_div(a.Tq, BT);          // query tiles, head by head
+    auto head_of = [&](int i) { return kh * group + i / ceil_div(a.Tq, BT); };
+    auto first_of = [&](int i) { return i % ceil_div(a.Tq, BT) * BT; };
+    auto load_do = [&](int i) {
+      const int h = head_of(i), q0 = first_of(i);
+      load_tile<DP>(sd, static_cast<const float*>(a.dout) + (((long long)b * a.Tq + q0) * a.H + h) * a.D, (long long)a.H * a.D,
+                    i < n ? a.Tq - q0 : 0, a.D);
+    };
+    auto load_q = [&](int i) {
+      const int h = head_of(i), q0 = first_of(i);
+      load_tile<DP>(sq, static_cast<const float*>(a.q) + ((long long)b * a.Tq + q0) * a.q_stride + (long long)h * a.D, a.q_stride,
+                    i < n ? a.Tq - q0 : 0, a.D);
+    };
+    load_do(0);
+    load_q(0);
+    // dO is read for the last time before Q is: its next tile is on its way during the last product, that of Q during the first
+    for (int i = 0; i < n; ++i) {
+      if (threadIdx.x < BT) {
+        const int t = first_of(i) + (int)threadIdx.x;
+        const long long row = ((long long)b * a.H + head_of(i)) * a.Tq + t;
+        const bool in = t < a.Tq;                                 // queries behind the last one: P = exp(-inf) = 0
+        slse[threadIdx.x] = in ? a.lse[row] * kLog2e : INFINITY;
+        sdelta[threadIdx.x] = in ? a.delta[row] : 0.f;
       }
+      landed<1>();
+      __syncthreads();
+      float s[4][4], dp[4][4];
+      rows_by_rows<DP>(sv, sd, dp, tx, ty);
+      landed<0>();
+      __syncthreads();
+      rows_by_rows<DP>(sk, sq, s, tx, ty);
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[x][j] = k0 + ty + 16 * x < len ? exp2f(fmaf(s[x][j], c, -slse[tx + 16 * j])) : 0.f;
+          sp[(ty + 16 * x) * PP + tx + 16 * j] = s[x][j];
+          dp[x][j] = s[x][j] * (dp[x][j] - sdelta[tx + 16 * j]);
+        }
+      __syncthreads();
+      scores_by_rows<DP>(sp, sd, dv, tx, ty);
+      __syncthreads();
+      load_do(i + 1);
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sp[(ty + 16 * x) * PP + tx + 16 * j] = dp[x][j];
+      __syncthreads();
+      scores_by_rows<DP>(sp, sq, dk, tx, ty);
+      __syncthreads();
+      load_q(i + 1);
     }
+    landed<0>();
   }
   // keys behind the length have gradient zero: their scores were zero throughout
   const float one[4] = {1.f, 1.f, 1.f, 1.f}, scale[4] = {a.scale, a.scale, a.scale, a.scale};
@@ -267,14 +301,18 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const Atten
       lse[i] = ty + 16 * i < rows ? a.lse[row] * kLog2e : INFINITY;
       delta[i] = ty + 16 * i < rows ? a.delta[row] : 0.f;
     }
+    load_tile<DP>(sv, v, a.v_stride, len, a.D);
+    load_tile<DP>(sk, k, a.k_stride, len, a.D);
+    // the next values are on their way from the first product on, the next keys during the next first product
     for (int k0 = 0; k0 < len; k0 += BT) {
-      __syncthreads();
-      load_tile<DP>(sk, k + k0 * a.k_stride, a.k_stride, len - k0, a.D);
-      load_tile<DP>(sv, v + k0 * a.v_stride, a.v_stride, len - k0, a.D);
+      landed<1>();
       __syncthreads();
       float s[4][4], dp[4][4];
-      rows_by_rows<DP>(sq, sk, s, tx, ty);
       rows_by_rows<DP>(sd, sv, dp, tx, ty);
+      landed<0>();
+      __syncthreads();
+      load_tile<DP>(sv, v + (k0 + BT) * a.v_stride, a.v_stride, len - k0 - BT, a.D);
+      rows_by_rows<DP>(sq, sk, s, tx, ty);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -283,7 +321,10 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const Atten
               k0 + tx + 16 * j < len ? exp2f(fmaf(s[i][j], c, -lse[i])) * (dp[i][j] - delta[i]) : 0.f;
       __syncthreads();
       scores_by_rows<DP>(sp, sk, dq, tx, ty);
+      __syncthreads();
+      load_tile<DP>(sk, k + (k0 + BT) * a.k_stride, a.k_stride, len - k0 - BT, a.D);
     }
+    landed<0>();
   }
   const float scale[4] = {a.scale, a.scale, a.scale, a.scale};
   store_tile<DP>(static_cast<float*>(a.dq) + qoff, a.q_stride, rows, a.D, dq, scale, tx, ty);
