@@ -33,20 +33,6 @@ __global__ void __launch_bounds__(256) attention_delta_kernel(const AttentionArg
   }
 }
 
-struct AttentionPlan { size_t status, parts, delta, total; };
-
-AttentionPlan attention_plan(const gshard_attention_config& c, bool backward) {
-  Carver w;
-  AttentionPlan p{};
-  p.status = w.take(256);
-  if (!backward && c.dtype == GSHARD_BF16 && !attention_is_few(true, c.batch, c.q_len, c.k_len, c.heads, c.kv_heads))
-    p.parts = w.take(4 * attention_parts_floats(c.batch, c.q_len, c.k_len, c.heads, c.kv_heads, c.head_dim));
-  if (backward)
-    p.delta = w.take(4 * (c.dtype == GSHARD_BF16 ? attention_stats_floats(c.batch, c.q_len, c.heads) : (size_t)c.batch * c.heads * c.q_len));
-  p.total = w.off;
-  return p;
-}
-
 int attention_validate(const gshard_attention_config* c) {
   if (!c || c->batch < 0 || c->q_len < 0 || c->k_len < 0 || c->heads <= 0 || c->kv_heads <= 0 || c->head_dim <= 0)
     return GSHARD_ERR_INVALID_ARG;
@@ -75,6 +61,24 @@ AttentionArgs attention_args(const gshard_attention_config& c, const void* q, co
   a.scale = c.scale;
   a.q_stride = c.q_stride; a.k_stride = c.k_stride; a.v_stride = c.v_stride;
   return a;
+}
+
+struct AttentionPlan { size_t status, delta, scratch, total; };
+
+AttentionPlan attention_plan(const gshard_attention_config& c, bool backward) {
+  const AttentionArgs a = attention_args(c, nullptr, nullptr, nullptr, nullptr);
+  const bool bf16 = c.dtype == GSHARD_BF16;
+  Carver w;
+  AttentionPlan p{};
+  p.status = w.take(256);
+  if (backward) {
+    if (!bf16) p.delta = w.take(4 * (size_t)c.batch * c.heads * c.q_len);
+    p.scratch = w.take(4 * (bf16 ? attention_umma_backward_floats(a) : attention_simt_backward_floats(a)));
+  } else if (!attention_is_few(bf16, a.B, a.Tq, a.Tk, a.H, a.Hkv)) {
+    p.scratch = w.take(4 * (bf16 ? attention_umma_forward_floats(a) : attention_simt_forward_floats(a)));
+  }
+  p.total = w.off;
+  return p;
 }
 
 int clear_status(void* workspace, cudaStream_t st) {
@@ -117,8 +121,8 @@ int gshard_cross_attention_forward(const gshard_attention_config* config, const 
   const bool bf16 = c.dtype == GSHARD_BF16;
   if (attention_is_few(bf16, a.B, a.Tq, a.Tk, a.H, a.Hkv)) return launch_attention_few(a, bf16, st);
   GS_CHECK(clear_status(workspace, st));
-  return bf16 ? launch_attention_umma_forward(a, reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + pl.parts), st)
-              : launch_attention_simt_forward(a, st);
+  float* scratch = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + pl.scratch);
+  return bf16 ? launch_attention_umma_forward(a, scratch, st) : launch_attention_simt_forward(a, scratch, st);
 }
 
 int gshard_cross_attention_backward(const gshard_attention_config* config, const void* q, const void* k, const void* v,
@@ -145,17 +149,18 @@ int gshard_cross_attention_backward(const gshard_attention_config* config, const
   NvtxRange range("gshard.attention.backward");
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   AttentionArgs a = attention_args(c, q, k, v, k_lengths);
+  float* scratch = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + pl.scratch);
   float* delta = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + pl.delta);
   a.o = const_cast<void*>(o); a.lse = const_cast<float*>(lse); a.dout = dout; a.delta = delta;
   a.dq = dq; a.dk = dk; a.dv = dv; a.status = static_cast<int*>(workspace);
   GS_CHECK(clear_status(workspace, st));
-  if (c.dtype == GSHARD_BF16) return launch_attention_umma_backward(a, delta, st);
+  if (c.dtype == GSHARD_BF16) return launch_attention_umma_backward(a, scratch, st);
   const long long rows = (long long)c.batch * c.q_len * c.heads;
   if (rows) {
     attention_delta_kernel<<<grid_for_rows(rows), 256, 0, st>>>(a, delta, rows);
     count_launch();
   }
-  return launch_attention_simt_backward(a, st);
+  return launch_attention_simt_backward(a, scratch, st);
 }
 
 }  // extern "C"

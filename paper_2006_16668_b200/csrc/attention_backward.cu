@@ -136,6 +136,10 @@ struct BackwardParams {
   int items;                                  // of dq
   Divisor by_tiles, by_heads, by_group;       // of q_tiles, a.H, the heads of a key head
   const int* prefix;                          // see count_blocks
+  // where the items do not fill the GPU they are parts: of an item's query tiles (dk, dv), or of the source (dq)
+  int kv_parts, kv_each, q_parts, q_keys;     // tiles of a part, keys of a part
+  Divisor by_kv_parts, by_q_parts;
+  float* part_kv; float* part_q;              // [parts][dv, dk][B, Tk, Hkv, D], [parts][B, Tq, H, D]
 };
 
 // zeroes the rows [from, to) of a tile of 128 rows x DP bf16 in two or one swizzled halves (zeros need no swizzle); whole warp
@@ -221,23 +225,26 @@ template <int DP> struct KvLayout {
   static_assert(bytes <= 232448, "shared memory budget");
 };
 
-struct KvItem { int b, kh, k0, n, len; };      // n: query tiles to walk
+struct KvItem { int b, kh, k0, len, part, i0, n; };      // n query tiles to walk, from i0 on
 
 // The i-th block of keys that has work: by source, key head, block, so that the blocks that walk the same queries run together and
 // every CTA gets its share whatever the lengths are.
 __device__ __forceinline__ KvItem kv_item_of(const BackwardParams& p, int i) {
+  KvItem t;
+  t.part = i;
+  i = p.by_kv_parts.split(t.part);
   int lo = 0, hi = p.a.B - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (__ldg(p.prefix + mid) * p.a.Hkv <= i) lo = mid; else hi = mid - 1;
   }
-  KvItem t;
   t.b = lo;
   const int first = __ldg(p.prefix + lo), count = __ldg(p.prefix + lo + 1) - first, r = i - first * p.a.Hkv;
   t.kh = r / count;
   t.k0 = r % count * kRows;
   t.len = source_length(p.a, lo);
-  t.n = p.a.H / p.a.Hkv * p.q_tiles;
+  t.i0 = t.part * p.kv_each;
+  t.n = min(p.kv_each, p.a.H / p.a.Hkv * p.q_tiles - t.i0);
   return t;
 }
 // The blocks of keys that have none are zero: the z-th of them.
@@ -317,7 +324,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
   const uint32_t tmem = *tmem_slot;
   const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DP;
 
-  const int items = __ldg(p.prefix + p.a.B) * p.a.Hkv, zeros = p.k_tiles * p.a.B * p.a.Hkv - items;
+  const int blocks = __ldg(p.prefix + p.a.B) * p.a.Hkv, items = blocks * p.kv_parts;
+  const int zeros = p.kv_parts > 1 ? 0 : p.k_tiles * p.a.B * p.a.Hkv - blocks;      // parts: the second launch writes all of dk and dv
   for (int z = blockIdx.x; z < zeros; z += gridDim.x) zero_block(p, z);
   bool ok = true;
   if (warp >= 8) {
@@ -338,7 +346,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           kv_phase ^= 1u;
           for (int i = 0; i < t.n; ++i) {
             if (!ptx::mbar_wait(empty + stage, phase ^ 1u, abort_flag)) { ok = false; break; }
-            int tile = i;
+            int tile = t.i0 + i;
             const int h = t.kh * group + p.by_tiles.split(tile);
             unsigned char* q = ring + stage * L::stage;
             ptx::mbar_arrive_expect_tx(full + stage, L::stage);
@@ -380,17 +388,20 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           if (last) ptx::umma_commit(v_empty);
         };
         auto step = [&] { if (++ahead == kStages) { ahead = 0; ahead_phase ^= 1u; } };
-        const int n = group * p.q_tiles;
+        auto tiles_of = [&](int it) { p.by_kv_parts.split(it); return min(p.kv_each, group * p.q_tiles - it * p.kv_each); };
+        int n = 0, next_n = tiles_of(blockIdx.x);
         if ((int)blockIdx.x < items) {
-          scores(true, n == 1);
-          if (ok) grads(true, n == 1);
+          scores(true, next_n == 1);
+          if (ok) grads(true, next_n == 1);
           step();
         }
         for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
           const bool more = it + (int)gridDim.x < items;
+          n = next_n;
+          next_n = tiles_of(it + gridDim.x);
           for (int i = 0; i < n && ok; ++i) {
             const unsigned char *q = ring + stage * L::stage, *d = q + L::tile;
-            const bool inner = i + 1 < n, fresh = !inner, last = inner ? i + 2 == n : n == 1;
+            const bool inner = i + 1 < n, fresh = !inner, last = inner ? i + 2 == n : next_n == 1;
             if (i == 0 && !wait(o_empty, item_phase ^ 1u)) break;       // the item before has left tensor memory
             if (!wait(p_full, turn)) break;
             ptx::tc_fence_after_sync();
@@ -475,6 +486,16 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       ptx::tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(o_empty);
+      if (p.kv_parts > 1) {                   // a part's sums, in fp32
+        if (zero) continue;
+        float* out = p.part_kv + ((((long long)(t.part * 2 + half) * p.a.B + t.b) * p.a.Tk + row0 + lane) * p.a.Hkv + t.kh) * p.a.D;
+#pragma unroll
+        for (int x = 0; x < DP; x += 4)
+          if (x < p.a.D)
+            *reinterpret_cast<float4*>(out + x) = make_float4(__uint_as_float(o[x]), __uint_as_float(o[x + 1]), __uint_as_float(o[x + 2]),
+                                                              __uint_as_float(o[x + 3]));
+        continue;
+      }
 #pragma unroll
       for (int j = 0; j < DP / 32; ++j) {
         uint32_t w[16];
@@ -569,12 +590,16 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   const uint32_t tmem = *tmem_slot;           // S (two buffers), dP, dq
   const uint32_t t_dp = tmem + 256, t_dq = tmem + 384;
 
-  // item: query tile (fastest), head, batch
-  auto tile_of = [&](int i) { p.by_tiles.split(i); return i; };
-  auto head_of = [&](int i) { int h = p.by_tiles.quotient(i); p.by_heads.split(h); return h; };
-  auto batch_of = [&](int i) { return p.by_heads.quotient(p.by_tiles.quotient(i)); };
+  // item: part of the source (fastest), query tile, head, batch
+  auto part_of = [&](int i) { p.by_q_parts.split(i); return i; };
+  auto rows_of = [&](int i) { return p.by_q_parts.quotient(i); };      // the item's rows: query tile, head and batch
+  auto tile_of = [&](int i) { i = rows_of(i); p.by_tiles.split(i); return i; };
+  auto head_of = [&](int i) { int h = p.by_tiles.quotient(rows_of(i)); p.by_heads.split(h); return h; };
+  auto batch_of = [&](int i) { return p.by_heads.quotient(p.by_tiles.quotient(rows_of(i))); };
+  auto first_of = [&](int i) { return part_of(i) * p.q_keys; };        // the item's keys: the first, and how many
+  auto length_of = [&](int i) { return min(max(source_length(p.a, batch_of(i)) - first_of(i), 0), p.q_keys); };
   // whether the last block has rows between its last key and the next multiple of 16, where its product ends, that TMA has not zeroed
-  auto ragged = [&](int len) { return (len & 15) != 0 && len < p.a.Tk; };
+  auto ragged = [&](int i, int len) { return (len & 15) != 0 && first_of(i) + len < p.a.Tk; };
 
   bool ok = true;
   if (warp >= 8) {
@@ -585,12 +610,12 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         const uint64_t again = ptx::policy_evict_last(), once = ptx::policy_evict_first();
         int ks = 0, vs = 0; uint32_t k_phase = 0, v_phase = 0, q_phase = 0;
         for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-          const int h = head_of(i), b = batch_of(i), kh = p.by_group.quotient(h), len = source_length(p.a, b);
+          const int h = head_of(i), b = batch_of(i), kh = p.by_group.quotient(h), len = length_of(i), first = first_of(i);
           if (len == 0) continue;
           auto load_k = [&](int k0) {
             if (!ptx::mbar_wait(k_empty + ks, k_phase ^ 1u, abort_flag)) { ok = false; return; }
             ptx::mbar_arrive_expect_tx(k_full + ks, L::tile);
-            load_rows<DP>(sk + ks * L::tile, &map_k, k_full + ks, kh, k0, b, again);
+            load_rows<DP>(sk + ks * L::tile, &map_k, k_full + ks, kh, first + k0, b, again);
             if (++ks == kK) { ks = 0; k_phase ^= 1u; }
           };
           load_k(0);
@@ -609,7 +634,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           for (int k0 = 0; k0 < len && ok; k0 += kRows) {
             if (!ptx::mbar_wait(v_empty + vs, v_phase ^ 1u, abort_flag)) { ok = false; break; }
             ptx::mbar_arrive_expect_tx(v_full + vs, L::tile);
-            load_rows<DP>(sv + vs * L::tile, &map_v, v_full + vs, kh, k0, b, again);
+            load_rows<DP>(sv + vs * L::tile, &map_v, v_full + vs, kh, first + k0, b, again);
             if (++vs == kV) { vs = 0; v_phase ^= 1u; }
             if (k0 + kRows < len) load_k(k0 + kRows);
           }
@@ -625,12 +650,12 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           return ok;
         };
         for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-          const int len = source_length(p.a, batch_of(i));
+          const int len = length_of(i);
           if (len == 0) continue;
           const int blocks = ceil_div(len, kRows);
           auto scores = [&](int j) {
             if (!wait(k_full + ks, k_phase)) return;
-            if (j == blocks - 1 && ragged(len) && !wait(k_clean + ks, k_phase)) return;
+            if (j == blocks - 1 && ragged(i, len) && !wait(k_clean + ks, k_phase)) return;
             mma_rows<DP>(tmem + (j & 1) * kRows, sq, sk + ks * L::tile);
             ptx::umma_commit(s_full + (j & 1));
             if (++ks == kK) { ks = 0; k_phase ^= 1u; }
@@ -669,11 +694,11 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       // It follows every stage, so that no phase of the barriers passes by unseen.
       int ks = 0; uint32_t k_phase = 0;
       for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-        const int len = source_length(p.a, batch_of(i));
+        const int len = length_of(i);
         for (int k0 = 0; k0 < len; k0 += kRows) {
           if (!ptx::mbar_wait_all(k_full + ks, k_phase, abort_flag)) { ok = false; break; }
           const int left = len - k0;
-          if (left <= kRows && ragged(len)) zero_rows<DP>(sk + ks * L::tile, left, (left + 15) & ~15, lane);
+          if (left <= kRows && ragged(i, len)) zero_rows<DP>(sk + ks * L::tile, left, (left + 15) & ~15, lane);
           if (lane == 0) {
             ptx::mbar_arrive(k_clean + ks);
             ptx::mbar_arrive(k_empty + ks);
@@ -691,16 +716,16 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     const int r = threadIdx.x & 127;
     uint32_t s_phase[2] = {0, 0}, dp_phase = 0, o_phase = 0;
     for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-      const int h = head_of(i), b = batch_of(i), len = source_length(p.a, b);
+      const int h = head_of(i), b = batch_of(i), len = length_of(i);
       const int q0 = tile_of(i) * kRows;
       const bool in = q0 + r < p.a.Tq;
       __nv_bfloat16* dq = static_cast<__nv_bfloat16*>(p.a.dq) + ((long long)b * p.a.Tq + q0 + r) * p.a.q_stride + (long long)h * p.a.D;
       if (len == 0) {
-        if (in && half == 0)
+        if (in && half == 0 && p.q_parts == 1)
           for (int d = 0; d < p.a.D; d += 8) *reinterpret_cast<uint4*>(dq + d) = make_uint4(0, 0, 0, 0);
         continue;
       }
-      const float* stat = p.stats + (long long)i * kStatFloats;
+      const float* stat = p.stats + (long long)rows_of(i) * kStatFloats;
       const float lse = __ldg(stat + r), delta = __ldg(stat + kRows + r);
       for (int j = 0; j * kRows < len; ++j) {
         const uint32_t my_s = tmem + (j & 1) * kRows + half * 64 + lanes, my_dp = t_dp + half * 64 + lanes;
@@ -743,7 +768,24 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       if (!ptx::mbar_wait_all(o_full, o_phase, abort_flag)) { ok = false; break; }
       o_phase ^= 1u;
       ptx::tc_fence_after_sync();
-      store_row<DP / 2>(t_dq + half * (DP / 2) + lanes, dq, half * (DP / 2), p.a.D, p.a.scale, in, false);
+      if (p.q_parts > 1) {                    // a part's sums, in fp32
+        float* out = p.part_q + ((((long long)part_of(i) * p.a.B + b) * p.a.Tq + q0 + r) * p.a.H + h) * p.a.D;
+#pragma unroll
+        for (int j = 0; j < DP / 64; ++j) {
+          uint32_t o[32];
+          ptx::tmem_ld_32x32(t_dq + half * (DP / 2) + j * 32 + lanes, o);
+          ptx::tmem_ld_wait();
+#pragma unroll
+          for (int x = 0; x < 32; x += 4) {
+            const int col = half * (DP / 2) + j * 32 + x;
+            if (in && col < p.a.D)
+              *reinterpret_cast<float4*>(out + col) = make_float4(__uint_as_float(o[x]), __uint_as_float(o[x + 1]), __uint_as_float(o[x + 2]),
+                                                                  __uint_as_float(o[x + 3]));
+          }
+        }
+      } else {
+  store_row<DP / 2>(t_dq + half * (DP / 2) + lanes, dq, half * (DP / 2), p.a.D, p.a.scale, in, false);
+      }
       ptx::tc_fence_before_sync();            // the next item's first dS says that dq has left tensor memory
     }
   }
@@ -770,6 +812,21 @@ int allow_shared(K kernel, int bytes) {
   return GSHARD_ERR_CUDA;
 }
 
+size_t prefix_floats(int B) { return ((size_t)B + 1 + 3) / 4 * 4; }        // what follows is read 16 bytes at a time
+size_t rows_floats(const AttentionArgs& a) { return (size_t)a.B * a.Tq * a.H * a.D; }
+
+// dk and dv: in query tiles of all the heads of a group; dq: in blocks of 128 keys
+struct BackwardSplit { Parts kv, q; size_t kv_floats, q_floats; };
+BackwardSplit split_of(const AttentionArgs& a) {
+  BackwardSplit s;
+  const int q_tiles = ceil_div(a.Tq, kRows), k_tiles = ceil_div(a.Tk, kRows);
+  s.kv = parts_of((long long)k_tiles * a.Hkv * a.B, q_tiles * (a.H / a.Hkv), 148);
+  s.q = parts_of((long long)q_tiles * a.H * a.B, k_tiles, 148);
+  s.kv_floats = s.kv.parts > 1 ? (size_t)s.kv.parts * 2 * a.B * a.Tk * a.Hkv * a.D : 0;
+  s.q_floats = s.q.parts > 1 ? s.q.parts * rows_floats(a) : 0;
+  return s;
+}
+
 template <int DP>
 int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   BackwardParams p;
@@ -777,13 +834,23 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   p.stats = stats;
   p.q_tiles = ceil_div(a.Tq, kRows);
   p.k_tiles = ceil_div(a.Tk, kRows);
-  p.items = p.q_tiles * a.H * a.B;
+  const BackwardSplit split = split_of(a);
+  p.kv_parts = split.kv.parts;
+  p.kv_each = split.kv.each;
+  p.q_parts = split.q.parts;
+  p.q_keys = split.q.each * kRows;
+  p.by_kv_parts = Divisor(p.kv_parts);
+  p.by_q_parts = Divisor(p.q_parts);
+  const int rows = p.q_tiles * a.H * a.B;     // tiles of rows
+  p.items = rows * p.q_parts;
   p.by_tiles = Divisor(std::max(1, p.q_tiles));
   p.by_heads = Divisor(a.H);
   p.by_group = Divisor(a.H / a.Hkv);
   const int kv_items = p.k_tiles * a.Hkv * a.B;
-  int* prefix = reinterpret_cast<int*>(stats + (size_t)p.items * kStatFloats);
+  int* prefix = reinterpret_cast<int*>(stats + (size_t)rows * kStatFloats);
   p.prefix = prefix;
+  p.part_kv = reinterpret_cast<float*>(prefix) + prefix_floats(a.B);
+  p.part_q = p.part_kv + split.kv_floats;
   attention_stats_kernel<<<(unsigned)((long long)a.B * p.q_tiles * ceil_div(kRows * a.H, kStatRows) + 1), 256, 0, st>>>(a, stats, prefix, p.q_tiles);
   count_launch();
   CUtensorMap q, k, v, dout, dk, dv;
@@ -802,7 +869,7 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
     return GSHARD_ERR_CUDA;
   if (kv_items) {
     GS_CHECK(allow_shared(attention_dkv_kernel<DP>, KvLayout<DP>::bytes));
-    attention_dkv_kernel<DP><<<std::min(kv_items, device_sms()), kThreads, KvLayout<DP>::bytes, st>>>(q, k, v, dout, dk, dv, p);
+    attention_dkv_kernel<DP><<<std::min(kv_items * p.kv_parts, device_sms()), kThreads, KvLayout<DP>::bytes, st>>>(q, k, v, dout, dk, dv, p);
     count_launch();
   }
   if (p.items) {
@@ -810,12 +877,23 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
     attention_dq_kernel<DP><<<std::min(p.items, device_sms()), kThreads, QLayout<DP>::bytes, st>>>(q, k, v, dout, p);
     count_launch();
   }
-  return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
+  if (cudaGetLastError() != cudaSuccess) return GSHARD_ERR_CUDA;
+  if (p.kv_parts > 1) {                       // [part][dv, dk]
+    const size_t one = (size_t)a.B * a.Tk * a.Hkv * a.D;
+    GS_CHECK(launch_join_gradient(a, true, p.part_kv, p.kv_parts, 0, a.dv, a.Tk, a.Hkv, a.v_stride, 1.f, st, 2 * one));
+    GS_CHECK(launch_join_gradient(a, true, p.part_kv + one, p.kv_parts, 0, a.dk, a.Tk, a.Hkv, a.k_stride, a.scale, st, 2 * one));
+  }
+  if (p.q_parts > 1)
+    GS_CHECK(launch_join_gradient(a, true, p.part_q, p.q_parts, p.q_keys, a.dq, a.Tq, a.H, a.q_stride, a.scale, st, rows_floats(a)));
+  return GSHARD_OK;
 }
 
 }  // namespace
 
-size_t attention_stats_floats(int B, int Tq, int H) { return (size_t)ceil_div(Tq, kRows) * kStatFloats * H * B + B + 1; }
+size_t attention_umma_backward_floats(const AttentionArgs& a) {
+  const BackwardSplit split = split_of(a);
+  return (size_t)ceil_div(a.Tq, kRows) * kStatFloats * a.H * a.B + prefix_floats(a.B) + split.kv_floats + split.q_floats;
+}
 
 int launch_attention_umma_backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   return a.D <= 64 ? backward<64>(a, stats, st) : backward<128>(a, stats, st);

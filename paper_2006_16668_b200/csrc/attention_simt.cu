@@ -6,8 +6,9 @@
 // reads of eight neighbouring rows fall into different banks; products take two fp32 values per instruction, along the
 // head dimension for the scores and along the columns for the outputs.
 // The backward runs over the scores twice, once per block of keys (dk, dv) and once per block of queries (dq): seven
-// products instead of five, but every gradient is summed by one block in a fixed order, without atomics.
+// products instead of five, but every gradient is summed in a fixed order, without atomics.
 #include "attention.cuh"
+#include "checks.cuh"
 #include "pack.cuh"
 #include "sm100_ptx.cuh"
 
@@ -116,6 +117,10 @@ __device__ __forceinline__ void store_tile(float* dst, long long stride, int row
     }
 }
 
+// An item's part of a long axis, `each` tiles of it.  More parts than one leave their sums in `out` [parts][B, tokens, heads, D]
+// (for dk and dv: dv, then dk), the forward's with their lse in powers of two, [parts][B, Tq, H].
+struct Split { int parts, each; float* out; float* lse; };
+
 template <typename F>
 __device__ __forceinline__ float over_columns(float v, F f) {       // over the 16 threads of a row
 #pragma unroll
@@ -124,16 +129,18 @@ __device__ __forceinline__ float over_columns(float v, F f) {       // over the 
 }
 
 template <int DP>
-__global__ void __launch_bounds__(kThreads) attention_simt_forward_kernel(const AttentionArgs a) {
+__global__ void __launch_bounds__(kThreads) attention_simt_forward_kernel(const AttentionArgs a, const Split split) {
   extern __shared__ __align__(16) float smem[];
   float *sq = smem, *sk = sq + BT * kPitch<DP>, *sv = sk + BT * kPitch<DP>, *sp = sv + BT * kPitch<DP>;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int tiles = ceil_div(a.Tq, BT);
-  const int q0 = blockIdx.x % tiles * BT, h = blockIdx.x / tiles % a.H, b = blockIdx.x / tiles / a.H;
-  const int kh = h / (a.H / a.Hkv), len = source_length(a, b), rows = min(BT, a.Tq - q0);
+  const int part = blockIdx.x % split.parts, item = blockIdx.x / split.parts;
+  const int q0 = item % tiles * BT, h = item / tiles % a.H, b = item / tiles / a.H;
+  const int kh = h / (a.H / a.Hkv), rows = min(BT, a.Tq - q0);
+  const int first = part * split.each * BT, len = min(max(source_length(a, b) - first, 0), split.each * BT);   // the part's keys
   const float* q = static_cast<const float*>(a.q) + ((long long)b * a.Tq + q0) * a.q_stride + (long long)h * a.D;
-  const float* k = static_cast<const float*>(a.k) + (long long)b * a.Tk * a.k_stride + (long long)kh * a.D;
-  const float* v = static_cast<const float*>(a.v) + (long long)b * a.Tk * a.v_stride + (long long)kh * a.D;
+  const float* k = static_cast<const float*>(a.k) + ((long long)b * a.Tk + first) * a.k_stride + (long long)kh * a.D;
+  const float* v = static_cast<const float*>(a.v) + ((long long)b * a.Tk + first) * a.v_stride + (long long)kh * a.D;
   load_tile<DP>(sq, q, a.q_stride, rows, a.D);
   f32x2 acc[4][DP / 64][2];
   clear<DP>(acc);
@@ -191,22 +198,26 @@ __global__ void __launch_bounds__(kThreads) attention_simt_forward_kernel(const 
   for (int i = 0; i < 4; ++i) {
     const float total = over_columns(sum[i], [](float x, float y) { return x + y; });
     factor[i] = len ? 1.f / total : 0.f;
-    if (a.lse && tx == 0 && ty + 16 * i < rows)
+    if (tx != 0 || ty + 16 * i >= rows) continue;
+    if (split.parts > 1)
+      split.lse[(((long long)part * a.B + b) * a.Tq + q0 + ty + 16 * i) * a.H + h] = len ? fmaf(top[i], c, log2f(total)) : -INFINITY;
+    else if (a.lse)
       a.lse[((long long)b * a.H + h) * a.Tq + q0 + ty + 16 * i] = len ? top[i] * a.scale + logf(total) : -INFINITY;
   }
-  store_tile<DP>(static_cast<float*>(a.o) + (((long long)b * a.Tq + q0) * a.H + h) * a.D, (long long)a.H * a.D, rows, a.D, acc, factor, tx,
-                    ty);
+  float* out = split.parts > 1 ? split.out + (long long)part * a.B * a.Tq * a.H * a.D : static_cast<float*>(a.o);
+  store_tile<DP>(out + (((long long)b * a.Tq + q0) * a.H + h) * a.D, (long long)a.H * a.D, rows, a.D, acc, factor, tx, ty);
 }
 
 // dk and dv of 64 keys: the score tiles are computed key by query, over the queries of every head that shares the keys.
 template <int DP>
-__global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const AttentionArgs a) {
+__global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const AttentionArgs a, const Split split) {
   extern __shared__ __align__(16) float smem[];
   float *sk = smem, *sv = sk + BT * kPitch<DP>, *sq = sv + BT * kPitch<DP>, *sd = sq + BT * kPitch<DP>, *sp = sd + BT * kPitch<DP>;
   float *slse = sp + BT * PP, *sdelta = slse + BT;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int tiles = ceil_div(a.Tk, BT);
-  const int k0 = blockIdx.x % tiles * BT, kh = blockIdx.x / tiles % a.Hkv, b = blockIdx.x / tiles / a.Hkv;
+  const int part = blockIdx.x % split.parts, item = blockIdx.x / split.parts;
+  const int k0 = item % tiles * BT, kh = item / tiles % a.Hkv, b = item / tiles / a.Hkv;
   const int len = source_length(a, b), rows = min(BT, a.Tk - k0), group = a.H / a.Hkv;
   const long long koff = ((long long)b * a.Tk + k0) * a.k_stride + (long long)kh * a.D;
   const long long voff = ((long long)b * a.Tk + k0) * a.v_stride + (long long)kh * a.D;
@@ -217,7 +228,7 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const Atte
   if (k0 < len) {
     load_tile<DP>(sk, static_cast<const float*>(a.k) + koff, a.k_stride, len - k0, a.D);
     load_tile<DP>(sv, static_cast<const float*>(a.v) + voff, a.v_stride, len - k0, a.D);
-    const int n = group * ceil_div(a.Tq, BT);          // query tiles, head by head
+    const int i0 = part * split.each, n = min(i0 + split.each, group * ceil_div(a.Tq, BT));       // query tiles, head by head
     auto head_of = [&](int i) { return kh * group + i / ceil_div(a.Tq, BT); };
     auto first_of = [&](int i) { return i % ceil_div(a.Tq, BT) * BT; };
     auto load_do = [&](int i) {
@@ -230,10 +241,10 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const Atte
       load_tile<DP>(sq, static_cast<const float*>(a.q) + ((long long)b * a.Tq + q0) * a.q_stride + (long long)h * a.D, a.q_stride,
                     i < n ? a.Tq - q0 : 0, a.D);
     };
-    load_do(0);
-    load_q(0);
+    load_do(i0);
+    load_q(i0);
     // dO is read for the last time before Q is: its next tile is on its way during the last product, that of Q during the first
-    for (int i = 0; i < n; ++i) {
+    for (int i = i0; i < n; ++i) {
       if (threadIdx.x < BT) {
         const int t = first_of(i) + (int)threadIdx.x;
         const long long row = ((long long)b * a.H + head_of(i)) * a.Tq + t;
@@ -271,23 +282,33 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dkv_kernel(const Atte
     }
     landed<0>();
   }
-  // keys behind the length have gradient zero: their scores were zero throughout
   const float one[4] = {1.f, 1.f, 1.f, 1.f}, scale[4] = {a.scale, a.scale, a.scale, a.scale};
+  if (split.parts > 1) {
+    if (k0 >= len) return;
+    const long long size = (long long)a.B * a.Tk * a.Hkv * a.D, pitch = (long long)a.Hkv * a.D;
+    float* out = split.out + part * 2 * size + ((long long)b * a.Tk + k0) * pitch + (long long)kh * a.D;
+    store_tile<DP>(out, pitch, rows, a.D, dv, one, tx, ty);
+    store_tile<DP>(out + size, pitch, rows, a.D, dk, one, tx, ty);
+    return;
+  }
+  // keys behind the length have gradient zero: their scores were zero throughout
   store_tile<DP>(static_cast<float*>(a.dk) + koff, a.k_stride, rows, a.D, dk, scale, tx, ty);
   store_tile<DP>(static_cast<float*>(a.dv) + voff, a.v_stride, rows, a.D, dv, one, tx, ty);
 }
 
 template <int DP>
-__global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const AttentionArgs a) {
+__global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const AttentionArgs a, const Split split) {
   extern __shared__ __align__(16) float smem[];
   float *sq = smem, *sd = sq + BT * kPitch<DP>, *sk = sd + BT * kPitch<DP>, *sv = sk + BT * kPitch<DP>, *sp = sv + BT * kPitch<DP>;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int tiles = ceil_div(a.Tq, BT);
-  const int q0 = blockIdx.x % tiles * BT, h = blockIdx.x / tiles % a.H, b = blockIdx.x / tiles / a.H;
-  const int kh = h / (a.H / a.Hkv), len = source_length(a, b), rows = min(BT, a.Tq - q0);
+  const int part = blockIdx.x % split.parts, item = blockIdx.x / split.parts;
+  const int q0 = item % tiles * BT, h = item / tiles % a.H, b = item / tiles / a.H;
+  const int kh = h / (a.H / a.Hkv), rows = min(BT, a.Tq - q0);
+  const int first = part * split.each * BT, len = min(max(source_length(a, b) - first, 0), split.each * BT);   // the part's keys
   const long long qoff = ((long long)b * a.Tq + q0) * a.q_stride + (long long)h * a.D;
-  const float* k = static_cast<const float*>(a.k) + (long long)b * a.Tk * a.k_stride + (long long)kh * a.D;
-  const float* v = static_cast<const float*>(a.v) + (long long)b * a.Tk * a.v_stride + (long long)kh * a.D;
+  const float* k = static_cast<const float*>(a.k) + ((long long)b * a.Tk + first) * a.k_stride + (long long)kh * a.D;
+  const float* v = static_cast<const float*>(a.v) + ((long long)b * a.Tk + first) * a.v_stride + (long long)kh * a.D;
   f32x2 dq[4][DP / 64][2];
   clear<DP>(dq);
   const float c = a.scale * kLog2e;
@@ -326,39 +347,81 @@ __global__ void __launch_bounds__(kThreads) attention_simt_dq_kernel(const Atten
     }
     landed<0>();
   }
+  if (split.parts > 1) {
+    const float one[4] = {1.f, 1.f, 1.f, 1.f};
+    float* out = split.out + (((long long)(part * a.B + b) * a.Tq + q0) * a.H + h) * a.D;
+    if (len) store_tile<DP>(out, (long long)a.H * a.D, rows, a.D, dq, one, tx, ty);
+    return;
+  }
   const float scale[4] = {a.scale, a.scale, a.scale, a.scale};
   store_tile<DP>(static_cast<float*>(a.dq) + qoff, a.q_stride, rows, a.D, dq, scale, tx, ty);
 }
 
 template <typename K>
-int launch(K kernel, long long blocks, int floats, const AttentionArgs& a, cudaStream_t st) {
+int launch(K kernel, long long blocks, int floats, const AttentionArgs& a, const Split& split, cudaStream_t st) {
   const int bytes = floats * 4;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
     cudaGetLastError();
     return GSHARD_ERR_CUDA;
   }
-  kernel<<<(unsigned)blocks, kThreads, bytes, st>>>(a);
+  kernel<<<(unsigned)(blocks * split.parts), kThreads, bytes, st>>>(a, split);
   count_launch();
   return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
 }
 
+// shared memory holds one block per SM with heads of 128 dimensions, and registers two with 64
+int slots_of(const AttentionArgs& a) { return a.D <= 64 ? 296 : 148; }
+long long q_blocks(const AttentionArgs& a) { return (long long)ceil_div(a.Tq, BT) * a.H * a.B; }
+long long k_blocks(const AttentionArgs& a) { return (long long)ceil_div(a.Tk, BT) * a.Hkv * a.B; }
+Parts source_parts(const AttentionArgs& a) { return parts_of(q_blocks(a), ceil_div(a.Tk, BT), slots_of(a)); }          // forward, dq
+Parts query_parts(const AttentionArgs& a) { return parts_of(k_blocks(a), ceil_div(a.Tq, BT) * (a.H / a.Hkv), slots_of(a)); }      // dk, dv
+size_t outputs_of(const AttentionArgs& a, int parts) { return parts > 1 ? (size_t)parts * a.B * a.Tq * a.H * a.D : 0; }
+
 template <int DP>
-int backward(const AttentionArgs& a, cudaStream_t st) {
+int backward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
   const int floats = 4 * BT * kPitch<DP> + BT * PP + 2 * BT;
-  const int rc = a.Tk ? launch(attention_simt_dkv_kernel<DP>, (long long)ceil_div(a.Tk, BT) * a.Hkv * a.B, floats, a, st) : GSHARD_OK;
-  if (rc != GSHARD_OK || !a.Tq) return rc;
-  return launch(attention_simt_dq_kernel<DP>, (long long)ceil_div(a.Tq, BT) * a.H * a.B, floats, a, st);
+  const Parts q = query_parts(a), s = source_parts(a);
+  if (a.Tk) {
+    GS_CHECK(launch(attention_simt_dkv_kernel<DP>, k_blocks(a), floats, a, Split{q.parts, q.each, scratch, nullptr}, st));
+    if (q.parts > 1) {
+      const size_t one = (size_t)a.B * a.Tk * a.Hkv * a.D;
+      GS_CHECK(launch_join_gradient(a, false, scratch, q.parts, 0, a.dv, a.Tk, a.Hkv, a.v_stride, 1.f, st, 2 * one));
+      GS_CHECK(launch_join_gradient(a, false, scratch + one, q.parts, 0, a.dk, a.Tk, a.Hkv, a.k_stride, a.scale, st, 2 * one));
+    }
+  }
+  if (!a.Tq) return GSHARD_OK;
+  GS_CHECK(launch(attention_simt_dq_kernel<DP>, q_blocks(a), floats, a, Split{s.parts, s.each, scratch, nullptr}, st));
+  if (s.parts == 1) return GSHARD_OK;
+  return launch_join_gradient(a, false, scratch, s.parts, s.each * BT, a.dq, a.Tq, a.H, a.q_stride, a.scale, st, outputs_of(a, s.parts) / s.parts);
 }
 
 template <int DP>
-int forward(const AttentionArgs& a, cudaStream_t st) {
-  return launch(attention_simt_forward_kernel<DP>, (long long)ceil_div(a.Tq, BT) * a.H * a.B, 3 * BT * kPitch<DP> + BT * PP, a, st);
+int forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
+  const Parts s = source_parts(a);
+  float* part_lse = scratch + outputs_of(a, s.parts);
+  GS_CHECK(launch(attention_simt_forward_kernel<DP>, q_blocks(a), 3 * BT * kPitch<DP> + BT * PP, a, Split{s.parts, s.each, scratch, part_lse}, st));
+  return s.parts > 1 ? launch_join_outputs(a, false, scratch, part_lse, s.parts, st) : GSHARD_OK;
 }
 
 }  // namespace
 
-int launch_attention_simt_forward(const AttentionArgs& a, cudaStream_t st) { return a.D <= 64 ? forward<64>(a, st) : forward<128>(a, st); }
+size_t attention_simt_forward_floats(const AttentionArgs& a) {
+  const int parts = source_parts(a).parts;
+  return parts > 1 ? outputs_of(a, parts) + (size_t)parts * a.B * a.Tq * a.H : 0;
+}
 
-int launch_attention_simt_backward(const AttentionArgs& a, cudaStream_t st) { return a.D <= 64 ? backward<64>(a, st) : backward<128>(a, st); }
+// dk and dv are joined before dq's parts are written
+size_t attention_simt_backward_floats(const AttentionArgs& a) {
+  const int parts = query_parts(a).parts;
+  return std::max(parts > 1 ? (size_t)parts * 2 * a.B * a.Tk * a.Hkv * a.D : 0, outputs_of(a, source_parts(a).parts));
+}
+
+int launch_attention_simt_forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
+  return a.D <= 64 ? forward<64>(a, scratch, st) : forward<128>(a, scratch, st);
+}
+
+int launch_attention_simt_backward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
+  return a.D <= 64 ? backward<64>(a, scratch, st) : backward<128>(a, scratch, st);
+}
 
 }  // namespace gshard

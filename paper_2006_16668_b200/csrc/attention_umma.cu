@@ -14,7 +14,7 @@
 // and sends it off through shared memory (bulk tensor stores) while the next item's first block is being worked on.
 //
 // Where the items do not fill the GPU and the source is long, an item is one of several parts of the source: it leaves its output in fp32
-// and the logarithm of its sums, and a second launch joins them in order (one head, 64 queries, 32768 keys: SPLIT_FIGURES us).
+// and the logarithm of its sums, and a second launch joins them in order (one head, 64 queries, 32768 keys: 46 us).
 //
 // Rows behind the source's length: scores are masked before the maximum; rows of V that hold something else are zeroed in
 // shared memory up to the next multiple of 16, where the last block's product ends.
@@ -522,45 +522,13 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
   }
 }
 
-// Joins the parts of a source: o = sum of w_p o_p with w_p = 2^(lse_p) over their sum; one warp per (token, head).
-__global__ void __launch_bounds__(256) attention_join_kernel(const ForwardParams p, long long rows) {
-  const int lane = threadIdx.x & 31, c = lane * 4;
-  for (long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += (long long)gridDim.x * 8) {
-    float top = -INFINITY;
-    for (int i = 0; i < p.parts; ++i) top = fmaxf(top, p.part_lse[i * rows + r]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < p.parts; ++i) {
-      const float lse = p.part_lse[i * rows + r];
-      if (lse == -INFINITY) continue;          // no key in this part
-      const float w = exp2f(lse - ref);
-      sum += w;
-      if (c < p.a.D) {
-        const float4 x = *reinterpret_cast<const float4*>(p.part_o + (i * rows + r) * p.a.D + c);
-        o[0] = fmaf(w, x.x, o[0]); o[1] = fmaf(w, x.y, o[1]); o[2] = fmaf(w, x.z, o[2]); o[3] = fmaf(w, x.w, o[3]);
-      }
-    }
-    const float factor = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] *= factor;
-    if (c < p.a.D) store_pack<__nv_bfloat16, 4>(static_cast<__nv_bfloat16*>(p.a.o) + r * p.a.D + c, o);
-    if (p.a.lse && lane == 0) {
-      const long long token = r / p.a.H;
-      p.a.lse[((token / p.a.Tq) * p.a.H + r % p.a.H) * p.a.Tq + token % p.a.Tq] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
-    }
-  }
-}
-
-// Parts of the sources: as many as fill the multiprocessors where the items do not, with four blocks of keys in each at least.
-int parts_of(int items, int Tk) {
-  if (items == 0) return 1;
-  return std::max(1, std::min(148 / items, ceil_div(Tk, kRows) / 4));
-}
-
 // Heads of a tile: with all of a group's heads in it the keys are read once for them; the output warps' 32 rows are whole tokens.
 int tile_heads(int group) { return 32 % group == 0 ? group : 1; }
 int tiles_of(int Tq, int group) { return ceil_div(Tq, kRows / tile_heads(group)) * (group / tile_heads(group)); }
 int items_of(int B, int Tq, int H, int Hkv) { return ceil_div(tiles_of(Tq, H / Hkv), 2) * Hkv * B; }
+
+// in blocks of 128 keys
+Parts source_parts(const AttentionArgs& a) { return parts_of(items_of(a.B, a.Tq, a.H, a.Hkv), ceil_div(a.Tk, kRows), 148); }
 
 template <int DP>
 int forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
@@ -572,11 +540,10 @@ int forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
   p.q_tiles = ceil_div(a.Tq, p.tokens);
   p.list = tiles_of(a.Tq, a.H / a.Hkv);
   p.pairs = ceil_div(p.list, 2);
-  const int items = p.pairs * a.Hkv * a.B, blocks = std::max(1, ceil_div(a.Tk, kRows));
-  p.parts = parts_of(items, a.Tk);
-  p.part_keys = ceil_div(blocks, p.parts) * kRows;
-  p.parts = ceil_div(blocks * kRows, p.part_keys);      // none without a block
-  p.items = items * p.parts;
+  const Parts parts = source_parts(a);
+  p.parts = parts.parts;
+  p.part_keys = parts.each * kRows;
+  p.items = p.pairs * a.Hkv * a.B * p.parts;
   p.by_parts = Divisor(p.parts);
   p.by_pairs = Divisor(p.pairs);
   p.by_kv_heads = Divisor(a.Hkv);
@@ -596,18 +563,15 @@ int forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {
   }
   kernel<<<std::min(p.items, device_sms()), kThreads, Layout<DP>::bytes, st>>>(mq, mk, mv, mo, p);
   count_launch();
-  if (p.parts > 1) {
-    attention_join_kernel<<<grid_for_rows(rows), 256, 0, st>>>(p, rows);
-    count_launch();
-  }
-  return cudaGetLastError() == cudaSuccess ? GSHARD_OK : GSHARD_ERR_CUDA;
+  if (cudaGetLastError() != cudaSuccess) return GSHARD_ERR_CUDA;
+  return p.parts > 1 ? launch_join_outputs(a, true, p.part_o, p.part_lse, p.parts, st) : GSHARD_OK;
 }
 
 }  // namespace
 
-size_t attention_parts_floats(int B, int Tq, int Tk, int H, int Hkv, int D) {
-  const int parts = parts_of(items_of(B, Tq, H, Hkv), Tk);
-  return parts > 1 ? (size_t)parts * B * Tq * H * (D + 1) : 0;
+size_t attention_umma_forward_floats(const AttentionArgs& a) {
+  const int parts = source_parts(a).parts;
+  return parts > 1 ? (size_t)parts * a.B * a.Tq * a.H * (a.D + 1) : 0;
 }
 
 int launch_attention_umma_forward(const AttentionArgs& a, float* scratch, cudaStream_t st) {

@@ -114,6 +114,10 @@ SIZES = [  # B, Tq, Tk, H, Hkv, D, lengths, k and v in one buffer
     (2, 20, 5000, 2, 1, 64, [4999, 700], True),
     (3, 13, 2500, 4, 2, 128, [2500, 0, 513], True),
     (1, 300, 4100, 1, 1, 40, [3000], False),
+    # few keys and many rows: parts of the queries
+    (1, 1500, 100, 8, 1, 128, [99], False),
+    (2, 1300, 300, 4, 2, 64, [300, 100], True),
+    (3, 900, 260, 6, 1, 40, [0, 130, 257], False),
 ]
 
 
@@ -141,8 +145,9 @@ def test_many_short_ragged_sources(Tq):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-def test_nothing_between_or_behind_the_rows_is_written(dtype):
-    t = make(2, 150, 140, 4, 2, 64, dtype, [100, 140], fused=True)
+@pytest.mark.parametrize("Tq", [150, 1300])
+def test_nothing_between_or_behind_the_rows_is_written(Tq, dtype):
+    t = make(2, Tq, 140, 4, 2, 64, dtype, [100, 140], fused=True)
     o, lse = forward(t)
     whole = torch.full((2, 140, 3, 2, 64), 7.0, dtype=dtype, device="cuda")
     wide = lambda x: torch.stack((x, x, x), 2)
