@@ -16,6 +16,10 @@
 //   Keys behind the source's length only make rows of their own; these are written as zero.
 // dq: a CTA owns 128 queries of one head and walks the source: S = Q K^T (two buffers), dP = dO V^T, dS over S,
 //   dq += dS K.  Keys behind the length: dS is zero, and rows of K that hold something else are zeroed in shared memory.
+// Both cut their walk into parts where the items do not fill the GPU.
+//
+// Bound by the tensor pipe and the threads' turns: 16 heads of 128, 4 x 4096 x 4096 tokens 1483 us (927 TFLOP/s of the five products, 1298
+// of the seven); 32 x 1000 x 1111 tokens, 4 key heads, 916 to 947 us, of it dk and dv 420, dq 368, statistics 71.
 #include <algorithm>
 
 #include "attention.cuh"
@@ -487,13 +491,13 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(o_empty);
       if (p.kv_parts > 1) {                   // a part's sums, in fp32
-        if (zero) continue;
         float* out = p.part_kv + ((((long long)(t.part * 2 + half) * p.a.B + t.b) * p.a.Tk + row0 + lane) * p.a.Hkv + t.kh) * p.a.D;
 #pragma unroll
         for (int x = 0; x < DP; x += 4)
-          if (x < p.a.D)
+          if (!zero && x < p.a.D)
             *reinterpret_cast<float4*>(out + x) = make_float4(__uint_as_float(o[x]), __uint_as_float(o[x + 1]), __uint_as_float(o[x + 2]),
                                                               __uint_as_float(o[x + 3]));
+        __syncwarp();
         continue;
       }
 #pragma unroll
@@ -784,7 +788,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           }
         }
       } else {
-  store_row<DP / 2>(t_dq + half * (DP / 2) + lanes, dq, half * (DP / 2), p.a.D, p.a.scale, in, false);
+        store_row<DP / 2>(t_dq + half * (DP / 2) + lanes, dq, half * (DP / 2), p.a.D, p.a.scale, in, false);
       }
       ptx::tc_fence_before_sync();            // the next item's first dS says that dq has left tensor memory
     }

@@ -9,6 +9,8 @@
 // registers, dq is added to where it lies, by one block in a fixed order, without atomics.  Blocks enough for the GPU come from parts
 // of the source and of the queries, with sums of their own that a second launch joins.  (8 x 517 x 333 tokens, 16 heads of 64: 417 us,
 // forward 169 us; separate kernels for dq and for dk and dv, with seven products, took 550 us.)
+// Bound by shared memory's operands (data pipe 78 % busy); 8 x 4 values per thread read a quarter less, but leave 8 warps per
+// multiprocessor: 2 % faster with heads of 64, a fifth slower with 128.
 #include "attention.cuh"
 #include "checks.cuh"
 #include "pack.cuh"
@@ -371,18 +373,19 @@ Cut cut_of(const AttentionArgs& a) {
   const double bytes_per_step = 50e6;
   Cut best{{1, k_units}, {1, q_units}, nullptr, nullptr};
   double least = -1;
-  for (int kn = 1; kn <= k_units && (kn == 1 || kn * blocks <= most); ++kn)
+  auto parts = [](int units, int n) { const int each = ceil_div(units, n); return Parts{ceil_div(units, each), each}; };
+  for (int kn = 1; kn <= k_units && (kn == 1 || kn * blocks <= most); ++kn) {
+    const Parts k = parts(k_units, kn);
+    if (k.parts != kn) continue;                        // the same as fewer parts
     for (int qn = 1; qn == 1 || (qn * 4 <= q_units && qn * kn * blocks <= most); ++qn) {
-      Parts k, q;
-      k.each = ceil_div(k_units, kn);
-      k.parts = ceil_div(k_units, k.each);
-      q.each = ceil_div(q_units, qn);
-      q.parts = ceil_div(q_units, q.each);
+      const Parts q = parts(q_units, qn);
+      if (q.parts != qn) continue;
       double cost = k.each * (q.each + 1.) * (1 + (double)blocks * k.parts * q.parts / slots_of(a));
       if (k.parts > 1) cost += 1 + 8. * k.parts * outputs_of(a) / bytes_per_step;
       if (q.parts > 1) cost += 1 + 16. * q.parts * keys_of(a) / bytes_per_step;
       if (least < 0 || cost < least) { best.k = k; best.q = q; least = cost; }
     }
+  }
   return best;
 }
 size_t part_q_floats(const AttentionArgs& a, const Cut& cut) { return cut.k.parts > 1 ? cut.k.parts * outputs_of(a) : 0; }
