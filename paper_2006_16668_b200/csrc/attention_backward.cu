@@ -560,9 +560,11 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   uint64_t* k_empty = k_full + kK;            // MMA, cleaning warp
   uint64_t* v_full = k_empty + kK;
   uint64_t* v_empty = v_full + kV;
-  uint64_t* q_full = v_empty + kV;            // queries and dO landed
-  uint64_t* q_empty = q_full + 1;
-  uint64_t* s_full = q_empty + 1;             // [2]
+  uint64_t* q_full = v_empty + kV;            // queries landed
+  uint64_t* q_empty = q_full + 1;             // ... and have been read for the last time
+  uint64_t* d_full = q_empty + 1;             // dO
+  uint64_t* d_empty = d_full + 1;
+  uint64_t* s_full = d_empty + 1;             // [2]
   uint64_t* dp_full = s_full + 2;
   uint64_t* ds_full = dp_full + 1;            // 8 warps: dS written, dP read
   uint64_t* o_full = ds_full + 1;
@@ -574,7 +576,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   if (threadIdx.x == 0) {
     for (int s = 0; s < kK; ++s) { ptx::mbar_init(k_full + s, 1); ptx::mbar_init(k_empty + s, 2); ptx::mbar_init(k_clean + s, 1); }
     for (int s = 0; s < kV; ++s) { ptx::mbar_init(v_full + s, 1); ptx::mbar_init(v_empty + s, 1); }
-    ptx::mbar_init(q_full, 1); ptx::mbar_init(q_empty, 1);
+    ptx::mbar_init(q_full, 1); ptx::mbar_init(q_empty, 1); ptx::mbar_init(d_full, 1); ptx::mbar_init(d_empty, 1);
     ptx::mbar_init(s_full, 1); ptx::mbar_init(s_full + 1, 1); ptx::mbar_init(dp_full, 1);
     ptx::mbar_init(ds_full, 8); ptx::mbar_init(o_full, 1);
     *abort_flag = 0;
@@ -624,10 +626,12 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           };
           load_k(0);
           if (!ok || !ptx::mbar_wait(q_empty, q_phase ^ 1u, abort_flag)) { ok = false; break; }
-          q_phase ^= 1u;
-          ptx::mbar_arrive_expect_tx(q_full, 2 * L::tile);
+          ptx::mbar_arrive_expect_tx(q_full, L::tile);
           load_rows<DP>(sq, &map_q, q_full, h, tile_of(i) * kRows, b, once);
-          load_rows<DP>(sd, &map_do, q_full, h, tile_of(i) * kRows, b, once);
+          if (!ptx::mbar_wait(d_empty, q_phase ^ 1u, abort_flag)) { ok = false; break; }
+          ptx::mbar_arrive_expect_tx(d_full, L::tile);
+          load_rows<DP>(sd, &map_do, d_full, h, tile_of(i) * kRows, b, once);
+          q_phase ^= 1u;
           if (const int n = i + gridDim.x; n < p.items) {         // the next item's rows into L2: they are loaded only when these have been read
 #pragma unroll
             for (int j = 0; j < DP / 64; ++j) {
@@ -662,6 +666,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             if (j == blocks - 1 && ragged(i, len) && !wait(k_clean + ks, k_phase)) return;
             mma_rows<DP>(tmem + (j & 1) * kRows, sq, sk + ks * L::tile);
             ptx::umma_commit(s_full + (j & 1));
+            if (j == blocks - 1) ptx::umma_commit(q_empty);
             if (++ks == kK) { ks = 0; k_phase ^= 1u; }
           };
           auto grads = [&](int j) {           // dP of block j
@@ -669,15 +674,15 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             mma_rows<DP>(t_dp, sd, sv + vs * L::tile);
             ptx::umma_commit(dp_full);
             ptx::umma_commit(v_empty + vs);
-            if (j == blocks - 1) ptx::umma_commit(q_empty);
+            if (j == blocks - 1) ptx::umma_commit(d_empty);
             if (++vs == kV) { vs = 0; v_phase ^= 1u; }
           };
           if (!wait(q_full, q_phase)) break;
-          q_phase ^= 1u;
           scores(0);
-          // a block's scores always go before its dP, so that "queries read" may follow the last dP
           if (ok && blocks > 1) scores(1);
-          if (ok) grads(0);
+          if (!ok || !wait(d_full, q_phase)) break;
+          q_phase ^= 1u;
+          grads(0);
           for (int j = 0; j < blocks && ok; ++j) {
             if (!wait(ds_full, ds_phase)) break;
             ptx::tc_fence_after_sync();
@@ -719,18 +724,29 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     const float c = p.a.scale * kLog2e;
     const int r = threadIdx.x & 127;
     uint32_t s_phase[2] = {0, 0}, dp_phase = 0, o_phase = 0;
+    // An item's length and its row's statistics are fetched while the item before leaves tensor memory.
+    int raw = 0;
+    float lse = 0.f, delta = 0.f;
+    auto fetch = [&](int i) {
+      if (i >= p.items) return;
+      const float* stat = p.stats + (long long)rows_of(i) * kStatFloats + r;
+      raw = p.a.Tk;
+      if (p.a.lengths) asm volatile("ld.global.b32 %0, [%1];" : "=r"(raw) : "l"(p.a.lengths + batch_of(i)));
+      asm volatile("ld.global.f32 %0, [%1];" : "=f"(lse) : "l"(stat));
+      asm volatile("ld.global.f32 %0, [%1];" : "=f"(delta) : "l"(stat + kRows));
+    };
+    fetch(blockIdx.x);
     for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-      const int h = head_of(i), b = batch_of(i), len = length_of(i);
+      const int h = head_of(i), b = batch_of(i), len = min(max(min(raw, p.a.Tk) - first_of(i), 0), p.q_keys);
       const int q0 = tile_of(i) * kRows;
       const bool in = q0 + r < p.a.Tq;
       __nv_bfloat16* dq = static_cast<__nv_bfloat16*>(p.a.dq) + ((long long)b * p.a.Tq + q0 + r) * p.a.q_stride + (long long)h * p.a.D;
       if (len == 0) {
         if (in && half == 0 && p.q_parts == 1)
           for (int d = 0; d < p.a.D; d += 8) *reinterpret_cast<uint4*>(dq + d) = make_uint4(0, 0, 0, 0);
+        fetch(i + gridDim.x);
         continue;
       }
-      const float* stat = p.stats + (long long)rows_of(i) * kStatFloats;
-      const float lse = __ldg(stat + r), delta = __ldg(stat + kRows + r);
       for (int j = 0; j * kRows < len; ++j) {
         const uint32_t my_s = tmem + (j & 1) * kRows + half * 64 + lanes, my_dp = t_dp + half * 64 + lanes;
         bool here = ptx::mbar_wait(s_full + (j & 1), s_phase[j & 1], abort_flag);
@@ -769,6 +785,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         if (lane == 0) ptx::mbar_arrive(ds_full);
       }
       if (!ok) break;
+      fetch(i + gridDim.x);
       if (!ptx::mbar_wait_all(o_full, o_phase, abort_flag)) { ok = false; break; }
       o_phase ^= 1u;
       ptx::tc_fence_after_sync();
