@@ -19,7 +19,7 @@
 // Both cut their walk into parts where the items do not fill the GPU.
 //
 // Bound by the tensor pipe and the threads' turns: 16 heads of 128, 4 x 4096 x 4096 tokens 1483 us (927 TFLOP/s of the five products, 1298
-// of the seven); 32 x 1000 x 1111 tokens, 4 key heads, 916 to 947 us, of it dk and dv 420, dq 368, statistics 71.
+// of the seven); 32 x 1000 x 1111 tokens, 4 key heads, kernels of 749 us: dk and dv 381, dq 323, statistics 44 (6.0 TB/s).
 #include <algorithm>
 
 #include "attention.cuh"
@@ -81,8 +81,9 @@ __device__ void count_blocks(const AttentionArgs& a, int* prefix) {
   if (threadIdx.x == 0) prefix[a.B] = base;
 }
 
-// A block takes 64 (query, head) rows of a tile, 16 lanes a row and four rows of
-// a group in flight; neighbouring rows are the heads of a token, which lie together in o and dout.
+// A block takes 64 (query, head) rows of a tile: eight neighbouring queries of each of eight heads (so that both what lies together in o
+// and dout and what lies together in the statistics is one block's), 16 lanes a row and four rows of a group in flight.  delta goes
+// through shared memory, after which a thread writes all of a row.
 constexpr int kStatRows = 64;
 // The last block counts the sources' blocks.
 __global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArgs a, float* stats, int* prefix, int q_tiles) {
@@ -91,17 +92,18 @@ __global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArg
     return;
   }
   constexpr int U = kStatRows / 16;
+  __shared__ float s_delta[kStatRows];
   const int part = threadIdx.x & 15, grp = threadIdx.x >> 4, c = part * 8;
   const int parts = ceil_div(kRows * a.H, kStatRows);
   const long long tile = blockIdx.x / parts;            // b * q_tiles + tile of the sequence
   const int b = (int)(tile / q_tiles), t0 = (int)(tile % q_tiles) * kRows;
-  const int r0 = (int)(blockIdx.x % parts) * kStatRows + grp;
+  const int r0 = (int)(blockIdx.x % parts) * kStatRows;
+  auto token_of = [&](int r) { return t0 + r / (8 * a.H) * 8 + r % 8; };
+  auto head_of = [&](int r) { return r % (8 * a.H) / 8; };
   Pack<__nv_bfloat16, 8> x[U], y[U];
-  float lse[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int r = r0 + u * 16, t = t0 + r / a.H, h = r % a.H;
-    lse[u] = part == 0 && r < kRows * a.H && t < a.Tq ? a.lse[((long long)b * a.H + h) * a.Tq + t] : 0.f;
+    const int r = r0 + grp + u * 16, t = token_of(r), h = head_of(r);
     x[u].raw = y[u].raw = make_uint4(0, 0, 0, 0);
     if (r < kRows * a.H && t < a.Tq && c < a.D) {
       const long long off = (((long long)b * a.Tq + t) * a.H + h) * a.D + c;
@@ -109,28 +111,31 @@ __global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArg
       y[u].load_once(static_cast<const __nv_bfloat16*>(a.dout) + off);
     }
   }
+  const int r = r0 + threadIdx.x, t = token_of(r), h = head_of(r);
+  const bool mine = threadIdx.x < kStatRows && r < kRows * a.H;
+  const float lse = mine && t < a.Tq ? a.lse[((long long)b * a.H + h) * a.Tq + t] : 0.f;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int r = r0 + u * 16, t = t0 + r / a.H, h = r % a.H;
     float delta = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) delta = fmaf(x[u].get(j), y[u].get(j), delta);
 #pragma unroll
     for (int off = 8; off; off >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, off);
-    if (part == 0 && r < kRows * a.H) {
-      const long long head = (long long)b * a.H + h;
-      float* out = stats + (head * q_tiles + t0 / kRows) * kStatFloats;
-      const int row = r / a.H;
-      out[row] = t < a.Tq ? lse[u] * kLog2e : INFINITY;
-      out[kRows + row] = delta;
-      alignas(16) unsigned short terms[8] = {};
-      put_terms(t < a.Tq ? -lse[u] / a.scale : -1e30f, terms);
-      put_terms(-delta, terms + 3);
-      uint4* step = reinterpret_cast<uint4*>(out + 2 * kRows) + row / 8 * 16 + row % 8;
-      step[0] = *reinterpret_cast<const uint4*>(terms);
-      step[8] = make_uint4(0, 0, 0, 0);
-    }
+    if (part == 0) s_delta[grp + u * 16] = delta;
   }
+  __syncthreads();
+  if (!mine) return;
+  const float delta = s_delta[threadIdx.x];
+  float* out = stats + (((long long)b * a.H + h) * q_tiles + t0 / kRows) * kStatFloats;
+  const int row = t - t0;
+  out[row] = t < a.Tq ? lse * kLog2e : INFINITY;
+  out[kRows + row] = delta;
+  alignas(16) unsigned short terms[8] = {};
+  put_terms(t < a.Tq ? -lse / a.scale : -1e30f, terms);
+  put_terms(-delta, terms + 3);
+  uint4* step = reinterpret_cast<uint4*>(out + 2 * kRows) + row / 8 * 16 + row % 8;
+  step[0] = *reinterpret_cast<const uint4*>(terms);
+  step[8] = make_uint4(0, 0, 0, 0);
 }
 
 struct BackwardParams {
