@@ -19,7 +19,8 @@
 // Both cut their walk into parts where the items do not fill the GPU.
 //
 // Bound by the tensor pipe and the threads' turns: 16 heads of 128, 4 x 4096 x 4096 tokens 1483 us (927 TFLOP/s of the five products, 1298
-// of the seven); 32 x 1000 x 1111 tokens, 4 key heads, kernels of 749 us: dk and dv 381, dq 323, statistics 44 (6.0 TB/s).
+// of the seven); 32 x 1000 x 1111 tokens, 4 key heads, kernels of 711 us: dk and dv 385, dq 281, statistics 44 (6.0 TB/s).
+// (dq stored row by row from registers: 324, a store touching 32 lines at once.)
 #include <algorithm>
 
 #include "attention.cuh"
@@ -201,25 +202,6 @@ __device__ __forceinline__ void mma_weights(uint32_t d, uint32_t a, const unsign
 __device__ __forceinline__ uint32_t pack2(float x, float y) {
   const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&b);
-}
-
-// COLS accumulator columns of this thread's row, times factor, to a row of D elements (column 0 of the thread's share is col0)
-template <int COLS>
-__device__ __forceinline__ void store_row(uint32_t taddr, __nv_bfloat16* out, int col0, int D, float factor, bool live, bool zero) {
-#pragma unroll
-  for (int j = 0; j < COLS / 32; ++j) {
-    uint32_t o[32];
-    ptx::tmem_ld_32x32(taddr + j * 32, o);
-    ptx::tmem_ld_wait();
-    if (!live) continue;
-#pragma unroll
-    for (int d = 0; d < 32; d += 8) {
-      float f[8];
-#pragma unroll
-      for (int x = 0; x < 8; ++x) f[x] = zero ? 0.f : __uint_as_float(o[d + x]) * factor;
-      if (col0 + j * 32 + d < D) store_pack<__nv_bfloat16, 8>(out + col0 + j * 32 + d, f);
-    }
-  }
 }
 
 template <int DP> struct KvLayout {
@@ -554,7 +536,8 @@ template <int DP> struct QLayout {
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                    const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const BackwardParams p) {
+                    const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
+                    const __grid_constant__ CUtensorMap map_dq, const BackwardParams p) {
   using L = QLayout<DP>;
   constexpr int kK = L::k_stages, kV = L::v_stages;
   extern __shared__ unsigned char smem_raw[];
@@ -574,12 +557,13 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   uint64_t* ds_full = dp_full + 1;            // 8 warps: dS written, dP read
   uint64_t* o_full = ds_full + 1;
   uint64_t* k_clean = o_full + 1;             // [kK] looked through for rows behind the last key
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(k_clean + kK);
+  uint64_t* out_read = k_clean + kK;          // [kK] 8 warps: an item's dq, staged in its last keys' place, has been read
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(out_read + kK);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kK; ++s) { ptx::mbar_init(k_full + s, 1); ptx::mbar_init(k_empty + s, 2); ptx::mbar_init(k_clean + s, 1); }
+    for (int s = 0; s < kK; ++s) { ptx::mbar_init(k_full + s, 1); ptx::mbar_init(k_empty + s, 2); ptx::mbar_init(k_clean + s, 1); ptx::mbar_init(out_read + s, 8); }
     for (int s = 0; s < kV; ++s) { ptx::mbar_init(v_full + s, 1); ptx::mbar_init(v_empty + s, 1); }
     ptx::mbar_init(q_full, 1); ptx::mbar_init(q_empty, 1); ptx::mbar_init(d_full, 1); ptx::mbar_init(d_empty, 1);
     ptx::mbar_init(s_full, 1); ptx::mbar_init(s_full + 1, 1); ptx::mbar_init(dp_full, 1);
@@ -590,6 +574,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     ptx::prefetch_tensormap(&map_k);
     ptx::prefetch_tensormap(&map_v);
     ptx::prefetch_tensormap(&map_do);
+    ptx::prefetch_tensormap(&map_dq);
   }
   if (warp == 9) {
     ptx::tmem_alloc(tmem_slot, 512);
@@ -620,11 +605,18 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       if (lane == 0) {
         const uint64_t again = ptx::policy_evict_last(), once = ptx::policy_evict_first();
         int ks = 0, vs = 0; uint32_t k_phase = 0, v_phase = 0, q_phase = 0;
+        uint32_t staged = 0, out_phase = 0;   // bit per stage: an item's last keys are in it
         for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
           const int h = head_of(i), b = batch_of(i), kh = p.by_group.quotient(h), len = length_of(i), first = first_of(i);
           if (len == 0) continue;
           auto load_k = [&](int k0) {
             if (!ptx::mbar_wait(k_empty + ks, k_phase ^ 1u, abort_flag)) { ok = false; return; }
+            if (staged >> ks & 1u) {
+              if (!ptx::mbar_wait(out_read + ks, out_phase >> ks & 1u, abort_flag)) { ok = false; return; }
+              out_phase ^= 1u << ks;
+              staged ^= 1u << ks;
+            }
+            if (k0 + kRows >= len && p.q_parts == 1) staged |= 1u << ks;
             ptx::mbar_arrive_expect_tx(k_full + ks, L::tile);
             load_rows<DP>(sk + ks * L::tile, &map_k, k_full + ks, kh, first + k0, b, again);
             if (++ks == kK) { ks = 0; k_phase ^= 1u; }
@@ -741,6 +733,8 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       asm volatile("ld.global.f32 %0, [%1];" : "=f"(delta) : "l"(stat + kRows));
     };
     fetch(blockIdx.x);
+    int stage = kK - 1;                       // of the item's last keys
+    bool staged = false;                      // this warp's store may still read its place there
     for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
       const int h = head_of(i), b = batch_of(i), len = min(max(min(raw, p.a.Tk) - first_of(i), 0), p.q_keys);
       const int q0 = tile_of(i) * kRows;
@@ -764,6 +758,13 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         ptx::tmem_ld_wait();
 #pragma unroll
         for (int x = 0; x < 64; ++x) s[x] = __float_as_uint(exp2_approx(fmaf(__uint_as_float(s[x]), c, -lse)));
+        if (staged) {
+          if (lane == 0) {
+            ptx::tma_store_wait_read();
+            ptx::mbar_arrive(out_read + stage);
+          }
+          staged = false;
+        }
         here = ptx::mbar_wait(dp_full, dp_phase, abort_flag);
         dp_phase ^= 1u;
         if (!__all_sync(0xffffffffu, here)) { ok = false; break; }
@@ -794,6 +795,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       if (!ptx::mbar_wait_all(o_full, o_phase, abort_flag)) { ok = false; break; }
       o_phase ^= 1u;
       ptx::tc_fence_after_sync();
+      stage = (stage + ceil_div(len, kRows)) % kK;
       if (p.q_parts > 1) {                    // a part's sums, in fp32
         float* out = p.part_q + ((((long long)part_of(i) * p.a.B + b) * p.a.Tq + q0 + r) * p.a.H + h) * p.a.D;
 #pragma unroll
@@ -810,10 +812,33 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           }
         }
       } else {
-        store_row<DP / 2>(t_dq + half * (DP / 2) + lanes, dq, half * (DP / 2), p.a.D, p.a.scale, in, false);
+        // through the place of the item's last keys, which no product reads any more: 32 rows of DP / 2 columns per warp
+        unsigned char* stg = sk + stage * L::tile + warp * 32 * DP;
+        uint32_t w[DP / 4];
+#pragma unroll
+        for (int j = 0; j < DP / 64; ++j) {
+          uint32_t o[32];
+          ptx::tmem_ld_32x32(t_dq + half * (DP / 2) + j * 32 + lanes, o);
+          ptx::tmem_ld_wait();
+#pragma unroll
+          for (int x = 0; x < 16; ++x)
+            w[j * 16 + x] = pack2(__uint_as_float(o[2 * x]) * p.a.scale, __uint_as_float(o[2 * x + 1]) * p.a.scale);
+        }
+#pragma unroll
+        for (int x = 0; x < DP / 16; ++x)     // 128-byte rows are swizzled
+          *reinterpret_cast<uint4*>(stg + lane * DP + (DP == 128 ? x ^ (lane & 7) : x) * 16) = make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]);
+        ptx::fence_proxy_async();
+        __syncwarp();
+        const int token0 = q0 + (warp & 3) * 32;
+        if (lane == 0 && token0 < p.a.Tq && half * (DP / 2) < p.a.D) {
+          ptx::tma_store_4d(&map_dq, stg, half * (DP / 2), h, token0, b);
+          ptx::tma_store_commit();
+        }
+        staged = true;
       }
       ptx::tc_fence_before_sync();            // the next item's first dS says that dq has left tensor memory
     }
+    if (lane == 0) ptx::tma_store_wait_all();
   }
 
   if (!ok) {
@@ -879,7 +904,7 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   p.part_q = p.part_kv + split.kv_floats;
   attention_stats_kernel<<<(unsigned)((long long)a.B * p.q_tiles * ceil_div(kRows * a.H, kStatRows) + 1), 256, 0, st>>>(a, stats, prefix, p.q_tiles);
   count_launch();
-  CUtensorMap q, k, v, dout, dk, dv;
+  CUtensorMap q, k, v, dout, dk, dv, dq;
   // Without queries or without keys the kernels write zeros and look through no map; they get valid ones all the same.
   const AttentionArgs& s = a;
   const bool both_there = a.Tq && a.Tk;
@@ -891,7 +916,8 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   };
   if (!map(&q, a.q, a.H, a.Tq, a.q_stride, kRows, 64) || !map(&dout, a.dout, a.H, a.Tq, o_stride, kRows, 64) ||
       !map(&k, a.k, a.Hkv, a.Tk, a.k_stride, kRows, 64) || !map(&v, a.v, a.Hkv, a.Tk, a.v_stride, kRows, 64) ||
-      !map(&dk, a.dk, a.Hkv, a.Tk, a.k_stride, 32, 32) || !map(&dv, a.dv, a.Hkv, a.Tk, a.v_stride, 32, 32))
+      !map(&dk, a.dk, a.Hkv, a.Tk, a.k_stride, 32, 32) || !map(&dv, a.dv, a.Hkv, a.Tk, a.v_stride, 32, 32) ||
+      !map(&dq, a.dq, a.H, a.Tq, a.q_stride, 32, DP / 2))
     return GSHARD_ERR_CUDA;
   if (kv_items) {
     GS_CHECK(allow_shared(attention_dkv_kernel<DP>, KvLayout<DP>::bytes));
@@ -900,7 +926,7 @@ int backward(const AttentionArgs& a, float* stats, cudaStream_t st) {
   }
   if (p.items) {
     GS_CHECK(allow_shared(attention_dq_kernel<DP>, QLayout<DP>::bytes));
-    attention_dq_kernel<DP><<<std::min(p.items, device_sms()), kThreads, QLayout<DP>::bytes, st>>>(q, k, v, dout, p);
+    attention_dq_kernel<DP><<<std::min(p.items, device_sms()), kThreads, QLayout<DP>::bytes, st>>>(q, k, v, dout, dq, p);
     count_launch();
   }
   if (cudaGetLastError() != cudaSuccess) return GSHARD_ERR_CUDA;
