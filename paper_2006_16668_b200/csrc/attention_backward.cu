@@ -38,10 +38,39 @@ constexpr int kScoreRegs = 216, kOtherRegs = 72;      // 2 x 128 x 216 + 128 x 7
 // statistics of a query tile: lse log2(e) [128], delta [128], and the operand [128 x 16] of their terms
 constexpr int kTermBytes = kRows * 16 * 2, kStatFloats = 2 * kRows + kTermBytes / 4;
 
+
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// 2^x of two values without the special-function unit: x = n + f, |f| <= 1/2, 2^f by its Taylor polynomial of degree 5 (relative error
+// 2.4e-6, far below the rounding of P to bf16), n into the exponent.  From 2^-126 down it stays there.
+__device__ __forceinline__ float2 exp2_poly(f32x2 x2) {
+  const float2 x = unpair(x2);
+  float lo, hi;
+  asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(lo) : "f"(x.x));
+  asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(hi) : "f"(x.y));
+  const f32x2 v = pair(lo, hi), t = add2(v, both(12582912.f)), f = add2(v, mul2(add2(t, both(-12582912.f)), both(-1.f)));
+  f32x2 p = fma2(f, both(1.3333558e-3f), both(9.6181291e-3f));
+  p = fma2(p, f, both(5.5504109e-2f));
+  p = fma2(p, f, both(2.4022651e-1f));
+  p = fma2(p, f, both(6.9314718e-1f));
+  p = fma2(p, f, both(1.f));
+  const float2 n = unpair(t);
+  return unpair(mul2(p, pair(__int_as_float((__float_as_int(n.x) << 23) + 0x3f800000), __int_as_float((__float_as_int(n.y) << 23) + 0x3f800000))));
+}
+
+// 2^x of two values, pair j of a row.  The special-function unit makes 16 a cycle: with heads of up to 64 dimensions, where that takes
+// as long as the products, a quarter of the pairs goes to the other unit (backward, 16 x 1024 x 1024 tokens, 16 heads of 64 on 4:
+// 282 -> 267 us; with heads of 128 710 -> 720, and the forward
+// 377 -> 399 with heads of 64).
+template <int DP>
+__device__ __forceinline__ float2 exp2_pair(f32x2 x2, int j) {
+  if (DP == 64 && j % 4 == 3) return exp2_poly(x2);
+  const float2 x = unpair(x2);
+  return make_float2(exp2_approx(x.x), exp2_approx(x.y));
 }
 
 // v as three bf16 terms, 16 bits of a word each from `at` on
@@ -435,10 +464,9 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         uint32_t w[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-          const float2 x = unpair(mul2(pair(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1])), c2));
-          const float e0 = exp2_approx(x.x), e1 = exp2_approx(x.y);
-          pr[j] = pair(e0, e1);
-          w[j] = pack2(e0, e1);
+          const float2 e = exp2_pair<DP>(mul2(pair(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1])), c2), j);
+          pr[j] = pair(e.x, e.y);
+          w[j] = pack2(e.x, e.y);
         }
         ptx::tmem_st_32x32(my_s, w);
         ptx::tmem_st_wait();
@@ -757,7 +785,11 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         ptx::tmem_ld_32x32(my_s + 32, s + 32);
         ptx::tmem_ld_wait();
 #pragma unroll
-        for (int x = 0; x < 64; ++x) s[x] = __float_as_uint(exp2_approx(fmaf(__uint_as_float(s[x]), c, -lse)));
+        for (int x = 0; x < 32; ++x) {
+          const float2 e = exp2_pair<DP>(fma2(pair(__uint_as_float(s[2 * x]), __uint_as_float(s[2 * x + 1])), both(c), both(-lse)), x);
+          s[2 * x] = __float_as_uint(e.x);
+          s[2 * x + 1] = __float_as_uint(e.y);
+        }
         if (staged) {
           if (lane == 0) {
             ptx::tma_store_wait_read();
