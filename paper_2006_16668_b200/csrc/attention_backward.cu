@@ -1,12 +1,12 @@
 // Cross attention backward in bf16 on the tensor cores.  The scores are computed twice, once per block of keys (dk, dv)
 // and once per tile of queries (dq): seven products instead of five, and every gradient is accumulated in one place
-// of tensor memory in a fixed order, without atomics and without partial sums in HBM.
+// of tensor memory in a fixed order, without atomics.
 //
 // Row statistics.  A first kernel writes, per tile of 128 queries, lse log2(e) and delta = sum over d of dout o in fp32, and both once
 // more as three bf16 terms each, laid out as the B operand of one MMA step: with ones as A that step adds -lse / scale to the scores
 // and -delta to dP (24 bits, as exact as fp32), for which the threads would have to read shared memory that the tensor core keeps
 // busy (32 16-byte loads per thread and tile, 900 of 3800 cycles).  Rows behind the last query are padded with -1e30 for the former, so
-// that their P is 0 and nothing else needs a mask there.
+// that their P is 0 (2^-126 at most) beside rows of dO that are zero, and nothing else needs a mask there.
 //
 // dk, dv: persistent CTAs; an item is 128 keys of one key head and walks the query tiles of all heads of its group.
 //   S^T = K Q^T and dP^T = V dO^T into tensor memory (a thread holds 64 of a key's 128 queries), P^T over S^T, dv += P^T dO,
@@ -15,12 +15,14 @@
 //   item's first products are under way while an item's dk and dv leave tensor memory.
 //   Keys behind the source's length only make rows of their own; these are written as zero.
 // dq: a CTA owns 128 queries of one head and walks the source: S = Q K^T (two buffers), dP = dO V^T, dS over S,
-//   dq += dS K.  Keys behind the length: dS is zero, and rows of K that hold something else are zeroed in shared memory.
+//   dq += dS K.  Keys behind the length: dS is zero, and rows of K that hold something else are zeroed in shared memory.  dq leaves as
+//   bulk tensor stores through the place of the item's last keys; stored from registers row by row, 32 lines at once, it took the
+//   kernel 324 us instead of 281 at the size below.
 // Both cut their walk into parts where the items do not fill the GPU.
 //
-// Bound by the tensor pipe and the threads' turns: 16 heads of 128, 4 x 4096 x 4096 tokens 1483 us (927 TFLOP/s of the five products, 1298
-// of the seven); 32 x 1000 x 1111 tokens, 4 key heads, kernels of 711 us: dk and dv 385, dq 281, statistics 44 (6.0 TB/s).
-// (dq stored row by row from registers: 324, a store touching 32 lines at once.)
+// Bound by the tensor pipe and the threads' turns (a tile of dk and dv takes about 3000 cycles for 2200 of products, a block of dq 2200 for
+// 1540): 16 heads of 128, 32 x 1000 x 1111 tokens, 4 key heads, kernels of 711 us: dk and dv 385, dq 281, statistics 44 (6.0 TB/s);
+// 4 x 4096 x 4096 tokens 1001 us with sources of half to all of the keys.
 #include <algorithm>
 
 #include "attention.cuh"
@@ -37,7 +39,6 @@ constexpr int kThreads = 384;                 // 8 warps on the scores; TMA, MMA
 constexpr int kScoreRegs = 216, kOtherRegs = 72;      // 2 x 128 x 216 + 128 x 72 = 384 x 168
 // statistics of a query tile: lse log2(e) [128], delta [128], and the operand [128 x 16] of their terms
 constexpr int kTermBytes = kRows * 16 * 2, kStatFloats = 2 * kRows + kTermBytes / 4;
-
 
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
@@ -64,8 +65,7 @@ __device__ __forceinline__ float2 exp2_poly(f32x2 x2) {
 
 // 2^x of two values, pair j of a row.  The special-function unit makes 16 a cycle: with heads of up to 64 dimensions, where that takes
 // as long as the products, a quarter of the pairs goes to the other unit (backward, 16 x 1024 x 1024 tokens, 16 heads of 64 on 4:
-// 282 -> 267 us; with heads of 128 710 -> 720, and the forward
-// 377 -> 399 with heads of 64).
+// 282 -> 267 us; with heads of 128 710 -> 720, and the forward with heads of 64 377 -> 399).
 template <int DP>
 __device__ __forceinline__ float2 exp2_pair(f32x2 x2, int j) {
   if (DP == 64 && j % 4 == 3) return exp2_poly(x2);
