@@ -764,7 +764,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     int stage = kK - 1;                       // of the item's last keys
     bool staged = false;                      // this warp's store may still read its place there
     for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
-      const int h = head_of(i), b = batch_of(i), len = min(max(min(raw, p.a.Tk) - first_of(i), 0), p.q_keys);
+      const int h = head_of(i), b = batch_of(i), len = min(max(min(max(raw, 0), p.a.Tk) - first_of(i), 0), p.q_keys);
       const int q0 = tile_of(i) * kRows;
       const bool in = q0 + r < p.a.Tq;
       __nv_bfloat16* dq = static_cast<__nv_bfloat16*>(p.a.dq) + ((long long)b * p.a.Tq + q0 + r) * p.a.q_stride + (long long)h * p.a.D;
