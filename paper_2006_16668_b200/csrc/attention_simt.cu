@@ -326,8 +326,15 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) attention_simt_bac
         store_tile<DP>(out, dq_stride, a.Tq - q0, a.D, dq, whole && k0 + BT >= k_last ? scale : one, tx, ty);
       }
       landed<0>();
+      // keys behind the length have gradient zero, also where dO or delta is no number and P = 0 times it is none either
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (k0 + ty + 16 * x >= len) {
+#pragma unroll
+          for (int d = 0; d < DP / 64; ++d) dk[x][d][0] = dk[x][d][1] = dv[x][d][0] = dv[x][d][1] = 0;
+        }
     }
-    if (cut.q.parts == 1) {                             // keys behind the length have gradient zero
+    if (cut.q.parts == 1) {
       store_tile<DP>(static_cast<float*>(a.dk) + koff, a.k_stride, rows, a.D, dk, scale, tx, ty);
       store_tile<DP>(static_cast<float*>(a.dv) + voff, a.v_stride, rows, a.D, dv, one, tx, ty);
     } else if (k0 < k_last) {

@@ -1,0 +1,53 @@
+"""Cross attention at the edges of its values: numbers that are none among the keys in use.  Bounds in
+decoder_reference, or beside the test."""
+import math
+
+import pytest
+import torch
+
+import decoder_reference as ref
+import test_gpu_cross_attention as attn
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _finite_like(got, want, bound, what):
+    """Finite where the formula is, there within bound of it, and nowhere else."""
+    got, there = got.double(), torch.isfinite(want)
+    assert torch.equal(torch.isfinite(got), there), f"{what}: finite where the formula is not, or the other way round"
+    assert ((got - want).abs()[there] <= bound[there]).all(), what
+
+
+VALUE_SIZES = [(2, 1, 200, 4, 2, 64, [200, 70]), (2, 3, 150, 2, 2, 128, [150, 0]), (2, 150, 300, 4, 2, 128, [300, 130]), (2, 200, 260, 4, 2, 64, [260, 100]),
+               (1, 40, 3000, 2, 1, 64, [2900]), (1, 1300, 200, 4, 1, 128, [190])]
+
+
+@pytest.mark.parametrize("dtype", [F32])
+@pytest.mark.parametrize("size", VALUE_SIZES)
+@pytest.mark.parametrize("name,bad", [("q", math.nan), ("k", math.nan), ("v", math.nan), ("v", math.inf), ("v", -math.inf), ("dout", math.nan),
+                                      ("dout", math.inf)])
+def test_a_number_that_is_none(name, bad, size, dtype):
+    """One NaN or infinity: what the formula keeps free of it stays as it was - other heads and sources, other columns of o, and dv, which
+    depends neither on v nor, but for one column, on dO."""
+    t = attn.make(*size[:6], dtype, size[6])
+    scale = size[5] ** -0.5
+    lengths = attn.lengths_of(t)
+    clean = {n: x.clone() if torch.is_tensor(x) else x for n, x in t.items()}
+    t[name][0, min(t[name].shape[1] - 1, 77), 0, 3] = bad
+    o, lse = attn.forward(t)
+    o_clean, lse_clean = attn.forward(clean)
+    (want, _), (want_lse, _) = ref.attention(t["q"], t["k"], t["v"], lengths, scale)
+    (_, bound), (_, lse_bound) = ref.attention(clean["q"], clean["k"], clean["v"], lengths, scale)
+    _finite_like(o, want, bound, "o")
+    _finite_like(lse, want_lse, lse_bound, "lse")
+    grads = attn.backward(t, o, lse)
+    wants = ref.attention_grad(t["q"], t["k"], t["v"], lengths, scale, o, lse, t["dout"])
+    bounds = ref.attention_grad(clean["q"], clean["k"], clean["v"], lengths, scale, o_clean, lse_clean, clean["dout"])
+    for got, (want, _), (_, bound), what in zip(grads, wants, bounds, ("dq", "dk", "dv")):
+        if what != "dq":
+            behind = (torch.arange(size[2], device="cuda") >= lengths[:, None])[:, :, None, None].expand_as(want)
+            assert not got[behind].any()
+            want = want.masked_fill(behind, 0.0)
+        _finite_like(got, want, bound, what)
