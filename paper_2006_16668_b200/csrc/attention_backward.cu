@@ -3,9 +3,10 @@
 // of tensor memory in a fixed order, without atomics.
 //
 // Row statistics.  A first kernel writes, per tile of 128 queries, lse log2(e) and delta = sum over d of dout o in fp32, and both once
-// more as three bf16 terms each, laid out as the B operand of one MMA step: with ones as A that step adds -lse / scale to the scores
-// and -delta to dP (24 bits, as exact as fp32), for which the threads would have to read shared memory that the tensor core keeps
-// busy (32 16-byte loads per thread and tile, 900 of 3800 cycles).  Rows behind the last query are padded with -1e30 for the former, so
+// more as three bf16 terms each, laid out as the first half of the B operand of an MMA step (the second is zeros): with ones as A
+// these steps add -lse / scale to the scores and -delta to dP (24 bits, as exact as fp32), for which the threads would have to read
+// shared memory that the tensor core keeps busy (32 16-byte loads per thread and tile, 900 of 3800 cycles).  The two operands share
+// nothing but zeros, so that a delta that is no number stays out of P.  Rows behind the last query are padded with -1e30 for the former, so
 // that their P is 0 (2^-126 at most) beside rows of dO that are zero, and nothing else needs a mask there.
 //
 // dk, dv: persistent CTAs; an item is 128 keys of one key head and walks the query tiles of all heads of its group.
@@ -37,8 +38,8 @@ namespace {
 constexpr int kRows = 128;
 constexpr int kThreads = 384;                 // 8 warps on the scores; TMA, MMA and two idle warps
 constexpr int kScoreRegs = 216, kOtherRegs = 72;      // 2 x 128 x 216 + 128 x 72 = 384 x 168
-// statistics of a query tile: lse log2(e) [128], delta [128], and the operand [128 x 16] of their terms
-constexpr int kTermBytes = kRows * 16 * 2, kStatFloats = 2 * kRows + kTermBytes / 4;
+// statistics of a query tile: lse log2(e) [128], delta [128], and the operands [128 x 8] of lse's terms and of delta's
+constexpr int kTermBytes = kRows * 8 * 2, kStatFloats = 2 * kRows + 2 * kTermBytes / 4;
 
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
@@ -160,12 +161,12 @@ __global__ void __launch_bounds__(256) attention_stats_kernel(const AttentionArg
   const int row = t - t0;
   out[row] = t < a.Tq ? lse * kLog2e : INFINITY;
   out[kRows + row] = delta;
-  alignas(16) unsigned short terms[8] = {};
-  put_terms(t < a.Tq ? -lse / a.scale : -1e30f, terms);
-  put_terms(-delta, terms + 3);
-  uint4* step = reinterpret_cast<uint4*>(out + 2 * kRows) + row / 8 * 16 + row % 8;
-  step[0] = *reinterpret_cast<const uint4*>(terms);
-  step[8] = make_uint4(0, 0, 0, 0);
+  alignas(16) unsigned short terms[2][8] = {};
+  put_terms(t < a.Tq ? -lse / a.scale : -1e30f, terms[0]);
+  put_terms(-delta, terms[1]);
+  uint4* step = reinterpret_cast<uint4*>(out + 2 * kRows) + row;
+  step[0] = *reinterpret_cast<const uint4*>(terms[0]);
+  step[kRows] = *reinterpret_cast<const uint4*>(terms[1]);
 }
 
 struct BackwardParams {
@@ -236,9 +237,9 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 template <int DP> struct KvLayout {
   static constexpr int tile = kRows * DP * 2;
   static constexpr int stages = DP == 128 ? 2 : 4;
-  static constexpr int stage = 2 * tile + kTermBytes;          // Q, dO, the terms of their statistics
+  static constexpr int stage = 2 * tile + 2 * kTermBytes;      // Q, dO, the terms of lse and of delta
   static constexpr int ring_off = 2 * tile;
-  static constexpr int ones_off = ring_off + stages * stage;   // [2] A operands of the terms' step: ones for lse's, for delta's
+  static constexpr int ones_off = ring_off + stages * stage;   // A operand of the terms' steps: ones in columns 0 to 2, then zeros
   static constexpr int out_off = ones_off + 2 * kTermBytes;    // 32 rows x 64 bytes per warp
   static constexpr int bar_off = out_off + 8 * 32 * 64;
   static constexpr int bytes = bar_off + 256 + 1024;
@@ -326,13 +327,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     ptx::prefetch_tensormap(&map_k);
     ptx::prefetch_tensormap(&map_v);
   }
-  // ones in columns 0 to 2 (the first operand) or 3 to 5 (the second) of every row
-  for (int x = threadIdx.x; x < 2 * kRows; x += kThreads) {
-    const int row = x % kRows;
-    uint4* step = reinterpret_cast<uint4*>(ones + x / kRows * kTermBytes) + row / 8 * 16 + row % 8;
-    step[0] = x < kRows ? make_uint4(0x3f803f80u, 0x3f80u, 0, 0) : make_uint4(0, 0x3f800000u, 0x3f803f80u, 0);
-    step[8] = make_uint4(0, 0, 0, 0);
-  }
+  for (int x = threadIdx.x; x < 2 * kRows; x += kThreads)
+    reinterpret_cast<uint4*>(ones)[x] = x < kRows ? make_uint4(0x3f803f80u, 0x3f80u, 0, 0) : make_uint4(0, 0, 0, 0);
   ptx::fence_proxy_async();
   if (warp == 9) {
     ptx::tmem_alloc(tmem_slot, 512);
@@ -372,8 +368,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             ptx::mbar_arrive_expect_tx(full + stage, L::stage);
             load_rows<DP>(q, &map_q, full + stage, h, tile * kRows, t.b, again);
             load_rows<DP>(q + L::tile, &map_do, full + stage, h, tile * kRows, t.b, again);
-            ptx::bulk_load(q + 2 * L::tile, p.stats + (((long long)t.b * p.a.H + h) * p.q_tiles + tile) * kStatFloats + 2 * kRows, kTermBytes,
-                           full + stage);
+            ptx::bulk_load(q + 2 * L::tile, p.stats + (((long long)t.b * p.a.H + h) * p.q_tiles + tile) * kStatFloats + 2 * kRows,
+                           2 * kTermBytes, full + stage);
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
         }
@@ -382,7 +378,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       // ------------------------------ MMA issuer (one elected thread runs all of it) ------------------
       if (ptx::elect_one()) {
         constexpr uint32_t idesc = ptx::make_idesc_bf16(kRows, kRows, false, false);
-        const uint32_t one_l = ptx::plain_desc_low(ones), one_d = ptx::plain_desc_low(ones + kTermBytes);
+        const unsigned char* zeros = ones + kTermBytes;
+        const uint32_t one = ptx::plain_desc_low(ones, zeros);
         auto wait = [&](uint64_t* bar, uint32_t parity) {
           if (ok) ok = ptx::mbar_wait(bar, parity & 1u, abort_flag);
           return ok;
@@ -395,7 +392,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           if (!wait(full + ahead, ahead_phase)) return;
           const unsigned char* q = ring + ahead * L::stage;
           mma_rows<DP>(t_s, sk, q);
-          ptx::umma_bf16_plain(t_s, one_l, ptx::plain_desc_low(q + 2 * L::tile), idesc, 1u);
+          ptx::umma_bf16_plain(t_s, one, ptx::plain_desc_low(q + 2 * L::tile, zeros), idesc, 1u);
           ptx::umma_commit(s_full);
           if (last) ptx::umma_commit(k_empty);
         };
@@ -403,7 +400,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           if (fresh) { if (!wait(v_full, v_phase)) return; v_phase ^= 1u; }
           const unsigned char* q = ring + ahead * L::stage;
           mma_rows<DP>(t_dp, sv, q + L::tile);
-          ptx::umma_bf16_plain(t_dp, one_d, ptx::plain_desc_low(q + 2 * L::tile), idesc, 1u);
+          ptx::umma_bf16_plain(t_dp, one, ptx::plain_desc_low(q + 2 * L::tile + kTermBytes, zeros), idesc, 1u);
           ptx::umma_commit(dp_full);
           if (last) ptx::umma_commit(v_empty);
         };

@@ -252,10 +252,12 @@ __device__ __forceinline__ void umma_bf16_low(uint32_t d_tmem, uint32_t a_low, u
       : "r"(d_tmem), "r"(a_low), "r"(b_low), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
       : "memory");
 }
-// One K = 16 step of operands without swizzle, K-major: 8 x 8 elements (128 bytes) lie together, the two halves of K next to one
-// another, 8-row groups 256 bytes apart.
-constexpr uint32_t kPlainDescHigh = (256u >> 4) | (1u << 14);
-__device__ __forceinline__ uint32_t plain_desc_low(const void* p) { return (smem_u32(p) >> 4) | (128u >> 4) << 16; }
+// One K = 16 step of operands without swizzle, K-major: 8 x 8 elements (128 bytes) lie together, 8-row groups one behind the other; the
+// first 8 of K start at p, the second at `second`, which lies behind it.
+constexpr uint32_t kPlainDescHigh = (128u >> 4) | (1u << 14);
+__device__ __forceinline__ uint32_t plain_desc_low(const void* p, const void* second) {
+  return (smem_u32(p) >> 4) | (smem_u32(second) - smem_u32(p)) >> 4 << 16;
+}
 __device__ __forceinline__ void umma_bf16_plain(uint32_t d_tmem, uint32_t a_low, uint32_t b_low, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t"

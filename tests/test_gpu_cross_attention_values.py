@@ -24,7 +24,7 @@ VALUE_SIZES = [(2, 1, 200, 4, 2, 64, [200, 70]), (2, 3, 150, 2, 2, 128, [150, 0]
                (1, 40, 3000, 2, 1, 64, [2900]), (1, 1300, 200, 4, 1, 128, [190])]
 
 
-@pytest.mark.parametrize("dtype", [F32])
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("size", VALUE_SIZES)
 @pytest.mark.parametrize("name,bad", [("q", math.nan), ("k", math.nan), ("v", math.nan), ("v", math.inf), ("v", -math.inf), ("dout", math.nan),
                                       ("dout", math.inf)])
