@@ -458,7 +458,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
         for (int j = 0; j < kRows; j += 2) m[j >> 1 & 3] = max3(m[j >> 1 & 3], __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
         const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
         if (k0 == 0) {
-          top = fmaxf(most, -1e30f);
+          top = most;
         } else {
           const bool grown = (most - top) * c > kSlack;
           if (__any_sync(0xffffffffu, grown)) {
@@ -476,7 +476,7 @@ attention_umma_forward_kernel(const __grid_constant__ CUtensorMap map_q, const _
             }
           }
         }
-        const f32x2 c2 = both(c), m2 = both(-top * c);
+        const f32x2 c2 = both(c), m2 = both(top == -INFINITY ? 0.f : -top * c);      // no score so far: no weight either, as 2^-inf
         f32x2 sum2[2] = {0, 0};
 #pragma unroll
         for (int h = 0; h < 4; ++h) {

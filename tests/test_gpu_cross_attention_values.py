@@ -1,4 +1,4 @@
-"""Cross attention at the edges of its values: numbers that are none among the keys in use.  Bounds in
+"""Cross attention at the edges of its values: scores far below zero and numbers that are none among the keys in use.  Bounds in
 decoder_reference, or beside the test."""
 import math
 
@@ -7,10 +7,34 @@ import torch
 
 import decoder_reference as ref
 import test_gpu_cross_attention as attn
+from operator_reference import HALF, U32
 
 pytestmark = pytest.mark.gpu
 
 BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("first", [0, 5, 200])
+@pytest.mark.parametrize("factor", [2.0, math.inf])
+@pytest.mark.parametrize("Tq", [1, 140])
+def test_scores_far_below_zero(Tq, factor, first, dtype):
+    """q.k is -2^110 for the keys from `first` on and -2^111 or minus infinity for those before, the scale 2^-66: the former share a row's
+    weight evenly, the latter have none.  Scores and weights are exact, so only the sum of the values (one fp32 rounding per 16 of them on the tensor cores, one per
+    key elsewhere) and the output are rounded."""
+    Tk, length, scale = 300, 290, 2.0 ** -66
+    t = attn.make(1, Tq, Tk, 2, 1, 64, dtype, [length])
+    t["q"].zero_()
+    t["q"][..., 0] = 2.0 ** 60
+    t["k"][:, :length].zero_()
+    t["k"][:, :length, :, 0] = -2.0 ** 50
+    t["k"][:, :first, :, 0] *= factor
+    o, lse = attn.forward(t, scale=scale)
+    v = t["v"][0, first:length, 0].double()
+    want, size = v.mean(0), v.abs().mean(0)
+    bound = (Tk + 16) * U32 * size + HALF[dtype] * (want.abs() + Tk * U32 * size)
+    assert torch.isfinite(o).all() and ((o[0].double() - want).abs() <= bound).all()
+    assert ((lse.double() + 2.0 ** 44).abs() <= 2.0 ** 22).all()          # four half steps of 2^44
 
 
 def _finite_like(got, want, bound, what):
