@@ -629,8 +629,9 @@ int gshard_gated_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_
  * addresses agree modulo 16 moves fastest.  The arrays are read during the call only.
  *   gshard_grad_norm: *sumsq = sum over all tensors of g^2 (double, device memory).
  *   gshard_grad_clip: norm = sqrt(*sumsq); outs = grads * (norm > max_norm ? max_norm / norm : 1), the factor in fp32 (below
- *   its normal numbers as 2^-126 times another), products rounded to the tensor's type; *norm (float, device memory, may be NULL).  A norm that is infinite or NaN
- *   leaves the gradients as they are (outs: copies), so that a caller can look at *norm and skip the step.
+ *   its normal numbers as 2^-126 times another), products rounded to the tensor's type; *norm (float, device
+ *   memory, may be NULL).  A norm that is infinite or NaN as a float leaves the gradients as they are (outs: copies), so that a caller can look
+ *   at *norm and skip the step; finite gradients whose norm lies beyond float's range are among these.
  * Several ranks (the experts' gradients of the expert-parallel form): add the ranks' *sumsq between the two calls.
  * An output may be its own gradient, and shares memory with no other tensor of the list (a tensor that is listed twice
  * counts twice, and would be scaled twice).

@@ -163,8 +163,8 @@ template <int N>
 __global__ void __launch_bounds__(kThreads) grad_clip_kernel(const __grid_constant__ GradTable<N> t, const double* sumsq, float max_norm,
                                                              float* norm_out) {
   const double norm = sqrt(*sumsq);
-  // a norm that is no number says nothing about the factor: the gradients pass unchanged
-  const double value = norm > (double)max_norm && norm < (double)INFINITY ? (double)max_norm / norm : 1.0;
+  // a norm that the caller sees as infinite or NaN leaves the gradients unchanged: finite ones whose norm is beyond fp32 among them
+  const double value = norm > (double)max_norm && (float)norm < INFINITY ? (double)max_norm / norm : 1.0;
   const bool low = value < 0x1p-126;
   const float a = low ? 0x1p-126f : 1.f, b = low ? fminf((float)(value * 0x1p126), 0x1.fffffep-1f) : (float)value;      // b == 1: a copy
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;

@@ -1,4 +1,6 @@
-"""Clipping where the factor leaves the range of fp32; bounds as for the other tests of the norm."""
+"""Clipping where the factor or the norm leaves the range of fp32; bounds as for the other tests of the norm."""
+import math
+
 import pytest
 import torch
 
@@ -19,3 +21,16 @@ def test_factors_below_the_normal_numbers(max_norm, dtype):
         grads = [g.clone()] if outs[0] is g else [g]
         target = grads if outs[0] is g else outs
         norms.check(grads, [g], target, max_norm, *norms.clip(grads, max_norm, target))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_norm_beyond_fp32_leaves_the_gradients(dtype):
+    """Finite gradients whose norm, 1e39, fp32 has no number for: the norm is reported as infinite, and the gradients are left."""
+    g = [torch.full((100,), 1e38, device="cuda").to(dtype), torch.ones(7, device="cuda")]
+    before = [x.clone() for x in g]
+    outs = [torch.zeros_like(x) for x in g]
+    sumsq, norm = norms.clip(g, 1.0, outs)
+    assert math.isfinite(sumsq) and norm == math.inf
+    assert all(torch.equal(o, b) for o, b in zip(outs, before))
+    norms.clip(g, 1.0)
+    assert all(torch.equal(x, b) for x, b in zip(g, before))
