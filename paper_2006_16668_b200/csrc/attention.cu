@@ -50,7 +50,9 @@ int attention_validate(const gshard_attention_config* c) {
   const int64_t most = std::max(c->q_len, c->k_len);
   if (most > (1 << 30) || (most + 63) / 64 * c->heads >= (1ll << 31) || (most + 63) / 64 * c->heads * c->batch >= (1ll << 31))
     return GSHARD_ERR_UNSUPPORTED_SHAPE;
-  if (std::max(c->q_len * c->q_stride, c->k_len * std::max(c->k_stride, c->v_stride)) >= (1ll << 38)) return GSHARD_ERR_UNSUPPORTED_SHAPE;
+  // by division: the products may pass 63 bits
+  auto spans_too_much = [](int64_t tokens, int64_t stride) { return tokens > 0 && stride > ((1ll << 38) - 1) / tokens; };
+  if (spans_too_much(c->q_len, c->q_stride) || spans_too_much(c->k_len, std::max(c->k_stride, c->v_stride))) return GSHARD_ERR_UNSUPPORTED_SHAPE;
   return GSHARD_OK;
 }
 
