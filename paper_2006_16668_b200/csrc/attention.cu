@@ -76,7 +76,7 @@ AttentionPlan attention_plan(const gshard_attention_config& c, bool backward) {
   if (backward) {
     if (!bf16) p.delta = w.take(4 * (size_t)c.batch * c.heads * c.q_len);
     p.scratch = w.take(4 * (bf16 ? attention_umma_backward_floats(a) : attention_simt_backward_floats(a)));
-  } else if (!attention_is_few(bf16, a.B, a.Tq, a.Tk, a.H, a.Hkv)) {
+  } else if (!attention_is_few(bf16, a.B, a.Tq, a.Tk, a.H, a.Hkv, a.D)) {
     p.scratch = w.take(4 * (bf16 ? attention_umma_forward_floats(a) : attention_simt_forward_floats(a)));
   }
   p.total = w.off;
@@ -121,7 +121,7 @@ int gshard_cross_attention_forward(const gshard_attention_config* config, const 
   AttentionArgs a = attention_args(c, q, k, v, k_lengths);
   a.o = o; a.lse = lse; a.status = static_cast<int*>(workspace);
   const bool bf16 = c.dtype == GSHARD_BF16;
-  if (attention_is_few(bf16, a.B, a.Tq, a.Tk, a.H, a.Hkv)) return launch_attention_few(a, bf16, st);
+  if (attention_is_few(bf16, a.B, a.Tq, a.Tk, a.H, a.Hkv, a.D)) return launch_attention_few(a, bf16, st);
   GS_CHECK(clear_status(workspace, st));
   float* scratch = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + pl.scratch);
   return bf16 ? launch_attention_umma_forward(a, scratch, st) : launch_attention_simt_forward(a, scratch, st);

@@ -65,7 +65,7 @@ inline Parts parts_of(long long blocks, int units, int slots) {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // attention_few.cu: up to 8 rows (queries x heads) per key head, in one launch
-bool attention_is_few(bool bf16, int B, int Tq, int Tk, int H, int Hkv);
+bool attention_is_few(bool bf16, int B, int Tq, int Tk, int H, int Hkv, int D);
 int launch_attention_few(const AttentionArgs& a, bool bf16, cudaStream_t st);
 
 // The kernels by type: attention_simt.cu, fp32 on the CUDA cores; attention_umma.cu and attention_backward.cu, bf16 on the tensor

@@ -211,19 +211,38 @@ int launch_few(const AttentionArgs& a, int rows, int splits, cudaStream_t st) {
 
 }  // namespace
 
-// Whether this kernel takes the call.  fp32: up to 8 rows (the other kernel pads them to 64).  bf16: by what it measured beside the
-// tensor cores' (which take any number of rows alike, and parts of the source), us, key heads of 128 x keys:
+// Whether this kernel takes the call.  It never spreads a key head over more than a cluster, the other kernels cut the source into parts,
+// but take tiles of 64 (fp32) or 128 rows.
+// bf16: by what it measured beside the tensor cores' (which take any number of rows alike), us, key heads of 128 x keys:
 //   rows                 1           2           4           8
 //   16 x 512         5.8 / 14.9  6.7 / 15    9.3 / 15   20.8 / 15
 //   128 x 512        9.4 / 16.5 15.6 / 17   21.8 / 17   51.7 / 17
 //   1024 x 2048      157 / 203   173 / 205   329 / 205   702 / 205
 //   16 x 32768        87 / 68    104 / 68    176 / 68    389 / 68
-bool attention_is_few(bool bf16, int B, int Tq, int Tk, int H, int Hkv) {
+// fp32: by estimates in us, fitted to what both kernels measured at 1 to 64 key heads and 2048 to 65536 keys: here the time of a block's keys
+// (5 to 8 rows run in two rounds from 9 key heads on); there a least, all tiles' time, and that of the join of the parts.  Over those 80
+// sizes with 1, 2, 4 and 8 rows the choice took at most a tenth longer than the better of the two.
+// Key heads of 128 x keys, as queries of one head per key head:
+//   rows                 1           2           4           8
+//   1 x 4096        12.6 / 47   15.6 / 47   24.6 / 47   35.5 / 47
+//   1 x 32768        120 / 82    138 / 85    230 / 84    301 / 86
+//   4 x 8192          34 / 56     39 / 57     64 / 58     85 / 58
+//   4 x 32768        123 / 142   141 / 144   236 / 145   314 / 146
+//   16 x 8192         38 / 141    46 / 142    75 / 141   166 / 142
+//   64 x 16384       155 / 998   203 / 998   293 / 998   790 / 998
+bool attention_is_few(bool bf16, int B, int Tq, int Tk, int H, int Hkv, int D) {
   const long long rows = (long long)Tq * (H / Hkv), heads = (long long)B * Hkv;
   if (rows > 8) return false;
-  if (!bf16) return true;
-  if (rows <= 2) return Tk <= 16384 || heads >= 64;
-  return heads <= 32 && Tk * rows <= (rows <= 4 ? 8192 : 2048);
+  if (bf16) {
+    if (rows <= 2) return Tk <= 16384 || heads >= 64;
+    return heads <= 32 && Tk * rows <= (rows <= 4 ? 8192 : 2048);
+  }
+  if (heads > 16) return true;
+  const double width = D <= 64 ? 0.5 : 1, tiles = (double)B * H * Tk;
+  const double per_key = rows == 1 ? 0.0292 : rows == 2 ? 0.0335 : rows <= 4 ? 0.0565 : 0.0745;
+  const double here = width * per_key * Tk / kMaxSplits * (rows > 4 && heads > 8 ? 2.2 : 1);
+  const double there = std::max(D <= 64 ? 29. : 43., 20 + width * 0.93e-3 * tiles) + 1.2e-3 * Tk / ((double)B * H);
+  return here <= there;
 }
 
 int launch_attention_few(const AttentionArgs& a, bool bf16, cudaStream_t st) {
