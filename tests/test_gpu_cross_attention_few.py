@@ -23,3 +23,16 @@ def test_long_sources(size, dtype):
     attn.check_forward(t, o, lse)
     only, _ = attn.forward(t, lse=False)
     assert torch.equal(only, o)
+
+
+FEW = [(2, 8, 150, 2, 2, 128, None), (1, 2, 200, 4, 1, 120, None), (1, 1, 1030, 2, 2, 72, None), (3, 4, 250, 2, 1, 96, [250, 0, 5]),
+       (2, 7, 260, 1, 1, 104, [259, 130]), (1, 3, 2000, 1, 1, 80, [1999]), (1, 5, 300, 1, 1, 24, None), (4, 1, 700, 16, 2, 128, [700, 1, 0, 650])]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("size", FEW)
+def test_few_rows(size, dtype):
+    t = attn.make(*size[:6], dtype, size[6])
+    o, lse = attn.forward(t)
+    attn.check_forward(t, o, lse)
+    attn.check_backward(t, o, lse, attn.backward(t, o, lse))
