@@ -61,8 +61,6 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 4 : R == 2 ? 3 : R == 4 ? 2
       const int h = kh * (a.H / a.Hkv) + r / a.Tq, t = r % a.Tq;
       load_pack<T, W>(static_cast<const T*>(a.q) + ((long long)b * a.Tq + t) * a.q_stride + (long long)h * a.D + d, q[r]);
     }
-#pragma unroll
-    for (int j = 0; j < W; ++j) q[r][j] *= c;
   }
   const T* k = static_cast<const T*>(a.k) + (long long)b * a.Tk * a.k_stride + (long long)kh * a.D + d;
   const T* v = static_cast<const T*>(a.v) + (long long)b * a.Tk * a.v_stride + (long long)kh * a.D + d;
@@ -91,12 +89,12 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 4 : R == 2 ? 3 : R == 4 ? 2
         m = fmaxf(m, s[u]);
       }
       const float ref = m == -INFINITY ? 0.f : m;
-      const float shrink = exp2f(top[r] - ref);
+      const float shrink = exp2f((top[r] - ref) * c);
       top[r] = m;
       float t = 0.f;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        s[u] = exp2f(s[u] - ref);
+        s[u] = exp2f((s[u] - ref) * c);        // c here, not in q: that product may be beyond fp32
         t += s[u];
       }
       sum[r] = fmaf(sum[r], shrink, t);
@@ -116,7 +114,7 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 4 : R == 2 ? 3 : R == 4 ? 2
     for (int off = LPR; off < 32; off <<= 1) {
       const float other = __shfl_xor_sync(0xffffffffu, top[r], off);
       const float m = fmaxf(top[r], other), ref = m == -INFINITY ? 0.f : m;
-      const float mine = exp2f(top[r] - ref);
+      const float mine = exp2f((top[r] - ref) * c);
       top[r] = m;
       // both sides add the same two terms, in the same order
       sum[r] *= mine;
@@ -144,7 +142,7 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 4 : R == 2 ? 3 : R == 4 ? 2
     float o = 0.f, t = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const float f = exp2f(s_top[w][r] - ref);
+      const float f = exp2f((s_top[w][r] - ref) * c);
       o = fmaf(s_out[w][r][col], f, o);
       t = fmaf(s_sum[w][r], f, t);
     }
@@ -167,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 4 : R == 2 ? 3 : R == 4 ? 2
       const float ref = m == -INFINITY ? 0.f : m;
       o[0] = o[1] = t = 0.f;
       for (int w = 0; w < splits; ++w) {
-        const float f = exp2f(ld_cluster_f32(ptx::map_to_cta(at_top, w)) - ref);
+        const float f = exp2f((ld_cluster_f32(ptx::map_to_cta(at_top, w)) - ref) * c);
         o[0] = fmaf(ld_cluster_f32(ptx::map_to_cta(at_out, w)), f, o[0]);
         o[1] = fmaf(ld_cluster_f32(ptx::map_to_cta(at_out + 4, w)), f, o[1]);
         t = fmaf(ld_cluster_f32(ptx::map_to_cta(at_sum, w)), f, t);
@@ -177,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 4 : R == 2 ? 3 : R == 4 ? 2
     o[0] *= factor; o[1] *= factor;
     const int h = kh * (a.H / a.Hkv) + r / a.Tq, q_row = r % a.Tq;
     store_pack<T, 2>(static_cast<T*>(a.o) + (((long long)b * a.Tq + q_row) * a.H + h) * a.D + col, o);
-    if (a.lse && col == 0) a.lse[((long long)b * a.H + h) * a.Tq + q_row] = len ? m * kLn2 + logf(t) : -INFINITY;
+    if (a.lse && col == 0) a.lse[((long long)b * a.H + h) * a.Tq + q_row] = len ? m * a.scale + logf(t) : -INFINITY;
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
   if (splits > 1) ptx::cluster_sync_all();         // no block leaves while another may still read its parts

@@ -37,6 +37,23 @@ def test_scores_far_below_zero(Tq, factor, first, dtype):
     assert ((lse.double() + 2.0 ** 44).abs() <= 2.0 ** 22).all()          # four half steps of 2^44
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Tq", [1, 140])
+@pytest.mark.parametrize("up", [True, False])
+def test_scales_at_the_ends_of_their_range(up, Tq, dtype):
+    """Queries of 2^64 on keys of 2^-126 with a scale of 2^66, and the other way round: the scores are -16 to -19 (or 2^-4 of that) though a query
+    times the scale is beyond fp32 (or below its normal numbers)."""
+    t = attn.make(1, Tq, 300, 2, 1, 64, dtype, [290])
+    e = 1 if up else -1
+    t["q"].zero_()
+    t["q"][..., 0] = 2.0 ** (64 * e)
+    t["k"][:, :290].zero_()
+    t["k"][:, :290, 0, 0] = -(2.0 ** (-126 * e)) * (1 + torch.arange(290, device="cuda") % 4 / 16).to(dtype)
+    scale = 2.0 ** (66 * e)
+    o, lse = attn.forward(t, scale=scale)
+    attn.check_forward(t, o, lse, scale)
+
+
 def _finite_like(got, want, bound, what):
     """Finite where the formula is, there within bound of it, and nowhere else."""
     got, there = got.double(), torch.isfinite(want)
