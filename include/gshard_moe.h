@@ -576,9 +576,13 @@ int gshard_moe_route_backward(const gshard_route_config* config, const void* log
  *   o [batch, q_len, heads, head_dim] packed, dtype; lse [batch, heads, q_len] float, may be NULL.
  * bf16: tensor cores, fp32 accumulation and softmax, the weights p rounded to bf16 as an operand of p v.  fp32: all
  * arithmetic in fp32.
- * Limits: head_dim a multiple of 8 up to 128, strides multiples of 16 bytes, scale from 1e-20 to 1e20; batch,
- * q_len and k_len may be 0.  workspace: gshard_cross_attention_workspace_bytes() bytes, 256-byte aligned; its first word
- * is the status word (gshard_moe_last_device_status).  Calls that share a workspace must be ordered on one stream. */
+ * q.k, and in the backward dS k and dS^T q, are formed in fp32 before they are scaled.  A NaN or infinity in q or k
+ * within the length may make all rows that it scores NaN, and with them the gradients of its heads.
+ * Limits: head_dim a multiple of 8 up to 128, strides multiples of 16 bytes, tokens times stride below 2^38
+ * elements, scale from 1e-20 to 1e20; batch, q_len and k_len may be 0.  A call without outputs launches nothing and
+ * leaves the workspace alone.  workspace: gshard_cross_attention_workspace_bytes() bytes, 256-byte aligned; its first
+ * word is the status word (gshard_moe_last_device_status).  Calls that share a workspace must be ordered on one
+ * stream. */
 typedef struct {
   int32_t batch, q_len, k_len, heads, kv_heads, head_dim;
   int32_t dtype;         /* gshard_dtype */
@@ -628,10 +632,11 @@ int gshard_gated_linear_backward(int64_t n_rows, int32_t K, int32_t cols, int32_
  * 0) and gshard_dtype.  outs: where the clipped gradients go, grads itself for in place; a pair of tensors whose
  * addresses agree modulo 16 moves fastest.  The arrays are read during the call only.
  *   gshard_grad_norm: *sumsq = sum over all tensors of g^2 (double, device memory).
- *   gshard_grad_clip: norm = sqrt(*sumsq); outs = grads * (norm > max_norm ? max_norm / norm : 1), the factor in fp32 (below
- *   its normal numbers as 2^-126 times another), products rounded to the tensor's type; *norm (float, device
- *   memory, may be NULL).  A norm that is infinite or NaN as a float leaves the gradients as they are (outs: copies), so that a caller can look
- *   at *norm and skip the step; finite gradients whose norm lies beyond float's range are among these.
+ *   gshard_grad_clip: norm = sqrt(*sumsq); outs = grads * (norm > max_norm ? max_norm / norm : 1), the factor in fp32
+ *   (below its normal numbers as 2^-126 times another), products rounded to the tensor's type; *norm (float, device
+ *   memory, may be NULL).  A norm that is infinite or NaN as a float leaves the gradients as they are (outs: copies),
+ *   so that a caller can look at *norm and skip the step; finite gradients whose norm lies beyond float's range are
+ *   among these.
  * Several ranks (the experts' gradients of the expert-parallel form): add the ranks' *sumsq between the two calls.
  * An output may be its own gradient, and shares memory with no other tensor of the list (a tensor that is listed twice
  * counts twice, and would be scaled twice).

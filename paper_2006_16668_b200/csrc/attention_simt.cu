@@ -7,8 +7,8 @@
 // head dimension for the scores and along the columns for the outputs.
 // The backward takes five products per tile of scores: a block walks blocks of keys, and for each of them the queries; dk and dv stay in
 // registers, dq is added to where it lies, by one block in a fixed order, without atomics.  Blocks enough for the GPU come from parts
-// of the source and of the queries, with sums of their own that a second launch joins.  (8 x 517 x 333 tokens, 16 heads of 64: 417 us,
-// forward 169 us; separate kernels for dq and for dk and dv, with seven products, took 550 us.)
+// of the source and of the queries, with sums of their own that a second launch joins.  (8 x 517 x 333 tokens, 16 heads of 64: 417 to 452 us,
+// forward 160 to 169 us; separate kernels for dq and for dk and dv, with seven products, took 550 us.)
 // Bound by shared memory's operands (data pipe 78 % busy); 8 x 4 values per thread read a quarter less, but leave 8 warps per
 // multiprocessor: 2 % faster with heads of 64, a fifth slower with 128.
 #include "attention.cuh"
